@@ -329,6 +329,134 @@ int qablora_merge_noalloc(const qblora_qweight* qw, const qblora_adapter* adapte
 int qablora_lowbit_gemm(const qblora_qweight* qw, const void* X, int64_t tokens, void* Y,
                         int y_dtype, void* ws, size_t ws_bytes, void* stream);
 
+/* =====================================================================================================================
+ * Between the products of a served decoder layer.  The paper stops at the linear layer (Sec. 3.3, 4: the merged 4-bit
+ * model is what is deployed); the calls below are what such a model runs between its q / k / v products and its o
+ * product: rotary positions (forward and inverse, so that they also serve fine-tuning), a paged key / value cache with
+ * the block tables and slot maps that address it, and the attention of the new tokens over that cache.
+ *
+ * Notation.  B requests.  Request b holds ctx[b] tokens in the cache and adds new[b] of them in this step; the new
+ * tokens of all requests lie behind one another in the rows of q, k, v: those of request b are rows
+ * cu_new[b] .. cu_new[b + 1] - 1.  A cache page holds page_size tokens; token position p of request b is entry
+ * p % page_size of page block_table[b][p / page_size]; its "slot" is page * page_size + p % page_size.
+ * ===================================================================================================================== */
+
+/* A [tokens][heads][head_dim] tensor with its last dimension contiguous; strides in elements. */
+typedef struct {
+  void* data;                        /* DEVICE */
+  int64_t token_stride, head_stride; /* elements */
+  int32_t heads;
+  int32_t dtype;                     /* qblora_dtype */
+} qblora_heads;
+
+/* Paged key / value cache, bf16.  Element d of head h of entry e of page n is at
+ * n * page_stride + e * token_stride + h * head_stride + d of k and of v (strides in elements, so both
+ * [page][entry][head][d] and [page][head][entry][d] orders are plain strides).  n_pages * page_size < 2^31; the
+ * element offsets are formed in 64 bits. */
+typedef struct {
+  void* k;                                        /* DEVICE bf16 */
+  void* v;                                        /* DEVICE bf16, same strides */
+  int64_t page_stride, token_stride, head_stride; /* elements */
+  int32_t n_pages, page_size, kv_heads, head_dim;
+} qblora_kv_cache;
+
+typedef enum {
+  QBLORA_ROPE_HALF = 0, /* pair j is (x[j], x[j + rotary_dim / 2]) */
+  QBLORA_ROPE_PAIRS = 1 /* pair j is (x[2 j], x[2 j + 1]) */
+} qblora_rope_layout;
+
+/* Frequencies stretched for contexts longer than the trained one.  With f_j = base^(-2 j / rotary_dim) / (2 pi) turns
+ * per position:
+ *   NONE    f_j
+ *   LINEAR  f_j / factor                                  (positions squeezed into the trained range)
+ *   BASE    f_j with base * factor^(d / (d - 2)), d = rotary_dim (the slowest pair is squeezed by factor, the fastest kept)
+ *   BANDED  f_j (w + (1 - w) / factor), w = clamp((trained_len * f_j - slow) / (fast - slow), 0, 1): pairs that turn more
+ *           than `fast` times over the trained length are kept, those below `slow` turns squeezed, a ramp between. */
+typedef enum {
+  QBLORA_ROPE_SCALE_NONE = 0,
+  QBLORA_ROPE_SCALE_LINEAR = 1,
+  QBLORA_ROPE_SCALE_BASE = 2,
+  QBLORA_ROPE_SCALE_BANDED = 3
+} qblora_rope_scale;
+
+typedef struct {
+  int32_t head_dim, rotary_dim; /* the first rotary_dim (even, <= head_dim) elements of a head are rotated, the rest copied */
+  int32_t layout;               /* qblora_rope_layout */
+  float amplitude;              /* multiplies the rotated part (1 unless the context scaling asks for another) */
+  const uint64_t* turns;        /* DEVICE [rotary_dim / 2]: turns per position in units of 2^-64 (qblora_rope_table) */
+} qblora_rope_cfg;
+
+/* Fills turns[rotary_dim / 2] (HOST out) with the frequencies above in units of 2^-64 turns.  As whole numbers: the angle
+ * of position p is then p * turns modulo 2^64, one wrapping integer product, so the reduction to one turn is exact at
+ * every position.  factor > 0 (ignored for NONE); trained_len, slow < fast: BANDED only. */
+int qblora_rope_table(int32_t rotary_dim, double base, int32_t scale, double factor, int64_t trained_len, double slow,
+                      double fast, uint64_t* turns);
+
+/*
+ * Rotary positions: pair j of every head of row t is turned by the angle positions[t] * f_j,
+ *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin);
+ * inverse != 0 turns by the negative angle (same amplitude), which is the backward pass: dx from dy.
+ *   positions DEVICE int32 [tokens].  x -> y and (optional, NULL to leave out) x2 -> y2: q and k in one launch.  y may be x
+ *   itself (same data and strides); any other overlap is not allowed.  All inputs have one dtype, all outputs one dtype.
+ *   Computed in fp32, rounded once.  Any strides and alignment (16-byte ones are read in wide words).
+ */
+int qblora_rope(const qblora_rope_cfg* cfg, int inverse, const int32_t* positions, int64_t tokens, const qblora_heads* x,
+                const qblora_heads* y, const qblora_heads* x2, const qblora_heads* y2, void* stream);
+
+/*
+ * Serving form: rotates q into q_out (bf16), rotates k and writes it, and v as it is, into the cache entry slots[t]
+ * (rounded to bf16 once).  slots DEVICE int32 [tokens]: a slot below 0 or past the cache writes nothing (padding rows).
+ * The slots of one call are distinct.  q, k, v have one dtype; q_out may be q itself where that is bf16.
+ */
+int qblora_rope_append(const qblora_rope_cfg* cfg, const int32_t* positions, const int32_t* slots, int64_t tokens,
+                       const qblora_heads* q, const qblora_heads* k, const qblora_heads* v, const qblora_heads* q_out,
+                       const qblora_kv_cache* cache, void* stream);
+
+/*
+ * Block tables and slot maps of one serving step, from the requests' lengths.  All arrays DEVICE int32.
+ *   ctx_len [B], new_len [B]; release [B] or NULL: nonzero = the request has ended, its ceil(ctx / page_size) pages go back
+ *     onto the free stack (in request order, then table order) before any page is taken, and it adds nothing.
+ *   block_table [B][width]: the first ceil(ctx / page_size) entries of a row are read, entries of pages taken now written.
+ *   free_pages [capacity]: the stack of free pages, its lowest free_count[0] entries valid; pages given back are written
+ *     behind them.  free_count_out[0]: entries left afterwards (must not be free_count itself).
+ *   A request is valid if ctx >= 0, new >= 0 and ctx + new <= width * page_size.  Admission is first come, first
+ *   served: a valid request is admitted if the pages that it and all valid requests before it need are there, and their
+ *   new tokens fit into `tokens` rows.  (So once one does not fit, none behind it is admitted.)  The a-th page taken (in
+ *   request order, then position order) is free_pages[free + given back - 1 - a].
+ *   Out: cu_new [B + 1] and kv_len [B] (ctx + admitted new tokens; 0 for a released request; an invalid one has its
+ *   ctx clamped to 0 .. width * page_size); positions [tokens], slots [tokens]: row cu_new[b] + i is position ctx + i of
+ *   request b; rows behind the last new token: position 0, slot -1.  admitted [B]: 1 or 0.
+ * One launch; nothing is synchronised, so it can be captured in a graph.  The outputs depend on the inputs alone, and a
+ * second call on the same inputs changes nothing.  1 <= B <= 8192, else QBLORA_ERR_UNSUPPORTED.
+ */
+int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t* release, int32_t n_requests,
+                   int32_t* block_table, int32_t width, int32_t* free_pages, int32_t capacity, const int32_t* free_count,
+                   int32_t* free_count_out, int32_t page_size, int32_t tokens, int32_t* cu_new, int32_t* kv_len,
+                   int32_t* positions, int32_t* slots, int32_t* admitted, void* stream);
+
+/*
+ * Attention of the new tokens over the paged cache (their own keys and values are in the cache already):
+ *   out[t][h] = sum_j softmax_j(scale * q[t][h] . k_j) v_j,   k_j, v_j of key head h / (q heads / kv_heads),
+ * over the keys j that the row sees: with p = kv_len[b] - new + i the position of the i-th new row of request b,
+ *   j < kv_len[b];  causal != 0: j <= p;  window > 0: j > p - window.
+ * A row that sees no key gives zeros and lse = -infinity.  Keys that a row does not see do not reach its result, whatever
+ * they hold (NaN and infinities too).  lse [tokens][q heads] fp32 (NULL to leave out) = log sum_j exp(scale * q . k_j).
+ * Rows that belong to no request are not written.
+ *   block_table [B][width], cu_new [B + 1], kv_len [B]: DEVICE int32, as written by qblora_kv_plan.
+ *   q, out: bf16.  head_dim % 8 == 0, at most 256; q heads a multiple of kv_heads; strides multiples of 8 elements and
+ *   16-byte aligned data for q, out and the cache.  scale: usually 1 / sqrt(head_dim).
+ *   Scores, softmax statistics and sums are fp32; the weights exp(s - max) are rounded to bf16 for their product with v.
+ * Lengths are read on the device only, so one captured graph serves every step of the same shape.  Lengths and table
+ * entries out of range are clamped and never lead outside the cache; a page number out of range sets the status word to
+ * QBLORA_ERR_INVALID_ARG (that request's results are then undefined).
+ * ws: qblora_attention_workspace_bytes(...) bytes.
+ */
+size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens);
+int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_table, int32_t width, const int32_t* cu_new,
+                           const int32_t* kv_len, int32_t n_requests, const qblora_heads* q, int64_t tokens, float scale,
+                           int causal, int32_t window, const qblora_heads* out, float* lse, void* ws, size_t ws_bytes,
+                           void* stream);
+
 #ifdef __cplusplus
 }
 #endif

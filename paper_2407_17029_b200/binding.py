@@ -26,12 +26,17 @@ F32, BF16 = 0, 1
 OP_QUANTIZE, OP_LINEAR_FWD, OP_LINEAR_BWD, OP_MERGE, OP_LOWBIT_GEMM, OP_MERGE_DENSE = range(6)
 # qblora_scale_op: the parameter-free operator pair around the adapter (Sec. 3.2; Sec. 4 scale-operator ablation)
 SCALE_AVGPOOL_REPEAT, SCALE_TRUNCATE_ZEROPAD, SCALE_SAMPLE_ZEROFILL = range(3)
+# qblora_rope_layout, qblora_rope_scale
+ROPE_HALF, ROPE_PAIRS = range(2)
+ROPE_SCALE_NONE, ROPE_SCALE_LINEAR, ROPE_SCALE_BASE, ROPE_SCALE_BANDED = range(4)
 
 EXPORTS = ["qblora_default_code_table", "qblora_workspace_bytes", "qblora_status_string",
            "qblora_device_status", "qblora_quantize_blockwise", "qblora_linear_fwd",
            "qblora_linear_bwd", "qablora_merge", "qablora_lowbit_gemm", "qblora_kernel_launches",
            "qblora_set_timing_events", "qablora_merge_noalloc", "qblora_merge_dense",
-           "qblora_quantize_minmax_nbit", "qblora_debug_set_wait_limit", "qblora_debug_drop_load", "qblora_debug_hold_producer", "qblora_dense_gemm", "qblora_pack_codes", "qblora_unpack_codes"]
+           "qblora_quantize_minmax_nbit", "qblora_debug_set_wait_limit", "qblora_debug_drop_load", "qblora_debug_hold_producer", "qblora_dense_gemm", "qblora_pack_codes", "qblora_unpack_codes",
+           "qblora_rope_table", "qblora_rope", "qblora_rope_append", "qblora_kv_plan", "qblora_attention_workspace_bytes",
+           "qblora_paged_attention"]
 
 
 class _CQWeight(ctypes.Structure):
@@ -46,6 +51,22 @@ class _CAdapter(ctypes.Structure):
     _fields_ = [("lambda_in", ctypes.c_int32), ("lambda_out", ctypes.c_int32),
                 ("rank", ctypes.c_int32), ("scaling", ctypes.c_float),
                 ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale_op", ctypes.c_int32)]
+
+
+class _CHeads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class _CKVCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _CRope(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("amplitude", ctypes.c_float), ("turns", ctypes.c_void_p)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -91,6 +112,15 @@ _lib.qblora_unpack_codes.argtypes = [ctypes.c_void_p, ctypes.c_int32, ctypes.c_i
 _lib.qblora_debug_set_wait_limit.argtypes = [ctypes.c_int64]
 _lib.qblora_debug_drop_load.argtypes = [ctypes.c_int32]
 _lib.qblora_debug_hold_producer.argtypes = [ctypes.c_int64]
+_vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+_lib.qblora_rope_table.argtypes = [_i32, ctypes.c_double, _i32, ctypes.c_double, _i64, ctypes.c_double, ctypes.c_double, _vp]
+_lib.qblora_rope.argtypes = [_vp, ctypes.c_int, _vp, _i64, _vp, _vp, _vp, _vp, _vp]
+_lib.qblora_rope_append.argtypes = [_vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.qblora_kv_plan.argtypes = [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.qblora_attention_workspace_bytes.restype = _sz
+_lib.qblora_attention_workspace_bytes.argtypes = [_vp, _i32, _i64]
+_lib.qblora_paged_attention.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i64, ctypes.c_float, ctypes.c_int, _i32, _vp,
+                                        _vp, _vp, _sz, _vp]
 
 
 def kernel_launches() -> int:
@@ -404,3 +434,190 @@ def unpack_codes(qw: QWeight, stream=None) -> QWeight:
     st = _lib.qblora_unpack_codes(qw.codes.data_ptr(), qw.d_out, qw.d_in, int(qw.code_bits), codes.data_ptr(), _stream_ptr(stream))
     _check(st, "qblora_unpack_codes")
     return QWeight(qw.d_out, qw.d_in, qw.block_in, qw.block_out, qw.qfmt, qw.code, codes, qw.alpha, qw.beta, 4)
+
+
+# ------------------------------------------------------------------------------ between the products of a served layer
+@dataclass
+class Rope:
+    """Rotary positions of a model: the first rotary_dim elements of every head are rotated, `table` from rope_table."""
+    head_dim: int
+    rotary_dim: int
+    layout: int
+    table: torch.Tensor              # int64 [rotary_dim / 2], device: turns per position in units of 2^-64
+    amplitude: float = 1.0
+
+    def c_struct(self) -> _CRope:
+        if self.table.dtype != torch.int64 or not self.table.is_contiguous() or 2 * self.table.numel() != self.rotary_dim:
+            raise ValueError("table: contiguous int64 [rotary_dim / 2], see rope_table")
+        c = _CRope()
+        c.head_dim, c.rotary_dim, c.layout, c.amplitude = self.head_dim, self.rotary_dim, self.layout, self.amplitude
+        c.turns = self.table.data_ptr()
+        return c
+
+
+@dataclass
+class KVCache:
+    """Paged cache: k and v bf16 [n_pages][page_size][kv_heads][head_dim] (any order in memory: permuted views are fine
+    as long as k and v agree and head_dim is contiguous)."""
+    k: torch.Tensor
+    v: torch.Tensor
+
+    @staticmethod
+    def empty(n_pages: int, page_size: int, kv_heads: int, head_dim: int, device="cuda") -> "KVCache":
+        shape = (n_pages, page_size, kv_heads, head_dim)
+        return KVCache(torch.empty(shape, dtype=torch.bfloat16, device=device),
+                       torch.empty(shape, dtype=torch.bfloat16, device=device))
+
+    def c_struct(self) -> _CKVCache:
+        k, v = self.k, self.v
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k, v: equal shapes and strides [n_pages][page_size][kv_heads][head_dim], head_dim contiguous")
+        if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+            raise ValueError("k, v: bf16")
+        c = _CKVCache()
+        c.k, c.v = k.data_ptr(), v.data_ptr()
+        c.page_stride, c.token_stride, c.head_stride = k.stride(0), k.stride(1), k.stride(2)
+        c.n_pages, c.page_size, c.kv_heads, c.head_dim = k.shape
+        return c
+
+
+@dataclass
+class KVPlan:
+    """Results of kv_plan (int32, device); see qblora_kv_plan."""
+    cu_new: torch.Tensor             # [B + 1] first row of each request
+    kv_len: torch.Tensor             # [B] cached tokens after the step
+    positions: torch.Tensor          # [tokens]
+    slots: torch.Tensor              # [tokens], -1 in unused rows
+    admitted: torch.Tensor           # [B]
+    free_count: torch.Tensor         # [1] pages left
+
+
+def _heads(t: torch.Tensor) -> _CHeads:
+    assert t.is_cuda and t.dim() == 3
+    if t.stride(2) != 1 and t.shape[2] > 1:
+        raise ValueError("[tokens][heads][head_dim]: head_dim contiguous")
+    c = _CHeads()
+    c.data, c.token_stride, c.head_stride, c.heads, c.dtype = t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _dt(t.dtype)
+    return c
+
+
+def _ints(t: torch.Tensor, n: int, name: str) -> int:
+    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: contiguous int32 device tensor of at least {n} entries")
+    return t.data_ptr()
+
+
+def rope_table(rotary_dim: int, base: float = 10000.0, scale: int = ROPE_SCALE_NONE, factor: float = 1.0,
+               trained_len: int = 0, slow: float = 1.0, fast: float = 32.0, device="cuda") -> torch.Tensor:
+    """qblora_rope_table: the rotation table of a model (int64 [rotary_dim / 2] on `device`)."""
+    if rotary_dim < 2 or rotary_dim % 2:
+        raise QbloraError(ERR_INVALID_ARG, "qblora_rope_table")
+    buf = (ctypes.c_int64 * (rotary_dim // 2))()
+    _check(_lib.qblora_rope_table(rotary_dim, base, scale, factor, trained_len, slow, fast, buf), "qblora_rope_table")
+    return torch.tensor(list(buf), dtype=torch.int64, device=device)
+
+
+def rope(cfg: Rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, inverse: bool = False,
+         out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None, stream=None):
+    """qblora_rope on q (and k) [tokens][heads][head_dim]; inverse=True is the backward pass (gradients in, gradients
+    out).  out_q / out_k may be q / k themselves.  Returns (q', k')."""
+    T = q.shape[0]
+    if q.shape[2] != cfg.head_dim or (k is not None and (k.shape[0] != T or k.shape[2] != cfg.head_dim)):
+        raise ValueError("q, k: [tokens][heads][head_dim]")
+    out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
+    if k is not None and out_k is None:
+        out_k = torch.empty(k.shape, dtype=out_q.dtype, device=k.device)
+    if out_q.shape != q.shape or (k is not None and out_k.shape != k.shape):
+        raise ValueError("outputs have the shapes of the inputs")
+    if T == 0:
+        return out_q, out_k
+    c, x, y = cfg.c_struct(), _heads(q), _heads(out_q)
+    x2, y2 = (_heads(k), _heads(out_k)) if k is not None else (None, None)
+    st = _lib.qblora_rope(ctypes.byref(c), int(bool(inverse)), _ints(positions, T, "positions"), T, ctypes.byref(x),
+                          ctypes.byref(y), _ref(x2), _ref(y2), _stream_ptr(stream))
+    _check(st, "qblora_rope")
+    return out_q, out_k
+
+
+def rope_append(cfg: Rope, positions: torch.Tensor, slots: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                cache: KVCache, out_q: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """qblora_rope_append: rotated q (bf16); rotated k and v go into the cache at `slots`."""
+    T = q.shape[0]
+    if k.shape[0] != T or v.shape != k.shape or q.shape[2] != cfg.head_dim or k.shape[2] != cfg.head_dim:
+        raise ValueError("q, k, v: [tokens][heads][head_dim]")
+    out_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out_q is None else out_q
+    if out_q.shape != q.shape:
+        raise ValueError("out_q has the shape of q")
+    if T == 0:
+        return out_q
+    c, cc = cfg.c_struct(), cache.c_struct()
+    cq, ck, cv, co = _heads(q), _heads(k), _heads(v), _heads(out_q)
+    st = _lib.qblora_rope_append(ctypes.byref(c), _ints(positions, T, "positions"), _ints(slots, T, "slots"), T,
+                                 ctypes.byref(cq), ctypes.byref(ck), ctypes.byref(cv), ctypes.byref(co), ctypes.byref(cc),
+                                 _stream_ptr(stream))
+    _check(st, "qblora_rope_append")
+    return out_q
+
+
+def kv_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor,
+            free_count: torch.Tensor, page_size: int, tokens: int, release: Optional[torch.Tensor] = None,
+            outs: Optional[Tuple] = None, stream=None) -> KVPlan:
+    """qblora_kv_plan: takes pages for the new tokens of every request (block_table and free_pages are updated in place)
+    and returns the step's row offsets, lengths, positions and slots.  `tokens`: rows of the step's buffers.
+    `outs`: preallocated (cu_new, kv_len, positions, slots, admitted, free_count)."""
+    if block_table.dim() != 2:
+        raise ValueError("block_table: [requests][width]")
+    B, width = block_table.shape
+    if outs is None:
+        outs = tuple(torch.empty(n, dtype=torch.int32, device=block_table.device) for n in (B + 1, B, tokens, tokens, B, 1))
+    plan = KVPlan(*outs)
+    st = _lib.qblora_kv_plan(_ints(ctx_len, B, "ctx_len"), _ints(new_len, B, "new_len"),
+                             _ints(release, B, "release") if release is not None else None, B,
+                             _ints(block_table, 1, "block_table"), width, _ints(free_pages, 1, "free_pages"),
+                             free_pages.numel(), _ints(free_count, 1, "free_count"), _ints(plan.free_count, 1, "free_count out"),
+                             int(page_size), int(tokens), _ints(plan.cu_new, B + 1, "cu_new"), _ints(plan.kv_len, B, "kv_len"),
+                             _ints(plan.positions, tokens, "positions"), _ints(plan.slots, tokens, "slots"),
+                             _ints(plan.admitted, B, "admitted"), _stream_ptr(stream))
+    _check(st, "qblora_kv_plan")
+    return plan
+
+
+def attention_workspace_bytes(cache: KVCache, q_heads: int, tokens: int) -> int:
+    c = cache.c_struct()
+    return int(_lib.qblora_attention_workspace_bytes(ctypes.byref(c), q_heads, tokens))
+
+
+def alloc_attention_workspace(cache: KVCache, q: torch.Tensor) -> torch.Tensor:
+    """Workspace for paged_attention calls with this cache and up to q.shape[0] tokens."""
+    n = max(attention_workspace_bytes(cache, q.shape[1], max(q.shape[0], 1)), 256)
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor,
+                    scale: Optional[float] = None, causal: bool = True, window: int = 0, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, need_lse: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
+    """qblora_paged_attention: q bf16 [tokens][q_heads][head_dim] -> (out, lse); lse (fp32 [tokens][q_heads]) is None
+    unless need_lse or a tensor for it is given.  scale defaults to head_dim^-1/2; window = 0: no window."""
+    T, H, D = q.shape
+    if D != cache.k.shape[3]:
+        raise ValueError("q: [tokens][q_heads][head_dim of the cache]")
+    if block_table.dim() != 2:
+        raise ValueError("block_table: [requests][width]")
+    B, width = block_table.shape
+    out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out is None else out
+    if lse is None and need_lse:
+        lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
+    if out.shape != q.shape or (lse is not None and (tuple(lse.shape) != (T, H) or lse.dtype != torch.float32 or not lse.is_contiguous())):
+        raise ValueError("out: shape of q; lse: contiguous fp32 [tokens][q_heads]")
+    if T == 0:
+        return out, lse
+    if ws is None:
+        ws = alloc_attention_workspace(cache, q)
+    cc, cq, co = cache.c_struct(), _heads(q), _heads(out)
+    st = _lib.qblora_paged_attention(ctypes.byref(cc), _ints(block_table, 1, "block_table"), width, _ints(cu_new, B + 1, "cu_new"),
+                                     _ints(kv_len, B, "kv_len"), B, ctypes.byref(cq), T,
+                                     float(D) ** -0.5 if scale is None else float(scale), int(bool(causal)), int(window),
+                                     ctypes.byref(co), lse.data_ptr() if lse is not None else None, ws.data_ptr(), ws.numel(),
+                                     _stream_ptr(stream))
+    _check(st, "qblora_paged_attention")
+    return out, lse

@@ -1,0 +1,230 @@
+// Rotary positions (qblora_rope) and their serving form that writes the paged cache (qblora_rope_append).
+//
+// Pair j of a head at position p is turned by p * f_j turns.  The table holds f_j in units of 2^-64 turns, so the angle
+// modulo one turn is the low 64 bits of one integer product; its top 32 bits, read as a signed number, are the angle in
+// units of 2^-32 turns, exact at every position (a product in fp32 is off by a hundredth of a radian at position 10^5).
+//
+// What bounds it: HBM, every element read once and written once.  So a thread computes the sines of eight pairs once and
+// applies them to the same chunk of several heads, loading 16-byte words.
+#include "serving.cuh"
+
+namespace qb {
+namespace {
+
+__device__ __forceinline__ void rope_angle(const RopeView& r, int pos, int pair, float& co, float& si) {
+  const uint64_t phase = (uint64_t)(int64_t)pos * __ldg(r.turns + pair);
+  const float half_turns = (float)(int32_t)(phase >> 32) * (1.0f / 2147483648.0f);   // angle / pi, in [-1, 1)
+  sincospif(half_turns, &si, &co);
+  co *= r.amp;
+  si *= r.amp * r.sign;
+}
+
+// offset of head 0 of slot's entry, or -1
+__device__ __forceinline__ int64_t cache_entry(const CacheView& c, int slot) {
+  if (slot < 0) return -1;
+  const int page = slot / c.page_size;
+  if (page >= c.n_pages) return -1;
+  return (int64_t)page * c.ps + (int64_t)(slot - page * c.page_size) * c.ts;
+}
+
+__device__ __forceinline__ float ld1(const float* p) { return *p; }
+__device__ __forceinline__ float ld1(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void st1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void st1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
+
+// Eight consecutive values.
+__device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+}
+__device__ __forceinline__ void ld8(const __nv_bfloat16* p, float (&x)[8]) {
+  const uint4 v = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    x[2 * i] = __uint_as_float(w[i] << 16);
+    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void st8(__nv_bfloat16* p, const float (&x)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+    w[i] = *reinterpret_cast<const uint32_t*>(&v);
+  }
+  *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Where head h of the concatenated list (q heads, k heads, v heads) of row t comes from and goes to.
+template <typename TI, typename TO>
+struct Place {
+  const TI* src;
+  TO* dst;        // nullptr: nothing is written
+  bool rotate;
+};
+template <typename TI, typename TO>
+__device__ __forceinline__ Place<TI, TO> place(const RopeCall& c, int64_t t, int64_t entry, int h) {
+  Place<TI, TO> r;
+  r.rotate = true;
+  if (h < c.q.heads) {
+    r.src = static_cast<const TI*>(c.q.data) + t * c.q.ts + (int64_t)h * c.q.hs;
+    r.dst = static_cast<TO*>(c.q_out.data) + t * c.q_out.ts + (int64_t)h * c.q_out.hs;
+    return r;
+  }
+  h -= c.q.heads;
+  if (h < c.k.heads) {
+    r.src = static_cast<const TI*>(c.k.data) + t * c.k.ts + (int64_t)h * c.k.hs;
+    if (c.slots) r.dst = entry < 0 ? nullptr : reinterpret_cast<TO*>(c.cache.k) + entry + (int64_t)h * c.cache.hs;
+    else r.dst = static_cast<TO*>(c.k_out.data) + t * c.k_out.ts + (int64_t)h * c.k_out.hs;
+    return r;
+  }
+  h -= c.k.heads;
+  r.rotate = false;
+  r.src = static_cast<const TI*>(c.v.data) + t * c.v.ts + (int64_t)h * c.v.hs;
+  r.dst = entry < 0 ? nullptr : reinterpret_cast<TO*>(c.cache.v) + entry + (int64_t)h * c.cache.hs;
+  return r;
+}
+
+// Wide form.  A thread owns one chunk of a row: 16 elements that hold eight whole pairs (or 16, or the last 8, elements
+// behind the rotated part), for `hpt` consecutive heads.
+template <typename TI, typename TO, int LAYOUT>
+__global__ void __launch_bounds__(256) rope_wide_kernel(const __grid_constant__ RopeCall c, int chunks, int hpt, int groups) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int chunk = (int)(id % chunks);
+  const int64_t rest = id / chunks;
+  const int group = (int)(rest % groups);
+  const int64_t t = rest / groups;
+  if (t >= c.T) return;
+  const int n_heads = c.q.heads + c.k.heads + c.v.heads;
+  const int h0 = group * hpt, h1 = min(h0 + hpt, n_heads);
+  const int rot_chunks = c.cfg.rot >> 4;
+  const bool rot = chunk < rot_chunks;
+  int e0, e1;      // first elements of the chunk's two halves of eight
+  float co[8], si[8];
+  if (rot) {
+    if (LAYOUT == QBLORA_ROPE_HALF) { e0 = chunk * 8; e1 = e0 + (c.cfg.rot >> 1); }
+    else { e0 = chunk * 16; e1 = e0 + 8; }
+    if (h0 < c.q.heads + c.k.heads) {
+      const int pos = __ldg(c.positions + t);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) rope_angle(c.cfg, pos, chunk * 8 + i, co[i], si[i]);
+    }
+  } else {
+    e0 = c.cfg.rot + (chunk - rot_chunks) * 16;
+    e1 = e0 + 8 < c.cfg.D ? e0 + 8 : -1;
+  }
+  const int64_t entry = c.slots ? cache_entry(c.cache, __ldg(c.slots + t)) : -1;
+#pragma unroll 4
+  for (int h = h0; h < h1; ++h) {
+    const Place<TI, TO> w = place<TI, TO>(c, t, entry, h);
+    float a[8], b[8];
+    ld8(w.src + e0, a);
+    if (e1 >= 0) ld8(w.src + e1, b);
+    if (rot && w.rotate) {
+      if (LAYOUT == QBLORA_ROPE_HALF) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float x = a[i], y = b[i];
+          a[i] = x * co[i] - y * si[i];
+          b[i] = y * co[i] + x * si[i];
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float x = a[2 * i], y = a[2 * i + 1];
+          a[2 * i] = x * co[i] - y * si[i];
+          a[2 * i + 1] = y * co[i] + x * si[i];
+          x = b[2 * i]; y = b[2 * i + 1];
+          b[2 * i] = x * co[4 + i] - y * si[4 + i];
+          b[2 * i + 1] = y * co[4 + i] + x * si[4 + i];
+        }
+      }
+    }
+    if (w.dst) {
+      st8(w.dst + e0, a);
+      if (e1 >= 0) st8(w.dst + e1, b);
+    }
+  }
+}
+
+// Any strides, alignment and even rotary size: one pair (or one element behind the rotated part) of one head per thread.
+template <typename TI, typename TO>
+__global__ void __launch_bounds__(256) rope_any_kernel(const __grid_constant__ RopeCall c) {
+  const int pairs = c.cfg.rot >> 1, items = pairs + (c.cfg.D - c.cfg.rot);
+  const int n_heads = c.q.heads + c.k.heads + c.v.heads;
+  const int64_t total = c.T * n_heads * items;
+  for (int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x; id < total; id += (int64_t)gridDim.x * 256) {
+    const int item = (int)(id % items);
+    const int64_t rest = id / items;
+    const int h = (int)(rest % n_heads);
+    const int64_t t = rest / n_heads;
+    const int64_t entry = c.slots ? cache_entry(c.cache, __ldg(c.slots + t)) : -1;
+    const Place<TI, TO> w = place<TI, TO>(c, t, entry, h);
+    if (!w.dst) continue;
+    if (item >= pairs) {
+      const int e = c.cfg.rot + item - pairs;
+      st1(w.dst + e, ld1(w.src + e));
+      continue;
+    }
+    const int e0 = c.cfg.layout == QBLORA_ROPE_HALF ? item : 2 * item;
+    const int e1 = c.cfg.layout == QBLORA_ROPE_HALF ? item + pairs : 2 * item + 1;
+    float x = ld1(w.src + e0), y = ld1(w.src + e1);
+    if (w.rotate) {
+      float co, si;
+      rope_angle(c.cfg, __ldg(c.positions + t), item, co, si);
+      const float u = x * co - y * si;
+      y = y * co + x * si;
+      x = u;
+    }
+    st1(w.dst + e0, x);
+    st1(w.dst + e1, y);
+  }
+}
+
+bool heads_wide(const HeadsView& v) {
+  if (v.heads == 0) return true;
+  const int per16 = v.dtype == QBLORA_BF16 ? 8 : 4;
+  return aligned16(v.data) && v.ts % per16 == 0 && v.hs % per16 == 0;
+}
+
+template <typename TI, typename TO>
+int launch_typed(const RopeCall& c, cudaStream_t st) {
+  const int n_heads = c.q.heads + c.k.heads + c.v.heads;
+  bool wide = c.cfg.D % 8 == 0 && c.cfg.rot % 16 == 0 && heads_wide(c.q) && heads_wide(c.k) && heads_wide(c.v) &&
+              heads_wide(c.q_out) && heads_wide(c.k_out);
+  if (c.slots)
+    wide = wide && aligned16(c.cache.k) && aligned16(c.cache.v) && c.cache.ps % 8 == 0 && c.cache.ts % 8 == 0 && c.cache.hs % 8 == 0;
+  if (wide) {
+    const int chunks = c.cfg.rot / 16 + (c.cfg.D - c.cfg.rot + 15) / 16;
+    int hpt = 8;   // heads per thread: enough to share the sines, fewer while that leaves the device idle
+    while (hpt > 1 && c.T * chunks * ((n_heads + hpt - 1) / hpt) < (int64_t)148 * 1024) hpt >>= 1;
+    const int groups = (n_heads + hpt - 1) / hpt;
+    const int64_t blocks = (c.T * chunks * groups + 255) / 256;
+    if (blocks > 0x7fffffff) return QBLORA_ERR_UNSUPPORTED;
+    if (c.cfg.layout == QBLORA_ROPE_HALF) rope_wide_kernel<TI, TO, QBLORA_ROPE_HALF><<<(unsigned)blocks, 256, 0, st>>>(c, chunks, hpt, groups);
+    else rope_wide_kernel<TI, TO, QBLORA_ROPE_PAIRS><<<(unsigned)blocks, 256, 0, st>>>(c, chunks, hpt, groups);
+  } else {
+    const int64_t total = c.T * n_heads * (c.cfg.D - c.cfg.rot / 2);
+    int64_t blocks = (total + 255) / 256;
+    if (blocks > 148 * 16) blocks = 148 * 16;
+    rope_any_kernel<TI, TO><<<(unsigned)blocks, 256, 0, st>>>(c);
+  }
+  count_launch();
+  QB_CUDA(cudaGetLastError());
+  return QBLORA_OK;
+}
+
+}  // namespace
+
+int launch_rope(const RopeCall& c, cudaStream_t st) {
+  const bool in32 = c.q.dtype == QBLORA_F32, out32 = !c.slots && c.q_out.dtype == QBLORA_F32;
+  if (in32) return out32 ? launch_typed<float, float>(c, st) : launch_typed<float, __nv_bfloat16>(c, st);
+  return out32 ? launch_typed<__nv_bfloat16, float>(c, st) : launch_typed<__nv_bfloat16, __nv_bfloat16>(c, st);
+}
+
+}  // namespace qb

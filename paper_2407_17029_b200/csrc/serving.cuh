@@ -1,0 +1,82 @@
+// Shared declarations of the calls between the products of a served layer: rotary positions, the paged cache's plan
+// and the attention over it (include/qblora.h, last part).
+#pragma once
+#include "common.cuh"
+
+namespace qb {
+
+struct HeadsView {
+  void* data;
+  int64_t ts, hs;   // token and head stride, elements
+  int heads, dtype;
+};
+
+struct CacheView {
+  __nv_bfloat16 *k, *v;
+  int64_t ps, ts, hs;   // page, entry and head stride, elements
+  int n_pages, page_size, kv_heads;
+};
+
+struct RopeView {
+  int D, rot, layout;
+  float amp, sign;   // sign: +1 forward, -1 inverse
+  const uint64_t* turns;
+};
+
+// y2 / cache: see qblora_rope and qblora_rope_append.  v.data == nullptr: plain rotation of one or two tensors.
+struct RopeCall {
+  RopeView cfg;
+  const int* positions;
+  const int* slots;
+  int64_t T;
+  HeadsView q, k, v, q_out, k_out;   // heads == 0: not there
+  CacheView cache;                   // used when slots != nullptr: k and v go there
+};
+int launch_rope(const RopeCall& c, cudaStream_t st);
+
+struct PlanCall {
+  const int *ctx, *add, *release;
+  int B;
+  int* table; int width;
+  int* stack; int capacity;
+  const int* count; int* count_out;
+  int page, T;
+  int *cu, *kv, *pos, *slots, *admitted;
+};
+constexpr int kPlanMaxRequests = 8192;
+int launch_kv_plan(const PlanCall& c, cudaStream_t st);
+
+struct AttnCall {
+  CacheView cache;
+  const int* table; int width;
+  const int *cu, *kv; int B;
+  const __nv_bfloat16* q; int64_t q_ts, q_hs;
+  __nv_bfloat16* out; int64_t o_ts, o_hs;
+  float* lse;
+  int64_t T;
+  int H, G, D;          // query heads, query heads per key head, head size
+  float scale;
+  int causal, window;
+  int* status;
+};
+
+// Rows and keys of one request, with every length forced into its range (they come from device memory).
+struct ReqView { int t0, n, kv; };
+__device__ __forceinline__ ReqView attn_request(const AttnCall& c, int b) {
+  ReqView r;
+  const int T = (int)c.T;
+  r.t0 = min(max(__ldg(c.cu + b), 0), T);
+  const int t1 = min(max(__ldg(c.cu + b + 1), r.t0), T);
+  r.n = t1 - r.t0;
+  const long long most = (long long)c.width * c.cache.page_size;
+  r.kv = (int)min((long long)max(__ldg(c.kv + b), 0), most);
+  return r;
+}
+// Keys [lo, hi) that the row at position p (may be negative) sees.
+__device__ __forceinline__ int attn_hi(const AttnCall& c, int kv, int p) { return c.causal ? max(0, min(kv, p + 1)) : kv; }
+__device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.window > 0 ? max(0, p - c.window + 1) : 0; }
+
+// General path: any head size up to 256, any page size.
+int launch_simt_attention(const AttnCall& c, cudaStream_t st);
+
+}  // namespace qb

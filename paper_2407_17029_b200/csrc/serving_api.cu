@@ -1,0 +1,149 @@
+// extern "C" entry points of the last part of include/qblora.h (rotary positions, paged cache plan, attention): host-side
+// argument checks and dispatch.  No device memory is allocated here.
+#include <cmath>
+#include <cstdlib>
+
+#include "serving.cuh"
+
+namespace qb {
+namespace {
+
+bool heads_ok(const qblora_heads* h, HeadsView* v) {
+  if (!h || !h->data || h->heads < 1 || h->token_stride < 0 || h->head_stride < 0) return false;
+  if (h->dtype != QBLORA_F32 && h->dtype != QBLORA_BF16) return false;
+  if (reinterpret_cast<uintptr_t>(h->data) % (h->dtype == QBLORA_F32 ? 4 : 2)) return false;
+  *v = {h->data, h->token_stride, h->head_stride, h->heads, h->dtype};
+  return true;
+}
+
+bool cache_ok(const qblora_kv_cache* c, CacheView* v) {
+  if (!c || !c->k || !c->v) return false;
+  if (reinterpret_cast<uintptr_t>(c->k) % 2 || reinterpret_cast<uintptr_t>(c->v) % 2) return false;
+  if (c->n_pages < 1 || c->page_size < 1 || c->kv_heads < 1 || c->head_dim < 1) return false;
+  if (c->page_stride < 0 || c->token_stride < 0 || c->head_stride < 0) return false;
+  if ((int64_t)c->n_pages * c->page_size >= (int64_t)1 << 31) return false;
+  *v = {static_cast<__nv_bfloat16*>(c->k), static_cast<__nv_bfloat16*>(c->v), c->page_stride, c->token_stride,
+        c->head_stride, c->n_pages, c->page_size, c->kv_heads};
+  return true;
+}
+
+bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
+  if (!c || !c->turns || reinterpret_cast<uintptr_t>(c->turns) % 8) return false;
+  if (c->head_dim < 2 || c->rotary_dim < 2 || c->rotary_dim % 2 || c->rotary_dim > c->head_dim) return false;
+  if (c->layout != QBLORA_ROPE_HALF && c->layout != QBLORA_ROPE_PAIRS) return false;
+  if (!std::isfinite(c->amplitude)) return false;
+  *v = {c->head_dim, c->rotary_dim, c->layout, c->amplitude, inverse ? -1.0f : 1.0f, c->turns};
+  return true;
+}
+
+bool int_ptr_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 4 == 0; }
+
+}  // namespace
+}  // namespace qb
+
+using namespace qb;
+
+extern "C" {
+
+int qblora_rope_table(int32_t rotary_dim, double base, int32_t scale, double factor, int64_t trained_len, double slow,
+                      double fast, uint64_t* turns) {
+  if (!turns || rotary_dim < 2 || rotary_dim % 2 || !(base > 1.0) || !std::isfinite(base)) return QBLORA_ERR_INVALID_ARG;
+  if (scale < QBLORA_ROPE_SCALE_NONE || scale > QBLORA_ROPE_SCALE_BANDED) return QBLORA_ERR_INVALID_ARG;
+  if (scale != QBLORA_ROPE_SCALE_NONE && !(factor > 0.0 && std::isfinite(factor))) return QBLORA_ERR_INVALID_ARG;
+  if (scale == QBLORA_ROPE_SCALE_BANDED && !(trained_len > 0 && slow < fast)) return QBLORA_ERR_INVALID_ARG;
+  if (scale == QBLORA_ROPE_SCALE_BASE) {
+    if (rotary_dim == 2) return QBLORA_ERR_INVALID_ARG;   // the exponent d / (d - 2) has no value
+    base *= std::pow(factor, (double)rotary_dim / (rotary_dim - 2));
+    if (!(base > 1.0)) return QBLORA_ERR_INVALID_ARG;
+  }
+  const double two_pi = 6.283185307179586476925;
+  for (int j = 0; j < rotary_dim / 2; ++j) {
+    double f = std::pow(base, -2.0 * j / rotary_dim) / two_pi;
+    if (scale == QBLORA_ROPE_SCALE_LINEAR) f /= factor;
+    if (scale == QBLORA_ROPE_SCALE_BANDED) {
+      double w = ((double)trained_len * f - slow) / (fast - slow);
+      w = w < 0.0 ? 0.0 : w > 1.0 ? 1.0 : w;
+      f = f * w + f / factor * (1.0 - w);
+    }
+    f -= std::floor(f);                                    // whole turns per position (factor < 1) change nothing
+    turns[j] = static_cast<uint64_t>(std::ldexp(f, 64));   // f < 1: below 2^64
+  }
+  return QBLORA_OK;
+}
+
+int qblora_rope(const qblora_rope_cfg* cfg, int inverse, const int32_t* positions, int64_t tokens, const qblora_heads* x,
+                const qblora_heads* y, const qblora_heads* x2, const qblora_heads* y2, void* stream) {
+  RopeCall c{};
+  if (!rope_ok(cfg, inverse, &c.cfg) || !int_ptr_ok(positions) || tokens < 1) return QBLORA_ERR_INVALID_ARG;
+  if (!heads_ok(x, &c.q) || !heads_ok(y, &c.q_out) || x->heads != y->heads) return QBLORA_ERR_INVALID_ARG;
+  if ((x2 == nullptr) != (y2 == nullptr)) return QBLORA_ERR_INVALID_ARG;
+  if (x2) {
+    if (!heads_ok(x2, &c.k) || !heads_ok(y2, &c.k_out) || x2->heads != y2->heads) return QBLORA_ERR_INVALID_ARG;
+    if (x2->dtype != x->dtype || y2->dtype != y->dtype) return QBLORA_ERR_INVALID_ARG;
+  }
+  c.positions = positions; c.T = tokens;
+  return launch_rope(c, static_cast<cudaStream_t>(stream));
+}
+
+int qblora_rope_append(const qblora_rope_cfg* cfg, const int32_t* positions, const int32_t* slots, int64_t tokens,
+                       const qblora_heads* q, const qblora_heads* k, const qblora_heads* v, const qblora_heads* q_out,
+                       const qblora_kv_cache* cache, void* stream) {
+  RopeCall c{};
+  if (!rope_ok(cfg, 0, &c.cfg) || !int_ptr_ok(positions) || !int_ptr_ok(slots) || tokens < 1) return QBLORA_ERR_INVALID_ARG;
+  if (!heads_ok(q, &c.q) || !heads_ok(k, &c.k) || !heads_ok(v, &c.v) || !heads_ok(q_out, &c.q_out)) return QBLORA_ERR_INVALID_ARG;
+  if (!cache_ok(cache, &c.cache)) return QBLORA_ERR_INVALID_ARG;
+  if (q->heads != q_out->heads || q_out->dtype != QBLORA_BF16 || k->dtype != q->dtype || v->dtype != q->dtype) return QBLORA_ERR_INVALID_ARG;
+  if (k->heads != cache->kv_heads || v->heads != cache->kv_heads || cfg->head_dim != cache->head_dim) return QBLORA_ERR_INVALID_ARG;
+  c.positions = positions; c.slots = slots; c.T = tokens;
+  return launch_rope(c, static_cast<cudaStream_t>(stream));
+}
+
+int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t* release, int32_t n_requests,
+                   int32_t* block_table, int32_t width, int32_t* free_pages, int32_t capacity, const int32_t* free_count,
+                   int32_t* free_count_out, int32_t page_size, int32_t tokens, int32_t* cu_new, int32_t* kv_len,
+                   int32_t* positions, int32_t* slots, int32_t* admitted, void* stream) {
+  if (!int_ptr_ok(ctx_len) || !int_ptr_ok(new_len) || !int_ptr_ok(block_table) || !int_ptr_ok(free_pages)) return QBLORA_ERR_INVALID_ARG;
+  if (!int_ptr_ok(free_count) || !int_ptr_ok(free_count_out) || free_count == free_count_out) return QBLORA_ERR_INVALID_ARG;
+  if (!int_ptr_ok(cu_new) || !int_ptr_ok(kv_len) || !int_ptr_ok(positions) || !int_ptr_ok(slots) || !int_ptr_ok(admitted)) return QBLORA_ERR_INVALID_ARG;
+  if (release && !int_ptr_ok(release)) return QBLORA_ERR_INVALID_ARG;
+  if (n_requests < 1 || width < 1 || capacity < 1 || page_size < 1 || tokens < 1) return QBLORA_ERR_INVALID_ARG;
+  if ((int64_t)capacity * page_size >= (int64_t)1 << 31 || (int64_t)width * page_size >= (int64_t)1 << 31) return QBLORA_ERR_INVALID_ARG;
+  if (n_requests > kPlanMaxRequests) return QBLORA_ERR_UNSUPPORTED;
+  PlanCall c{ctx_len, new_len, release, n_requests, block_table, width, free_pages, capacity, free_count, free_count_out,
+             page_size, tokens, cu_new, kv_len, positions, slots, admitted};
+  return launch_kv_plan(c, static_cast<cudaStream_t>(stream));
+}
+
+size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens) {
+  if (!cache || cache->kv_heads < 1 || q_heads < 1 || q_heads % cache->kv_heads || tokens < 1) return 0;
+  return kStatusBytes;
+}
+
+int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_table, int32_t width, const int32_t* cu_new,
+                           const int32_t* kv_len, int32_t n_requests, const qblora_heads* q, int64_t tokens, float scale,
+                           int causal, int32_t window, const qblora_heads* out, float* lse, void* ws, size_t ws_bytes,
+                           void* stream) {
+  AttnCall c{};
+  HeadsView qv, ov;
+  if (!cache_ok(cache, &c.cache) || !heads_ok(q, &qv) || !heads_ok(out, &ov)) return QBLORA_ERR_INVALID_ARG;
+  if (!int_ptr_ok(block_table) || !int_ptr_ok(cu_new) || !int_ptr_ok(kv_len) || (lse && !int_ptr_ok(lse))) return QBLORA_ERR_INVALID_ARG;
+  if (width < 1 || n_requests < 1 || tokens < 1 || tokens >= (int64_t)1 << 31 || window < 0 || !std::isfinite(scale)) return QBLORA_ERR_INVALID_ARG;
+  if ((int64_t)width * cache->page_size >= (int64_t)1 << 31) return QBLORA_ERR_INVALID_ARG;
+  if (qv.dtype != QBLORA_BF16 || ov.dtype != QBLORA_BF16 || qv.heads != ov.heads || qv.heads % cache->kv_heads) return QBLORA_ERR_INVALID_ARG;
+  if (cache->head_dim % 8) return QBLORA_ERR_INVALID_ARG;
+  if (!aligned16(q->data) || !aligned16(out->data) || !aligned16(cache->k) || !aligned16(cache->v)) return QBLORA_ERR_INVALID_ARG;
+  if (qv.ts % 8 || qv.hs % 8 || ov.ts % 8 || ov.hs % 8 || c.cache.ps % 8 || c.cache.ts % 8 || c.cache.hs % 8) return QBLORA_ERR_INVALID_ARG;
+  if (cache->head_dim > 256) return QBLORA_ERR_UNSUPPORTED;
+  if (!ws || !aligned16(ws) || ws_bytes < qblora_attention_workspace_bytes(cache, q->heads, tokens)) return QBLORA_ERR_WORKSPACE;
+  c.table = block_table; c.width = width; c.cu = cu_new; c.kv = kv_len; c.B = n_requests;
+  c.q = static_cast<const __nv_bfloat16*>(qv.data); c.q_ts = qv.ts; c.q_hs = qv.hs;
+  c.out = static_cast<__nv_bfloat16*>(ov.data); c.o_ts = ov.ts; c.o_hs = ov.hs;
+  c.lse = lse; c.T = tokens; c.H = qv.heads; c.G = qv.heads / cache->kv_heads; c.D = cache->head_dim;
+  c.scale = scale; c.causal = causal != 0; c.window = window;
+  c.status = static_cast<int*>(ws);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  QB_CUDA(cudaMemsetAsync(ws, 0, 16, st));
+  return launch_simt_attention(c, st);
+}
+
+}  // extern "C"
