@@ -76,6 +76,13 @@ __device__ __forceinline__ ReqView attn_request(const AttnCall& c, int b) {
 __device__ __forceinline__ int attn_hi(const AttnCall& c, int kv, int p) { return c.causal ? max(0, min(kv, p + 1)) : kv; }
 __device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.window > 0 ? max(0, p - c.window + 1) : 0; }
 
+// Few rows per key head (paged_attn.cu): requests of at most `narrow_rows` rows (new tokens * G).  `scratch`:
+// paged_attention_scratch_bytes, its first kPagedCounterBytes zeroed on the stream before the launch.
+constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;
+constexpr size_t kPagedCounterBytes = kPagedMaxSms * kPagedMaxPerSm * 4;
+size_t paged_attention_scratch_bytes(int head_dim);
+int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
+
 // General path: any head size up to 256, any page size.
 int launch_simt_attention(const AttnCall& c, cudaStream_t st);
 

@@ -36,6 +36,11 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
   return true;
 }
 
+bool force_general() {
+  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
+  return e && e[0] == '1';
+}
+
 bool int_ptr_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
 }  // namespace
@@ -116,7 +121,8 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
 
 size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens) {
   if (!cache || cache->kv_heads < 1 || q_heads < 1 || q_heads % cache->kv_heads || tokens < 1) return 0;
-  return kStatusBytes;
+  if (cache->head_dim < 1 || cache->head_dim > 256) return 0;
+  return kStatusBytes + paged_attention_scratch_bytes(cache->head_dim);
 }
 
 int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_table, int32_t width, const int32_t* cu_new,
@@ -133,7 +139,7 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   if (cache->head_dim % 8) return QBLORA_ERR_INVALID_ARG;
   if (!aligned16(q->data) || !aligned16(out->data) || !aligned16(cache->k) || !aligned16(cache->v)) return QBLORA_ERR_INVALID_ARG;
   if (qv.ts % 8 || qv.hs % 8 || ov.ts % 8 || ov.hs % 8 || c.cache.ps % 8 || c.cache.ts % 8 || c.cache.hs % 8) return QBLORA_ERR_INVALID_ARG;
-  if (cache->head_dim > 256) return QBLORA_ERR_UNSUPPORTED;
+  if (cache->head_dim > 256 || tokens * q->heads >= (int64_t)1 << 31) return QBLORA_ERR_UNSUPPORTED;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_attention_workspace_bytes(cache, q->heads, tokens)) return QBLORA_ERR_WORKSPACE;
   c.table = block_table; c.width = width; c.cu = cu_new; c.kv = kv_len; c.B = n_requests;
   c.q = static_cast<const __nv_bfloat16*>(qv.data); c.q_ts = qv.ts; c.q_hs = qv.hs;
@@ -142,8 +148,9 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   c.scale = scale; c.causal = causal != 0; c.window = window;
   c.status = static_cast<int*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  QB_CUDA(cudaMemsetAsync(ws, 0, 16, st));
-  return launch_simt_attention(c, st);
+  QB_CUDA(cudaMemsetAsync(ws, 0, kStatusBytes + kPagedCounterBytes, st));   // status word and arrival counters
+  if (force_general()) return launch_simt_attention(c, st);
+  return launch_paged_attention(c, 0x7fffffff, static_cast<char*>(ws) + kStatusBytes, st);
 }
 
 }  // extern "C"
