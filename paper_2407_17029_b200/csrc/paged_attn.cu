@@ -148,6 +148,8 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
   const int wr = warp / WK, wk = warp % WK;
   const uint32_t smem = ptx::smem_u32(pa_smem);
 
+  // the tcgen05 kernel of the same call reads nothing of this one's and may start as SMs become free
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // ---- the line: units before each request, total, this CTA's share -----------------------------------------------
   const int per = (c.B + PA_THREADS - 1) / PA_THREADS;
   const int b_lo = min(tid * per, c.B), b_hi = min(b_lo + per, c.B);

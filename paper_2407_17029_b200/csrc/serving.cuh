@@ -83,6 +83,15 @@ constexpr size_t kPagedCounterBytes = kPagedMaxSms * kPagedMaxPerSm * 4;
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
 
+// Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows.  `counters`:
+// kWideCounterBytes, zeroed on the stream; `scratch`: tc_attention_scratch_bytes.  `behind_narrow`: the kernel in front on the stream is
+// launch_paged_attention's of the same call, and this one may start beside it.
+constexpr int kWideMaxRequests = 1024;
+constexpr size_t kWideCounterBytes = 2 * kPagedMaxSms * 4;
+bool tc_attention_supported(const AttnCall& c);
+size_t tc_attention_scratch_bytes(int head_dim);
+int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, bool behind_narrow, cudaStream_t st);
+
 // General path: any head size up to 256, any page size.
 int launch_simt_attention(const AttnCall& c, cudaStream_t st);
 

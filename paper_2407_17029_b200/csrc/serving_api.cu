@@ -36,6 +36,9 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
   return true;
 }
 
+// Requests with more rows (new tokens x query heads per key head) go to the tcgen05 kernel.
+constexpr int kNarrowRows = 64;
+
 bool force_general() {
   const char* e = std::getenv("QBLORA_FORCE_GENERAL");
   return e && e[0] == '1';
@@ -122,7 +125,7 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
 size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens) {
   if (!cache || cache->kv_heads < 1 || q_heads < 1 || q_heads % cache->kv_heads || tokens < 1) return 0;
   if (cache->head_dim < 1 || cache->head_dim > 256) return 0;
-  return kStatusBytes + paged_attention_scratch_bytes(cache->head_dim);
+  return kStatusBytes + kWideCounterBytes + paged_attention_scratch_bytes(cache->head_dim) + tc_attention_scratch_bytes(cache->head_dim);
 }
 
 int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_table, int32_t width, const int32_t* cu_new,
@@ -148,9 +151,15 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   c.scale = scale; c.causal = causal != 0; c.window = window;
   c.status = static_cast<int*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  QB_CUDA(cudaMemsetAsync(ws, 0, kStatusBytes + kPagedCounterBytes, st));   // status word and arrival counters
+  // status word, arrival counters of both kernels (which begin their scratch areas)
+  const bool wide = tc_attention_supported(c) && tokens * c.G > kNarrowRows;
+  char* wide_ws = static_cast<char*>(ws) + kStatusBytes;
+  char* narrow_ws = wide_ws + kWideCounterBytes;
+  QB_CUDA(cudaMemsetAsync(ws, 0, kStatusBytes + kWideCounterBytes + kPagedCounterBytes, st));
   if (force_general()) return launch_simt_attention(c, st);
-  return launch_paged_attention(c, 0x7fffffff, static_cast<char*>(ws) + kStatusBytes, st);
+  const int rc = launch_paged_attention(c, wide ? kNarrowRows : 0x7fffffff, narrow_ws, st);
+  if (rc || !wide) return rc;
+  return launch_tc_attention(c, kNarrowRows, wide_ws, narrow_ws + paged_attention_scratch_bytes(c.D), true, st);
 }
 
 }  // extern "C"

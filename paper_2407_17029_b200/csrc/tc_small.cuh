@@ -48,4 +48,8 @@ enum { TM_BF16 = 0, TM_U8 = 1, TM_U32 = 2, TM_F32 = 3 };
 int make_tensor_map_2d_typed(void* tm, int elem, const void* ptr, uint64_t inner, uint64_t rows, uint64_t pitch_bytes,
                              uint32_t box_inner, uint32_t box_rows, int swizzle_bytes);
 
+// bf16 tensor map of 3 or 4 dimensions, innermost contiguous, 128-byte swizzle.  pitch_bytes[i]: bytes between neighbours of
+// dimension i + 1.
+int make_tensor_map_nd(void* tm, int rank, const void* ptr, const uint64_t* dims, const uint64_t* pitch_bytes, const uint32_t* box);
+
 }  // namespace qb

@@ -271,6 +271,19 @@ int make_tensor_map_2d_typed(void* tm, int elem, const void* ptr, uint64_t inner
   return r == CUDA_SUCCESS ? QBLORA_OK : QBLORA_ERR_CUDA;
 }
 
+int make_tensor_map_nd(void* tm, int rank, const void* ptr, const uint64_t* dims, const uint64_t* pitch_bytes, const uint32_t* box) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn || rank < 3 || rank > 4) return QBLORA_ERR_CUDA;
+  cuuint64_t d[4], st[3];
+  cuuint32_t b[4], estr[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) { d[i] = dims[i]; b[i] = box[i]; }
+  for (int i = 0; i + 1 < rank; ++i) st[i] = pitch_bytes[i];
+  const CUresult r = fn(static_cast<CUtensorMap*>(tm), CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(ptr), d, st,
+                        b, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? QBLORA_OK : QBLORA_ERR_CUDA;
+}
+
 int small_gemm_splits(int M, int N, int K) {
   const int n64 = (N + 63) / 64 * 64;
   const int bn = n64 < 256 ? n64 : 256;

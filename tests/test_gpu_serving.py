@@ -285,6 +285,20 @@ def test_attention_chunks(H, Hkv):
     _attend([65, 300], [65, 301], H, Hkv, 64)
 
 
+@pytest.mark.parametrize("H,Hkv,D,new,kv", [
+    (8, 8, 128, [900, 1, 333], [2900, 700, 333]),           # shares of many tiles that cross items and requests
+    (16, 16, 64, [700, 650], [3000, 650]),
+    (32, 4, 128, [500], [5000]),                             # shared keys
+    (64, 64, 64, [2600], [2600]),                            # more than four items per SM: whole items
+    (40, 40, 128, [1600, 1, 1700], [1700, 9, 1700]),
+])
+def test_attention_long_chunks(H, Hkv, D, new, kv):
+    _attend(new, kv, H, Hkv, D)
+    if H < 40:
+        _attend(new, kv, H, Hkv, D, window=300, seed=2)
+        _attend(new, kv, H, Hkv, D, page=128, causal=False, seed=3)
+
+
 @pytest.mark.parametrize("order", ["nhd", "hnd"])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 20), (True, 130), (False, 50), (True, 4000)])
 def test_attention_masks_and_orders(order, causal, window):
