@@ -1,0 +1,43 @@
+// Register-fragment helpers of the attention kernels that use mma.sync.m16n8k16 (bf16 operands, fp32 sums).
+#pragma once
+#include "common.cuh"
+
+namespace qb {
+
+__device__ __forceinline__ float fast_exp2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// x / d for 0 <= x < 2^31 and m = fast_div_magic(d) = ceil(2^32 / d) (0 for d = 1): the product's high word is the quotient
+// or one more.
+__device__ __forceinline__ int fast_div(int x, int d, uint32_t m) {
+  if (m == 0) return x;
+  const int q = (int)__umulhi((uint32_t)x, m);
+  return q * (long long)d > x ? q - 1 : q;
+}
+inline uint32_t fast_div_magic(uint32_t d) { return d == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
+
+__device__ __forceinline__ void frag_ldm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void frag_ldm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void frag_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// a NaN or infinity among two bf16 values; the two with such values set to zero
+__device__ __forceinline__ bool bf16x2_odd(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ uint32_t bf16x2_clean(uint32_t x) {
+  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
+  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
+  return x;
+}
+
+}  // namespace qb

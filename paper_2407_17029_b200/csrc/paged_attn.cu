@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "mma_frag.cuh"
 #include "serving.cuh"
 #include "tc_ptx.cuh"
 
@@ -35,54 +36,31 @@ struct PaParams {
   float scale2;         // scale * log2 e
   int narrow_rows;      // requests with more rows (new tokens * G) than this belong to the tcgen05 kernel
   int min_units;        // key tiles per share below which fewer shares are made
+  uint32_t div_page, div_group;   // 2^32 / divisor, rounded up (fast_div)
   uint32_t* counters;   // [grid] zeroed before the launch
   float* part_o;        // [2 * grid][ROWS][DP]
   float* part_ml;       // [2 * grid][ROWS][2]
 };
 
-__device__ __forceinline__ float pa_exp2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 __device__ __forceinline__ void pa_cp16(uint32_t dst, const void* src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 __device__ __forceinline__ void pa_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void pa_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void pa_ldm4(uint32_t (&r)[4], uint32_t a) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void pa_ldm4t(uint32_t (&r)[4], uint32_t a) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
-}
-__device__ __forceinline__ void pa_mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
-      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ bool pa_odd(uint32_t x) {   // a NaN or infinity among two bf16 values
-  return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u;
-}
-__device__ __forceinline__ uint32_t pa_clean(uint32_t x) {
-  if ((x & 0x7f80u) == 0x7f80u) x &= 0xffff0000u;
-  if ((x & 0x7f800000u) == 0x7f800000u) x &= 0x0000ffffu;
-  return x;
-}
-
 // Keys [lo, lo + 64 * tiles) that the rows of tile rt of a request see, at least one (possibly empty) tile.
-struct PaRange { int lo, hi, tiles; };
+// [all_lo, all_hi): the keys that every row of the tile sees.
+struct PaRange { int lo, hi, tiles, all_lo, all_hi; };
 template <int ROWS>
-__device__ __forceinline__ PaRange pa_range(const AttnCall& c, const ReqView& r, int rt) {
-  const int i0 = rt * ROWS / c.G, i1 = min(r.n - 1, (rt * ROWS + ROWS - 1) / c.G);
+__device__ __forceinline__ PaRange pa_range(const PaParams& p, const ReqView& r, int rt) {
+  const AttnCall& c = p.c;
+  const int i0 = fast_div(rt * ROWS, c.G, p.div_group), i1 = min(r.n - 1, fast_div(rt * ROWS + ROWS - 1, c.G, p.div_group));
   PaRange k;
   k.hi = attn_hi(c, r.kv, r.kv - r.n + i1);
   k.lo = min(attn_lo(c, r.kv - r.n + i0), k.hi);
   k.tiles = max(1, (k.hi - k.lo + PA_TILE - 1) / PA_TILE);
+  k.all_lo = attn_lo(c, r.kv - r.n + i1);
+  k.all_hi = attn_hi(c, r.kv, r.kv - r.n + i0);
   return k;
 }
 template <int ROWS>
@@ -96,7 +74,7 @@ template <int ROWS>
 __device__ __forceinline__ int pa_head_units(const PaParams& p, const ReqView& r) {
   int u = 0;
   const int nrt = pa_row_tiles<ROWS>(p, r);
-  for (int rt = 0; rt < nrt; ++rt) u += pa_range<ROWS>(p.c, r, rt).tiles;
+  for (int rt = 0; rt < nrt; ++rt) u += pa_range<ROWS>(p, r, rt).tiles;
   return u;
 }
 
@@ -106,7 +84,7 @@ struct PaCursor {
   int b, h, rt, nrt, tile;
   ReqView r;
   PaRange k;
-  __device__ __forceinline__ void enter_tile(const PaParams& p) { k = pa_range<ROWS>(p.c, r, rt); }
+  __device__ __forceinline__ void enter_tile(const PaParams& p) { k = pa_range<ROWS>(p, r, rt); }
   __device__ __forceinline__ void next(const PaParams& p) {
     if (++tile < k.tiles) return;
     tile = 0;
@@ -126,8 +104,7 @@ template <int DP, int WR, int STAGES>
 struct PaShape {
   static constexpr int ROWS = 16 * WR, WK = 4 / WR;
   static constexpr int KV_BYTES = PA_TILE * DP * 2;          // K or V of a stage
-  static constexpr int Q_BYTES = ROWS * DP * 2;
-  static constexpr int STAGE = 2 * KV_BYTES + Q_BYTES;
+  static constexpr int STAGE = 2 * KV_BYTES;
   static constexpr int SMEM = STAGES * STAGE;
 };
 
@@ -212,7 +189,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
   // thread < 64: page number of its key in the tile (or -1), and, when that number has arrived, the key's offset
   auto key_page = [&](const PaCursor<ROWS>& at) -> int {
     const int j = at.k.lo + at.tile * PA_TILE + tid;
-    return j < at.k.hi ? __ldg(c.table + (long long)at.b * c.width + j / c.cache.page_size) : -1;
+    return j < at.k.hi ? __ldg(c.table + (long long)at.b * c.width + fast_div(j, c.cache.page_size, p.div_page)) : -1;
   };
   auto key_offset = [&](const PaCursor<ROWS>& at, int page) -> long long {
     const int j = at.k.lo + at.tile * PA_TILE + tid;
@@ -221,42 +198,36 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
       atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
       return -1;
     }
-    return (long long)page * c.cache.ps + (long long)(j % c.cache.page_size) * c.cache.ts + (long long)at.h * c.cache.hs;
+    const int entry = j - fast_div(j, c.cache.page_size, p.div_page) * c.cache.page_size;
+    return (long long)page * c.cache.ps + (long long)entry * c.cache.ts + (long long)at.h * c.cache.hs;
   };
   const int ch = tid % CH;                        // this thread's 16-byte column in K, V and Q rows
   const bool col = ch * 8 < c.D;
-  auto load_tile = [&](const PaCursor<ROWS>& at, int stage, int buf, bool with_q) {
-    const uint32_t sk = smem + stage * Sh::STAGE, sv = sk + Sh::KV_BYTES, sq = sv + Sh::KV_BYTES;
+  const uint32_t my_dst = (uint32_t)((tid / CH) * DP * 2 + ((ch ^ ((tid / CH) & 7)) << 4));
+  auto load_tile = [&](int stage, int buf) {
+    const uint32_t sk = smem + stage * Sh::STAGE + my_dst;
 #pragma unroll
     for (int i = 0; i < PA_TILE * CH / PA_THREADS; ++i) {
-      const int row = tid / CH + i * (PA_THREADS / CH);
+      // rows of one thread are PA_THREADS / CH apart; where that is 4 or less the swizzle changes from row to row
+      constexpr int STEP = PA_THREADS / CH;
+      const int row = tid / CH + i * STEP;
       const long long off = s_off[buf][row];
       const bool there = off >= 0 && col;
       const long long o = there ? off + ch * 8 : 0;
-      const uint32_t d = (uint32_t)(row * DP * 2 + ((ch ^ (row & 7)) << 4));
-      pa_cp16(sk + d, c.cache.k + o, there);
-      pa_cp16(sv + d, c.cache.v + o, there);
-    }
-    if (with_q) {
-#pragma unroll
-      for (int i = 0; i < (ROWS * CH + PA_THREADS - 1) / PA_THREADS; ++i) {
-        const int row = tid / CH + i * (PA_THREADS / CH);
-        if (row < ROWS) {
-          const int rr = at.rt * ROWS + row, tok = rr / c.G;
-          const bool there = tok < at.r.n && col;
-          const long long o = there ? (long long)(at.r.t0 + tok) * c.q_ts + (long long)(at.h * c.G + rr - tok * c.G) * c.q_hs + ch * 8 : 0;
-          pa_cp16(sq + (uint32_t)(row * DP * 2 + ((ch ^ (row & 7)) << 4)), c.q + o, there);
-        }
-      }
+      const uint32_t d = STEP % 8 == 0 ? sk + i * STEP * DP * 2
+                                       : smem + stage * Sh::STAGE + (uint32_t)(row * DP * 2 + ((ch ^ (row & 7)) << 4));
+      pa_cp16(d, c.cache.k + o, there);
+      pa_cp16(d + Sh::KV_BYTES, c.cache.v + o, there);
     }
   };
 
   // prologue: STAGES - 1 tiles on their way; from then on `ld` is the next tile to load and `page` its page numbers,
   // fetched one iteration before they are needed
   long long issued = 0;
-  int buf = 0, page = tid < PA_TILE ? key_page(ld) : -1;
+  int buf = 0, page = tid < PA_TILE ? key_page(ld) : -1, ld_stage = 0;
   auto load_next = [&]() {
-    load_tile(ld, (int)(issued % STAGES), buf, issued == 0 || ld.tile == 0);
+    load_tile(ld_stage, buf);
+    if (++ld_stage == STAGES) ld_stage = 0;
     buf ^= 1;
     if (++issued < units) {
       ld.next(p);
@@ -275,21 +246,33 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
   float o[DP / 8][4], m[2], l[2];
   uint32_t qf[DP / 16][4];
   bool first_segment = true;
+  int r0 = 0, hi[2] = {0, 0}, lo[2] = {0, 0};
 
+  int stage = -1;
   for (long long it = 0; it < units; ++it) {
-    const int stage = (int)(it % STAGES);
+    if (++stage == STAGES) stage = 0;
     if (issued < units && tid < PA_TILE) s_off[buf][tid] = key_offset(ld, page);
     pa_wait<STAGES - 2>();
     __syncthreads();
     if (issued < units) load_next();
     pa_commit();
 
-    const uint32_t sk = smem + stage * Sh::STAGE, sv = sk + Sh::KV_BYTES, sq = sv + Sh::KV_BYTES;
+    const uint32_t sk = smem + stage * Sh::STAGE, sv = sk + Sh::KV_BYTES;
     if (it == 0 || cu.tile == 0) {
+      r0 = cu.rt * ROWS;
 #pragma unroll
-      for (int k = 0; k < DP / 16; ++k) {
-        const int row = wr * 16 + (lane & 15), chunk = 2 * k + (lane >> 4);
-        pa_ldm4(qf[k], sq + (uint32_t)(row * DP * 2 + ((chunk ^ (row & 7)) << 4)));
+      for (int i = 0; i < 2; ++i) {                        // this lane's two rows: queries, and the keys they see
+        const int gr = r0 + wr * 16 + (lane >> 2) + 8 * i, tok = fast_div(gr, c.G, p.div_group);
+        const int pos = cu.r.kv - cu.r.n + min(tok, cu.r.n - 1);
+        hi[i] = attn_hi(c, cu.r.kv, pos);
+        lo[i] = attn_lo(c, pos);
+        const uint32_t* q = reinterpret_cast<const uint32_t*>(c.q + (long long)(cu.r.t0 + tok) * c.q_ts +
+                                                              (long long)(cu.h * c.G + gr - tok * c.G) * c.q_hs) + (lane & 3);
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k) {
+          qf[k][i] = tok < cu.r.n && 16 * k < c.D ? __ldg(q + 8 * k) : 0u;
+          qf[k][2 + i] = tok < cu.r.n && 16 * k + 8 < c.D ? __ldg(q + 8 * k + 4) : 0u;
+        }
       }
 #pragma unroll
       for (int i = 0; i < DP / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -308,27 +291,19 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
         // matrices: keys 0-7 chunk 2k, keys 0-7 chunk 2k+1, keys 8-15 chunk 2k, keys 8-15 chunk 2k+1
         const int row = wk * KPW + n2 * 16 + (lane & 7) + ((lane >> 4) << 3), chunk = 2 * k + ((lane >> 3) & 1);
         uint32_t kf[4];
-        pa_ldm4(kf, sk + (uint32_t)(row * DP * 2 + ((chunk ^ (row & 7)) << 4)));
-        pa_mma(s[2 * n2], qf[k], kf[0], kf[1]);
-        pa_mma(s[2 * n2 + 1], qf[k], kf[2], kf[3]);
+        frag_ldm4(kf, sk + (uint32_t)(row * DP * 2 + ((chunk ^ (row & 7)) << 4)));
+        frag_mma(s[2 * n2], qf[k], kf[0], kf[1]);
+        frag_mma(s[2 * n2 + 1], qf[k], kf[2], kf[3]);
       }
     }
     // masks: only where some row does not see some key of the tile
     const int k0 = cu.k.lo + cu.tile * PA_TILE;
-    const int r0 = cu.rt * ROWS, tok0 = r0 / c.G, tok1 = min(cu.r.n - 1, (r0 + ROWS - 1) / c.G), p0 = cu.r.kv - cu.r.n;
-    const bool partial = k0 + PA_TILE > attn_hi(c, cu.r.kv, p0 + tok0) || k0 < attn_lo(c, p0 + tok1);
-    int hi[2], lo[2];
+    const bool partial = k0 + PA_TILE > cu.k.all_hi || k0 < cu.k.all_lo;
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[n][e] *= p.scale2;
     if (partial) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int pos = p0 + min(cu.r.n - 1, (r0 + wr * 16 + (lane >> 2) + 8 * i) / c.G);
-        hi[i] = attn_hi(c, cu.r.kv, pos);
-        lo[i] = attn_lo(c, pos);
-      }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -346,13 +321,13 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
       t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 1));
       t = fmaxf(t, __shfl_xor_sync(0xffffffffu, t, 2));
       const float base = t == -INFINITY ? 0.f : t;       // nothing seen yet: all weights are 2^-inf = 0
-      f[i] = pa_exp2(m[i] - base);
+      f[i] = fast_exp2(m[i] - base);
       m[i] = t;
       float sum = 0.f;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        s[n][2 * i] = pa_exp2(s[n][2 * i] - base);
-        s[n][2 * i + 1] = pa_exp2(s[n][2 * i + 1] - base);
+        s[n][2 * i] = fast_exp2(s[n][2 * i] - base);
+        s[n][2 * i + 1] = fast_exp2(s[n][2 * i + 1] - base);
         sum += s[n][2 * i] + s[n][2 * i + 1];
       }
       l[i] = l[i] * f[i] + sum;                          // this lane's part; joined over the quad at the end
@@ -373,16 +348,16 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
       for (int n2 = 0; n2 < DP / 16; ++n2) {
         const int row = wk * KPW + k * 16 + (lane & 15), chunk = 2 * n2 + (lane >> 4);
         uint32_t vf[4];
-        pa_ldm4t(vf, sv + (uint32_t)(row * DP * 2 + ((chunk ^ (row & 7)) << 4)));
+        frag_ldm4t(vf, sv + (uint32_t)(row * DP * 2 + ((chunk ^ (row & 7)) << 4)));
         if (partial) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            odd |= pa_odd(vf[e]);
-            vf[e] = pa_clean(vf[e]);                     // 0 * NaN must not reach the rows that do not see the key
+            odd |= bf16x2_odd(vf[e]);
+            vf[e] = bf16x2_clean(vf[e]);                     // 0 * NaN must not reach the rows that do not see the key
           }
         }
-        pa_mma(o[2 * n2], a, vf[0], vf[1]);
-        pa_mma(o[2 * n2 + 1], a, vf[2], vf[3]);
+        frag_mma(o[2 * n2], a, vf[0], vf[1]);
+        frag_mma(o[2 * n2 + 1], a, vf[2], vf[3]);
       }
     }
     if (partial && __any_sync(0xffffffffu, odd)) {
@@ -393,7 +368,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
         for (int n = 0; n < DP / 8; ++n) {
           const uint32_t w = *reinterpret_cast<const uint32_t*>(pa_smem + stage * Sh::STAGE + Sh::KV_BYTES + row * DP * 2 +
                                                                 ((n ^ (row & 7)) << 4) + 4 * (lane & 3));
-          if (!pa_odd(w)) continue;
+          if (!bf16x2_odd(w)) continue;
           const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -438,7 +413,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int w = 0; w < WK; ++w) {
-          const float g = pa_exp2(s_m[w0 + w][rr] - base);
+          const float g = fast_exp2(s_m[w0 + w][rr] - base);
           L += s_l[w0 + w][rr] * g;
           const float4 v = *reinterpret_cast<const float4*>(so + ((w0 + w) * 16 + rr) * DP + 4 * x);
           acc.x += v.x * g; acc.y += v.y * g; acc.z += v.z * g; acc.w += v.w * g;
@@ -448,7 +423,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
           if (x == 0) *reinterpret_cast<float2*>(p.part_ml + ((long long)slot * ROWS + row) * 2) = make_float2(M, L);
           continue;
         }
-        const int gr = r0 + row, tok = gr / c.G;
+        const int gr = r0 + row, tok = fast_div(gr, c.G, p.div_group);
         if (tok >= cu.r.n || 4 * x >= c.D) continue;
         const int head = cu.h * c.G + gr - tok * c.G;
         const float inv = L == 0.f ? 0.f : 1.f / L;
@@ -474,7 +449,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
           // the item is the first share's last segment: its slot is 1 unless that share begins with the item
           const int slot0 = 2 * first + (total * first / shares == item_first ? 0 : 1);
           for (int row = y; row < ROWS; row += STEP) {
-            const int gr = r0 + row, tok = gr / c.G;
+            const int gr = r0 + row, tok = fast_div(gr, c.G, p.div_group);
             if (tok >= cu.r.n) break;
             float M = -INFINITY;
             for (int q = first; q <= last; ++q)
@@ -487,7 +462,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
               const long long at = (long long)(q == first ? slot0 : 2 * q) * ROWS + row;
               const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + at * 2));
               const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * DP + 4 * x));
-              const float g = pa_exp2(ml.x - base);
+              const float g = fast_exp2(ml.x - base);
               L += ml.y * g;
               acc.x += v.x * g; acc.y += v.y * g; acc.z += v.z * g; acc.w += v.w * g;
             }
@@ -538,10 +513,10 @@ int pa_launch(PaParams p, char* scratch, cudaStream_t st) {
 
 template <int DP>
 int pa_launch_rows(const PaParams& p, int wr, char* scratch, cudaStream_t st) {
-  constexpr int S1 = DP == 64 ? 4 : 3, S2 = DP == 64 ? 4 : 2, S4 = DP == 64 ? 3 : 2;
-  if (wr == 1) return pa_launch<DP, 1, S1>(p, scratch, st);
-  if (wr == 2) return pa_launch<DP, 2, S2>(p, scratch, st);
-  return pa_launch<DP, 4, S4>(p, scratch, st);
+  constexpr int S = DP == 64 ? 5 : 3;
+  if (wr == 1) return pa_launch<DP, 1, S>(p, scratch, st);
+  if (wr == 2) return pa_launch<DP, 2, S>(p, scratch, st);
+  return pa_launch<DP, 4, S>(p, scratch, st);
 }
 
 // Row tiles of 16, 32 or 64 rows.  The host knows rows only on average: G per new token, tokens / requests new tokens.
@@ -563,6 +538,8 @@ int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cu
   p.scale2 = c.scale * 1.4426950408889634f;
   p.narrow_rows = narrow_rows;
   p.min_units = 1;
+  p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
+  p.div_group = fast_div_magic((uint32_t)c.G);
   const int wr = pa_row_form(c);
   if (c.D <= 64) return pa_launch_rows<64>(p, wr, scratch, st);
   if (c.D <= 128) return pa_launch_rows<128>(p, wr, scratch, st);

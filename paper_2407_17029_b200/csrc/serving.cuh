@@ -83,6 +83,10 @@ constexpr size_t kPagedCounterBytes = kPagedMaxSms * kPagedMaxPerSm * 4;
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
 
+// The same for head sizes 64 and 128 with pages that fit its tiles (paged_warp.cu), same scratch.
+bool paged_warp_supported(const AttnCall& c);
+int launch_paged_warp(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
+
 // Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows.  `counters`:
 // kWideCounterBytes, zeroed on the stream; `scratch`: tc_attention_scratch_bytes.  `behind_narrow`: the kernel in front on the stream is
 // launch_paged_attention's of the same call, and this one may start beside it.
@@ -91,6 +95,9 @@ constexpr size_t kWideCounterBytes = 2 * kPagedMaxSms * 4;
 bool tc_attention_supported(const AttnCall& c);
 size_t tc_attention_scratch_bytes(int head_dim);
 int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, bool behind_narrow, cudaStream_t st);
+
+// TMA maps (CUtensorMap) of the cache's K and V.
+int make_cache_maps(const AttnCall& c, int box_keys, void* tm_k, void* tm_v);
 
 // General path: any head size up to 256, any page size.
 int launch_simt_attention(const AttnCall& c, cudaStream_t st);

@@ -157,7 +157,8 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   char* narrow_ws = wide_ws + kWideCounterBytes;
   QB_CUDA(cudaMemsetAsync(ws, 0, kStatusBytes + kWideCounterBytes + kPagedCounterBytes, st));
   if (force_general()) return launch_simt_attention(c, st);
-  const int rc = launch_paged_attention(c, wide ? kNarrowRows : 0x7fffffff, narrow_ws, st);
+  const int narrow = wide ? kNarrowRows : 0x7fffffff;
+  const int rc = paged_warp_supported(c) ? launch_paged_warp(c, narrow, narrow_ws, st) : launch_paged_attention(c, narrow, narrow_ws, st);
   if (rc || !wide) return rc;
   return launch_tc_attention(c, kNarrowRows, wide_ws, narrow_ws + paged_attention_scratch_bytes(c.D), true, st);
 }

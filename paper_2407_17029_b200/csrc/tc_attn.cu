@@ -696,13 +696,7 @@ int ta_launch(const TaParams& p0, char* counters, char* scratch, bool behind_nar
     const int rc = make_tensor_map_nd(&tq, 3, c.q, dims, pt, box);
     if (rc) return rc;
   }
-  const uint64_t dims[4] = {(uint64_t)D, (uint64_t)c.cache.page_size, (uint64_t)c.cache.kv_heads, (uint64_t)c.cache.n_pages};
-  const uint64_t pt[3] = {pitch(c.cache.page_size, c.cache.ts, D), pitch(c.cache.kv_heads, c.cache.hs, D),
-                          pitch(c.cache.n_pages, c.cache.ps, D)};
-  const uint32_t box[4] = {64, (uint32_t)p.box_keys, 1, 1};
-  int rc = make_tensor_map_nd(&tk, 4, c.cache.k, dims, pt, box);
-  if (rc) return rc;
-  rc = make_tensor_map_nd(&tv, 4, c.cache.v, dims, pt, box);
+  const int rc = make_cache_maps(c, p.box_keys, &tk, &tv);
   if (rc) return rc;
 
   cudaLaunchConfig_t cfg = {};
@@ -722,6 +716,17 @@ int ta_launch(const TaParams& p0, char* counters, char* scratch, bool behind_nar
 }
 
 }  // namespace
+
+// Boxes of 64 elements of a head x `box_keys` entries of a page.
+int make_cache_maps(const AttnCall& c, int box_keys, void* tm_k, void* tm_v) {
+  // a dimension of one entry may come with any stride: give the map one it accepts
+  auto pitch = [&](int64_t n, int64_t stride) { return (uint64_t)(n > 1 ? stride : c.D) * 2; };
+  const uint64_t dims[4] = {(uint64_t)c.D, (uint64_t)c.cache.page_size, (uint64_t)c.cache.kv_heads, (uint64_t)c.cache.n_pages};
+  const uint64_t pt[3] = {pitch(c.cache.page_size, c.cache.ts), pitch(c.cache.kv_heads, c.cache.hs), pitch(c.cache.n_pages, c.cache.ps)};
+  const uint32_t box[4] = {64, (uint32_t)box_keys, 1, 1};
+  const int rc = make_tensor_map_nd(tm_k, 4, c.cache.k, dims, pt, box);
+  return rc ? rc : make_tensor_map_nd(tm_v, 4, c.cache.v, dims, pt, box);
+}
 
 bool tc_attention_supported(const AttnCall& c) {
   if (c.D != 64 && c.D != 128) return false;
