@@ -13,8 +13,8 @@ __device__ __forceinline__ float fast_exp2(float x) {
 // or one more.
 __device__ __forceinline__ int fast_div(int x, int d, uint32_t m) {
   if (m == 0) return x;
-  const int q = (int)__umulhi((uint32_t)x, m);
-  return q * (long long)d > x ? q - 1 : q;
+  const uint32_t q = __umulhi((uint32_t)x, m);
+  return (int)(q * (uint32_t)d > (uint32_t)x ? q - 1 : q);   // q d <= x + d < 2^32
 }
 inline uint32_t fast_div_magic(uint32_t d) { return d == 1 ? 0u : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
 

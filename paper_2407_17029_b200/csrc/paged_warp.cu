@@ -16,7 +16,7 @@
 // results do not depend on timing.
 //
 // Entries behind a request's keys: whole pages are asked for at a page number past the cache, which TMA fills with zeros;
-// the rest of the last page is masked (scores set to -infinity, V words to zero).
+// the rest of the last page is masked (scores set to -infinity, V set to zero in shared memory).
 #include <cuda.h>
 
 #include <algorithm>
@@ -232,6 +232,14 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     };
     for (int s = 0; s < PW_STAGES && issued < units; ++s) issue(0);
 
+    // ldmatrix offsets of this lane: row and swizzled chunk pair i of a 128-byte span, for K (as it lies) and V (transposed)
+    uint32_t xk[4], xv[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int rk = (lane & 7) + ((lane >> 4) << 3), rv = lane & 15;
+      xk[i] = (uint32_t)(rk * 128 + (((2 * i + ((lane >> 3) & 1)) ^ (rk & 7)) << 4));
+      xv[i] = (uint32_t)(rv * 128 + (((2 * i + (lane >> 4)) ^ (rv & 7)) << 4));
+    }
     float o[MT][D / 8][4], m[MT][2], l[MT][2];
     uint32_t qf[MT == 1 ? D / 16 : 1][4];
     int r0 = 0, hi[MT][2], lo[MT][2];
@@ -287,7 +295,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int n = 0; n < NT; ++n) s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
-      const int krow = (lane & 7) + ((lane >> 4) << 3);        // row of the lane's ldmatrix address inside 16 keys
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint32_t qa[MT][4];
@@ -303,9 +310,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
 #pragma unroll
         for (int n2 = 0; n2 < NT / 2; ++n2) {
-          const uint32_t at = sk + (uint32_t)((k >> 2) * (KT * 128) + (n2 * 16 + krow) * 128 + (((2 * (k & 3) + ((lane >> 3) & 1)) ^ (krow & 7)) << 4));
           uint32_t kf[4];
-          frag_ldm4(kf, at);
+          frag_ldm4(kf, sk + xk[k & 3] + (uint32_t)((k >> 2) * (KT * 128) + n2 * 2048));
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
             frag_mma(s[t][2 * n2], qa[t], kf[0], kf[1]);
@@ -315,13 +321,10 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       const int k0 = cu.k.lo + cu.tile * KT;
       const bool partial = k0 + KT > cu.k.all_hi || k0 < cu.k.all_lo;
+      bool odd = false;                                    // a NaN or infinity in V of a tile with masked keys
+      if (partial) {
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][n][e] *= p.scale2;
-        if (partial) {
+        for (int t = 0; t < MT; ++t)
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -329,13 +332,34 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               const int j = k0 + n * 8 + 2 * (lane & 3) + (e & 1);
               if (j >= hi[t][e >> 1] || j < lo[t][e >> 1]) s[t][n][e] = -INFINITY;
             }
+        // 0 * NaN must not reach rows that do not see a key: V of keys that no row sees becomes zero, other NaNs and infinities
+        // are taken out and given back below
+#pragma unroll 1
+        for (int i = lane; i < Sh::KV_BYTES / 16; i += 32) {
+          const int key = k0 + (i >> 3) % KT;
+          uint32_t w[4];
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(sv + 16 * i) : "memory");
+          bool hit = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            hit |= bf16x2_odd(w[e]);
+            w[e] = key >= cu.k.hi ? 0u : bf16x2_clean(w[e]);
+          }
+          if (key >= cu.k.hi || hit) st_shared_v4(sv + 16 * i, w[0], w[1], w[2], w[3]);
+          odd |= hit && key < cu.k.hi;
         }
+        odd = __any_sync(0xffffffffu, odd);
+        fence_async_proxy();                               // before the slot's next copy
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
         float f[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float x = m[t][i];
+          float x = s[t][0][2 * i];
 #pragma unroll
           for (int n = 0; n < NT; ++n) x = fmaxf(x, fmaxf(s[t][n][2 * i], s[t][n][2 * i + 1]));
+          x = fmaxf(m[t][i], x * p.scale2);
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
           const float b_ = x == -INFINITY ? 0.f : x;       // nothing seen yet: all weights are 2^-inf = 0
@@ -344,8 +368,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           float sum = 0.f;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            s[t][n][2 * i] = fast_exp2(s[t][n][2 * i] - b_);
-            s[t][n][2 * i + 1] = fast_exp2(s[t][n][2 * i + 1] - b_);
+            s[t][n][2 * i] = fast_exp2(fmaf(s[t][n][2 * i], p.scale2, -b_));
+            s[t][n][2 * i + 1] = fast_exp2(fmaf(s[t][n][2 * i + 1], p.scale2, -b_));
             sum += s[t][n][2 * i] + s[t][n][2 * i + 1];
           }
           l[t][i] = l[t][i] * f[i] + sum;                  // this lane's part; joined over the quad at the end
@@ -355,7 +379,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           for (int n = 0; n < D / 8; ++n) { o[t][n][0] *= f[0]; o[t][n][1] *= f[0]; o[t][n][2] *= f[1]; o[t][n][3] *= f[1]; }
         }
       }
-      bool odd = false;                                    // a NaN or infinity in V of a tile with masked keys
 #pragma unroll
       for (int k = 0; k < KT / 16; ++k) {
         uint32_t a[MT][4];
@@ -366,28 +389,10 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           a[t][2] = pack_bf16x2(s[t][2 * k + 1][0], s[t][2 * k + 1][1]);
           a[t][3] = pack_bf16x2(s[t][2 * k + 1][2], s[t][2 * k + 1][3]);
         }
-        // words of keys that no row sees: zero
-        uint32_t keep[2] = {0xffffffffu, 0xffffffffu};
-        if (partial) {
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int j = k0 + k * 16 + 8 * i + 2 * (lane & 3);
-            keep[i] = j + 1 < cu.k.hi ? 0xffffffffu : j < cu.k.hi ? 0x0000ffffu : 0u;
-          }
-        }
 #pragma unroll
         for (int n2 = 0; n2 < D / 16; ++n2) {
-          const int row = k * 16 + (lane & 15);
           uint32_t vf[4];
-          frag_ldm4t(vf, sv + (uint32_t)((n2 >> 2) * (KT * 128) + row * 128 + (((2 * (n2 & 3) + (lane >> 4)) ^ (row & 7)) << 4)));
-          if (partial) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              vf[e] &= keep[e & 1];
-              odd |= bf16x2_odd(vf[e]);
-              vf[e] = bf16x2_clean(vf[e]);                 // 0 * NaN must not reach the rows that do not see the key
-            }
-          }
+          frag_ldm4t(vf, sv + xv[n2 & 3] + (uint32_t)((n2 >> 2) * (KT * 128) + k * 2048));
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
             frag_mma(o[t][2 * n2], a[t], vf[0], vf[1]);
@@ -395,16 +400,16 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           }
         }
       }
-      if (partial && __any_sync(0xffffffffu, odd)) {
-        // rare: give the values that were taken out back to the rows that see them
-        for (int kk = 0; kk < KT; ++kk) {
-          const int j = k0 + kk;
-          if (j >= cu.k.hi) break;
+      if (odd) {
+        // rare: the values that were taken out, read again, for the rows that see them
+        for (int j = max(k0, 0); j < min(k0 + KT, cu.k.hi); ++j) {
+          const int x = fast_div(j, c.cache.page_size, p.div_page), pg = __ldg(c.table + (long long)cu.b * c.width + x);
+          if (pg < 0 || pg >= c.cache.n_pages) continue;
+          const __nv_bfloat16* v = c.cache.v + (long long)pg * c.cache.ps + (long long)(j - x * c.cache.page_size) * c.cache.ts +
+                                   (long long)cu.h * c.cache.hs + 2 * (lane & 3);
 #pragma unroll
           for (int n = 0; n < D / 8; ++n) {
-            uint32_t w;
-            asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w)
-                         : "r"(sv + (uint32_t)((n >> 3) * (KT * 128) + kk * 128 + (((n & 7) ^ (kk & 7)) << 4) + 4 * (lane & 3))) : "memory");
+            const uint32_t w = *reinterpret_cast<const uint32_t*>(v + 8 * n);
             if (!bf16x2_odd(w)) continue;
             const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
 #pragma unroll
@@ -561,7 +566,7 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* sc
 static_assert(PW_WARPS <= kPagedMaxPerSm, "the scratch of paged_attn.cu holds this kernel's parts too");
 
 bool paged_warp_supported(const AttnCall& c) {
-  if (c.D != 64 && c.D != 128) return false;
+  if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f)) return false;
   const int kt = c.D == 64 ? 64 : 32, pg = c.cache.page_size;
   // a tile is whole boxes of one page each; at most 32 boxes, one per lane
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);
