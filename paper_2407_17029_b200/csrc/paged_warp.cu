@@ -5,15 +5,16 @@
 // a key head); partial triples (maximum, sum, weighted values) over disjoint keys join in any grouping.
 //
 // What bounds it: the cache's bytes, so each warp is made to need little else.  All key tiles of all items (request,
-// key head, row tile) are put in one line and cut into equal shares, one per WARP.  A warp streams its share through a ring
-// of its own -- lane i issues box i of a tile as the ring's slot becomes free, nothing waits for another warp -- and
-// does both products for the whole tile, so a tile costs a warp one wait, one maximum and one rescale.  (With the four
-// warps of a CTA sharing each tile, a 64-key tile cost 2160 warp instructions instead of about 500, and the kernel
-// was bound by them: 4.5 TB/s.)  In flight per SM: 4 warps x 3 slots x 16 KB.
+// key head, row tile) are put in one line and cut into shares.  Every warp starts with one share and then takes the
+// next one that nobody has taken, the later ones shorter: SMs do not get equal parts of a saturated memory (with one equal share per warp the
+// slowest CTA of a 1 GB call ended 20 % after the median).  A warp streams its shares through a ring of its own -- lane i
+// issues box i of a tile as the ring's slot becomes free, across the borders of items and shares, and nothing waits for
+// another warp -- and does both products for the whole tile, so a tile costs a warp one wait, one maximum and one rescale.
+// In flight per SM: 8 warps x 3 slots x 8 KB.
 //
-// An item cut by a share's border leaves partial triples in the workspace; when all warps of a CTA are done it joins
-// the items that lie within its own shares, and of the items that reach into other CTAs those that it finished last, in share order:
-// results do not depend on timing.
+// An item cut by a share's border leaves partial triples in the workspace, which a second kernel joins in share order:
+// results do not depend on timing.  (Joined by whichever warp came last, the joins of a call fell to the few warps that ended
+// last, one row after the other: 5 to 65 us at the end of a 45 to 180 us call.)
 //
 // Entries behind a request's keys: whole pages are asked for at a page number past the cache, which TMA fills with zeros;
 // the rest of the last page is masked (scores set to -infinity, V set to zero in shared memory).
@@ -31,31 +32,38 @@ namespace qb {
 using namespace ptx;
 namespace {
 
-constexpr int PW_WARPS = 4, PW_THREADS = PW_WARPS * 32;
-constexpr int PW_STAGES = 3;
+constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
+constexpr int PW_MAX_LEVELS = kPagedSharesPerWarp;
+constexpr int PW_FINE = 8;       // key tiles of the shortest shares
 constexpr float PW_LN2 = 0.69314718055994530942f;
 
 template <int D, int MT>
 struct PwShape {
   static constexpr int ROWS = 16 * MT;
-  static constexpr int KT = D == 64 ? 64 : 32;            // keys per tile: 16 KB of K and V
+  static constexpr int KT = D == 64 ? 32 : 16;            // keys per tile: 8 KB of K and V
+  static constexpr int STAGES = MT == 1 ? 3 : 2;
   static constexpr int KV_BYTES = KT * D * 2;
   static constexpr int STAGE = 2 * KV_BYTES;
   static constexpr int Q_BYTES = MT == 1 ? 0 : ROWS * D * 2;   // per warp; one row tile's queries stay in registers
-  static constexpr int WARP_BYTES = PW_STAGES * STAGE + Q_BYTES;
+  static constexpr int WARP_BYTES = STAGES * STAGE + Q_BYTES;
   static constexpr int SMEM = PW_WARPS * WARP_BYTES + 1024;
 };
+
+// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i).
+struct PwCut { long long slot0, first; int n, t0, r0, rows, h, pad; };
+static_assert(sizeof(PwCut) == kPagedCutBytes, "scratch layout");
 
 struct PwParams {
   AttnCall c;
   float scale2;              // scale * log2 e
   int narrow_rows;           // requests with more rows than this belong to the tcgen05 kernel
-  int min_units;             // a share has at least so many key tiles
+  int max_levels;            // of shares, at most PW_MAX_LEVELS
   int box_keys;              // keys per TMA box: min(page_size, KT)
   uint32_t div_page, div_group;
   uint32_t zero;             // 0, but not to the compiler
   long long wait_limit;
-  uint32_t* counters;        // [grid], zeroed
+  uint32_t* counters;        // [0]: shares taken; [1 + g]: share g begins inside an item, and is the first that does.  Zeroed
+  PwCut* cuts;               // [shares] that item
   float* part_o;             // [2 * shares][ROWS][D]
   float* part_ml;            // [2 * shares][ROWS][2]
 };
@@ -107,22 +115,88 @@ struct PwCursor {
   }
 };
 
-// An item that the shares of a CTA cut.
-struct PwCut { int valid, b, h, rt, first_cta, last_cta; long long first_unit; int tiles; };
+// Joins the parts of cut items: eight share borders per CTA, whose cut items all its warps work on, RB rows x PB parts of a
+// row at a time in flight per warp, D / 4 lanes a row.
+constexpr int PJ_THREADS = 256, PJ_CUTS = 8;
+template <int D, int ROWS, int RB, int PB>
+__device__ __forceinline__ void pw_join_block(const PwParams& p, const PwCut& x) {
+  constexpr int LANES = D / 4, STEP = 32 / LANES;          // a warp has STEP rows at a time, RB deep
+  const AttnCall& c = p.c;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = (lane % LANES) * 4;
+  for (int rb = warp * RB * STEP; rb < x.rows; rb += (PJ_THREADS / 32) * RB * STEP) {
+    const int row0 = rb + lane / LANES;                    // this lane's rows: row0 + STEP r
+    float M[RB], L[RB];
+    float4 acc[RB];
+#pragma unroll
+    for (int r = 0; r < RB; ++r) { M[r] = -INFINITY; L[r] = 0.f; acc[r] = make_float4(0.f, 0.f, 0.f, 0.f); }
+    for (int i0 = 0; i0 < x.n; i0 += PB) {
+      float2 ml[RB][PB];
+      float4 v[RB][PB];
+#pragma unroll
+      for (int r = 0; r < RB; ++r)
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+          ml[r][i] = make_float2(-INFINITY, 0.f);
+          v[r][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          const int k = i0 + i, row = row0 + STEP * r;
+          if (k < x.n && row < x.rows) {
+            const long long at = (k == 0 ? x.slot0 : 2 * (x.first + k)) * ROWS + row;
+            ml[r][i] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + at * 2));
+            v[r][i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + col));
+          }
+        }
+#pragma unroll
+      for (int r = 0; r < RB; ++r) {
+        float mn = M[r];
+#pragma unroll
+        for (int i = 0; i < PB; ++i) mn = fmaxf(mn, ml[r][i].x);
+        const float b = mn == -INFINITY ? 0.f : mn, f = fast_exp2(M[r] - b);
+        M[r] = mn;
+        L[r] *= f; acc[r].x *= f; acc[r].y *= f; acc[r].z *= f; acc[r].w *= f;
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+          const float g = fast_exp2(ml[r][i].x - b);
+          L[r] += ml[r][i].y * g;
+          acc[r].x += v[r][i].x * g; acc[r].y += v[r][i].y * g; acc[r].z += v[r][i].z * g; acc[r].w += v[r][i].w * g;
+        }
+      }
+    }
+#pragma unroll
+    for (int r = 0; r < RB; ++r) {
+      const int row = row0 + STEP * r;
+      if (row >= x.rows) continue;
+      const int gr = x.r0 + row, tok = fast_div(gr, c.G, p.div_group), head = x.h * c.G + gr - tok * c.G;
+      const float inv = L[r] == 0.f ? 0.f : 1.f / L[r];
+      *reinterpret_cast<uint2*>(c.out + (long long)(x.t0 + tok) * c.o_ts + (long long)head * c.o_hs + col) =
+          make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
+      if (c.lse && col == 0) c.lse[(long long)(x.t0 + tok) * c.H + head] = L[r] == 0.f ? -INFINITY : (M[r] + log2f(L[r])) * PW_LN2;
+    }
+  }
+}
+template <int D, int ROWS>
+__global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const __grid_constant__ PwParams p) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
+  const int g0 = blockIdx.x * PJ_CUTS;
+  for (int i = 0; i < PJ_CUTS; ++i) {
+    if (!__ldcg(p.counters + 1 + g0 + i)) continue;
+    const PwCut x = p.cuts[g0 + i];
+    if (x.n <= 4) pw_join_block<D, ROWS, 2, 4>(p, x);
+    else pw_join_block<D, ROWS, 1, 16>(p, x);
+  }
+}
 
 template <int D, int MT>
 __global__ void __launch_bounds__(PW_THREADS, 1)
 paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ PwParams p) {
   using Sh = PwShape<D, MT>;
-  constexpr int ROWS = Sh::ROWS, KT = Sh::KT, HALVES = D / 64, NT = KT / 8;
+  constexpr int ROWS = Sh::ROWS, KT = Sh::KT, HALVES = D / 64, NT = KT / 8, PW_STAGES = Sh::STAGES;
   using Cursor = PwCursor<ROWS, KT>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[PW_WARPS * PW_STAGES];
-  __shared__ long long s_scan[PW_WARPS];
-  __shared__ int s_start_b[PW_WARPS];
-  __shared__ long long s_start_u[PW_WARPS];
-  __shared__ PwCut s_cut[PW_WARPS + 1];
-  __shared__ int s_ready[PW_WARPS + 1];
+  __shared__ long long s_scan[PW_WARPS], s_units[PW_THREADS];
+  __shared__ long long s_base[PW_MAX_LEVELS + 1], s_each[PW_MAX_LEVELS];
+  __shared__ Cursor s_next[PW_WARPS];          // where the next share of each warp begins
   const AttnCall& c = p.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -135,8 +209,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   if (lane == 0) {
     for (int s = 0; s < PW_STAGES; ++s) mbar_init(full + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    s_cut[warp + 1].valid = 0;
-    if (warp == 0) s_cut[0].valid = 0;
   }
 
   // ---- the line: units before each request, all units, the shares -----------------------------------------------------
@@ -161,49 +233,78 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     if (w < warp) incl += s_scan[w];
     total += s_scan[w];
   }
-  const long long shares = min((long long)gridDim.x * PW_WARPS, max(1LL, total / p.min_units));
-  auto share_begin = [&](long long g) { return total * g / shares; };
-  const long long g0 = (long long)blockIdx.x * PW_WARPS;
-  if (total == 0 || g0 >= shares) return;
-  for (int w = 0; w < PW_WARPS; ++w) {
-    if (g0 + w >= shares) break;
-    const long long u0 = share_begin(g0 + w);
-    if (incl - mine <= u0 && u0 < incl) {   // one thread of the CTA: the request that holds unit u0
-      long long u = incl - mine;
-      int b = b_lo;
-      for (;; ++b) {
-        const ReqView r = attn_request(c, b);
-        if (!pw_mine(p, r)) continue;
-        const long long n = (long long)pw_head_units<ROWS, KT>(p, r) * c.cache.kv_heads;
-        if (u0 < u + n) break;
-        u += n;
-      }
-      s_start_b[w] = b;
-      s_start_u[w] = u0 - u;
+  s_units[tid] = incl;
+  __syncthreads();
+  // Shares: level k hands every warp one share; the levels' parts of the line are 1/2, 1/4, ... with the last two equal, so
+  // the shares that are taken late are short.  A share has more tiles than the ring has slots (then at most one share's
+  // beginning is in the ring besides the current one).
+  const long long per_level = min((long long)gridDim.x * PW_WARPS, max(1LL, total / (PW_STAGES + 1)));
+  int levels = 1;
+  while (levels < p.max_levels && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
+  const long long shares = per_level * levels;
+  if (tid == 0) {
+    long long at = 0;
+    for (int k = 0; k < levels; ++k) {
+      s_base[k] = at;
+      s_each[k] = k + 1 < levels ? (total >> (k + 1)) / per_level : (total - at) / per_level;
+      at += s_each[k] * per_level;
     }
+    s_base[levels] = total;
   }
   __syncthreads();
-  const long long g = g0 + warp;
-  const long long u0 = g < shares ? share_begin(g) : 0, u1 = g < shares ? share_begin(g + 1) : 0;
-  const int units = (int)(u1 - u0);
+  // of the last level, the first `extra` shares have one tile more
+  const long long last_each = s_each[levels - 1], extra = total - s_base[levels - 1] - last_each * per_level;
+  auto share_begin = [&](long long g) -> long long {
+    if (g >= shares) return total;
+    const int k = (int)(g / per_level);
+    const long long i = g - k * per_level;
+    return s_base[k] + i * s_each[k] + (k + 1 == levels ? min(i, extra) : 0);
+  };
+  auto share_of = [&](long long u) {
+    int k = 0;
+    while (k + 1 < levels && u >= s_base[k + 1]) ++k;
+    const long long v = u - s_base[k], each = s_each[k];
+    if (k + 1 < levels) return k * per_level + v / each;
+    const long long cut = extra * (each + 1);
+    return k * per_level + (v < cut ? v / (each + 1) : extra + (v - cut) / each);
+  };
+  const long long g_first = (long long)blockIdx.x * PW_WARPS + warp;
+  if (total == 0 || g_first >= per_level) return;
+
+  // the cursor of unit u: a search over the threads' sums, a walk over that thread's requests
+  auto locate = [&](Cursor& at, long long u) {
+    int a = 0, e = PW_THREADS;
+    while (a < e) { const int x = (a + e) >> 1; if (s_units[x] > u) e = x; else a = x + 1; }
+    long long rest = u - (a ? s_units[a - 1] : 0);
+    int hu = 1;
+    for (at.b = a * per;; ++at.b) {
+      at.r = attn_request(c, at.b);
+      if (!pw_mine(p, at.r)) continue;
+      hu = pw_head_units<ROWS, KT>(p, at.r);
+      if (rest < (long long)hu * c.cache.kv_heads) break;
+      rest -= (long long)hu * c.cache.kv_heads;
+    }
+    at.h = (int)(rest >> 31 ? rest / hu : (long long)((uint32_t)rest / (uint32_t)hu));
+    int left = (int)(rest - (long long)at.h * hu);
+    at.nrt = pw_row_tiles<ROWS>(p, at.r);
+    at.rt = 0;
+    at.k = pw_range<ROWS, KT>(p, at.r, 0);
+    while (left >= at.k.tiles) { left -= at.k.tiles; ++at.rt; at.k = pw_range<ROWS, KT>(p, at.r, at.rt); }
+    at.tile = left;
+  };
 
   bool ok = true;
   int odd_pages = 0;
-  if (units > 0) {
+  {
+    long long g = g_first, u0 = share_begin(g), u1 = share_begin(g + 1);   // the share being computed
+    long long g_next = 0;                                                  // lane 0: the share after it
+    if (lane == 0 && levels > 1) g_next = (long long)atomicAdd(p.counters, 1u) + per_level;
+    else g_next = shares;
     Cursor ld;
-    ld.b = s_start_b[warp];
-    ld.r = attn_request(c, ld.b);
-    ld.nrt = pw_row_tiles<ROWS>(p, ld.r);
-    {
-      const int hu = pw_head_units<ROWS, KT>(p, ld.r);
-      ld.h = (int)(s_start_u[warp] / hu);
-      int rest = (int)(s_start_u[warp] - (long long)ld.h * hu);
-      ld.rt = 0;
-      ld.k = pw_range<ROWS, KT>(p, ld.r, 0);
-      while (rest >= ld.k.tiles) { rest -= ld.k.tiles; ++ld.rt; ld.k = pw_range<ROWS, KT>(p, ld.r, ld.rt); }
-      ld.tile = rest;
-    }
+    locate(ld, u0);
     Cursor cu = ld;
+    int ld_left = (int)(u1 - u0);            // tiles of the share being loaded that are not issued yet
+    long long ld_next_g = -1;                // the share being loaded, where that is the one after g; `shares` or more: none left
 
     // ---- loads: lane i issues box i: (K or V, half of the head, run of keys) ------------------------------------------
     const int runs = KT / p.box_keys;                 // boxes along the keys
@@ -218,19 +319,33 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       entry = key - j * c.cache.page_size;
       return __ldg(c.table + (long long)ld.b * c.width + j);
     };
-    int issued = 0, entry, page = lookup(entry), st_ld = 0;
+    uint32_t issued = 0, done = 0;
+    int entry, page = lookup(entry), st_ld = 0;
     auto issue = [&](uint32_t dep) {
       if (page < 0 || page > c.cache.n_pages) { odd_pages = 1; page = c.cache.n_pages; }
-      const bool past = page == c.cache.n_pages && ld.k.lo + ld.tile * KT + my_run * p.box_keys < ld.k.hi;
-      if (lane < n_boxes && past) odd_pages = 1;
+      if (lane < n_boxes && page == c.cache.n_pages && ld.k.lo + ld.tile * KT + my_run * p.box_keys < ld.k.hi) odd_pages = 1;
       if (lane == 0) mbar_arrive_expect_tx(full + 8 * st_ld, Sh::STAGE);
       __syncwarp();
       if (lane < n_boxes)
         tma_load_4d(ring + st_ld * Sh::STAGE + my_dst + dep, my_kv ? &tm_v : &tm_k, full + 8 * st_ld, my_half * 64, entry, ld.h, page);
       if (++st_ld == PW_STAGES) st_ld = 0;
-      if (++issued < units) { ld.next(p); page = lookup(entry); }
+      ++issued;
+      if (--ld_left > 0) ld.next(p);
+      else {
+        ld_next_g = __shfl_sync(0xffffffffu, g_next, 0);
+        if (ld_next_g >= shares) return;                       // ld_left stays 0: nothing more to issue
+        const long long b0 = share_begin(ld_next_g);
+        locate(ld, b0);
+        ld_left = (int)(share_begin(ld_next_g + 1) - b0);
+        if (lane == 0) {
+          s_next[warp] = ld;
+          g_next = (long long)atomicAdd(p.counters, 1u) + per_level;
+        }
+        __syncwarp();
+      }
+      page = lookup(entry);
     };
-    for (int s = 0; s < PW_STAGES && issued < units; ++s) issue(0);
+    for (int s = 0; s < PW_STAGES && ld_left > 0; ++s) issue(0);
 
     // ldmatrix offsets of this lane: row and swizzled chunk pair i of a 128-byte span, for K (as it lies) and V (transposed)
     uint32_t xk[4], xv[4];
@@ -245,10 +360,23 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     int r0 = 0, hi[MT][2], lo[MT][2];
     int stage = 0;
     uint32_t ph = 0;
-    bool first_segment = true;
+    bool first_segment = true, fresh = true;     // of the share; of the item
+    long long u = u0;                            // the tile being computed
 
-    for (int it = 0; it < units; ++it) {
-      if (it == 0 || cu.tile == 0) {
+    while (true) {
+      if (fresh) {
+        fresh = false;
+        if (first_segment && cu.tile > 0 && lane == 0) {
+          // this share begins inside an item: the first share that does tells the join kernel about it
+          const long long item_first = u0 - cu.tile, first = g - 1;
+          if (share_begin(first) <= item_first) {
+            const int n = (int)(share_of(item_first + cu.k.tiles - 1) - first) + 1;
+            // its first part is the first share's last segment (slot 1) unless that share begins with the item; the others' first (slot 0)
+            p.cuts[g] = PwCut{2 * first + (share_begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
+                              min(ROWS, cu.r.n * c.G - cu.rt * ROWS), cu.h, 0};
+            p.counters[1 + g] = 1;
+          }
+        }
         r0 = cu.rt * ROWS;
 #pragma unroll
         for (int t = 0; t < MT; ++t)
@@ -289,12 +417,41 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, ph, c.status, p.wait_limit))) { ok = false; break; }
       const uint32_t sk = ring + stage * Sh::STAGE, sv = sk + Sh::KV_BYTES;
 
-      // scores: fragment n covers keys 8 n .. 8 n + 7 (lane: rows lane / 4 and + 8, keys 2 (lane % 4) + {0, 1})
-      float s[MT][NT][4];
+      const int k0 = cu.k.lo + cu.tile * KT;
+      const bool partial = k0 + KT > cu.k.all_hi || k0 < cu.k.all_lo;
+      bool odd = false;                                    // a NaN or infinity in V of a tile with masked keys
+      if (partial) {
+        // 0 * NaN must not reach rows that do not see a key: V of keys that no row sees becomes zero, other NaNs and infinities
+        // are taken out and given back below
+#pragma unroll 1
+        for (int i = lane; i < Sh::KV_BYTES / 16; i += 32) {
+          const int key = k0 + (i >> 3) % KT;
+          uint32_t w[4];
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(sv + 16 * i) : "memory");
+          bool hit = false;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            hit |= bf16x2_odd(w[e]);
+            w[e] = key >= cu.k.hi ? 0u : bf16x2_clean(w[e]);
+          }
+          if (key >= cu.k.hi || hit) st_shared_v4(sv + 16 * i, w[0], w[1], w[2], w[3]);
+          odd |= hit && key < cu.k.hi;
+        }
+        odd = __any_sync(0xffffffffu, odd);
+        fence_async_proxy();                               // before the slot's next copy
+      }
+
+      // scores: fragment n covers keys 8 n .. 8 n + 7 (lane: rows lane / 4 and + 8, keys 2 (lane % 4) + {0, 1}); with few
+      // fragments, even and odd steps of the contraction are summed apart, so that an MMA does not wait for the one before
+      constexpr int SPLIT = MT * NT < 4 ? 2 : 1;
+      float s[MT][NT][4], s2[SPLIT == 2 ? MT : 1][SPLIT == 2 ? NT : 1][4];
 #pragma unroll
       for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+        for (int n = 0; n < NT; ++n) {
+          s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
+          if (SPLIT == 2) s2[t][n][0] = s2[t][n][1] = s2[t][n][2] = s2[t][n][3] = 0.f;
+        }
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
         uint32_t qa[MT][4];
@@ -314,14 +471,30 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
           frag_ldm4(kf, sk + xk[k & 3] + (uint32_t)((k >> 2) * (KT * 128) + n2 * 2048));
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
-            frag_mma(s[t][2 * n2], qa[t], kf[0], kf[1]);
-            frag_mma(s[t][2 * n2 + 1], qa[t], kf[2], kf[3]);
+            if (SPLIT == 2 && (k & 1)) {
+              frag_mma(s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? 2 * n2 : 0], qa[t], kf[0], kf[1]);
+              frag_mma(s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? 2 * n2 + 1 : 0], qa[t], kf[2], kf[3]);
+            } else {
+              frag_mma(s[t][2 * n2], qa[t], kf[0], kf[1]);
+              frag_mma(s[t][2 * n2 + 1], qa[t], kf[2], kf[3]);
+            }
           }
         }
       }
-      const int k0 = cu.k.lo + cu.tile * KT;
-      const bool partial = k0 + KT > cu.k.all_hi || k0 < cu.k.all_lo;
-      bool odd = false;                                    // a NaN or infinity in V of a tile with masked keys
+      // V's fragments are on their way during the softmax
+      uint32_t vf[KT / 16][D / 16][4];
+#pragma unroll
+      for (int k = 0; k < KT / 16; ++k)
+#pragma unroll
+        for (int n2 = 0; n2 < D / 16; ++n2) frag_ldm4t(vf[k][n2], sv + xv[n2 & 3] + (uint32_t)((n2 >> 2) * (KT * 128) + k * 2048));
+      if (SPLIT == 2) {
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[t][n][e] += s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? n : 0][e];
+      }
       if (partial) {
 #pragma unroll
         for (int t = 0; t < MT; ++t)
@@ -332,24 +505,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               const int j = k0 + n * 8 + 2 * (lane & 3) + (e & 1);
               if (j >= hi[t][e >> 1] || j < lo[t][e >> 1]) s[t][n][e] = -INFINITY;
             }
-        // 0 * NaN must not reach rows that do not see a key: V of keys that no row sees becomes zero, other NaNs and infinities
-        // are taken out and given back below
-#pragma unroll 1
-        for (int i = lane; i < Sh::KV_BYTES / 16; i += 32) {
-          const int key = k0 + (i >> 3) % KT;
-          uint32_t w[4];
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(sv + 16 * i) : "memory");
-          bool hit = false;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            hit |= bf16x2_odd(w[e]);
-            w[e] = key >= cu.k.hi ? 0u : bf16x2_clean(w[e]);
-          }
-          if (key >= cu.k.hi || hit) st_shared_v4(sv + 16 * i, w[0], w[1], w[2], w[3]);
-          odd |= hit && key < cu.k.hi;
-        }
-        odd = __any_sync(0xffffffffu, odd);
-        fence_async_proxy();                               // before the slot's next copy
       }
 #pragma unroll
       for (int t = 0; t < MT; ++t) {
@@ -391,12 +546,10 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
 #pragma unroll
         for (int n2 = 0; n2 < D / 16; ++n2) {
-          uint32_t vf[4];
-          frag_ldm4t(vf, sv + xv[n2 & 3] + (uint32_t)((n2 >> 2) * (KT * 128) + k * 2048));
 #pragma unroll
           for (int t = 0; t < MT; ++t) {
-            frag_mma(o[t][2 * n2], a[t], vf[0], vf[1]);
-            frag_mma(o[t][2 * n2 + 1], a[t], vf[2], vf[3]);
+            frag_mma(o[t][2 * n2], a[t], vf[k][n2][0], vf[k][n2][1]);
+            frag_mma(o[t][2 * n2 + 1], a[t], vf[k][n2][2], vf[k][n2][3]);
           }
         }
       }
@@ -425,7 +578,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       // The slot is free when every lane's fragments have been read.  Each was an operand of an MMA whose result is in o, so
       // the copy's address is made to depend on all of o: it cannot be issued while a load is still on its way.
-      if (issued < units) {
+      ++done;
+      if (ld_left > 0) {
         uint32_t dep = 0;
 #pragma unroll
         for (int n = 0; n < D / 8; ++n) dep |= __float_as_uint(o[0][n][0]);
@@ -435,8 +589,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (++stage == PW_STAGES) { stage = 0; ph ^= 1u; }
 
       // ---- end of an item, or of this share's part of it --------------------------------------------------------------
-      if (cu.tile + 1 == cu.k.tiles || it + 1 == units) {
-        const long long item_first = u0 + it - cu.tile;
+      if (cu.tile + 1 == cu.k.tiles || u + 1 == u1) {
+        const long long item_first = u - cu.tile;
         const bool whole = item_first >= u0 && item_first + cu.k.tiles <= u1;
         const long long slot = 2 * g + (first_segment ? 0 : 1);
 #pragma unroll
@@ -464,77 +618,24 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
               if ((lane & 3) == 0) *reinterpret_cast<float2*>(p.part_ml + (slot * ROWS + row) * 2) = make_float2(m[t][i], sum);
             }
           }
-        if (!whole && lane == 0) {
-          // of the warps of a CTA, the first that holds a part announces the item
-          const bool opens = item_first >= u0, enters = warp == 0 && first_segment && item_first < u0;
-          if (opens || enters) {
-            PwCut& x = s_cut[enters ? 0 : warp + 1];
-            x.valid = 1; x.b = cu.b; x.h = cu.h; x.rt = cu.rt; x.first_unit = item_first; x.tiles = cu.k.tiles;
-          }
-        }
         first_segment = false;
+        fresh = true;
       }
-      cu.next(p);
+      if (++u < u1) { cu.next(p); continue; }
+      // the next share: its tiles are on their way already
+      if (ld_next_g < 0 || ld_next_g >= shares) break;
+      g = ld_next_g;
+      ld_next_g = -1;
+      u = u0 = share_begin(g);
+      u1 = share_begin(g + 1);
+      cu = s_next[warp];
+      first_segment = fresh = true;
     }
     if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
-      for (int j = max(0, issued - PW_STAGES); j < issued; ++j)
-        mbar_wait(full + 8 * (j % PW_STAGES), (uint32_t)(j / PW_STAGES) & 1u, c.status, p.wait_limit);
+      for (uint32_t j = done; j < issued; ++j) mbar_wait(full + 8 * (j % PW_STAGES), (j / PW_STAGES) & 1u, c.status, p.wait_limit);
     }
     if (__any_sync(0xffffffffu, odd_pages) && lane == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
-  }
 
-  // ---- joins ------------------------------------------------------------------------------------------------------------
-  __threadfence();
-  __syncthreads();
-  auto share_of = [&](long long u) {
-    long long x = u * shares / total;
-    while (share_begin(x + 1) <= u) ++x;
-    while (share_begin(x) > u) --x;
-    return x;
-  };
-  if (tid <= PW_WARPS) {
-    PwCut& x = s_cut[tid];
-    int ready = 0;
-    if (x.valid) {
-      x.first_cta = (int)(share_of(x.first_unit) / PW_WARPS);
-      x.last_cta = (int)(share_of(x.first_unit + x.tiles - 1) / PW_WARPS);
-      // at most one item leaves a CTA's shares at their end: the counter of the CTA it starts in is its own
-      ready = x.first_cta == x.last_cta || atomicAdd(p.counters + x.first_cta, 1u) == (uint32_t)(x.last_cta - x.first_cta);
-    }
-    s_ready[tid] = ready;
-  }
-  __syncthreads();
-  __threadfence();
-  constexpr int LANES = D / 4;                            // lanes per row (16 or 32), four columns each
-  for (int w = 0; w <= PW_WARPS; ++w) {
-    if (!s_ready[w]) continue;
-    const PwCut x = s_cut[w];
-    const ReqView r = attn_request(c, x.b);
-    const long long first = share_of(x.first_unit), last = share_of(x.first_unit + x.tiles - 1);
-    const long long slot0 = 2 * first + (share_begin(first) == x.first_unit ? 0 : 1);
-    const int r0 = x.rt * ROWS, rows = min(ROWS, r.n * c.G - r0), col = (tid % LANES) * 4;
-    for (int row = tid / LANES; row < rows; row += PW_THREADS / LANES) {
-      const int gr = r0 + row, tok = fast_div(gr, c.G, p.div_group), head = x.h * c.G + gr - tok * c.G;
-      // one pass: the running maximum moves along with the parts
-      float M = -INFINITY, L = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-      for (long long q = first; q <= last; ++q) {
-        const long long at = (q == first ? slot0 : 2 * q) * ROWS + row;
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + at * 2));
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + col));
-        const float mn = fmaxf(M, ml.x), b_ = mn == -INFINITY ? 0.f : mn;
-        const float fa = fast_exp2(M - b_), fb = fast_exp2(ml.x - b_);
-        M = mn;
-        L = L * fa + ml.y * fb;
-        acc.x = acc.x * fa + v.x * fb; acc.y = acc.y * fa + v.y * fb;
-        acc.z = acc.z * fa + v.z * fb; acc.w = acc.w * fa + v.w * fb;
-      }
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      *reinterpret_cast<uint2*>(c.out + (long long)(r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + col) =
-          make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
-      if (c.lse && col == 0) c.lse[(long long)(r.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * PW_LN2;
-    }
   }
 }
 
@@ -552,22 +653,33 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* sc
   }
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int grid = std::min(sms, kPagedMaxSms);
+  p.max_levels = PW_MAX_LEVELS / MT;      // the scratch holds as many rows for either form
   p.counters = reinterpret_cast<uint32_t*>(scratch);
   p.part_ml = reinterpret_cast<float*>(scratch + kPagedCounterBytes);
-  p.part_o = p.part_ml + (size_t)2 * kPagedMaxSms * PW_WARPS * Sh::ROWS * 2;
+  p.part_o = p.part_ml + (size_t)2 * kPagedMaxShares * Sh::ROWS * 2 / MT;
+  p.cuts = reinterpret_cast<PwCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D / MT);
   kernel<<<grid, PW_THREADS, Sh::SMEM, st>>>(tk, tv, p);
-  count_launch();
   QB_CUDA(cudaGetLastError());
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((grid * PW_WARPS * p.max_levels + PJ_CUTS - 1) / PJ_CUTS));
+  cfg.blockDim = dim3(PJ_THREADS);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D, Sh::ROWS>, p));
+  count_launch(2);
   return QBLORA_OK;
 }
 
 }  // namespace
 
-static_assert(PW_WARPS <= kPagedMaxPerSm, "the scratch of paged_attn.cu holds this kernel's parts too");
+static_assert(PW_WARPS == kPagedWarps, "shares per SM");
 
 bool paged_warp_supported(const AttnCall& c) {
   if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f)) return false;
-  const int kt = c.D == 64 ? 64 : 32, pg = c.cache.page_size;
+  const int kt = c.D == 64 ? 32 : 16, pg = c.cache.page_size;
   // a tile is whole boxes of one page each; at most 32 boxes, one per lane
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);
 }
@@ -577,8 +689,7 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* scratch, cudaStr
   p.c = c;
   p.scale2 = c.scale * 1.4426950408889634f;
   p.narrow_rows = narrow_rows;
-  p.min_units = 2;
-  p.box_keys = std::min(c.cache.page_size, c.D == 64 ? 64 : 32);
+  p.box_keys = std::min(c.cache.page_size, c.D == 64 ? 32 : 16);
   p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
   p.div_group = fast_div_magic((uint32_t)c.G);
   p.wait_limit = wait_limit_cycles();

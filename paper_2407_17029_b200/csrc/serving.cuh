@@ -79,7 +79,9 @@ __device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.wind
 // Few rows per key head (paged_attn.cu): requests of at most `narrow_rows` rows (new tokens * G).  `scratch`:
 // paged_attention_scratch_bytes, its first kPagedCounterBytes zeroed on the stream before the launch.
 constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;
-constexpr size_t kPagedCounterBytes = kPagedMaxSms * kPagedMaxPerSm * 4;
+constexpr int kPagedWarps = 8, kPagedSharesPerWarp = 4;     // of paged_warp.cu
+constexpr int kPagedMaxShares = kPagedMaxSms * kPagedWarps * kPagedSharesPerWarp;
+constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256, kPagedCutBytes = 40;
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
 
