@@ -1,5 +1,4 @@
-// Attention over the paged cache for few rows per key head (decoding, drafted tokens), and for the head and page sizes that
-// the tcgen05 kernel does not take.
+// Attention over the paged cache for the head sizes, page sizes and scales that paged_warp.cu and tc_attn.cu do not take.
 //
 // Mathematics.  A tile is ROWS = 16 WR rows of one request and one key head: row r is token r / G, query head r % G of the
 // group that shares the key head, so shared keys are read once for all of them.  Keys are taken 64 at a time with the
@@ -34,7 +33,6 @@ constexpr float PA_LN2 = 0.69314718055994530942f;
 struct PaParams {
   AttnCall c;
   float scale2;         // scale * log2 e
-  int narrow_rows;      // requests with more rows (new tokens * G) than this belong to the tcgen05 kernel
   int min_units;        // key tiles per share below which fewer shares are made
   uint32_t div_page, div_group;   // 2^32 / divisor, rounded up (fast_div)
   uint32_t* counters;   // [grid] zeroed before the launch
@@ -65,7 +63,7 @@ __device__ __forceinline__ PaRange pa_range(const PaParams& p, const ReqView& r,
 }
 template <int ROWS>
 __device__ __forceinline__ bool pa_mine(const PaParams& p, const ReqView& r) {
-  return r.n > 0 && (long long)r.n * p.c.G <= p.narrow_rows;
+  return r.n > 0;
 }
 template <int ROWS>
 __device__ __forceinline__ int pa_row_tiles(const PaParams& p, const ReqView& r) { return (r.n * p.c.G + ROWS - 1) / ROWS; }
@@ -125,8 +123,6 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
   const int wr = warp / WK, wk = warp % WK;
   const uint32_t smem = ptx::smem_u32(pa_smem);
 
-  // the tcgen05 kernel of the same call reads nothing of this one's and may start as SMs become free
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   // ---- the line: units before each request, total, this CTA's share -----------------------------------------------
   const int per = (c.B + PA_THREADS - 1) / PA_THREADS;
   const int b_lo = min(tid * per, c.B), b_hi = min(b_lo + per, c.B);
@@ -484,7 +480,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
 }
 
 template <int DP, int WR, int STAGES>
-int pa_launch(PaParams p, char* scratch, cudaStream_t st) {
+int pa_launch(PaParams p, char* counters, char* scratch, cudaStream_t st) {
   using Sh = PaShape<DP, WR, STAGES>;
   static std::atomic<int> per_sm[64];   // resident CTAs per SM of this form, 0 = not asked yet
   int dev = 0, sms = 0;
@@ -502,8 +498,8 @@ int pa_launch(PaParams p, char* scratch, cudaStream_t st) {
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   sms = std::min(sms, kPagedMaxSms);
   const int grid = sms * occ;
-  p.counters = reinterpret_cast<uint32_t*>(scratch);
-  p.part_ml = reinterpret_cast<float*>(scratch + kPagedCounterBytes);
+  p.counters = reinterpret_cast<uint32_t*>(counters);
+  p.part_ml = reinterpret_cast<float*>(scratch);
   p.part_o = p.part_ml + (size_t)2 * kPagedMaxSms * kPagedMaxPerSm * Sh::ROWS * 2;
   kernel<<<grid, PA_THREADS, Sh::SMEM, st>>>(p);
   count_launch();
@@ -512,11 +508,11 @@ int pa_launch(PaParams p, char* scratch, cudaStream_t st) {
 }
 
 template <int DP>
-int pa_launch_rows(const PaParams& p, int wr, char* scratch, cudaStream_t st) {
+int pa_launch_rows(const PaParams& p, int wr, char* counters, char* scratch, cudaStream_t st) {
   constexpr int S = DP == 64 ? 5 : 3;
-  if (wr == 1) return pa_launch<DP, 1, S>(p, scratch, st);
-  if (wr == 2) return pa_launch<DP, 2, S>(p, scratch, st);
-  return pa_launch<DP, 4, S>(p, scratch, st);
+  if (wr == 1) return pa_launch<DP, 1, S>(p, counters, scratch, st);
+  if (wr == 2) return pa_launch<DP, 2, S>(p, counters, scratch, st);
+  return pa_launch<DP, 4, S>(p, counters, scratch, st);
 }
 
 // Row tiles of 16, 32 or 64 rows.  The host knows rows only on average: G per new token, tokens / requests new tokens.
@@ -531,21 +527,20 @@ size_t paged_attention_scratch_bytes(int head_dim) {
   // rows of partial results: 2 parts per share, 64-row tiles here, 16-row tiles (or half as many of 32) in paged_warp.cu
   const int dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
   const size_t here = (size_t)2 * kPagedMaxSms * kPagedMaxPerSm * 64, there = (size_t)2 * kPagedMaxShares * 16;
-  return kPagedCounterBytes + std::max(here * (dp + 2) * 4, there * (dp + 2) * 4 + kPagedMaxShares * kPagedCutBytes);
+  return std::max(here * (dp + 2) * 4, there * (dp + 2) * 4 + kPagedMaxShares * sizeof(JoinCut));
 }
 
-int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st) {
+int launch_paged_attention(const AttnCall& c, char* counters, char* scratch, cudaStream_t st) {
   PaParams p{};
   p.c = c;
   p.scale2 = c.scale * 1.4426950408889634f;
-  p.narrow_rows = narrow_rows;
   p.min_units = 1;
   p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
   p.div_group = fast_div_magic((uint32_t)c.G);
   const int wr = pa_row_form(c);
-  if (c.D <= 64) return pa_launch_rows<64>(p, wr, scratch, st);
-  if (c.D <= 128) return pa_launch_rows<128>(p, wr, scratch, st);
-  return pa_launch_rows<256>(p, wr, scratch, st);
+  if (c.D <= 64) return pa_launch_rows<64>(p, wr, counters, scratch, st);
+  if (c.D <= 128) return pa_launch_rows<128>(p, wr, counters, scratch, st);
+  return pa_launch_rows<256>(p, wr, counters, scratch, st);
 }
 
 }  // namespace qb

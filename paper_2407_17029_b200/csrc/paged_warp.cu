@@ -23,7 +23,7 @@
 #include <algorithm>
 #include <atomic>
 
-#include "mma_frag.cuh"
+#include "paged_join.cuh"
 #include "serving.cuh"
 #include "tc_ptx.cuh"
 #include "tc_small.cuh"
@@ -33,7 +33,7 @@ using namespace ptx;
 namespace {
 
 constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
-constexpr int PW_MAX_LEVELS = kPagedSharesPerWarp;
+constexpr int PW_MAX_LEVELS = kPagedLevels;
 constexpr int PW_FINE = 8;       // key tiles of the shortest shares
 constexpr float PW_LN2 = 0.69314718055994530942f;
 
@@ -49,10 +49,6 @@ struct PwShape {
   static constexpr int SMEM = PW_WARPS * WARP_BYTES + 1024;
 };
 
-// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i).
-struct PwCut { long long slot0, first; int n, t0, r0, rows, h, pad; };
-static_assert(sizeof(PwCut) == kPagedCutBytes, "scratch layout");
-
 struct PwParams {
   AttnCall c;
   float scale2;              // scale * log2 e
@@ -63,7 +59,7 @@ struct PwParams {
   uint32_t zero;             // 0, but not to the compiler
   long long wait_limit;
   uint32_t* counters;        // [0]: shares taken; [1 + g]: share g begins inside an item, and is the first that does.  Zeroed
-  PwCut* cuts;               // [shares] that item
+  JoinCut* cuts;             // [shares] that item
   float* part_o;             // [2 * shares][ROWS][D]
   float* part_ml;            // [2 * shares][ROWS][2]
 };
@@ -95,19 +91,25 @@ __device__ __forceinline__ int pw_head_units(const PwParams& p, const ReqView& r
   return u;
 }
 
+struct PwReq { int t0, n, kv, head_units; };     // a request as the scan saw it
+
 template <int ROWS, int KT>
 struct PwCursor {
   int b, h, rt, nrt, tile;
   ReqView r;
   PwRange k;
-  __device__ __forceinline__ void next(const PwParams& p) {
+  // known: the requests of the scan, in shared memory; nullptr where there are too many
+  __device__ __forceinline__ void next(const PwParams& p, const PwReq* known) {
     if (++tile < k.tiles) return;
     tile = 0;
     if (++rt == nrt) {
       rt = 0;
       if (++h == p.c.cache.kv_heads) {
         h = 0;
-        do { ++b; if (b >= p.c.B) return; r = attn_request(p.c, b); } while (!pw_mine(p, r));
+        do {
+          if (++b >= p.c.B) return;
+          r = known ? ReqView{known[b].t0, known[b].n, known[b].kv} : attn_request(p.c, b);
+        } while (!pw_mine(p, r));
         nrt = pw_row_tiles<ROWS>(p, r);
       }
     }
@@ -115,75 +117,18 @@ struct PwCursor {
   }
 };
 
-// Joins the parts of cut items: eight share borders per CTA, whose cut items all its warps work on, RB rows x PB parts of a
-// row at a time in flight per warp, D / 4 lanes a row.
-constexpr int PJ_THREADS = 256, PJ_CUTS = 8;
-template <int D, int ROWS, int RB, int PB>
-__device__ __forceinline__ void pw_join_block(const PwParams& p, const PwCut& x) {
-  constexpr int LANES = D / 4, STEP = 32 / LANES;          // a warp has STEP rows at a time, RB deep
-  const AttnCall& c = p.c;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, col = (lane % LANES) * 4;
-  for (int rb = warp * RB * STEP; rb < x.rows; rb += (PJ_THREADS / 32) * RB * STEP) {
-    const int row0 = rb + lane / LANES;                    // this lane's rows: row0 + STEP r
-    float M[RB], L[RB];
-    float4 acc[RB];
-#pragma unroll
-    for (int r = 0; r < RB; ++r) { M[r] = -INFINITY; L[r] = 0.f; acc[r] = make_float4(0.f, 0.f, 0.f, 0.f); }
-    for (int i0 = 0; i0 < x.n; i0 += PB) {
-      float2 ml[RB][PB];
-      float4 v[RB][PB];
-#pragma unroll
-      for (int r = 0; r < RB; ++r)
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-          ml[r][i] = make_float2(-INFINITY, 0.f);
-          v[r][i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          const int k = i0 + i, row = row0 + STEP * r;
-          if (k < x.n && row < x.rows) {
-            const long long at = (k == 0 ? x.slot0 : 2 * (x.first + k)) * ROWS + row;
-            ml[r][i] = __ldcg(reinterpret_cast<const float2*>(p.part_ml + at * 2));
-            v[r][i] = __ldcg(reinterpret_cast<const float4*>(p.part_o + at * D + col));
-          }
-        }
-#pragma unroll
-      for (int r = 0; r < RB; ++r) {
-        float mn = M[r];
-#pragma unroll
-        for (int i = 0; i < PB; ++i) mn = fmaxf(mn, ml[r][i].x);
-        const float b = mn == -INFINITY ? 0.f : mn, f = fast_exp2(M[r] - b);
-        M[r] = mn;
-        L[r] *= f; acc[r].x *= f; acc[r].y *= f; acc[r].z *= f; acc[r].w *= f;
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-          const float g = fast_exp2(ml[r][i].x - b);
-          L[r] += ml[r][i].y * g;
-          acc[r].x += v[r][i].x * g; acc[r].y += v[r][i].y * g; acc[r].z += v[r][i].z * g; acc[r].w += v[r][i].w * g;
-        }
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < RB; ++r) {
-      const int row = row0 + STEP * r;
-      if (row >= x.rows) continue;
-      const int gr = x.r0 + row, tok = fast_div(gr, c.G, p.div_group), head = x.h * c.G + gr - tok * c.G;
-      const float inv = L[r] == 0.f ? 0.f : 1.f / L[r];
-      *reinterpret_cast<uint2*>(c.out + (long long)(x.t0 + tok) * c.o_ts + (long long)head * c.o_hs + col) =
-          make_uint2(pack_bf16x2(acc[r].x * inv, acc[r].y * inv), pack_bf16x2(acc[r].z * inv, acc[r].w * inv));
-      if (c.lse && col == 0) c.lse[(long long)(x.t0 + tok) * c.H + head] = L[r] == 0.f ? -INFINITY : (M[r] + log2f(L[r])) * PW_LN2;
-    }
-  }
-}
-template <int D, int ROWS>
-__global__ void __launch_bounds__(PJ_THREADS) paged_join_kernel(const __grid_constant__ PwParams p) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
+  __shared__ JoinShared list;
   asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
-  const int g0 = blockIdx.x * PJ_CUTS;
-  for (int i = 0; i < PJ_CUTS; ++i) {
-    if (!__ldcg(p.counters + 1 + g0 + i)) continue;
-    const PwCut x = p.cuts[g0 + i];
-    if (x.n <= 4) pw_join_block<D, ROWS, 2, 4>(p, x);
-    else pw_join_block<D, ROWS, 1, 16>(p, x);
-  }
+  join_all<D, 256>(c, j, &list);
+}
+
+// status word and counters
+__global__ void __launch_bounds__(256) attention_reset_kernel(uint4* ws, int n) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) ws[i] = make_uint4(0, 0, 0, 0);
 }
 
 template <int D, int MT>
@@ -194,8 +139,9 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   using Cursor = PwCursor<ROWS, KT>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t s_full[PW_WARPS * PW_STAGES];
-  __shared__ long long s_scan[PW_WARPS], s_units[PW_THREADS];
-  __shared__ long long s_base[PW_MAX_LEVELS + 1], s_each[PW_MAX_LEVELS];
+  __shared__ long long s_scan[PW_WARPS];
+  __shared__ int s_units[PW_THREADS], s_base[PW_MAX_LEVELS + 1], s_each[PW_MAX_LEVELS];
+  __shared__ PwReq s_req[PW_THREADS];
   __shared__ Cursor s_next[PW_WARPS];          // where the next share of each warp begins
   const AttnCall& c = p.c;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -204,8 +150,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const uint32_t sq = base + PW_WARPS * PW_STAGES * Sh::STAGE + warp * Sh::Q_BYTES;
   const uint32_t full = smem_u32(s_full + warp * PW_STAGES);
 
-  // the tcgen05 kernel of the same call reads nothing of this one's and may start as SMs become free
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane == 0) {
     for (int s = 0; s < PW_STAGES; ++s) mbar_init(full + 8 * s, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -217,8 +161,11 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   long long mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     const ReqView r = attn_request(c, b);
-    if (pw_mine(p, r)) mine += (long long)pw_head_units<ROWS, KT>(p, r) * c.cache.kv_heads;
+    const int hu = pw_mine(p, r) ? pw_head_units<ROWS, KT>(p, r) : 0;
+    mine += (long long)hu * c.cache.kv_heads;
+    if (per == 1) s_req[b] = PwReq{r.t0, r.n, r.kv, hu};
   }
+  const PwReq* known = per == 1 ? s_req : nullptr;
   long long incl = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
@@ -227,65 +174,78 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
   if (lane == 31) s_scan[warp] = incl;
   __syncthreads();
-  long long total = 0;
+  long long total_ = 0;
 #pragma unroll
   for (int w = 0; w < PW_WARPS; ++w) {
     if (w < warp) incl += s_scan[w];
-    total += s_scan[w];
+    total_ += s_scan[w];
   }
-  s_units[tid] = incl;
-  __syncthreads();
+  s_units[tid] = (int)min(incl, 0x7fffffffLL);
+  // From here on this kernel writes what the reset kernel clears; and the kernel behind it, which reads nothing that this
+  // one writes before it has waited for its end, may start as SMs become free.
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (total_ == 0) return;
+  if (total_ > 0x7fffffffLL) {   // 2^31 tiles are 10^13 bytes of keys and values and more: the lengths cannot be meant
+    if (tid == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
+    return;
+  }
+  const int total = (int)total_;
   // Shares: level k hands every warp one share; the levels' parts of the line are 1/2, 1/4, ... with the last two equal, so
   // the shares that are taken late are short.  A share has more tiles than the ring has slots (then at most one share's
   // beginning is in the ring besides the current one).
-  const long long per_level = min((long long)gridDim.x * PW_WARPS, max(1LL, total / (PW_STAGES + 1)));
+  const int per_level = min((int)gridDim.x * PW_WARPS, max(1, total / (PW_STAGES + 1)));
   int levels = 1;
   while (levels < p.max_levels && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
-  const long long shares = per_level * levels;
+  const int shares = per_level * levels;
   if (tid == 0) {
-    long long at = 0;
+    int at = 0;
     for (int k = 0; k < levels; ++k) {
       s_base[k] = at;
-      s_each[k] = k + 1 < levels ? (total >> (k + 1)) / per_level : (total - at) / per_level;
+      s_each[k] = (k + 1 < levels ? total >> (k + 1) : total - at) / per_level;
       at += s_each[k] * per_level;
     }
     s_base[levels] = total;
   }
   __syncthreads();
   // of the last level, the first `extra` shares have one tile more
-  const long long last_each = s_each[levels - 1], extra = total - s_base[levels - 1] - last_each * per_level;
-  auto share_begin = [&](long long g) -> long long {
+  const int extra = total - s_base[levels - 1] - s_each[levels - 1] * per_level;
+  auto share_begin = [&](int g) -> int {
     if (g >= shares) return total;
-    const int k = (int)(g / per_level);
-    const long long i = g - k * per_level;
+    const int k = g / per_level, i = g - k * per_level;
     return s_base[k] + i * s_each[k] + (k + 1 == levels ? min(i, extra) : 0);
   };
-  auto share_of = [&](long long u) {
+  auto share_of = [&](int u) -> int {
     int k = 0;
     while (k + 1 < levels && u >= s_base[k + 1]) ++k;
-    const long long v = u - s_base[k], each = s_each[k];
+    const int v = u - s_base[k], each = s_each[k];
     if (k + 1 < levels) return k * per_level + v / each;
-    const long long cut = extra * (each + 1);
+    const int cut = extra * (each + 1);
     return k * per_level + (v < cut ? v / (each + 1) : extra + (v - cut) / each);
   };
-  const long long g_first = (long long)blockIdx.x * PW_WARPS + warp;
-  if (total == 0 || g_first >= per_level) return;
+  const int g_first = (int)blockIdx.x * PW_WARPS + warp;
+  if (g_first >= per_level) return;
 
   // the cursor of unit u: a search over the threads' sums, a walk over that thread's requests
-  auto locate = [&](Cursor& at, long long u) {
+  auto locate = [&](Cursor& at, int u) {
     int a = 0, e = PW_THREADS;
     while (a < e) { const int x = (a + e) >> 1; if (s_units[x] > u) e = x; else a = x + 1; }
-    long long rest = u - (a ? s_units[a - 1] : 0);
-    int hu = 1;
-    for (at.b = a * per;; ++at.b) {
-      at.r = attn_request(c, at.b);
-      if (!pw_mine(p, at.r)) continue;
-      hu = pw_head_units<ROWS, KT>(p, at.r);
-      if (rest < (long long)hu * c.cache.kv_heads) break;
-      rest -= (long long)hu * c.cache.kv_heads;
+    int rest = u - (a ? s_units[a - 1] : 0), hu = 1;
+    if (known) {
+      at.b = a;
+      at.r = ReqView{known[a].t0, known[a].n, known[a].kv};
+      hu = known[a].head_units;
+    } else {
+      for (at.b = a * per;; ++at.b) {
+        at.r = attn_request(c, at.b);
+        if (!pw_mine(p, at.r)) continue;
+        hu = pw_head_units<ROWS, KT>(p, at.r);
+        if (rest < (long long)hu * c.cache.kv_heads) break;
+        rest -= hu * c.cache.kv_heads;
+      }
     }
-    at.h = (int)(rest >> 31 ? rest / hu : (long long)((uint32_t)rest / (uint32_t)hu));
-    int left = (int)(rest - (long long)at.h * hu);
+    at.h = rest / hu;
+    int left = rest - at.h * hu;
     at.nrt = pw_row_tiles<ROWS>(p, at.r);
     at.rt = 0;
     at.k = pw_range<ROWS, KT>(p, at.r, 0);
@@ -296,15 +256,14 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   bool ok = true;
   int odd_pages = 0;
   {
-    long long g = g_first, u0 = share_begin(g), u1 = share_begin(g + 1);   // the share being computed
-    long long g_next = 0;                                                  // lane 0: the share after it
-    if (lane == 0 && levels > 1) g_next = (long long)atomicAdd(p.counters, 1u) + per_level;
-    else g_next = shares;
+    int g = g_first, u0 = share_begin(g), u1 = share_begin(g + 1);   // the share being computed
+    int g_next = shares;                                             // lane 0: the share after it
+    if (lane == 0 && levels > 1) g_next = (int)atomicAdd(p.counters, 1u) + per_level;
     Cursor ld;
     locate(ld, u0);
     Cursor cu = ld;
-    int ld_left = (int)(u1 - u0);            // tiles of the share being loaded that are not issued yet
-    long long ld_next_g = -1;                // the share being loaded, where that is the one after g; `shares` or more: none left
+    int ld_left = u1 - u0;            // tiles of the share being loaded that are not issued yet
+    int ld_next_g = -1;                // the share being loaded, where that is the one after g; `shares` or more: none left
 
     // ---- loads: lane i issues box i: (K or V, half of the head, run of keys) ------------------------------------------
     const int runs = KT / p.box_keys;                 // boxes along the keys
@@ -330,16 +289,16 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         tma_load_4d(ring + st_ld * Sh::STAGE + my_dst + dep, my_kv ? &tm_v : &tm_k, full + 8 * st_ld, my_half * 64, entry, ld.h, page);
       if (++st_ld == PW_STAGES) st_ld = 0;
       ++issued;
-      if (--ld_left > 0) ld.next(p);
+      if (--ld_left > 0) ld.next(p, known);
       else {
         ld_next_g = __shfl_sync(0xffffffffu, g_next, 0);
         if (ld_next_g >= shares) return;                       // ld_left stays 0: nothing more to issue
-        const long long b0 = share_begin(ld_next_g);
+        const int b0 = share_begin(ld_next_g);
         locate(ld, b0);
-        ld_left = (int)(share_begin(ld_next_g + 1) - b0);
+        ld_left = share_begin(ld_next_g + 1) - b0;
         if (lane == 0) {
           s_next[warp] = ld;
-          g_next = (long long)atomicAdd(p.counters, 1u) + per_level;
+          g_next = (int)atomicAdd(p.counters, 1u) + per_level;
         }
         __syncwarp();
       }
@@ -361,18 +320,18 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     int stage = 0;
     uint32_t ph = 0;
     bool first_segment = true, fresh = true;     // of the share; of the item
-    long long u = u0;                            // the tile being computed
+    int u = u0;                                  // the tile being computed
 
     while (true) {
       if (fresh) {
         fresh = false;
         if (first_segment && cu.tile > 0 && lane == 0) {
           // this share begins inside an item: the first share that does tells the join kernel about it
-          const long long item_first = u0 - cu.tile, first = g - 1;
+          const int item_first = u0 - cu.tile, first = g - 1;
           if (share_begin(first) <= item_first) {
-            const int n = (int)(share_of(item_first + cu.k.tiles - 1) - first) + 1;
+            const int n = share_of(item_first + cu.k.tiles - 1) - first + 1;
             // its first part is the first share's last segment (slot 1) unless that share begins with the item; the others' first (slot 0)
-            p.cuts[g] = PwCut{2 * first + (share_begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
+            p.cuts[g] = JoinCut{2 * first + (share_begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
                               min(ROWS, cu.r.n * c.G - cu.rt * ROWS), cu.h, 0};
             p.counters[1 + g] = 1;
           }
@@ -590,9 +549,9 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
       // ---- end of an item, or of this share's part of it --------------------------------------------------------------
       if (cu.tile + 1 == cu.k.tiles || u + 1 == u1) {
-        const long long item_first = u - cu.tile;
+        const int item_first = u - cu.tile;
         const bool whole = item_first >= u0 && item_first + cu.k.tiles <= u1;
-        const long long slot = 2 * g + (first_segment ? 0 : 1);
+        const long long slot = 2 * g + (first_segment ? 0 : 1);   // of partial results
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -621,7 +580,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         first_segment = false;
         fresh = true;
       }
-      if (++u < u1) { cu.next(p); continue; }
+      if (++u < u1) { cu.next(p, known); continue; }
       // the next share: its tiles are on their way already
       if (ld_next_g < 0 || ld_next_g >= shares) break;
       g = ld_next_g;
@@ -640,7 +599,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 }
 
 template <int D, int MT>
-int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* scratch, cudaStream_t st) {
+int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, JoinCall* join, cudaStream_t st) {
   using Sh = PwShape<D, MT>;
   static std::atomic<bool> attr_set[64];
   int dev = 0, sms = 0;
@@ -654,28 +613,42 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* sc
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int grid = std::min(sms, kPagedMaxSms);
   p.max_levels = PW_MAX_LEVELS / MT;      // the scratch holds as many rows for either form
-  p.counters = reinterpret_cast<uint32_t*>(scratch);
-  p.part_ml = reinterpret_cast<float*>(scratch + kPagedCounterBytes);
+  p.counters = reinterpret_cast<uint32_t*>(counters);
+  p.part_ml = reinterpret_cast<float*>(scratch);
   p.part_o = p.part_ml + (size_t)2 * kPagedMaxShares * Sh::ROWS * 2 / MT;
-  p.cuts = reinterpret_cast<PwCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D / MT);
-  kernel<<<grid, PW_THREADS, Sh::SMEM, st>>>(tk, tv, p);
-  QB_CUDA(cudaGetLastError());
+  p.cuts = reinterpret_cast<JoinCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D / MT);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((grid * PW_WARPS * p.max_levels + PJ_CUTS - 1) / PJ_CUTS));
-  cfg.blockDim = dim3(PJ_THREADS);
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3(PW_THREADS);
+  cfg.dynamicSmemBytes = Sh::SMEM;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr; cfg.numAttrs = 1;
-  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D, Sh::ROWS>, p));
-  count_launch(2);
+  QB_CUDA(cudaLaunchKernelEx(&cfg, kernel, tk, tv, p));
+  count_launch();
+  JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, grid * PW_WARPS * p.max_levels, Sh::ROWS, p.div_group};
+  if (join) { *join = j; return QBLORA_OK; }
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
+  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D>, p.c, j));
+  count_launch();
   return QBLORA_OK;
 }
 
 }  // namespace
 
 static_assert(PW_WARPS == kPagedWarps, "shares per SM");
+
+int launch_attention_reset(void* ws, cudaStream_t st) {
+  constexpr int n = (int)(kAttnResetBytes / 16);
+  static_assert(kAttnResetBytes % 16 == 0, "whole words");
+  attention_reset_kernel<<<(n + 255) / 256, 256, 0, st>>>(static_cast<uint4*>(ws), n);
+  count_launch();
+  QB_CUDA(cudaGetLastError());
+  return QBLORA_OK;
+}
 
 bool paged_warp_supported(const AttnCall& c) {
   if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f)) return false;
@@ -684,7 +657,7 @@ bool paged_warp_supported(const AttnCall& c) {
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);
 }
 
-int launch_paged_warp(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st) {
+int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, JoinCall* join, cudaStream_t st) {
   PwParams p{};
   p.c = c;
   p.scale2 = c.scale * 1.4426950408889634f;
@@ -698,8 +671,8 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* scratch, cudaStr
   if (rc) return rc;
   // Row tiles of 16 or 32 rows.  The host knows rows only on average: G per new token, tokens / requests new tokens.
   const bool one = ((c.T + c.B - 1) / c.B) * c.G <= 16;
-  if (c.D == 64) return one ? pw_launch<64, 1>(p, tk, tv, scratch, st) : pw_launch<64, 2>(p, tk, tv, scratch, st);
-  return one ? pw_launch<128, 1>(p, tk, tv, scratch, st) : pw_launch<128, 2>(p, tk, tv, scratch, st);
+  if (c.D == 64) return one ? pw_launch<64, 1>(p, tk, tv, counters, scratch, join, st) : pw_launch<64, 2>(p, tk, tv, counters, scratch, join, st);
+  return one ? pw_launch<128, 1>(p, tk, tv, counters, scratch, join, st) : pw_launch<128, 2>(p, tk, tv, counters, scratch, join, st);
 }
 
 }  // namespace qb

@@ -76,27 +76,42 @@ __device__ __forceinline__ ReqView attn_request(const AttnCall& c, int b) {
 __device__ __forceinline__ int attn_hi(const AttnCall& c, int kv, int p) { return c.causal ? max(0, min(kv, p + 1)) : kv; }
 __device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.window > 0 ? max(0, p - c.window + 1) : 0; }
 
-// Few rows per key head (paged_attn.cu): requests of at most `narrow_rows` rows (new tokens * G).  `scratch`:
-// paged_attention_scratch_bytes, its first kPagedCounterBytes zeroed on the stream before the launch.
-constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;
-constexpr int kPagedWarps = 8, kPagedSharesPerWarp = 4;     // of paged_warp.cu
-constexpr int kPagedMaxShares = kPagedMaxSms * kPagedWarps * kPagedSharesPerWarp;
-constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256, kPagedCutBytes = 40;
-size_t paged_attention_scratch_bytes(int head_dim);
-int launch_paged_attention(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
-
-// The same for head sizes 64 and 128 with pages that fit its tiles (paged_warp.cu), same scratch.
-bool paged_warp_supported(const AttnCall& c);
-int launch_paged_warp(const AttnCall& c, int narrow_rows, char* scratch, cudaStream_t st);
-
-// Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows.  `counters`:
-// kWideCounterBytes, zeroed on the stream; `scratch`: tc_attention_scratch_bytes.  `behind_narrow`: the kernel in front on the stream is
-// launch_paged_attention's of the same call, and this one may start beside it.
-constexpr int kWideMaxRequests = 1024;
+// ---- attention: layout of the caller's workspace, after the status word
+//   counters that every call zeroes (launch_attention_reset), then the parts of paged_attn.cu or paged_warp.cu, then those of
+//   tc_attn.cu
+constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;       // resident CTAs of paged_attn.cu
+constexpr int kPagedWarps = 8, kPagedLevels = 4;            // warps per SM, and shares per warp, of paged_warp.cu
+constexpr int kPagedMaxShares = kPagedMaxSms * kPagedWarps * kPagedLevels;
 constexpr size_t kWideCounterBytes = 2 * kPagedMaxSms * 4;
+constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256;
+constexpr size_t kAttnResetBytes = kStatusBytes + kWideCounterBytes + kPagedCounterBytes;
+int launch_attention_reset(void* ws, cudaStream_t st);
+
+// Any head size up to 256, any page size and strides that are multiples of 8 elements (paged_attn.cu).
+size_t paged_attention_scratch_bytes(int head_dim);
+int launch_paged_attention(const AttnCall& c, char* counters, char* scratch, cudaStream_t st);
+
+// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i).
+struct JoinCut { int slot0, first, n, t0, r0, rows, h, pad; };
+struct JoinCall {
+  const uint32_t* flags;      // [borders]: share g is the first that begins inside some item
+  const JoinCut* cuts;        // [borders]: that item
+  const float *part_o, *part_ml;
+  int borders, rows_per_slot;
+  uint32_t div_group;
+};
+
+// Few rows per key head, head sizes 64 and 128, pages that fit its tiles (paged_warp.cu): requests of at most `narrow_rows` rows
+// (new tokens * G).  With `join` the caller joins the parts (paged_join.cuh); without, a kernel behind it does.
+bool paged_warp_supported(const AttnCall& c);
+int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, JoinCall* join, cudaStream_t st);
+
+// Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows, and the joins of the kernel in front, behind
+// which this one may start as SMs become free.
+constexpr int kWideMaxRequests = 1024;
 bool tc_attention_supported(const AttnCall& c);
 size_t tc_attention_scratch_bytes(int head_dim);
-int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, bool behind_narrow, cudaStream_t st);
+int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join, char* counters, char* scratch, cudaStream_t st);
 
 // TMA maps (CUtensorMap) of the cache's K and V.
 int make_cache_maps(const AttnCall& c, int box_keys, void* tm_k, void* tm_v);

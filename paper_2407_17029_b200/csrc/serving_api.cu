@@ -125,7 +125,7 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
 size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens) {
   if (!cache || cache->kv_heads < 1 || q_heads < 1 || q_heads % cache->kv_heads || tokens < 1) return 0;
   if (cache->head_dim < 1 || cache->head_dim > 256) return 0;
-  return kStatusBytes + kWideCounterBytes + paged_attention_scratch_bytes(cache->head_dim) + tc_attention_scratch_bytes(cache->head_dim);
+  return kAttnResetBytes + paged_attention_scratch_bytes(cache->head_dim) + tc_attention_scratch_bytes(cache->head_dim);
 }
 
 int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_table, int32_t width, const int32_t* cu_new,
@@ -151,16 +151,18 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   c.scale = scale; c.causal = causal != 0; c.window = window;
   c.status = static_cast<int*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  // status word, arrival counters of both kernels (which begin their scratch areas)
-  const bool wide = tc_attention_supported(c) && tokens * c.G > kNarrowRows;
-  char* wide_ws = static_cast<char*>(ws) + kStatusBytes;
-  char* narrow_ws = wide_ws + kWideCounterBytes;
-  QB_CUDA(cudaMemsetAsync(ws, 0, kStatusBytes + kWideCounterBytes + kPagedCounterBytes, st));
+  int rc = launch_attention_reset(ws, st);
+  if (rc) return rc;
   if (force_general()) return launch_simt_attention(c, st);
-  const int narrow = wide ? kNarrowRows : 0x7fffffff;
-  const int rc = paged_warp_supported(c) ? launch_paged_warp(c, narrow, narrow_ws, st) : launch_paged_attention(c, narrow, narrow_ws, st);
-  if (rc || !wide) return rc;
-  return launch_tc_attention(c, kNarrowRows, wide_ws, narrow_ws + paged_attention_scratch_bytes(c.D), true, st);
+  char* wide_counters = static_cast<char*>(ws) + kStatusBytes;
+  char* counters = wide_counters + kWideCounterBytes;
+  char* scratch = counters + kPagedCounterBytes;
+  if (!paged_warp_supported(c)) return launch_paged_attention(c, counters, scratch, st);
+  if (!tc_attention_supported(c) || tokens * c.G <= kNarrowRows) return launch_paged_warp(c, 0x7fffffff, counters, scratch, nullptr, st);
+  JoinCall join;
+  rc = launch_paged_warp(c, kNarrowRows, counters, scratch, &join, st);
+  if (rc) return rc;
+  return launch_tc_attention(c, kNarrowRows, join, wide_counters, scratch + paged_attention_scratch_bytes(c.D), st);
 }
 
 }  // extern "C"

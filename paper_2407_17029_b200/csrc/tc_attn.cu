@@ -26,6 +26,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "paged_join.cuh"
 #include "serving.cuh"
 #include "tc_ptx.cuh"
 #include "tc_small.cuh"
@@ -50,6 +51,7 @@ struct TaShape {
 
 struct TaParams {
   AttnCall c;
+  JoinCall join;          // what paged_warp.cu has left to join
   float scale2;
   int narrow_rows;        // requests with at most so many rows belong to paged_attn.cu
   int tokens_per_tile;    // 128 / G
@@ -186,6 +188,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ long long s_warp_u[TA_THREADS / 32];
   __shared__ int s_odd[8];         // segment number + 1 where a value was taken out of V
   __shared__ int s_join[2];
+  __shared__ JoinShared s_list;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AttnCall& c = p.c;
@@ -257,8 +260,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
   }
   if (!some) {
-    // nothing may follow this grid in the stream before the kernel in front of it has ended
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");     // the kernel in front has ended
+    join_all<D, TA_THREADS>(c, p.join, &s_list);
     return;
   }
 
@@ -664,11 +667,12 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the kernel in front has ended
+  join_all<D, TA_THREADS>(c, p.join, &s_list);
 }
 
 template <int D>
-int ta_launch(const TaParams& p0, char* counters, char* scratch, bool behind_narrow, cudaStream_t st) {
+int ta_launch(const TaParams& p0, char* counters, char* scratch, cudaStream_t st) {
   using Sh = TaShape<D>;
   static std::atomic<bool> attr_set[64];
   int dev = 0, sms = 0;
@@ -708,7 +712,7 @@ int ta_launch(const TaParams& p0, char* counters, char* scratch, bool behind_nar
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = behind_narrow ? 1 : 0;
+  cfg.numAttrs = 1;
   QB_CUDA(cudaLaunchKernelEx(&cfg, kernel, tq, tk, tv, p));
   count_launch();
   QB_CUDA(cudaGetLastError());
@@ -740,15 +744,16 @@ size_t tc_attention_scratch_bytes(int head_dim) {
   return (size_t)2 * kPagedMaxSms * 2 * 128 * (head_dim + 2) * 4;
 }
 
-int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, bool behind_narrow, cudaStream_t st) {
+int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join, char* counters, char* scratch, cudaStream_t st) {
   TaParams p{};
   p.c = c;
+  p.join = join;
   p.scale2 = c.scale * 1.4426950408889634f;
   p.narrow_rows = narrow_rows;
   p.tokens_per_tile = TA_TILE / c.G;
   p.box_keys = std::min(c.cache.page_size, TA_TILE);
   p.wait_limit = wait_limit_cycles();
-  return c.D == 64 ? ta_launch<64>(p, counters, scratch, behind_narrow, st) : ta_launch<128>(p, counters, scratch, behind_narrow, st);
+  return c.D == 64 ? ta_launch<64>(p, counters, scratch, st) : ta_launch<128>(p, counters, scratch, st);
 }
 
 }  // namespace qb
