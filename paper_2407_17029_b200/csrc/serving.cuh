@@ -82,7 +82,8 @@ __device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.wind
 constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;       // resident CTAs of paged_attn.cu
 constexpr int kPagedWarps = 8, kPagedLevels = 4;            // warps per SM, and shares per warp, of paged_warp.cu
 constexpr int kPagedMaxShares = kPagedMaxSms * kPagedWarps * kPagedLevels;
-constexpr size_t kWideCounterBytes = 2 * kPagedMaxSms * 4;
+constexpr int kWideRounds = 3, kWideMaxShares = kPagedMaxSms * kWideRounds;     // of tc_attn.cu
+constexpr size_t kWideCounterBytes = (size_t)(1 + 2 * kWideMaxShares) * 4 / 256 * 256 + 256;
 constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256;
 constexpr size_t kAttnResetBytes = kStatusBytes + kWideCounterBytes + kPagedCounterBytes;
 int launch_attention_reset(void* ws, cudaStream_t st);

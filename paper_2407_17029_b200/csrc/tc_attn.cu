@@ -38,14 +38,16 @@ namespace {
 constexpr int TA_THREADS = 384;
 constexpr int TA_TILE = 128;            // rows per row tile, keys per key tile
 constexpr float TA_LN2 = 0.69314718055994530942f;
+constexpr long long TA_L2_BYTES = 96000000;
+constexpr int TA_SEGS = 4;              // segments handed out ahead
 constexpr float TA_SLACK = 8.0f;        // how far (in powers of two) a row's maximum may run ahead of m
 
 template <int D>
 struct TaShape {
   static constexpr int STAGES = D == 64 ? 6 : 4;            // K and V tiles take turns; even, so V keeps to odd stages
   static constexpr int TILE_BYTES = TA_TILE * D * 2;        // one Q, K or V tile
-  static constexpr int BARS = 2 * STAGES + STAGES + 12;     // full, empty, clean; s, p, o_full, o_free, q_full, q_empty x 2
-  static constexpr int LIST_BYTES = kWideMaxRequests * 16;
+  static constexpr int BARS = 3 * STAGES + 14 + 2 * TA_SEGS;   // full, empty, clean; seven for each row tile; the segments' two
+  static constexpr int LIST_BYTES = kWideMaxRequests * 12;
   static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + LIST_BYTES + BARS * 8 + 64 + 1024;
 };
 
@@ -57,9 +59,10 @@ struct TaParams {
   int tokens_per_tile;    // 128 / G
   int box_keys;           // keys per TMA box: min(page_size, 128)
   long long wait_limit;
-  uint32_t* counters;     // [2 * grid], zeroed
-  float* part_o;          // [2 * grid][2 row tiles][D / 4][128 rows][4]
-  float* part_ml;         // [2 * grid][2][128][2]
+  uint32_t div_page;
+  uint32_t* counters;     // zeroed; [0]: items dealt out, [1 + 2 * share + row tile]: parts of the item that the share cuts first
+  float* part_o;          // [2 * shares][2 row tiles][D / 4][128 rows][4]
+  float* part_ml;         // [2 * shares][2][128][2]
 };
 
 __device__ __forceinline__ float ta_exp2(float x) {
@@ -68,16 +71,68 @@ __device__ __forceinline__ float ta_exp2(float x) {
   return y;
 }
 
-// One stretch of key tiles [ja, jb) of an item.
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float y;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// two fp32 values in a 64-bit register
+__device__ __forceinline__ uint64_t pack2(float a, float b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ uint64_t pack2u(uint32_t a, uint32_t b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "r"(a), "r"(b));
+  return y;
+}
+__device__ __forceinline__ float lo2(uint64_t x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float hi2(uint64_t x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+// 2^x of two values, x <= 2^7, without the special-function unit: x = n + f with n whole and |f| <= 1/2, 2^f by the polynomial of
+// degree 4 with the smallest largest relative error on that interval (2.7e-6, from a Remez exchange), n added to the exponent.
+// Below 2^-126 the result is 2^-126; NaN does not survive (the caller's maximum has caught it).
+__device__ __forceinline__ uint64_t exp2_fma2(uint64_t x) {
+  x = pack2(fmaxf(lo2(x), -126.f), fmaxf(hi2(x), -126.f));
+  const uint64_t magic = pack2(12582912.f, 12582912.f), minus_magic = pack2(-12582912.f, -12582912.f);   // 1.5 * 2^23
+  const uint64_t t = add2(x, magic);                       // n in the low bits
+  const uint64_t n = add2(t, minus_magic);
+  const uint64_t f = fma2(n, pack2(-1.f, -1.f), x);
+  uint64_t y = fma2(f, pack2(0.009570102207362652f, 0.009570102207362652f), pack2(0.05591785907745361f, 0.05591785907745361f));
+  y = fma2(y, f, pack2(0.240247443318367f, 0.240247443318367f));
+  y = fma2(y, f, pack2(0.6931217908859253f, 0.6931217908859253f));
+  y = fma2(y, f, pack2(0.9999992847442627f, 0.9999992847442627f));
+  const uint32_t a = (uint32_t)y + ((uint32_t)t << 23), b = (uint32_t)(y >> 32) + ((uint32_t)(t >> 32) << 23);
+  return pack2u(a, b);
+}
+
+// One stretch of key tiles [ja, jb) of an item, as the loading warp hands it to the others.
 struct TaSeg {
+  int valid;               // 0: no more
   ReqView r;
   int b, h, tok0;          // request, key head, first token of the pair
   int lo;                  // first key of tile 0, a multiple of 128
   int nt[2];               // key tiles that each row tile sees
-  int ja, jb, tiles;       // this stretch, and all tiles of the item
-  long long first_unit;    // of the item in the line
+  int full_lo[2], full_hi[2];   // tiles in this range have only keys that every row of the row tile sees
+  int stop;                // keys from here on are seen by no row of the pair
+  int ja, jb;
+  int whole;               // the stretch is the item
+  int slot, slot0, first, last;   // where not: its place for partial results, that of the item's first part, shares first .. last
   __device__ __forceinline__ int end(int t) const { return min(jb, nt[t]); }
-  __device__ __forceinline__ int last() const { return max(end(0), end(1)); }
+  __device__ __forceinline__ int last_tile() const { return max(end(0), end(1)); }
+  __device__ __forceinline__ bool partial(int t, int j) const { return j < full_lo[t] || j >= full_hi[t]; }
+  // whether V of tile j has to be cleaned
+  __device__ __forceinline__ bool dirty(int j) const { return (j < end(0) && partial(0, j)) || (j < end(1) && partial(1, j)); }
 };
 
 __device__ __forceinline__ int ta_pair_tiles(const TaParams& p, const ReqView& r, int q, int* nt, int* lo) {
@@ -98,68 +153,80 @@ __device__ __forceinline__ int ta_pairs(const TaParams& p, const ReqView& r) {
 struct TaWalk {
   const int* req;            // [n]
   const int* items;          // [n] inclusive sums
-  const long long* units;    // [n] inclusive sums
+  const int* units;          // [n] inclusive sums of key tiles
   int n;
-  bool whole;                // whole items are dealt out
-  long long u, u1, total, shares;
-  int k;
+  bool dealt;                // whole items are dealt out one by one
+  int share, shares, total, u, u1;
 
-  __device__ __forceinline__ bool next(const TaParams& p, TaSeg& s) {
-    int wi, q;
-    const int hkv = p.c.cache.kv_heads;
-    if (whole) {
-      // rounds of gridDim.x items, every second one backwards: with the longest items first the shares come out even
-      const int g = gridDim.x;
-      const long long i = (long long)k * g + ((k & 1) ? g - 1 - (int)blockIdx.x : (int)blockIdx.x);
-      ++k;
-      if (i >= items[n - 1]) return false;
-      wi = find(items, (int)i);
-      const int local = (int)i - (wi ? items[wi - 1] : 0);
-      s.b = req[wi];
-      s.r = attn_request(p.c, s.b);
-      const int np = ta_pairs(p, s.r);
-      // Pairs with the most keys first.  While the request's keys fit the L2 (126 MB) the key heads run fastest, which sorts
-      // items by length; beyond that all pairs of a key head come one after another, so that the CTAs in flight
-      // stream the keys of few heads.
-      if ((long long)s.r.kv * hkv * p.c.D * 4 <= 96000000LL) { q = np - 1 - local / hkv; s.h = local % hkv; }
-      else { s.h = local / np; q = np - 1 - local % np; }
-      s.tiles = ta_pair_tiles(p, s.r, q, s.nt, &s.lo);
-      s.ja = 0; s.jb = s.tiles; s.first_unit = 0;
-    } else {
-      if (u >= u1) return false;
-      int a = 0, e = n;
-      while (a < e) { const int m = (a + e) >> 1; if (units[m] > u) e = m; else a = m + 1; }
-      wi = a;
-      const long long base = wi ? units[wi - 1] : 0;
-      const long long hu = (units[wi] - base) / hkv;
-      s.b = req[wi];
-      s.r = attn_request(p.c, s.b);
-      s.h = (int)((u - base) / hu);
-      long long rest = u - base - s.h * hu;
-      q = 0;
-      s.tiles = ta_pair_tiles(p, s.r, 0, s.nt, &s.lo);
-      while (rest >= s.tiles) { rest -= s.tiles; ++q; s.tiles = ta_pair_tiles(p, s.r, q, s.nt, &s.lo); }
-      s.ja = (int)rest;
-      s.jb = (int)min((long long)s.tiles, rest + (u1 - u));
-      s.first_unit = u - rest;
-      u += s.jb - s.ja;
-    }
-    s.tok0 = 2 * q * p.tokens_per_tile;
-    return true;
-  }
   __device__ __forceinline__ int find(const int* sums, int x) const {
     int a = 0, e = n;
     while (a < e) { const int m = (a + e) >> 1; if (sums[m] > x) e = m; else a = m + 1; }
     return a;
   }
+  __device__ __forceinline__ int begin(int s) const { return (int)((long long)total * s / shares); }
+  __device__ __forceinline__ int share_of(int x) const {
+    int s = (int)((long long)x * shares / total);
+    while (begin(s + 1) <= x) ++s;
+    while (begin(s) > x) --s;
+    return s;
+  }
+  // called by all lanes of the loading warp
+  __device__ __forceinline__ bool next(const TaParams& p, TaSeg& s) {
+    const int hkv = p.c.cache.kv_heads;
+    int wi, q, tiles, first_unit = 0;
+    if (dealt) {
+      int i = 0;
+      if ((threadIdx.x & 31) == 0) i = (int)atomicAdd(p.counters, 1u);
+      i = __shfl_sync(0xffffffffu, i, 0);
+      if (i >= items[n - 1]) return false;
+      wi = find(items, i);
+      const int local = i - (wi ? items[wi - 1] : 0);
+      s.b = req[wi];
+      s.r = attn_request(p.c, s.b);
+      q = ta_pairs(p, s.r) - 1 - local / hkv;        // the longest first: the last ones to be dealt out are short
+      s.h = local % hkv;
+      tiles = ta_pair_tiles(p, s.r, q, s.nt, &s.lo);
+      s.ja = 0; s.jb = tiles;
+    } else {
+      while (u >= u1) {
+        share += gridDim.x;
+        if (share >= shares) return false;
+        u = begin(share); u1 = begin(share + 1);
+      }
+      wi = find(units, u);
+      const int base = wi ? units[wi - 1] : 0, hu = (units[wi] - base) / hkv;
+      s.b = req[wi];
+      s.r = attn_request(p.c, s.b);
+      s.h = (u - base) / hu;
+      int rest = u - base - s.h * hu;
+      q = 0;
+      tiles = ta_pair_tiles(p, s.r, 0, s.nt, &s.lo);
+      while (rest >= tiles) { rest -= tiles; ++q; tiles = ta_pair_tiles(p, s.r, q, s.nt, &s.lo); }
+      s.ja = rest;
+      s.jb = min(tiles, rest + (u1 - u));
+      first_unit = u - rest;
+      s.slot = 2 * share + (begin(share) == u ? 0 : 1);   // a share's first stretch, or its last
+      u += s.jb - s.ja;
+    }
+    s.valid = 1;
+    s.whole = s.ja == 0 && s.jb == tiles;
+    if (!s.whole) {
+      s.first = share_of(first_unit);
+      s.last = share_of(first_unit + tiles - 1);
+      s.slot0 = 2 * s.first + (begin(s.first) == first_unit ? 0 : 1);
+    }
+    s.tok0 = 2 * q * p.tokens_per_tile;
+    const int p0 = s.r.kv - s.r.n;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int i0 = s.tok0 + t * p.tokens_per_tile, i1 = min(s.r.n, i0 + p.tokens_per_tile) - 1;
+      s.full_hi[t] = max(0, attn_hi(p.c, s.r.kv, p0 + i0) - s.lo) / TA_TILE;
+      s.full_lo[t] = (max(0, attn_lo(p.c, p0 + i1) - s.lo) + TA_TILE - 1) / TA_TILE;
+    }
+    s.stop = attn_hi(p.c, s.r.kv, p0 + min(s.r.n, s.tok0 + 2 * p.tokens_per_tile) - 1);
+    return true;
+  }
 };
-
-// whether some row of the row tiles that take part in tile j does not see some of its keys
-__device__ __forceinline__ bool ta_partial(const TaParams& p, const TaSeg& s, int t, int j) {
-  const int i0 = s.tok0 + t * p.tokens_per_tile, i1 = min(s.r.n, i0 + p.tokens_per_tile) - 1, p0 = s.r.kv - s.r.n;
-  const int k0 = s.lo + j * TA_TILE;
-  return k0 + TA_TILE > attn_hi(p.c, s.r.kv, p0 + i0) || k0 < attn_lo(p.c, p0 + i1);
-}
 
 template <int D>
 __global__ void __launch_bounds__(TA_THREADS, 1)
@@ -176,18 +243,23 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
   auto clean = [&](int s) { return bars + 8u * (2 * STAGES + s); };
   auto pairbar = [&](int which, int t) { return bars + 8u * (3 * STAGES + 2 * which + t); };
-  enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5 };
-  const uint32_t tmem_slot = bars + 8u * (3 * STAGES + 12);
+  enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5, P_HALF = 6 };
+  auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 14 + (i & (TA_SEGS - 1))); };
+  auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 14 + TA_SEGS + (i & (TA_SEGS - 1))); };
+  const uint32_t tmem_slot = bars + 8u * Sh::BARS;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(base_g + (tmem_slot - base));
   uint8_t* list = base_g + (2 + STAGES) * TB + Sh::BARS * 8 + 64;
-  long long* l_units = reinterpret_cast<long long*>(list);
-  int* l_req = reinterpret_cast<int*>(list + kWideMaxRequests * 8);
+  int* l_units = reinterpret_cast<int*>(list);
+  int* l_req = l_units + kWideMaxRequests;
   int* l_items = l_req + kWideMaxRequests;
-  __shared__ int s_n;
+  __shared__ int s_n, s_over;
+  __shared__ unsigned long long s_kv;              // keys of this kernel's requests
+
   __shared__ int s_warp_n[TA_THREADS / 32], s_warp_i[TA_THREADS / 32];
   __shared__ long long s_warp_u[TA_THREADS / 32];
   __shared__ int s_odd[8];         // segment number + 1 where a value was taken out of V
   __shared__ int s_join[2];
+  __shared__ TaSeg s_seg[TA_SEGS];
   __shared__ JoinShared s_list;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -198,6 +270,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   {
     int n_before = 0, i_before = 0;
     long long u_before = 0;
+    if (tid == 0) s_kv = 0;
+    __syncthreads();
     for (int b0 = 0; b0 < c.B; b0 += TA_THREADS) {
       const int b = b0 + tid;
       int take = 0, items = 0;
@@ -206,6 +280,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         const ReqView r = attn_request(c, b);
         if ((long long)r.n * c.G > p.narrow_rows) {
           take = 1;
+          atomicAdd(&s_kv, (unsigned long long)r.kv);
           const int np = ta_pairs(p, r);
           items = np * hkv;
           int nt[2], lo;
@@ -233,30 +308,38 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (take) {
         l_req[n_before + ni - 1] = b;
         l_items[n_before + ni - 1] = i_before + ii;
-        l_units[n_before + ni - 1] = u_before + ui;
+        l_units[n_before + ni - 1] = (int)min(u_before + ui, 0x7fffffffLL);
       }
       n_before = n_all; i_before = i_all; u_before = u_all;
       __syncthreads();
     }
-    if (tid == 0) s_n = n_before;
+    if (tid == 0) { s_n = n_before; s_over = u_before > 0x7fffffffLL; }
     if (tid < 8) s_odd[tid] = 0;
   }
   __syncthreads();
   TaWalk walk;
   walk.n = s_n;
   walk.req = l_req; walk.items = l_items; walk.units = l_units;
-  walk.k = 0; walk.u = walk.u1 = 0; walk.total = walk.shares = 1; walk.whole = true;
   bool some = walk.n > 0;
+  if (some && s_over) {     // 2^31 key tiles and more: the lengths cannot be meant
+    if (tid == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
+    some = false;
+  }
   if (some) {
-    walk.whole = l_items[walk.n - 1] >= 4 * (int)gridDim.x;
     walk.total = l_units[walk.n - 1];
-    walk.shares = min((long long)gridDim.x, walk.total);
-    if (!walk.whole) {
-      if ((long long)blockIdx.x >= walk.shares) some = false;
-      else {
-        walk.u = walk.total * blockIdx.x / walk.shares;
-        walk.u1 = walk.total * (blockIdx.x + 1) / walk.shares;
-      }
+    const int grid = (int)gridDim.x;
+    // With several items per SM and all keys and values in the L2 (126 MB), whole items are dealt out, the long ones first.
+    // Otherwise the line of all key tiles is cut into equal shares, in up to three rounds: the CTAs of a round work on a
+    // contiguous part of the line, so that fewer key heads are streamed at a time.
+    const long long bytes = (long long)s_kv * hkv * D * 4;
+    walk.dealt = l_items[walk.n - 1] >= 4 * grid && bytes <= TA_L2_BYTES;
+    const int rounds = (int)min(min((long long)kWideRounds, bytes / TA_L2_BYTES + 1), max(1LL, (long long)walk.total / (256LL * grid)));
+    walk.shares = min(grid * rounds, walk.total);
+    walk.share = (int)blockIdx.x;
+    walk.u = walk.u1 = 0;
+    if (!walk.dealt) {
+      some = walk.share < walk.shares;
+      if (some) { walk.u = walk.begin(walk.share); walk.u1 = walk.begin(walk.share + 1); }
     }
   }
   if (!some) {
@@ -270,10 +353,12 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // count of the stage's turns in step (a parity wait cannot tell turns apart that are two or more behind)
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), s & 1 ? 3 : 1); mbar_init(clean(s), 64); }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 128);
+      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 128); mbar_init(pairbar(P_HALF, t), 128);
       mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 128);
       mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1);
     }
+    // readers of a segment: the MMA thread, the two cleaning warps, the eight softmax warps
+    for (int i = 0; i < TA_SEGS; ++i) { mbar_init(seg_full(i), 1); mbar_init(seg_empty(i), 11); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -286,33 +371,55 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   const uint32_t tmem = *tmem_slot_g;
   const uint32_t tS = tmem, tO = tmem + 256;    // S (and P): 2 x 128 columns, O: 2 x D columns
 
-  TaSeg sg;
+  // The next segment, for every role but the loads; `n` counts them.  false: there is none, or a wait has run out.
+  auto take = [&](TaSeg& sg, int n, bool& ok) {
+    ok = mbar_wait(seg_full(n), (uint32_t)(n / TA_SEGS) & 1u, c.status, p.wait_limit);
+    if (!ok) return false;
+    sg = s_seg[n & (TA_SEGS - 1)];
+    return sg.valid != 0;
+  };
+  // registers: 384 threads x 168 at launch = 128 x 88 + 256 x 208
+  if (warp >= 8) {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp == 8) {
     // ------------------------------------------------------------------------------------------------ loads (TMA)
     const int boxes = TA_TILE / p.box_keys;
     const uint32_t box_bytes = (uint32_t)p.box_keys * 128u;
     const uint32_t q_bytes = (uint32_t)(p.tokens_per_tile * c.G) * D * 2;
-    uint32_t it = 0, uq[2] = {0, 0};
+    uint32_t it = 0, uq0 = 0, uq1 = 0;
     bool ok = true;
-    while (ok && walk.next(p, sg)) {
-      const int e = sg.last();
-      if (sg.ja >= e) continue;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      ok = ok && __all_sync(0xffffffffu, mbar_wait(bar, parity, c.status, p.wait_limit));
+      return ok;
+    };
+    TaSeg sg;
+    for (int n = 0;; ++n) {
+      const bool more = walk.next(p, sg);
+      if (!wait(seg_empty(n), ((uint32_t)(n / TA_SEGS) & 1u) ^ 1u)) break;
+      if (lane == 0) {
+        sg.valid = more;
+        s_seg[n & (TA_SEGS - 1)] = sg;
+        mbar_arrive(seg_full(n));
+      }
+      if (!more) break;
+      const int e = sg.last_tile();
       for (int j = sg.ja; j < e && ok; ++j) {
         // lane i < boxes: page of the tile's i-th box; one past the cache (a box of zeros) behind the request's keys
         int page = c.cache.n_pages, entry = 0;
         const int key = sg.lo + j * TA_TILE + lane * p.box_keys;
         if (lane < boxes && key < sg.r.kv) {
-          page = __ldg(c.table + (long long)sg.b * c.width + key / c.cache.page_size);
-          entry = key % c.cache.page_size;
+          const int x = fast_div(key, c.cache.page_size, p.div_page);
+          page = __ldg(c.table + (long long)sg.b * c.width + x);
+          entry = key - x * c.cache.page_size;
           if (page < 0 || page >= c.cache.n_pages) {
             atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
             page = c.cache.n_pages;
           }
         }
-#pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++it) {
           const int s = it % STAGES;
-          if (!__all_sync(0xffffffffu, mbar_wait(empty(s), ((it / STAGES) & 1u) ^ 1u, c.status, p.wait_limit))) { ok = false; break; }
+          if (!wait(empty(s), ((it / STAGES) & 1u) ^ 1u)) break;
           if (lane == 0) mbar_arrive_expect_tx(full(s), TB);
           __syncwarp();
           if (lane < boxes) {
@@ -321,124 +428,128 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             for (int hf = 0; hf < HALVES; ++hf)
               tma_load_4d(dst + hf * (TA_TILE * 128), kv ? &tm_v : &tm_k, full(s), hf * 64, entry, sg.h, page);
           }
-          ++it;
           if (kv == 0 && j == sg.ja) {
-            for (int t = 0; t < 2 && ok; ++t) {
-              if (sg.ja >= sg.end(t)) continue;
-              if (!__all_sync(0xffffffffu, mbar_wait(pairbar(Q_EMPTY, t), (uq[t] & 1u) ^ 1u, c.status, p.wait_limit))) { ok = false; break; }
-              ++uq[t];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              uint32_t& uq = t ? uq1 : uq0;
+              if (sg.ja >= sg.end(t) || !wait(pairbar(Q_EMPTY, t), (uq & 1u) ^ 1u)) continue;
+              ++uq;
               if (lane == 0) {
                 mbar_arrive_expect_tx(pairbar(Q_FULL, t), q_bytes);
+#pragma unroll
                 for (int hf = 0; hf < HALVES; ++hf)
                   tma_load_3d(sQ + t * TB + hf * (TA_TILE * 128), &tm_q, pairbar(Q_FULL, t), hf * 64, sg.h * c.G,
                               sg.r.t0 + sg.tok0 + t * p.tokens_per_tile);
               }
               __syncwarp();
             }
-            if (!ok) break;
+            if (!ok) { ++it; break; }
           }
         }
       }
+      if (!ok) break;
     }
     if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
       const uint32_t lo = it > (uint32_t)STAGES ? it - STAGES : 0;
       for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % STAGES), (j / STAGES) & 1u, c.status, p.wait_limit);
-      for (int t = 0; t < 2; ++t)
-        if (uq[t]) mbar_wait(pairbar(Q_FULL, t), (uq[t] - 1) & 1u, c.status, p.wait_limit);
+      if (uq0) mbar_wait(pairbar(Q_FULL, 0), (uq0 - 1) & 1u, c.status, p.wait_limit);
+      if (uq1) mbar_wait(pairbar(Q_FULL, 1), (uq1 - 1) & 1u, c.status, p.wait_limit);
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------------------------------------------ MMA issuer
     if (lane == 0) {
       const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TA_TILE >> 3) << 17) | ((uint32_t)(TA_TILE >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TA_TILE >> 4) << 24);
-      uint32_t it = 0, ns[2] = {0, 0}, nseg[2] = {0, 0}, clean_ph = 0;
+      const uint64_t dq = smem_desc(0, 16, 1024) | ((sQ & 0x3FFFFu) >> 4), dk = smem_desc(0, 16, 1024) | ((sKV & 0x3FFFFu) >> 4),
+                     dv = smem_desc(0, TA_TILE * 128, 1024) | ((sKV & 0x3FFFFu) >> 4);
+      uint32_t it = 0, ns0 = 0, ns1 = 0, nseg0 = 0, nseg1 = 0, clean_ph = 0;
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok && !mbar_wait(bar, parity, c.status, p.wait_limit)) ok = false;
+        ok = ok && mbar_wait(bar, parity, c.status, p.wait_limit);
         return ok;
       };
       auto scores = [&](int t, int stage) {
 #pragma unroll
         for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = (uint32_t)(k >> 2) * (TA_TILE * 128) + (uint32_t)(k & 3) * 32;
-          tc_mma(tS + t * 128, smem_desc(sQ + t * TB + off, 16, 1024), smem_desc(sKV + stage * TB + off, 16, 1024), idesc_s, k ? 1u : 0u);
+          const uint32_t off = ((uint32_t)(k >> 2) * (TA_TILE * 128) + (uint32_t)(k & 3) * 32) >> 4;
+          tc_mma(tS + t * 128, dq + (uint32_t)t * (TB >> 4) + off, dk + (uint32_t)stage * (TB >> 4) + off, idesc_s, k ? 1u : 0u);
         }
         tc_commit(pairbar(S_FULL, t));
       };
-      while (ok && walk.next(p, sg)) {
-        const int e = sg.last(), e0[2] = {sg.end(0), sg.end(1)};
+      TaSeg sg;
+      for (int n = 0; ok && take(sg, n, ok); ++n) {
+        mbar_arrive(seg_empty(n));
+        const int e0 = sg.end(0), e1 = sg.end(1), e = max(e0, e1);
         if (sg.ja >= e) continue;
-        const uint32_t it0 = it;
-        auto stage_of = [&](uint32_t i) { return (int)(i % STAGES); };
-        auto phase_of = [&](uint32_t i) { return (i / STAGES) & 1u; };
-        if (!wait(full(stage_of(it0)), phase_of(it0))) break;
-        tc_fence_after();
-        for (int t = 0; t < 2; ++t) {
-          if (sg.ja >= e0[t]) continue;
-          if (!wait(pairbar(Q_FULL, t), nseg[t] & 1u)) break;
-          tc_fence_after();
-          scores(t, stage_of(it0));
-          if (sg.ja + 1 >= e0[t]) tc_commit(pairbar(Q_EMPTY, t));
-        }
-        if (!ok) break;
-        tc_commit(empty(stage_of(it0)));
-        for (int j = sg.ja; j < e && ok; ++j) {
-          const uint32_t iv = it0 + 2 * (uint32_t)(j - sg.ja) + 1, ik = iv + 1;   // V of tile j, K of tile j + 1
-          bool v_seen = false, k_seen = false;
-          const bool dirty = (j < e0[0] && ta_partial(p, sg, 0, j)) || (j < e0[1] && ta_partial(p, sg, 1, j));
+        {
+          const int s = it % STAGES;
+          wait(full(s), (it / STAGES) & 1u);
+#pragma unroll
           for (int t = 0; t < 2; ++t) {
-            if (j >= e0[t]) continue;
-            if (!v_seen) {
-              if (!wait(full(stage_of(iv)), phase_of(iv))) break;
-              if (dirty) {
-                const int s = stage_of(iv);
-                if (!wait(clean(s), (clean_ph >> s) & 1u)) break;
-                clean_ph ^= 1u << s;
-              }
-              v_seen = true;
-            }
-            if (!wait(pairbar(P_READY, t), ns[t] & 1u)) break;
-            ++ns[t];
-            if (j == sg.ja && !wait(pairbar(O_FREE, t), (nseg[t] & 1u) ^ 1u)) break;
+            const int et = t ? e1 : e0;
+            if (sg.ja >= et || !wait(pairbar(Q_FULL, t), (t ? nseg1 : nseg0) & 1u)) continue;
+            tc_fence_after();
+            scores(t, s);
+            if (sg.ja + 1 >= et) tc_commit(pairbar(Q_EMPTY, t));
+          }
+          if (!ok) break;
+          tc_commit(empty(s));
+        }
+        for (int j = sg.ja; j < e && ok; ++j, it += 2) {
+          const int sv = (it + 1) % STAGES, sk = (it + 2) % STAGES;          // V of tile j, K of tile j + 1
+          if (!wait(full(sv), ((it + 1) / STAGES) & 1u)) break;
+          if (sg.dirty(j)) {
+            if (!wait(clean(sv), (clean_ph >> sv) & 1u)) break;
+            clean_ph ^= 1u << sv;
+          }
+          if (j + 1 < e && !wait(full(sk), ((it + 2) / STAGES) & 1u)) break;
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const int et = t ? e1 : e0;
+            uint32_t &ns = t ? ns1 : ns0, &nseg = t ? nseg1 : nseg0;
+            if (j >= et || !ok) continue;
+            // the first 64 keys' weights, then the rest
+            if (!wait(pairbar(P_HALF, t), ns & 1u)) continue;
+            if (j == sg.ja && !wait(pairbar(O_FREE, t), (nseg & 1u) ^ 1u)) continue;
+            tc_fence_after();
+            auto weighted = [&](int k) {
+              tc_mma_ta(tO + t * D, tS + t * 128 + k * 8, dv + (uint32_t)sv * (TB >> 4) + (uint32_t)k * 128u, idesc_o, (j > sg.ja || k) ? 1u : 0u);
+            };
+#pragma unroll
+            for (int k = 0; k < TA_TILE / 32; ++k) weighted(k);
+            if (!wait(pairbar(P_READY, t), ns & 1u)) continue;
+            ++ns;
             tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < TA_TILE / 16; ++k)
-              tc_mma_ta(tO + t * D, tS + t * 128 + k * 8, smem_desc(sKV + stage_of(iv) * TB + k * 2048, TA_TILE * 128, 1024), idesc_o,
-                        (j > sg.ja || k) ? 1u : 0u);
-            if (j + 1 == e0[t]) { tc_commit(pairbar(O_FULL, t)); ++nseg[t]; }
+            for (int k = TA_TILE / 32; k < TA_TILE / 16; ++k) weighted(k);
+            if (j + 1 == et) { tc_commit(pairbar(O_FULL, t)); ++nseg; }
             else {
-              if (!k_seen) {
-                if (!wait(full(stage_of(ik)), phase_of(ik))) break;
-                tc_fence_after();
-                k_seen = true;
-              }
-              scores(t, stage_of(ik));
-              if (j + 2 >= e0[t]) tc_commit(pairbar(Q_EMPTY, t));
+              scores(t, sk);
+              if (j + 2 >= et) tc_commit(pairbar(Q_EMPTY, t));
             }
           }
           if (!ok) break;
-          tc_commit(empty(stage_of(iv)));
-          if (j + 1 < e) tc_commit(empty(stage_of(ik)));
+          tc_commit(empty(sv));
+          if (j + 1 < e) tc_commit(empty(sk));
         }
-        it = it0 + 2 * (uint32_t)(e - sg.ja);
       }
     }
-  } else if (warp >= 10) {
+  } else {
     // ------------------------------------------------------------------------------------------------ V cleaning
     const int ct = tid - 320;
     uint32_t it = 0;
-    int seg = 0;
     bool ok = true;
-    for (; ok && walk.next(p, sg); ++seg) {
-      const int e = sg.last();
-      const int p0 = sg.r.kv - sg.r.n;
-      // keys from here on are seen by no row of the pair
-      const int stop = attn_hi(c, sg.r.kv, p0 + min(sg.r.n, sg.tok0 + 2 * p.tokens_per_tile) - 1);
+    TaSeg sg;
+    for (int n = 0; ok; ++n) {
+      if (!__all_sync(0xffffffffu, take(sg, n, ok))) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(n));
+      const int e = sg.last_tile();
       for (int j = sg.ja; j < e; ++j, it += 2) {
         const uint32_t iv = it + 1;
         const int s = iv % STAGES;
         if (!__all_sync(0xffffffffu, mbar_wait(full(s), (iv / STAGES) & 1u, c.status, p.wait_limit))) { ok = false; break; }
-        if (!((j < sg.end(0) && ta_partial(p, sg, 0, j)) || (j < sg.end(1) && ta_partial(p, sg, 1, j)))) {
+        if (!sg.dirty(j)) {
           if (lane == 0) mbar_arrive(empty(s));
           continue;
         }
@@ -448,34 +559,35 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         for (int i = ct; i < TB / 16; i += 64) {
           uint4* w = reinterpret_cast<uint4*>(v + i * 16);
           const int key = k0 + ((i >> 3) & (TA_TILE - 1));        // [half][128 keys][128 bytes]
-          if (key >= stop) { *w = make_uint4(0, 0, 0, 0); continue; }
+          if (key >= sg.stop) { *w = make_uint4(0, 0, 0, 0); continue; }
           uint4 x = *w;
-          uint32_t* y = reinterpret_cast<uint32_t*>(&x);
-          bool hit = false;
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            if ((y[q] & 0x7f80u) == 0x7f80u) { y[q] &= 0xffff0000u; hit = true; }
-            if ((y[q] & 0x7f800000u) == 0x7f800000u) { y[q] &= 0x0000ffffu; hit = true; }
+          if (bf16x2_odd(x.x) || bf16x2_odd(x.y) || bf16x2_odd(x.z) || bf16x2_odd(x.w)) {
+            *w = make_uint4(bf16x2_clean(x.x), bf16x2_clean(x.y), bf16x2_clean(x.z), bf16x2_clean(x.w));
+            odd = true;
           }
-          if (hit) { *w = x; odd = true; }
         }
-        if (odd) s_odd[seg & 7] = seg + 1;
+        if (odd) s_odd[n & 7] = n + 1;
         fence_async_proxy();
         mbar_arrive(clean(s));
         __syncwarp();
         if (lane == 0) mbar_arrive(empty(s));
       }
     }
+  }
   } else {
     // ------------------------------------------------------------------------------------------------ softmax, output
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tSr = tS + t * 128 + lanes, tOr = tO + t * D + lanes;
     const int tok_in = row / c.G, head_in = row - tok_in * c.G;
     uint32_t ns = 0, nseg = 0;
-    int seg = 0;
     bool ok = true;
-    for (; ok && walk.next(p, sg); ++seg) {
+    TaSeg sg;
+    for (int n = 0; ok; ++n) {
+      if (!__all_sync(0xffffffffu, take(sg, n, ok))) break;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(n));
       const int e = sg.end(t), p0 = sg.r.kv - sg.r.n;
       const int tok = sg.tok0 + t * p.tokens_per_tile + tok_in;
       const bool real = tok_in < p.tokens_per_tile && tok < sg.r.n;
@@ -491,24 +603,24 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_ld_wait();
 #pragma unroll
         for (int q = 0; q < 4; ++q) tc_ready32(s + q * 32);
-        if (ta_partial(p, sg, t, j)) {
+        if (t ? sg.partial(1, j) : sg.partial(0, j)) {
           const int k0 = sg.lo + j * TA_TILE, h_ = hi - k0, l_ = lo - k0;
 #pragma unroll
           for (int i = 0; i < 128; ++i)
             if (i >= h_ || i < l_) s[i] = 0xff800000u;
         }
+        // maximum, NaNs included: a NaN among the scores makes all weights of the row NaN
         float mx[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = __uint_as_float(s[q]);
+        for (int q = 0; q < 4; ++q) mx[q] = max3_nan(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
 #pragma unroll
-        for (int i = 4; i < 128; i += 8) {
+        for (int i = 12; i + 8 <= 128; i += 8) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            mx[q] = fmaxf(mx[q], __uint_as_float(s[i + q]));
-            if (i + 4 + q < 128) mx[q] = fmaxf(mx[q], __uint_as_float(s[i + 4 + q]));
-          }
+          for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(s[i + q]), __uint_as_float(s[i + 4 + q]));
         }
-        const float mt = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale2;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(s[124 + q]), mx[q]);
+        const float mt = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]) * p.scale2;
         const bool grow = mt > m + TA_SLACK;
         if (__any_sync(0xffffffffu, grow)) {
           const float mn = grow ? mt : m;
@@ -526,25 +638,28 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
         }
-        const float base = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        const float base = mt != mt || mt == INFINITY ? __int_as_float(0x7fc00000) : m == -INFINITY ? 0.f : m;
+        const uint64_t scale2x2 = pack2(p.scale2, p.scale2), base2 = pack2(-base, -base);
+        uint64_t sum2[2] = {0, 0};
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           uint32_t w[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
-            const float a = ta_exp2(fmaf(__uint_as_float(s[q * 64 + 2 * i]), p.scale2, -base));
-            const float b = ta_exp2(fmaf(__uint_as_float(s[q * 64 + 2 * i + 1]), p.scale2, -base));
-            sum[2 * (i & 1)] += a;
-            sum[2 * (i & 1) + 1] += b;
-            w[i] = pack_bf16x2(a, b);
+            const uint64_t x = fma2(pack2u(s[q * 64 + 2 * i], s[q * 64 + 2 * i + 1]), scale2x2, base2);
+            // a quarter of the exponentials on the FMA pipe: the others alone keep the special-function unit as busy as the
+            // products keep the tensor pipe
+            const uint64_t e = (i & 3) == 3 ? exp2_fma2(x) : pack2(ta_exp2(lo2(x)), ta_exp2(hi2(x)));
+            sum2[i & 1] = add2(sum2[i & 1], e);
+            w[i] = pack_bf16x2(lo2(e), hi2(e));
           }
           tc_st32(tSr + q * 32, w);
+          tc_st_wait();
+          tc_fence_before();
+          mbar_arrive(pairbar(q == 0 ? P_HALF : P_READY, t));
         }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        tc_st_wait();
-        tc_fence_before();
-        mbar_arrive(pairbar(P_READY, t));
+        sum2[0] = add2(sum2[0], sum2[1]);
+        l += lo2(sum2[0]) + hi2(sum2[0]);
       }
       if (!ok) break;
       const bool worked = sg.ja < e;
@@ -553,23 +668,12 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ++nseg;
         tc_fence_after();
       }
-      const bool whole = sg.ja == 0 && sg.jb == sg.tiles;
-      const bool odd = s_odd[seg & 7] == seg + 1;
+      // a row that has seen a score has l >= 1: the largest weight is at least 1 by the choice of m.  Less means none (the
+      // polynomial's smallest weight is not zero)
+      if (l < 0.5f) l = 0.f;
+      const bool odd = s_odd[n & 7] == n + 1;
       const int head = sg.h * c.G + head_in;
       const float inv = l == 0.f ? 0.f : 1.f / l;
-      int first = 0, last = 0, slot = 0;
-      if (!whole) {
-        auto share_of = [&](long long u) {
-          long long x = u * walk.shares / walk.total;
-          while (walk.total * (x + 1) / walk.shares <= u) ++x;
-          while (walk.total * x / walk.shares > u) --x;
-          return (int)x;
-        };
-        first = share_of(sg.first_unit);
-        last = share_of(sg.first_unit + sg.tiles - 1);
-        // a share's first stretch has slot 0, its last slot 1
-        slot = 2 * (int)blockIdx.x + (walk.total * blockIdx.x / walk.shares == sg.first_unit + sg.ja ? 0 : 1);
-      }
 #pragma unroll 1
       for (int q = 0; q < D / 32; ++q) {
         uint32_t o[32];
@@ -582,8 +686,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (odd && real) {
           // rare: values that were taken out of V go to the rows that see their key
-          for (int j = sg.ja; j < sg.last(); ++j) {
-            if (!((j < sg.end(0) && ta_partial(p, sg, 0, j)) || (j < sg.end(1) && ta_partial(p, sg, 1, j)))) continue;
+          for (int j = sg.ja; j < sg.last_tile(); ++j) {
+            if (!sg.dirty(j)) continue;
             const int k0 = sg.lo + j * TA_TILE;
             for (int key = max(k0, lo); key < min(k0 + TA_TILE, hi); ++key) {
               const int page = __ldg(c.table + (long long)sg.b * c.width + key / c.cache.page_size);
@@ -598,7 +702,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
         }
-        if (whole) {
+        if (sg.whole) {
           if (real) {
             uint4* out = reinterpret_cast<uint4*>(c.out + (long long)(sg.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + q * 32);
 #pragma unroll
@@ -611,27 +715,26 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
         } else {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + (long long)(slot * 2 + t) * D * 128);
+          float4* dst = reinterpret_cast<float4*>(p.part_o + (long long)(sg.slot * 2 + t) * D * 128);
 #pragma unroll
           for (int i = 0; i < 8; ++i)
             dst[(q * 8 + i) * 128 + row] = make_float4(__uint_as_float(o[4 * i]), __uint_as_float(o[4 * i + 1]),
                                                        __uint_as_float(o[4 * i + 2]), __uint_as_float(o[4 * i + 3]));
         }
       }
-      if (whole) {
+      if (sg.whole) {
         if (real && c.lse) c.lse[(long long)(sg.r.t0 + tok) * c.H + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * TA_LN2;
         continue;
       }
-      reinterpret_cast<float2*>(p.part_ml)[(slot * 2 + t) * 128 + row] = make_float2(m, l);
+      reinterpret_cast<float2*>(p.part_ml)[(sg.slot * 2 + t) * 128 + row] = make_float2(m, l);
       __threadfence();
-      asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
-      if (row == 0) s_join[t] = atomicAdd(p.counters + 2 * first + t, 1u) == (uint32_t)(last - first);
-      asm volatile("bar.sync %0, 128;" ::"r"(1 + t) : "memory");
+      if (t == 0) asm volatile("bar.sync 1, 128;" ::: "memory"); else asm volatile("bar.sync 2, 128;" ::: "memory");
+      if (row == 0) s_join[t] = atomicAdd(p.counters + 1 + 2 * sg.first + t, 1u) == (uint32_t)(sg.last - sg.first);
+      if (t == 0) asm volatile("bar.sync 1, 128;" ::: "memory"); else asm volatile("bar.sync 2, 128;" ::: "memory");
       if (s_join[t]) {
         __threadfence();
-        // the first share's part of the item is its last stretch, unless that share begins with the item
-        const int slot0 = 2 * first + (walk.total * first / walk.shares == sg.first_unit ? 0 : 1);
-        auto part = [&](int x) { return ((x == first ? slot0 : 2 * x) * 2 + t); };
+        const int first = sg.first, last = sg.last;
+        auto part = [&](int x) { return (x == first ? sg.slot0 : 2 * x) * 2 + t; };
         float M = -INFINITY;
         for (int x = first; x <= last; ++x) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x);
         const float mb = M == -INFINITY ? 0.f : M;
@@ -642,19 +745,26 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         const float iv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll 1
-        for (int q = 0; q < D / 8; ++q) {
-          float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        for (int q = 0; q < D / 64; ++q) {                     // 64 columns at a time: 16 loads in flight
+          float4 a[16];
+#pragma unroll
+          for (int i = 0; i < 16; ++i) a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           for (int x = first; x <= last; ++x) {
             const float g = ta_exp2(__ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x - mb);
-            const float4* src = reinterpret_cast<const float4*>(p.part_o + (long long)part(x) * D * 128);
-            const float4 u = __ldcg(src + (2 * q) * 128 + row), v = __ldcg(src + (2 * q + 1) * 128 + row);
-            a.x += u.x * g; a.y += u.y * g; a.z += u.z * g; a.w += u.w * g;
-            b.x += v.x * g; b.y += v.y * g; b.z += v.z * g; b.w += v.w * g;
+            const float4* src = reinterpret_cast<const float4*>(p.part_o + (long long)part(x) * D * 128) + q * 16 * 128 + row;
+            float4 v[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[i] = __ldcg(src + i * 128);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) { a[i].x += v[i].x * g; a[i].y += v[i].y * g; a[i].z += v[i].z * g; a[i].w += v[i].w * g; }
           }
-          if (real)
-            *reinterpret_cast<uint4*>(c.out + (long long)(sg.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + q * 8) =
-                make_uint4(pack_bf16x2(a.x * iv, a.y * iv), pack_bf16x2(a.z * iv, a.w * iv), pack_bf16x2(b.x * iv, b.y * iv),
-                           pack_bf16x2(b.z * iv, b.w * iv));
+          if (real) {
+            uint4* out = reinterpret_cast<uint4*>(c.out + (long long)(sg.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + q * 64);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              out[i] = make_uint4(pack_bf16x2(a[2 * i].x * iv, a[2 * i].y * iv), pack_bf16x2(a[2 * i].z * iv, a[2 * i].w * iv),
+                                  pack_bf16x2(a[2 * i + 1].x * iv, a[2 * i + 1].y * iv), pack_bf16x2(a[2 * i + 1].z * iv, a[2 * i + 1].w * iv));
+          }
         }
         if (real && c.lse) c.lse[(long long)(sg.r.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * TA_LN2;
       }
@@ -688,7 +798,7 @@ int ta_launch(const TaParams& p0, char* counters, char* scratch, cudaStream_t st
   const AttnCall& c = p.c;
   p.counters = reinterpret_cast<uint32_t*>(counters);
   p.part_ml = reinterpret_cast<float*>(scratch);
-  p.part_o = p.part_ml + (size_t)2 * kPagedMaxSms * 2 * 128 * 2;
+  p.part_o = p.part_ml + (size_t)2 * kWideMaxShares * 2 * 128 * 2;
 
   // a dimension of one entry may come with any stride: give the map one it accepts
   auto pitch = [](int64_t n, int64_t stride, int64_t other) { return (uint64_t)(n > 1 ? stride : other) * 2; };
@@ -741,7 +851,7 @@ bool tc_attention_supported(const AttnCall& c) {
 
 size_t tc_attention_scratch_bytes(int head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
-  return (size_t)2 * kPagedMaxSms * 2 * 128 * (head_dim + 2) * 4;
+  return (size_t)2 * kWideMaxShares * 2 * 128 * (head_dim + 2) * 4;
 }
 
 int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join, char* counters, char* scratch, cudaStream_t st) {
@@ -752,6 +862,7 @@ int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join
   p.narrow_rows = narrow_rows;
   p.tokens_per_tile = TA_TILE / c.G;
   p.box_keys = std::min(c.cache.page_size, TA_TILE);
+  p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
   p.wait_limit = wait_limit_cycles();
   return c.D == 64 ? ta_launch<64>(p, counters, scratch, st) : ta_launch<128>(p, counters, scratch, st);
 }
