@@ -65,15 +65,9 @@ struct TaParams {
   float* part_ml;         // [2 * shares][2][128][2]
 };
 
-__device__ __forceinline__ float ta_exp2(float x) {
+__device__ __forceinline__ float max3(float a, float b, float c) {
   float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-__device__ __forceinline__ float max3_nan(float a, float b, float c) {
-  float y;
-  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
   return y;
 }
 // two fp32 values in a 64-bit register
@@ -99,23 +93,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
   return y;
 }
-// 2^x of two values, x <= 2^7, without the special-function unit: x = n + f with n whole and |f| <= 1/2, 2^f by the polynomial of
-// degree 4 with the smallest largest relative error on that interval (2.7e-6, from a Remez exchange), n added to the exponent.
-// Below 2^-126 the result is 2^-126; NaN does not survive (the caller's maximum has caught it).
-__device__ __forceinline__ uint64_t exp2_fma2(uint64_t x) {
-  x = pack2(fmaxf(lo2(x), -126.f), fmaxf(hi2(x), -126.f));
-  const uint64_t magic = pack2(12582912.f, 12582912.f), minus_magic = pack2(-12582912.f, -12582912.f);   // 1.5 * 2^23
-  const uint64_t t = add2(x, magic);                       // n in the low bits
-  const uint64_t n = add2(t, minus_magic);
-  const uint64_t f = fma2(n, pack2(-1.f, -1.f), x);
-  uint64_t y = fma2(f, pack2(0.009570102207362652f, 0.009570102207362652f), pack2(0.05591785907745361f, 0.05591785907745361f));
-  y = fma2(y, f, pack2(0.240247443318367f, 0.240247443318367f));
-  y = fma2(y, f, pack2(0.6931217908859253f, 0.6931217908859253f));
-  y = fma2(y, f, pack2(0.9999992847442627f, 0.9999992847442627f));
-  const uint32_t a = (uint32_t)y + ((uint32_t)t << 23), b = (uint32_t)(y >> 32) + ((uint32_t)(t >> 32) << 23);
-  return pack2u(a, b);
-}
-
 // One stretch of key tiles [ja, jb) of an item, as the loading warp hands it to the others.
 struct TaSeg {
   int valid;               // 0: no more
@@ -353,8 +330,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // count of the stage's turns in step (a parity wait cannot tell turns apart that are two or more behind)
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), s & 1 ? 3 : 1); mbar_init(clean(s), 64); }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 128); mbar_init(pairbar(P_HALF, t), 128);
-      mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 128);
+      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 4); mbar_init(pairbar(P_HALF, t), 4);
+      mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 4);
       mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1);
     }
     // readers of a segment: the MMA thread, the two cleaning warps, the eight softmax warps
@@ -609,22 +586,21 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           for (int i = 0; i < 128; ++i)
             if (i >= h_ || i < l_) s[i] = 0xff800000u;
         }
-        // maximum, NaNs included: a NaN among the scores makes all weights of the row NaN
         float mx[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = max3_nan(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
+        for (int q = 0; q < 4; ++q) mx[q] = max3(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
 #pragma unroll
         for (int i = 12; i + 8 <= 128; i += 8) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(s[i + q]), __uint_as_float(s[i + 4 + q]));
+          for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(s[i + q]), __uint_as_float(s[i + 4 + q]));
         }
 #pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = max3_nan(mx[q], __uint_as_float(s[124 + q]), mx[q]);
-        const float mt = max3_nan(max3_nan(mx[0], mx[1], mx[2]), mx[3], mx[3]) * p.scale2;
+        for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(s[124 + q]), mx[q]);
+        const float mt = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * p.scale2;
         const bool grow = mt > m + TA_SLACK;
         if (__any_sync(0xffffffffu, grow)) {
           const float mn = grow ? mt : m;
-          const float f = m == mn ? 1.f : ta_exp2(m - mn);          // m = -infinity: 0
+          const float f = m == mn ? 1.f : fast_exp2(m - mn);          // m = -infinity: 0
           m = mn;
           l *= f;
           if (j > sg.ja) {
@@ -638,7 +614,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             }
           }
         }
-        const float base = mt != mt || mt == INFINITY ? __int_as_float(0x7fc00000) : m == -INFINITY ? 0.f : m;
+        const float base = m == -INFINITY ? 0.f : m;
         const uint64_t scale2x2 = pack2(p.scale2, p.scale2), base2 = pack2(-base, -base);
         uint64_t sum2[2] = {0, 0};
 #pragma unroll
@@ -647,16 +623,15 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
           for (int i = 0; i < 32; ++i) {
             const uint64_t x = fma2(pack2u(s[q * 64 + 2 * i], s[q * 64 + 2 * i + 1]), scale2x2, base2);
-            // a quarter of the exponentials on the FMA pipe: the others alone keep the special-function unit as busy as the
-            // products keep the tensor pipe
-            const uint64_t e = (i & 3) == 3 ? exp2_fma2(x) : pack2(ta_exp2(lo2(x)), ta_exp2(hi2(x)));
-            sum2[i & 1] = add2(sum2[i & 1], e);
-            w[i] = pack_bf16x2(lo2(e), hi2(e));
+            const float ea = fast_exp2(lo2(x)), eb = fast_exp2(hi2(x));
+            sum2[i & 1] = add2(sum2[i & 1], pack2(ea, eb));
+            w[i] = pack_bf16x2(ea, eb);
           }
           tc_st32(tSr + q * 32, w);
           tc_st_wait();
           tc_fence_before();
-          mbar_arrive(pairbar(q == 0 ? P_HALF : P_READY, t));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(pairbar(q == 0 ? P_HALF : P_READY, t));
         }
         sum2[0] = add2(sum2[0], sum2[1]);
         l += lo2(sum2[0]) + hi2(sum2[0]);
@@ -668,9 +643,6 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         ++nseg;
         tc_fence_after();
       }
-      // a row that has seen a score has l >= 1: the largest weight is at least 1 by the choice of m.  Less means none (the
-      // polynomial's smallest weight is not zero)
-      if (l < 0.5f) l = 0.f;
       const bool odd = s_odd[n & 7] == n + 1;
       const int head = sg.h * c.G + head_in;
       const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -679,7 +651,11 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         uint32_t o[32];
         if (worked) {
           tc_ld32(tOr + q * 32, o);
-          if (q == D / 32 - 1) { tc_fence_before(); mbar_arrive(pairbar(O_FREE, t)); }
+          if (q == D / 32 - 1) {
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pairbar(O_FREE, t));
+          }
         } else {
 #pragma unroll
           for (int i = 0; i < 32; ++i) o[i] = 0;
@@ -741,7 +717,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         float L = 0.f;
         for (int x = first; x <= last; ++x) {
           const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row);
-          L += ml.y * ta_exp2(ml.x - mb);
+          L += ml.y * fast_exp2(ml.x - mb);
         }
         const float iv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll 1
@@ -750,7 +726,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
           for (int i = 0; i < 16; ++i) a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
           for (int x = first; x <= last; ++x) {
-            const float g = ta_exp2(__ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x - mb);
+            const float g = fast_exp2(__ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x - mb);
             const float4* src = reinterpret_cast<const float4*>(p.part_o + (long long)part(x) * D * 128) + q * 16 * 128 + row;
             float4 v[16];
 #pragma unroll
