@@ -46,7 +46,7 @@ template <int D>
 struct TaShape {
   static constexpr int STAGES = D == 64 ? 6 : 4;            // K and V tiles take turns; even, so V keeps to odd stages
   static constexpr int TILE_BYTES = TA_TILE * D * 2;        // one Q, K or V tile
-  static constexpr int BARS = 3 * STAGES + 14 + 2 * TA_SEGS;   // full, empty, clean; seven for each row tile; the segments' two
+  static constexpr int BARS = 3 * STAGES + 14 + 2 * TA_SEGS + 2;   // full, empty, clean; seven for each row tile; the segments' two; join
   static constexpr int LIST_BYTES = kWideMaxRequests * 12;
   static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + LIST_BYTES + BARS * 8 + 64 + 1024;
 };
@@ -223,6 +223,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5, P_HALF = 6 };
   auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 14 + (i & (TA_SEGS - 1))); };
   auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 14 + TA_SEGS + (i & (TA_SEGS - 1))); };
+  auto joinbar = [&](int t) { return bars + 8u * (3 * STAGES + 14 + 2 * TA_SEGS + t); };
   const uint32_t tmem_slot = bars + 8u * Sh::BARS;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(base_g + (tmem_slot - base));
   uint8_t* list = base_g + (2 + STAGES) * TB + Sh::BARS * 8 + 64;
@@ -332,7 +333,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     for (int t = 0; t < 2; ++t) {
       mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 4); mbar_init(pairbar(P_HALF, t), 4);
       mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 4);
-      mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1);
+      mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1); mbar_init(joinbar(t), 4);
     }
     // readers of a segment: the MMA thread, the two cleaning warps, the eight softmax warps
     for (int i = 0; i < TA_SEGS; ++i) { mbar_init(seg_full(i), 1); mbar_init(seg_empty(i), 11); }
@@ -558,20 +559,25 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tSr = tS + t * 128 + lanes, tOr = tO + t * D + lanes;
     const int tok_in = row / c.G, head_in = row - tok_in * c.G;
-    uint32_t ns = 0, nseg = 0;
+    uint32_t ns = 0, nseg = 0, nj = 0;
     bool ok = true;
-    TaSeg sg;
+    auto wait = [&](uint32_t bar, uint32_t parity) {     // one answer for the warp
+      ok = __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, c.status, p.wait_limit));
+      return ok;
+    };
     for (int n = 0; ok; ++n) {
-      if (!__all_sync(0xffffffffu, take(sg, n, ok))) break;
-      __syncwarp();
-      if (lane == 0) mbar_arrive(seg_empty(n));
+      // the segment is read where it lies: only what the key loop needs stays in registers
+      if (!wait(seg_full(n), (uint32_t)(n / TA_SEGS) & 1u)) break;
+      const TaSeg& sg = s_seg[n & (TA_SEGS - 1)];
+      if (!sg.valid) break;
       const int e = sg.end(t), p0 = sg.r.kv - sg.r.n;
       const int tok = sg.tok0 + t * p.tokens_per_tile + tok_in;
       const bool real = tok_in < p.tokens_per_tile && tok < sg.r.n;
       const int hi = real ? attn_hi(c, sg.r.kv, p0 + tok) : sg.r.kv, lo = real ? attn_lo(c, p0 + tok) : 0;
+      const int full_lo = t ? sg.full_lo[1] : sg.full_lo[0], full_hi = t ? sg.full_hi[1] : sg.full_hi[0], ja = sg.ja, seg_lo = sg.lo;
       float m = -INFINITY, l = 0.f;
-      for (int j = sg.ja; j < e; ++j) {
-        if (!mbar_wait(pairbar(S_FULL, t), ns & 1u, c.status, p.wait_limit)) { ok = false; break; }
+      for (int j = ja; j < e; ++j) {
+        if (!wait(pairbar(S_FULL, t), ns & 1u)) break;
         ++ns;
         tc_fence_after();
         uint32_t s[128];
@@ -580,8 +586,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_ld_wait();
 #pragma unroll
         for (int q = 0; q < 4; ++q) tc_ready32(s + q * 32);
-        if (t ? sg.partial(1, j) : sg.partial(0, j)) {
-          const int k0 = sg.lo + j * TA_TILE, h_ = hi - k0, l_ = lo - k0;
+        if (j < full_lo || j >= full_hi) {
+          const int k0 = seg_lo + j * TA_TILE, h_ = hi - k0, l_ = lo - k0;
 #pragma unroll
           for (int i = 0; i < 128; ++i)
             if (i >= h_ || i < l_) s[i] = 0xff800000u;
@@ -603,7 +609,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           const float f = m == mn ? 1.f : fast_exp2(m - mn);          // m = -infinity: 0
           m = mn;
           l *= f;
-          if (j > sg.ja) {
+          if (j > ja) {
 #pragma unroll 1
             for (int q = 0; q < D / 32; ++q) {
               uint32_t o[32];
@@ -637,9 +643,9 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         l += lo2(sum2[0]) + hi2(sum2[0]);
       }
       if (!ok) break;
-      const bool worked = sg.ja < e;
+      const bool worked = ja < e;
       if (worked) {
-        if (!mbar_wait(pairbar(O_FULL, t), nseg & 1u, c.status, p.wait_limit)) { ok = false; break; }
+        if (!wait(pairbar(O_FULL, t), nseg & 1u)) break;
         ++nseg;
         tc_fence_after();
       }
@@ -700,13 +706,20 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       if (sg.whole) {
         if (real && c.lse) c.lse[(long long)(sg.r.t0 + tok) * c.H + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * TA_LN2;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(seg_empty(n));
         continue;
       }
       reinterpret_cast<float2*>(p.part_ml)[(sg.slot * 2 + t) * 128 + row] = make_float2(m, l);
       __threadfence();
-      if (t == 0) asm volatile("bar.sync 1, 128;" ::: "memory"); else asm volatile("bar.sync 2, 128;" ::: "memory");
+      // the row tile's warps: parts written, then the news of who came last (bounded waits, like every other)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(joinbar(t));
+      if (!wait(joinbar(t), nj++ & 1u)) break;
       if (row == 0) s_join[t] = atomicAdd(p.counters + 1 + 2 * sg.first + t, 1u) == (uint32_t)(sg.last - sg.first);
-      if (t == 0) asm volatile("bar.sync 1, 128;" ::: "memory"); else asm volatile("bar.sync 2, 128;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) mbar_arrive(joinbar(t));
+      if (!wait(joinbar(t), nj++ & 1u)) break;
       if (s_join[t]) {
         __threadfence();
         const int first = sg.first, last = sg.last;
@@ -744,6 +757,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         }
         if (real && c.lse) c.lse[(long long)(sg.r.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * TA_LN2;
       }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(seg_empty(n));
     }
   }
 
