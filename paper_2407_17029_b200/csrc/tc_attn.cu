@@ -240,7 +240,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ TaSeg s_seg[TA_SEGS];
   __shared__ JoinShared s_list;
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const AttnCall& c = p.c;
   const int hkv = c.cache.kv_heads;
 
@@ -435,81 +435,116 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
   } else if (warp == 9) {
     // ------------------------------------------------------------------------------------------------ MMA issuer
-    if (lane == 0) {
+    // The whole warp walks the loop on values that are the same in every lane, and one elected lane issues: the operands
+    // of an MMA then lie in uniform registers, and an issue takes 12 cycles instead of 60 (one lane's private loop), less
+    // than the MMA's 64.
+    {
+      auto uni = [](int x) { return __shfl_sync(0xffffffffu, x, 0); };
+      uint32_t leader;
+      asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(leader));
+      const uint32_t uQ = uni((int)sQ), uKV = uni((int)sKV), ub = uni((int)bars), uT = uni((int)tmem);
+      auto ufull = [&](int i) { return ub + 8u * i; };
+      auto uempty = [&](int i) { return ub + 8u * (STAGES + i); };
+      auto uclean = [&](int i) { return ub + 8u * (2 * STAGES + i); };
+      auto upair = [&](int which, int t) { return ub + 8u * (3 * STAGES + 2 * which + t); };
       const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TA_TILE >> 3) << 17) | ((uint32_t)(TA_TILE >> 4) << 24);
       const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TA_TILE >> 4) << 24);
-      const uint64_t dq = smem_desc(0, 16, 1024) | ((sQ & 0x3FFFFu) >> 4), dk = smem_desc(0, 16, 1024) | ((sKV & 0x3FFFFu) >> 4),
-                     dv = smem_desc(0, TA_TILE * 128, 1024) | ((sKV & 0x3FFFFu) >> 4);
-      uint32_t it = 0, ns0 = 0, ns1 = 0, nseg0 = 0, nseg1 = 0, clean_ph = 0;
+      const uint64_t dq = smem_desc(0, 16, 1024) | ((uQ & 0x3FFFFu) >> 4), dk = smem_desc(0, 16, 1024) | ((uKV & 0x3FFFFu) >> 4),
+                     dv = smem_desc(0, TA_TILE * 128, 1024) | ((uKV & 0x3FFFFu) >> 4);
+      uint32_t ns0 = 0, ns1 = 0, nseg0 = 0, nseg1 = 0, clean_ph = 0, full_ph = 0;   // phases of the ring's stages, a bit each
+      int sk = 0;                                             // stage of the next K tile; V's is the one behind it
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        ok = ok && mbar_wait(bar, parity, c.status, p.wait_limit);
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, c.status, p.wait_limit));
         return ok;
       };
-      auto scores = [&](int t, int stage) {
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint32_t off = ((uint32_t)(k >> 2) * (TA_TILE * 128) + (uint32_t)(k & 3) * 32) >> 4;
-          tc_mma(tS + t * 128, dq + (uint32_t)t * (TB >> 4) + off, dk + (uint32_t)stage * (TB >> 4) + off, idesc_s, k ? 1u : 0u);
-        }
-        tc_commit(pairbar(S_FULL, t));
+      auto wait_full = [&](int s) {
+        const bool w = wait(ufull(s), (full_ph >> s) & 1u);
+        full_ph ^= 1u << s;
+        return w;
       };
-      TaSeg sg;
-      for (int n = 0; ok && take(sg, n, ok); ++n) {
-        mbar_arrive(seg_empty(n));
-        const int e0 = sg.end(0), e1 = sg.end(1), e = max(e0, e1);
-        if (sg.ja >= e) continue;
-        {
-          const int s = it % STAGES;
-          wait(full(s), (it / STAGES) & 1u);
+      auto scores = [&](int t, int stage) {
+        const uint64_t a = dq + (uint32_t)t * (TB >> 4), b = dk + (uint32_t)stage * (TB >> 4);
+        if (leader) {
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            const int et = t ? e1 : e0;
-            if (sg.ja >= et || !wait(pairbar(Q_FULL, t), (t ? nseg1 : nseg0) & 1u)) continue;
-            tc_fence_after();
-            scores(t, s);
-            if (sg.ja + 1 >= et) tc_commit(pairbar(Q_EMPTY, t));
+          for (int k = 0; k < D / 16; ++k) {
+            const uint32_t off = ((uint32_t)(k >> 2) * (TA_TILE * 128) + (uint32_t)(k & 3) * 32) >> 4;
+            tc_mma(uT + t * 128, a + off, b + off, idesc_s, k ? 1u : 0u);
           }
-          if (!ok) break;
-          tc_commit(empty(s));
+          tc_commit(upair(S_FULL, t));
         }
-        for (int j = sg.ja; j < e && ok; ++j, it += 2) {
-          const int sv = (it + 1) % STAGES, sk = (it + 2) % STAGES;          // V of tile j, K of tile j + 1
-          if (!wait(full(sv), ((it + 1) / STAGES) & 1u)) break;
-          if (sg.dirty(j)) {
-            if (!wait(clean(sv), (clean_ph >> sv) & 1u)) break;
+      };
+      auto commit = [&](uint32_t bar) { if (leader) tc_commit(bar); };
+      for (int n = 0;; ++n) {
+        if (!wait(seg_full(n), (uint32_t)(n / TA_SEGS) & 1u)) break;
+        const TaSeg& sg = s_seg[n & (TA_SEGS - 1)];
+        const int valid = uni(sg.valid), ja = uni(sg.ja), e0 = uni(sg.end(0)), e1 = uni(sg.end(1)), fl0 = uni(sg.full_lo[0]),
+                  fl1 = uni(sg.full_lo[1]), fh0 = uni(sg.full_hi[0]), fh1 = uni(sg.full_hi[1]), e = max(e0, e1);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(seg_empty(n));
+        if (!valid) break;
+        if (ja >= e) continue;
+        if (!wait_full(sk)) break;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const int et = t ? e1 : e0;
+          if (ja >= et || !wait(upair(Q_FULL, t), (t ? nseg1 : nseg0) & 1u)) continue;
+          tc_fence_after();
+          scores(t, sk);
+          if (ja + 1 >= et) commit(upair(Q_EMPTY, t));
+        }
+        if (!ok) break;
+        commit(uempty(sk));
+        for (int j = ja; j < e; ++j) {
+          // The issuer is at most a few MMAs ahead of the tensor pipe: what it waits for here, the pipe soon waits for too.
+          const int sv = sk + 1;                              // V of tile j
+          sk = sv + 1 == STAGES ? 0 : sv + 1;                 // K of tile j + 1
+          if (!wait_full(sv)) break;
+          if ((j < e0 && (j < fl0 || j >= fh0)) || (j < e1 && (j < fl1 || j >= fh1))) {
+            if (!wait(uclean(sv), (clean_ph >> sv) & 1u)) break;
             clean_ph ^= 1u << sv;
           }
-          if (j + 1 < e && !wait(full(sk), ((it + 2) / STAGES) & 1u)) break;
+          bool k_seen = false;
+          const uint64_t bv = dv + (uint32_t)sv * (TB >> 4);
 #pragma unroll
           for (int t = 0; t < 2; ++t) {
             const int et = t ? e1 : e0;
             uint32_t &ns = t ? ns1 : ns0, &nseg = t ? nseg1 : nseg0;
             if (j >= et || !ok) continue;
-            // the first 64 keys' weights, then the rest
-            if (!wait(pairbar(P_HALF, t), ns & 1u)) continue;
-            if (j == sg.ja && !wait(pairbar(O_FREE, t), (nseg & 1u) ^ 1u)) continue;
-            tc_fence_after();
             auto weighted = [&](int k) {
-              tc_mma_ta(tO + t * D, tS + t * 128 + k * 8, dv + (uint32_t)sv * (TB >> 4) + (uint32_t)k * 128u, idesc_o, (j > sg.ja || k) ? 1u : 0u);
+              tc_mma_ta(uT + 256 + t * D, uT + t * 128 + k * 8, bv + (uint32_t)k * 128u, idesc_o, (j > ja || k) ? 1u : 0u);
             };
+            // the first 64 keys' weights, then the rest
+            if (j == ja && !wait(upair(O_FREE, t), (nseg & 1u) ^ 1u)) continue;
+            if (!wait(upair(P_HALF, t), ns & 1u)) continue;
+            tc_fence_after();
+            if (leader) {
 #pragma unroll
-            for (int k = 0; k < TA_TILE / 32; ++k) weighted(k);
-            if (!wait(pairbar(P_READY, t), ns & 1u)) continue;
+              for (int k = 0; k < TA_TILE / 32; ++k) weighted(k);
+            }
+            if (!wait(upair(P_READY, t), ns & 1u)) continue;
             ++ns;
             tc_fence_after();
+            if (leader) {
 #pragma unroll
-            for (int k = TA_TILE / 32; k < TA_TILE / 16; ++k) weighted(k);
-            if (j + 1 == et) { tc_commit(pairbar(O_FULL, t)); ++nseg; }
+              for (int k = TA_TILE / 32; k < TA_TILE / 16; ++k) weighted(k);
+            }
+            if (j + 1 == et) { commit(upair(O_FULL, t)); ++nseg; }
             else {
+              if (!k_seen) {
+                if (!wait_full(sk)) continue;
+                tc_fence_after();
+                k_seen = true;
+              }
               scores(t, sk);
-              if (j + 2 >= et) tc_commit(pairbar(Q_EMPTY, t));
+              if (j + 2 >= et) commit(upair(Q_EMPTY, t));
             }
           }
           if (!ok) break;
-          tc_commit(empty(sv));
-          if (j + 1 < e) tc_commit(empty(sk));
+          commit(uempty(sv));
+          if (j + 1 < e) commit(uempty(sk));
         }
+        if (!ok) break;
       }
     }
   } else {
