@@ -5,9 +5,10 @@
 //   S = Q K^T          tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
 //   P = 2^(S c - m)    one thread per row; bf16 P goes back to tensor memory, over S
 //   O += P V           tcgen05.mma, A = P from tensor memory, V as an MN-major B operand, O (fp32) in tensor memory
-// m moves only when a row's maximum has grown by more than 2^8 (weights up to 2^8 are as exact as weights up to 1, and
-// l uses the same m); then O is scaled in tensor memory by the row's thread.  That is safe without a further wait: the
-// commit that announces S of tile j covers P V of tile j - 1, and P V of tile j waits for this thread.
+// m need not be the maximum: weights of 2^40 are as exact as weights of 1 (both have the same 8 and 24 bits), so m is a row's
+// maximum over its first tile and moves only when a tile's sum of weights shows that the scores have outgrown it; then O
+// is scaled in tensor memory by the row's thread.  That is safe without a further wait: the commit that announces S of tile
+// j covers P V of tile j - 1, and P V of tile j waits for this thread.
 //
 // Roles (one CTA per SM, 384 threads): warps 0-3 and 4-7 are the softmax of two row tiles that share every K and V stage
 // -- while one tile's softmax runs, the tensor core works for the other --, warp 8 loads (TMA), warp 9 issues the MMAs,
@@ -40,13 +41,14 @@ constexpr int TA_TILE = 128;            // rows per row tile, keys per key tile
 constexpr float TA_LN2 = 0.69314718055994530942f;
 constexpr long long TA_L2_BYTES = 96000000;
 constexpr int TA_SEGS = 4;              // segments handed out ahead
-constexpr float TA_SLACK = 8.0f;        // how far (in powers of two) a row's maximum may run ahead of m
+constexpr float TA_SLACK = 8.0f;        // where the maximum is looked for: how far (in powers of two) it may be ahead of m
+constexpr float TA_OUTGROWN = 1.099511627776e12f;   // 2^40: a tile's sum of weights that asks for a new m
 
 template <int D>
 struct TaShape {
   static constexpr int STAGES = D == 64 ? 6 : 4;            // K and V tiles take turns; even, so V keeps to odd stages
   static constexpr int TILE_BYTES = TA_TILE * D * 2;        // one Q, K or V tile
-  static constexpr int BARS = 3 * STAGES + 14 + 2 * TA_SEGS + 2;   // full, empty, clean; seven for each row tile; the segments' two; join
+  static constexpr int BARS = 3 * STAGES + 12 + 2 * TA_SEGS + 2;   // full, empty, clean; six for each row tile; the segments' two; join
   static constexpr int LIST_BYTES = kWideMaxRequests * 12;
   static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + LIST_BYTES + BARS * 8 + 64 + 1024;
 };
@@ -220,10 +222,10 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
   auto clean = [&](int s) { return bars + 8u * (2 * STAGES + s); };
   auto pairbar = [&](int which, int t) { return bars + 8u * (3 * STAGES + 2 * which + t); };
-  enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5, P_HALF = 6 };
-  auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 14 + (i & (TA_SEGS - 1))); };
-  auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 14 + TA_SEGS + (i & (TA_SEGS - 1))); };
-  auto joinbar = [&](int t) { return bars + 8u * (3 * STAGES + 14 + 2 * TA_SEGS + t); };
+  enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5 };
+  auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 12 + (i & (TA_SEGS - 1))); };
+  auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 12 + TA_SEGS + (i & (TA_SEGS - 1))); };
+  auto joinbar = [&](int t) { return bars + 8u * (3 * STAGES + 12 + 2 * TA_SEGS + t); };
   const uint32_t tmem_slot = bars + 8u * Sh::BARS;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(base_g + (tmem_slot - base));
   uint8_t* list = base_g + (2 + STAGES) * TB + Sh::BARS * 8 + 64;
@@ -331,7 +333,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     // count of the stage's turns in step (a parity wait cannot tell turns apart that are two or more behind)
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), s & 1 ? 3 : 1); mbar_init(clean(s), 64); }
     for (int t = 0; t < 2; ++t) {
-      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 4); mbar_init(pairbar(P_HALF, t), 4);
+      mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 4);
       mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 4);
       mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1); mbar_init(joinbar(t), 4);
     }
@@ -511,23 +513,14 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             const int et = t ? e1 : e0;
             uint32_t &ns = t ? ns1 : ns0, &nseg = t ? nseg1 : nseg0;
             if (j >= et || !ok) continue;
-            auto weighted = [&](int k) {
-              tc_mma_ta(uT + 256 + t * D, uT + t * 128 + k * 8, bv + (uint32_t)k * 128u, idesc_o, (j > ja || k) ? 1u : 0u);
-            };
-            // the first 64 keys' weights, then the rest
             if (j == ja && !wait(upair(O_FREE, t), (nseg & 1u) ^ 1u)) continue;
-            if (!wait(upair(P_HALF, t), ns & 1u)) continue;
-            tc_fence_after();
-            if (leader) {
-#pragma unroll
-              for (int k = 0; k < TA_TILE / 32; ++k) weighted(k);
-            }
             if (!wait(upair(P_READY, t), ns & 1u)) continue;
             ++ns;
             tc_fence_after();
             if (leader) {
 #pragma unroll
-              for (int k = TA_TILE / 32; k < TA_TILE / 16; ++k) weighted(k);
+              for (int k = 0; k < TA_TILE / 16; ++k)
+                tc_mma_ta(uT + 256 + t * D, uT + t * 128 + k * 8, bv + (uint32_t)k * 128u, idesc_o, (j > ja || k) ? 1u : 0u);
             }
             if (j + 1 == et) { commit(upair(O_FULL, t)); ++nseg; }
             else {
@@ -610,7 +603,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const bool real = tok_in < p.tokens_per_tile && tok < sg.r.n;
       const int hi = real ? attn_hi(c, sg.r.kv, p0 + tok) : sg.r.kv, lo = real ? attn_lo(c, p0 + tok) : 0;
       const int full_lo = t ? sg.full_lo[1] : sg.full_lo[0], full_hi = t ? sg.full_hi[1] : sg.full_hi[0], ja = sg.ja, seg_lo = sg.lo;
-      float m = -INFINITY, l = 0.f;
+      float m = real ? -INFINITY : 0.f, l = 0.f;       // rows that are none need no maximum
       for (int j = ja; j < e; ++j) {
         if (!wait(pairbar(S_FULL, t), ns & 1u)) break;
         ++ns;
@@ -627,55 +620,63 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           for (int i = 0; i < 128; ++i)
             if (i >= h_ || i < l_) s[i] = 0xff800000u;
         }
-        float mx[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = max3(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
-#pragma unroll
-        for (int i = 12; i + 8 <= 128; i += 8) {
-#pragma unroll
-          for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(s[i + q]), __uint_as_float(s[i + 4 + q]));
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(s[124 + q]), mx[q]);
-        const float mt = max3(max3(mx[0], mx[1], mx[2]), mx[3], mx[3]) * p.scale2;
-        const bool grow = mt > m + TA_SLACK;
-        if (__any_sync(0xffffffffu, grow)) {
-          const float mn = grow ? mt : m;
-          const float f = m == mn ? 1.f : fast_exp2(m - mn);          // m = -infinity: 0
-          m = mn;
-          l *= f;
-          if (j > ja) {
+        // The weights are taken with the m there is; only where a row has none yet, or where its sum shows that the scores
+        // have outgrown m (bf16 and fp32 hold weights up to 2^40 as exactly as weights up to 1), the maximum is
+        // looked for and the tile done again with it.  That saves a pass over the scores of almost every tile.
+        float sum = 0.f;
 #pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
-              uint32_t o[32];
-              tc_ld32(tOr + q * 32, o);
+        for (int pass = __any_sync(0xffffffffu, m == -INFINITY) ? 1 : 0; pass < 2; ++pass) {
+          if (pass == 1) {
+            float mx[4];
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tc_st32(tOr + q * 32, o);
+            for (int q = 0; q < 4; ++q) mx[q] = max3(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
+#pragma unroll
+            for (int i = 12; i + 8 <= 128; i += 8) {
+#pragma unroll
+              for (int q = 0; q < 4; ++q) mx[q] = max3(mx[q], __uint_as_float(s[i + q]), __uint_as_float(s[i + 4 + q]));
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], __uint_as_float(s[124 + q]));
+            const float mt = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * p.scale2;
+            const float mn = mt > m + TA_SLACK ? mt : m;
+            const float f = m == mn ? 1.f : fast_exp2(m - mn);        // m = -infinity: 0
+            m = mn;
+            l *= f;
+            if (j > ja) {
+#pragma unroll 1
+              for (int q = 0; q < D / 32; ++q) {
+                uint32_t o[32];
+                tc_ld32(tOr + q * 32, o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                tc_st32(tOr + q * 32, o);
+              }
             }
           }
-        }
-        const float base = m == -INFINITY ? 0.f : m;
-        const uint64_t scale2x2 = pack2(p.scale2, p.scale2), base2 = pack2(-base, -base);
-        uint64_t sum2[2] = {0, 0};
+          const float base = m == -INFINITY ? 0.f : m;
+          const uint64_t scale2x2 = pack2(p.scale2, p.scale2), base2 = pack2(-base, -base);
+          uint64_t sum2[2] = {0, 0};
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          uint32_t w[32];
+          for (int q = 0; q < 2; ++q) {
+            uint32_t w[32];
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            const uint64_t x = fma2(pack2u(s[q * 64 + 2 * i], s[q * 64 + 2 * i + 1]), scale2x2, base2);
-            const float ea = fast_exp2(lo2(x)), eb = fast_exp2(hi2(x));
-            sum2[i & 1] = add2(sum2[i & 1], pack2(ea, eb));
-            w[i] = pack_bf16x2(ea, eb);
+            for (int i = 0; i < 32; ++i) {
+              const uint64_t x = fma2(pack2u(s[q * 64 + 2 * i], s[q * 64 + 2 * i + 1]), scale2x2, base2);
+              const float ea = fast_exp2(lo2(x)), eb = fast_exp2(hi2(x));
+              sum2[i & 1] = add2(sum2[i & 1], pack2(ea, eb));
+              w[i] = pack_bf16x2(ea, eb);
+            }
+            tc_st32(tSr + q * 32, w);
           }
-          tc_st32(tSr + q * 32, w);
-          tc_st_wait();
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(pairbar(q == 0 ? P_HALF : P_READY, t));
+          sum2[0] = add2(sum2[0], sum2[1]);
+          sum = lo2(sum2[0]) + hi2(sum2[0]);
+          if (!__any_sync(0xffffffffu, !(sum < TA_OUTGROWN))) break;
         }
-        sum2[0] = add2(sum2[0], sum2[1]);
-        l += lo2(sum2[0]) + hi2(sum2[0]);
+        l += sum;
+        tc_st_wait();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(pairbar(P_READY, t));
       }
       if (!ok) break;
       const bool worked = ja < e;
