@@ -614,7 +614,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         tc_ld_wait();
 #pragma unroll
         for (int q = 0; q < 4; ++q) tc_ready32(s + q * 32);
-        if (j < full_lo || j >= full_hi) {
+        if (__any_sync(0xffffffffu, j < full_lo || j >= full_hi)) {      // (a vote: the selects are to be branched around)
           const int k0 = seg_lo + j * TA_TILE, h_ = hi - k0, l_ = lo - k0;
 #pragma unroll
           for (int i = 0; i < 128; ++i)
@@ -626,7 +626,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         float sum = 0.f;
 #pragma unroll 1
         for (int pass = __any_sync(0xffffffffu, m == -INFINITY) ? 1 : 0; pass < 2; ++pass) {
-          if (pass == 1) {
+          if (__builtin_expect(pass == 1, 0)) {
             float mx[4];
 #pragma unroll
             for (int q = 0; q < 4; ++q) mx[q] = max3(__uint_as_float(s[q]), __uint_as_float(s[4 + q]), __uint_as_float(s[8 + q]));
