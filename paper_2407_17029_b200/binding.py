@@ -224,16 +224,24 @@ class Adapter:
         return c
 
 
+# the current stream's handle without building a Stream object, where this torch has that call (a microsecond a launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", None)
+
+
 def _stream_ptr(stream) -> int:
-    s = torch.cuda.current_stream() if stream is None else stream
-    return s.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is None or _raw_device is None or not torch.cuda.is_initialized():
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_raw_device())
 
 
 def _dt(torch_dtype) -> int:
-    if torch_dtype == torch.float32:
-        return F32
-    if torch_dtype == torch.bfloat16:
+    if torch_dtype is torch.bfloat16:
         return BF16
+    if torch_dtype is torch.float32:
+        return F32
     raise ValueError(f"unsupported dtype {torch_dtype}")
 
 
@@ -447,12 +455,10 @@ class Rope:
     amplitude: float = 1.0
 
     def c_struct(self) -> _CRope:
-        if self.table.dtype != torch.int64 or not self.table.is_contiguous() or 2 * self.table.numel() != self.rotary_dim:
+        t = self.table
+        if t.dtype is not torch.int64 or not t.is_contiguous() or 2 * t.numel() != self.rotary_dim:
             raise ValueError("table: contiguous int64 [rotary_dim / 2], see rope_table")
-        c = _CRope()
-        c.head_dim, c.rotary_dim, c.layout, c.amplitude = self.head_dim, self.rotary_dim, self.layout, self.amplitude
-        c.turns = self.table.data_ptr()
-        return c
+        return _CRope(self.head_dim, self.rotary_dim, self.layout, self.amplitude, t.data_ptr())
 
 
 @dataclass
@@ -470,15 +476,12 @@ class KVCache:
 
     def c_struct(self) -> _CKVCache:
         k, v = self.k, self.v
-        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+        shape, stride = k.shape, k.stride()
+        if len(shape) != 4 or shape != v.shape or stride != v.stride() or stride[3] != 1:
             raise ValueError("k, v: equal shapes and strides [n_pages][page_size][kv_heads][head_dim], head_dim contiguous")
-        if k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16:
+        if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
             raise ValueError("k, v: bf16")
-        c = _CKVCache()
-        c.k, c.v = k.data_ptr(), v.data_ptr()
-        c.page_stride, c.token_stride, c.head_stride = k.stride(0), k.stride(1), k.stride(2)
-        c.n_pages, c.page_size, c.kv_heads, c.head_dim = k.shape
-        return c
+        return _CKVCache(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], *shape)
 
 
 @dataclass
@@ -493,16 +496,14 @@ class KVPlan:
 
 
 def _heads(t: torch.Tensor) -> _CHeads:
-    assert t.is_cuda and t.dim() == 3
-    if t.stride(2) != 1 and t.shape[2] > 1:
-        raise ValueError("[tokens][heads][head_dim]: head_dim contiguous")
-    c = _CHeads()
-    c.data, c.token_stride, c.head_stride, c.heads, c.dtype = t.data_ptr(), t.stride(0), t.stride(1), t.shape[1], _dt(t.dtype)
-    return c
+    stride = t.stride()
+    if len(stride) != 3 or stride[2] != 1 and t.shape[2] > 1 or not t.is_cuda:
+        raise ValueError("[tokens][heads][head_dim] device tensor, head_dim contiguous")
+    return _CHeads(t.data_ptr(), stride[0], stride[1], t.shape[1], _dt(t.dtype))
 
 
 def _ints(t: torch.Tensor, n: int, name: str) -> int:
-    if not t.is_cuda or t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous() or not t.is_cuda:
         raise ValueError(f"{name}: contiguous int32 device tensor of at least {n} entries")
     return t.data_ptr()
 
@@ -521,41 +522,44 @@ def rope(cfg: Rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.
          out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None, stream=None):
     """qblora_rope on q (and k) [tokens][heads][head_dim]; inverse=True is the backward pass (gradients in, gradients
     out).  out_q / out_k may be q / k themselves.  Returns (q', k')."""
-    T = q.shape[0]
-    if q.shape[2] != cfg.head_dim or (k is not None and (k.shape[0] != T or k.shape[2] != cfg.head_dim)):
+    shape, k_shape = q.shape, None if k is None else k.shape
+    T, D = shape[0], cfg.head_dim
+    if shape[2] != D or (k is not None and (k_shape[0] != T or k_shape[2] != D)):
         raise ValueError("q, k: [tokens][heads][head_dim]")
-    out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out_q is None else out_q
+    if out_q is None:
+        out_q = torch.empty(shape, dtype=q.dtype, device=q.device)
     if k is not None and out_k is None:
-        out_k = torch.empty(k.shape, dtype=out_q.dtype, device=k.device)
-    if out_q.shape != q.shape or (k is not None and out_k.shape != k.shape):
+        out_k = torch.empty(k_shape, dtype=out_q.dtype, device=k.device)
+    if out_q.shape != shape or (k is not None and out_k.shape != k_shape):
         raise ValueError("outputs have the shapes of the inputs")
     if T == 0:
         return out_q, out_k
-    c, x, y = cfg.c_struct(), _heads(q), _heads(out_q)
-    x2, y2 = (_heads(k), _heads(out_k)) if k is not None else (None, None)
-    st = _lib.qblora_rope(ctypes.byref(c), int(bool(inverse)), _ints(positions, T, "positions"), T, ctypes.byref(x),
-                          ctypes.byref(y), _ref(x2), _ref(y2), _stream_ptr(stream))
-    _check(st, "qblora_rope")
+    by = ctypes.byref
+    st = _lib.qblora_rope(by(cfg.c_struct()), bool(inverse), _ints(positions, T, "positions"), T, by(_heads(q)), by(_heads(out_q)),
+                          None if k is None else by(_heads(k)), None if k is None else by(_heads(out_k)), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_rope")
     return out_q, out_k
 
 
 def rope_append(cfg: Rope, positions: torch.Tensor, slots: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                 cache: KVCache, out_q: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """qblora_rope_append: rotated q (bf16); rotated k and v go into the cache at `slots`."""
-    T = q.shape[0]
-    if k.shape[0] != T or v.shape != k.shape or q.shape[2] != cfg.head_dim or k.shape[2] != cfg.head_dim:
+    shape, k_shape = q.shape, k.shape
+    T, D = shape[0], cfg.head_dim
+    if k_shape[0] != T or v.shape != k_shape or shape[2] != D or k_shape[2] != D:
         raise ValueError("q, k, v: [tokens][heads][head_dim]")
-    out_q = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out_q is None else out_q
-    if out_q.shape != q.shape:
+    if out_q is None:
+        out_q = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+    elif out_q.shape != shape:
         raise ValueError("out_q has the shape of q")
     if T == 0:
         return out_q
-    c, cc = cfg.c_struct(), cache.c_struct()
-    cq, ck, cv, co = _heads(q), _heads(k), _heads(v), _heads(out_q)
-    st = _lib.qblora_rope_append(ctypes.byref(c), _ints(positions, T, "positions"), _ints(slots, T, "slots"), T,
-                                 ctypes.byref(cq), ctypes.byref(ck), ctypes.byref(cv), ctypes.byref(co), ctypes.byref(cc),
-                                 _stream_ptr(stream))
-    _check(st, "qblora_rope_append")
+    by = ctypes.byref
+    st = _lib.qblora_rope_append(by(cfg.c_struct()), _ints(positions, T, "positions"), _ints(slots, T, "slots"), T, by(_heads(q)),
+                                 by(_heads(k)), by(_heads(v)), by(_heads(out_q)), by(cache.c_struct()), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_rope_append")
     return out_q
 
 
@@ -570,16 +574,17 @@ def kv_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Ten
     B, width = block_table.shape
     if outs is None:
         outs = tuple(torch.empty(n, dtype=torch.int32, device=block_table.device) for n in (B + 1, B, tokens, tokens, B, 1))
-    plan = KVPlan(*outs)
+    cu_new, kv_len, positions, slots, admitted, free_out = outs
     st = _lib.qblora_kv_plan(_ints(ctx_len, B, "ctx_len"), _ints(new_len, B, "new_len"),
-                             _ints(release, B, "release") if release is not None else None, B,
+                             None if release is None else _ints(release, B, "release"), B,
                              _ints(block_table, 1, "block_table"), width, _ints(free_pages, 1, "free_pages"),
-                             free_pages.numel(), _ints(free_count, 1, "free_count"), _ints(plan.free_count, 1, "free_count out"),
-                             int(page_size), int(tokens), _ints(plan.cu_new, B + 1, "cu_new"), _ints(plan.kv_len, B, "kv_len"),
-                             _ints(plan.positions, tokens, "positions"), _ints(plan.slots, tokens, "slots"),
-                             _ints(plan.admitted, B, "admitted"), _stream_ptr(stream))
-    _check(st, "qblora_kv_plan")
-    return plan
+                             free_pages.numel(), _ints(free_count, 1, "free_count"), _ints(free_out, 1, "free_count out"),
+                             page_size, tokens, _ints(cu_new, B + 1, "cu_new"), _ints(kv_len, B, "kv_len"),
+                             _ints(positions, tokens, "positions"), _ints(slots, tokens, "slots"),
+                             _ints(admitted, B, "admitted"), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_kv_plan")
+    return KVPlan(cu_new, kv_len, positions, slots, admitted, free_out)
 
 
 def attention_workspace_bytes(cache: KVCache, q_heads: int, tokens: int) -> int:
@@ -598,26 +603,29 @@ def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, 
                     lse: Optional[torch.Tensor] = None, need_lse: bool = False, ws: Optional[torch.Tensor] = None, stream=None):
     """qblora_paged_attention: q bf16 [tokens][q_heads][head_dim] -> (out, lse); lse (fp32 [tokens][q_heads]) is None
     unless need_lse or a tensor for it is given.  scale defaults to head_dim^-1/2; window = 0: no window."""
-    T, H, D = q.shape
-    if D != cache.k.shape[3]:
+    shape = q.shape
+    T, H, D = shape
+    cc = cache.c_struct()
+    if D != cc.head_dim:
         raise ValueError("q: [tokens][q_heads][head_dim of the cache]")
-    if block_table.dim() != 2:
-        raise ValueError("block_table: [requests][width]")
     B, width = block_table.shape
-    out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device) if out is None else out
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
     if lse is None and need_lse:
         lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
-    if out.shape != q.shape or (lse is not None and (tuple(lse.shape) != (T, H) or lse.dtype != torch.float32 or not lse.is_contiguous())):
-        raise ValueError("out: shape of q; lse: contiguous fp32 [tokens][q_heads]")
+    if out.shape != shape or (lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda)):
+        raise ValueError("out: shape of q; lse: contiguous fp32 device tensor [tokens][q_heads]")
     if T == 0:
         return out, lse
     if ws is None:
         ws = alloc_attention_workspace(cache, q)
-    cc, cq, co = cache.c_struct(), _heads(q), _heads(out)
-    st = _lib.qblora_paged_attention(ctypes.byref(cc), _ints(block_table, 1, "block_table"), width, _ints(cu_new, B + 1, "cu_new"),
-                                     _ints(kv_len, B, "kv_len"), B, ctypes.byref(cq), T,
-                                     float(D) ** -0.5 if scale is None else float(scale), int(bool(causal)), int(window),
-                                     ctypes.byref(co), lse.data_ptr() if lse is not None else None, ws.data_ptr(), ws.numel(),
-                                     _stream_ptr(stream))
-    _check(st, "qblora_paged_attention")
+    elif not ws.is_cuda or ws.dtype is not torch.uint8:
+        raise ValueError("ws: uint8 device tensor")
+    by = ctypes.byref
+    st = _lib.qblora_paged_attention(by(cc), _ints(block_table, 1, "block_table"), width, _ints(cu_new, B + 1, "cu_new"),
+                                     _ints(kv_len, B, "kv_len"), B, by(_heads(q)), T, D ** -0.5 if scale is None else scale,
+                                     bool(causal), window, by(_heads(out)), None if lse is None else lse.data_ptr(),
+                                     ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_paged_attention")
     return out, lse

@@ -32,20 +32,27 @@ __device__ __forceinline__ float ld1(const __nv_bfloat16* p) { return __bfloat16
 __device__ __forceinline__ void st1(float* p, float x) { *p = x; }
 __device__ __forceinline__ void st1(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
-// Eight consecutive values.
-__device__ __forceinline__ void ld8(const float* p, float (&x)[8]) {
-  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-  x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-}
-__device__ __forceinline__ void ld8(const __nv_bfloat16* p, float (&x)[8]) {
-  const uint4 v = *reinterpret_cast<const uint4*>(p);
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+// Eight consecutive values, as loaded (so that several loads can be on their way) and as floats.
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   }
-}
+};
+template <> struct Eight<__nv_bfloat16> {
+  uint4 v;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { v = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+};
 __device__ __forceinline__ void st8(float* p, const float (&x)[8]) {
   *reinterpret_cast<float4*>(p) = make_float4(x[0], x[1], x[2], x[3]);
   *reinterpret_cast<float4*>(p + 4) = make_float4(x[4], x[5], x[6], x[7]);
@@ -119,35 +126,49 @@ __global__ void __launch_bounds__(256) rope_wide_kernel(const __grid_constant__ 
     e1 = e0 + 8 < c.cfg.D ? e0 + 8 : -1;
   }
   const int64_t entry = c.slots ? cache_entry(c.cache, __ldg(c.slots + t)) : -1;
-#pragma unroll 4
-  for (int h = h0; h < h1; ++h) {
-    const Place<TI, TO> w = place<TI, TO>(c, t, entry, h);
-    float a[8], b[8];
-    ld8(w.src + e0, a);
-    if (e1 >= 0) ld8(w.src + e1, b);
-    if (rot && w.rotate) {
-      if (LAYOUT == QBLORA_ROPE_HALF) {
+  // UNROLL heads at a time: all their loads go out before the first store (a store may alias a load, so the compiler would
+  // not move one in front of the other)
+  constexpr int UNROLL = sizeof(TI) == 2 ? 4 : 2;
+  for (int hb = h0; hb < h1; hb += UNROLL) {
+    Eight<TI> ra[UNROLL], rb[UNROLL];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float x = a[i], y = b[i];
-          a[i] = x * co[i] - y * si[i];
-          b[i] = y * co[i] + x * si[i];
-        }
-      } else {
+    for (int u = 0; u < UNROLL; ++u) {
+      if (hb + u >= h1) break;
+      const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u);
+      ra[u].load(w.src + e0);
+      if (e1 >= 0) rb[u].load(w.src + e1);
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          float x = a[2 * i], y = a[2 * i + 1];
-          a[2 * i] = x * co[i] - y * si[i];
-          a[2 * i + 1] = y * co[i] + x * si[i];
-          x = b[2 * i]; y = b[2 * i + 1];
-          b[2 * i] = x * co[4 + i] - y * si[4 + i];
-          b[2 * i + 1] = y * co[4 + i] + x * si[4 + i];
+    for (int u = 0; u < UNROLL; ++u) {
+      if (hb + u >= h1) break;
+      const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u);
+      float a[8], b[8];
+      ra[u].get(a);
+      if (e1 >= 0) rb[u].get(b);
+      if (rot && w.rotate) {
+        if (LAYOUT == QBLORA_ROPE_HALF) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float x = a[i], y = b[i];
+            a[i] = x * co[i] - y * si[i];
+            b[i] = y * co[i] + x * si[i];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float x = a[2 * i], y = a[2 * i + 1];
+            a[2 * i] = x * co[i] - y * si[i];
+            a[2 * i + 1] = y * co[i] + x * si[i];
+            x = b[2 * i]; y = b[2 * i + 1];
+            b[2 * i] = x * co[4 + i] - y * si[4 + i];
+            b[2 * i + 1] = y * co[4 + i] + x * si[4 + i];
+          }
         }
       }
-    }
-    if (w.dst) {
-      st8(w.dst + e0, a);
-      if (e1 >= 0) st8(w.dst + e1, b);
+      if (w.dst) {
+        st8(w.dst + e0, a);
+        if (e1 >= 0) st8(w.dst + e1, b);
+      }
     }
   }
 }
