@@ -524,7 +524,7 @@ int pa_row_form(const AttnCall& c) {
 }  // namespace
 
 size_t paged_attention_scratch_bytes(int head_dim) {
-  // rows of partial results: 2 parts per share, 64-row tiles here, 16-row tiles (or half as many of 32) in paged_warp.cu
+  // rows of partial results: 2 parts per share, 64-row tiles here, 16-row tiles in paged_warp.cu
   const int dp = head_dim <= 64 ? 64 : head_dim <= 128 ? 128 : 256;
   const size_t here = (size_t)2 * kPagedMaxSms * kPagedMaxPerSm * 64, there = (size_t)2 * kPagedMaxShares * 16;
   return std::max(here * (dp + 2) * 4, there * (dp + 2) * 4 + kPagedMaxShares * sizeof(JoinCut));

@@ -1,7 +1,7 @@
 // Attention over the paged cache for few rows per key head (decoding, drafted tokens): the form that streams the cache
 // with TMA.  Head sizes 64 and 128, pages that fit its tiles; paged_attn.cu takes the rest.
 //
-// Mathematics as in paged_attn.cu: a running softmax in base 2 over row tiles of 16 MT rows (tokens x query heads that share
+// Mathematics as in paged_attn.cu: a running softmax in base 2 over row tiles of 16 rows (tokens x query heads that share
 // a key head); partial triples (maximum, sum, weighted values) over disjoint keys join in any grouping.
 //
 // What bounds it: the cache's bytes, so each warp is made to need little else.  All key tiles of all items (request,
@@ -35,25 +35,23 @@ namespace {
 constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
 constexpr int PW_MAX_LEVELS = kPagedLevels;
 constexpr int PW_FINE = 8;       // key tiles of the shortest shares
+constexpr float PW_OUTGROWN = 1.099511627776e12f;   // 2^40
 constexpr float PW_LN2 = 0.69314718055994530942f;
 
-template <int D, int MT>
+template <int D>
 struct PwShape {
-  static constexpr int ROWS = 16 * MT;
+  static constexpr int ROWS = 16;
   static constexpr int KT = D == 64 ? 32 : 16;            // keys per tile: 8 KB of K and V
-  static constexpr int STAGES = MT == 1 ? 3 : 2;
+  static constexpr int STAGES = 3;
   static constexpr int KV_BYTES = KT * D * 2;
   static constexpr int STAGE = 2 * KV_BYTES;
-  static constexpr int Q_BYTES = MT == 1 ? 0 : ROWS * D * 2;   // per warp; one row tile's queries stay in registers
-  static constexpr int WARP_BYTES = STAGES * STAGE + Q_BYTES;
-  static constexpr int SMEM = PW_WARPS * WARP_BYTES + 1024;
+  static constexpr int SMEM = PW_WARPS * STAGES * STAGE + 1024;
 };
 
 struct PwParams {
   AttnCall c;
   float scale2;              // scale * log2 e
   int narrow_rows;           // requests with more rows than this belong to the tcgen05 kernel
-  int max_levels;            // of shares, at most PW_MAX_LEVELS
   int box_keys;              // keys per TMA box: min(page_size, KT)
   uint32_t div_page, div_group;
   uint32_t zero;             // 0, but not to the compiler
@@ -131,10 +129,10 @@ __global__ void __launch_bounds__(256) attention_reset_kernel(uint4* ws, int n) 
   if (i < n) ws[i] = make_uint4(0, 0, 0, 0);
 }
 
-template <int D, int MT>
+template <int D>
 __global__ void __launch_bounds__(PW_THREADS, 1)
 paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ PwParams p) {
-  using Sh = PwShape<D, MT>;
+  using Sh = PwShape<D>;
   constexpr int ROWS = Sh::ROWS, KT = Sh::KT, HALVES = D / 64, NT = KT / 8, PW_STAGES = Sh::STAGES;
   using Cursor = PwCursor<ROWS, KT>;
   extern __shared__ uint8_t smem_raw[];
@@ -147,7 +145,6 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t ring = base + warp * (PW_STAGES * Sh::STAGE);
-  const uint32_t sq = base + PW_WARPS * PW_STAGES * Sh::STAGE + warp * Sh::Q_BYTES;
   const uint32_t full = smem_u32(s_full + warp * PW_STAGES);
 
   if (lane == 0) {
@@ -196,7 +193,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   // beginning is in the ring besides the current one).
   const int per_level = min((int)gridDim.x * PW_WARPS, max(1, total / (PW_STAGES + 1)));
   int levels = 1;
-  while (levels < p.max_levels && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
+  while (levels < PW_MAX_LEVELS && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
   const int shares = per_level * levels;
   if (tid == 0) {
     int at = 0;
@@ -314,9 +311,9 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       xk[i] = (uint32_t)(rk * 128 + (((2 * i + ((lane >> 3) & 1)) ^ (rk & 7)) << 4));
       xv[i] = (uint32_t)(rv * 128 + (((2 * i + (lane >> 4)) ^ (rv & 7)) << 4));
     }
-    float o[MT][D / 8][4], m[MT][2], l[MT][2];
-    uint32_t qf[MT == 1 ? D / 16 : 1][4];
-    int r0 = 0, hi[MT][2], lo[MT][2];
+    float o[D / 8][4], m[2], l[2];
+    uint32_t qf[D / 16][4];
+    int r0 = 0, hi[2], lo[2];
     int stage = 0;
     uint32_t ph = 0;
     bool first_segment = true, fresh = true;     // of the share; of the item
@@ -338,40 +335,23 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
         r0 = cu.rt * ROWS;
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int i = 0; i < 2; ++i) {                 // this lane's rows: the keys they see
+          const int gr = r0 + (lane >> 2) + 8 * i, tok = fast_div(gr, c.G, p.div_group);
+          const int pos = cu.r.kv - cu.r.n + min(tok, cu.r.n - 1);
+          hi[i] = attn_hi(c, cu.r.kv, pos);
+          lo[i] = attn_lo(c, pos);
+          const uint32_t* q = reinterpret_cast<const uint32_t*>(c.q + (long long)(cu.r.t0 + tok) * c.q_ts +
+                                                                (long long)(cu.h * c.G + gr - tok * c.G) * c.q_hs) + (lane & 3);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {                 // this lane's rows: the keys they see
-            const int gr = r0 + t * 16 + (lane >> 2) + 8 * i, tok = fast_div(gr, c.G, p.div_group);
-            const int pos = cu.r.kv - cu.r.n + min(tok, cu.r.n - 1);
-            hi[t][i] = attn_hi(c, cu.r.kv, pos);
-            lo[t][i] = attn_lo(c, pos);
-            if (MT == 1) {
-              const uint32_t* q = reinterpret_cast<const uint32_t*>(c.q + (long long)(cu.r.t0 + tok) * c.q_ts +
-                                                                    (long long)(cu.h * c.G + gr - tok * c.G) * c.q_hs) + (lane & 3);
-#pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                qf[MT == 1 ? k : 0][i] = tok < cu.r.n ? __ldg(q + 8 * k) : 0u;
-                qf[MT == 1 ? k : 0][2 + i] = tok < cu.r.n ? __ldg(q + 8 * k + 4) : 0u;
-              }
-            }
-            m[t][i] = -INFINITY;
-            l[t][i] = 0.f;
+          for (int k = 0; k < D / 16; ++k) {
+            qf[k][i] = tok < cu.r.n ? __ldg(q + 8 * k) : 0u;
+            qf[k][2 + i] = tok < cu.r.n ? __ldg(q + 8 * k + 4) : 0u;
           }
-        if (MT > 1) {
-          __syncwarp();
-          for (int i = lane; i < ROWS * (D / 8); i += 32) {
-            const int row = i / (D / 8), ch = i % (D / 8), gr = r0 + row, tok = fast_div(gr, c.G, p.div_group);
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (tok < cu.r.n)
-              v = __ldg(reinterpret_cast<const uint4*>(c.q + (long long)(cu.r.t0 + tok) * c.q_ts + (long long)(cu.h * c.G + gr - tok * c.G) * c.q_hs) + ch);
-            st_shared_v4(sq + (uint32_t)(row * D * 2 + ((ch ^ (row & 7)) << 4)), v.x, v.y, v.z, v.w);
-          }
-          __syncwarp();
+          m[i] = tok < cu.r.n ? -INFINITY : 0.f;      // rows that are none need no maximum
+          l[i] = 0.f;
         }
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
-#pragma unroll
-          for (int n = 0; n < D / 8; ++n) o[t][n][0] = o[t][n][1] = o[t][n][2] = o[t][n][3] = 0.f;
+        for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
       }
       if (!__all_sync(0xffffffffu, mbar_wait(full + 8 * stage, ph, c.status, p.wait_limit))) { ok = false; break; }
       const uint32_t sk = ring + stage * Sh::STAGE, sv = sk + Sh::KV_BYTES;
@@ -402,41 +382,25 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 
       // scores: fragment n covers keys 8 n .. 8 n + 7 (lane: rows lane / 4 and + 8, keys 2 (lane % 4) + {0, 1}); with few
       // fragments, even and odd steps of the contraction are summed apart, so that an MMA does not wait for the one before
-      constexpr int SPLIT = MT * NT < 4 ? 2 : 1;
-      float s[MT][NT][4], s2[SPLIT == 2 ? MT : 1][SPLIT == 2 ? NT : 1][4];
+      constexpr int SPLIT = NT < 4 ? 2 : 1;
+      float s[NT][4], s2[SPLIT == 2 ? NT : 1][4];
 #pragma unroll
-      for (int t = 0; t < MT; ++t)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.f;
-          if (SPLIT == 2) s2[t][n][0] = s2[t][n][1] = s2[t][n][2] = s2[t][n][3] = 0.f;
-        }
+      for (int n = 0; n < NT; ++n) {
+        s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
+        if (SPLIT == 2) s2[n][0] = s2[n][1] = s2[n][2] = s2[n][3] = 0.f;
+      }
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        uint32_t qa[MT][4];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          if (MT == 1) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qa[t][e] = qf[MT == 1 ? k : 0][e];
-          } else {
-            const int row = t * 16 + (lane & 15), ch = 2 * k + (lane >> 4);
-            frag_ldm4(qa[t], sq + (uint32_t)(row * D * 2 + ((ch ^ (row & 7)) << 4)));
-          }
-        }
 #pragma unroll
         for (int n2 = 0; n2 < NT / 2; ++n2) {
           uint32_t kf[4];
           frag_ldm4(kf, sk + xk[k & 3] + (uint32_t)((k >> 2) * (KT * 128) + n2 * 2048));
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            if (SPLIT == 2 && (k & 1)) {
-              frag_mma(s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? 2 * n2 : 0], qa[t], kf[0], kf[1]);
-              frag_mma(s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? 2 * n2 + 1 : 0], qa[t], kf[2], kf[3]);
-            } else {
-              frag_mma(s[t][2 * n2], qa[t], kf[0], kf[1]);
-              frag_mma(s[t][2 * n2 + 1], qa[t], kf[2], kf[3]);
-            }
+          if (SPLIT == 2 && (k & 1)) {
+            frag_mma(s2[SPLIT == 2 ? 2 * n2 : 0], qf[k], kf[0], kf[1]);
+            frag_mma(s2[SPLIT == 2 ? 2 * n2 + 1 : 0], qf[k], kf[2], kf[3]);
+          } else {
+            frag_mma(s[2 * n2], qf[k], kf[0], kf[1]);
+            frag_mma(s[2 * n2 + 1], qf[k], kf[2], kf[3]);
           }
         }
       }
@@ -448,68 +412,69 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         for (int n2 = 0; n2 < D / 16; ++n2) frag_ldm4t(vf[k][n2], sv + xv[n2 & 3] + (uint32_t)((n2 >> 2) * (KT * 128) + k * 2048));
       if (SPLIT == 2) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[t][n][e] += s2[SPLIT == 2 ? t : 0][SPLIT == 2 ? n : 0][e];
+          for (int e = 0; e < 4; ++e) s[n][e] += s2[SPLIT == 2 ? n : 0][e];
       }
       if (partial) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int j = k0 + n * 8 + 2 * (lane & 3) + (e & 1);
-              if (j >= hi[t][e >> 1] || j < lo[t][e >> 1]) s[t][n][e] = -INFINITY;
-            }
+          for (int e = 0; e < 4; ++e) {
+            const int j = k0 + n * 8 + 2 * (lane & 3) + (e & 1);
+            if (j >= hi[e >> 1] || j < lo[e >> 1]) s[n][e] = -INFINITY;
+          }
       }
+      // Weights with the m there is; only where a row has none yet, or where a sum shows that the scores have outgrown m (fp32
+      // and bf16 hold weights of 2^40 as exactly as weights of 1), the maximum is looked for and they are done again.
+      float w[NT][4], sum[2];
+      bool again = __any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY);
+#pragma unroll 1
+      for (;;) {
+        if (again) {
+          float f[2];
 #pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        float f[2];
+          for (int i = 0; i < 2; ++i) {
+            float x = s[0][2 * i];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x = fmaxf(x, fmaxf(s[n][2 * i], s[n][2 * i + 1]));
+            x = fmaxf(m[i], x * p.scale2);
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            f[i] = m[i] == x ? 1.f : fast_exp2(m[i] - x);
+            m[i] = x;
+            l[i] *= f[i];
+          }
+#pragma unroll
+          for (int n = 0; n < D / 8; ++n) { o[n][0] *= f[0]; o[n][1] *= f[0]; o[n][2] *= f[1]; o[n][3] *= f[1]; }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float x = s[t][0][2 * i];
-#pragma unroll
-          for (int n = 0; n < NT; ++n) x = fmaxf(x, fmaxf(s[t][n][2 * i], s[t][n][2 * i + 1]));
-          x = fmaxf(m[t][i], x * p.scale2);
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          const float b_ = x == -INFINITY ? 0.f : x;       // nothing seen yet: all weights are 2^-inf = 0
-          f[i] = fast_exp2(m[t][i] - b_);
-          m[t][i] = x;
-          float sum = 0.f;
+          const float b = m[i] == -INFINITY ? 0.f : m[i];      // nothing seen yet: all weights are 2^-inf = 0
+          sum[i] = 0.f;
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            s[t][n][2 * i] = fast_exp2(fmaf(s[t][n][2 * i], p.scale2, -b_));
-            s[t][n][2 * i + 1] = fast_exp2(fmaf(s[t][n][2 * i + 1], p.scale2, -b_));
-            sum += s[t][n][2 * i] + s[t][n][2 * i + 1];
+            w[n][2 * i] = fast_exp2(fmaf(s[n][2 * i], p.scale2, -b));
+            w[n][2 * i + 1] = fast_exp2(fmaf(s[n][2 * i + 1], p.scale2, -b));
+            sum[i] += w[n][2 * i] + w[n][2 * i + 1];
           }
-          l[t][i] = l[t][i] * f[i] + sum;                  // this lane's part; joined over the quad at the end
         }
-        if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
-#pragma unroll
-          for (int n = 0; n < D / 8; ++n) { o[t][n][0] *= f[0]; o[t][n][1] *= f[0]; o[t][n][2] *= f[1]; o[t][n][3] *= f[1]; }
-        }
+        if (again || !__any_sync(0xffffffffu, !(sum[0] < PW_OUTGROWN) || !(sum[1] < PW_OUTGROWN))) break;
+        again = true;
       }
+      l[0] += sum[0];                                          // this lane's part; joined over the quad at the end
+      l[1] += sum[1];
 #pragma unroll
       for (int k = 0; k < KT / 16; ++k) {
-        uint32_t a[MT][4];
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-          a[t][0] = pack_bf16x2(s[t][2 * k][0], s[t][2 * k][1]);
-          a[t][1] = pack_bf16x2(s[t][2 * k][2], s[t][2 * k][3]);
-          a[t][2] = pack_bf16x2(s[t][2 * k + 1][0], s[t][2 * k + 1][1]);
-          a[t][3] = pack_bf16x2(s[t][2 * k + 1][2], s[t][2 * k + 1][3]);
-        }
+        uint32_t a[4];
+        a[0] = pack_bf16x2(w[2 * k][0], w[2 * k][1]);
+        a[1] = pack_bf16x2(w[2 * k][2], w[2 * k][3]);
+        a[2] = pack_bf16x2(w[2 * k + 1][0], w[2 * k + 1][1]);
+        a[3] = pack_bf16x2(w[2 * k + 1][2], w[2 * k + 1][3]);
 #pragma unroll
         for (int n2 = 0; n2 < D / 16; ++n2) {
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            frag_mma(o[t][2 * n2], a[t], vf[k][n2][0], vf[k][n2][1]);
-            frag_mma(o[t][2 * n2 + 1], a[t], vf[k][n2][2], vf[k][n2][3]);
-          }
+          frag_mma(o[2 * n2], a, vf[k][n2][0], vf[k][n2][1]);
+          frag_mma(o[2 * n2 + 1], a, vf[k][n2][2], vf[k][n2][3]);
         }
       }
       if (odd) {
@@ -525,13 +490,11 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             if (!bf16x2_odd(w)) continue;
             const float v0 = __uint_as_float(w << 16), v1 = __uint_as_float(w & 0xffff0000u);
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                if (j >= hi[t][i] || j < lo[t][i]) continue;
-                if ((w & 0x7f80u) == 0x7f80u) o[t][n][2 * i] += v0;
-                if ((w & 0x7f800000u) == 0x7f800000u) o[t][n][2 * i + 1] += v1;
-              }
+            for (int i = 0; i < 2; ++i) {
+              if (j >= hi[i] || j < lo[i]) continue;
+              if ((w & 0x7f80u) == 0x7f80u) o[n][2 * i] += v0;
+              if ((w & 0x7f800000u) == 0x7f800000u) o[n][2 * i + 1] += v1;
+            }
           }
         }
       }
@@ -541,7 +504,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (ld_left > 0) {
         uint32_t dep = 0;
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) dep |= __float_as_uint(o[0][n][0]);
+        for (int n = 0; n < D / 8; ++n) dep |= __float_as_uint(o[n][0]);
         __syncwarp();
         issue(dep & p.zero);
       }
@@ -553,30 +516,28 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         const bool whole = item_first >= u0 && item_first + cu.k.tiles <= u1;
         const long long slot = 2 * g + (first_segment ? 0 : 1);   // of partial results
 #pragma unroll
-        for (int t = 0; t < MT; ++t)
+        for (int i = 0; i < 2; ++i) {
+          float sum = l[i];
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+          const int row = (lane >> 2) + 8 * i, gr = r0 + row, tok = fast_div(gr, c.G, p.div_group);
+          if (tok >= cu.r.n) continue;
+          if (whole) {
+            const int head = cu.h * c.G + gr - tok * c.G;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            __nv_bfloat16* out = c.out + (long long)(cu.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + 2 * (lane & 3);
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float sum = l[t][i];
-            sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-            sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-            const int row = t * 16 + (lane >> 2) + 8 * i, gr = r0 + row, tok = fast_div(gr, c.G, p.div_group);
-            if (tok >= cu.r.n) continue;
-            if (whole) {
-              const int head = cu.h * c.G + gr - tok * c.G;
-              const float inv = sum == 0.f ? 0.f : 1.f / sum;
-              __nv_bfloat16* out = c.out + (long long)(cu.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + 2 * (lane & 3);
+            for (int n = 0; n < D / 8; ++n)
+              *reinterpret_cast<uint32_t*>(out + 8 * n) = pack_bf16x2(o[n][2 * i] * inv, o[n][2 * i + 1] * inv);
+            if (c.lse && (lane & 3) == 0)
+              c.lse[(long long)(cu.r.t0 + tok) * c.H + head] = sum == 0.f ? -INFINITY : (m[i] + log2f(sum)) * PW_LN2;
+          } else {
+            float* d = p.part_o + (slot * ROWS + row) * D + 2 * (lane & 3);
 #pragma unroll
-              for (int n = 0; n < D / 8; ++n)
-                *reinterpret_cast<uint32_t*>(out + 8 * n) = pack_bf16x2(o[t][n][2 * i] * inv, o[t][n][2 * i + 1] * inv);
-              if (c.lse && (lane & 3) == 0)
-                c.lse[(long long)(cu.r.t0 + tok) * c.H + head] = sum == 0.f ? -INFINITY : (m[t][i] + log2f(sum)) * PW_LN2;
-            } else {
-              float* d = p.part_o + (slot * ROWS + row) * D + 2 * (lane & 3);
-#pragma unroll
-              for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(d + 8 * n) = make_float2(o[t][n][2 * i], o[t][n][2 * i + 1]);
-              if ((lane & 3) == 0) *reinterpret_cast<float2*>(p.part_ml + (slot * ROWS + row) * 2) = make_float2(m[t][i], sum);
-            }
+            for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(d + 8 * n) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+            if ((lane & 3) == 0) *reinterpret_cast<float2*>(p.part_ml + (slot * ROWS + row) * 2) = make_float2(m[i], sum);
           }
+        }
         first_segment = false;
         fresh = true;
       }
@@ -598,25 +559,24 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 }
 
-template <int D, int MT>
+template <int D>
 int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, JoinCall* join, cudaStream_t st) {
-  using Sh = PwShape<D, MT>;
+  using Sh = PwShape<D>;
   static std::atomic<bool> attr_set[64];
   int dev = 0, sms = 0;
   QB_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
-  auto kernel = paged_warp_kernel<D, MT>;
+  auto kernel = paged_warp_kernel<D>;
   if (!attr_set[dev].load(std::memory_order_acquire)) {
     QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM));
     attr_set[dev].store(true, std::memory_order_release);
   }
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int grid = std::min(sms, kPagedMaxSms);
-  p.max_levels = PW_MAX_LEVELS / MT;      // the scratch holds as many rows for either form
   p.counters = reinterpret_cast<uint32_t*>(counters);
   p.part_ml = reinterpret_cast<float*>(scratch);
-  p.part_o = p.part_ml + (size_t)2 * kPagedMaxShares * Sh::ROWS * 2 / MT;
-  p.cuts = reinterpret_cast<JoinCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D / MT);
+  p.part_o = p.part_ml + (size_t)2 * kPagedMaxShares * Sh::ROWS * 2;
+  p.cuts = reinterpret_cast<JoinCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3(PW_THREADS);
@@ -628,7 +588,7 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
   cfg.attrs = attr; cfg.numAttrs = 1;
   QB_CUDA(cudaLaunchKernelEx(&cfg, kernel, tk, tv, p));
   count_launch();
-  JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, grid * PW_WARPS * p.max_levels, Sh::ROWS, p.div_group};
+  JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, grid * PW_WARPS * PW_MAX_LEVELS, Sh::ROWS, p.div_group};
   if (join) { *join = j; return QBLORA_OK; }
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
@@ -669,10 +629,7 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* 
   CUtensorMap tk, tv;
   int rc = make_cache_maps(c, p.box_keys, &tk, &tv);
   if (rc) return rc;
-  // Row tiles of 16 or 32 rows.  The host knows rows only on average: G per new token, tokens / requests new tokens.
-  const bool one = ((c.T + c.B - 1) / c.B) * c.G <= 16;
-  if (c.D == 64) return one ? pw_launch<64, 1>(p, tk, tv, counters, scratch, join, st) : pw_launch<64, 2>(p, tk, tv, counters, scratch, join, st);
-  return one ? pw_launch<128, 1>(p, tk, tv, counters, scratch, join, st) : pw_launch<128, 2>(p, tk, tv, counters, scratch, join, st);
+  return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, join, st) : pw_launch<128>(p, tk, tv, counters, scratch, join, st);
 }
 
 }  // namespace qb

@@ -36,8 +36,10 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
   return true;
 }
 
-// Requests with more rows (new tokens x query heads per key head) go to the tcgen05 kernel.
-constexpr int kNarrowRows = 64;
+// Requests with more rows (new tokens x query heads per key head) than one row tile of paged_warp.cu go to the tcgen05 kernel:
+// a second row tile there reads the keys and values again, while 128 rows cost the tcgen05 kernel what 17 do.  Measured, 32
+// requests of 2000 to 4000 keys, 8 key heads: 24 rows 136 us there, 112 us here; 64 rows 250 and 115; 12 rows 98 us there.
+constexpr int kNarrowRows = 16;
 
 bool force_general() {
   const char* e = std::getenv("QBLORA_FORCE_GENERAL");
