@@ -118,6 +118,7 @@ struct PwCursor {
 template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
   __shared__ JoinShared list;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
   join_all<D, 256>(c, j, &list);
 }
@@ -560,7 +561,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
 }
 
 template <int D>
-int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, JoinCall* join, cudaStream_t st) {
+int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, cudaStream_t st) {
   using Sh = PwShape<D>;
   static std::atomic<bool> attr_set[64];
   int dev = 0, sms = 0;
@@ -589,7 +590,6 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
   QB_CUDA(cudaLaunchKernelEx(&cfg, kernel, tk, tv, p));
   count_launch();
   JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, grid * PW_WARPS * PW_MAX_LEVELS, Sh::ROWS, p.div_group};
-  if (join) { *join = j; return QBLORA_OK; }
   cfg.blockDim = dim3(256);
   cfg.dynamicSmemBytes = 0;
   QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D>, p.c, j));
@@ -617,7 +617,7 @@ bool paged_warp_supported(const AttnCall& c) {
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);
 }
 
-int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, JoinCall* join, cudaStream_t st) {
+int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st) {
   PwParams p{};
   p.c = c;
   p.scale2 = c.scale * 1.4426950408889634f;
@@ -629,7 +629,7 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* 
   CUtensorMap tk, tv;
   int rc = make_cache_maps(c, p.box_keys, &tk, &tv);
   if (rc) return rc;
-  return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, join, st) : pw_launch<128>(p, tk, tv, counters, scratch, join, st);
+  return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, st) : pw_launch<128>(p, tk, tv, counters, scratch, st);
 }
 
 }  // namespace qb

@@ -103,16 +103,16 @@ struct JoinCall {
 };
 
 // Few rows per key head, head sizes 64 and 128, pages that fit its tiles (paged_warp.cu): requests of at most `narrow_rows` rows
-// (new tokens * G).  With `join` the caller joins the parts (paged_join.cuh); without, a kernel behind it does.
+// (new tokens * G), and a second kernel that joins their parts.
 bool paged_warp_supported(const AttnCall& c);
-int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, JoinCall* join, cudaStream_t st);
+int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
 
-// Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows, and the joins of the kernel in front, behind
-// which this one may start as SMs become free.
+// Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows.  Launched behind launch_paged_warp, beside whose
+// kernels it may start as SMs become free.
 constexpr int kWideMaxRequests = 1024;
 bool tc_attention_supported(const AttnCall& c);
 size_t tc_attention_scratch_bytes(int head_dim);
-int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join, char* counters, char* scratch, cudaStream_t st);
+int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
 
 // TMA maps (CUtensorMap) of the cache's K and V.
 int make_cache_maps(const AttnCall& c, int box_keys, void* tm_k, void* tm_v);

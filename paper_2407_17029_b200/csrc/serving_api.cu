@@ -36,10 +36,12 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
   return true;
 }
 
-// Requests with more rows (new tokens x query heads per key head) than one row tile of paged_warp.cu go to the tcgen05 kernel:
-// a second row tile there reads the keys and values again, while 128 rows cost the tcgen05 kernel what 17 do.  Measured, 32
-// requests of 2000 to 4000 keys, 8 key heads: 24 rows 136 us there, 112 us here; 64 rows 250 and 115; 12 rows 98 us there.
-constexpr int kNarrowRows = 16;
+// Requests with more rows (new tokens x query heads per key head) than this go to the tcgen05 kernel.  A second row tile of
+// paged_warp.cu reads the keys and values again, while 128 rows cost the tcgen05 kernel what 17 do; but its set-up is longer and
+// the two kernels of a mixed call run one after the other.  Measured, 32 requests of 2000 to 4000 keys, 8 key heads: 12 rows
+// 98 us there; 24 rows 136 us there, 112 here; 40 rows 186 and 114; 64 rows 250 and 115.  16 requests of 12 to 28 rows: 50 us
+// with all of them there, 73 us with those above 16 rows here.
+constexpr int kNarrowRows = 32;
 
 bool force_general() {
   const char* e = std::getenv("QBLORA_FORCE_GENERAL");
@@ -160,11 +162,10 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   char* counters = wide_counters + kWideCounterBytes;
   char* scratch = counters + kPagedCounterBytes;
   if (!paged_warp_supported(c)) return launch_paged_attention(c, counters, scratch, st);
-  if (!tc_attention_supported(c) || tokens * c.G <= kNarrowRows) return launch_paged_warp(c, 0x7fffffff, counters, scratch, nullptr, st);
-  JoinCall join;
-  rc = launch_paged_warp(c, kNarrowRows, counters, scratch, &join, st);
+  if (!tc_attention_supported(c) || tokens * c.G <= kNarrowRows) return launch_paged_warp(c, 0x7fffffff, counters, scratch, st);
+  rc = launch_paged_warp(c, kNarrowRows, counters, scratch, st);
   if (rc) return rc;
-  return launch_tc_attention(c, kNarrowRows, join, wide_counters, scratch + paged_attention_scratch_bytes(c.D), st);
+  return launch_tc_attention(c, kNarrowRows, wide_counters, scratch + paged_attention_scratch_bytes(c.D), st);
 }
 
 }  // extern "C"

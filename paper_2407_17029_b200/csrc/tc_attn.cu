@@ -27,7 +27,7 @@
 #include <algorithm>
 #include <atomic>
 
-#include "paged_join.cuh"
+#include "mma_frag.cuh"
 #include "serving.cuh"
 #include "tc_ptx.cuh"
 #include "tc_small.cuh"
@@ -55,7 +55,6 @@ struct TaShape {
 
 struct TaParams {
   AttnCall c;
-  JoinCall join;          // what paged_warp.cu has left to join
   float scale2;
   int narrow_rows;        // requests with at most so many rows belong to paged_attn.cu
   int tokens_per_tile;    // 128 / G
@@ -135,19 +134,18 @@ struct TaWalk {
   const int* units;          // [n] inclusive sums of key tiles
   int n;
   bool dealt;                // whole items are dealt out one by one
-  int share, shares, total, u, u1;
+  int share, shares, each, extra, u, u1;
 
   __device__ __forceinline__ int find(const int* sums, int x) const {
     int a = 0, e = n;
     while (a < e) { const int m = (a + e) >> 1; if (sums[m] > x) e = m; else a = m + 1; }
     return a;
   }
-  __device__ __forceinline__ int begin(int s) const { return (int)((long long)total * s / shares); }
+  // the first total % shares shares have one tile more
+  __device__ __forceinline__ int begin(int s) const { return s * each + min(s, extra); }
   __device__ __forceinline__ int share_of(int x) const {
-    int s = (int)((long long)x * shares / total);
-    while (begin(s + 1) <= x) ++s;
-    while (begin(s) > x) --s;
-    return s;
+    const int cut = extra * (each + 1);
+    return x < cut ? x / (each + 1) : extra + (x - cut) / each;
   }
   // called by all lanes of the loading warp
   __device__ __forceinline__ bool next(const TaParams& p, TaSeg& s) {
@@ -240,7 +238,6 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ int s_odd[8];         // segment number + 1 where a value was taken out of V
   __shared__ int s_join[2];
   __shared__ TaSeg s_seg[TA_SEGS];
-  __shared__ JoinShared s_list;
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   const AttnCall& c = p.c;
@@ -306,15 +303,17 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     some = false;
   }
   if (some) {
-    walk.total = l_units[walk.n - 1];
+    const int total = l_units[walk.n - 1];
     const int grid = (int)gridDim.x;
     // With several items per SM and all keys and values in the L2 (126 MB), whole items are dealt out, the long ones first.
     // Otherwise the line of all key tiles is cut into equal shares, in up to three rounds: the CTAs of a round work on a
     // contiguous part of the line, so that fewer key heads are streamed at a time.
     const long long bytes = (long long)s_kv * hkv * D * 4;
     walk.dealt = l_items[walk.n - 1] >= 4 * grid && bytes <= TA_L2_BYTES;
-    const int rounds = (int)min(min((long long)kWideRounds, bytes / TA_L2_BYTES + 1), max(1LL, (long long)walk.total / (256LL * grid)));
-    walk.shares = min(grid * rounds, walk.total);
+    const int rounds = (int)min(min((long long)kWideRounds, bytes / TA_L2_BYTES + 1), max(1LL, (long long)total / (256LL * grid)));
+    walk.shares = min(grid * rounds, total);
+    walk.each = total / walk.shares;
+    walk.extra = total - walk.each * walk.shares;
     walk.share = (int)blockIdx.x;
     walk.u = walk.u1 = 0;
     if (!walk.dealt) {
@@ -323,8 +322,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     }
   }
   if (!some) {
-    asm volatile("griddepcontrol.wait;" ::: "memory");     // the kernel in front has ended
-    join_all<D, TA_THREADS>(c, p.join, &s_list);
+    // nothing may follow this grid in the stream before the kernels in front of it have ended
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     return;
   }
 
@@ -760,26 +759,31 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         __threadfence();
         const int first = sg.first, last = sg.last;
         auto part = [&](int x) { return (x == first ? sg.slot0 : 2 * x) * 2 + t; };
-        float M = -INFINITY;
-        for (int x = first; x <= last; ++x) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x);
-        const float mb = M == -INFINITY ? 0.f : M;
-        float L = 0.f;
-        for (int x = first; x <= last; ++x) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row);
-          L += ml.y * fast_exp2(ml.x - mb);
+        const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row;
+        float M = -INFINITY, L = 0.f;
+        for (int x = first; x <= last; x += 4) {               // four parts' statistics in flight
+          float2 v[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[i] = x + i <= last ? __ldcg(ml + part(x + i) * 128) : make_float2(-INFINITY, 0.f);
+          const float mn = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), M), mb = mn == -INFINITY ? 0.f : mn;
+          L *= fast_exp2(M - mb);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) L += v[i].y * fast_exp2(v[i].x - mb);
+          M = mn;
         }
-        const float iv = L == 0.f ? 0.f : 1.f / L;
+        const float mb = M == -INFINITY ? 0.f : M, iv = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll 1
         for (int q = 0; q < D / 64; ++q) {                     // 64 columns at a time: 16 loads in flight
           float4 a[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
           for (int x = first; x <= last; ++x) {
-            const float g = fast_exp2(__ldcg(reinterpret_cast<const float2*>(p.part_ml) + part(x) * 128 + row).x - mb);
             const float4* src = reinterpret_cast<const float4*>(p.part_o + (long long)part(x) * D * 128) + q * 16 * 128 + row;
             float4 v[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) v[i] = __ldcg(src + i * 128);
+            const float g = fast_exp2(__ldcg(ml + part(x) * 128).x - mb);
 #pragma unroll
             for (int i = 0; i < 16; ++i) { a[i].x += v[i].x * g; a[i].y += v[i].y * g; a[i].z += v[i].z * g; a[i].w += v[i].w * g; }
           }
@@ -804,8 +808,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");       // the kernel in front has ended
-  join_all<D, TA_THREADS>(c, p.join, &s_list);
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // as above
 }
 
 template <int D>
@@ -881,10 +884,9 @@ size_t tc_attention_scratch_bytes(int head_dim) {
   return (size_t)2 * kWideMaxShares * 2 * 128 * (head_dim + 2) * 4;
 }
 
-int launch_tc_attention(const AttnCall& c, int narrow_rows, const JoinCall& join, char* counters, char* scratch, cudaStream_t st) {
+int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st) {
   TaParams p{};
   p.c = c;
-  p.join = join;
   p.scale2 = c.scale * 1.4426950408889634f;
   p.narrow_rows = narrow_rows;
   p.tokens_per_tile = TA_TILE / c.G;
