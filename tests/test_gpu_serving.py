@@ -228,6 +228,15 @@ def test_plan_random_steps(seed):
     _run_plan(ctx, new, gone, page, sum(new) + 3, width, want if seed % 2 else want // 2, seed)
 
 
+def test_plan_most_requests():
+    r = torch.Generator().manual_seed(7)
+    B = 8192
+    ctx = torch.randint(0, 40, (B,), generator=r).tolist()
+    new = torch.randint(0, 3, (B,), generator=r).tolist()
+    ref = _run_plan(ctx, new, [b % 17 == 0 for b in range(B)], 16, sum(new), 4, 6000)
+    assert ref["admitted"][-1] == 1
+
+
 # ---------------------------------------------------------------------------------------------------------- attention
 def _attend(new, kv, H, Hkv, D, page=16, order="nhd", causal=True, window=0, seed=1, scale=None, qstd=1.5, std=1.0, edit=None,
             q_view=False, fill=float("nan")):
@@ -365,6 +374,70 @@ def test_attention_masked_keys_hold_anything(bad, new, kv):
         assert bool(torch.isfinite(out[-1, G:2 * G][:, keep]).all())
 
 
+@pytest.mark.parametrize("new", [1, 5, 60, 300])
+def test_attention_seen_values_that_are_not_finite(new):
+    # far from every mask: an infinite value reaches its column of every row, a NaN key every column
+    qb = _qb()
+    g = _gen(12)
+    kv, H, Hkv, D = 900, 4, 2, 128
+    ck, cv, table, ks, vs = make_cache(g, [kv], 16, Hkv, D, fill=0.0)
+    at = lambda c, j: c[int(table[0, j // 16]), j % 16]  # noqa: E731
+    at(cv, 200)[0, 7] = float("inf")
+    at(ck, 333)[1, 64] = float("nan")
+    q = torch.randn(new, H, D, generator=g, device=DEV).to(torch.bfloat16)
+    out, lse = qb.paged_attention(q, qb.KVCache(ck, cv), table, offsets([new]), torch.tensor([kv], dtype=torch.int32, device=DEV),
+                                  need_lse=True)
+    assert not bool(torch.isfinite(out[:, :2, 7]).any())
+    keep = torch.ones(D, dtype=torch.bool, device=DEV)
+    keep[7] = False
+    assert bool(torch.isfinite(out[:, :2][..., keep]).all()) and bool(torch.isfinite(lse[:, :2]).all())
+    assert bool(out[:, 2:].isnan().all()) and bool(lse[:, 2:].isnan().all())
+
+
+@pytest.mark.parametrize("new,kv", [([1, 1], [3000, 700]), ([6], [1500]), ([260, 40], [900, 640])])
+@pytest.mark.parametrize("jump", [30.0, 300.0])
+def test_attention_one_key_far_above_the_others(new, kv, jump):
+    # one late key outgrows the maximum of the first tile by 2^43 or 2^433: weights of fp32's range and beyond it
+    def plant(ks, vs, q, at):
+        t = 0
+        for b in range(len(new)):
+            for j in (kv[b] // 2, kv[b] - new[b] - 1):
+                u = q[t + new[b] // 2, 0].float()
+                ks[b][j, 0] = (u * (jump * 128 ** 0.5 / float(u @ u))).to(torch.bfloat16)
+                at(b, j)[0][0] = ks[b][j, 0]
+            t += new[b]
+    _attend(new, kv, 4, 1, 128, edit=plant, qstd=1.0, std=0.5)
+    _attend(new, kv, 2, 1, 64, edit=plant, qstd=1.0, std=0.5)
+
+
+@pytest.mark.parametrize("new,kv,D,window", [([1, 4, 40], [77, 130, 300], 128, 0), ([3, 20], [0, 64], 64, 9), ([2], [40], 24, 0)])
+def test_attention_general_path(monkeypatch, new, kv, D, window):
+    monkeypatch.setenv("QBLORA_FORCE_GENERAL", "1")
+    _attend(new, kv, 6, 2, D, window=window)
+
+
+def test_attention_on_two_streams_at_once():
+    qb = _qb()
+    g = _gen(21)
+    jobs = []
+    for new, kv in (([1] * 20, [1700] * 20), ([500], [2300])):
+        ck, cv, table, _, _ = make_cache(g, kv, 32, 4, 128, fill=0.0)
+        q = torch.randn(sum(new), 16, 128, generator=g, device=DEV).to(torch.bfloat16)
+        cache = qb.KVCache(ck, cv)
+        args = (q, cache, table, offsets(new), torch.tensor(kv, dtype=torch.int32, device=DEV))
+        jobs.append((args, qb.alloc_attention_workspace(cache, q), torch.cuda.Stream(), qb.paged_attention(*args)[0]))
+    torch.cuda.synchronize()
+    outs = [[], []]
+    for _ in range(10):
+        for i, (args, ws, st, _) in enumerate(jobs):
+            with torch.cuda.stream(st):
+                outs[i].append(qb.paged_attention(*args, ws=ws)[0])
+    torch.cuda.synchronize()
+    for i, (_, ws, _, ref) in enumerate(jobs):
+        assert all(torch.equal(o, ref) for o in outs[i])
+        assert qb.device_status(ws) == qb.OK
+
+
 def test_attention_on_another_stream_and_in_a_graph():
     # lengths and tables change between replays of one captured call
     qb = _qb()
@@ -480,3 +553,51 @@ def test_refusals_on_device_tensors():
         cnt = i(1)
         qb.kv_plan(i(1), i(1), i(1, 4), i(8), cnt, 16, 4, outs=(i(2), i(1), i(4), i(4), i(1), cnt))
     torch.cuda.synchronize()
+
+
+def test_a_merged_layer_decodes_as_it_would_over_the_whole_sequence():
+    # quantized linears -> plan -> rotary + append -> attention -> linear, in chunks and single tokens, against the same layer
+    # in 64 bits over each whole sequence.  The linears' bf16 outputs and the cache are shared, so what differs is rounding:
+    # the rotated q and k (2^-8 each, on scores of size s: 2 * 2^-8 * s), the weights and the result, as in tests/_serving.py.
+    qb = _qb()
+    g = _gen(31)
+    Dm, H, Hkv, D, page = 512, 8, 2, 64, 16
+    W = [torch.randn(n, Dm, generator=g, device=DEV) * 0.06 for n in (H * D, Hkv * D, Hkv * D)]
+    lin = [qb.quantize_blockwise(w, 64, 1, qb.FMT_AFFINE_MINMAX) for w in W]
+    rope = qb.Rope(D, D, qb.ROPE_HALF, qb.rope_table(D))
+    lens, B = [70, 3, 33], 3
+    X = [torch.randn(n, Dm, generator=g, device=DEV).to(torch.bfloat16) for n in lens]
+    cache = qb.KVCache.empty(24, page, Hkv, D)
+    cache.k.fill_(float("nan"))
+    cache.v.fill_(float("nan"))
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    table, stack, count = i32([[-1] * 8] * B), torch.randperm(24, generator=g, device=DEV).to(torch.int32), i32([24])
+    done, outs, proj = [0] * B, [[] for _ in range(B)], [[] for _ in range(B)]
+    for step in range(40):
+        new = [min(n - d, 40 if step == 0 else 1) for n, d in zip(lens, done)]
+        if not sum(new):
+            break
+        T = sum(new) + 2
+        plan = qb.kv_plan(i32(done), i32(new), table, stack, count, page, T)
+        count = plan.free_count
+        rows = torch.cat([X[b][done[b]:done[b] + new[b]] for b in range(B)] + [torch.zeros(2, Dm, dtype=torch.bfloat16, device=DEV)])
+        q, k, v = (qb.lowbit_gemm(w, rows).view(T, -1, D) for w in lin)
+        rq = qb.rope_append(rope, plan.positions, plan.slots, q, k, v, cache)
+        o, _ = qb.paged_attention(rq, cache, table, plan.cu_new, plan.kv_len)
+        assert plan.admitted.tolist() == [1] * B
+        t = 0
+        for b in range(B):
+            outs[b].append(o[t:t + new[b]])
+            proj[b].append((q[t:t + new[b]], k[t:t + new[b]], v[t:t + new[b]]))
+            t += new[b]
+            done[b] += new[b]
+    assert done == lens
+    for b in range(B):
+        q, k, v = (torch.cat([p[i] for p in proj[b]]) for i in range(3))
+        pos = torch.arange(lens[b], device=DEV)
+        rq, _ = ref_rope(q, pos, table_turns(rope.table), D, False)
+        rk, _ = ref_rope(k, pos, table_turns(rope.table), D, False)
+        ref, bound, _, _ = ref_attention(rq, [rk], [v], [lens[b]], [lens[b]], D ** -0.5)
+        S = torch.einsum("nhd,jhd->hnj", rq.abs(), rk.repeat_interleave(H // Hkv, 1).abs()).amax(-1).T * D ** -0.5
+        A = v.double().abs().amax()                                            # no weighted mean of |v| exceeds the largest |v|
+        within(torch.cat(outs[b]), ref, bound + (2.0 ** -7 * S)[..., None] * 2 * A, f"request {b}")
