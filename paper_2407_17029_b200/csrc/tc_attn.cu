@@ -40,6 +40,7 @@ constexpr int TA_THREADS = 384;
 constexpr int TA_TILE = 128;            // rows per row tile, keys per key tile
 constexpr float TA_LN2 = 0.69314718055994530942f;
 constexpr long long TA_L2_BYTES = 96000000;
+constexpr int TA_CUT = 6;               // key tiles that the cuts of a share cost
 constexpr int TA_SEGS = 4;              // segments handed out ahead
 constexpr float TA_SLACK = 8.0f;        // where the maximum is looked for: how far (in powers of two) it may be ahead of m
 constexpr float TA_OUTGROWN = 1.099511627776e12f;   // 2^40: a tile's sum of weights that asks for a new m
@@ -232,6 +233,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   int* l_items = l_req + kWideMaxRequests;
   __shared__ int s_n, s_over;
   __shared__ unsigned long long s_kv;              // keys of this kernel's requests
+  __shared__ int s_most, s_least;                  // key tiles of its longest and shortest item
+  __shared__ int s_key[TA_THREADS];
 
   __shared__ int s_warp_n[TA_THREADS / 32], s_warp_i[TA_THREADS / 32];
   __shared__ long long s_warp_u[TA_THREADS / 32];
@@ -247,7 +250,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   {
     int n_before = 0, i_before = 0;
     long long u_before = 0;
-    if (tid == 0) s_kv = 0;
+    if (tid == 0) { s_kv = 0; s_most = 0; s_least = 0x7fffffff; }
     __syncthreads();
     for (int b0 = 0; b0 < c.B; b0 += TA_THREADS) {
       const int b = b0 + tid;
@@ -261,8 +264,14 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           const int np = ta_pairs(p, r);
           items = np * hkv;
           int nt[2], lo;
-          for (int q = 0; q < np; ++q) units += ta_pair_tiles(p, r, q, nt, &lo);
+          int most = 0, least = 0x7fffffff;
+          for (int q = 0; q < np; ++q) {
+            const int u = ta_pair_tiles(p, r, q, nt, &lo);
+            units += u; most = max(most, u); least = min(least, u);
+          }
           units *= hkv;
+          atomicMax(&s_most, most);
+          atomicMin(&s_least, least);
         }
       }
       int ni = take, ii = items;
@@ -305,11 +314,14 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   if (some) {
     const int total = l_units[walk.n - 1];
     const int grid = (int)gridDim.x;
-    // With several items per SM and all keys and values in the L2 (126 MB), whole items are dealt out, the long ones first.
-    // Otherwise the line of all key tiles is cut into equal shares, in up to three rounds: the CTAs of a round work on a
-    // contiguous part of the line, so that fewer key heads are streamed at a time.
+    // Whole items are dealt out, the long ones first, where that ends about as early as equal shares of the line of all key
+    // tiles would: the last items to be dealt are the shortest, half of one is lost on average, while a share's borders
+    // cut two items, which costs about six key tiles (parts written, read and joined).  And only with all keys and values
+    // in the L2 (126 MB), since it works on all key heads at once.  Shares are taken in up to three rounds: the CTAs of a
+    // round work on a contiguous part of the line, so that fewer key heads are streamed at a time.
     const long long bytes = (long long)s_kv * hkv * D * 4;
-    walk.dealt = l_items[walk.n - 1] >= 4 * grid && bytes <= TA_L2_BYTES;
+    const int mean = total / grid;
+    walk.dealt = max(s_most, mean + (l_items[walk.n - 1] > grid ? s_least / 2 : 0)) <= mean + TA_CUT && bytes <= TA_L2_BYTES;
     const int rounds = (int)min(min((long long)kWideRounds, bytes / TA_L2_BYTES + 1), max(1LL, (long long)total / (256LL * grid)));
     walk.shares = min(grid * rounds, total);
     walk.each = total / walk.shares;
@@ -320,6 +332,34 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       some = walk.share < walk.shares;
       if (some) { walk.u = walk.begin(walk.share); walk.u1 = walk.begin(walk.share + 1); }
     }
+  }
+  if (some && walk.dealt && walk.n > 1 && walk.n <= TA_THREADS) {
+    // requests with the longest items first (in any order the result is the same)
+    int b = 0, items = 0, units = 0, key = 0;
+    if (tid < walk.n) {
+      b = l_req[tid];
+      items = l_items[tid] - (tid ? l_items[tid - 1] : 0);
+      units = l_units[tid] - (tid ? l_units[tid - 1] : 0);
+      const ReqView r = attn_request(c, b);
+      int nt[2], lo;
+      key = ta_pair_tiles(p, r, ta_pairs(p, r) - 1, nt, &lo);
+      s_key[tid] = key;
+    }
+    __syncthreads();
+    int rank = 0, i_before = 0, u_before = 0;
+    if (tid < walk.n) {
+      for (int i = 0; i < walk.n; ++i) {
+        const bool first = s_key[i] > key || (s_key[i] == key && i < tid);
+        rank += first;
+        if (first) {
+          i_before += l_items[i] - (i ? l_items[i - 1] : 0);
+          u_before += l_units[i] - (i ? l_units[i - 1] : 0);
+        }
+      }
+    }
+    __syncthreads();
+    if (tid < walk.n) { l_req[rank] = b; l_items[rank] = i_before + items; l_units[rank] = u_before + units; }
+    __syncthreads();
   }
   if (!some) {
     // nothing may follow this grid in the stream before the kernels in front of it have ended
