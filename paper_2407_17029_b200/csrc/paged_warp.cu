@@ -22,6 +22,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <mutex>
 
 #include "paged_join.cuh"
 #include "serving.cuh"
@@ -115,120 +116,33 @@ struct PwCursor {
   }
 };
 
-template <int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
-  __shared__ JoinShared list;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
-  join_all<D, 256>(c, j, &list);
-}
+// The line of all key tiles and its shares (all arrays in shared memory).
+template <int ROWS, int KT>
+struct PwLine {
+  const PwReq* known;        // the requests, where there is one for each thread; else nullptr
+  const int* units;          // [threads] inclusive sums of tiles over each thread's `per` requests
+  const int *base, *each;    // [levels + 1], [levels]: first tile of a level, tiles of its shares
+  int per, per_level, levels, shares, total, extra;   // of the last level, the first `extra` shares have one tile more
 
-// status word and counters
-__global__ void __launch_bounds__(256) attention_reset_kernel(uint4* ws, int n) {
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int i = blockIdx.x * 256 + threadIdx.x;
-  if (i < n) ws[i] = make_uint4(0, 0, 0, 0);
-}
-
-template <int D>
-__global__ void __launch_bounds__(PW_THREADS, 1)
-paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ PwParams p) {
-  using Sh = PwShape<D>;
-  constexpr int ROWS = Sh::ROWS, KT = Sh::KT, HALVES = D / 64, NT = KT / 8, PW_STAGES = Sh::STAGES;
-  using Cursor = PwCursor<ROWS, KT>;
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_full[PW_WARPS * PW_STAGES];
-  __shared__ long long s_scan[PW_WARPS];
-  __shared__ int s_units[PW_THREADS], s_base[PW_MAX_LEVELS + 1], s_each[PW_MAX_LEVELS];
-  __shared__ PwReq s_req[PW_THREADS];
-  __shared__ Cursor s_next[PW_WARPS];          // where the next share of each warp begins
-  const AttnCall& c = p.c;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t ring = base + warp * (PW_STAGES * Sh::STAGE);
-  const uint32_t full = smem_u32(s_full + warp * PW_STAGES);
-
-  if (lane == 0) {
-    for (int s = 0; s < PW_STAGES; ++s) mbar_init(full + 8 * s, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-
-  // ---- the line: units before each request, all units, the shares -----------------------------------------------------
-  const int per = (c.B + PW_THREADS - 1) / PW_THREADS;
-  const int b_lo = min(tid * per, c.B), b_hi = min(b_lo + per, c.B);
-  long long mine = 0;
-  for (int b = b_lo; b < b_hi; ++b) {
-    const ReqView r = attn_request(c, b);
-    const int hu = pw_mine(p, r) ? pw_head_units<ROWS, KT>(p, r) : 0;
-    mine += (long long)hu * c.cache.kv_heads;
-    if (per == 1) s_req[b] = PwReq{r.t0, r.n, r.kv, hu};
-  }
-  const PwReq* known = per == 1 ? s_req : nullptr;
-  long long incl = mine;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const long long y = __shfl_up_sync(0xffffffffu, incl, d);
-    if (lane >= d) incl += y;
-  }
-  if (lane == 31) s_scan[warp] = incl;
-  __syncthreads();
-  long long total_ = 0;
-#pragma unroll
-  for (int w = 0; w < PW_WARPS; ++w) {
-    if (w < warp) incl += s_scan[w];
-    total_ += s_scan[w];
-  }
-  s_units[tid] = (int)min(incl, 0x7fffffffLL);
-  // From here on this kernel writes what the reset kernel clears; and the kernel behind it, which reads nothing that this
-  // one writes before it has waited for its end, may start as SMs become free.
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (total_ == 0) return;
-  if (total_ > 0x7fffffffLL) {   // 2^31 tiles are 10^13 bytes of keys and values and more: the lengths cannot be meant
-    if (tid == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
-    return;
-  }
-  const int total = (int)total_;
-  // Shares: level k hands every warp one share; the levels' parts of the line are 1/2, 1/4, ... with the last two equal, so
-  // the shares that are taken late are short.  A share has more tiles than the ring has slots (then at most one share's
-  // beginning is in the ring besides the current one).
-  const int per_level = min((int)gridDim.x * PW_WARPS, max(1, total / (PW_STAGES + 1)));
-  int levels = 1;
-  while (levels < PW_MAX_LEVELS && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
-  const int shares = per_level * levels;
-  if (tid == 0) {
-    int at = 0;
-    for (int k = 0; k < levels; ++k) {
-      s_base[k] = at;
-      s_each[k] = (k + 1 < levels ? total >> (k + 1) : total - at) / per_level;
-      at += s_each[k] * per_level;
-    }
-    s_base[levels] = total;
-  }
-  __syncthreads();
-  // of the last level, the first `extra` shares have one tile more
-  const int extra = total - s_base[levels - 1] - s_each[levels - 1] * per_level;
-  auto share_begin = [&](int g) -> int {
+  __device__ __forceinline__ int begin(int g) const {
     if (g >= shares) return total;
     const int k = g / per_level, i = g - k * per_level;
-    return s_base[k] + i * s_each[k] + (k + 1 == levels ? min(i, extra) : 0);
-  };
-  auto share_of = [&](int u) -> int {
+    return base[k] + i * each[k] + (k + 1 == levels ? min(i, extra) : 0);
+  }
+  __device__ __forceinline__ int share_of(int u) const {
     int k = 0;
-    while (k + 1 < levels && u >= s_base[k + 1]) ++k;
-    const int v = u - s_base[k], each = s_each[k];
-    if (k + 1 < levels) return k * per_level + v / each;
-    const int cut = extra * (each + 1);
-    return k * per_level + (v < cut ? v / (each + 1) : extra + (v - cut) / each);
-  };
-  const int g_first = (int)blockIdx.x * PW_WARPS + warp;
-  if (g_first >= per_level) return;
-
-  // the cursor of unit u: a search over the threads' sums, a walk over that thread's requests
-  auto locate = [&](Cursor& at, int u) {
+    while (k + 1 < levels && u >= base[k + 1]) ++k;
+    const int v = u - base[k], n = each[k];
+    if (k + 1 < levels) return k * per_level + v / n;
+    const int cut = extra * (n + 1);
+    return k * per_level + (v < cut ? v / (n + 1) : extra + (v - cut) / n);
+  }
+  // the cursor of tile u: a search over the threads' sums, a walk over that thread's requests
+  __device__ __forceinline__ void locate(const PwParams& p, PwCursor<ROWS, KT>& at, int u) const {
+    const AttnCall& c = p.c;
     int a = 0, e = PW_THREADS;
-    while (a < e) { const int x = (a + e) >> 1; if (s_units[x] > u) e = x; else a = x + 1; }
-    int rest = u - (a ? s_units[a - 1] : 0), hu = 1;
+    while (a < e) { const int x = (a + e) >> 1; if (units[x] > u) e = x; else a = x + 1; }
+    int rest = u - (a ? units[a - 1] : 0), hu = 1;
     if (known) {
       at.b = a;
       at.r = ReqView{known[a].t0, known[a].n, known[a].kv};
@@ -249,19 +163,139 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     at.k = pw_range<ROWS, KT>(p, at.r, 0);
     while (left >= at.k.tiles) { left -= at.k.tiles; ++at.rt; at.k = pw_range<ROWS, KT>(p, at.r, at.rt); }
     at.tile = left;
-  };
+  }
+};
+
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
+  __shared__ JoinShared list;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
+  join_all<D, 256>(c, j, &list);
+}
+
+// status word and counters
+__global__ void __launch_bounds__(256) attention_reset_kernel(uint4* ws, int n) {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i < n) ws[i] = make_uint4(0, 0, 0, 0);
+}
+
+template <int D, bool CLUSTER>
+__global__ void __launch_bounds__(PW_THREADS, 1)
+paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ PwParams p) {
+  using Sh = PwShape<D>;
+  constexpr int ROWS = Sh::ROWS, KT = Sh::KT, HALVES = D / 64, NT = KT / 8, PW_STAGES = Sh::STAGES;
+  using Cursor = PwCursor<ROWS, KT>;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t s_full[PW_WARPS * PW_STAGES];
+  __shared__ long long s_scan[PW_WARPS];
+  __shared__ int s_units[PW_THREADS], s_base[PW_MAX_LEVELS + 1], s_each[PW_MAX_LEVELS];
+  __shared__ PwReq s_req[PW_THREADS];
+  __shared__ float2 s_ml[PW_WARPS + 1][16];    // CLUSTER: (m, l) of each warp's and of the CTA's part
+  __shared__ Cursor s_next[PW_WARPS];          // where the next share of each warp begins
+  const AttnCall& c = p.c;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
+  const uint32_t ring = base + warp * (PW_STAGES * Sh::STAGE);
+  const uint32_t full = smem_u32(s_full + warp * PW_STAGES);
+
+  if (lane == 0) {
+    for (int s = 0; s < PW_STAGES; ++s) mbar_init(full + 8 * s, 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+
+  PwLine<ROWS, KT> line{};           // not CLUSTER: the shares
+  int g = 0, u0, u1, g_next = 0;     // the share being computed, its tiles [u0, u1); lane 0: the share after it
+  Cursor ld;
+  if constexpr (CLUSTER) {
+    // one item per cluster, its tiles in equal parts for the cluster's warps: no line, no workspace, nothing to prepare
+    const int cs = (int)cluster_ctas(), item = (int)blockIdx.x / cs;
+    ld.h = item % c.cache.kv_heads;
+    ld.b = item / c.cache.kv_heads % c.B;
+    ld.rt = item / c.cache.kv_heads / c.B;       // last, so that the row tiles that requests do not have come after all others
+    ld.r = attn_request(c, ld.b);
+    ld.nrt = pw_row_tiles<ROWS>(p, ld.r);
+    if (ld.rt >= ld.nrt) return;     // the whole cluster
+    ld.k = pw_range<ROWS, KT>(p, ld.r, ld.rt);
+    const int parts = cs * PW_WARPS, me = (int)cluster_ctarank() * PW_WARPS + warp;
+    u0 = (int)((long long)ld.k.tiles * me / parts);
+    u1 = (int)((long long)ld.k.tiles * (me + 1) / parts);
+    ld.tile = u0;
+  } else {
+    // ---- the line: units before each request, all units, the shares -----------------------------------------------------
+    const int per = (c.B + PW_THREADS - 1) / PW_THREADS;
+    const int b_lo = min(tid * per, c.B), b_hi = min(b_lo + per, c.B);
+    long long mine = 0;
+    for (int b = b_lo; b < b_hi; ++b) {
+      const ReqView r = attn_request(c, b);
+      const int hu = pw_mine(p, r) ? pw_head_units<ROWS, KT>(p, r) : 0;
+      mine += (long long)hu * c.cache.kv_heads;
+      if (per == 1) s_req[b] = PwReq{r.t0, r.n, r.kv, hu};
+    }
+    const PwReq* known = per == 1 ? s_req : nullptr;
+    long long incl = mine;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, incl, d);
+      if (lane >= d) incl += y;
+    }
+    if (lane == 31) s_scan[warp] = incl;
+    __syncthreads();
+    long long total_ = 0;
+#pragma unroll
+    for (int w = 0; w < PW_WARPS; ++w) {
+      if (w < warp) incl += s_scan[w];
+      total_ += s_scan[w];
+    }
+    s_units[tid] = (int)min(incl, 0x7fffffffLL);
+    // From here on this kernel writes what the reset kernel clears; and the kernel behind it, which reads nothing that this
+    // one writes before it has waited for its end, may start as SMs become free.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (total_ == 0) return;
+    if (total_ > 0x7fffffffLL) {   // 2^31 tiles are 10^13 bytes of keys and values and more: the lengths cannot be meant
+      if (tid == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
+      return;
+    }
+    const int total = (int)total_;
+    // Shares: level k hands every warp one share; the levels' parts of the line are 1/2, 1/4, ... with the last two equal, so
+    // the shares that are taken late are short.  A share has more tiles than the ring has slots (then at most one share's
+    // beginning is in the ring besides the current one).
+    const int per_level = min((int)gridDim.x * PW_WARPS, max(1, total / (PW_STAGES + 1)));
+    int levels = 1;
+    while (levels < PW_MAX_LEVELS && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
+    const int shares = per_level * levels;
+    if (tid == 0) {
+      int at = 0;
+      for (int k = 0; k < levels; ++k) {
+        s_base[k] = at;
+        s_each[k] = (k + 1 < levels ? total >> (k + 1) : total - at) / per_level;
+        at += s_each[k] * per_level;
+      }
+      s_base[levels] = total;
+    }
+    __syncthreads();
+    // of the last level, the first `extra` shares have one tile more
+    const int extra = total - s_base[levels - 1] - s_each[levels - 1] * per_level;
+    line.known = known; line.units = s_units; line.base = s_base; line.each = s_each; line.per = per;
+    line.per_level = per_level; line.levels = levels; line.shares = shares; line.total = total; line.extra = extra;
+    g = (int)blockIdx.x * PW_WARPS + warp;
+    if (g >= per_level) return;
+    u0 = line.begin(g);
+    u1 = line.begin(g + 1);
+    g_next = shares;
+    if (lane == 0 && levels > 1) g_next = (int)atomicAdd(p.counters, 1u) + per_level;
+    line.locate(p, ld, u0);
+  }
+  const PwReq* known = line.known;
 
   bool ok = true;
   int odd_pages = 0;
   {
-    int g = g_first, u0 = share_begin(g), u1 = share_begin(g + 1);   // the share being computed
-    int g_next = shares;                                             // lane 0: the share after it
-    if (lane == 0 && levels > 1) g_next = (int)atomicAdd(p.counters, 1u) + per_level;
-    Cursor ld;
-    locate(ld, u0);
     Cursor cu = ld;
     int ld_left = u1 - u0;            // tiles of the share being loaded that are not issued yet
-    int ld_next_g = -1;                // the share being loaded, where that is the one after g; `shares` or more: none left
+    int ld_next_g = -1;               // the share being loaded, where that is the one after g; `shares` or more: none left
 
     // ---- loads: lane i issues box i: (K or V, half of the head, run of keys) ------------------------------------------
     const int runs = KT / p.box_keys;                 // boxes along the keys
@@ -277,7 +311,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       return __ldg(c.table + (long long)ld.b * c.width + j);
     };
     uint32_t issued = 0, done = 0;
-    int entry, page = lookup(entry), st_ld = 0;
+    int entry = 0, page = ld_left > 0 ? lookup(entry) : c.cache.n_pages, st_ld = 0;
     auto issue = [&](uint32_t dep) {
       if (page < 0 || page > c.cache.n_pages) { odd_pages = 1; page = c.cache.n_pages; }
       if (lane < n_boxes && page == c.cache.n_pages && ld.k.lo + ld.tile * KT + my_run * p.box_keys < ld.k.hi) odd_pages = 1;
@@ -290,13 +324,13 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (--ld_left > 0) ld.next(p, known);
       else {
         ld_next_g = __shfl_sync(0xffffffffu, g_next, 0);
-        if (ld_next_g >= shares) return;                       // ld_left stays 0: nothing more to issue
-        const int b0 = share_begin(ld_next_g);
-        locate(ld, b0);
-        ld_left = share_begin(ld_next_g + 1) - b0;
+        if (ld_next_g >= line.shares) return;                  // ld_left stays 0: nothing more to issue
+        const int b0 = line.begin(ld_next_g);
+        line.locate(p, ld, b0);
+        ld_left = line.begin(ld_next_g + 1) - b0;
         if (lane == 0) {
           s_next[warp] = ld;
-          g_next = (int)atomicAdd(p.counters, 1u) + per_level;
+          g_next = (int)atomicAdd(p.counters, 1u) + line.per_level;
         }
         __syncwarp();
       }
@@ -320,16 +354,21 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     bool first_segment = true, fresh = true;     // of the share; of the item
     int u = u0;                                  // the tile being computed
 
-    while (true) {
+    if (CLUSTER && u0 == u1) {                    // more warps than tiles
+      m[0] = m[1] = -INFINITY;
+      l[0] = l[1] = 0.f;
+#pragma unroll
+      for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
+    } else while (true) {
       if (fresh) {
         fresh = false;
-        if (first_segment && cu.tile > 0 && lane == 0) {
+        if (!CLUSTER && first_segment && cu.tile > 0 && lane == 0) {
           // this share begins inside an item: the first share that does tells the join kernel about it
           const int item_first = u0 - cu.tile, first = g - 1;
-          if (share_begin(first) <= item_first) {
-            const int n = share_of(item_first + cu.k.tiles - 1) - first + 1;
+          if (line.begin(first) <= item_first) {
+            const int n = line.share_of(item_first + cu.k.tiles - 1) - first + 1;
             // its first part is the first share's last segment (slot 1) unless that share begins with the item; the others' first (slot 0)
-            p.cuts[g] = JoinCut{2 * first + (share_begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
+            p.cuts[g] = JoinCut{2 * first + (line.begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
                               min(ROWS, cu.r.n * c.G - cu.rt * ROWS), cu.h, 0};
             p.counters[1 + g] = 1;
           }
@@ -512,7 +551,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (++stage == PW_STAGES) { stage = 0; ph ^= 1u; }
 
       // ---- end of an item, or of this share's part of it --------------------------------------------------------------
-      if (cu.tile + 1 == cu.k.tiles || u + 1 == u1) {
+      if (CLUSTER && u + 1 == u1) break;
+      if (!CLUSTER && (cu.tile + 1 == cu.k.tiles || u + 1 == u1)) {
         const int item_first = u - cu.tile;
         const bool whole = item_first >= u0 && item_first + cu.k.tiles <= u1;
         const long long slot = 2 * g + (first_segment ? 0 : 1);   // of partial results
@@ -544,11 +584,11 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       if (++u < u1) { cu.next(p, known); continue; }
       // the next share: its tiles are on their way already
-      if (ld_next_g < 0 || ld_next_g >= shares) break;
+      if (ld_next_g < 0 || ld_next_g >= line.shares) break;
       g = ld_next_g;
       ld_next_g = -1;
-      u = u0 = share_begin(g);
-      u1 = share_begin(g + 1);
+      u = u0 = line.begin(g);
+      u1 = line.begin(g + 1);
       cu = s_next[warp];
       first_segment = fresh = true;
     }
@@ -557,6 +597,67 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     }
     if (__any_sync(0xffffffffu, odd_pages) && lane == 0) atomicExch(c.status, (int)QBLORA_ERR_INVALID_ARG);
 
+    if constexpr (CLUSTER) {
+      // ---- the warps' parts become the CTA's in its shared memory, the CTAs' the item's through the cluster's ------------
+      static_assert(16 * D * 4 <= Sh::STAGE, "a warp's part fits a slot of its ring, the CTA's the next slot of the first ring");
+      const int r0 = cu.rt * ROWS, rows = min(ROWS, cu.r.n * c.G - r0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float sum = l[i];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        const int row = (lane >> 2) + 8 * i;
+        float* d = reinterpret_cast<float*>(smem_raw + (ring - raw)) + row * D + 2 * (lane & 3);
+#pragma unroll
+        for (int n = 0; n < D / 8; ++n) *reinterpret_cast<float2*>(d + 8 * n) = make_float2(o[n][2 * i], o[n][2 * i + 1]);
+        if ((lane & 3) == 0) s_ml[warp][row] = make_float2(m[i], sum);
+      }
+      __syncthreads();
+      constexpr int LANES = D / 4;
+      const uint32_t cta_part = base + Sh::STAGE;
+      for (int i = tid; i < rows * LANES; i += PW_THREADS) {
+        const int row = i / LANES, col = i % LANES;
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int w = 0; w < PW_WARPS; ++w) M = fmaxf(M, s_ml[w][row].x);
+        const float b = M == -INFINITY ? 0.f : M;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < PW_WARPS; ++w) {
+          const float2 ml = s_ml[w][row];
+          const float f = fast_exp2(ml.x - b);
+          const float4 v = *reinterpret_cast<const float4*>(smem_raw + (base - raw) + w * (PW_STAGES * Sh::STAGE) + (row * D + 4 * col) * 4);
+          L += ml.y * f;
+          acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+        }
+        *reinterpret_cast<float4*>(smem_raw + (cta_part - raw) + (row * D + 4 * col) * 4) = acc;
+        if (col == 0) s_ml[PW_WARPS][row] = make_float2(M, L);
+      }
+      cluster_sync_all();
+      const int cs = (int)cluster_ctas(), rank = (int)cluster_ctarank();
+      const uint32_t cta_ml = smem_u32(&s_ml[PW_WARPS][0]);
+      for (int i = tid; i < rows * LANES; i += PW_THREADS) {
+        const int row = i / LANES, col = i % LANES;
+        if (row % cs != rank) continue;
+        float M = -INFINITY, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int x = 0; x < cs; ++x) {
+          const float2 ml = ld_cluster2(map_to_cta(cta_ml + 8 * row, x));
+          const float4 v = ld_cluster4(map_to_cta(cta_part + (row * D + 4 * col) * 4, x));
+          const float mn = fmaxf(M, ml.x), b = mn == -INFINITY ? 0.f : mn, fa = fast_exp2(M - b), fb = fast_exp2(ml.x - b);
+          M = mn;
+          L = L * fa + ml.y * fb;
+          acc.x = acc.x * fa + v.x * fb; acc.y = acc.y * fa + v.y * fb;
+          acc.z = acc.z * fa + v.z * fb; acc.w = acc.w * fa + v.w * fb;
+        }
+        const int gr = r0 + row, tok = fast_div(gr, c.G, p.div_group), head = cu.h * c.G + gr - tok * c.G;
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        *reinterpret_cast<uint2*>(c.out + (long long)(cu.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + 4 * col) =
+            make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+        if (c.lse && col == 0) c.lse[(long long)(cu.r.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * PW_LN2;
+      }
+      cluster_sync_all();              // no CTA leaves while another reads its part
+    }
   }
 }
 
@@ -567,7 +668,7 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
   int dev = 0, sms = 0;
   QB_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
-  auto kernel = paged_warp_kernel<D>;
+  auto kernel = paged_warp_kernel<D, false>;
   if (!attr_set[dev].load(std::memory_order_acquire)) {
     QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM));
     attr_set[dev].store(true, std::memory_order_release);
@@ -597,6 +698,88 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
   return QBLORA_OK;
 }
 
+// Clusters of `1 << i` CTAs that the device holds at once, for i = 0 ... 4; 0 where it does not take that size.
+struct PwResident { int n[5]; };
+
+template <int D>
+int pw_resident(const PwResident** out) {
+  using Sh = PwShape<D>;
+  static PwResident table[64];
+  static std::atomic<bool> ready[64];
+  static std::mutex once;
+  int dev = 0;
+  QB_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
+  if (!ready[dev].load(std::memory_order_acquire)) {
+    std::lock_guard<std::mutex> hold(once);
+    auto kernel = paged_warp_kernel<D, true>;
+    QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM));
+    const bool wide = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    for (int i = 0; i < 5; ++i) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(1u << i);
+      cfg.blockDim = dim3(PW_THREADS);
+      cfg.dynamicSmemBytes = Sh::SMEM;
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim = {1u << i, 1, 1};
+      cfg.attrs = attr; cfg.numAttrs = 1;
+      int n = 0;
+      if ((i == 4 && !wide) || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) n = 0;
+      table[dev].n[i] = n;
+    }
+    (void)cudaGetLastError();
+    ready[dev].store(true, std::memory_order_release);
+  }
+  *out = &table[dev];
+  return QBLORA_OK;
+}
+
+// No request has more rows than the call.
+int pw_row_tiles_bound(const AttnCall& c) { return (int)((c.T * c.G + 15) / 16); }
+
+// CTAs per cluster; 0: not this form.  The largest size with which all items are resident at once (a second wave costs more
+// than the split gains: 16 items of 513 keys, clusters of 4 11.1 us, of 8 15.3 us).  Then the lengths, which the host does not
+// know, are bounded by the table's width, because a cluster's item has only its own SMs and the line has them all.  Measured
+// (D 128, line / cluster):
+//   one request: 8 heads, 2 keys 15.7 / 10.3 us, 513 14.9 / 10.3, 8192 34 / 18.5, 32768 62 / 43;  2 heads, 32768 86 / 28;
+//                16 heads (clusters of 4), 8192 30 / 26.6, 32768 68 / 76;
+//   several, which may be uneven -- all keys in one of them at worst: 4 x 8 heads (clusters of 4), 8192 41 / 33, worst 34 / 27;
+//                at 32768 115 / 98, worst 62 / 75;  8 x 8 heads (2), 2048 22.5 / 18.5;  8 x 16 heads (1), 2048 36 / 31.
+int pw_cluster_size(const AttnCall& c, const PwResident& r) {
+  const int64_t tiles = std::min<int64_t>((int64_t)c.B * pw_row_tiles_bound(c), c.B + c.T * c.G / 16);   // of all requests, at most
+  const int64_t items = tiles * c.cache.kv_heads, keys = (int64_t)c.width * c.cache.page_size;
+  for (int i = 4; i >= 0; --i)
+    if (items <= r.n[i]) return keys <= ((c.B == 1 ? 4096LL : 2048LL) << i) ? 1 << i : 0;
+  return 0;
+}
+
+template <int D>
+int pw_launch_cluster(const PwParams& p, const CUtensorMap& tk, const CUtensorMap& tv, int cs, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.c.B * p.c.cache.kv_heads * pw_row_tiles_bound(p.c) * cs));
+  cfg.blockDim = dim3(PW_THREADS);
+  cfg.dynamicSmemBytes = PwShape<D>::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim = {(unsigned)cs, 1, 1};
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_warp_kernel<D, true>, tk, tv, p));
+  count_launch();
+  return QBLORA_OK;
+}
+
+int pw_params(const AttnCall& c, PwParams* p, CUtensorMap* tk, CUtensorMap* tv) {
+  p->c = c;
+  p->scale2 = c.scale * 1.4426950408889634f;
+  p->box_keys = std::min(c.cache.page_size, c.D == 64 ? 32 : 16);
+  p->div_page = fast_div_magic((uint32_t)c.cache.page_size);
+  p->div_group = fast_div_magic((uint32_t)c.G);
+  p->wait_limit = wait_limit_cycles();
+  return make_cache_maps(c, p->box_keys, tk, tv);
+}
+
 }  // namespace
 
 static_assert(PW_WARPS == kPagedWarps, "shares per SM");
@@ -619,17 +802,29 @@ bool paged_warp_supported(const AttnCall& c) {
 
 int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st) {
   PwParams p{};
-  p.c = c;
-  p.scale2 = c.scale * 1.4426950408889634f;
-  p.narrow_rows = narrow_rows;
-  p.box_keys = std::min(c.cache.page_size, c.D == 64 ? 32 : 16);
-  p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
-  p.div_group = fast_div_magic((uint32_t)c.G);
-  p.wait_limit = wait_limit_cycles();
   CUtensorMap tk, tv;
-  int rc = make_cache_maps(c, p.box_keys, &tk, &tv);
+  const int rc = pw_params(c, &p, &tk, &tv);
   if (rc) return rc;
+  p.narrow_rows = narrow_rows;
   return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, st) : pw_launch<128>(p, tk, tv, counters, scratch, st);
+}
+
+int paged_cluster_size(const AttnCall& c, int* size) {
+  *size = 0;
+  if (!paged_warp_supported(c) || c.T * c.G > 32) return QBLORA_OK;
+  const PwResident* r = nullptr;
+  const int rc = c.D == 64 ? pw_resident<64>(&r) : pw_resident<128>(&r);
+  if (rc) return rc;
+  *size = pw_cluster_size(c, *r);
+  return QBLORA_OK;
+}
+
+int launch_paged_cluster(const AttnCall& c, int size, cudaStream_t st) {
+  PwParams p{};
+  CUtensorMap tk, tv;
+  const int rc = pw_params(c, &p, &tk, &tv);
+  if (rc) return rc;
+  return c.D == 64 ? pw_launch_cluster<64>(p, tk, tv, size, st) : pw_launch_cluster<128>(p, tk, tv, size, st);
 }
 
 }  // namespace qb

@@ -107,6 +107,11 @@ struct JoinCall {
 bool paged_warp_supported(const AttnCall& c);
 int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
 
+// The same kernel for calls so small that every item has a cluster of CTAs to itself: one launch, no workspace but the status
+// word (zeroed on the stream).  paged_cluster_size gives the CTAs per cluster, 0 where the call is none of these.
+int paged_cluster_size(const AttnCall& c, int* size);
+int launch_paged_cluster(const AttnCall& c, int size, cudaStream_t st);
+
 // Many rows per key head (tc_attn.cu): requests with more than `narrow_rows` rows.  Launched behind launch_paged_warp, beside whose
 // kernels it may start as SMs become free.
 constexpr int kWideMaxRequests = 1024;

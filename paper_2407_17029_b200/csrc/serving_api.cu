@@ -155,7 +155,17 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   c.scale = scale; c.causal = causal != 0; c.window = window;
   c.status = static_cast<int*>(ws);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  int rc = launch_attention_reset(ws, st);
+  int rc = QBLORA_OK;
+  if (!force_general()) {
+    int cluster = 0;
+    rc = paged_cluster_size(c, &cluster);
+    if (rc) return rc;
+    if (cluster) {
+      QB_CUDA(cudaMemsetAsync(ws, 0, 16, st));
+      return launch_paged_cluster(c, cluster, st);
+    }
+  }
+  rc = launch_attention_reset(ws, st);
   if (rc) return rc;
   if (force_general()) return launch_simt_attention(c, st);
   char* wide_counters = static_cast<char*>(ws) + kStatusBytes;

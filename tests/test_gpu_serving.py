@@ -288,6 +288,36 @@ def test_attention_head_sizes(D):
     _attend([1, 3, 20, 70], [50, 200, 20, 333], 4, 2, D)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,kv,H,Hkv", [
+    ([1], [2000], 8, 1), ([1], [1], 4, 4), ([1], [513], 32, 8), ([4], [900], 32, 4), ([1], [700], 16, 16), ([1], [333], 34, 34),
+    ([1], [129], 80, 80), ([1] * 6, [1, 0, 17, 400, 2, 96], 16, 4), ([0, 3, 0, 2, 1], [5, 3, 0, 700, 257], 15, 3),
+    ([17, 1, 0, 14], [17, 300, 9, 5], 3, 3), ([1] * 9, [40 * i + 1 for i in range(9)], 21, 7), ([32], [33], 2, 2),
+])
+def test_attention_calls_of_few_rows(new, kv, H, Hkv, D):
+    # every number of CTAs per key head, more of them than key tiles, row tiles that few requests have
+    _attend(new, kv, H, Hkv, D)
+    _attend(new, kv, H, Hkv, D, page=8, order="hnd", causal=False, seed=2)
+    _attend(new, kv, H, Hkv, D, page=64, window=100, q_view=True, seed=3)
+
+
+@pytest.mark.parametrize("new,kv", [([1], [5000]), ([2, 0, 1, 1], [900, 5, 1, 0]), ([1] * 5, [3000, 3, 17, 64, 2000])])
+def test_attention_does_not_depend_on_the_tables_width(new, kv):
+    # columns behind a request's pages are never read; a wide table's call may be worked on in another way
+    qb = _qb()
+    g = _gen(21)
+    ck, cv, table, ks, vs = make_cache(g, kv, 16, 4, 128)
+    q = torch.randn(sum(new), 16, 128, generator=g, device=DEV).to(torch.bfloat16)
+    ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, 128 ** -0.5)
+    for width in (table.shape[1], 1024, 9000, 100000):
+        wide = torch.full((len(kv), width), -1, dtype=torch.int32, device=DEV)
+        wide[:, :table.shape[1]] = table
+        out, lse = qb.paged_attention(q, qb.KVCache(ck, cv), wide, offsets(new), torch.tensor(kv, dtype=torch.int32, device=DEV),
+                                      need_lse=True)
+        within(out, ref, bound, "out")
+        within(lse, rl, lb, "lse")
+
+
 @pytest.mark.parametrize("H,Hkv", HEADS)
 def test_attention_chunks(H, Hkv):
     _attend([1, 37, 128, 1, 200], [600, 37, 129, 1, 777], H, Hkv, 128)
