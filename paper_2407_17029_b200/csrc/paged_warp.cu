@@ -337,6 +337,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       page = lookup(entry);
     };
     for (int s = 0; s < PW_STAGES && ld_left > 0; ++s) issue(0);
+    if constexpr (CLUSTER) asm volatile("griddepcontrol.wait;" ::: "memory");   // the status word is cleared
 
     // ldmatrix offsets of this lane: row and swizzled chunk pair i of a 128-byte span, for K (as it lies) and V (transposed)
     uint32_t xk[4], xv[4];
@@ -761,10 +762,12 @@ int pw_launch_cluster(const PwParams& p, const CUtensorMap& tk, const CUtensorMa
   cfg.blockDim = dim3(PW_THREADS);
   cfg.dynamicSmemBytes = PwShape<D>::SMEM;
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim = {(unsigned)cs, 1, 1};
-  cfg.attrs = attr; cfg.numAttrs = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 2;
   QB_CUDA(cudaLaunchKernelEx(&cfg, paged_warp_kernel<D, true>, tk, tv, p));
   count_launch();
   return QBLORA_OK;
@@ -784,8 +787,8 @@ int pw_params(const AttnCall& c, PwParams* p, CUtensorMap* tk, CUtensorMap* tv) 
 
 static_assert(PW_WARPS == kPagedWarps, "shares per SM");
 
-int launch_attention_reset(void* ws, cudaStream_t st) {
-  constexpr int n = (int)(kAttnResetBytes / 16);
+int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st) {
+  const int n = (int)(bytes / 16);
   static_assert(kAttnResetBytes % 16 == 0, "whole words");
   attention_reset_kernel<<<(n + 255) / 256, 256, 0, st>>>(static_cast<uint4*>(ws), n);
   count_launch();

@@ -86,7 +86,7 @@ constexpr int kWideRounds = 3, kWideMaxShares = kPagedMaxSms * kWideRounds;     
 constexpr size_t kWideCounterBytes = (size_t)(1 + 2 * kWideMaxShares) * 4 / 256 * 256 + 256;
 constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256;
 constexpr size_t kAttnResetBytes = kStatusBytes + kWideCounterBytes + kPagedCounterBytes;
-int launch_attention_reset(void* ws, cudaStream_t st);
+int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st);    // zeroes that many, a multiple of 16
 
 // Any head size up to 256, any page size and strides that are multiples of 8 elements (paged_attn.cu).
 size_t paged_attention_scratch_bytes(int head_dim);
