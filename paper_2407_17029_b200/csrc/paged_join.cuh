@@ -3,7 +3,11 @@
 //
 // A part is (m, l, o) per row: running maximum in base 2, sum of weights, sum of weighted values, over some of the item's keys.
 // With M = max m_i:  l = sum l_i 2^(m_i - M),  o = sum o_i 2^(m_i - M),  out = o / l,  lse = (M + log2 l) ln 2.
-// Parts are taken in share order, so results do not depend on timing.
+// Parts are taken in a fixed order, so results do not depend on timing (the order of the lists of cut items does, and has no
+// influence on them).
+//
+// What bounds it is latency: a row's parts are a few KB that lie in L2.  So a row of a short item is one warp's, with 16 parts in
+// flight, rows go evenly over all warps of the device, and only an item of more than kJoinShort parts takes a CTA per row.
 #pragma once
 #include "mma_frag.cuh"
 #include "serving.cuh"
@@ -11,80 +15,85 @@
 
 namespace qb {
 
-// Rows rb .. (STEP = 128 / D of them, below r1) of one item by one warp, PB parts in flight, D / 4 lanes a row.
+struct JoinAcc { float M, L; float4 o; };
+
+// Parts a, a + step, ... below x.n of one row: this lane's 4 columns.
 template <int D, int PB>
-__device__ __forceinline__ void join_rows(const AttnCall& c, const JoinCall& j, const JoinCut& x, int rb, int r1) {
-  constexpr int LANES = D / 4;
-  const int lane = threadIdx.x & 31, col = (lane % LANES) * 4, row = rb + lane / LANES;
-  if (row >= r1) return;
-  float M = -INFINITY, L = 0.f;
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i0 = 0; i0 < x.n; i0 += PB) {
+__device__ __forceinline__ JoinAcc join_parts(const AttnCall& c, const JoinCall& j, const JoinCut& x, int row, int col, int a, int step) {
+  JoinAcc r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+  for (int i0 = a; i0 < x.n; i0 += PB * step) {
     float2 ml[PB];
     float4 v[PB];
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       ml[i] = make_float2(-INFINITY, 0.f);
       v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-      const int k = i0 + i;
+      const int k = i0 + i * step;
       if (k < x.n) {
-        const long long at = (long long)(k == 0 ? x.slot0 : 2 * (x.first + k)) * j.rows_per_slot + row;
+        const long long at = (long long)(k == 0 ? x.slot0 : 2 * (x.first + k * c.cache.kv_heads)) * j.rows_per_slot + row;
         ml[i] = __ldcg(reinterpret_cast<const float2*>(j.part_ml + at * 2));
         v[i] = __ldcg(reinterpret_cast<const float4*>(j.part_o + at * D + col));
       }
     }
-    float mn = M;
+    float mn = r.M;
 #pragma unroll
     for (int i = 0; i < PB; ++i) mn = fmaxf(mn, ml[i].x);
-    const float b = mn == -INFINITY ? 0.f : mn, f = fast_exp2(M - b);
-    M = mn;
-    L *= f; acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+    const float b = mn == -INFINITY ? 0.f : mn, f = fast_exp2(r.M - b);
+    r.M = mn;
+    r.L *= f; r.o.x *= f; r.o.y *= f; r.o.z *= f; r.o.w *= f;
 #pragma unroll
     for (int i = 0; i < PB; ++i) {
       const float g = fast_exp2(ml[i].x - b);
-      L += ml[i].y * g;
-      acc.x += v[i].x * g; acc.y += v[i].y * g; acc.z += v[i].z * g; acc.w += v[i].w * g;
+      r.L += ml[i].y * g;
+      r.o.x += v[i].x * g; r.o.y += v[i].y * g; r.o.z += v[i].z * g; r.o.w += v[i].w * g;
     }
   }
-  const int gr = x.r0 + row, tok = fast_div(gr, c.G, j.div_group), head = x.h * c.G + gr - tok * c.G;
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  *reinterpret_cast<uint2*>(c.out + (long long)(x.t0 + tok) * c.o_ts + (long long)head * c.o_hs + col) =
-      make_uint2(ptx::pack_bf16x2(acc.x * inv, acc.y * inv), ptx::pack_bf16x2(acc.z * inv, acc.w * inv));
-  if (c.lse && col == 0) c.lse[(long long)(x.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.69314718055994530942f;
+  return r;
 }
 
-// All cut items, spread over the grid by share border and quarter of the rows (neighbouring CTAs get the quarters of one
-// item); the pieces of a CTA go round its warps, so that they run side by side.  Called by all threads of the CTA.
-constexpr int kJoinList = (4 * kPagedMaxShares + 63) / 64;
-struct JoinShared { int n; short quarter[kJoinList]; JoinCut cut[kJoinList]; };
-template <int D, int THREADS>
-__device__ __forceinline__ void join_all(const AttnCall& c, const JoinCall& j, JoinShared* sh) {
-  constexpr int STEP = 32 / (D / 4);
-  const int tid = threadIdx.x, warp = tid >> 5;
-  if (tid == 0) sh->n = 0;
-  __syncthreads();
-  for (int i = blockIdx.x + tid * gridDim.x; i < 4 * j.borders; i += THREADS * gridDim.x) {
-    const int g = i >> 2;
-    if (__ldcg(j.flags + g)) {
-      const JoinCut x = j.cuts[g];
-      const int rows = (x.rows + 3) / 4, r = (i & 3) * rows;        // this quarter's rows
-      if (r < x.rows) {
-        const int at = atomicAdd(&sh->n, 1);
-        sh->cut[at] = x;
-        sh->quarter[at] = (short)r;
-      }
-    }
+__device__ __forceinline__ void join_store(const AttnCall& c, const JoinCall& j, const JoinCut& x, int row, int col, const JoinAcc& r) {
+  const int gr = x.r0 + row, tok = fast_div(gr, c.G, j.div_group), head = x.h * c.G + gr - tok * c.G;
+  const float inv = r.L == 0.f ? 0.f : 1.f / r.L;
+  *reinterpret_cast<uint2*>(c.out + (long long)(x.t0 + tok) * c.o_ts + (long long)head * c.o_hs + col) =
+      make_uint2(ptx::pack_bf16x2(r.o.x * inv, r.o.y * inv), ptx::pack_bf16x2(r.o.z * inv, r.o.w * inv));
+  if (c.lse && col == 0)
+    c.lse[(long long)(x.t0 + tok) * c.H + head] = r.L == 0.f ? -INFINITY : (r.M + log2f(r.L)) * 0.69314718055994530942f;
+}
+
+// All cut items.  Called by all threads of the CTA.
+template <int D>
+struct JoinShared { float2 ml[kJoinThreads / (D / 4)]; float4 o[kJoinThreads]; };
+template <int D>
+__device__ __forceinline__ void join_all(const AttnCall& c, const JoinCall& j, JoinShared<D>* sh) {
+  constexpr int LANES = D / 4, GROUPS = kJoinThreads / LANES;    // lanes of a row; rows that a CTA works on side by side
+  const int tid = threadIdx.x, grp = tid / LANES, lane = tid % LANES, col = 4 * lane;
+  const int n_short = (int)__ldcg(j.counts), n_long = (int)__ldcg(j.counts + 1), rows = (int)__ldcg(j.counts + 2);
+  for (long long i = (long long)grp * gridDim.x + blockIdx.x; i < (long long)n_short * rows; i += (long long)GROUPS * gridDim.x) {
+    const int row = (int)(i / n_short);
+    const JoinCut x = j.cuts[i - (long long)row * n_short];
+    if (row < x.rows) join_store(c, j, x, row, col, join_parts<D, 16>(c, j, x, row, col, 0, 1));
   }
-  __syncthreads();
-  int next = warp;                                         // pieces until this warp's next one
-  for (int i = 0; i < sh->n; ++i) {
-    const JoinCut& x = sh->cut[i];
-    const int r0 = sh->quarter[i], r1 = min(x.rows, r0 + (x.rows + 3) / 4);
-    for (int rb = r0; rb < r1; rb += STEP) {
-      if (next-- > 0) continue;
-      next = THREADS / 32 - 1;
-      join_rows<D, 8>(c, j, x, rb, r1);
+  for (long long i = blockIdx.x; i < (long long)n_long * rows; i += gridDim.x) {
+    const int row = (int)(i / n_long);
+    const JoinCut x = j.cuts[kPagedMaxShares - 1 - (i - (long long)row * n_long)];
+    if (row >= x.rows) continue;                              // all threads of the CTA alike
+    const JoinAcc a = join_parts<D, 8>(c, j, x, row, col, grp, GROUPS);
+    sh->o[tid] = a.o;
+    if (lane == 0) sh->ml[grp] = make_float2(a.M, a.L);
+    __syncthreads();
+    if (grp == 0) {
+      JoinAcc r{-INFINITY, 0.f, make_float4(0.f, 0.f, 0.f, 0.f)};
+      for (int g = 0; g < GROUPS; ++g) r.M = fmaxf(r.M, sh->ml[g].x);
+      const float b = r.M == -INFINITY ? 0.f : r.M;
+      for (int g = 0; g < GROUPS; ++g) {
+        const float f = fast_exp2(sh->ml[g].x - b);
+        const float4 v = sh->o[g * LANES + lane];
+        r.L += sh->ml[g].y * f;
+        r.o.x += v.x * f; r.o.y += v.y * f; r.o.z += v.z * f; r.o.w += v.w * f;
+      }
+      join_store(c, j, x, row, col, r);
     }
+    __syncthreads();
   }
 }
 

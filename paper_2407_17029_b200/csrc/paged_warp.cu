@@ -35,7 +35,7 @@ namespace {
 
 constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
 constexpr int PW_MAX_LEVELS = kPagedLevels;
-constexpr int PW_FINE = 8;       // key tiles of the shortest shares
+constexpr int PW_FINE = 11;       // key tiles of the shortest shares
 constexpr float PW_OUTGROWN = 1.099511627776e12f;   // 2^40
 constexpr float PW_LN2 = 0.69314718055994530942f;
 
@@ -57,8 +57,8 @@ struct PwParams {
   uint32_t div_page, div_group;
   uint32_t zero;             // 0, but not to the compiler
   long long wait_limit;
-  uint32_t* counters;        // [0]: shares taken; [1 + g]: share g begins inside an item, and is the first that does.  Zeroed
-  JoinCut* cuts;             // [shares] that item
+  uint32_t* counters;        // [0]: shares taken; [1 ... 3]: JoinCall::counts.  Zeroed
+  JoinCut* cuts;             // JoinCall::cuts
   float* part_o;             // [2 * shares][ROWS][D]
   float* part_ml;            // [2 * shares][ROWS][2]
 };
@@ -90,7 +90,7 @@ __device__ __forceinline__ int pw_head_units(const PwParams& p, const ReqView& r
   return u;
 }
 
-struct PwReq { int t0, n, kv, head_units; };     // a request as the scan saw it
+struct PwReq { int t0, n, kv; };     // a request as the scan saw it
 
 template <int ROWS, int KT>
 struct PwCursor {
@@ -103,33 +103,32 @@ struct PwCursor {
     tile = 0;
     if (++rt == nrt) {
       rt = 0;
-      if (++h == p.c.cache.kv_heads) {
-        h = 0;
-        do {
-          if (++b >= p.c.B) return;
-          r = known ? ReqView{known[b].t0, known[b].n, known[b].kv} : attn_request(p.c, b);
-        } while (!pw_mine(p, r));
-        nrt = pw_row_tiles<ROWS>(p, r);
-      }
+      do {
+        if (++b >= p.c.B) return;
+        r = known ? ReqView{known[b].t0, known[b].n, known[b].kv} : attn_request(p.c, b);
+      } while (!pw_mine(p, r));
+      nrt = pw_row_tiles<ROWS>(p, r);
     }
     k = pw_range<ROWS, KT>(p, r, rt);
   }
 };
 
-// The line of all key tiles and its shares (all arrays in shared memory).
+// The line of all key tiles of one key head (they are alike for all) and its shares: share g is part g / kv_heads of the line
+// for key head g % kv_heads.  All arrays in shared memory.
 template <int ROWS, int KT>
 struct PwLine {
   const PwReq* known;        // the requests, where there is one for each thread; else nullptr
   const int* units;          // [threads] inclusive sums of tiles over each thread's `per` requests
   const int *base, *each;    // [levels + 1], [levels]: first tile of a level, tiles of its shares
-  int per, per_level, levels, shares, total, extra;   // of the last level, the first `extra` shares have one tile more
+  int per, per_level, levels, total, extra;   // parts per level; of the last level, the first `extra` parts have one tile more
 
-  __device__ __forceinline__ int begin(int g) const {
-    if (g >= shares) return total;
-    const int k = g / per_level, i = g - k * per_level;
+  // part x of the line begins at; tile u belongs to part
+  __device__ __forceinline__ int begin(int x) const {
+    if (x >= per_level * levels) return total;
+    const int k = x / per_level, i = x - k * per_level;
     return base[k] + i * each[k] + (k + 1 == levels ? min(i, extra) : 0);
   }
-  __device__ __forceinline__ int share_of(int u) const {
+  __device__ __forceinline__ int part_of(int u) const {
     int k = 0;
     while (k + 1 < levels && u >= base[k + 1]) ++k;
     const int v = u - base[k], n = each[k];
@@ -142,22 +141,20 @@ struct PwLine {
     const AttnCall& c = p.c;
     int a = 0, e = PW_THREADS;
     while (a < e) { const int x = (a + e) >> 1; if (units[x] > u) e = x; else a = x + 1; }
-    int rest = u - (a ? units[a - 1] : 0), hu = 1;
+    int rest = u - (a ? units[a - 1] : 0);
     if (known) {
       at.b = a;
       at.r = ReqView{known[a].t0, known[a].n, known[a].kv};
-      hu = known[a].head_units;
     } else {
       for (at.b = a * per;; ++at.b) {
         at.r = attn_request(c, at.b);
         if (!pw_mine(p, at.r)) continue;
-        hu = pw_head_units<ROWS, KT>(p, at.r);
-        if (rest < (long long)hu * c.cache.kv_heads) break;
-        rest -= hu * c.cache.kv_heads;
+        const int hu = pw_head_units<ROWS, KT>(p, at.r);
+        if (rest < hu) break;
+        rest -= hu;
       }
     }
-    at.h = rest / hu;
-    int left = rest - at.h * hu;
+    int left = rest;
     at.nrt = pw_row_tiles<ROWS>(p, at.r);
     at.rt = 0;
     at.k = pw_range<ROWS, KT>(p, at.r, 0);
@@ -167,11 +164,11 @@ struct PwLine {
 };
 
 template <int D>
-__global__ void __launch_bounds__(256) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
-  __shared__ JoinShared list;
+__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
+  __shared__ JoinShared<D> sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
-  join_all<D, 256>(c, j, &list);
+  join_all<D>(c, j, &sh);
 }
 
 // status word and counters
@@ -206,6 +203,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 
   PwLine<ROWS, KT> line{};           // not CLUSTER: the shares
+  int shares = 0, first_taken = 0;   // all shares; those that the warps begin with
   int g = 0, u0, u1, g_next = 0;     // the share being computed, its tiles [u0, u1); lane 0: the share after it
   Cursor ld;
   if constexpr (CLUSTER) {
@@ -230,8 +228,8 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     for (int b = b_lo; b < b_hi; ++b) {
       const ReqView r = attn_request(c, b);
       const int hu = pw_mine(p, r) ? pw_head_units<ROWS, KT>(p, r) : 0;
-      mine += (long long)hu * c.cache.kv_heads;
-      if (per == 1) s_req[b] = PwReq{r.t0, r.n, r.kv, hu};
+      mine += hu;
+      if (per == 1) s_req[b] = PwReq{r.t0, r.n, r.kv};
     }
     const PwReq* known = per == 1 ? s_req : nullptr;
     long long incl = mine;
@@ -262,10 +260,10 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // Shares: level k hands every warp one share; the levels' parts of the line are 1/2, 1/4, ... with the last two equal, so
     // the shares that are taken late are short.  A share has more tiles than the ring has slots (then at most one share's
     // beginning is in the ring besides the current one).
-    const int per_level = min((int)gridDim.x * PW_WARPS, max(1, total / (PW_STAGES + 1)));
+    const int heads = c.cache.kv_heads;
+    const int per_level = min(max(1, (int)gridDim.x * PW_WARPS / heads), max(1, total / (PW_STAGES + 1)));
     int levels = 1;
     while (levels < PW_MAX_LEVELS && (total >> (levels + 1)) / per_level >= PW_FINE) ++levels;
-    const int shares = per_level * levels;
     if (tid == 0) {
       int at = 0;
       for (int k = 0; k < levels; ++k) {
@@ -279,14 +277,21 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     // of the last level, the first `extra` shares have one tile more
     const int extra = total - s_base[levels - 1] - s_each[levels - 1] * per_level;
     line.known = known; line.units = s_units; line.base = s_base; line.each = s_each; line.per = per;
-    line.per_level = per_level; line.levels = levels; line.shares = shares; line.total = total; line.extra = extra;
+    line.per_level = per_level; line.levels = levels; line.total = total; line.extra = extra;
+    first_taken = per_level * heads;
+    shares = first_taken * levels;
     g = (int)blockIdx.x * PW_WARPS + warp;
-    if (g >= per_level) return;
-    u0 = line.begin(g);
-    u1 = line.begin(g + 1);
+    if (g >= first_taken) {            // a warp too many for the first level
+      if (lane == 0) g = levels > 1 ? (int)atomicAdd(p.counters, 1u) + first_taken : shares;
+      g = __shfl_sync(0xffffffffu, g, 0);
+      if (g >= shares) return;
+    }
+    u0 = line.begin(g / heads);
+    u1 = line.begin(g / heads + 1);
     g_next = shares;
-    if (lane == 0 && levels > 1) g_next = (int)atomicAdd(p.counters, 1u) + per_level;
+    if (lane == 0 && levels > 1) g_next = (int)atomicAdd(p.counters, 1u) + first_taken;
     line.locate(p, ld, u0);
+    ld.h = g % heads;
   }
   const PwReq* known = line.known;
 
@@ -324,13 +329,14 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       if (--ld_left > 0) ld.next(p, known);
       else {
         ld_next_g = __shfl_sync(0xffffffffu, g_next, 0);
-        if (ld_next_g >= line.shares) return;                  // ld_left stays 0: nothing more to issue
-        const int b0 = line.begin(ld_next_g);
+        if (ld_next_g >= shares) return;                       // ld_left stays 0: nothing more to issue
+        const int x = ld_next_g / c.cache.kv_heads, b0 = line.begin(x);
         line.locate(p, ld, b0);
-        ld_left = line.begin(ld_next_g + 1) - b0;
+        ld.h = ld_next_g - x * c.cache.kv_heads;
+        ld_left = line.begin(x + 1) - b0;
         if (lane == 0) {
           s_next[warp] = ld;
-          g_next = (int)atomicAdd(p.counters, 1u) + line.per_level;
+          g_next = (int)atomicAdd(p.counters, 1u) + first_taken;
         }
         __syncwarp();
       }
@@ -365,13 +371,15 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         fresh = false;
         if (!CLUSTER && first_segment && cu.tile > 0 && lane == 0) {
           // this share begins inside an item: the first share that does tells the join kernel about it
-          const int item_first = u0 - cu.tile, first = g - 1;
-          if (line.begin(first) <= item_first) {
-            const int n = line.share_of(item_first + cu.k.tiles - 1) - first + 1;
+          const int item_first = u0 - cu.tile, part = g / c.cache.kv_heads - 1, first = g - c.cache.kv_heads;
+          if (line.begin(part) <= item_first) {
+            const int n = line.part_of(item_first + cu.k.tiles - 1) - part + 1;
             // its first part is the first share's last segment (slot 1) unless that share begins with the item; the others' first (slot 0)
-            p.cuts[g] = JoinCut{2 * first + (line.begin(first) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
+            const bool many = n > kJoinShort;
+            const int at = (int)atomicAdd(p.counters + (many ? 2 : 1), 1u);
+            atomicMax(p.counters + 3, (uint32_t)min(ROWS, cu.r.n * c.G - cu.rt * ROWS));
+            p.cuts[many ? kPagedMaxShares - 1 - at : at] = JoinCut{2 * first + (line.begin(part) == item_first ? 0 : 1), first, n, cu.r.t0, cu.rt * ROWS,
                               min(ROWS, cu.r.n * c.G - cu.rt * ROWS), cu.h, 0};
-            p.counters[1 + g] = 1;
           }
         }
         r0 = cu.rt * ROWS;
@@ -585,11 +593,11 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
       }
       if (++u < u1) { cu.next(p, known); continue; }
       // the next share: its tiles are on their way already
-      if (ld_next_g < 0 || ld_next_g >= line.shares) break;
+      if (ld_next_g < 0 || ld_next_g >= shares) break;
       g = ld_next_g;
       ld_next_g = -1;
-      u = u0 = line.begin(g);
-      u1 = line.begin(g + 1);
+      u = u0 = line.begin(g / c.cache.kv_heads);
+      u1 = line.begin(g / c.cache.kv_heads + 1);
       cu = s_next[warp];
       first_segment = fresh = true;
     }
@@ -662,6 +670,16 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 }
 
+// where the workspace holds what
+template <int D>
+void pw_workspace(PwParams* p, char* counters, char* scratch) {
+  constexpr int ROWS = PwShape<D>::ROWS;
+  p->counters = reinterpret_cast<uint32_t*>(counters);
+  p->part_ml = reinterpret_cast<float*>(scratch);
+  p->part_o = p->part_ml + (size_t)2 * kPagedMaxShares * ROWS * 2;
+  p->cuts = reinterpret_cast<JoinCut*>(p->part_o + (size_t)2 * kPagedMaxShares * ROWS * D);
+}
+
 template <int D>
 int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, cudaStream_t st) {
   using Sh = PwShape<D>;
@@ -675,13 +693,9 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
     attr_set[dev].store(true, std::memory_order_release);
   }
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  const int grid = std::min(sms, kPagedMaxSms);
-  p.counters = reinterpret_cast<uint32_t*>(counters);
-  p.part_ml = reinterpret_cast<float*>(scratch);
-  p.part_o = p.part_ml + (size_t)2 * kPagedMaxShares * Sh::ROWS * 2;
-  p.cuts = reinterpret_cast<JoinCut*>(p.part_o + (size_t)2 * kPagedMaxShares * Sh::ROWS * D);
+  pw_workspace<D>(&p, counters, scratch);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)grid);
+  cfg.gridDim = dim3((unsigned)std::min(sms, kPagedMaxSms));
   cfg.blockDim = dim3(PW_THREADS);
   cfg.dynamicSmemBytes = Sh::SMEM;
   cfg.stream = st;
@@ -691,10 +705,26 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
   cfg.attrs = attr; cfg.numAttrs = 1;
   QB_CUDA(cudaLaunchKernelEx(&cfg, kernel, tk, tv, p));
   count_launch();
-  JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, grid * PW_WARPS * PW_MAX_LEVELS, Sh::ROWS, p.div_group};
-  cfg.blockDim = dim3(256);
-  cfg.dynamicSmemBytes = 0;
-  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D>, p.c, j));
+  return QBLORA_OK;
+}
+
+template <int D>
+int pw_launch_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st) {
+  int dev = 0, sms = 0;
+  QB_CUDA(cudaGetDevice(&dev));
+  QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  PwParams p{};
+  pw_workspace<D>(&p, counters, scratch);
+  const JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, PwShape<D>::ROWS, fast_div_magic((uint32_t)c.G)};
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * sms));
+  cfg.blockDim = dim3(kJoinThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = 1;
+  QB_CUDA(cudaLaunchKernelEx(&cfg, paged_join_kernel<D>, c, j));
   count_launch();
   return QBLORA_OK;
 }
@@ -797,7 +827,7 @@ int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st) {
 }
 
 bool paged_warp_supported(const AttnCall& c) {
-  if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f)) return false;
+  if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f) || c.cache.kv_heads > kPagedMaxSms * kPagedWarps) return false;
   const int kt = c.D == 64 ? 32 : 16, pg = c.cache.page_size;
   // a tile is whole boxes of one page each; at most 32 boxes, one per lane
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);
@@ -810,6 +840,10 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* 
   if (rc) return rc;
   p.narrow_rows = narrow_rows;
   return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, st) : pw_launch<128>(p, tk, tv, counters, scratch, st);
+}
+
+int launch_paged_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st) {
+  return c.D == 64 ? pw_launch_join<64>(c, counters, scratch, st) : pw_launch_join<128>(c, counters, scratch, st);
 }
 
 int paged_cluster_size(const AttnCall& c, int* size) {

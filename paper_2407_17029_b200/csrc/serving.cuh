@@ -92,20 +92,22 @@ int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st);    // zeroe
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const AttnCall& c, char* counters, char* scratch, cudaStream_t st);
 
-// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i).
+// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i kv_heads).
 struct JoinCut { int slot0, first, n, t0, r0, rows, h, pad; };
+constexpr int kJoinThreads = 256, kJoinShort = 32;
 struct JoinCall {
-  const uint32_t* flags;      // [borders]: share g is the first that begins inside some item
-  const JoinCut* cuts;        // [borders]: that item
+  const uint32_t* counts;     // [3]: items of at most kJoinShort parts; of more; most rows of an item
+  const JoinCut* cuts;        // [kPagedMaxShares]: the first from the front, the others from the back
   const float *part_o, *part_ml;
-  int borders, rows_per_slot;
+  int rows_per_slot;
   uint32_t div_group;
 };
 
 // Few rows per key head, head sizes 64 and 128, pages that fit its tiles (paged_warp.cu): requests of at most `narrow_rows` rows
-// (new tokens * G), and a second kernel that joins their parts.
+// (new tokens * G), and a second kernel that joins their parts; a kernel launched between the two may not end before the first.
 bool paged_warp_supported(const AttnCall& c);
 int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
+int launch_paged_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st);
 
 // The same kernel for calls so small that every item has a cluster of CTAs to itself: one launch, no workspace but the status
 // word (zeroed on the stream).  paged_cluster_size gives the CTAs per cluster, 0 where the call is none of these.

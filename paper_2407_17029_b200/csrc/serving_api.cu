@@ -179,10 +179,16 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   char* counters = wide_counters + kWideCounterBytes;
   char* scratch = counters + kPagedCounterBytes;
   if (!paged_warp_supported(c)) return launch_paged_attention(c, counters, scratch, st);
-  if (!tc_attention_supported(c) || tokens * c.G <= kNarrowRows) return launch_paged_warp(c, 0x7fffffff, counters, scratch, st);
-  rc = launch_paged_warp(c, kNarrowRows, counters, scratch, st);
-  if (rc) return rc;
-  return launch_tc_attention(c, kNarrowRows, wide_counters, scratch + paged_attention_scratch_bytes(c.D), st);
+  const bool wide = tc_attention_supported(c) && tokens * c.G > kNarrowRows;     // there may be requests for the tcgen05 form
+  // Where the mean is above the border there are some for certain: their kernel comes before the join, so that it takes over SMs
+  // as the first kernel leaves them.  Otherwise it is probably empty and nothing should wait for it.
+  const bool wide_first = wide && tokens * c.G > (int64_t)kNarrowRows * n_requests;
+  char* wide_scratch = scratch + paged_attention_scratch_bytes(c.D);
+  rc = launch_paged_warp(c, wide ? kNarrowRows : 0x7fffffff, counters, scratch, st);
+  if (!rc && wide_first) rc = launch_tc_attention(c, kNarrowRows, wide_counters, wide_scratch, st);
+  if (!rc) rc = launch_paged_join(c, counters, scratch, st);
+  if (!rc && wide && !wide_first) rc = launch_tc_attention(c, kNarrowRows, wide_counters, wide_scratch, st);
+  return rc;
 }
 
 }  // extern "C"

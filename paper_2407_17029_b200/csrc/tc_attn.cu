@@ -243,6 +243,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ TaSeg s_seg[TA_SEGS];
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the join kernel, where it comes after this one
   const AttnCall& c = p.c;
   const int hkv = c.cache.kv_heads;
 
