@@ -4,17 +4,23 @@
 // Mathematics as in paged_attn.cu: a running softmax in base 2 over row tiles of 16 rows (tokens x query heads that share
 // a key head); partial triples (maximum, sum, weighted values) over disjoint keys join in any grouping.
 //
-// What bounds it: the cache's bytes, so each warp is made to need little else.  All key tiles of all items (request,
-// key head, row tile) are put in one line and cut into shares.  Every warp starts with one share and then takes the
-// next one that nobody has taken, the later ones shorter: SMs do not get equal parts of a saturated memory (with one equal share per warp the
-// slowest CTA of a 1 GB call ended 20 % after the median).  A warp streams its shares through a ring of its own -- lane i
-// issues box i of a tile as the ring's slot becomes free, across the borders of items and shares, and nothing waits for
-// another warp -- and does both products for the whole tile, so a tile costs a warp one wait, one maximum and one rescale.
-// In flight per SM: 8 warps x 3 slots x 8 KB.
+// What bounds it: the cache's bytes, so each warp is made to need little else.  The key tiles of all (request, row tile) pairs
+// are put in one line, alike for every key head, and the line is cut into parts; a share is one part for one key head, and
+// the heads of a part are neighbouring shares, so that warps which run at the same time read the same pages (with each head's
+// tiles in a row instead, 6 requests x 40 heads x 15k keys took 309 us, now 290).  Every warp starts with one share and then
+// takes the next one that nobody has taken, the later ones shorter: SMs do not get equal parts of a saturated memory (with
+// one equal share per warp the slowest CTA of a 1 GB call ended 20 % after the median).  A warp streams its shares through a
+// ring of its own -- lane i issues box i of a tile as the ring's slot becomes free, across the borders of items and shares,
+// and nothing waits for another warp -- and does both products for the whole tile with the maximum that there is; a new one is
+// looked for only where a sum shows that the scores have outgrown it.  In flight per SM: 8 warps x 3 slots x 8 KB.
 //
-// An item cut by a share's border leaves partial triples in the workspace, which a second kernel joins in share order:
-// results do not depend on timing.  (Joined by whichever warp came last, the joins of a call fell to the few warps that ended
-// last, one row after the other: 5 to 65 us at the end of a 45 to 180 us call.)
+// An item cut by a share's border leaves partial triples in the workspace, which a second kernel joins (paged_join.cuh); joined
+// by whichever warp came last, the joins of a call fell to the few warps that ended last, one row after the other: 5 to
+// 65 us at the end of a 45 to 180 us call.  Calls of very few rows have a form without either (CLUSTER): one cluster of CTAs
+// per item, joined through the cluster's shared memory.
+//
+// Measured, D 128: 64 requests of 30 to 8100 keys, 8 key heads of 4 query heads, 1.07 GB: 187 us = 5.7 TB/s, of which the join
+// kernel about 8; 6 requests of 15k keys, 40 heads, 1.87 GB: 290 us = 6.5 TB/s, the rate of a copy.
 //
 // Entries behind a request's keys: whole pages are asked for at a page number past the cache, which TMA fills with zeros;
 // the rest of the last page is masked (scores set to -infinity, V set to zero in shared memory).

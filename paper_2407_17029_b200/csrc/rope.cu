@@ -5,6 +5,8 @@
 // units of 2^-32 turns, exact at every position (a product in fp32 is off by a hundredth of a radian at position 10^5).
 //
 // What bounds it: HBM, every element read once and written once, in 16-byte words with several loads in flight per thread.
+// Measured: fp32, 8191 rows of 40 + 40 heads of 128, 671 MB: 119.5 us = 5.6 TB/s (a copy: 6.5); bf16, 4095 rows of
+// 52 + 52 + 52 heads into a cache, 327 MB: 57.8 us = 5.7 TB/s; one row: 2.7 us in a graph.
 #include "serving.cuh"
 
 namespace qb {
@@ -130,54 +132,54 @@ __global__ void __launch_bounds__(RW_THREADS, 4) rope_wide_kernel(const __grid_c
     e1 = e0 + 8 < c.cfg.D ? e0 + 8 : -1;
   }
   for (int tt = 0; tt < n; ++tt) {
-  const int64_t t = t0 + tt;
-  const int64_t entry = c.slots ? cache_entry(c.cache, __ldg(c.slots + t)) : -1;
-  const float *co = s_cos + tt * RW_MAX_PAIRS + chunk * 8, *si = s_sin + tt * RW_MAX_PAIRS + chunk * 8;
-  // UNROLL heads at a time: all their loads go out before the first store (a store may alias a load, so the compiler would not
-  // move one in front of the other)
-  constexpr int UNROLL = sizeof(TI) == 2 ? 2 : 1;
-  for (int hb = h0 + slot; hb < h1; hb += UNROLL * per) {
-    Eight<TI> ra[UNROLL], rb[UNROLL];
+    const int64_t t = t0 + tt;
+    const int64_t entry = c.slots ? cache_entry(c.cache, __ldg(c.slots + t)) : -1;
+    const float *co = s_cos + tt * RW_MAX_PAIRS + chunk * 8, *si = s_sin + tt * RW_MAX_PAIRS + chunk * 8;
+    // UNROLL heads at a time: all their loads go out before the first store (a store may alias a load, so the compiler would not
+    // move one in front of the other)
+    constexpr int UNROLL = sizeof(TI) == 2 ? 2 : 1;
+    for (int hb = h0 + slot; hb < h1; hb += UNROLL * per) {
+      Eight<TI> ra[UNROLL], rb[UNROLL];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      if (hb + u * per >= h1) break;
-      const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u * per);
-      ra[u].load(w.src + e0);
-      if (e1 >= 0) rb[u].load(w.src + e1);
-    }
+      for (int u = 0; u < UNROLL; ++u) {
+        if (hb + u * per >= h1) break;
+        const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u * per);
+        ra[u].load(w.src + e0);
+        if (e1 >= 0) rb[u].load(w.src + e1);
+      }
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-      if (hb + u * per >= h1) break;
-      const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u * per);
-      float a[8], b[8];
-      ra[u].get(a);
-      if (e1 >= 0) rb[u].get(b);
-      if (rot && w.rotate) {
-        if (LAYOUT == QBLORA_ROPE_HALF) {
+      for (int u = 0; u < UNROLL; ++u) {
+        if (hb + u * per >= h1) break;
+        const Place<TI, TO> w = place<TI, TO>(c, t, entry, hb + u * per);
+        float a[8], b[8];
+        ra[u].get(a);
+        if (e1 >= 0) rb[u].get(b);
+        if (rot && w.rotate) {
+          if (LAYOUT == QBLORA_ROPE_HALF) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float x = a[i], y = b[i];
-            a[i] = x * co[i] - y * si[i];
-            b[i] = y * co[i] + x * si[i];
-          }
-        } else {
+            for (int i = 0; i < 8; ++i) {
+              const float x = a[i], y = b[i];
+              a[i] = x * co[i] - y * si[i];
+              b[i] = y * co[i] + x * si[i];
+            }
+          } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float x = a[2 * i], y = a[2 * i + 1];
-            a[2 * i] = x * co[i] - y * si[i];
-            a[2 * i + 1] = y * co[i] + x * si[i];
-            x = b[2 * i]; y = b[2 * i + 1];
-            b[2 * i] = x * co[4 + i] - y * si[4 + i];
-            b[2 * i + 1] = y * co[4 + i] + x * si[4 + i];
+            for (int i = 0; i < 4; ++i) {
+              float x = a[2 * i], y = a[2 * i + 1];
+              a[2 * i] = x * co[i] - y * si[i];
+              a[2 * i + 1] = y * co[i] + x * si[i];
+              x = b[2 * i]; y = b[2 * i + 1];
+              b[2 * i] = x * co[4 + i] - y * si[4 + i];
+              b[2 * i + 1] = y * co[4 + i] + x * si[4 + i];
+            }
           }
         }
-      }
-      if (w.dst) {
-        st8(w.dst + e0, a);
-        if (e1 >= 0) st8(w.dst + e1, b);
+        if (w.dst) {
+          st8(w.dst + e0, a);
+          if (e1 >= 0) st8(w.dst + e1, b);
+        }
       }
     }
-  }
   }
 }
 
