@@ -54,7 +54,7 @@ template <int D>
 struct TaShape {
   static constexpr int STAGES = D == 64 ? 6 : 4;            // K and V tiles take turns; even, so V keeps to odd stages
   static constexpr int TILE_BYTES = TA_TILE * D * 2;        // one Q, K or V tile
-  static constexpr int BARS = 3 * STAGES + 12 + 2 * TA_SEGS + 2;   // full, empty, clean; six for each row tile; the segments' two; join
+  static constexpr int BARS = 3 * STAGES + 12 + 3 * TA_SEGS + 2;   // full, empty, clean; six for each row tile; the segments' three; join
   static constexpr int LIST_BYTES = kWideMaxRequests * 12;
   static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + LIST_BYTES + BARS * 8 + 64 + 1024;
 };
@@ -106,6 +106,7 @@ struct TaSeg {
   ReqView r;
   int b, h, tok0;          // request, key head, first token of the pair
   int lo;                  // first key of tile 0, a multiple of 128
+  int solo;                // there is only the first row tile: both softmax groups work for it, on every other key tile each
   int nt[2];               // key tiles that each row tile sees
   int full_lo[2], full_hi[2];   // tiles in this range have only keys that every row of the row tile sees
   int stop;                // keys from here on are seen by no row of the pair
@@ -199,6 +200,7 @@ struct TaWalk {
       s.slot0 = 2 * s.first + (begin(s.first) == first_unit ? 0 : 1);
     }
     s.tok0 = 2 * q * p.tokens_per_tile;
+    s.solo = s.tok0 + p.tokens_per_tile >= s.r.n;
     const int p0 = s.r.kv - s.r.n;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
@@ -230,6 +232,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 12 + (i & (TA_SEGS - 1))); };
   auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 12 + TA_SEGS + (i & (TA_SEGS - 1))); };
   auto joinbar = [&](int t) { return bars + 8u * (3 * STAGES + 12 + 2 * TA_SEGS + t); };
+  auto mail = [&](int i) { return bars + 8u * (3 * STAGES + 14 + 2 * TA_SEGS + (i & (TA_SEGS - 1))); };
   const uint32_t tmem_slot = bars + 8u * Sh::BARS;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(base_g + (tmem_slot - base));
   uint8_t* list = base_g + (2 + STAGES) * TB + Sh::BARS * 8 + 64;
@@ -246,6 +249,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ int s_odd[8];         // segment number + 1 where a value was taken out of V
   __shared__ int s_join[2];
   __shared__ TaSeg s_seg[TA_SEGS];
+  __shared__ float2 s_mail[TA_SEGS][TA_TILE];     // (m, l) of the second softmax group where both work for one row tile
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");     // the join kernel, where it comes after this one
@@ -383,7 +387,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1); mbar_init(joinbar(t), 4);
     }
     // readers of a segment: the MMA thread, the two cleaning warps, the eight softmax warps
-    for (int i = 0; i < TA_SEGS; ++i) { mbar_init(seg_full(i), 1); mbar_init(seg_empty(i), 11); }
+    for (int i = 0; i < TA_SEGS; ++i) { mbar_init(seg_full(i), 1); mbar_init(seg_empty(i), 11); mbar_init(mail(i), 4); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 9) {
@@ -498,7 +502,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(D >> 3) << 17) | ((uint32_t)(TA_TILE >> 4) << 24);
       const uint64_t dq = smem_desc(0, 16, 1024) | ((uQ & 0x3FFFFu) >> 4), dk = smem_desc(0, 16, 1024) | ((uKV & 0x3FFFFu) >> 4),
                      dv = smem_desc(0, TA_TILE * 128, 1024) | ((uKV & 0x3FFFFu) >> 4);
-      uint32_t ns0 = 0, ns1 = 0, nseg0 = 0, nseg1 = 0, clean_ph = 0, full_ph = 0;   // phases of the ring's stages, a bit each
+      uint32_t ns0 = 0, ns1 = 0, nseg0 = 0, nseg1 = 0, nq1 = 0, clean_ph = 0, full_ph = 0;   // phases of the ring's stages, a bit each
       int sk = 0;                                             // stage of the next K tile; V's is the one behind it
       bool ok = true;
       auto wait = [&](uint32_t bar, uint32_t parity) {
@@ -510,8 +514,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         full_ph ^= 1u << s;
         return w;
       };
-      auto scores = [&](int t, int stage) {
-        const uint64_t a = dq + (uint32_t)t * (TB >> 4), b = dk + (uint32_t)stage * (TB >> 4);
+      auto scores = [&](int t, int qt, int stage) {            // S of t, from row tile qt and the K of a stage
+        const uint64_t a = dq + (uint32_t)qt * (TB >> 4), b = dk + (uint32_t)stage * (TB >> 4);
         if (leader) {
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
@@ -526,18 +530,70 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         if (!wait(seg_full(n), (uint32_t)(n / TA_SEGS) & 1u)) break;
         const TaSeg& sg = s_seg[n & (TA_SEGS - 1)];
         const int valid = uni(sg.valid), ja = uni(sg.ja), e0 = uni(sg.end(0)), e1 = uni(sg.end(1)), fl0 = uni(sg.full_lo[0]),
-                  fl1 = uni(sg.full_lo[1]), fh0 = uni(sg.full_hi[0]), fh1 = uni(sg.full_hi[1]), e = max(e0, e1);
+                  fl1 = uni(sg.full_lo[1]), fh0 = uni(sg.full_hi[0]), fh1 = uni(sg.full_hi[1]), e = max(e0, e1), solo = uni(sg.solo);
         __syncwarp();
         if (lane == 0) mbar_arrive(seg_empty(n));
         if (!valid) break;
         if (ja >= e) continue;
+        if (solo) {
+          // one row tile: S and O of t = 0 and 1 are those of even and odd key tiles, so that the products of one go with the
+          // exponentials of the other here too.  K of tile j + 2 is asked for behind P V of tile j.
+          auto ring = [&](int s, int by) { return s + by >= STAGES ? s + by - STAGES : s + by; };
+          if (!wait_full(sk) || !wait(upair(Q_FULL, 0), nseg0 & 1u)) break;
+          tc_fence_after();
+          scores(0, 0, sk);
+          commit(uempty(sk));
+          if (ja + 1 < e) {
+            const int s1 = ring(sk, 2);
+            if (!wait_full(s1)) break;
+            tc_fence_after();
+            scores(1, 0, s1);
+            commit(uempty(s1));
+          }
+          if (ja + 2 >= e) commit(upair(Q_EMPTY, 0));
+          for (int j0 = ja; j0 < e && ok; j0 += 2) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+              const int j = j0 + t, sv = sk + 1, s2 = ring(sk, 4 % STAGES);
+              uint32_t &ns = t ? ns1 : ns0, &nseg = t ? nseg1 : nseg0;
+              if (j >= e || !ok || !wait_full(sv)) continue;
+              if (j < fl0 || j >= fh0) {
+                if (!wait(uclean(sv), (clean_ph >> sv) & 1u)) continue;
+                clean_ph ^= 1u << sv;
+              }
+              if (j0 == ja && !wait(upair(O_FREE, t), (nseg & 1u) ^ 1u)) continue;
+              if (!wait(upair(P_READY, t), ns & 1u)) continue;
+              ++ns;
+              tc_fence_after();
+              const uint64_t bv = dv + (uint32_t)sv * (TB >> 4);
+              if (leader) {
+#pragma unroll
+                for (int k = 0; k < TA_TILE / 16; ++k)
+                  tc_mma_ta(uT + 256 + t * D, uT + t * 128 + k * 8, bv + (uint32_t)k * 128u, idesc_o, (j0 > ja || k) ? 1u : 0u);
+              }
+              commit(uempty(sv));
+              if (j + 2 >= e) { commit(upair(O_FULL, t)); ++nseg; }
+              else {
+                if (!wait_full(s2)) continue;
+                tc_fence_after();
+                scores(t, 0, s2);
+                commit(uempty(s2));
+                if (j + 3 >= e) commit(upair(Q_EMPTY, 0));
+              }
+              sk = ring(sk, 2);
+            }
+          }
+          if (!ok) break;
+          continue;
+        }
         if (!wait_full(sk)) break;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
           const int et = t ? e1 : e0;
-          if (ja >= et || !wait(upair(Q_FULL, t), (t ? nseg1 : nseg0) & 1u)) continue;
+          if (ja >= et || !wait(upair(Q_FULL, t), (t ? nq1 : nseg0) & 1u)) continue;
+          if (t) ++nq1;
           tc_fence_after();
-          scores(t, sk);
+          scores(t, t, sk);
           if (ja + 1 >= et) commit(upair(Q_EMPTY, t));
         }
         if (!ok) break;
@@ -574,7 +630,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
                 tc_fence_after();
                 k_seen = true;
               }
-              scores(t, sk);
+              scores(t, t, sk);
               if (j + 2 >= et) commit(upair(Q_EMPTY, t));
             }
           }
@@ -632,7 +688,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tSr = tS + t * 128 + lanes, tOr = tO + t * D + lanes;
     const int tok_in = row / c.G, head_in = row - tok_in * c.G;
-    uint32_t ns = 0, nseg = 0, nj = 0;
+    uint32_t ns = 0, nseg = 0, nj = 0, nseg1 = 0;     // nseg1: nseg of the second group, for the first
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {     // one answer for the warp
       ok = __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, c.status, p.wait_limit));
@@ -643,13 +699,15 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!wait(seg_full(n), (uint32_t)(n / TA_SEGS) & 1u)) break;
       const TaSeg& sg = s_seg[n & (TA_SEGS - 1)];
       if (!sg.valid) break;
-      const int e = sg.end(t), p0 = sg.r.kv - sg.r.n;
-      const int tok = sg.tok0 + t * p.tokens_per_tile + tok_in;
+      const bool solo = sg.solo;
+      const int rt = solo ? 0 : t, e = sg.end(rt), step = solo ? 2 : 1, p0 = sg.r.kv - sg.r.n;
+      const int tok = sg.tok0 + rt * p.tokens_per_tile + tok_in;
       const bool real = tok_in < p.tokens_per_tile && tok < sg.r.n;
       const int hi = real ? attn_hi(c, sg.r.kv, p0 + tok) : sg.r.kv, lo = real ? attn_lo(c, p0 + tok) : 0;
-      const int full_lo = t ? sg.full_lo[1] : sg.full_lo[0], full_hi = t ? sg.full_hi[1] : sg.full_hi[0], ja = sg.ja, seg_lo = sg.lo;
+      const int full_lo = rt ? sg.full_lo[1] : sg.full_lo[0], full_hi = rt ? sg.full_hi[1] : sg.full_hi[0], seg_lo = sg.lo;
+      const int ja = sg.ja + (solo ? t : 0);
       float m = real ? -INFINITY : 0.f, l = 0.f;       // rows that are none need no maximum
-      for (int j = ja; j < e; ++j) {
+      for (int j = ja; j < e; j += step) {
         if (!wait(pairbar(S_FULL, t), ns & 1u)) break;
         ++ns;
         tc_fence_after();
@@ -725,11 +783,36 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       }
       if (!ok) break;
       const bool worked = ja < e;
+      if (t == 1) {
+        // a letter for every segment, so that the letters' barriers keep step with the segments
+        if (solo) s_mail[n & (TA_SEGS - 1)][row] = make_float2(m, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(mail(n));
+        if (solo) {                                  // the first group does the rest
+          nseg += worked;
+          if (lane == 0) mbar_arrive(seg_empty(n));
+          continue;
+        }
+      }
       if (worked) {
         if (!wait(pairbar(O_FULL, t), nseg & 1u)) break;
         ++nseg;
         tc_fence_after();
       }
+      const bool worked1 = t == 0 && (solo ? ja + 1 < e : sg.ja < sg.end(1)), both = solo && worked1;
+      float f0 = 1.f, f1 = 0.f;
+      if (both) {
+        // (the letter comes first: behind it O_FULL of t = 1 cannot be two turns behind)
+        if (!wait(mail(n), (uint32_t)(n / TA_SEGS) & 1u) || !wait(pairbar(O_FULL, 1), nseg1 & 1u)) break;
+        tc_fence_after();
+        const float2 ml = s_mail[n & (TA_SEGS - 1)][row];
+        const float M = fmaxf(m, ml.x), b = M == -INFINITY ? 0.f : M;
+        f0 = fast_exp2(m - b);
+        f1 = fast_exp2(ml.x - b);
+        l = l * f0 + ml.y * f1;
+        m = M;
+      }
+      nseg1 += worked1;
       const bool odd = s_odd[n & 7] == n + 1;
       const int head = sg.h * c.G + head_in;
       const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -738,10 +821,19 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         uint32_t o[32];
         if (worked) {
           tc_ld32(tOr + q * 32, o);
+          if (both) {
+            uint32_t o1[32];
+            tc_ld32(tOr + D + q * 32, o1);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f0 + __uint_as_float(o1[i]) * f1);
+          }
           if (q == D / 32 - 1) {
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(pairbar(O_FREE, t));
+            if (lane == 0) {
+              mbar_arrive(pairbar(O_FREE, t));
+              if (both) mbar_arrive(pairbar(O_FREE, 1));
+            }
           }
         } else {
 #pragma unroll
