@@ -1,13 +1,15 @@
 // Joining of partial attention results: items (row tiles of one request and key head) whose keys several warps of
-// paged_warp.cu have worked on.
+// paged_warp.cu or several CTAs of tc_attn.cu have worked on.
 //
 // A part is (m, l, o) per row: running maximum in base 2, sum of weights, sum of weighted values, over some of the item's keys.
 // With M = max m_i:  l = sum l_i 2^(m_i - M),  o = sum o_i 2^(m_i - M),  out = o / l,  lse = (M + log2 l) ln 2.
 // Parts are taken in a fixed order, so results do not depend on timing (the order of the lists of cut items does, and has no
-// influence on them).
+// influence on them).  Nothing here waits for another CTA: all parts are there when the kernel starts.
 //
 // What bounds it is latency: a row's parts are a few KB that lie in L2.  So a row of a short item is one warp's, with 16 parts in
-// flight, rows go evenly over all warps of the device, and only an item of more than kJoinShort parts takes a CTA per row.
+// flight, rows go evenly over all warps of the device, and only an item of more than kJoinShort parts takes a CTA per row.  Of
+// tc_attn.cu's row tiles a warp takes 32 rows x 32 columns, a lane per row, as its parts lie.  (Joined in tc_attn.cu by the CTA that
+// came last, two or three parts of 128 x 128 took 14 us at the end of a call; here about 3, all of them side by side.)
 #pragma once
 #include "mma_frag.cuh"
 #include "serving.cuh"
@@ -62,7 +64,111 @@ __device__ __forceinline__ void join_store(const AttnCall& c, const JoinCall& j,
 
 // All cut items.  Called by all threads of the CTA.
 template <int D>
-struct JoinShared { float2 ml[kJoinThreads / (D / 4)]; float4 o[kJoinThreads]; };
+struct JoinShared { float2 ml[kJoinThreads]; float4 o[8 * kJoinThreads]; };
+
+struct JoinWideAcc { float M, L; float4 o[8]; };
+// Parts a, a + step, ... below x.n of one row: 32 columns.
+template <int D>
+__device__ __forceinline__ void join_wide_parts(const JoinCall& j, const JoinCut& x, int row, int cg, int a, int step, JoinWideAcc& r) {
+  constexpr int PB = 2;
+  r.M = -INFINITY;
+  r.L = 0.f;
+#pragma unroll
+  for (int q = 0; q < 8; ++q) r.o[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = a; i0 < x.n; i0 += PB * step) {
+    float2 ml[PB];
+    float4 v[PB][8];
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      const int k = i0 + i * step;
+      ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+      for (int q = 0; q < 8; ++q) v[i][q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k < x.n) {
+        const long long slot = (k == 0 ? 2LL * x.slot0 : 4LL * (x.first + k)) + x.tile;
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(j.wide_ml) + slot * 128 + row);
+        const float4* o = reinterpret_cast<const float4*>(j.wide_o) + (slot * (D / 4) + cg * 8) * 128 + row;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[i][q] = __ldcg(o + q * 128);
+      }
+    }
+    float mn = r.M;
+#pragma unroll
+    for (int i = 0; i < PB; ++i) mn = fmaxf(mn, ml[i].x);
+    const float b = mn == -INFINITY ? 0.f : mn, f = fast_exp2(r.M - b);
+    r.M = mn;
+    r.L *= f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) { r.o[q].x *= f; r.o[q].y *= f; r.o[q].z *= f; r.o[q].w *= f; }
+#pragma unroll
+    for (int i = 0; i < PB; ++i) {
+      const float g = fast_exp2(ml[i].x - b);
+      r.L += ml[i].y * g;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) {
+        r.o[q].x += v[i][q].x * g; r.o[q].y += v[i][q].y * g; r.o[q].z += v[i][q].z * g; r.o[q].w += v[i][q].w * g;
+      }
+    }
+  }
+}
+__device__ __forceinline__ void join_wide_store(const AttnCall& c, const JoinCall& j, const JoinCut& x, int row, int cg, const JoinWideAcc& r) {
+  if (row >= x.rows) return;
+  const int tok = fast_div(row, c.G, j.div_group), head = x.h * c.G + row - tok * c.G;
+  const float inv = r.L == 0.f ? 0.f : 1.f / r.L;
+  uint4* out = reinterpret_cast<uint4*>(c.out + (long long)(x.t0 + tok) * c.o_ts + (long long)head * c.o_hs + cg * 32);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)
+    out[q] = make_uint4(ptx::pack_bf16x2(r.o[2 * q].x * inv, r.o[2 * q].y * inv), ptx::pack_bf16x2(r.o[2 * q].z * inv, r.o[2 * q].w * inv),
+                        ptx::pack_bf16x2(r.o[2 * q + 1].x * inv, r.o[2 * q + 1].y * inv), ptx::pack_bf16x2(r.o[2 * q + 1].z * inv, r.o[2 * q + 1].w * inv));
+  if (c.lse && cg == 0)
+    c.lse[(long long)(x.t0 + tok) * c.H + head] = r.L == 0.f ? -INFINITY : (r.M + log2f(r.L)) * 0.69314718055994530942f;
+}
+template <int D>
+__device__ __forceinline__ void join_wide_all(const AttnCall& c, const JoinCall& j, JoinShared<D>* sh) {
+  constexpr int COLS = D / 32, PIECES = 4 * COLS, WARPS = kJoinThreads / 32;     // a row tile's pieces of 32 rows x 32 columns
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int n_short = (int)__ldcg(j.wide_counts), n_long = (int)__ldcg(j.wide_counts + 1);
+  for (int i = warp * gridDim.x + blockIdx.x; i < n_short * PIECES; i += WARPS * gridDim.x) {
+    const int piece = i / n_short, cg = piece % COLS, r0 = piece / COLS * 32;
+    const JoinCut x = j.wide_cuts[i - piece * n_short];
+    if (r0 >= x.rows) continue;
+    JoinWideAcc r;
+    join_wide_parts<D>(j, x, r0 + lane, cg, 0, 1, r);
+    join_wide_store(c, j, x, r0 + lane, cg, r);
+  }
+  for (int i = blockIdx.x; i < n_long * PIECES; i += gridDim.x) {
+    const int piece = i / n_long, cg = piece % COLS, r0 = piece / COLS * 32;
+    const JoinCut x = j.wide_cuts[2 * kWideMaxShares - 1 - (i - piece * n_long)];
+    if (r0 >= x.rows) continue;                               // all threads of the CTA alike
+    JoinWideAcc r;
+    join_wide_parts<D>(j, x, r0 + lane, cg, warp, WARPS, r);
+    sh->ml[tid] = make_float2(r.M, r.L);
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sh->o[q * kJoinThreads + tid] = r.o[q];
+    __syncthreads();
+    if (warp == 0) {
+      r.M = -INFINITY;
+      for (int w = 0; w < WARPS; ++w) r.M = fmaxf(r.M, sh->ml[w * 32 + lane].x);
+      const float b = r.M == -INFINITY ? 0.f : r.M;
+      r.L = 0.f;
+#pragma unroll
+      for (int q = 0; q < 8; ++q) r.o[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < WARPS; ++w) {
+        const float2 ml = sh->ml[w * 32 + lane];
+        const float f = fast_exp2(ml.x - b);
+        r.L += ml.y * f;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          const float4 v = sh->o[q * kJoinThreads + w * 32 + lane];
+          r.o[q].x += v.x * f; r.o[q].y += v.y * f; r.o[q].z += v.z * f; r.o[q].w += v.w * f;
+        }
+      }
+      join_wide_store(c, j, x, r0 + lane, cg, r);
+    }
+    __syncthreads();
+  }
+}
+
 template <int D>
 __device__ __forceinline__ void join_all(const AttnCall& c, const JoinCall& j, JoinShared<D>* sh) {
   constexpr int LANES = D / 4, GROUPS = kJoinThreads / LANES;    // lanes of a row; rows that a CTA works on side by side

@@ -170,11 +170,12 @@ struct PwLine {
 };
 
 template <int D>
-__global__ void __launch_bounds__(kJoinThreads) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
+__global__ void __launch_bounds__(kJoinThreads, 2) paged_join_kernel(const __grid_constant__ AttnCall c, const __grid_constant__ JoinCall j) {
   __shared__ JoinShared<D> sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");       // the parts are written
   join_all<D>(c, j, &sh);
+  join_wide_all<D>(c, j, &sh);
 }
 
 // status word and counters
@@ -715,13 +716,14 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
 }
 
 template <int D>
-int pw_launch_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st) {
+int pw_launch_join(const AttnCall& c, char* counters, char* scratch, char* wide_counters, char* wide_scratch, cudaStream_t st) {
   int dev = 0, sms = 0;
   QB_CUDA(cudaGetDevice(&dev));
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   PwParams p{};
   pw_workspace<D>(&p, counters, scratch);
-  const JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, PwShape<D>::ROWS, fast_div_magic((uint32_t)c.G)};
+  JoinCall j{p.counters + 1, p.cuts, p.part_o, p.part_ml, PwShape<D>::ROWS, fast_div_magic((uint32_t)c.G)};
+  tc_attention_join(D, wide_counters, wide_scratch, &j);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(2 * sms));
   cfg.blockDim = dim3(kJoinThreads);
@@ -848,8 +850,9 @@ int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* 
   return c.D == 64 ? pw_launch<64>(p, tk, tv, counters, scratch, st) : pw_launch<128>(p, tk, tv, counters, scratch, st);
 }
 
-int launch_paged_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st) {
-  return c.D == 64 ? pw_launch_join<64>(c, counters, scratch, st) : pw_launch_join<128>(c, counters, scratch, st);
+int launch_paged_join(const AttnCall& c, char* counters, char* scratch, char* wide_counters, char* wide_scratch, cudaStream_t st) {
+  return c.D == 64 ? pw_launch_join<64>(c, counters, scratch, wide_counters, wide_scratch, st)
+                   : pw_launch_join<128>(c, counters, scratch, wide_counters, wide_scratch, st);
 }
 
 int paged_cluster_size(const AttnCall& c, int* size) {

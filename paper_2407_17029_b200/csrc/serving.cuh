@@ -83,7 +83,7 @@ constexpr int kPagedMaxSms = 160, kPagedMaxPerSm = 4;       // resident CTAs of 
 constexpr int kPagedWarps = 8, kPagedLevels = 4;            // warps per SM, and shares per warp, of paged_warp.cu
 constexpr int kPagedMaxShares = kPagedMaxSms * kPagedWarps * kPagedLevels;
 constexpr int kWideRounds = 3, kWideMaxShares = kPagedMaxSms * kWideRounds;     // of tc_attn.cu
-constexpr size_t kWideCounterBytes = (size_t)(1 + 2 * kWideMaxShares) * 4 / 256 * 256 + 256;
+constexpr size_t kWideCounterBytes = 256;
 constexpr size_t kPagedCounterBytes = (size_t)(1 + kPagedMaxShares) * 4 / 256 * 256 + 256;
 constexpr size_t kAttnResetBytes = kStatusBytes + kWideCounterBytes + kPagedCounterBytes;
 int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st);    // zeroes that many, a multiple of 16
@@ -92,22 +92,27 @@ int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st);    // zeroe
 size_t paged_attention_scratch_bytes(int head_dim);
 int launch_paged_attention(const AttnCall& c, char* counters, char* scratch, cudaStream_t st);
 
-// An item that shares cut: `n` parts, part 0 in slot `slot0`, part i in slot 2 (first + i kv_heads).
-struct JoinCut { int slot0, first, n, t0, r0, rows, h, pad; };
-constexpr int kJoinThreads = 256, kJoinShort = 32;
+// An item that shares cut: `n` parts.  Of paged_warp.cu: part 0 in slot `slot0`, part i in slot 2 (first + i kv_heads).  Of tc_attn.cu,
+// one row tile of it: part 0 in slot 2 slot0 + tile, part i in slot 4 (first + i) + tile.
+struct JoinCut { int slot0, first, n, t0, r0, rows, h, tile; };
+constexpr int kJoinThreads = 256, kJoinShort = 32, kJoinWideShort = 8;
 struct JoinCall {
   const uint32_t* counts;     // [3]: items of at most kJoinShort parts; of more; most rows of an item
   const JoinCut* cuts;        // [kPagedMaxShares]: the first from the front, the others from the back
   const float *part_o, *part_ml;
   int rows_per_slot;
   uint32_t div_group;
+  const uint32_t* wide_counts;   // [2]: row tiles of at most kJoinWideShort parts; of more
+  const JoinCut* wide_cuts;      // [2 kWideMaxShares] likewise
+  const float *wide_o, *wide_ml; // [slot][D / 4][128 rows][4], [slot][128][2]
 };
 
 // Few rows per key head, head sizes 64 and 128, pages that fit its tiles (paged_warp.cu): requests of at most `narrow_rows` rows
-// (new tokens * G), and a second kernel that joins their parts; a kernel launched between the two may not end before the first.
+// (new tokens * G).
 bool paged_warp_supported(const AttnCall& c);
 int launch_paged_warp(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
-int launch_paged_join(const AttnCall& c, char* counters, char* scratch, cudaStream_t st);
+// Joins the parts that it and tc_attn.cu have left.  A kernel launched between may not end before the kernels in front of it.
+int launch_paged_join(const AttnCall& c, char* counters, char* scratch, char* wide_counters, char* wide_scratch, cudaStream_t st);
 
 // The same kernel for calls so small that every item has a cluster of CTAs to itself: one launch, no workspace but the status
 // word (zeroed on the stream).  paged_cluster_size gives the CTAs per cluster, 0 where the call is none of these.
@@ -119,6 +124,7 @@ int launch_paged_cluster(const AttnCall& c, int size, cudaStream_t st);
 constexpr int kWideMaxRequests = 1024;
 bool tc_attention_supported(const AttnCall& c);
 size_t tc_attention_scratch_bytes(int head_dim);
+void tc_attention_join(int head_dim, char* counters, char* scratch, JoinCall* j);     // the wide part of it
 int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st);
 
 // TMA maps (CUtensorMap) of the cache's K and V.

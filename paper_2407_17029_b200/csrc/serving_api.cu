@@ -38,9 +38,9 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
 
 // Requests with more rows (new tokens x query heads per key head) than this go to the tcgen05 kernel.  A second row tile of
 // paged_warp.cu reads the keys and values again, while 128 rows cost the tcgen05 kernel what 17 do; but its set-up is longer and
-// the two kernels of a mixed call run one after the other.  Measured, 32 requests of 2000 to 4000 keys, 8 key heads: 12 rows
-// 98 us there; 24 rows 136 us there, 112 here; 40 rows 186 and 114; 64 rows 250 and 115.  16 requests of 12 to 28 rows: 50 us
-// with all of them there, 73 us with those above 16 rows here.
+// the two kernels of a call whose requests straddle the border run one after the other.  Measured, 32 requests of 2000 to 4000 keys,
+// 8 key heads: 12 rows 83 us there; 24 rows 131 us there, 102 here; 40 rows 104 here.  16 requests of 12 to 28 rows: 49 us
+// with all of them there, 61 us with those above 16 rows here.
 constexpr int kNarrowRows = 32;
 
 bool force_general() {
@@ -180,14 +180,10 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   char* scratch = counters + kPagedCounterBytes;
   if (!paged_warp_supported(c)) return launch_paged_attention(c, counters, scratch, st);
   const bool wide = tc_attention_supported(c) && tokens * c.G > kNarrowRows;     // there may be requests for the tcgen05 form
-  // Where the mean is above the border there are some for certain: their kernel comes before the join, so that it takes over SMs
-  // as the first kernel leaves them.  Otherwise it is probably empty and nothing should wait for it.
-  const bool wide_first = wide && tokens * c.G > (int64_t)kNarrowRows * n_requests;
   char* wide_scratch = scratch + paged_attention_scratch_bytes(c.D);
   rc = launch_paged_warp(c, wide ? kNarrowRows : 0x7fffffff, counters, scratch, st);
-  if (!rc && wide_first) rc = launch_tc_attention(c, kNarrowRows, wide_counters, wide_scratch, st);
-  if (!rc) rc = launch_paged_join(c, counters, scratch, st);
-  if (!rc && wide && !wide_first) rc = launch_tc_attention(c, kNarrowRows, wide_counters, wide_scratch, st);
+  if (!rc && wide) rc = launch_tc_attention(c, kNarrowRows, wide_counters, wide_scratch, st);
+  if (!rc) rc = launch_paged_join(c, counters, scratch, wide_counters, wide_scratch, st);
   return rc;
 }
 

@@ -17,8 +17,8 @@
 //
 // Work: items = (request, key head, pair of row tiles), each a run of key tiles.  Whole items are dealt out, longest first, to
 // whichever CTA is free, where that ends about as early as equal shares would (the rule stands at its place below);
-// else the line of all key tiles is cut into equal shares, up to three per CTA, and the CTA that finishes a cut item last
-// joins its parts in share order.
+// else the line of all key tiles is cut into equal shares, up to three per CTA, and a kernel behind this one joins the parts of cut
+// items (paged_join.cuh).
 //
 // What bounds it: S of both row tiles reads 8 KB of shared memory per 64 tensor cycles, the full rate (128 x 128 x 128 measured
 // alone: Q K^T 531 cycles, P V 522 of 512), and the exponentials take as many cycles as the products (16 per cycle and SM),
@@ -54,7 +54,7 @@ template <int D>
 struct TaShape {
   static constexpr int STAGES = D == 64 ? 6 : 4;            // K and V tiles take turns; even, so V keeps to odd stages
   static constexpr int TILE_BYTES = TA_TILE * D * 2;        // one Q, K or V tile
-  static constexpr int BARS = 3 * STAGES + 12 + 3 * TA_SEGS + 2;   // full, empty, clean; six for each row tile; the segments' three; join
+  static constexpr int BARS = 3 * STAGES + 12 + 3 * TA_SEGS;       // full, empty, clean; six for each row tile; the segments' three
   static constexpr int LIST_BYTES = kWideMaxRequests * 12;
   static constexpr int SMEM = (2 + STAGES) * TILE_BYTES + LIST_BYTES + BARS * 8 + 64 + 1024;
 };
@@ -67,7 +67,8 @@ struct TaParams {
   int box_keys;           // keys per TMA box: min(page_size, 128)
   long long wait_limit;
   uint32_t div_page;
-  uint32_t* counters;     // zeroed; [0]: items dealt out, [1 + 2 * share + row tile]: parts of the item that the share cuts first
+  uint32_t* counters;     // zeroed; [0]: items dealt out, [1], [2]: JoinCall::wide_counts
+  JoinCut* cuts;          // JoinCall::wide_cuts
   float* part_o;          // [2 * shares][2 row tiles][D / 4][128 rows][4]
   float* part_ml;         // [2 * shares][2][128][2]
 };
@@ -231,8 +232,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   enum { S_FULL = 0, P_READY = 1, O_FULL = 2, O_FREE = 3, Q_FULL = 4, Q_EMPTY = 5 };
   auto seg_full = [&](int i) { return bars + 8u * (3 * STAGES + 12 + (i & (TA_SEGS - 1))); };
   auto seg_empty = [&](int i) { return bars + 8u * (3 * STAGES + 12 + TA_SEGS + (i & (TA_SEGS - 1))); };
-  auto joinbar = [&](int t) { return bars + 8u * (3 * STAGES + 12 + 2 * TA_SEGS + t); };
-  auto mail = [&](int i) { return bars + 8u * (3 * STAGES + 14 + 2 * TA_SEGS + (i & (TA_SEGS - 1))); };
+  auto mail = [&](int i) { return bars + 8u * (3 * STAGES + 12 + 2 * TA_SEGS + (i & (TA_SEGS - 1))); };
   const uint32_t tmem_slot = bars + 8u * Sh::BARS;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(base_g + (tmem_slot - base));
   uint8_t* list = base_g + (2 + STAGES) * TB + Sh::BARS * 8 + 64;
@@ -247,7 +247,6 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
   __shared__ int s_warp_n[TA_THREADS / 32], s_warp_i[TA_THREADS / 32];
   __shared__ long long s_warp_u[TA_THREADS / 32];
   __shared__ int s_odd[8];         // segment number + 1 where a value was taken out of V
-  __shared__ int s_join[2];
   __shared__ TaSeg s_seg[TA_SEGS];
   __shared__ float2 s_mail[TA_SEGS][TA_TILE];     // (m, l) of the second softmax group where both work for one row tile
 
@@ -384,7 +383,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     for (int t = 0; t < 2; ++t) {
       mbar_init(pairbar(S_FULL, t), 1); mbar_init(pairbar(P_READY, t), 4);
       mbar_init(pairbar(O_FULL, t), 1); mbar_init(pairbar(O_FREE, t), 4);
-      mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1); mbar_init(joinbar(t), 4);
+      mbar_init(pairbar(Q_FULL, t), 1); mbar_init(pairbar(Q_EMPTY, t), 1);
     }
     // readers of a segment: the MMA thread, the two cleaning warps, the eight softmax warps
     for (int i = 0; i < TA_SEGS; ++i) { mbar_init(seg_full(i), 1); mbar_init(seg_empty(i), 11); mbar_init(mail(i), 4); }
@@ -688,7 +687,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t tSr = tS + t * 128 + lanes, tOr = tO + t * D + lanes;
     const int tok_in = row / c.G, head_in = row - tok_in * c.G;
-    uint32_t ns = 0, nseg = 0, nj = 0, nseg1 = 0;     // nseg1: nseg of the second group, for the first
+    uint32_t ns = 0, nseg = 0, nseg1 = 0;     // nseg1: nseg of the second group, for the first
     bool ok = true;
     auto wait = [&](uint32_t bar, uint32_t parity) {     // one answer for the warp
       ok = __all_sync(0xffffffffu, ok && mbar_wait(bar, parity, c.status, p.wait_limit));
@@ -884,56 +883,13 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
         continue;
       }
       reinterpret_cast<float2*>(p.part_ml)[(sg.slot * 2 + t) * 128 + row] = make_float2(m, l);
-      __threadfence();
-      // the row tile's warps: parts written, then the news of who came last (bounded waits, like every other)
-      __syncwarp();
-      if (lane == 0) mbar_arrive(joinbar(t));
-      if (!wait(joinbar(t), nj++ & 1u)) break;
-      if (row == 0) s_join[t] = atomicAdd(p.counters + 1 + 2 * sg.first + t, 1u) == (uint32_t)(sg.last - sg.first);
-      __syncwarp();
-      if (lane == 0) mbar_arrive(joinbar(t));
-      if (!wait(joinbar(t), nj++ & 1u)) break;
-      if (s_join[t]) {
-        __threadfence();
-        const int first = sg.first, last = sg.last;
-        auto part = [&](int x) { return (x == first ? sg.slot0 : 2 * x) * 2 + t; };
-        const float2* ml = reinterpret_cast<const float2*>(p.part_ml) + row;
-        float M = -INFINITY, L = 0.f;
-        for (int x = first; x <= last; x += 4) {               // four parts' statistics in flight
-          float2 v[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) v[i] = x + i <= last ? __ldcg(ml + part(x + i) * 128) : make_float2(-INFINITY, 0.f);
-          const float mn = fmaxf(fmaxf(fmaxf(v[0].x, v[1].x), fmaxf(v[2].x, v[3].x)), M), mb = mn == -INFINITY ? 0.f : mn;
-          L *= fast_exp2(M - mb);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) L += v[i].y * fast_exp2(v[i].x - mb);
-          M = mn;
-        }
-        const float mb = M == -INFINITY ? 0.f : M, iv = L == 0.f ? 0.f : 1.f / L;
-#pragma unroll 1
-        for (int q = 0; q < D / 64; ++q) {                     // 64 columns at a time: 16 loads in flight
-          float4 a[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-          for (int x = first; x <= last; ++x) {
-            const float4* src = reinterpret_cast<const float4*>(p.part_o + (long long)part(x) * D * 128) + q * 16 * 128 + row;
-            float4 v[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[i] = __ldcg(src + i * 128);
-            const float g = fast_exp2(__ldcg(ml + part(x) * 128).x - mb);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) { a[i].x += v[i].x * g; a[i].y += v[i].y * g; a[i].z += v[i].z * g; a[i].w += v[i].w * g; }
-          }
-          if (real) {
-            uint4* out = reinterpret_cast<uint4*>(c.out + (long long)(sg.r.t0 + tok) * c.o_ts + (long long)head * c.o_hs + q * 64);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              out[i] = make_uint4(pack_bf16x2(a[2 * i].x * iv, a[2 * i].y * iv), pack_bf16x2(a[2 * i].z * iv, a[2 * i].w * iv),
-                                  pack_bf16x2(a[2 * i + 1].x * iv, a[2 * i + 1].y * iv), pack_bf16x2(a[2 * i + 1].z * iv, a[2 * i + 1].w * iv));
-          }
-        }
-        if (real && c.lse) c.lse[(long long)(sg.r.t0 + tok) * c.H + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * TA_LN2;
+      // the second of the shares that cut the item tells the join kernel about this row tile of it
+      if (row == 0 && (sg.slot >> 1) == sg.first + 1 && real) {
+        const int parts = sg.last - sg.first + 1;
+        const bool many = parts > kJoinWideShort;
+        const int at = (int)atomicAdd(p.counters + (many ? 2 : 1), 1u);
+        p.cuts[many ? 2 * kWideMaxShares - 1 - at : at] =
+            JoinCut{sg.slot0, sg.first, parts, sg.r.t0 + tok, 0, min(p.tokens_per_tile, sg.r.n - tok) * c.G, sg.h, t};
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(seg_empty(n));
@@ -967,6 +923,7 @@ int ta_launch(const TaParams& p0, char* counters, char* scratch, cudaStream_t st
   p.counters = reinterpret_cast<uint32_t*>(counters);
   p.part_ml = reinterpret_cast<float*>(scratch);
   p.part_o = p.part_ml + (size_t)2 * kWideMaxShares * 2 * 128 * 2;
+  p.cuts = reinterpret_cast<JoinCut*>(p.part_o + (size_t)2 * kWideMaxShares * 2 * 128 * D);
 
   // a dimension of one entry may come with any stride: give the map one it accepts
   auto pitch = [](int64_t n, int64_t stride, int64_t other) { return (uint64_t)(n > 1 ? stride : other) * 2; };
@@ -1019,7 +976,14 @@ bool tc_attention_supported(const AttnCall& c) {
 
 size_t tc_attention_scratch_bytes(int head_dim) {
   if (head_dim != 64 && head_dim != 128) return 0;
-  return (size_t)2 * kWideMaxShares * 2 * 128 * (head_dim + 2) * 4;
+  return (size_t)2 * kWideMaxShares * 2 * 128 * (head_dim + 2) * 4 + (size_t)2 * kWideMaxShares * sizeof(JoinCut);
+}
+
+void tc_attention_join(int head_dim, char* counters, char* scratch, JoinCall* j) {
+  j->wide_counts = reinterpret_cast<uint32_t*>(counters) + 1;
+  j->wide_ml = reinterpret_cast<float*>(scratch);
+  j->wide_o = j->wide_ml + (size_t)2 * kWideMaxShares * 2 * 128 * 2;
+  j->wide_cuts = reinterpret_cast<const JoinCut*>(j->wide_o + (size_t)2 * kWideMaxShares * 2 * 128 * head_dim);
 }
 
 int launch_tc_attention(const AttnCall& c, int narrow_rows, char* counters, char* scratch, cudaStream_t st) {
