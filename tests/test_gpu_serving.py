@@ -338,6 +338,19 @@ def test_attention_long_chunks(H, Hkv, D, new, kv):
         _attend(new, kv, H, Hkv, D, page=128, causal=False, seed=3)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("new,kv,H,Hkv", [
+    ([40], [20001], 1, 1),            # one row tile cut into as many parts as there are SMs
+    ([200], [9000], 1, 1),            # two row tiles
+    ([34, 1, 33], [129, 40, 3000], 2, 2), ([127], [128], 1, 1), ([128, 129], [256, 385], 1, 1),   # one key tile to each, or few
+    ([11, 5, 40], [700, 2100, 900], 12, 3), ([300, 2], [4000, 3], 6, 2),
+])
+def test_attention_items_cut_many_times(new, kv, H, Hkv, D):
+    _attend(new, kv, H, Hkv, D)
+    _attend(new, kv, H, Hkv, D, page=32, causal=False, seed=2)
+    _attend(new, kv, H, Hkv, D, page=128, window=500, q_view=True, seed=3)
+
+
 @pytest.mark.parametrize("order", ["nhd", "hnd"])
 @pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 1), (True, 20), (True, 130), (False, 50), (True, 4000)])
 def test_attention_masks_and_orders(order, causal, window):
