@@ -221,7 +221,10 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     ld.rt = item / c.cache.kv_heads / c.B;       // last, so that the row tiles that requests do not have come after all others
     ld.r = attn_request(c, ld.b);
     ld.nrt = pw_row_tiles<ROWS>(p, ld.r);
-    if (ld.rt >= ld.nrt) return;     // the whole cluster
+    if (ld.rt >= ld.nrt) {           // the whole cluster; but no grid ends before the one in front of it
+      asm volatile("griddepcontrol.wait;" ::: "memory");
+      return;
+    }
     ld.k = pw_range<ROWS, KT>(p, ld.r, ld.rt);
     const int parts = cs * PW_WARPS, me = (int)cluster_ctarank() * PW_WARPS + warp;
     u0 = (int)((long long)ld.k.tiles * me / parts);

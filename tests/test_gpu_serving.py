@@ -543,6 +543,41 @@ def test_attention_page_number_out_of_range_is_reported():
         assert qb.device_status(ws) == qb.ERR_INVALID_ARG
 
 
+@pytest.mark.parametrize("new", [[1], [0, 0], [1, 40]])
+def test_attention_status_is_cleared_by_every_replay(new):
+    qb = _qb()
+    g = _gen(31)
+    kv = [400] * len(new)
+    ck, cv, table, ks, vs = make_cache(g, kv, 16, 2, 128, fill=0.0)
+    q = torch.randn(max(sum(new), 1), 8, 128, generator=g, device=DEV).to(torch.bfloat16)
+    cache = qb.KVCache(ck, cv)
+    ws = qb.alloc_attention_workspace(cache, q)
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device=DEV)
+    lens, cu = torch.tensor(kv, dtype=torch.int32, device=DEV), offsets(new)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        qb.paged_attention(q, cache, table, cu, lens, out=out, lse=lse, ws=ws)
+        st.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            qb.paged_attention(q, cache, table, cu, lens, out=out, lse=lse, ws=ws)
+        good = table[-1, 7].clone()
+        for page, want in ((1 << 30, qb.ERR_INVALID_ARG), (good, qb.OK), (-1, qb.ERR_INVALID_ARG), (good, qb.OK)):
+            table[-1, 7] = page
+            out.fill_(5.0)
+            ws[:4].fill_(0xFF)
+            graph.replay()
+            st.synchronize()
+            assert qb.device_status(ws) == (want if sum(new) else qb.OK)
+        if sum(new):
+            ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, 128 ** -0.5)
+            within(out, ref, bound, "out")
+            within(lse, rl, lb, "lse")
+        else:
+            assert bool((out == 5.0).all())
+
+
 @pytest.mark.parametrize("new", [1, 130])
 def test_attention_offsets_past_32_bits(new):
     # a cache of 2.2e9 elements each for k and v: the request's pages lie at its end
