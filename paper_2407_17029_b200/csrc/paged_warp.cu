@@ -680,6 +680,13 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
   }
 }
 
+// CTAs of the line: one per SM; 0 without a device
+int pw_ctas() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+  return std::min(sms, kPagedMaxSms);
+}
+
 // where the workspace holds what
 template <int D>
 void pw_workspace(PwParams* p, char* counters, char* scratch) {
@@ -694,7 +701,7 @@ template <int D>
 int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* counters, char* scratch, cudaStream_t st) {
   using Sh = PwShape<D>;
   static std::atomic<bool> attr_set[64];
-  int dev = 0, sms = 0;
+  int dev = 0;
   QB_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
   auto kernel = paged_warp_kernel<D, false>;
@@ -702,10 +709,9 @@ int pw_launch(PwParams p, const CUtensorMap& tk, const CUtensorMap& tv, char* co
     QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Sh::SMEM));
     attr_set[dev].store(true, std::memory_order_release);
   }
-  QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   pw_workspace<D>(&p, counters, scratch);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)std::min(sms, kPagedMaxSms));
+  cfg.gridDim = dim3((unsigned)pw_ctas());
   cfg.blockDim = dim3(PW_THREADS);
   cfg.dynamicSmemBytes = Sh::SMEM;
   cfg.stream = st;
@@ -838,7 +844,10 @@ int launch_attention_reset(void* ws, size_t bytes, cudaStream_t st) {
 }
 
 bool paged_warp_supported(const AttnCall& c) {
-  if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f) || c.cache.kv_heads > kPagedMaxSms * kPagedWarps) return false;
+  if ((c.D != 64 && c.D != 128) || !(c.scale > 0.f)) return false;
+  // every warp of the line begins with one share of the first level, which has at least one share for each key head: with more
+  // key heads than warps nobody would take the last ones
+  if (c.cache.kv_heads > pw_ctas() * kPagedWarps) return false;
   const int kt = c.D == 64 ? 32 : 16, pg = c.cache.page_size;
   // a tile is whole boxes of one page each; at most 32 boxes, one per lane
   return pg % 8 == 0 && (pg <= kt ? kt % pg == 0 : pg % kt == 0);

@@ -679,3 +679,11 @@ def test_a_merged_layer_decodes_as_it_would_over_the_whole_sequence():
         S = torch.einsum("nhd,jhd->hnj", rq.abs(), rk.repeat_interleave(H // Hkv, 1).abs()).amax(-1).T * D ** -0.5
         A = v.double().abs().amax()                                            # no weighted mean of |v| exceeds the largest |v|
         within(torch.cat(outs[b]), ref, bound + (2.0 ** -7 * S)[..., None] * 2 * A, f"request {b}")
+
+
+@pytest.mark.parametrize("D,new,kv", [(64, [3, 1], [40, 7]), (128, [2], [33]), (64, [5], [900])])
+def test_attention_more_key_heads_than_warps(D, new, kv):
+    # eight warps per SM stream the cache; one, a few and many key heads more than that, and as many
+    warps = 8 * torch.cuda.get_device_properties(0).multi_processor_count
+    for Hkv in (warps, warps + 1, warps + 96):
+        _attend(new, kv, Hkv, Hkv, D)
