@@ -449,6 +449,7 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
  * Lengths are read on the device only, so one captured graph serves every step of the same shape.  Lengths and table
  * entries out of range are clamped and never lead outside the cache; a page number out of range sets the status word to
  * QBLORA_ERR_INVALID_ARG (that request's results are then undefined).
+ * Table entries of pages that no row of the request sees (wholly in front of its window, or behind its keys) are not read.
  * ws: qblora_attention_workspace_bytes(...) bytes.
  */
 size_t qblora_attention_workspace_bytes(const qblora_kv_cache* cache, int32_t q_heads, int64_t tokens);

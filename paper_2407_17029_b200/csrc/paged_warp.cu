@@ -69,7 +69,9 @@ struct PwParams {
   float* part_ml;            // [2 * shares][ROWS][2]
 };
 
-struct PwRange { int lo, hi, tiles, all_lo, all_hi; };
+// Keys [first, hi) that some row of a row tile sees, in `tiles` tiles from lo on, which is first rounded down; [all_lo, all_hi): those
+// that every row sees.
+struct PwRange { int lo, hi, tiles, first, all_lo, all_hi; };
 template <int ROWS, int KT>
 __device__ __forceinline__ PwRange pw_range(const PwParams& p, const ReqView& r, int rt) {
   const AttnCall& c = p.c;
@@ -77,7 +79,8 @@ __device__ __forceinline__ PwRange pw_range(const PwParams& p, const ReqView& r,
   const int p0 = r.kv - r.n;
   PwRange k;
   k.hi = attn_hi(c, r.kv, p0 + i1);
-  k.lo = min(attn_lo(c, p0 + i0), k.hi) & ~(KT - 1);
+  k.first = min(attn_lo(c, p0 + i0), k.hi);
+  k.lo = k.first & ~(KT - 1);
   k.tiles = max(1, (k.hi - k.lo + KT - 1) / KT);
   k.all_lo = attn_lo(c, p0 + i1);
   k.all_hi = attn_hi(c, r.kv, p0 + i0);
@@ -317,19 +320,22 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
     const int n_boxes = 2 * HALVES * runs;            // at most 32
     const int my_run = lane / (2 * HALVES), my_half = (lane >> 1) % HALVES, my_kv = lane & 1;
     const uint32_t my_dst = (uint32_t)(my_kv * Sh::KV_BYTES + my_half * (KT * 128) + my_run * p.box_keys * 128);
-    auto lookup = [&](int& entry) -> int {            // page of this lane's box; past the cache: zeros
+    // page of this lane's box.  A box of keys that no row sees is filled with zeros (entry -1) and its page not looked up: the page
+    // behind the request's keys is not there yet, the one in front of a window may have been given back.
+    auto lookup = [&](int& entry) -> int {
       const int key = ld.k.lo + ld.tile * KT + my_run * p.box_keys;
-      entry = 0;
-      if (lane >= n_boxes || key >= ld.k.hi) return c.cache.n_pages;
+      entry = -1;
+      if (lane >= n_boxes || key >= ld.k.hi || key + p.box_keys <= ld.k.first) return 0;
       const int j = fast_div(key, c.cache.page_size, p.div_page);
       entry = key - j * c.cache.page_size;
       return __ldg(c.table + (long long)ld.b * c.width + j);
     };
     uint32_t issued = 0, done = 0;
-    int entry = 0, page = ld_left > 0 ? lookup(entry) : c.cache.n_pages, st_ld = 0;
+    int entry = -1, page = ld_left > 0 ? lookup(entry) : 0, st_ld = 0;
     auto issue = [&](uint32_t dep) {
-      if (page < 0 || page > c.cache.n_pages) { odd_pages = 1; page = c.cache.n_pages; }
-      if (lane < n_boxes && page == c.cache.n_pages && ld.k.lo + ld.tile * KT + my_run * p.box_keys < ld.k.hi) odd_pages = 1;
+      const bool none = entry < 0, odd_page = !none && (page < 0 || page >= c.cache.n_pages);
+      odd_pages |= odd_page;
+      if (none || odd_page) { page = c.cache.n_pages; entry = 0; }     // past the cache: zeros
       if (lane == 0) mbar_arrive_expect_tx(full + 8 * st_ld, Sh::STAGE);
       __syncwarp();
       if (lane < n_boxes)

@@ -107,6 +107,7 @@ struct TaSeg {
   ReqView r;
   int b, h, tok0;          // request, key head, first token of the pair
   int lo;                  // first key of tile 0, a multiple of 128
+  int seen;                // first key that some row of the pair sees
   int solo;                // there is only the first row tile: both softmax groups work for it, on every other key tile each
   int nt[2];               // key tiles that each row tile sees
   int full_lo[2], full_hi[2];   // tiles in this range have only keys that every row of the row tile sees
@@ -209,6 +210,7 @@ struct TaWalk {
       s.full_hi[t] = max(0, attn_hi(p.c, s.r.kv, p0 + i0) - s.lo) / TA_TILE;
       s.full_lo[t] = (max(0, attn_lo(p.c, p0 + i1) - s.lo) + TA_TILE - 1) / TA_TILE;
     }
+    s.seen = attn_lo(p.c, p0 + s.tok0);
     s.stop = attn_hi(p.c, s.r.kv, p0 + min(s.r.n, s.tok0 + 2 * p.tokens_per_tile) - 1);
     return true;
   }
@@ -432,10 +434,11 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
       if (!more) break;
       const int e = sg.last_tile();
       for (int j = sg.ja; j < e && ok; ++j) {
-        // lane i < boxes: page of the tile's i-th box; one past the cache (a box of zeros) behind the request's keys
+        // lane i < boxes: page of the tile's i-th box.  A box of keys that no row of the pair sees is filled with zeros (one page past
+        // the cache) and its page not looked up: those in front of a window may have been given back
         int page = c.cache.n_pages, entry = 0;
         const int key = sg.lo + j * TA_TILE + lane * p.box_keys;
-        if (lane < boxes && key < sg.r.kv) {
+        if (lane < boxes && key < sg.stop && key + p.box_keys > sg.seen) {
           const int x = fast_div(key, c.cache.page_size, p.div_page);
           page = __ldg(c.table + (long long)sg.b * c.width + x);
           entry = key - x * c.cache.page_size;

@@ -687,3 +687,34 @@ def test_attention_more_key_heads_than_warps(D, new, kv):
     warps = 8 * torch.cuda.get_device_properties(0).multi_processor_count
     for Hkv in (warps, warps + 1, warps + 96):
         _attend(new, kv, Hkv, Hkv, D)
+
+
+@pytest.mark.parametrize("general", [False, True])
+@pytest.mark.parametrize("page,D", [(8, 64), (8, 128), (16, 64), (16, 128), (64, 128), (24, 128), (5, 40)])
+@pytest.mark.parametrize("new,kv,window", [
+    ([1], [700], 30), ([2, 1], [513, 90], 9), ([1] * 40, [37 * i + 1 for i in range(40)], 100), ([40, 3], [900, 333], 77),
+    ([200, 1], [1500, 640], 1), ([150], [150], 20), ([300], [2000], 500),
+])
+def test_attention_pages_in_front_of_the_window_may_be_gone(monkeypatch, general, page, D, new, kv, window):
+    # a server gives pages back that lie wholly in front of the window: their entries hold no page number any more
+    qb = _qb()
+    if general:
+        monkeypatch.setenv("QBLORA_FORCE_GENERAL", "1")
+    H, Hkv = 6, 2
+    g = _gen(41)
+    ck, cv, table, ks, vs = make_cache(g, kv, page, Hkv, D)
+    q = torch.randn(sum(new), H, D, generator=g, device=DEV).to(torch.bfloat16)
+    gone = 0
+    for b, (n, L) in enumerate(zip(new, kv)):
+        e = max(0, L - n - window + 1) // page
+        table[b, :e] = -1 if b % 2 else 1 << 30
+        gone += e
+    assert gone or max(kv) == 150
+    cache = qb.KVCache(ck, cv)
+    ws = qb.alloc_attention_workspace(cache, q)
+    out, lse = qb.paged_attention(q, cache, table, offsets(new), torch.tensor(kv, dtype=torch.int32, device=DEV), window=window,
+                                  need_lse=True, ws=ws)
+    assert qb.device_status(ws) == qb.OK
+    ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, D ** -0.5, window=window)
+    within(out, ref, bound, "out")
+    within(lse, rl, lb, "lse")
