@@ -237,6 +237,15 @@ def _stream_ptr(stream) -> int:
     return _raw_stream(_raw_device())
 
 
+def _empty(shape, dtype, device, stream) -> torch.Tensor:
+    """A workspace or result of a call on `stream`, as one made under torch.cuda.stream(stream): memory of the current stream would
+    be handed out again there as soon as a workspace is dropped, while the call's kernels on `stream` still use it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _dt(torch_dtype) -> int:
     if torch_dtype is torch.bfloat16:
         return BF16
@@ -255,9 +264,9 @@ def workspace_bytes(op: int, qw: QWeight, ad: Optional[Adapter], tokens: int) ->
     return int(_lib.qblora_workspace_bytes(op, ctypes.byref(cq), _ref(ca), tokens))
 
 
-def alloc_workspace(op: int, qw: QWeight, ad: Optional[Adapter], tokens: int) -> torch.Tensor:
+def alloc_workspace(op: int, qw: QWeight, ad: Optional[Adapter], tokens: int, stream=None) -> torch.Tensor:
     n = max(workspace_bytes(op, qw, ad, tokens), 256)
-    return torch.empty(n, dtype=torch.uint8, device=qw.codes.device)
+    return _empty(n, torch.uint8, qw.codes.device, stream)
 
 
 def device_status(ws: torch.Tensor, stream=None) -> int:
@@ -277,9 +286,9 @@ def quantize_blockwise(W: torch.Tensor, block_in: int = 64, block_out: int = 1,
         assert (out.d_out, out.d_in, out.block_in, out.block_out, out.qfmt) == (d_out, d_in, block_in, block_out, qfmt)
         codes, alpha, beta = out.codes, out.alpha, out.beta
     else:
-        codes = torch.empty((d_out, d_in // 2), dtype=torch.uint8, device=W.device)
-        alpha = torch.empty((max(d_out // block_out, 1), max(d_in // block_in, 1)), dtype=torch.float32, device=W.device)
-        beta = torch.empty_like(alpha) if qfmt == FMT_AFFINE_MINMAX else None
+        codes = _empty((d_out, d_in // 2), torch.uint8, W.device, stream)
+        alpha = _empty((max(d_out // block_out, 1), max(d_in // block_in, 1)), torch.float32, W.device, stream)
+        beta = _empty(alpha.shape, torch.float32, W.device, stream) if qfmt == FMT_AFFINE_MINMAX else None
     ctab = (ctypes.c_float * 16)(*code) if code is not None else None
     st = _lib.qblora_quantize_blockwise(W.data_ptr(), _dt(W.dtype), d_out, d_in, block_in, block_out, qfmt,
                                         ctab, codes.data_ptr(), alpha.data_ptr(),
@@ -294,9 +303,9 @@ def quantize_minmax_nbit(W: torch.Tensor, bits: int, block_in: int = 64, block_o
     The codes stay one per nibble, so the result is an ordinary min-max QWeight for every other call."""
     assert W.is_cuda and W.is_contiguous() and W.dim() == 2
     d_out, d_in = W.shape
-    codes = torch.empty((d_out, d_in // 2), dtype=torch.uint8, device=W.device)
-    alpha = torch.empty((max(d_out // block_out, 1), max(d_in // block_in, 1)), dtype=torch.float32, device=W.device)
-    beta = torch.empty_like(alpha)
+    codes = _empty((d_out, d_in // 2), torch.uint8, W.device, stream)
+    alpha = _empty((max(d_out // block_out, 1), max(d_in // block_in, 1)), torch.float32, W.device, stream)
+    beta = _empty(alpha.shape, torch.float32, W.device, stream)
     st = _lib.qblora_quantize_minmax_nbit(W.data_ptr(), _dt(W.dtype), d_out, d_in, block_in, block_out, int(bits),
                                           codes.data_ptr(), alpha.data_ptr(), beta.data_ptr(), _stream_ptr(stream))
     _check(st, "qblora_quantize_minmax_nbit")
@@ -307,9 +316,9 @@ def linear_fwd(qw: QWeight, ad: Optional[Adapter], X: torch.Tensor, out_dtype=to
                ws: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     assert X.is_cuda and X.is_contiguous() and X.dtype == torch.bfloat16
     T = X.shape[0]
-    Y = out if out is not None else torch.empty((T, qw.d_out), dtype=out_dtype, device=X.device)
+    Y = out if out is not None else _empty((T, qw.d_out), out_dtype, X.device, stream)
     if ws is None:
-        ws = alloc_workspace(OP_LINEAR_FWD, qw, ad, T)
+        ws = alloc_workspace(OP_LINEAR_FWD, qw, ad, T, stream)
     cq = qw.c_struct()
     ca = ad.c_struct() if ad is not None else None
     st = _lib.qblora_linear_fwd(ctypes.byref(cq), _ref(ca), X.data_ptr(), T, Y.data_ptr(), _dt(Y.dtype),
@@ -328,15 +337,15 @@ def linear_bwd(qw: QWeight, ad: Optional[Adapter], X: Optional[torch.Tensor], dY
     if outs is not None:
         dX, dA, dB = outs
     else:
-        dX = torch.empty((T, qw.d_in), dtype=dx_dtype, device=dev) if need_dx else None
+        dX = _empty((T, qw.d_in), dx_dtype, dev, stream) if need_dx else None
         dA = dB = None
         if ad is not None:
             if need_da:
-                dA = torch.empty(tuple(ad.A.shape), dtype=torch.float32, device=dev)
+                dA = _empty(tuple(ad.A.shape), torch.float32, dev, stream)
             if need_db and ad.B is not None:
-                dB = torch.empty(tuple(ad.B.shape), dtype=torch.float32, device=dev)
+                dB = _empty(tuple(ad.B.shape), torch.float32, dev, stream)
     if ws is None:
-        ws = alloc_workspace(OP_LINEAR_BWD, qw, ad, T)
+        ws = alloc_workspace(OP_LINEAR_BWD, qw, ad, T, stream)
     cq = qw.c_struct()
     ca = ad.c_struct() if ad is not None else None
     p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
@@ -354,9 +363,9 @@ def merge(qw: QWeight, ad: Adapter, in_place: bool = False, ws: Optional[torch.T
     if qw.beta is None:
         raise QbloraError(ERR_INVALID_ARG, "qablora_merge")
     if beta_out is None:
-        beta_out = qw.beta if in_place else torch.empty_like(qw.beta)
+        beta_out = qw.beta if in_place else _empty(qw.beta.shape, torch.float32, qw.beta.device, stream)
     if ws is None:
-        ws = alloc_workspace(OP_MERGE, qw, ad, 0)
+        ws = alloc_workspace(OP_MERGE, qw, ad, 0, stream)
     cq = qw.c_struct()
     ca = ad.c_struct()
     st = _lib.qablora_merge(ctypes.byref(cq), ctypes.byref(ca), beta_out.data_ptr(), ws.data_ptr(),
@@ -368,9 +377,9 @@ def merge(qw: QWeight, ad: Adapter, in_place: bool = False, ws: Optional[torch.T
 def merge_dense(qw: QWeight, ad: Optional[Adapter], out: Optional[torch.Tensor] = None,
                 ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """Dense 16-bit merge: bf16 [d_out][d_in] = dequantized weight + s * dense adapter update."""
-    W = out if out is not None else torch.empty((qw.d_out, qw.d_in), dtype=torch.bfloat16, device=qw.codes.device)
+    W = out if out is not None else _empty((qw.d_out, qw.d_in), torch.bfloat16, qw.codes.device, stream)
     if ws is None:
-        ws = alloc_workspace(OP_MERGE_DENSE, qw, ad, 0)
+        ws = alloc_workspace(OP_MERGE_DENSE, qw, ad, 0, stream)
     cq = qw.c_struct()
     ca = ad.c_struct() if ad is not None else None
     st = _lib.qblora_merge_dense(ctypes.byref(cq), _ref(ca), W.data_ptr(), ws.data_ptr(), ws.numel(),
@@ -397,9 +406,9 @@ def lowbit_gemm(qw: QWeight, X: torch.Tensor, out_dtype=torch.bfloat16, ws: Opti
                 out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     assert X.is_cuda and X.is_contiguous() and X.dtype == torch.bfloat16
     T = X.shape[0]
-    Y = out if out is not None else torch.empty((T, qw.d_out), dtype=out_dtype, device=X.device)
+    Y = out if out is not None else _empty((T, qw.d_out), out_dtype, X.device, stream)
     if ws is None:
-        ws = alloc_workspace(OP_LOWBIT_GEMM, qw, None, T)
+        ws = alloc_workspace(OP_LOWBIT_GEMM, qw, None, T, stream)
     cq = qw.c_struct()
     st = _lib.qablora_lowbit_gemm(ctypes.byref(cq), X.data_ptr(), T, Y.data_ptr(), _dt(Y.dtype),
                                   ws.data_ptr(), ws.numel(), _stream_ptr(stream))
@@ -414,9 +423,9 @@ def dense_gemm(W: torch.Tensor, X: torch.Tensor, out_dtype=torch.bfloat16, ws: O
     assert X.is_cuda and X.is_contiguous() and X.dtype == torch.bfloat16 and X.shape[1] == W.shape[1]
     T = X.shape[0]
     d_out, d_in = W.shape
-    Y = out if out is not None else torch.empty((T, d_out), dtype=out_dtype, device=X.device)
+    Y = out if out is not None else _empty((T, d_out), out_dtype, X.device, stream)
     if ws is None:
-        ws = torch.empty(256, dtype=torch.uint8, device=X.device)
+        ws = _empty(256, torch.uint8, X.device, stream)
     st = _lib.qblora_dense_gemm(W.data_ptr(), d_out, d_in, X.data_ptr(), T, Y.data_ptr(), _dt(Y.dtype), ws.data_ptr(),
                                 ws.numel(), _stream_ptr(stream))
     _check(st, "qblora_dense_gemm")
@@ -426,8 +435,8 @@ def dense_gemm(W: torch.Tensor, X: torch.Tensor, out_dtype=torch.bfloat16, ws: O
 def pack_codes(qw: QWeight, bits: int, stream=None) -> QWeight:
     """qblora_pack_codes: the same weight with its codes in dense `bits`-bit storage (bits = 2 or 3)."""
     assert qw.code_bits == 4
-    packed = torch.empty((qw.d_out, qw.d_in * bits // 8), dtype=torch.uint8, device=qw.codes.device)
-    ws = torch.empty(256, dtype=torch.uint8, device=qw.codes.device)
+    packed = _empty((qw.d_out, qw.d_in * bits // 8), torch.uint8, qw.codes.device, stream)
+    ws = _empty(256, torch.uint8, qw.codes.device, stream)
     st = _lib.qblora_pack_codes(qw.codes.data_ptr(), qw.d_out, qw.d_in, int(bits), packed.data_ptr(), ws.data_ptr(), ws.numel(),
                                 _stream_ptr(stream))
     _check(st, "qblora_pack_codes")
@@ -438,7 +447,7 @@ def pack_codes(qw: QWeight, bits: int, stream=None) -> QWeight:
 def unpack_codes(qw: QWeight, stream=None) -> QWeight:
     """qblora_unpack_codes: dense storage back to one code per nibble."""
     assert qw.code_bits in (2, 3)
-    codes = torch.empty((qw.d_out, qw.d_in // 2), dtype=torch.uint8, device=qw.codes.device)
+    codes = _empty((qw.d_out, qw.d_in // 2), torch.uint8, qw.codes.device, stream)
     st = _lib.qblora_unpack_codes(qw.codes.data_ptr(), qw.d_out, qw.d_in, int(qw.code_bits), codes.data_ptr(), _stream_ptr(stream))
     _check(st, "qblora_unpack_codes")
     return QWeight(qw.d_out, qw.d_in, qw.block_in, qw.block_out, qw.qfmt, qw.code, codes, qw.alpha, qw.beta, 4)
@@ -527,9 +536,9 @@ def rope(cfg: Rope, positions: torch.Tensor, q: torch.Tensor, k: Optional[torch.
     if shape[2] != D or (k is not None and (k_shape[0] != T or k_shape[2] != D)):
         raise ValueError("q, k: [tokens][heads][head_dim]")
     if out_q is None:
-        out_q = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out_q = _empty(shape, q.dtype, q.device, stream)
     if k is not None and out_k is None:
-        out_k = torch.empty(k_shape, dtype=out_q.dtype, device=k.device)
+        out_k = _empty(k_shape, out_q.dtype, k.device, stream)
     if out_q.shape != shape or (k is not None and out_k.shape != k_shape):
         raise ValueError("outputs have the shapes of the inputs")
     if T == 0:
@@ -550,7 +559,7 @@ def rope_append(cfg: Rope, positions: torch.Tensor, slots: torch.Tensor, q: torc
     if k_shape[0] != T or v.shape != k_shape or shape[2] != D or k_shape[2] != D:
         raise ValueError("q, k, v: [tokens][heads][head_dim]")
     if out_q is None:
-        out_q = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        out_q = _empty(shape, torch.bfloat16, q.device, stream)
     elif out_q.shape != shape:
         raise ValueError("out_q has the shape of q")
     if T == 0:
@@ -573,7 +582,7 @@ def kv_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Ten
         raise ValueError("block_table: [requests][width]")
     B, width = block_table.shape
     if outs is None:
-        outs = tuple(torch.empty(n, dtype=torch.int32, device=block_table.device) for n in (B + 1, B, tokens, tokens, B, 1))
+        outs = tuple(_empty(n, torch.int32, block_table.device, stream) for n in (B + 1, B, tokens, tokens, B, 1))
     cu_new, kv_len, positions, slots, admitted, free_out = outs
     st = _lib.qblora_kv_plan(_ints(ctx_len, B, "ctx_len"), _ints(new_len, B, "new_len"),
                              None if release is None else _ints(release, B, "release"), B,
@@ -592,10 +601,10 @@ def attention_workspace_bytes(cache: KVCache, q_heads: int, tokens: int) -> int:
     return int(_lib.qblora_attention_workspace_bytes(ctypes.byref(c), q_heads, tokens))
 
 
-def alloc_attention_workspace(cache: KVCache, q: torch.Tensor) -> torch.Tensor:
-    """Workspace for paged_attention calls with this cache and up to q.shape[0] tokens."""
+def alloc_attention_workspace(cache: KVCache, q: torch.Tensor, stream=None) -> torch.Tensor:
+    """Workspace for paged_attention calls (on `stream`) with this cache and up to q.shape[0] tokens."""
     n = max(attention_workspace_bytes(cache, q.shape[1], max(q.shape[0], 1)), 256)
-    return torch.empty(n, dtype=torch.uint8, device=q.device)
+    return _empty(n, torch.uint8, q.device, stream)
 
 
 def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, cu_new: torch.Tensor, kv_len: torch.Tensor,
@@ -610,15 +619,15 @@ def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, 
         raise ValueError("q: [tokens][q_heads][head_dim of the cache]")
     B, width = block_table.shape
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=q.device)
+        out = _empty(shape, torch.bfloat16, q.device, stream)
     if lse is None and need_lse:
-        lse = torch.empty((T, H), dtype=torch.float32, device=q.device)
+        lse = _empty((T, H), torch.float32, q.device, stream)
     if out.shape != shape or (lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_contiguous() or not lse.is_cuda)):
         raise ValueError("out: shape of q; lse: contiguous fp32 device tensor [tokens][q_heads]")
     if T == 0:
         return out, lse
     if ws is None:
-        ws = alloc_attention_workspace(cache, q)
+        ws = alloc_attention_workspace(cache, q, stream)
     elif not ws.is_cuda or ws.dtype is not torch.uint8:
         raise ValueError("ws: uint8 device tensor")
     by = ctypes.byref

@@ -718,3 +718,60 @@ def test_attention_pages_in_front_of_the_window_may_be_gone(monkeypatch, general
     ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, D ** -0.5, window=window)
     within(out, ref, bound, "out")
     within(lse, rl, lb, "lse")
+
+
+def test_calls_on_a_stream_own_their_memory_there(monkeypatch):
+    # what a call on another stream allocates (workspaces above all, which it drops when it returns) comes from that stream's
+    # memory: taken from the current stream's, the next tensor made there could lie in it while the kernels still run
+    qb = _qb()
+    g = _gen(51)
+    kv, D = [900, 40, 300], 128
+    new = [1, 40, 3]
+    ck, cv, table, ks, vs = make_cache(g, kv, 16, 2, D, fill=0.0)
+    q = torch.randn(sum(new), 8, D, generator=g, device=DEV).to(torch.bfloat16)
+    k = torch.randn(sum(new), 2, D, generator=g, device=DEV).to(torch.bfloat16)
+    cache, cu, lens = qb.KVCache(ck, cv), offsets(new), torch.tensor(kv, dtype=torch.int32, device=DEV)
+    rope = qb.Rope(D, D, qb.ROPE_HALF, qb.rope_table(D))
+    pos, slots = torch.zeros(sum(new), dtype=torch.int32, device=DEV), torch.full((sum(new),), -1, dtype=torch.int32, device=DEV)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device=DEV)  # noqa: E731
+    ctx, one, tab, free, count = i32([3]), i32([1]), i32([[0, -1]]), i32([1, 2]), i32([2])
+    x = torch.randn(3, 256, generator=g, device=DEV).to(torch.bfloat16)
+    w = torch.randn(128, 256, generator=g, device=DEV)
+    ad = qb.Adapter(64, 8, 4, 1.0, torch.randn(4, 4, generator=g, device=DEV).bfloat16(), torch.randn(4, 16, generator=g, device=DEV).bfloat16())
+    qw = qb.quantize_blockwise(w, 64, 1, qb.FMT_AFFINE_MINMAX)
+    q2, wb = qb.quantize_minmax_nbit(w, 2), w.bfloat16()
+    dy = torch.randn(3, 128, generator=g, device=DEV).to(torch.bfloat16)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    made, real = [], torch.empty
+
+    def empty(*a, **kw):
+        made.append(torch.cuda.current_stream().cuda_stream)
+        return real(*a, **kw)
+
+    calls = [lambda s: qb.paged_attention(q, cache, table, cu, lens, need_lse=True, stream=s), lambda s: qb.rope(rope, pos, q, k, stream=s),
+             lambda s: qb.rope_append(rope, pos, slots, q, k, k, cache, stream=s),
+             lambda s: qb.kv_plan(ctx, one, tab, free, count, 16, 2, stream=s), lambda s: qb.linear_fwd(qw, ad, x, stream=s),
+             lambda s: qb.linear_bwd(qw, ad, x, dy, stream=s), lambda s: qb.merge(qw, ad, stream=s), lambda s: qb.merge_dense(qw, ad, stream=s),
+             lambda s: qb.lowbit_gemm(qw, x, stream=s), lambda s: qb.dense_gemm(wb, x, stream=s),
+             lambda s: qb.quantize_blockwise(w, 64, 1, qb.FMT_AFFINE_MINMAX, stream=s), lambda s: qb.quantize_minmax_nbit(w, 2, stream=s),
+             lambda s: qb.unpack_codes(qb.pack_codes(q2, 2, stream=s), stream=s)]
+    monkeypatch.setattr(torch, "empty", empty)
+    for i, call in enumerate(calls):
+        made.clear()
+        call(side)
+        torch.cuda.synchronize()
+        assert made and set(made) == {side.cuda_stream}, (i, made)
+    monkeypatch.undo()
+
+    # and the results are right while the current stream takes and overwrites memory of the workspace's size at once
+    ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, D ** -0.5)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(2000000)
+        out, lse = qb.paged_attention(q, cache, table, cu, lens, need_lse=True, stream=side)
+        real(qb.attention_workspace_bytes(cache, 8, sum(new)), dtype=torch.uint8, device=DEV).fill_(0x7F)
+        torch.cuda.synchronize()
+        within(out, ref, bound, "out")
+        within(lse, rl, lb, "lse")
