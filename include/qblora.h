@@ -418,7 +418,7 @@ int qblora_rope_append(const qblora_rope_cfg* cfg, const int32_t* positions, con
  *     onto the free stack (in request order, then table order) before any page is taken, and it adds nothing.
  *   block_table [B][width]: the first ceil(ctx / page_size) entries of a row are read, entries of pages taken now written.
  *   free_pages [capacity]: the stack of free pages, its lowest free_count[0] entries valid; pages given back are written
- *     behind them.  free_count_out[0]: entries left afterwards (must not be free_count itself).
+ *     behind them.  free_count_out[0]: entries left afterwards.
  *   A request is valid if ctx >= 0, new >= 0 and ctx + new <= width * page_size.  Admission is first come, first
  *   served: a valid request is admitted if the pages that it and all valid requests before it need are there, and their
  *   new tokens fit into `tokens` rows.  (So once one does not fit, none behind it is admitted.)  The a-th page taken (in
@@ -426,6 +426,8 @@ int qblora_rope_append(const qblora_rope_cfg* cfg, const int32_t* positions, con
  *   Out: cu_new [B + 1] and kv_len [B] (ctx + admitted new tokens; 0 for a released request; an invalid one has its
  *   ctx clamped to 0 .. width * page_size); positions [tokens], slots [tokens]: row cu_new[b] + i is position ctx + i of
  *   request b; rows behind the last new token: position 0, slot -1.  admitted [B]: 1 or 0.
+ * No array that is written (outputs, block_table, free_pages) may overlap another array of the call, else
+ * QBLORA_ERR_INVALID_ARG: lengths are read throughout, so kv_len cannot be written over ctx_len, nor free_count_out over free_count.
  * One launch; nothing is synchronised, so it can be captured in a graph.  The outputs depend on the inputs alone, and a
  * second call on the same inputs changes nothing.  1 <= B <= 8192, else QBLORA_ERR_UNSUPPORTED.
  */

@@ -50,6 +50,13 @@ bool force_general() {
 
 bool int_ptr_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 
+// An array of n int32 values of a call; p may be NULL.
+struct IntSpan { const int32_t* p; int64_t n; };
+bool overlap(const IntSpan& a, const IntSpan& b) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
+  return a.p && b.p && a0 < b0 + (uintptr_t)b.n * 4 && b0 < a0 + (uintptr_t)a.n * 4;
+}
+
 }  // namespace
 }  // namespace qb
 
@@ -121,6 +128,13 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
   if (n_requests < 1 || width < 1 || capacity < 1 || page_size < 1 || tokens < 1) return QBLORA_ERR_INVALID_ARG;
   if ((int64_t)capacity * page_size >= (int64_t)1 << 31 || (int64_t)width * page_size >= (int64_t)1 << 31) return QBLORA_ERR_INVALID_ARG;
   if (n_requests > kPlanMaxRequests) return QBLORA_ERR_UNSUPPORTED;
+  // Every CTA reads the lengths for itself, whenever it runs: nothing that is written may lie in what is read, or in another output.
+  const IntSpan arrays[] = {{block_table, (int64_t)n_requests * width}, {free_pages, capacity}, {free_count_out, 1}, {cu_new, n_requests + 1},
+                            {kv_len, n_requests}, {positions, tokens}, {slots, tokens}, {admitted, n_requests},      // written
+                            {ctx_len, n_requests}, {new_len, n_requests}, {release, n_requests}, {free_count, 1}};   // read only
+  for (int i = 0; i < 8; ++i)
+    for (int j = i + 1; j < 12; ++j)
+      if (overlap(arrays[i], arrays[j])) return QBLORA_ERR_INVALID_ARG;
   PlanCall c{ctx_len, new_len, release, n_requests, block_table, width, free_pages, capacity, free_count, free_count_out,
              page_size, tokens, cu_new, kv_len, positions, slots, admitted};
   return launch_kv_plan(c, static_cast<cudaStream_t>(stream));

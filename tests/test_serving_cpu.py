@@ -136,3 +136,23 @@ def test_plan_refusals(qb):
                dict(T=0), dict(cnt_out=P), dict(cu=None), dict(adm=None), dict(cap=1 << 28), dict(width=1 << 28)]:
         assert call(**kw) == qb.ERR_INVALID_ARG, kw
     assert call(B=8193) == qb.ERR_UNSUPPORTED
+
+
+def test_plan_refuses_arrays_that_overlap():
+    # every CTA reads the lengths for itself, so an output over an input (kv_len over ctx_len, the in-place step) is a race.  The
+    # check stands before the launch; the call without overlap is not made.
+    from paper_2407_17029_b200 import binding as qb
+    B, width, cap, T = 4, 8, 64, 9
+    sizes = dict(ctx=B, new=B, rel=B, table=B * width, stack=cap, cnt=1, cnt_out=1, cu=B + 1, kv=B, pos=T, slots=T, adm=B)
+    addr, at = {}, P
+    for name, n in sizes.items():
+        addr[name] = at
+        at += n * 4
+    order = ["ctx", "new", "rel", B, "table", width, "stack", cap, "cnt", "cnt_out", 16, T, "cu", "kv", "pos", "slots", "adm"]
+    call = lambda a: qb._lib.qblora_kv_plan(*[a[x] if isinstance(x, str) else x for x in order], None)  # noqa: E731
+    read_only = {"ctx", "new", "rel", "cnt"}
+    for out in sizes.keys() - read_only:
+        for other in sizes.keys() - {out}:
+            # the same start, and the output's first word over the other's last one
+            for where in (addr[other], addr[other] + (sizes[other] - 1) * 4):
+                assert call({**addr, out: where}) == qb.ERR_INVALID_ARG, (out, other)
