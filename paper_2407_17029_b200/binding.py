@@ -465,8 +465,8 @@ class Rope:
 
     def c_struct(self) -> _CRope:
         t = self.table
-        if t.dtype is not torch.int64 or not t.is_contiguous() or 2 * t.numel() != self.rotary_dim:
-            raise ValueError("table: contiguous int64 [rotary_dim / 2], see rope_table")
+        if t.dtype is not torch.int64 or not t.is_cuda or not t.is_contiguous() or 2 * t.numel() != self.rotary_dim:
+            raise ValueError("table: contiguous int64 device tensor [rotary_dim / 2], see rope_table")
         return _CRope(self.head_dim, self.rotary_dim, self.layout, self.amplitude, t.data_ptr())
 
 
@@ -483,13 +483,13 @@ class KVCache:
         return KVCache(torch.empty(shape, dtype=torch.bfloat16, device=device),
                        torch.empty(shape, dtype=torch.bfloat16, device=device))
 
-    def c_struct(self) -> _CKVCache:
+    def c_struct(self, sizes_only: bool = False) -> _CKVCache:
         k, v = self.k, self.v
         shape, stride = k.shape, k.stride()
         if len(shape) != 4 or shape != v.shape or stride != v.stride() or stride[3] != 1:
             raise ValueError("k, v: equal shapes and strides [n_pages][page_size][kv_heads][head_dim], head_dim contiguous")
-        if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16:
-            raise ValueError("k, v: bf16")
+        if k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16 or not (sizes_only or k.is_cuda and v.is_cuda):
+            raise ValueError("k, v: bf16 device tensors")
         return _CKVCache(k.data_ptr(), v.data_ptr(), stride[0], stride[1], stride[2], *shape)
 
 
@@ -597,7 +597,7 @@ def kv_plan(ctx_len: torch.Tensor, new_len: torch.Tensor, block_table: torch.Ten
 
 
 def attention_workspace_bytes(cache: KVCache, q_heads: int, tokens: int) -> int:
-    c = cache.c_struct()
+    c = cache.c_struct(sizes_only=True)
     return int(_lib.qblora_attention_workspace_bytes(ctypes.byref(c), q_heads, tokens))
 
 
@@ -628,8 +628,8 @@ def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, 
         return out, lse
     if ws is None:
         ws = alloc_attention_workspace(cache, q, stream)
-    elif not ws.is_cuda or ws.dtype is not torch.uint8:
-        raise ValueError("ws: uint8 device tensor")
+    elif not ws.is_cuda or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws: contiguous uint8 device tensor")
     by = ctypes.byref
     st = _lib.qblora_paged_attention(by(cc), _ints(block_table, 1, "block_table"), width, _ints(cu_new, B + 1, "cu_new"),
                                      _ints(kv_len, B, "kv_len"), B, by(_heads(q)), T, D ** -0.5 if scale is None else scale,

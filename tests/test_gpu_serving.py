@@ -775,3 +775,14 @@ def test_calls_on_a_stream_own_their_memory_there(monkeypatch):
         torch.cuda.synchronize()
         within(out, ref, bound, "out")
         within(lse, rl, lb, "lse")
+
+
+def test_workspaces_that_are_smaller_than_they_look_are_refused():
+    qb = _qb()
+    cache = qb.KVCache.empty(4, 16, 2, 128)
+    q = torch.zeros(3, 8, 128, dtype=torch.bfloat16, device=DEV)
+    i = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)  # noqa: E731
+    for ws in (torch.empty(1, dtype=torch.uint8, device=DEV).expand(1 << 30), torch.empty(1 << 20, dtype=torch.uint8, device=DEV)[::2],
+               torch.empty(1 << 30, dtype=torch.uint8), torch.empty(1 << 20, device=DEV)):
+        with pytest.raises(ValueError):
+            qb.paged_attention(q, cache, i(1, 4), i(2), i(1), ws=ws)

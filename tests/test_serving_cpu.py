@@ -156,3 +156,16 @@ def test_plan_refuses_arrays_that_overlap():
             # the same start, and the output's first word over the other's last one
             for where in (addr[other], addr[other] + (sizes[other] - 1) * 4):
                 assert call({**addr, out: where}) == qb.ERR_INVALID_ARG, (out, other)
+
+
+def test_tables_and_caches_in_host_memory_are_refused(qb):
+    import torch
+    table = qb.rope_table(64, device="cpu")
+    with pytest.raises(ValueError):
+        qb.Rope(64, 64, qb.ROPE_HALF, table).c_struct()
+    with pytest.raises(ValueError):
+        qb.KVCache.empty(4, 16, 2, 64, device="cpu").c_struct()
+    assert qb.attention_workspace_bytes(qb.KVCache.empty(4, 16, 2, 64, device="cpu"), 2, 1) >= 256      # sizes can be asked for
+    x, pos = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
+    with pytest.raises(ValueError):
+        qb.rope(qb.Rope(64, 64, qb.ROPE_HALF, table), pos, x)
