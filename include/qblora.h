@@ -448,6 +448,7 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
  *   q, out: bf16.  head_dim % 8 == 0, at most 256; q heads a multiple of kv_heads; strides multiples of 8 elements and
  *   16-byte aligned data for q, out and the cache.  scale: usually 1 / sqrt(head_dim).
  *   Scores, softmax statistics and sums are fp32; the weights exp(s - max) are rounded to bf16 for their product with v.
+ *   The sums over v carry weights of up to 2^10, so finite results are certain for |v| up to 2^117 / keys of the row.
  * Lengths are read on the device only, so one captured graph serves every step of the same shape.  Lengths and table
  * entries out of range are clamped and never lead outside the cache; a page number out of range sets the status word to
  * QBLORA_ERR_INVALID_ARG (that request's results are then undefined).

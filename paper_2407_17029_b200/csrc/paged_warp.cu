@@ -42,7 +42,7 @@ namespace {
 constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
 constexpr int PW_MAX_LEVELS = kPagedLevels;
 constexpr int PW_FINE = 11;       // key tiles of the shortest shares
-constexpr float PW_OUTGROWN = 1.099511627776e12f;   // 2^40
+constexpr float PW_OUTGROWN = 1024.0f;   // a lane's sum of a tile's weights that asks for a new maximum
 constexpr float PW_LN2 = 0.69314718055994530942f;
 
 template <int D>
@@ -490,8 +490,9 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
             if (j >= hi[e >> 1] || j < lo[e >> 1]) s[n][e] = -INFINITY;
           }
       }
-      // Weights with the m there is; only where a row has none yet, or where a sum shows that the scores have outgrown m (fp32
-      // and bf16 hold weights of 2^40 as exactly as weights of 1), the maximum is looked for and they are done again.
+      // Weights with the m there is; only where a row has none yet, or where a sum shows that the scores have outgrown m, the
+      // maximum is looked for and they are done again.  Weights of 2^10 are as exact as weights of 1; but what o can hold shrinks by
+      // that factor (with 2^40 here, values of 2^90 overflowed).
       float w[NT][4], sum[2];
       bool again = __any_sync(0xffffffffu, m[0] == -INFINITY || m[1] == -INFINITY);
 #pragma unroll 1

@@ -5,9 +5,9 @@
 //   S = Q K^T          tcgen05.mma, operands in shared memory, S (fp32) in tensor memory
 //   P = 2^(S c - m)    one thread per row; bf16 P goes back to tensor memory, over S
 //   O += P V           tcgen05.mma, A = P from tensor memory, V as an MN-major B operand, O (fp32) in tensor memory
-// m need not be the maximum: weights of 2^40 are as exact as weights of 1 (both have the same 8 and 24 bits), so m is a row's
-// maximum over its first tile and moves only when a tile's sum of weights shows that the scores have outgrown it; then O
-// is scaled in tensor memory by the row's thread.  That is safe without a further wait: the commit that announces S of tile
+// m need not be the maximum: weights of 2^10 are as exact as weights of 1 (both have the same 8 and 24 bits), so m is a row's
+// maximum over its first tile and moves only when a tile's sum of weights shows that the scores have outgrown it (by more, values
+// of a size that bf16 still holds would overflow O); then O is scaled in tensor memory by the row's thread.  That is safe without a further wait: the commit that announces S of tile
 // j covers P V of tile j - 1, and P V of tile j waits for this thread.
 //
 // Roles (one CTA per SM, 384 threads): warps 0-3 and 4-7 are the softmax of two row tiles that share every K and V stage
@@ -47,8 +47,7 @@ constexpr float TA_LN2 = 0.69314718055994530942f;
 constexpr long long TA_L2_BYTES = 96000000;
 constexpr int TA_CUT = 6;               // key tiles that the cuts of a share cost
 constexpr int TA_SEGS = 4;              // segments handed out ahead
-constexpr float TA_SLACK = 8.0f;        // where the maximum is looked for: how far (in powers of two) it may be ahead of m
-constexpr float TA_OUTGROWN = 1.099511627776e12f;   // 2^40: a tile's sum of weights that asks for a new m
+constexpr float TA_OUTGROWN = 1024.0f;  // a tile's sum of weights that asks for a new m (at most 128 with m the maximum)
 
 template <int D>
 struct TaShape {
@@ -726,8 +725,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
             if (i >= h_ || i < l_) s[i] = 0xff800000u;
         }
         // The weights are taken with the m there is; only where a row has none yet, or where its sum shows that the scores
-        // have outgrown m (bf16 and fp32 hold weights up to 2^40 as exactly as weights up to 1), the maximum is
-        // looked for and the tile done again with it.  That saves a pass over the scores of almost every tile.
+        // have outgrown m, the maximum is looked for and the tile done again with it.  That saves a pass over the scores of almost every tile.
         float sum = 0.f;
 #pragma unroll 1
         for (int pass = __any_sync(0xffffffffu, m == -INFINITY) ? 1 : 0; pass < 2; ++pass) {
@@ -743,7 +741,7 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
 #pragma unroll
             for (int q = 0; q < 4; ++q) mx[q] = fmaxf(mx[q], __uint_as_float(s[124 + q]));
             const float mt = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * p.scale2;
-            const float mn = mt > m + TA_SLACK ? mt : m;
+            const float mn = fmaxf(m, mt);
             const float f = m == mn ? 1.f : fast_exp2(m - mn);        // m = -infinity: 0
             m = mn;
             l *= f;

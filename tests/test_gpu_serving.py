@@ -786,3 +786,25 @@ def test_workspaces_that_are_smaller_than_they_look_are_refused():
                torch.empty(1 << 30, dtype=torch.uint8), torch.empty(1 << 20, device=DEV)):
         with pytest.raises(ValueError):
             qb.paged_attention(q, cache, i(1, 4), i(2), i(1), ws=ws)
+
+
+@pytest.mark.parametrize("size", [2.0 ** 100, 2.0 ** -100])
+@pytest.mark.parametrize("run", [16, 32, 128, 300])
+@pytest.mark.parametrize("D,new,kv", [(128, [1], [4000]), (64, [1, 1, 1, 1], [2000, 900, 40, 600]), (128, [1] * 40, [900] * 40),
+                                      (128, [20, 3], [900, 333]), (64, [150], [1500]), (128, [300, 40], [1000, 700]), (96, [5], [700])])
+def test_attention_large_and_small_values_under_rising_scores(size, run, D, new, kv):
+    # runs of keys with scores 26 above the ones in front of them (weights up to 2^37 of theirs), and values whose products with
+    # such weights would leave the range of fp32: the result is a weighted mean of the values and stays within theirs
+    def plant(ks, vs, q, at):
+        g = _gen(7)
+        u = torch.randn(D, generator=g, device=DEV)
+        u *= (D / float(u @ u)) ** 0.5
+        q.copy_((u + 0.05 * torch.randn(q.shape, generator=g, device=DEV)).to(torch.bfloat16))
+        for b in range(len(ks)):
+            for j in range(kv[b]):
+                ks[b][j] = (u * (26.0 * (j // run % 2) / D ** 0.5)).to(torch.bfloat16)
+                vs[b][j] *= size
+                k, v = at(b, j)
+                k.copy_(ks[b][j])
+                v.copy_(vs[b][j])
+    _attend(new, kv, 8, 2, D, edit=plant)
