@@ -773,7 +773,8 @@ tc_attention_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_const
           }
           sum2[0] = add2(sum2[0], sum2[1]);
           sum = lo2(sum2[0]) + hi2(sum2[0]);
-          if (!__any_sync(0xffffffffu, !(sum < TA_OUTGROWN))) break;
+          // rows that are none do not vote: what they hold is other requests' queries, or what an earlier kernel left in shared memory
+          if (!__any_sync(0xffffffffu, real && !(sum < TA_OUTGROWN))) break;
         }
         l += sum;
         tc_st_wait();

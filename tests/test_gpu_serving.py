@@ -808,3 +808,30 @@ def test_attention_large_and_small_values_under_rising_scores(size, run, D, new,
                 k.copy_(ks[b][j])
                 v.copy_(vs[b][j])
     _attend(new, kv, 8, 2, D, edit=plant)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [3, 5, 7, 24])
+def test_attention_does_not_depend_on_what_shared_memory_held(G, D):
+    # G does not divide 128, so the last rows of a query tile are never filled; and a request's last tile holds rows of the next
+    # request.  Neither may have a say in how the rows that are there are worked on: results are equal bit for bit.
+    qb = _qb()
+    g = _gen(61)
+    new, kv = [300, 50], [900, 700]
+    ck, cv, table, ks, vs = make_cache(g, kv, 16, 4, D)
+    q = torch.randn(sum(new), 4 * G, D, generator=g, device=DEV).to(torch.bfloat16)
+    args = (qb.KVCache(ck, cv), table, offsets(new), torch.tensor(kv, dtype=torch.int32, device=DEV))
+    pk, pv, ptable, _, _ = make_cache(g, [512], 16, 64, D, fill=0.0)
+    outs = []
+    for held in (0.0, float("nan"), 3e38, 1.0):
+        fill = torch.full((512, 64, D), held, dtype=torch.bfloat16, device=DEV)          # 128 items: most SMs' query tiles
+        qb.paged_attention(fill, qb.KVCache(pk, pv), ptable, offsets([512]), torch.tensor([512], dtype=torch.int32, device=DEV))
+        outs.append(qb.paged_attention(q, *args, need_lse=True))
+        other = q.clone()
+        other[300:] = held                                                              # the second request's queries
+        outs.append([t[:300] for t in qb.paged_attention(other, *args, need_lse=True)])
+    for out, lse in outs:
+        assert torch.equal(out[:300], outs[0][0][:300]) and torch.equal(lse[:300], outs[0][1][:300])
+    ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, D ** -0.5)
+    within(outs[0][0], ref, bound, "out")
+    within(outs[0][1], rl, lb, "lse")
