@@ -443,6 +443,7 @@ paged_warp_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constan
         }
         odd = __any_sync(0xffffffffu, odd);
         fence_async_proxy();                               // before the slot's next copy
+        __syncwarp();                                      // every lane's fragments hold what other lanes have cleaned (a vote orders no memory)
       }
 
       // scores: fragment n covers keys 8 n .. 8 n + 7 (lane: rows lane / 4 and + 8, keys 2 (lane % 4) + {0, 1}); with few
