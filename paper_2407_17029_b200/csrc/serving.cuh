@@ -74,7 +74,7 @@ __device__ __forceinline__ ReqView attn_request(const AttnCall& c, int b) {
 }
 // Keys [lo, hi) that the row at position p (may be negative) sees.
 __device__ __forceinline__ int attn_hi(const AttnCall& c, int kv, int p) { return c.causal ? max(0, min(kv, p + 1)) : kv; }
-__device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.window > 0 ? max(0, p - c.window + 1) : 0; }
+__device__ __forceinline__ int attn_lo(const AttnCall& c, int p) { return c.window > 0 && p >= c.window ? p - c.window + 1 : 0; }
 
 // ---- attention: layout of the caller's workspace, after the status word
 //   counters that every call zeroes (launch_attention_reset), then the parts of paged_attn.cu or paged_warp.cu, then those of

@@ -835,3 +835,14 @@ def test_attention_does_not_depend_on_what_shared_memory_held(G, D):
     ref, bound, rl, lb = ref_attention(q, ks, vs, new, kv, D ** -0.5)
     within(outs[0][0], ref, bound, "out")
     within(outs[0][1], rl, lb, "lse")
+
+
+@pytest.mark.parametrize("window", [(1 << 31) - 1, (1 << 31) - 3])
+def test_attention_widest_windows(monkeypatch, window):
+    # a window that never ends, also for rows in front of the sequence (fewer keys than new rows)
+    for new, kv in (([6], [2]), ([1, 9], [40, 3]), ([300], [10]), ([70, 1], [5, 900])):
+        for causal in (True, False):
+            _attend(new, kv, 4, 2, 128, causal=causal, window=window)
+            _attend(new, kv, 4, 2, 40, causal=causal, window=window)
+    monkeypatch.setenv("QBLORA_FORCE_GENERAL", "1")
+    _attend([6], [2], 4, 2, 64, causal=False, window=window)
