@@ -397,7 +397,8 @@ int qblora_rope_table(int32_t rotary_dim, double base, int32_t scale, double fac
  *   (a, b) -> amplitude * (a cos - b sin, b cos + a sin);
  * inverse != 0 turns by the negative angle (same amplitude), which is the backward pass: dx from dy.
  *   positions DEVICE int32 [tokens].  x -> y and (optional, NULL to leave out) x2 -> y2: q and k in one launch.  y may be x
- *   itself (same data and strides); any other overlap is not allowed.  All inputs have one dtype, all outputs one dtype.
+ *   itself (same data, strides and dtype); any other overlap is not allowed, and one that begins at the same address is refused.
+ *   All inputs have one dtype, all outputs one dtype.
  *   Computed in fp32, rounded once.  Any strides and alignment (16-byte ones are read in wide words).
  */
 int qblora_rope(const qblora_rope_cfg* cfg, int inverse, const int32_t* positions, int64_t tokens, const qblora_heads* x,

@@ -16,6 +16,11 @@ bool heads_ok(const qblora_heads* h, HeadsView* v) {
   return true;
 }
 
+// y may be x itself, not x's memory in another type or order: elements are written while others of x are still to be read
+bool in_place_ok(const HeadsView& x, const HeadsView& y, int64_t tokens) {
+  return x.data != y.data || (x.dtype == y.dtype && (x.ts == y.ts || tokens == 1) && (x.hs == y.hs || x.heads == 1));
+}
+
 bool cache_ok(const qblora_kv_cache* c, CacheView* v) {
   if (!c || !c->k || !c->v) return false;
   if (reinterpret_cast<uintptr_t>(c->k) % 2 || reinterpret_cast<uintptr_t>(c->v) % 2) return false;
@@ -99,7 +104,9 @@ int qblora_rope(const qblora_rope_cfg* cfg, int inverse, const int32_t* position
   if (x2) {
     if (!heads_ok(x2, &c.k) || !heads_ok(y2, &c.k_out) || x2->heads != y2->heads) return QBLORA_ERR_INVALID_ARG;
     if (x2->dtype != x->dtype || y2->dtype != y->dtype) return QBLORA_ERR_INVALID_ARG;
+    if (!in_place_ok(c.k, c.k_out, tokens) || x2->data == y->data || x->data == y2->data || y->data == y2->data) return QBLORA_ERR_INVALID_ARG;
   }
+  if (!in_place_ok(c.q, c.q_out, tokens)) return QBLORA_ERR_INVALID_ARG;
   c.positions = positions; c.T = tokens;
   return launch_rope(c, static_cast<cudaStream_t>(stream));
 }
@@ -113,6 +120,7 @@ int qblora_rope_append(const qblora_rope_cfg* cfg, const int32_t* positions, con
   if (!cache_ok(cache, &c.cache)) return QBLORA_ERR_INVALID_ARG;
   if (q->heads != q_out->heads || q_out->dtype != QBLORA_BF16 || k->dtype != q->dtype || v->dtype != q->dtype) return QBLORA_ERR_INVALID_ARG;
   if (k->heads != cache->kv_heads || v->heads != cache->kv_heads || cfg->head_dim != cache->head_dim) return QBLORA_ERR_INVALID_ARG;
+  if (!in_place_ok(c.q, c.q_out, tokens) || q_out->data == k->data || q_out->data == v->data) return QBLORA_ERR_INVALID_ARG;
   c.positions = positions; c.slots = slots; c.T = tokens;
   return launch_rope(c, static_cast<cudaStream_t>(stream));
 }

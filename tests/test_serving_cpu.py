@@ -169,3 +169,20 @@ def test_tables_and_caches_in_host_memory_are_refused(qb):
     x, pos = torch.zeros(3, 2, 64), torch.zeros(3, dtype=torch.int32)
     with pytest.raises(ValueError):
         qb.rope(qb.Rope(64, 64, qb.ROPE_HALF, table), pos, x)
+
+
+def test_rope_refuses_its_input_in_another_type_or_order(qb):
+    # in place means the same elements at the same places; the check stands before the launch, and no call without overlap is made
+    cfg = qb._CRope()
+    cfg.head_dim, cfg.rotary_dim, cfg.layout, cfg.amplitude, cfg.turns = 128, 64, 0, 1.0, P
+    r = ctypes.byref
+    Q, K, R = 1 << 20, 2 << 20, 3 << 20
+    h = lambda data, heads=2, **kw: _heads(qb, heads, data=data, **kw)  # noqa: E731
+    for x, y in [(h(Q, dtype=0), h(Q, dtype=1)), (h(Q), h(Q, ts=2048)), (h(Q), h(Q, hs=256))]:
+        assert qb._lib.qblora_rope(r(cfg), 0, P, 3, r(x), r(y), None, None, None) == qb.ERR_INVALID_ARG
+        assert qb._lib.qblora_rope(r(cfg), 0, P, 3, r(h(K, dtype=x.dtype)), r(h(R, dtype=y.dtype)), r(x), r(y), None) == qb.ERR_INVALID_ARG
+    for y, y2 in [(K, R), (R, Q), (R, R)]:                    # q' over k, k' over q, both to one place
+        assert qb._lib.qblora_rope(r(cfg), 0, P, 3, r(h(Q)), r(h(y)), r(h(K)), r(h(y2)), None) == qb.ERR_INVALID_ARG
+    for q, o in [(h(Q, dtype=0), h(Q)), (h(Q), h(Q, ts=2048)), (h(Q), h(K)), (h(Q), h(R))]:
+        k, v = h(K, dtype=q.dtype), h(R, dtype=q.dtype)
+        assert qb._lib.qblora_rope_append(r(cfg), P, P, 3, r(q), r(k), r(v), r(o), r(_cache(qb)), None) == qb.ERR_INVALID_ARG
