@@ -445,7 +445,7 @@ int qblora_kv_plan(const int32_t* ctx_len, const int32_t* new_len, const int32_t
  * A row that sees no key gives zeros and lse = -infinity.  Keys that a row does not see do not reach its result, whatever
  * they hold (NaN and infinities too).  lse [tokens][q heads] fp32 (NULL to leave out) = log sum_j exp(scale * q . k_j).
  * Rows that belong to no request are not written.
- *   block_table [B][width], cu_new [B + 1], kv_len [B]: DEVICE int32, as written by qblora_kv_plan.
+ *   block_table [B][width], cu_new [B + 1], kv_len [B]: DEVICE int32, as written by qblora_kv_plan; width * page_size <= 2^31 - 256.
  *   q, out: bf16.  head_dim % 8 == 0, at most 256; q heads a multiple of kv_heads; strides multiples of 8 elements and
  *   16-byte aligned data for q, out and the cache.  scale: usually 1 / sqrt(head_dim).
  *   Scores, softmax statistics and sums are fp32; the weights exp(s - max) are rounded to bf16 for their product with v.

@@ -163,7 +163,8 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
   if (!cache_ok(cache, &c.cache) || !heads_ok(q, &qv) || !heads_ok(out, &ov)) return QBLORA_ERR_INVALID_ARG;
   if (!int_ptr_ok(block_table) || !int_ptr_ok(cu_new) || !int_ptr_ok(kv_len) || (lse && !int_ptr_ok(lse))) return QBLORA_ERR_INVALID_ARG;
   if (width < 1 || n_requests < 1 || tokens < 1 || tokens >= (int64_t)1 << 31 || window < 0 || !std::isfinite(scale)) return QBLORA_ERR_INVALID_ARG;
-  if ((int64_t)width * cache->page_size >= (int64_t)1 << 31) return QBLORA_ERR_INVALID_ARG;
+  // key numbers are rounded up to whole tiles (of at most 128 keys) in 32 bits
+  if ((int64_t)width * cache->page_size > ((int64_t)1 << 31) - 256) return QBLORA_ERR_INVALID_ARG;
   if (qv.dtype != QBLORA_BF16 || ov.dtype != QBLORA_BF16 || qv.heads != ov.heads || qv.heads % cache->kv_heads) return QBLORA_ERR_INVALID_ARG;
   if (cache->head_dim % 8) return QBLORA_ERR_INVALID_ARG;
   if (!aligned16(q->data) || !aligned16(out->data) || !aligned16(cache->k) || !aligned16(cache->v)) return QBLORA_ERR_INVALID_ARG;

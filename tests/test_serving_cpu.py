@@ -186,3 +186,13 @@ def test_rope_refuses_its_input_in_another_type_or_order(qb):
     for q, o in [(h(Q, dtype=0), h(Q)), (h(Q), h(Q, ts=2048)), (h(Q), h(K)), (h(Q), h(R))]:
         k, v = h(K, dtype=q.dtype), h(R, dtype=q.dtype)
         assert qb._lib.qblora_rope_append(r(cfg), P, P, 3, r(q), r(k), r(v), r(o), r(_cache(qb)), None) == qb.ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("page", [1, 8, 16, 64, 256])
+def test_attention_refuses_tables_whose_last_tile_passes_31_bits(qb, page):
+    # lengths are clamped to width * page_size; rounded up to a tile they still have to be a 32-bit number
+    r = lambda x: ctypes.byref(x)  # noqa: E731
+    for keys, want in (((1 << 31) - page, qb.ERR_WORKSPACE if page == 256 else qb.ERR_INVALID_ARG), ((1 << 31) - 256, qb.ERR_WORKSPACE)):
+        got = qb._lib.qblora_paged_attention(r(_cache(qb, page_size=page, page_stride=page * 256)), P, keys // page, P, P, 1, r(_heads(qb)), 3,
+                                             1.0, 1, 0, r(_heads(qb)), None, None, 0, None)
+        assert got == want, (page, keys)
