@@ -36,7 +36,6 @@ constexpr float PA_LN2 = 0.69314718055994530942f;
 struct PaParams {
   AttnCall c;
   float scale2;         // scale * log2 e
-  int min_units;        // key tiles per share below which fewer shares are made
   uint32_t div_page, div_group;   // 2^32 / divisor, rounded up (fast_div)
   uint32_t* counters;   // [grid] zeroed before the launch
   float* part_o;        // [2 * grid][ROWS][DP]
@@ -64,10 +63,7 @@ __device__ __forceinline__ PaRange pa_range(const PaParams& p, const ReqView& r,
   k.all_hi = attn_hi(c, r.kv, r.kv - r.n + i0);
   return k;
 }
-template <int ROWS>
-__device__ __forceinline__ bool pa_mine(const PaParams& p, const ReqView& r) {
-  return r.n > 0;
-}
+__device__ __forceinline__ bool pa_mine(const ReqView& r) { return r.n > 0; }
 template <int ROWS>
 __device__ __forceinline__ int pa_row_tiles(const PaParams& p, const ReqView& r) { return (r.n * p.c.G + ROWS - 1) / ROWS; }
 // key tiles of one key head of a request
@@ -93,7 +89,7 @@ struct PaCursor {
       rt = 0;
       if (++h == p.c.cache.kv_heads) {
         h = 0;
-        do { ++b; if (b >= p.c.B) return; r = attn_request(p.c, b); } while (!pa_mine<ROWS>(p, r));
+        do { ++b; if (b >= p.c.B) return; r = attn_request(p.c, b); } while (!pa_mine(r));
         nrt = pa_row_tiles<ROWS>(p, r);
       }
     }
@@ -132,7 +128,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
   long long mine = 0;
   for (int b = b_lo; b < b_hi; ++b) {
     const ReqView r = attn_request(c, b);
-    if (pa_mine<ROWS>(p, r)) mine += (long long)pa_head_units<ROWS>(p, r) * c.cache.kv_heads;
+    if (pa_mine(r)) mine += (long long)pa_head_units<ROWS>(p, r) * c.cache.kv_heads;
   }
   long long incl = mine;
 #pragma unroll
@@ -149,7 +145,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
     total += s_scan[w];
   }
   incl += before;
-  const long long shares = min((long long)gridDim.x, max(1LL, total / p.min_units));
+  const long long shares = min((long long)gridDim.x, max(1LL, total));
   if ((long long)blockIdx.x >= shares) return;
   const long long u0 = total * blockIdx.x / shares, u1 = total * (blockIdx.x + 1) / shares;
   if (u0 >= u1) return;
@@ -158,7 +154,7 @@ __global__ void __launch_bounds__(PA_THREADS) paged_attention_kernel(const __gri
     int b = b_lo;
     for (;; ++b) {
       const ReqView r = attn_request(c, b);
-      if (!pa_mine<ROWS>(p, r)) continue;
+      if (!pa_mine(r)) continue;
       const long long n = (long long)pa_head_units<ROWS>(p, r) * c.cache.kv_heads;
       if (u0 < u + n) break;
       u += n;
@@ -537,7 +533,6 @@ int launch_paged_attention(const AttnCall& c, char* counters, char* scratch, cud
   PaParams p{};
   p.c = c;
   p.scale2 = c.scale * 1.4426950408889634f;
-  p.min_units = 1;
   p.div_page = fast_div_magic((uint32_t)c.cache.page_size);
   p.div_group = fast_div_magic((uint32_t)c.G);
   const int wr = pa_row_form(c);
