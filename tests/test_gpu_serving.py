@@ -846,3 +846,30 @@ def test_attention_widest_windows(monkeypatch, window):
             _attend(new, kv, 4, 2, 40, causal=causal, window=window)
     monkeypatch.setenv("QBLORA_FORCE_GENERAL", "1")
     _attend([6], [2], 4, 2, 64, causal=False, window=window)
+
+
+@pytest.mark.parametrize("B", [257, 300, 385, 500, 1024, 1025, 1500])
+@pytest.mark.parametrize("D,H,Hkv,window", [(64, 4, 2, 0), (128, 3, 1, 25)])
+def test_attention_calls_of_many_requests(B, D, H, Hkv, window):
+    # more requests than a CTA has threads (256 in the line form, 384 in the tcgen05 form), than the tcgen05 form lists (1024); with
+    # and without prompts among them
+    kv = [(37 * b) % 150 for b in range(B)]
+    new = [min(b % 4, kv[b]) for b in range(B)]
+    _attend(new, kv, H, Hkv, D, window=window, seed=B)
+    for b, n in ((B // 2, 150), (B - 2, 400), (3, 40)):
+        new[b], kv[b] = n, n + 70 * (b % 3)
+    _attend(new, kv, H, Hkv, D, window=window, seed=B + 1)
+    new = [max(1, b % 23) for b in range(B)] if B <= 500 else new                      # and many of either kind
+    _attend(new, [n + 30 for n in new], H, Hkv, D, page=32, window=window, seed=B + 2)
+
+
+def test_the_serving_example_runs():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    cmd = [sys.executable, os.path.join(root, "examples", "serve_layer.py"), "--hidden", "512", "--heads", "8", "--kv-heads", "2",
+           "--dim", "64", "--prompts", "70,3,130", "--steps", "6"]
+    done = subprocess.run(cmd, capture_output=True, text=True, timeout=240, cwd=root)
+    assert done.returncode == 0, done.stderr[-2000:]
+    assert "[75, 8, 135] cached tokens" in done.stdout
