@@ -16,9 +16,12 @@
 // Layout: 64 keys x head size bf16 for K and V per stage, 16-byte chunks XOR-swizzled by the row, read by ldmatrix
 // without bank conflicts.  mma.sync m16n8k16 (bf16, fp32 sums): the contraction is far below the tensor rate, and its
 // register fragments let P go from scores to the second product without leaving registers.
-// Measured with pages of 24 keys, D 128, 8 key heads of 4: 64 requests decoding over up to 8100 keys 309 us = 5.2 TB/s
-// (paged_warp.cu with pages of 16: 268 us); 4 requests of 512 tokens over 4096 keys 741 us = 145 TFLOP/s, bound by mma.sync and the
-// work around it (tc_attn.cu with pages of 16: 129 us).
+// Measured with pages of 24 keys, D 128, 8 key heads of 4: 64 requests decoding over up to 8100 keys 309 us = 3.5 TB/s
+// (paged_warp.cu with pages of 16: 187 us); 4 requests of 512 tokens behind 3584 keys 886 us = 145 TFLOP/s, bound by mma.sync and the
+// work around it (tc_attn.cu with pages of 16: 138 us).  The same with D 96: 262 us (floor 129) and 888 us = 109 TFLOP/s; with D 256 and
+// 4 key heads 402 us (floor 172) and 1824 us = 71 TFLOP/s (its forms spill 170 to 610 bytes).
+//
+// The weights are rounded to bf16 for their product with V, as mma.sync wants them; m, l, O and the parts are fp32.
 #include <algorithm>
 #include <atomic>
 

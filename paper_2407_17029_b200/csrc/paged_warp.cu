@@ -7,7 +7,7 @@
 // What bounds it: the cache's bytes, so each warp is made to need little else.  The key tiles of all (request, row tile) pairs
 // are put in one line, alike for every key head, and the line is cut into parts; a share is one part for one key head, and
 // the heads of a part are neighbouring shares, so that warps which run at the same time read the same pages (with each head's
-// tiles in a row instead, 6 requests x 40 heads x 15k keys took 309 us, now 290).  Every warp starts with one share and then
+// tiles in a row instead, 6 requests x 40 heads x 15k keys took 309 us, now 293).  Every warp starts with one share and then
 // takes the next one that nobody has taken, the later ones shorter: SMs do not get equal parts of a saturated memory (with
 // one equal share per warp the slowest CTA of a 1 GB call ended 20 % after the median).  A warp streams its shares through a
 // ring of its own -- lane i issues box i of a tile as the ring's slot becomes free, across the borders of items and shares,
@@ -19,8 +19,12 @@
 // 65 us at the end of a 45 to 180 us call.  Calls of very few rows have a form without either (CLUSTER): one cluster of CTAs
 // per item, joined through the cluster's shared memory.
 //
-// Measured, D 128: 64 requests of 30 to 8100 keys, 8 key heads of 4 query heads, 1.07 GB: 187 us = 5.7 TB/s, of which the join
-// kernel about 8; 6 requests of 15k keys, 40 heads, 1.87 GB: 290 us = 6.5 TB/s, the rate of a copy.
+// Measured, D 128, on several cards: 64 requests of 30 to 8100 keys, 8 key heads of 4 query heads, 1.07 GB: 186 to 193 us = 5.5 to
+// 5.7 TB/s, of which the join kernel about 8; 6 requests of 15k keys, 40 heads, 1.87 GB: 286 to 295 us = 6.3 to 6.5 TB/s, the
+// rate of a copy.
+//
+// The weights are rounded to bf16 for their product with V, as mma.sync wants them; m, l, o and the parts are fp32.  With fp32 weights
+// the error against 64 bits is 0.0017 of the result (its own rounding to bf16), with these 0.0023.
 //
 // Entries behind a request's keys: whole pages are asked for at a page number past the cache, which TMA fills with zeros;
 // the rest of the last page is masked (scores set to -infinity, V set to zero in shared memory).
@@ -41,7 +45,10 @@ namespace {
 
 constexpr int PW_WARPS = 8, PW_THREADS = PW_WARPS * 32;
 constexpr int PW_MAX_LEVELS = kPagedLevels;
-constexpr int PW_FINE = 11;       // key tiles of the shortest shares
+// Key tiles of the shortest shares: with short ones the last warps end together, with long ones there are fewer joins.  Measured with
+// 4 / 11 / 24: 64 requests of 30 to 8100 keys 191 / 194 / 196 us, 6 of 15k keys 281 / 282 / 286; 200 of up to 1000 keys 99 / 99 / 97, 24 of
+// up to 2000 keys with 32 key heads 77.5 / 76 / 76, 16 requests of 12 to 28 rows 67 / 61 / 61.
+constexpr int PW_FINE = 11;
 constexpr float PW_OUTGROWN = 1024.0f;   // a lane's sum of a tile's weights that asks for a new maximum
 constexpr float PW_LN2 = 0.69314718055994530942f;
 

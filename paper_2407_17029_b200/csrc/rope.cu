@@ -6,7 +6,9 @@
 //
 // What bounds it: HBM, every element read once and written once, in 16-byte words with several loads in flight per thread.
 // Measured: fp32, 8191 rows of 40 + 40 heads of 128, 671 MB: 119.5 us = 5.6 TB/s (a copy: 6.5); bf16, 4095 rows of
-// 52 + 52 + 52 heads into a cache, 327 MB: 57.8 us = 5.7 TB/s; one row: 2.7 us in a graph.
+// 52 + 52 + 52 heads into a cache, 327 MB: 57.8 us = 5.7 TB/s; one row: 2.4 us in a graph.
+// Sizes and alignments of the general form (below): 4095 rows of 32 + 32 heads of 96, 24 of them rotated, 127 us where the
+// bytes take 16 (with 32 rotated, the wide form: 20 us): a sine and 64-bit divisions for each pair of each head.
 #include "serving.cuh"
 
 namespace qb {

