@@ -253,7 +253,6 @@ lowbit_gemv_t1_kernel(const __grid_constant__ CUtensorMap tm_c, const __grid_con
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    if (blockIdx.x == 0) *p.status = 0;   // any give-up below is written at least a wait limit later
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), GT_WARPS); }
     mbar_init(red_done, GT_WARPS);
     mbar_init(red_free, 1);
@@ -292,8 +291,10 @@ lowbit_gemv_t1_kernel(const __grid_constant__ CUtensorMap tm_c, const __grid_con
     const int g = lane >> 2, tg = lane & 3;
     // The weights are constants, x and Y are not: in a chain of launches (one decode step) this kernel may
     // have been started before its predecessor finished (programmatic dependent launch), so the producer
-    // streams weights at once while everything that reads x or writes results waits here.
+    // streams weights at once while everything that reads x or writes memory waits here (the status word too:
+    // its place may be what the kernels in front still read).  A give-up is written at least a wait limit later.
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (blockIdx.x == 0 && tid == 0) *p.status = 0;
     // ---- once per CTA, while the first tiles are in flight: fragments and group sums of x.
     // Item = (group, tg): 16 values of x; the four tg lanes of an item are neighbours.  Every group's
     // 64 values get their own power-of-two prescale 2^-e (max |x| 2^-e in [2^14, 2^15)), so no pass over
@@ -606,7 +607,6 @@ lowbit_gemv_ko_kernel(const __grid_constant__ CUtensorMap tm_c, const __grid_con
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   if (tid == 0) {
-    if (blockIdx.x == 0) *p.status = 0;   // any give-up below is written at least a wait limit later
     for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), GT_WARPS); }
     mbar_init(red_done, GT_WARPS);
     mbar_init(red_free, p.T);
@@ -653,6 +653,7 @@ lowbit_gemv_ko_kernel(const __grid_constant__ CUtensorMap tm_c, const __grid_con
     // ------------------------------------------------------------------ fragment loader (one lane)
     if (lane == 0) {
       asm volatile("griddepcontrol.wait;" ::: "memory");   // the fragments are complete and visible
+      if (blockIdx.x == 0) *p.status = 0;   // not before: its place may be what the kernels in front still read
       uint32_t xit = 0;
       bool ok = true;
       for (int pass = 0; pass < n_pass && ok; ++pass) {

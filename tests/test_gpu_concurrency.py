@@ -101,3 +101,30 @@ def test_two_host_threads_on_their_own_streams():
     for t in threads:
         t.join()
     assert not errors, errors
+
+
+@pytest.mark.parametrize("tokens", [1, 4])
+def test_decode_products_write_nothing_before_the_kernels_in_front_have_ended(tokens):
+    # Decode products are chained: each may start while the ones in front of it still run.  In stream order it is fine to use the
+    # input of one as the workspace of the next, so the next may write its status word only when the one in front has ended,
+    # which here waits for a large product in front of it in turn.
+    from paper_2407_17029_b200 import binding as qb
+    dev = torch.device("cuda", 0)
+    g = torch.Generator(device=dev).manual_seed(5)
+    make = lambda o, i: qb.quantize_blockwise(torch.randn(o, i, device=dev, generator=g) * 0.02, 64, 1, qb.FMT_AFFINE_MINMAX)  # noqa: E731
+    large, first, second = make(8192, 8192), make(512, 32768), make(128, 256)
+    xl = torch.randn(1, 8192, device=dev, generator=g).to(torch.bfloat16)
+    x0 = torch.randn(tokens, 32768, device=dev, generator=g).to(torch.bfloat16)
+    x2 = torch.randn(tokens, 256, device=dev, generator=g).to(torch.bfloat16)
+    wl = qb.alloc_workspace(qb.OP_LOWBIT_GEMM, large, None, 1)
+    w1 = qb.alloc_workspace(qb.OP_LOWBIT_GEMM, first, None, tokens)
+    w2 = torch.empty(max(2 * x0.numel(), qb.workspace_bytes(qb.OP_LOWBIT_GEMM, second, None, tokens)), dtype=torch.uint8, device=dev)
+    x = w2[:2 * x0.numel()].view(torch.bfloat16).view_as(x0)
+    want, want2 = qb.lowbit_gemm(first, x0, torch.float32, ws=w1), qb.lowbit_gemm(second, x2, torch.float32)
+    for _ in range(100):
+        x.copy_(x0)
+        qb.lowbit_gemm(large, xl, ws=wl)
+        got = qb.lowbit_gemm(first, x, torch.float32, ws=w1)
+        got2 = qb.lowbit_gemm(second, x2, torch.float32, ws=w2)
+        assert torch.equal(got, want) and torch.equal(got2, want2)
+    assert qb.device_status(w2) == qb.OK and qb.device_status(w1) == qb.OK
