@@ -462,6 +462,126 @@ int qblora_paged_attention(const qblora_kv_cache* cache, const int32_t* block_ta
                            int causal, int32_t window, const qblora_heads* out, float* lse, void* ws, size_t ws_bytes,
                            void* stream);
 
+/* =====================================================================================================================
+ * Many adapters over one frozen weight.  The paper trains and merges one adapter per weight (Sec. 3.2, 3.3); the calls
+ * below serve and train a bank of them beside the same weight: every request (or training sequence) names its own adapter,
+ * and one AdamW step updates them all.
+ *
+ * Notation.  Request b has the rows cu[b] .. cu[b + 1] - 1 of X and Y and uses adapter ids[b] of the bank, or none.
+ * P = d_in / lambda_in, Q = d_out / lambda_out, x' as in qblora_linear_fwd (AvgPool & repeat_interleave; lambda = 1 on both
+ * sides is the unpooled low-rank adapter).
+ * ===================================================================================================================== */
+
+/* n_adapters adapters of one linear layer, one slot each.  An adapter of a lower rank has zeros in the columns of A and the
+ * rows of B behind it; `ranks` then only saves the work on them (columns and rows from ranks[a], rounded up to a multiple of
+ * 16, on are not read). */
+typedef struct {
+  int32_t d_in, d_out;           /* of the layer */
+  int32_t lambda_in, lambda_out;
+  int32_t n_adapters, rank;      /* rank: of the slots */
+  const void* A;                 /* DEVICE bf16 [n_adapters][P][rank] */
+  const void* B;                 /* DEVICE bf16 [n_adapters][rank][Q] */
+  const float* scaling;          /* DEVICE [n_adapters]: s of each adapter */
+  const int32_t* ranks;          /* DEVICE [n_adapters], clamped to 0 .. rank; NULL = all `rank` */
+} qblora_adapter_bank;
+
+/*
+ * Rows of one step sorted by adapter: rows[start[a]] .. rows[start[a + 1] - 1] are the rows of all requests that use adapter a,
+ * in rising order; the entries of `rows` from start[n_adapters] on are -1.
+ *   cu [n_requests + 1] (rising), ids [n_requests]: DEVICE int32; an id outside 0 .. n_adapters - 1 (usually -1) means none.
+ *   rows [tokens], start [n_adapters + 1]: DEVICE int32 out, outside cu and ids.  tokens: rows of the step's buffers; offsets are
+ *   clamped to it.
+ * Once per step: every layer's calls read the same plan.  One launch, nothing is synchronised.
+ * 1 <= n_requests <= 8192 and 1 <= n_adapters <= 4096, else QBLORA_ERR_UNSUPPORTED.
+ */
+int qblora_adapter_plan(const int32_t* cu, const int32_t* ids, int32_t n_requests, int32_t n_adapters, int64_t tokens,
+                        int32_t* rows, int32_t* start, void* stream);
+
+/*
+ * The adapters' term, added to what the shared projection (qblora_linear_fwd without adapter, qablora_lowbit_gemm,
+ * qblora_dense_gemm) has written: for every row t of adapter a in the plan
+ *   Y[t][o] += scaling[a] * ((x'_t A_a) B_a)[o / lambda_out],
+ * formed in fp32 and rounded once.  Rows that are not in the plan are left as they were.
+ *   rows [tokens], start [n_adapters + 1]: DEVICE int32, as written by qblora_adapter_plan (each row at most once; entries out of
+ *   range are passed over).  X DEVICE bf16, x_stride elements between rows; Y DEVICE bf16 or fp32 (y_dtype), y_stride likewise;
+ *   X and Y do not overlap.  x' and x' A are carried as pairs of bf16 numbers, within 2^-16.
+ * Any sizes; rank and Q multiples of 8, rank <= 256, d_in, d_out and the strides multiples of 8 and all tensors 16-byte
+ * aligned take the fast kernels.
+ *   ws: qblora_adapters_workspace_bytes(bank, tokens, 0) bytes.
+ */
+size_t qblora_adapters_workspace_bytes(const qblora_adapter_bank* bank, int64_t tokens, int backward);
+int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, const int32_t* start, const void* X,
+                        int64_t x_stride, int64_t tokens, void* Y, int64_t y_stride, int y_dtype, void* ws, size_t ws_bytes,
+                        void* stream);
+
+/*
+ * Its backward pass.  With dv_t = scaling[a] * (sums of lambda_out neighbours of dY_t), du_t = dv_t B_a^T, u_t = x'_t A_a:
+ *   dX[t][i] += (du_t A_a^T)[i / lambda_in] / lambda_in        (on what the shared projection's backward pass has written)
+ *   dA[a] = sum over its rows of x'_t^T du_t,   dB[a] = sum of u_t^T dv_t      (fp32 [n][P][rank], [n][rank][Q])
+ * dA and dB are written whole: zeros for adapters without rows, and from ranks[a] (rounded up to 16) on.  Rows of dX that are
+ * not in the plan are left as they were.  Any of dX, dA, dB may be NULL (skipped).
+ *   dY DEVICE bf16, dX DEVICE bf16 or fp32 (dx_dtype); strides in elements.  X is not needed (may be NULL) without dA and dB.
+ *   ws: qblora_adapters_workspace_bytes(bank, tokens, 1) bytes.  Sums run in a fixed order: equal inputs, equal bits.
+ */
+int qblora_adapters_bwd(const qblora_adapter_bank* bank, const int32_t* rows, const int32_t* start, const void* X,
+                        int64_t x_stride, const void* dY, int64_t dy_stride, int64_t tokens, void* dX, int64_t dx_stride,
+                        int dx_dtype, float* dA, float* dB, void* ws, size_t ws_bytes, void* stream);
+
+/* One trained tensor of an AdamW step (all pointers DEVICE, n elements, contiguous). */
+typedef struct {
+  float* p;                 /* the parameter in 32 bits, updated */
+  const void* g;            /* its gradient, g_dtype F32 or BF16 */
+  void* copy;               /* bf16 copy of the updated parameter (what the layer reads); NULL to leave out */
+  void* m;                  /* first average:  fp32, or uint8 codes */
+  void* v;                  /* second average: fp32, or uint8 codes of its square root */
+  float* m_scale;           /* 8-bit states: one scale per 256 elements, [(n + 255) / 256]; else NULL */
+  float* v_scale;
+  int64_t n;
+  int32_t g_dtype;          /* qblora_dtype */
+  int32_t state_bits;       /* 32 or 8 */
+  float lr_mult;            /* multiplies the learning rate */
+  float weight_decay;
+} qblora_adamw_tensor;
+
+typedef struct {
+  const float* lr;          /* DEVICE [1]: learning rate, so that a captured step can follow a schedule */
+  int32_t* steps;           /* DEVICE [1]: steps taken so far (>= 0); the call adds one */
+  double beta1, beta2;      /* 0 <= beta < 1 */
+  double eps;               /* >= 0 */
+  float max_norm;           /* > 0: gradients are scaled by min(1, max_norm / norm); 0: not */
+  uint32_t seed;            /* of the rounding of 8-bit states */
+  float* norm;              /* DEVICE out [1]: the gradients' global 2-norm; NULL: only formed where max_norm asks for it */
+} qblora_adamw_cfg;
+
+/*
+ * AdamW over many tensors at once.  With g~ = min(1, max_norm / norm) g and t = steps + 1, for every element of every tensor
+ *   m = beta1 m + (1 - beta1) g~;   v = beta2 v + (1 - beta2) g~^2;
+ *   p = p - lr lr_mult (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p);   copy = bf16(p).
+ * Everything is formed in fp32 from the stored states; the update uses m and v before they are stored again.
+ *
+ * States in 8 bits: m and r = sqrt(v) are held as e4m3 codes (sign, 4 exponent bits with bias 7, 3 mantissa bits; the largest
+ * number is 448) times one fp32 scale per block of 256 consecutive elements, scale = (largest |m| of the block) / 448.  A value
+ * is rounded to one of its two neighbours by chance, with the probabilities that keep its expected value: v moves by a thousandth of
+ * itself per step at beta2 = 0.999, which rounding to nearest would undo every time.  The chance is a hash: element i of a tensor is
+ * number e = 256 * (blocks of the tensors in front of it) + i of the call, and with mix(x): x ^= x >> 16, x *= 0xA3C59AC3,
+ * x ^= x >> 15, x *= 0x5D8E3B97, x ^= x >> 16 (32 bits), h = mix(e * 0x9E3779B1 + mix(mix(seed) + t)); the low 16 bits of h
+ * belong to m, the high ones to r: the neighbour further from zero is taken if the fraction of the way to it plus bits / 65536 is
+ * at least 1.  Equal inputs give equal bits.  States that are not finite are held as NaN and do not count for the scale; a block
+ * whose largest value is below 2^-118 is held as zeros.
+ *
+ * The norm is summed over the gradients of all tensors in the call (blocks of squares in fp32, their sum in fp64, in a fixed
+ * order).  Where it is formed and is not finite, the step is left out: nothing but *norm is written.
+ *
+ * qblora_adamw_prepare lays the tensors' table into ws and returns in *blocks the number that the step wants; ws then belongs to
+ * these tensors (their addresses, not their values) until it is prepared again.  At most 65536 tensors, 2^31 - 1 blocks.
+ * No tensor may overlap another.  qblora_adamw_step may be captured in a graph: lr, steps and the gradients' values are
+ * read when it runs.  Two steps over one ws run one after the other.
+ */
+size_t qblora_adamw_workspace_bytes(int32_t n_tensors);
+int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, void* ws, size_t ws_bytes, int64_t* blocks,
+                         void* stream);
+int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t blocks, void* ws, size_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

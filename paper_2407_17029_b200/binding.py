@@ -36,7 +36,9 @@ EXPORTS = ["qblora_default_code_table", "qblora_workspace_bytes", "qblora_status
            "qblora_set_timing_events", "qablora_merge_noalloc", "qblora_merge_dense",
            "qblora_quantize_minmax_nbit", "qblora_debug_set_wait_limit", "qblora_debug_drop_load", "qblora_debug_hold_producer", "qblora_dense_gemm", "qblora_pack_codes", "qblora_unpack_codes",
            "qblora_rope_table", "qblora_rope", "qblora_rope_append", "qblora_kv_plan", "qblora_attention_workspace_bytes",
-           "qblora_paged_attention"]
+           "qblora_paged_attention",
+           "qblora_adapter_plan", "qblora_adapters_workspace_bytes", "qblora_adapters_fwd", "qblora_adapters_bwd",
+           "qblora_adamw_workspace_bytes", "qblora_adamw_prepare", "qblora_adamw_step"]
 
 
 class _CQWeight(ctypes.Structure):
@@ -67,6 +69,24 @@ class _CKVCache(ctypes.Structure):
 class _CRope(ctypes.Structure):
     _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
                 ("amplitude", ctypes.c_float), ("turns", ctypes.c_void_p)]
+
+
+class _CAdapterBank(ctypes.Structure):
+    _fields_ = [("d_in", ctypes.c_int32), ("d_out", ctypes.c_int32), ("lambda_in", ctypes.c_int32), ("lambda_out", ctypes.c_int32),
+                ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("A", ctypes.c_void_p), ("B", ctypes.c_void_p),
+                ("scaling", ctypes.c_void_p), ("ranks", ctypes.c_void_p)]
+
+
+class _CAdamWTensor(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_void_p), ("g", ctypes.c_void_p), ("copy", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("n", ctypes.c_int64),
+                ("g_dtype", ctypes.c_int32), ("state_bits", ctypes.c_int32), ("lr_mult", ctypes.c_float),
+                ("weight_decay", ctypes.c_float)]
+
+
+class _CAdamWCfg(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_void_p), ("steps", ctypes.c_void_p), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("max_norm", ctypes.c_float), ("seed", ctypes.c_uint32), ("norm", ctypes.c_void_p)]
 
 
 if not os.path.exists(LIB_PATH):
@@ -121,6 +141,15 @@ _lib.qblora_attention_workspace_bytes.restype = _sz
 _lib.qblora_attention_workspace_bytes.argtypes = [_vp, _i32, _i64]
 _lib.qblora_paged_attention.argtypes = [_vp, _vp, _i32, _vp, _vp, _i32, _vp, _i64, ctypes.c_float, ctypes.c_int, _i32, _vp,
                                         _vp, _vp, _sz, _vp]
+_lib.qblora_adapter_plan.argtypes = [_vp, _vp, _i32, _i32, _i64, _vp, _vp, _vp]
+_lib.qblora_adapters_workspace_bytes.restype = _sz
+_lib.qblora_adapters_workspace_bytes.argtypes = [_vp, _i64, ctypes.c_int]
+_lib.qblora_adapters_fwd.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _vp, _i64, ctypes.c_int, _vp, _sz, _vp]
+_lib.qblora_adapters_bwd.argtypes = [_vp, _vp, _vp, _vp, _i64, _vp, _i64, _i64, _vp, _i64, ctypes.c_int, _vp, _vp, _vp, _sz, _vp]
+_lib.qblora_adamw_workspace_bytes.restype = _sz
+_lib.qblora_adamw_workspace_bytes.argtypes = [_i32]
+_lib.qblora_adamw_prepare.argtypes = [_vp, _i32, _vp, _sz, _vp, _vp]
+_lib.qblora_adamw_step.argtypes = [_vp, _i32, _i64, _vp, _sz, _vp]
 
 
 def kernel_launches() -> int:
@@ -638,3 +667,229 @@ def paged_attention(q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, 
     if st != OK:
         _check(st, "qblora_paged_attention")
     return out, lse
+
+
+# ------------------------------------------------------------------------------------ many adapters over one frozen weight
+@dataclass
+class AdapterBank:
+    """Adapters of one layer, a slot each: A bf16 [n][P][rank], B bf16 [n][rank][Q], scaling fp32 [n] (device, contiguous).
+    An adapter of a lower rank has zeros behind it; `ranks` (int32 [n]) saves the work on them."""
+    d_in: int
+    d_out: int
+    lambda_in: int
+    lambda_out: int
+    A: torch.Tensor
+    B: torch.Tensor
+    scaling: torch.Tensor
+    ranks: Optional[torch.Tensor] = None
+
+    def c_struct(self) -> _CAdapterBank:
+        A, B, s, k = self.A, self.B, self.scaling, self.ranks
+        if self.lambda_in < 1 or self.lambda_out < 1 or A.dim() != 3:
+            raise ValueError("lambda_in, lambda_out >= 1; A: [n][d_in / lambda_in][rank]")
+        n, P, r = A.shape
+        if P * self.lambda_in != self.d_in or tuple(B.shape) != (n, r, self.d_out // self.lambda_out) or B.shape[2] * self.lambda_out != self.d_out:
+            raise ValueError("A: [n][d_in / lambda_in][rank], B: [n][rank][d_out / lambda_out]")
+        if A.dtype is not torch.bfloat16 or B.dtype is not torch.bfloat16 or not (A.is_contiguous() and B.is_contiguous() and A.is_cuda and B.is_cuda):
+            raise ValueError("A, B: contiguous bf16 device tensors")
+        if s.dtype is not torch.float32 or s.numel() != n or not s.is_contiguous() or not s.is_cuda:
+            raise ValueError("scaling: contiguous fp32 device tensor [n]")
+        return _CAdapterBank(self.d_in, self.d_out, self.lambda_in, self.lambda_out, n, r, A.data_ptr(), B.data_ptr(), s.data_ptr(),
+                             None if k is None else _ints(k, n, "ranks"))
+
+
+@dataclass
+class AdapterPlan:
+    """Rows of a step sorted by adapter (int32, device); see qblora_adapter_plan."""
+    rows: torch.Tensor               # [tokens] row numbers, -1 behind the last one
+    start: torch.Tensor              # [n_adapters + 1] first entry of each adapter
+
+
+def adapter_plan(cu_rows: torch.Tensor, adapter_ids: torch.Tensor, n_adapters: int, tokens: int, outs: Optional[Tuple] = None,
+                 stream=None) -> AdapterPlan:
+    """qblora_adapter_plan: request b has the rows cu_rows[b] .. cu_rows[b + 1] - 1 and uses adapter_ids[b] (-1: none).
+    `tokens`: rows of the step's buffers.  `outs`: preallocated (rows, start)."""
+    B = adapter_ids.numel()
+    rows, start = outs if outs is not None else (_empty(n, torch.int32, adapter_ids.device, stream) for n in (tokens, n_adapters + 1))
+    st = _lib.qblora_adapter_plan(_ints(cu_rows, B + 1, "cu_rows"), _ints(adapter_ids, B, "adapter_ids"), B, n_adapters, tokens,
+                                  _ints(rows, tokens, "rows"), _ints(start, n_adapters + 1, "start"), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_adapter_plan")
+    return AdapterPlan(rows, start)
+
+
+def _rows(t: torch.Tensor, tokens: int, width: int, name: str, dtypes=(torch.bfloat16,)) -> int:
+    """Checks a [tokens][width] tensor with contiguous rows; returns its row stride."""
+    if t.dim() != 2 or t.shape[0] != tokens or t.shape[1] != width or not t.is_cuda or t.dtype not in dtypes:
+        raise ValueError(f"{name}: [{tokens}][{width}] device tensor of {' or '.join(str(d) for d in dtypes)}")
+    if (t.stride(1) != 1 and width > 1) or (t.stride(0) < width and tokens > 1):
+        raise ValueError(f"{name}: rows are contiguous and do not overlap")
+    return max(t.stride(0), width)
+
+
+def adapters_workspace_bytes(bank: AdapterBank, tokens: int, backward: bool = False) -> int:
+    return int(_lib.qblora_adapters_workspace_bytes(ctypes.byref(bank.c_struct()), tokens, bool(backward)))
+
+
+def alloc_adapters_workspace(bank: AdapterBank, tokens: int, backward: bool = False, stream=None) -> torch.Tensor:
+    """Workspace for adapters_fwd (or adapters_bwd) calls (on `stream`) with banks of this size and up to `tokens` rows."""
+    return _empty(max(adapters_workspace_bytes(bank, max(tokens, 1), backward), 256), torch.uint8, bank.A.device, stream)
+
+
+def _workspace(ws: torch.Tensor) -> torch.Tensor:
+    if not ws.is_cuda or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws: contiguous uint8 device tensor")
+    return ws
+
+
+def adapters_fwd(bank: AdapterBank, plan: AdapterPlan, X: torch.Tensor, Y: torch.Tensor, ws: Optional[torch.Tensor] = None,
+                 stream=None) -> torch.Tensor:
+    """qblora_adapters_fwd: adds every planned row's adapter term to Y [tokens][d_out] (bf16 or fp32, what the shared
+    projection of X has written) in place; returns Y."""
+    T = X.shape[0]
+    xs = _rows(X, T, bank.d_in, "X")
+    ys = _rows(Y, T, bank.d_out, "Y", (torch.bfloat16, torch.float32))
+    c = bank.c_struct()
+    if T == 0:
+        return Y
+    ws = alloc_adapters_workspace(bank, T, stream=stream) if ws is None else _workspace(ws)
+    st = _lib.qblora_adapters_fwd(ctypes.byref(c), _ints(plan.rows, T, "rows"), _ints(plan.start, c.n_adapters + 1, "start"), X.data_ptr(),
+                                  xs, T, Y.data_ptr(), ys, _dt(Y.dtype), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_adapters_fwd")
+    return Y
+
+
+def adapters_bwd(bank: AdapterBank, plan: AdapterPlan, X: Optional[torch.Tensor], dY: torch.Tensor, dX: Optional[torch.Tensor] = None,
+                 need_da: bool = True, need_db: bool = True, outs: Optional[Tuple] = None, ws: Optional[torch.Tensor] = None,
+                 stream=None):
+    """qblora_adapters_bwd: adds the adapters' part to dX [tokens][d_in] (bf16 or fp32, what the shared projection's backward
+    pass has written; None: not wanted) in place and returns (dX, dA, dB), dA and dB fp32 of the shapes of A and B.
+    `outs`: preallocated (dA, dB), entries None where not wanted."""
+    T = dY.shape[0]
+    ds = _rows(dY, T, bank.d_out, "dY")
+    c = bank.c_struct()
+    if outs is not None:
+        dA, dB = outs
+        for g, like, name in ((dA, bank.A, "dA"), (dB, bank.B, "dB")):
+            if g is not None and (g.shape != like.shape or g.dtype is not torch.float32 or not g.is_contiguous() or not g.is_cuda):
+                raise ValueError(f"{name}: contiguous fp32 device tensor of the shape of {name[1]}")
+    else:
+        dA = _empty(bank.A.shape, torch.float32, dY.device, stream) if need_da else None
+        dB = _empty(bank.B.shape, torch.float32, dY.device, stream) if need_db else None
+    gs = _rows(dX, T, bank.d_in, "dX", (torch.bfloat16, torch.float32)) if dX is not None else 0
+    xs = _rows(X, T, bank.d_in, "X") if X is not None else 0
+    if T == 0:
+        for g in (dA, dB):
+            if g is not None:
+                _zero(g, stream)
+        return dX, dA, dB
+    ws = alloc_adapters_workspace(bank, T, backward=True, stream=stream) if ws is None else _workspace(ws)
+    p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    st = _lib.qblora_adapters_bwd(ctypes.byref(c), _ints(plan.rows, T, "rows"), _ints(plan.start, c.n_adapters + 1, "start"), p(X), xs,
+                                  dY.data_ptr(), ds, T, p(dX), gs, _dt(dX.dtype) if dX is not None else BF16, p(dA), p(dB),
+                                  ws.data_ptr(), ws.numel(), _stream_ptr(stream))
+    if st != OK:
+        _check(st, "qblora_adapters_bwd")
+    return dX, dA, dB
+
+
+def _zero(t: torch.Tensor, stream) -> None:
+    if stream is None:
+        t.zero_()
+    else:
+        with torch.cuda.stream(stream):
+            t.zero_()
+
+
+class AdamW:
+    """qblora_adamw_step over a list of tensors; the table of their addresses is made here, once.
+
+    params fp32, grads fp32 or bf16, copies (optional) bf16: lists of contiguous device tensors of equal sizes; an entry of copies may
+    be None.  state_bits 32 or 8 (or a list): states m, v are fp32 tensors, or float8_e4m3fn codes of the first average and of
+    the second one's square root with one fp32 scale per 256 elements in m_scale, v_scale.  They start at zero; `states` takes
+    kept ones (a dict of lists with these names), `steps` a kept count (int32 [1], device).  lr: a number, or an fp32 device tensor [1]
+    that a schedule writes; lr_mult and weight_decay: numbers or lists.  max_norm > 0 clips by the global norm, need_norm asks
+    for it alone (self.norm, fp32 [1])."""
+
+    def __init__(self, params, grads, copies=None, state_bits=32, states=None, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay=0.0, lr_mult=1.0, max_norm: float = 0.0, need_norm: bool = False, seed: int = 0, steps=None, stream=None):
+        n = len(params)
+        if n < 1 or len(grads) != n or (copies is not None and len(copies) != n):
+            raise ValueError("params, grads, copies: lists of equal length, at least one tensor")
+        each = lambda x: list(x) if isinstance(x, (list, tuple)) else [x] * n  # noqa: E731
+        bits, decay, mult = each(state_bits), each(weight_decay), each(lr_mult)
+        if len(bits) != n or len(decay) != n or len(mult) != n or any(b not in (8, 32) for b in bits):
+            raise ValueError("state_bits (8 or 32), weight_decay, lr_mult: a value, or a list with one for each tensor")
+        self.device = params[0].device
+        self.params, self.grads, self.copies = list(params), list(grads), list(copies) if copies is not None else [None] * n
+        new = lambda shape, dtype: _zeros(shape, dtype, self.device, stream)  # noqa: E731
+        blocks = [(p.numel() + 255) // 256 for p in self.params]
+        states = states or {}
+        make = {"m": lambda k: new(self.params[k].shape, torch.float32 if bits[k] == 32 else torch.float8_e4m3fn),
+                "m_scale": lambda k: new((blocks[k],), torch.float32) if bits[k] == 8 else None}
+        make["v"], make["v_scale"] = make["m"], make["m_scale"]
+        if any(k not in make or len(v) != n for k, v in states.items()):
+            raise ValueError("states: lists named m, v, m_scale, v_scale with an entry for each tensor")
+        self.m, self.v, self.m_scale, self.v_scale = ([states[name][k] if states.get(name) is not None else make[name](k) for k in range(n)]
+                                                      for name in ("m", "v", "m_scale", "v_scale"))
+        self.steps = steps if steps is not None else new((1,), torch.int32)
+        if not isinstance(lr, torch.Tensor):
+            value, lr = float(lr), new((1,), torch.float32)
+            with torch.cuda.stream(stream) if stream is not None else torch.cuda.stream(torch.cuda.current_stream(self.device)):
+                lr.fill_(value)
+        self.lr = lr
+        self.norm = new((1,), torch.float32) if need_norm or max_norm > 0 else None
+        for t, dtype, name in ((self.steps, torch.int32, "steps"), (self.lr, torch.float32, "lr")):
+            if t.dtype is not dtype or t.numel() != 1 or t.device != self.device or not t.is_cuda:
+                raise ValueError(f"{name}: {dtype} tensor [1] on the parameters' device")
+        table = (_CAdamWTensor * n)()
+        for k in range(n):
+            size = self.params[k].numel()
+            state = torch.float32 if bits[k] == 32 else torch.float8_e4m3fn
+            for t, dtypes, count, name in ((self.params[k], (torch.float32,), size, "params"), (self.grads[k], (torch.float32, torch.bfloat16), size, "grads"),
+                                           (self.copies[k], (torch.bfloat16, None), size, "copies"), (self.m[k], (state,), size, "m"), (self.v[k], (state,), size, "v"),
+                                           (self.m_scale[k] if bits[k] == 8 else None, (torch.float32, None) if bits[k] == 32 else (torch.float32,), blocks[k], "m_scale"),
+                                           (self.v_scale[k] if bits[k] == 8 else None, (torch.float32, None) if bits[k] == 32 else (torch.float32,), blocks[k], "v_scale")):
+                if t is None and None in dtypes:
+                    continue
+                if t is None or t.dtype not in dtypes or t.numel() != count or not t.is_contiguous() or t.device != self.device or not t.is_cuda:
+                    raise ValueError(f"{name}[{k}]: contiguous {dtypes[0]} tensor of {count} elements on the parameters' device")
+            p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+            table[k] = _CAdamWTensor(p(self.params[k]), p(self.grads[k]), p(self.copies[k]), p(self.m[k]), p(self.v[k]),
+                                     p(self.m_scale[k]) if bits[k] == 8 else None, p(self.v_scale[k]) if bits[k] == 8 else None, size,
+                                     _dt(self.grads[k].dtype), bits[k], mult[k], decay[k])
+        self._n, self._blocks, self._table = n, ctypes.c_int64(), table
+        self.ws = _empty(max(int(_lib.qblora_adamw_workspace_bytes(n)), 256), torch.uint8, self.device, stream)
+        self._cfg = _CAdamWCfg(self.lr.data_ptr(), self.steps.data_ptr(), float(betas[0]), float(betas[1]), float(eps), float(max_norm),
+                               int(seed) & 0xffffffff, p(self.norm))
+        self._prepare(stream)
+
+    def _prepare(self, stream):
+        _check(_lib.qblora_adamw_prepare(self._table, self._n, self.ws.data_ptr(), self.ws.numel(), ctypes.byref(self._blocks), _stream_ptr(stream)),
+               "qblora_adamw_prepare")
+
+    def set_grads(self, grads, stream=None) -> None:
+        """Other gradient tensors from the next step on (a new table; not while a captured step of this object may run)."""
+        if len(grads) != self._n:
+            raise ValueError("grads: one tensor for each parameter")
+        for k, g in enumerate(grads):
+            if g.dtype not in (torch.float32, torch.bfloat16) or g.numel() != self.params[k].numel() or not g.is_contiguous() or g.device != self.device:
+                raise ValueError(f"grads[{k}]: contiguous fp32 or bf16 tensor of the parameter's size and device")
+        for k, g in enumerate(grads):
+            self._table[k].g, self._table[k].g_dtype = g.data_ptr(), _dt(g.dtype)
+        self.grads = list(grads)
+        self._prepare(stream)
+
+    def step(self, stream=None) -> Optional[torch.Tensor]:
+        """One step on the gradients as they are when it runs; returns the norm's tensor, where it is formed."""
+        st = _lib.qblora_adamw_step(ctypes.byref(self._cfg), self._n, self._blocks.value, self.ws.data_ptr(), self.ws.numel(), _stream_ptr(stream))
+        if st != OK:
+            _check(st, "qblora_adamw_step")
+        return self.norm
+
+
+def _zeros(shape, dtype, device, stream) -> torch.Tensor:
+    t = _empty(shape, torch.uint8 if dtype is torch.float8_e4m3fn else dtype, device, stream)
+    _zero(t, stream)
+    return t.view(dtype) if dtype is torch.float8_e4m3fn else t

@@ -1,0 +1,430 @@
+// AdamW over many tensors at once, states in 32 bits or in 8, with the global gradient norm and clipping
+// (qblora_adamw_prepare, qblora_adamw_step; the formulas stand in include/qblora.h).
+//
+// What bounds it: memory.  An element moves 30 bytes with states in 32 bits (p, m, v in and out, g in, the bf16 copy out) and
+// 16 to 18 with states in 8.  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane:
+// a scale's block lies within a warp, so its maximum is five shuffles and no element is read twice.  The tensors are a table in the
+// workspace; a warp finds its block's tensor by a search over the first blocks, which 24 warps per SM hide.  Lane l holds elements
+// 4 l .. 4 l + 3 and 128 + 4 l .. of the block, so every load and store of a warp is one contiguous run.
+//
+// One launch without the norm, two with it: the step's count is read by every CTA as it starts and written by the CTA that
+// ends last.
+#include <cfloat>
+#include <cmath>
+
+#include "common.cuh"
+
+namespace qb {
+namespace {
+
+constexpr int AW_BLOCK = 256, AW_WARPS = 8, AW_THREADS = AW_WARPS * 32;
+constexpr int AW_NORM_CTAS = 592;              // most CTAs of the norm kernel: 4 on each of 148 SMs
+constexpr int AW_MAX_TENSORS = 65536;
+
+struct AwTensor {
+  float* p; const void* g; __nv_bfloat16* copy; void* m; void* v; float* m_scale; float* v_scale;
+  long long n;
+  uint32_t first;                              // its first block
+  int g16, bits8, wide;                        // wide: every pointer allows the vector accesses
+  float lr_mult, decay;
+};
+
+// The workspace: control words, the norm's parts, the table, the first blocks.
+struct AwControl {
+  uint32_t norm_ticket, step_ticket;           // CTAs that have come to their end; back to 0 after every call
+  float factor;                                // of the gradients; negative: leave the step out
+  uint32_t blocks;                             // of all tensors
+};
+constexpr size_t kAwParts = kStatusBytes;
+constexpr size_t kAwTable = kAwParts + AW_NORM_CTAS * 8 + 128;
+static_assert(sizeof(AwControl) <= kStatusBytes && kAwTable % 16 == 0, "layout");
+size_t aw_first_at(int n) { return kAwTable + align_up((size_t)n * sizeof(AwTensor), 16); }
+
+struct AwView {
+  AwControl* ctl; double* parts; const AwTensor* table; const uint32_t* first; int n;
+};
+AwView aw_view(void* ws, int n) {
+  char* w = static_cast<char*>(ws);
+  return {reinterpret_cast<AwControl*>(w), reinterpret_cast<double*>(w + kAwParts), reinterpret_cast<const AwTensor*>(w + kAwTable),
+          reinterpret_cast<const uint32_t*>(w + aw_first_at(n)), n};
+}
+
+struct AwStep {
+  AwView w;
+  const float* lr; int* steps; float* norm;
+  double log_b1, log_b2;                       // -infinity for a beta of 0
+  float b1, b2, c1, c2, eps, max_norm;         // c = 1 - beta
+  uint32_t seed;
+  int clipped;                                 // the norm kernel runs in front
+};
+
+// ---- the table ---------------------------------------------------------------------------------------------------------
+constexpr int AW_TABLE_PART = 32;              // entries per launch: they travel as kernel arguments
+struct AwTablePart { AwTensor t[AW_TABLE_PART]; };
+__global__ void __launch_bounds__(AW_TABLE_PART) adamw_table_kernel(const __grid_constant__ AwTablePart part, int at, int count, int n,
+                                                                    uint32_t blocks, char* ws, size_t first_at) {
+  const int i = threadIdx.x;
+  AwTensor* table = reinterpret_cast<AwTensor*>(ws + kAwTable);
+  uint32_t* first = reinterpret_cast<uint32_t*>(ws + first_at);
+  if (i < count) { table[at + i] = part.t[i]; first[at + i] = part.t[i].first; }
+  if (at + count == n && i == 0) {
+    first[n] = blocks;
+    AwControl* c = reinterpret_cast<AwControl*>(ws);
+    *c = AwControl{0u, 0u, 1.0f, blocks};
+  }
+}
+
+// tensor of block b: the last k with first[k] <= b that has blocks.  `k` is a guess: the tensor of the warp's block before.
+__device__ __forceinline__ int aw_find(const AwView& w, uint32_t b, int k) {
+  if (__ldg(w.first + k) <= b && b < __ldg(w.first + k + 1)) return k;
+  int lo = 0, hi = w.n;                        // first[lo] <= b < first[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (__ldg(w.first + mid) <= b) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// ---- 256 elements of a warp: lane l holds 4 l + e and 128 + 4 l + e in x[e] and x[4 + e] -------------------------------------
+__device__ __forceinline__ int aw_elem(int lane, int i) { return (i >> 2) * 128 + 4 * lane + (i & 3); }
+
+__device__ __forceinline__ void aw_load_f32(const float* a, long long base, int left, bool wide, int lane, float (&x)[8]) {
+  if (wide && left >= AW_BLOCK) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 v = *reinterpret_cast<const float4*>(a + base + h * 128 + 4 * lane);
+      x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? a[base + aw_elem(lane, i)] : 0.f;
+}
+__device__ __forceinline__ void aw_store_f32(float* a, long long base, int left, bool wide, int lane, const float (&x)[8]) {
+  if (wide && left >= AW_BLOCK) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      *reinterpret_cast<float4*>(a + base + h * 128 + 4 * lane) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (aw_elem(lane, i) < left) a[base + aw_elem(lane, i)] = x[i];
+}
+__device__ __forceinline__ void aw_load_g(const AwTensor& t, long long base, int left, int lane, float (&x)[8]) {
+  if (!t.g16) { aw_load_f32(static_cast<const float*>(t.g), base, left, t.wide, lane, x); return; }
+  const __nv_bfloat16* a = static_cast<const __nv_bfloat16*>(t.g);
+  if (t.wide && left >= AW_BLOCK) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint2 v = *reinterpret_cast<const uint2*>(a + base + h * 128 + 4 * lane);
+      x[4 * h] = __uint_as_float(v.x << 16); x[4 * h + 1] = __uint_as_float(v.x & 0xffff0000u);
+      x[4 * h + 2] = __uint_as_float(v.y << 16); x[4 * h + 3] = __uint_as_float(v.y & 0xffff0000u);
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? __bfloat162float(a[base + aw_elem(lane, i)]) : 0.f;
+}
+
+// ---- 8-bit states --------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t aw_mix(uint32_t x) {
+  x = (x ^ (x >> 16)) * 0xA3C59AC3u;
+  x = (x ^ (x >> 15)) * 0x5D8E3B97u;
+  return x ^ (x >> 16);
+}
+// e4m3 code -> fp32 (exact): its exponent and mantissa bits at the lower end of fp32's exponent and the top of its mantissa are the
+// number times 2^-120, also where it is subnormal.  The two NaN codes do not fit that pattern.
+__device__ __forceinline__ float aw_from_code(uint32_t c) {
+  const uint32_t low = c & 0x7fu;
+  const float x = low == 0x7fu ? __uint_as_float(0x7fc00000u) : __uint_as_float((low << 20)) * 0x1p120f;
+  return __uint_as_float(__float_as_uint(x) | (c & 0x80u) << 24);
+}
+// y in [0, 448], 16 random bits -> code of one of y's neighbours
+__device__ __forceinline__ uint32_t aw_to_code(float y, uint32_t bits16) {
+  if (y >= 0x1p-6f) return ((__float_as_uint(y) + (bits16 << 4)) >> 20) - 960u;   // drops 20 of 23 mantissa bits, moves the bias from 127 to 7
+  return (uint32_t)floorf(fmaf(y, 512.0f, (float)bits16 * 0x1p-16f));             // steps of 2^-9
+}
+
+__device__ __forceinline__ void aw_load_codes(const void* a, long long base, int left, bool wide, int lane, float scale, float (&x)[8]) {
+  const uint8_t* c = static_cast<const uint8_t*>(a);
+  if (wide && left >= AW_BLOCK) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t w = *reinterpret_cast<const uint32_t*>(c + base + h * 128 + 4 * lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[4 * h + e] = aw_from_code((w >> (8 * e)) & 0xffu) * scale;
+    }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? aw_from_code(c[base + aw_elem(lane, i)]) * scale : 0.f;
+}
+// `shift`: which 16 of the random bits
+__device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long base, int left, bool wide, int lane, const float (&x)[8],
+                                               const uint32_t (&rnd)[8], int shift) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = fabsf(x[i]);
+    if (y <= FLT_MAX) top = fmaxf(top, y);     // NaN and infinity do not count
+  }
+#pragma unroll
+  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  if (top < 0x1p-118f) top = 0.f;
+  const float inv = top > 0.f ? __fdiv_rn(448.0f, top) : 0.f;
+  uint32_t w[2] = {0u, 0u};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float y = fabsf(x[i]);
+    uint32_t code = y <= FLT_MAX ? aw_to_code(fminf(y * inv, 448.0f), (rnd[i] >> shift) & 0xffffu) : 0x7fu;
+    code |= x[i] < 0.f ? 0x80u : 0u;
+    w[i >> 2] |= code << (8 * (i & 3));
+  }
+  uint8_t* c = static_cast<uint8_t*>(a);
+  if (wide && left >= AW_BLOCK) {
+    *reinterpret_cast<uint32_t*>(c + base + 4 * lane) = w[0];
+    *reinterpret_cast<uint32_t*>(c + base + 128 + 4 * lane) = w[1];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (aw_elem(lane, i) < left) c[base + aw_elem(lane, i)] = (uint8_t)(w[i >> 2] >> (8 * (i & 3)));
+  }
+  if (lane == 0) *scale = top * (1.0f / 448.0f);
+}
+
+// ---- the step --------------------------------------------------------------------------------------------------------------
+__global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_constant__ AwStep s) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const AwView& w = s.w;
+  const int taken = *reinterpret_cast<volatile const int*>(s.steps);
+  const float factor = s.clipped ? *reinterpret_cast<volatile const float*>(&w.ctl->factor) : 1.0f;
+  const uint32_t blocks = w.ctl->blocks;
+  if (factor >= 0.f) {
+    const double now = (double)taken + 1.0;
+    // 1 - beta^t, without the cancellation that beta^t near 1 would bring
+    const float fix1 = -expm1f((float)(now * s.log_b1)), fix2 = -expm1f((float)(now * s.log_b2));
+    const float lr = *s.lr;
+    const uint32_t key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
+    int k = 0;
+    for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
+      k = aw_find(w, b, k);
+      const AwTensor t = w.table[k];
+      const long long base = (long long)(b - t.first) * AW_BLOCK;
+      const int left = (int)min((long long)AW_BLOCK, t.n - base);
+      float g[8], p[8], m[8], v[8];
+      aw_load_g(t, base, left, lane, g);
+      aw_load_f32(t.p, base, left, t.wide, lane, p);
+      if (t.bits8) {
+        aw_load_codes(t.m, base, left, t.wide, lane, t.m_scale[b - t.first], m);
+        aw_load_codes(t.v, base, left, t.wide, lane, t.v_scale[b - t.first], v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= v[i];
+      } else {
+        aw_load_f32(static_cast<const float*>(t.m), base, left, t.wide, lane, m);
+        aw_load_f32(static_cast<const float*>(t.v), base, left, t.wide, lane, v);
+      }
+      const float rate = lr * t.lr_mult;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float x = g[i] * factor;
+        m[i] = fmaf(s.b1, m[i], s.c1 * x);
+        v[i] = fmaf(s.b2, v[i], s.c2 * x * x);
+        const float up = __fdividef(__fdividef(m[i], fix1), sqrtf(__fdividef(v[i], fix2)) + s.eps);
+        p[i] = fmaf(-rate, fmaf(t.decay, p[i], up), p[i]);
+      }
+      aw_store_f32(t.p, base, left, t.wide, lane, p);
+      if (t.copy) {
+        if (t.wide && left >= AW_BLOCK) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const __nv_bfloat162 a = __floats2bfloat162_rn(p[4 * h], p[4 * h + 1]), c = __floats2bfloat162_rn(p[4 * h + 2], p[4 * h + 3]);
+            *reinterpret_cast<uint2*>(t.copy + base + h * 128 + 4 * lane) =
+                make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&c));
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (aw_elem(lane, i) < left) t.copy[base + aw_elem(lane, i)] = __float2bfloat16_rn(p[i]);
+        }
+      }
+      if (t.bits8) {
+        uint32_t rnd[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          rnd[i] = aw_mix((b * AW_BLOCK + aw_elem(lane, i)) * 0x9E3779B1u + key);
+          v[i] = sqrtf(v[i]);
+        }
+        aw_store_codes(t.m, t.m_scale + (b - t.first), base, left, t.wide, lane, m, rnd, 0);
+        aw_store_codes(t.v, t.v_scale + (b - t.first), base, left, t.wide, lane, v, rnd, 16);
+      } else {
+        aw_store_f32(static_cast<float*>(t.m), base, left, t.wide, lane, m);
+        aw_store_f32(static_cast<float*>(t.v), base, left, t.wide, lane, v);
+      }
+    }
+  }
+  // every CTA has read the count when the last one comes here
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (atomicAdd(&w.ctl->step_ticket, 1u) + 1u == gridDim.x) {
+      w.ctl->step_ticket = 0u;
+      if (factor >= 0.f) *s.steps = taken + 1;
+    }
+  }
+}
+
+// ---- the norm: every CTA sums its blocks, the one that ends last the CTAs' sums, in order -----------------------------------------
+__global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_constant__ AwStep s) {
+  __shared__ double s_sum[AW_WARPS];
+  __shared__ bool s_last;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const AwView& w = s.w;
+  const uint32_t blocks = w.ctl->blocks;
+  double sum = 0.0;
+  int k = 0;
+  for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
+    k = aw_find(w, b, k);
+    const AwTensor t = w.table[k];
+    const long long base = (long long)(b - t.first) * AW_BLOCK;
+    float g[8], q = 0.f;
+    aw_load_g(t, base, (int)min((long long)AW_BLOCK, t.n - base), lane, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q = fmaf(g[i], g[i], q);
+    sum += (double)q;
+  }
+  auto join = [&](double x) {                  // over the CTA; the result in thread 0
+#pragma unroll
+    for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
+    if (lane == 0) s_sum[warp] = x;
+    __syncthreads();
+    x = 0.0;
+    if (threadIdx.x == 0)
+      for (int i = 0; i < AW_WARPS; ++i) x += s_sum[i];
+    return x;
+  };
+  sum = join(sum);
+  if (threadIdx.x == 0) {
+    w.parts[blockIdx.x] = sum;
+    __threadfence();
+    s_last = atomicAdd(&w.ctl->norm_ticket, 1u) + 1u == gridDim.x;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  sum = 0.0;
+  for (int i = threadIdx.x; i < (int)gridDim.x; i += AW_THREADS) sum += *reinterpret_cast<volatile double*>(w.parts + i);
+  sum = join(sum);
+  if (threadIdx.x == 0) {
+    const float norm = (float)sqrt(sum);
+    w.ctl->norm_ticket = 0u;
+    // a norm past fp32's range is not finite either
+    w.ctl->factor = !(norm <= FLT_MAX) ? -1.0f : s.max_norm > 0.f && norm > s.max_norm ? __fdiv_rn(s.max_norm, norm) : 1.0f;
+    if (s.norm) *s.norm = norm;
+  }
+}
+
+bool ptr_ok(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+int sm_count(int* sms) {
+  int dev = 0;
+  QB_CUDA(cudaGetDevice(&dev));
+  QB_CUDA(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  return QBLORA_OK;
+}
+
+}  // namespace
+}  // namespace qb
+
+using namespace qb;
+
+extern "C" {
+
+size_t qblora_adamw_workspace_bytes(int32_t n_tensors) {
+  if (n_tensors < 1 || n_tensors > AW_MAX_TENSORS) return 0;
+  return align_up(aw_first_at(n_tensors) + (size_t)(n_tensors + 1) * 4, 256);
+}
+
+int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, void* ws, size_t ws_bytes, int64_t* blocks,
+                         void* stream) {
+  if (!tensors || !blocks || n_tensors < 1) return QBLORA_ERR_INVALID_ARG;
+  if (n_tensors > AW_MAX_TENSORS) return QBLORA_ERR_UNSUPPORTED;
+  int64_t total = 0;
+  for (int i = 0; i < n_tensors; ++i) {
+    const qblora_adamw_tensor& t = tensors[i];
+    if (t.n < 0 || (t.g_dtype != QBLORA_F32 && t.g_dtype != QBLORA_BF16) || (t.state_bits != 32 && t.state_bits != 8)) return QBLORA_ERR_INVALID_ARG;
+    if (!std::isfinite(t.lr_mult) || !std::isfinite(t.weight_decay)) return QBLORA_ERR_INVALID_ARG;
+    if (t.n == 0) continue;
+    const size_t sa = t.state_bits == 8 ? 1 : 4;
+    if (!ptr_ok(t.p, 4) || !ptr_ok(t.g, t.g_dtype == QBLORA_F32 ? 4 : 2) || !ptr_ok(t.m, sa) || !ptr_ok(t.v, sa)) return QBLORA_ERR_INVALID_ARG;
+    if (t.copy && !ptr_ok(t.copy, 2)) return QBLORA_ERR_INVALID_ARG;
+    if (t.state_bits == 8 && (!ptr_ok(t.m_scale, 4) || !ptr_ok(t.v_scale, 4))) return QBLORA_ERR_INVALID_ARG;
+    if (t.n > (int64_t)AW_BLOCK * 0x7fffffff) return QBLORA_ERR_UNSUPPORTED;
+    total += (t.n + AW_BLOCK - 1) / AW_BLOCK;
+    if (total > 0x7fffffff) return QBLORA_ERR_UNSUPPORTED;
+  }
+  if (!ws || !aligned16(ws) || ws_bytes < qblora_adamw_workspace_bytes(n_tensors)) return QBLORA_ERR_WORKSPACE;
+  uint32_t first = 0;
+  for (int at = 0; at < n_tensors; at += AW_TABLE_PART) {
+    AwTablePart part{};
+    const int count = n_tensors - at < AW_TABLE_PART ? n_tensors - at : AW_TABLE_PART;
+    for (int i = 0; i < count; ++i) {
+      const qblora_adamw_tensor& t = tensors[at + i];
+      AwTensor& d = part.t[i];
+      d.p = t.p; d.g = t.g; d.copy = static_cast<__nv_bfloat16*>(t.copy); d.m = t.m; d.v = t.v; d.m_scale = t.m_scale; d.v_scale = t.v_scale;
+      d.n = t.n; d.first = first; d.g16 = t.g_dtype == QBLORA_BF16; d.bits8 = t.state_bits == 8;
+      d.lr_mult = t.lr_mult; d.decay = t.weight_decay;
+      const size_t sa = d.bits8 ? 4 : 16;
+      d.wide = t.n > 0 && ptr_ok(t.p, 16) && ptr_ok(t.g, d.g16 ? 8 : 16) && ptr_ok(t.m, sa) && ptr_ok(t.v, sa) &&
+               (!t.copy || ptr_ok(t.copy, 8));
+      first += (uint32_t)((t.n + AW_BLOCK - 1) / AW_BLOCK);
+    }
+    adamw_table_kernel<<<1, AW_TABLE_PART, 0, static_cast<cudaStream_t>(stream)>>>(part, at, count, n_tensors, (uint32_t)total,
+                                                                                   static_cast<char*>(ws), aw_first_at(n_tensors));
+    count_launch();
+    QB_CUDA(cudaGetLastError());
+  }
+  *blocks = total;
+  return QBLORA_OK;
+}
+
+int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t blocks, void* ws, size_t ws_bytes, void* stream) {
+  if (!cfg || n_tensors < 1 || n_tensors > AW_MAX_TENSORS || blocks < 0 || blocks > 0x7fffffff) return QBLORA_ERR_INVALID_ARG;
+  if (!ptr_ok(cfg->lr, 4) || !ptr_ok(cfg->steps, 4) || (cfg->norm && !ptr_ok(cfg->norm, 4))) return QBLORA_ERR_INVALID_ARG;
+  if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return QBLORA_ERR_INVALID_ARG;
+  if (!(cfg->eps >= 0.0 && std::isfinite(cfg->eps)) || !(cfg->max_norm >= 0.f && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
+  if (!ws || !aligned16(ws) || ws_bytes < qblora_adamw_workspace_bytes(n_tensors)) return QBLORA_ERR_WORKSPACE;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  AwStep s{};
+  s.w = aw_view(ws, n_tensors);
+  s.lr = cfg->lr; s.steps = cfg->steps; s.norm = cfg->norm;
+  s.log_b1 = std::log(cfg->beta1); s.log_b2 = std::log(cfg->beta2);
+  s.b1 = (float)cfg->beta1; s.b2 = (float)cfg->beta2; s.c1 = (float)(1.0 - cfg->beta1); s.c2 = (float)(1.0 - cfg->beta2);
+  s.eps = (float)cfg->eps; s.max_norm = cfg->max_norm; s.seed = cfg->seed;
+  s.clipped = cfg->max_norm > 0.f || cfg->norm != nullptr;
+  int sms = 0;
+  const int rc = sm_count(&sms);
+  if (rc) return rc;
+  const int64_t want = (blocks + AW_WARPS - 1) / AW_WARPS;
+  if (s.clipped) {
+    int64_t grid = 4LL * sms < AW_NORM_CTAS ? 4LL * sms : AW_NORM_CTAS;
+    if (grid > want) grid = want;
+    if (grid < 1) grid = 1;
+    adamw_norm_kernel<<<(unsigned)grid, AW_THREADS, 0, st>>>(s);
+    count_launch();
+    QB_CUDA(cudaGetLastError());
+  }
+  int64_t grid = 3LL * sms;
+  if (grid > want) grid = want;
+  if (grid < 1) grid = 1;
+  cudaLaunchConfig_t lc = {};
+  lc.gridDim = dim3((unsigned)grid);
+  lc.blockDim = dim3(AW_THREADS);
+  lc.stream = st;
+  QB_CUDA(cudaLaunchKernelEx(&lc, adamw_kernel, s));
+  count_launch();
+  return QBLORA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,138 @@
+// Rows of a step sorted by adapter, from the requests' offsets and adapters (qblora_adapter_plan).
+//
+// A request's rows are neighbours before and after, so the requests are sorted, not the rows: the place of request b is the
+// number of rows of all lower adapters, start[a], and of the requests in front of it with the same adapter.  Chunks of 32 requests
+// are one warp's: the lanes with the same adapter find one another by a vote, and each learns what its fellows in front of it bring.
+// Across chunks one warp walks in order over a table of running sums, one step of a few instructions per chunk.  Whole numbers
+// only, no order but the requests': the result does not depend on the launch.
+//
+// What bounds it: latency.  One launch, in which every CTA forms the sums for itself in shared memory; the rows are then spread
+// over the grid.
+#include <atomic>
+
+#include "adapters.cuh"
+
+namespace qb {
+namespace {
+
+constexpr int AP_THREADS = 256;
+
+__global__ void __launch_bounds__(AP_THREADS) adapter_plan_kernel(const __grid_constant__ AdapterPlanCall c) {
+  extern __shared__ int ap_smem[];
+  int* s_cu = ap_smem;                   // [R + 1] offsets
+  int* s_id = s_cu + c.R + 1;            // [R] adapter or -1
+  int* s_pre = s_id + c.R;               // [R] rows of the same adapter in front, within the chunk; then the request's place
+  int* s_lead = s_pre + c.R;             // [R] first request of the chunk with the same adapter
+  int* s_sum = s_lead + c.R;             // [R] at that request: rows of the chunk for the adapter; then those of earlier chunks
+  int* s_at = s_sum + c.R;               // [n + 1] rows per adapter, then offsets, then running sums
+  __shared__ int s_warp[AP_THREADS / 32];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  for (int b = tid; b <= c.R; b += AP_THREADS) s_cu[b] = min(max(__ldg(c.cu + b), 0), c.T);
+  for (int a = tid; a <= c.n; a += AP_THREADS) s_at[a] = 0;
+  __syncthreads();
+  for (int b0 = warp * 32; b0 < c.R; b0 += AP_THREADS) {
+    const int b = b0 + lane;
+    int a = -1, len = 0;
+    if (b < c.R) {
+      const int id = __ldg(c.ids + b);
+      len = max(s_cu[b + 1] - s_cu[b], 0);
+      a = id >= 0 && id < c.n && len > 0 ? id : -1;
+      if (a < 0) len = 0;
+    }
+    const unsigned same = __match_any_sync(0xffffffffu, a);
+    int before = 0, all = 0;
+    for (unsigned left = __reduce_or_sync(0xffffffffu, a >= 0 ? same : 0u); left; left &= left - 1) {
+      const int j = __ffs(left) - 1, x = __shfl_sync(0xffffffffu, len, j);
+      if ((same >> j) & 1u) {
+        all += x;
+        if (j < lane) before += x;
+      }
+    }
+    if (b < c.R) {
+      const int lead = __ffs(same) - 1;
+      s_id[b] = a;
+      s_pre[b] = before;
+      s_lead[b] = b0 + lead;
+      s_sum[b] = lead == lane ? all : 0;
+      if (a >= 0 && lead == lane) atomicAdd(&s_at[a], all);
+    }
+  }
+  __syncthreads();
+  // exclusive sums over the adapters: thread t has `per` neighbours
+  const int per = (c.n + AP_THREADS - 1) / AP_THREADS, lo = min(tid * per, c.n), hi = min(lo + per, c.n);
+  int mine = 0;
+  for (int a = lo; a < hi; ++a) mine += s_at[a];
+  int incl = mine;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, d);
+    if (lane >= d) incl += y;
+  }
+  if (lane == 31) s_warp[warp] = incl;
+  __syncthreads();
+  int at = incl - mine, total = 0;
+#pragma unroll
+  for (int w = 0; w < AP_THREADS / 32; ++w) {
+    if (w < warp) at += s_warp[w];
+    total += s_warp[w];
+  }
+  for (int a = lo; a < hi; ++a) {
+    const int x = s_at[a];
+    s_at[a] = at;
+    if (blockIdx.x == 0) c.start[a] = min(at, c.T);
+    at += x;
+  }
+  if (blockIdx.x == 0 && tid == 0) c.start[c.n] = min(total, c.T);
+  __syncthreads();
+  if (warp == 0) {
+    for (int b0 = 0; b0 < c.R; b0 += 32) {
+      const int b = b0 + lane;
+      if (b < c.R && s_id[b] >= 0 && s_lead[b] == b) {
+        const int a = s_id[b], x = s_at[a];
+        s_at[a] = x + s_sum[b];
+        s_sum[b] = x;
+      }
+      __syncwarp();
+    }
+  }
+  __syncthreads();
+  for (int b = tid; b < c.R; b += AP_THREADS) s_pre[b] += s_sum[s_lead[b]];
+  __syncthreads();
+
+  const int gid = blockIdx.x * AP_THREADS + tid, gn = gridDim.x * AP_THREADS;
+  for (int64_t t = gid; t < (int64_t)c.T; t += gn) {
+    if (t >= total) c.rows[t] = -1;
+    if (t < s_cu[0] || t >= s_cu[c.R]) continue;
+    int b = 0, e = c.R;                  // s_cu[b] <= t < s_cu[e]
+    while (e - b > 1) {
+      const int mid = (b + e) >> 1;
+      if (s_cu[mid] <= (int)t) b = mid; else e = mid;
+    }
+    if (s_id[b] < 0) continue;
+    const int64_t j = (int64_t)s_pre[b] + (t - s_cu[b]);
+    if (j >= 0 && j < c.T) c.rows[j] = (int)t;     // (always, for rising offsets)
+  }
+}
+
+}  // namespace
+
+int launch_adapter_plan(const AdapterPlanCall& c, cudaStream_t st) {
+  constexpr int most = (5 * kPlanMaxAdapterRequests + kMaxAdapters + 2) * 4;
+  static std::atomic<bool> attr_set[64];
+  int dev = 0;
+  QB_CUDA(cudaGetDevice(&dev));
+  if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
+  if (!attr_set[dev].load(std::memory_order_acquire)) {
+    QB_CUDA(cudaFuncSetAttribute(adapter_plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most));
+    attr_set[dev].store(true, std::memory_order_release);
+  }
+  int64_t grid = ((int64_t)c.T + AP_THREADS - 1) / AP_THREADS;
+  if (grid > 148) grid = 148;
+  adapter_plan_kernel<<<(unsigned)grid, AP_THREADS, (size_t)(5 * c.R + c.n + 2) * 4, st>>>(c);
+  count_launch();
+  QB_CUDA(cudaGetLastError());
+  return QBLORA_OK;
+}
+
+}  // namespace qb
