@@ -548,7 +548,7 @@ typedef struct {
   int32_t* steps;           /* DEVICE [1]: steps taken so far (>= 0); the call adds one */
   double beta1, beta2;      /* 0 <= beta < 1 */
   double eps;               /* >= 0 */
-  float max_norm;           /* > 0: gradients are scaled by min(1, max_norm / norm); 0: not */
+  double max_norm;          /* > 0: gradients are scaled by min(1, max_norm / norm); 0: not */
   uint32_t seed;            /* of the rounding of 8-bit states */
   float* norm;              /* DEVICE out [1]: the gradients' global 2-norm; NULL: only formed where max_norm asks for it */
 } qblora_adamw_cfg;
@@ -557,7 +557,8 @@ typedef struct {
  * AdamW over many tensors at once.  With g~ = min(1, max_norm / norm) g and t = steps + 1, for every element of every tensor
  *   m = beta1 m + (1 - beta1) g~;   v = beta2 v + (1 - beta2) g~^2;
  *   p = p - lr lr_mult (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p);   copy = bf16(p).
- * Everything is formed in fp32 from the stored states; the update uses m and v before they are stored again.
+ * Everything is formed in fp32 from the stored states; the update uses m and v before they are stored again.  m and v take one
+ * rounding per operation in the order written (g~ * g~ before its factor), so states in 8 bits are unique.
  *
  * States in 8 bits: m and r = sqrt(v) are held as e4m3 codes (sign, 4 exponent bits with bias 7, 3 mantissa bits; the largest
  * number is 448) times one fp32 scale per block of 256 consecutive elements, scale = (largest |m| of the block) / 448.  A value
@@ -569,10 +570,9 @@ typedef struct {
  * at least 1.  Equal inputs give equal bits.  States that are not finite are held as NaN and do not count for the scale; a block
  * whose largest value is below 2^-118 is held as zeros.
  *
- * The norm is summed over the gradients of all tensors in the call (blocks of squares in fp32, their sum in fp64, in a fixed
- * order).  Where it is formed and is not finite, the step is left out: nothing but *norm is written.
+ * The norm is summed over the gradients of all tensors in the call, in fp64 and in a fixed order.  Where it is formed and is not finite, the step is left out: nothing but *norm is written.
  *
- * qblora_adamw_prepare lays the tensors' table into ws and returns in *blocks the number that the step wants; ws then belongs to
+ * qblora_adamw_prepare lays the tensors' table into ws and writes to *blocks the number that the step wants (an opaque one); ws then belongs to
  * these tensors (their addresses, not their values) until it is prepared again.  At most 65536 tensors, 2^31 - 1 blocks.
  * No tensor may overlap another.  qblora_adamw_step may be captured in a graph: lr, steps and the gradients' values are
  * read when it runs.  Two steps over one ws run one after the other.

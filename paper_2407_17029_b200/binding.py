@@ -86,7 +86,7 @@ class _CAdamWTensor(ctypes.Structure):
 
 class _CAdamWCfg(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_void_p), ("steps", ctypes.c_void_p), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
-                ("eps", ctypes.c_double), ("max_norm", ctypes.c_float), ("seed", ctypes.c_uint32), ("norm", ctypes.c_void_p)]
+                ("eps", ctypes.c_double), ("max_norm", ctypes.c_double), ("seed", ctypes.c_uint32), ("norm", ctypes.c_void_p)]
 
 
 if not os.path.exists(LIB_PATH):

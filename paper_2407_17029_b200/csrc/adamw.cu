@@ -12,6 +12,8 @@
 #include <cfloat>
 #include <cmath>
 
+#include <cuda_fp16.h>
+
 #include "common.cuh"
 
 namespace qb {
@@ -52,8 +54,8 @@ AwView aw_view(void* ws, int n) {
 struct AwStep {
   AwView w;
   const float* lr; int* steps; float* norm;
-  double log_b1, log_b2;                       // -infinity for a beta of 0
-  float b1, b2, c1, c2, eps, max_norm;         // c = 1 - beta
+  double log_b1, log_b2, max_norm;             // log: -infinity for a beta of 0
+  float b1, b2, c1, c2, eps;                   // c = 1 - beta
   uint32_t seed;
   int clipped;                                 // the norm kernel runs in front
 };
@@ -133,53 +135,75 @@ __device__ __forceinline__ uint32_t aw_mix(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x5D8E3B97u;
   return x ^ (x >> 16);
 }
-// e4m3 code -> fp32 (exact): its exponent and mantissa bits at the lower end of fp32's exponent and the top of its mantissa are the
-// number times 2^-120, also where it is subnormal.  The two NaN codes do not fit that pattern.
-__device__ __forceinline__ float aw_from_code(uint32_t c) {
-  const uint32_t low = c & 0x7fu;
-  const float x = low == 0x7fu ? __uint_as_float(0x7fc00000u) : __uint_as_float((low << 20)) * 0x1p120f;
-  return __uint_as_float(__float_as_uint(x) | (c & 0x80u) << 24);
+// four e4m3 codes -> fp32 (exact)
+__device__ __forceinline__ void aw_from_codes(uint32_t w, float* x) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    uint32_t p;
+    asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(p) : "r"(w >> (16 * h)));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p));
+    x[2 * h] = f.x;
+    x[2 * h + 1] = f.y;
+  }
 }
-// y in [0, 448], 16 random bits -> code of one of y's neighbours
-__device__ __forceinline__ uint32_t aw_to_code(float y, uint32_t bits16) {
-  if (y >= 0x1p-6f) return ((__float_as_uint(y) + (bits16 << 4)) >> 20) - 960u;   // drops 20 of 23 mantissa bits, moves the bias from 127 to 7
-  return (uint32_t)floorf(fmaf(y, 512.0f, (float)bits16 * 0x1p-16f));             // steps of 2^-9
-}
-
 __device__ __forceinline__ void aw_load_codes(const void* a, long long base, int left, bool wide, int lane, float scale, float (&x)[8]) {
   const uint8_t* c = static_cast<const uint8_t*>(a);
+  uint32_t w[2] = {0u, 0u};
   if (wide && left >= AW_BLOCK) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(c + base + h * 128 + 4 * lane);
+    for (int h = 0; h < 2; ++h) w[h] = *reinterpret_cast<const uint32_t*>(c + base + h * 128 + 4 * lane);
+  } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * h + e] = aw_from_code((w >> (8 * e)) & 0xffu) * scale;
-    }
-    return;
+    for (int i = 0; i < 8; ++i)
+      if (aw_elem(lane, i) < left) w[i >> 2] |= (uint32_t)c[base + aw_elem(lane, i)] << (8 * (i & 3));
   }
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? aw_from_code(c[base + aw_elem(lane, i)]) * scale : 0.f;
+  for (int h = 0; h < 2; ++h) aw_from_codes(w[h], x + 4 * h);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], scale);
 }
-// `shift`: which 16 of the random bits
+// The neighbour of y by chance: with y 2^-120, e4m3's exponent is at the lower end of fp32's, where its subnormal numbers are subnormal
+// too, and 20 bits of the mantissa are to go.  What the random bits, added to the upper 16 of them, carry out decides.  `shift`: which 16
+// of the random bits.  Codes in the top byte of z.
+__device__ __forceinline__ uint32_t aw_round(float y, uint32_t rnd, int shift) {
+  const uint32_t bits16 = shift ? rnd >> 16 : rnd & 0xffffu;
+  return (__float_as_uint(fminf(y, 448.0f * 0x1p-120f)) + (bits16 << 4)) << 4;
+}
 __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long base, int left, bool wide, int lane, const float (&x)[8],
                                                const uint32_t (&rnd)[8], int shift) {
-  float top = 0.f;
+  uint32_t all = 0u;                           // the largest magnitude, as bits (which order like the numbers; NaN above all)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = fabsf(x[i]);
-    if (y <= FLT_MAX) top = fmaxf(top, y);     // NaN and infinity do not count
+  for (int i = 0; i < 8; ++i) all = max(all, __float_as_uint(x[i]) & 0x7fffffffu);
+  all = __reduce_max_sync(0xffffffffu, all);
+  const bool odd = all >= 0x7f800000u;         // NaN or infinity: they do not count
+  if (odd) {
+    all = 0u;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t y = __float_as_uint(x[i]) & 0x7fffffffu;
+      if (y < 0x7f800000u) all = max(all, y);
+    }
+    all = __reduce_max_sync(0xffffffffu, all);
   }
-#pragma unroll
-  for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float top = __uint_as_float(all);
   if (top < 0x1p-118f) top = 0.f;
-  const float inv = top > 0.f ? __fdiv_rn(448.0f, top) : 0.f;
-  uint32_t w[2] = {0u, 0u};
+  const float inv = top > 0.f ? __fmul_rn(__frcp_rn(top), 448.0f) * 0x1p-120f : 0.f;
+  uint32_t w[2];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float y = fabsf(x[i]);
-    uint32_t code = y <= FLT_MAX ? aw_to_code(fminf(y * inv, 448.0f), (rnd[i] >> shift) & 0xffffu) : 0x7fu;
-    code |= x[i] < 0.f ? 0x80u : 0u;
-    w[i >> 2] |= code << (8 * (i & 3));
+  for (int h = 0; h < 2; ++h) {
+    uint32_t z[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = aw_round(fabsf(x[4 * h + e]) * inv, rnd[4 * h + e], shift);
+    const uint32_t code = __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
+    const float* y = x + 4 * h;
+    const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0073),
+                                      __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0073), 0x5410);
+    w[h] = code | (sign & 0x80808080u);
+  }
+  if (odd) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if ((__float_as_uint(x[i]) & 0x7fffffffu) >= 0x7f800000u) w[i >> 2] |= 0x7fu << (8 * (i & 3));
   }
   uint8_t* c = static_cast<uint8_t*>(a);
   if (wide && left >= AW_BLOCK) {
@@ -194,7 +218,9 @@ __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long 
 }
 
 // ---- the step --------------------------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_constant__ AwStep s) {
+// BITS: of the states of all tensors; 0: they are mixed
+template <int BITS>
+__global__ void __launch_bounds__(AW_THREADS, BITS == 8 ? 4 : 3) adamw_kernel(const __grid_constant__ AwStep s) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const AwView& w = s.w;
@@ -205,7 +231,7 @@ __global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_const
     const double now = (double)taken + 1.0;
     // 1 - beta^t, without the cancellation that beta^t near 1 would bring
     const float fix1 = -expm1f((float)(now * s.log_b1)), fix2 = -expm1f((float)(now * s.log_b2));
-    const float lr = *s.lr;
+    const float lr = *s.lr, up1 = __fdiv_rn(1.0f, fix1), up2 = sqrtf(__fdiv_rn(1.0f, fix2));
     const uint32_t key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
     int k = 0;
     for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
@@ -216,22 +242,25 @@ __global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_const
       float g[8], p[8], m[8], v[8];
       aw_load_g(t, base, left, lane, g);
       aw_load_f32(t.p, base, left, t.wide, lane, p);
-      if (t.bits8) {
+      const bool bits8 = BITS == 8 || (BITS == 0 && t.bits8);
+      if (bits8) {
         aw_load_codes(t.m, base, left, t.wide, lane, t.m_scale[b - t.first], m);
         aw_load_codes(t.v, base, left, t.wide, lane, t.v_scale[b - t.first], v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= v[i];
+        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
       } else {
         aw_load_f32(static_cast<const float*>(t.m), base, left, t.wide, lane, m);
         aw_load_f32(static_cast<const float*>(t.v), base, left, t.wide, lane, v);
       }
       const float rate = lr * t.lr_mult;
+      float root[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = g[i] * factor;
-        m[i] = fmaf(s.b1, m[i], s.c1 * x);
-        v[i] = fmaf(s.b2, v[i], s.c2 * x * x);
-        const float up = __fdividef(__fdividef(m[i], fix1), sqrtf(__fdividef(v[i], fix2)) + s.eps);
+        const float x = __fmul_rn(g[i], factor);
+        m[i] = __fadd_rn(__fmul_rn(s.b1, m[i]), __fmul_rn(s.c1, x));
+        v[i] = __fadd_rn(__fmul_rn(s.b2, v[i]), __fmul_rn(s.c2, __fmul_rn(x, x)));
+        root[i] = __fsqrt_rn(v[i]);
+        const float up = __fdividef(m[i] * up1, fmaf(root[i], up2, s.eps));
         p[i] = fmaf(-rate, fmaf(t.decay, p[i], up), p[i]);
       }
       aw_store_f32(t.p, base, left, t.wide, lane, p);
@@ -249,15 +278,12 @@ __global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_const
             if (aw_elem(lane, i) < left) t.copy[base + aw_elem(lane, i)] = __float2bfloat16_rn(p[i]);
         }
       }
-      if (t.bits8) {
+      if (bits8) {
         uint32_t rnd[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          rnd[i] = aw_mix((b * AW_BLOCK + aw_elem(lane, i)) * 0x9E3779B1u + key);
-          v[i] = sqrtf(v[i]);
-        }
+        for (int i = 0; i < 8; ++i) rnd[i] = aw_mix((b * AW_BLOCK + aw_elem(lane, i)) * 0x9E3779B1u + key);
         aw_store_codes(t.m, t.m_scale + (b - t.first), base, left, t.wide, lane, m, rnd, 0);
-        aw_store_codes(t.v, t.v_scale + (b - t.first), base, left, t.wide, lane, v, rnd, 16);
+        aw_store_codes(t.v, t.v_scale + (b - t.first), base, left, t.wide, lane, root, rnd, 16);
       } else {
         aw_store_f32(static_cast<float*>(t.m), base, left, t.wide, lane, m);
         aw_store_f32(static_cast<float*>(t.v), base, left, t.wide, lane, v);
@@ -284,15 +310,15 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_con
   const uint32_t blocks = w.ctl->blocks;
   double sum = 0.0;
   int k = 0;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the step waits for this grid's end before it reads anything
   for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
     k = aw_find(w, b, k);
     const AwTensor t = w.table[k];
     const long long base = (long long)(b - t.first) * AW_BLOCK;
-    float g[8], q = 0.f;
+    float g[8];
     aw_load_g(t, base, (int)min((long long)AW_BLOCK, t.n - base), lane, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q = fmaf(g[i], g[i], q);
-    sum += (double)q;
+    for (int i = 0; i < 8; ++i) sum = fma((double)g[i], (double)g[i], sum);
   }
   auto join = [&](double x) {                  // over the CTA; the result in thread 0
 #pragma unroll
@@ -317,10 +343,11 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_con
   for (int i = threadIdx.x; i < (int)gridDim.x; i += AW_THREADS) sum += *reinterpret_cast<volatile double*>(w.parts + i);
   sum = join(sum);
   if (threadIdx.x == 0) {
-    const float norm = (float)sqrt(sum);
+    const double root = sqrt(sum);
+    const float norm = (float)root;
     w.ctl->norm_ticket = 0u;
     // a norm past fp32's range is not finite either
-    w.ctl->factor = !(norm <= FLT_MAX) ? -1.0f : s.max_norm > 0.f && norm > s.max_norm ? __fdiv_rn(s.max_norm, norm) : 1.0f;
+    w.ctl->factor = !(norm <= FLT_MAX) ? -1.0f : s.max_norm > 0.0 && root > s.max_norm ? (float)(s.max_norm / root) : 1.0f;
     if (s.norm) *s.norm = norm;
   }
 }
@@ -351,6 +378,7 @@ int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, 
   if (!tensors || !blocks || n_tensors < 1) return QBLORA_ERR_INVALID_ARG;
   if (n_tensors > AW_MAX_TENSORS) return QBLORA_ERR_UNSUPPORTED;
   int64_t total = 0;
+  int kinds = 0;                               // 1: some states in 32 bits, 2: some in 8
   for (int i = 0; i < n_tensors; ++i) {
     const qblora_adamw_tensor& t = tensors[i];
     if (t.n < 0 || (t.g_dtype != QBLORA_F32 && t.g_dtype != QBLORA_BF16) || (t.state_bits != 32 && t.state_bits != 8)) return QBLORA_ERR_INVALID_ARG;
@@ -360,6 +388,7 @@ int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, 
     if (!ptr_ok(t.p, 4) || !ptr_ok(t.g, t.g_dtype == QBLORA_F32 ? 4 : 2) || !ptr_ok(t.m, sa) || !ptr_ok(t.v, sa)) return QBLORA_ERR_INVALID_ARG;
     if (t.copy && !ptr_ok(t.copy, 2)) return QBLORA_ERR_INVALID_ARG;
     if (t.state_bits == 8 && (!ptr_ok(t.m_scale, 4) || !ptr_ok(t.v_scale, 4))) return QBLORA_ERR_INVALID_ARG;
+    kinds |= t.state_bits == 8 ? 2 : 1;
     if (t.n > (int64_t)AW_BLOCK * 0x7fffffff) return QBLORA_ERR_UNSUPPORTED;
     total += (t.n + AW_BLOCK - 1) / AW_BLOCK;
     if (total > 0x7fffffff) return QBLORA_ERR_UNSUPPORTED;
@@ -385,15 +414,18 @@ int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, 
     count_launch();
     QB_CUDA(cudaGetLastError());
   }
-  *blocks = total;
+  *blocks = total | (int64_t)kinds << 32;
   return QBLORA_OK;
 }
 
 int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t blocks, void* ws, size_t ws_bytes, void* stream) {
-  if (!cfg || n_tensors < 1 || n_tensors > AW_MAX_TENSORS || blocks < 0 || blocks > 0x7fffffff) return QBLORA_ERR_INVALID_ARG;
+  if (!cfg || n_tensors < 1 || n_tensors > AW_MAX_TENSORS || blocks < 0) return QBLORA_ERR_INVALID_ARG;
+  const int kinds = (int)(blocks >> 32);       // as qblora_adamw_prepare has put them together
+  blocks &= 0xffffffff;
+  if (kinds > 3 || blocks > 0x7fffffff) return QBLORA_ERR_INVALID_ARG;
   if (!ptr_ok(cfg->lr, 4) || !ptr_ok(cfg->steps, 4) || (cfg->norm && !ptr_ok(cfg->norm, 4))) return QBLORA_ERR_INVALID_ARG;
   if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return QBLORA_ERR_INVALID_ARG;
-  if (!(cfg->eps >= 0.0 && std::isfinite(cfg->eps)) || !(cfg->max_norm >= 0.f && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
+  if (!(cfg->eps >= 0.0 && std::isfinite(cfg->eps)) || !(cfg->max_norm >= 0.0 && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adamw_workspace_bytes(n_tensors)) return QBLORA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   AwStep s{};
@@ -402,7 +434,7 @@ int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t bl
   s.log_b1 = std::log(cfg->beta1); s.log_b2 = std::log(cfg->beta2);
   s.b1 = (float)cfg->beta1; s.b2 = (float)cfg->beta2; s.c1 = (float)(1.0 - cfg->beta1); s.c2 = (float)(1.0 - cfg->beta2);
   s.eps = (float)cfg->eps; s.max_norm = cfg->max_norm; s.seed = cfg->seed;
-  s.clipped = cfg->max_norm > 0.f || cfg->norm != nullptr;
+  s.clipped = cfg->max_norm > 0.0 || cfg->norm != nullptr;
   int sms = 0;
   const int rc = sm_count(&sms);
   if (rc) return rc;
@@ -415,14 +447,18 @@ int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t bl
     count_launch();
     QB_CUDA(cudaGetLastError());
   }
-  int64_t grid = 3LL * sms;
+  int64_t grid = (kinds == 2 ? 4LL : 3LL) * sms;
   if (grid > want) grid = want;
   if (grid < 1) grid = 1;
   cudaLaunchConfig_t lc = {};
   lc.gridDim = dim3((unsigned)grid);
   lc.blockDim = dim3(AW_THREADS);
   lc.stream = st;
-  QB_CUDA(cudaLaunchKernelEx(&lc, adamw_kernel, s));
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  lc.attrs = attr; lc.numAttrs = s.clipped ? 1 : 0;
+  QB_CUDA(cudaLaunchKernelEx(&lc, kinds == 2 ? adamw_kernel<8> : kinds == 3 ? adamw_kernel<0> : adamw_kernel<32>, s));
   count_launch();
   return QBLORA_OK;
 }
