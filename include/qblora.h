@@ -547,7 +547,7 @@ typedef struct {
   const float* lr;          /* DEVICE [1]: learning rate, so that a captured step can follow a schedule */
   int32_t* steps;           /* DEVICE [1]: steps taken so far (>= 0); the call adds one */
   double beta1, beta2;      /* 0 <= beta < 1 */
-  double eps;               /* >= 0 */
+  double eps;               /* 0, or a normal fp32 number */
   double max_norm;          /* > 0: gradients are scaled by min(1, max_norm / norm); 0: not */
   uint32_t seed;            /* of the rounding of 8-bit states */
   float* norm;              /* DEVICE out [1]: the gradients' global 2-norm; NULL: only formed where max_norm asks for it */

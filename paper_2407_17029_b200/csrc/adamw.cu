@@ -90,43 +90,79 @@ __device__ __forceinline__ int aw_find(const AwView& w, uint32_t b, int k) {
 // ---- 256 elements of a warp: lane l holds 4 l + e and 128 + 4 l + e in x[e] and x[4 + e] -------------------------------------
 __device__ __forceinline__ int aw_elem(int lane, int i) { return (i >> 2) * 128 + 4 * lane + (i & 3); }
 
-__device__ __forceinline__ void aw_load_f32(const float* a, long long base, int left, bool wide, int lane, float (&x)[8]) {
-  if (wide && left >= AW_BLOCK) {
+template <bool FULL>
+__device__ __forceinline__ void aw_load_f32(const float* a, long long base, int left, int lane, float (&x)[8]) {
+  if constexpr (FULL) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const float4 v = *reinterpret_cast<const float4*>(a + base + h * 128 + 4 * lane);
       x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? a[base + aw_elem(lane, i)] : 0.f;
+    for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? a[base + aw_elem(lane, i)] : 0.f;
+  }
 }
-__device__ __forceinline__ void aw_store_f32(float* a, long long base, int left, bool wide, int lane, const float (&x)[8]) {
-  if (wide && left >= AW_BLOCK) {
+template <bool FULL>
+__device__ __forceinline__ void aw_store_f32(float* a, long long base, int left, int lane, const float (&x)[8]) {
+  if constexpr (FULL) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
       *reinterpret_cast<float4*>(a + base + h * 128 + 4 * lane) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (aw_elem(lane, i) < left) a[base + aw_elem(lane, i)] = x[i];
+    for (int i = 0; i < 8; ++i)
+      if (aw_elem(lane, i) < left) a[base + aw_elem(lane, i)] = x[i];
+  }
 }
+template <bool FULL>
 __device__ __forceinline__ void aw_load_g(const AwTensor& t, long long base, int left, int lane, float (&x)[8]) {
-  if (!t.g16) { aw_load_f32(static_cast<const float*>(t.g), base, left, t.wide, lane, x); return; }
+  if (!t.g16) { aw_load_f32<FULL>(static_cast<const float*>(t.g), base, left, lane, x); return; }
   const __nv_bfloat16* a = static_cast<const __nv_bfloat16*>(t.g);
-  if (t.wide && left >= AW_BLOCK) {
+  if constexpr (FULL) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint2 v = *reinterpret_cast<const uint2*>(a + base + h * 128 + 4 * lane);
       x[4 * h] = __uint_as_float(v.x << 16); x[4 * h + 1] = __uint_as_float(v.x & 0xffff0000u);
       x[4 * h + 2] = __uint_as_float(v.y << 16); x[4 * h + 3] = __uint_as_float(v.y & 0xffff0000u);
     }
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? __bfloat162float(a[base + aw_elem(lane, i)]) : 0.f;
+    for (int i = 0; i < 8; ++i) x[i] = aw_elem(lane, i) < left ? __bfloat162float(a[base + aw_elem(lane, i)]) : 0.f;
+  }
+}
+
+// Two fp32 operations in one instruction, each rounded by itself.
+__device__ __forceinline__ unsigned long long aw_two(float a, float b) {
+  unsigned long long v;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b));
+  return v;
+}
+__device__ __forceinline__ void aw_split(unsigned long long v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ unsigned long long aw_mul2(unsigned long long a, unsigned long long b) {
+  unsigned long long v;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+  return v;
+}
+__device__ __forceinline__ unsigned long long aw_fma2(unsigned long long a, unsigned long long b, unsigned long long c) {
+  unsigned long long v;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+  return v;
+}
+__device__ __forceinline__ float aw_rcp(float x) {
+  float y;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float aw_sqrt(float x) {
+  float y;
+  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float aw_max(float a, float b) {          // NaN if one is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
 }
 
 // ---- 8-bit states --------------------------------------------------------------------------------------------------------
@@ -135,21 +171,22 @@ __device__ __forceinline__ uint32_t aw_mix(uint32_t x) {
   x = (x ^ (x >> 15)) * 0x5D8E3B97u;
   return x ^ (x >> 16);
 }
-// four e4m3 codes -> fp32 (exact)
-__device__ __forceinline__ void aw_from_codes(uint32_t w, float* x) {
+// eight e4m3 codes -> fp32 (exact) times the scale
+__device__ __forceinline__ void aw_from_codes(const uint32_t (&w)[2], float scale, float (&x)[8]) {
+  const unsigned long long both = aw_two(scale, scale);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
+  for (int h = 0; h < 4; ++h) {
     uint32_t p;
-    asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(p) : "r"(w >> (16 * h)));
+    asm("{\n .reg .b16 c;\n cvt.u16.u32 c, %1;\n cvt.rn.f16x2.e4m3x2 %0, c;\n}" : "=r"(p) : "r"(w[h >> 1] >> (16 * (h & 1))));
     const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p));
-    x[2 * h] = f.x;
-    x[2 * h + 1] = f.y;
+    aw_split(aw_mul2(aw_two(f.x, f.y), both), x[2 * h], x[2 * h + 1]);
   }
 }
-__device__ __forceinline__ void aw_load_codes(const void* a, long long base, int left, bool wide, int lane, float scale, float (&x)[8]) {
+template <bool FULL>
+__device__ __forceinline__ void aw_load_codes(const void* a, long long base, int left, int lane, uint32_t (&w)[2]) {
   const uint8_t* c = static_cast<const uint8_t*>(a);
-  uint32_t w[2] = {0u, 0u};
-  if (wide && left >= AW_BLOCK) {
+  w[0] = w[1] = 0u;
+  if constexpr (FULL) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) w[h] = *reinterpret_cast<const uint32_t*>(c + base + h * 128 + 4 * lane);
   } else {
@@ -157,24 +194,22 @@ __device__ __forceinline__ void aw_load_codes(const void* a, long long base, int
     for (int i = 0; i < 8; ++i)
       if (aw_elem(lane, i) < left) w[i >> 2] |= (uint32_t)c[base + aw_elem(lane, i)] << (8 * (i & 3));
   }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) aw_from_codes(w[h], x + 4 * h);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = __fmul_rn(x[i], scale);
 }
 // The neighbour of y by chance: with y 2^-120, e4m3's exponent is at the lower end of fp32's, where its subnormal numbers are subnormal
 // too, and 20 bits of the mantissa are to go.  What the random bits, added to the upper 16 of them, carry out decides.  `shift`: which 16
-// of the random bits.  Codes in the top byte of z.
+// of the random bits.  Codes in the top byte of z.  The block's largest y may be three units of fp32 above 448 (its factor and the product
+// are rounded): 3 + 16 * 65535 still carries nothing out.
 __device__ __forceinline__ uint32_t aw_round(float y, uint32_t rnd, int shift) {
   const uint32_t bits16 = shift ? rnd >> 16 : rnd & 0xffffu;
-  return (__float_as_uint(fminf(y, 448.0f * 0x1p-120f)) + (bits16 << 4)) << 4;
+  return (__float_as_uint(y) + (bits16 << 4)) << 4;
 }
-__device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long base, int left, bool wide, int lane, const float (&x)[8],
+template <bool FULL>
+__device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long base, int left, int lane, const float (&x)[8],
                                                const uint32_t (&rnd)[8], int shift) {
-  uint32_t all = 0u;                           // the largest magnitude, as bits (which order like the numbers; NaN above all)
+  float most = fabsf(x[0]);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) all = max(all, __float_as_uint(x[i]) & 0x7fffffffu);
-  all = __reduce_max_sync(0xffffffffu, all);
+  for (int i = 1; i < 8; ++i) most = aw_max(most, fabsf(x[i]));
+  uint32_t all = __reduce_max_sync(0xffffffffu, __float_as_uint(most) & 0x7fffffffu);    // bits order like the numbers, NaN above all
   const bool odd = all >= 0x7f800000u;         // NaN or infinity: they do not count
   if (odd) {
     all = 0u;
@@ -193,12 +228,12 @@ __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long 
   for (int h = 0; h < 2; ++h) {
     uint32_t z[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = aw_round(fabsf(x[4 * h + e]) * inv, rnd[4 * h + e], shift);
+    for (int e = 0; e < 4; ++e) z[e] = aw_round(fabsf(x[4 * h + e] * inv), rnd[4 * h + e], shift);
     const uint32_t code = __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
     const float* y = x + 4 * h;
     const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0073),
                                       __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0073), 0x5410);
-    w[h] = code | (sign & 0x80808080u);
+    w[h] = (code & 0x7f7f7f7fu) | (sign & 0x80808080u);
   }
   if (odd) {
 #pragma unroll
@@ -206,7 +241,7 @@ __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long 
       if ((__float_as_uint(x[i]) & 0x7fffffffu) >= 0x7f800000u) w[i >> 2] |= 0x7fu << (8 * (i & 3));
   }
   uint8_t* c = static_cast<uint8_t*>(a);
-  if (wide && left >= AW_BLOCK) {
+  if constexpr (FULL) {
     *reinterpret_cast<uint32_t*>(c + base + 4 * lane) = w[0];
     *reinterpret_cast<uint32_t*>(c + base + 128 + 4 * lane) = w[1];
   } else {
@@ -218,77 +253,164 @@ __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long 
 }
 
 // ---- the step --------------------------------------------------------------------------------------------------------------
+struct AwNow { float factor, lr, up1, up2; uint32_t key; };
+
+// What a block of tensor t is loaded into.
+template <int BITS>
+struct AwRaw { float g[8], p[8], m[BITS == 8 ? 1 : 8], v[BITS == 8 ? 1 : 8], ms, vs; uint32_t cm[2], cv[2]; };
+
+// FULL: 256 elements, every pointer aligned.
+template <int BITS, bool FULL>
+__device__ __forceinline__ void aw_fetch(const AwTensor& t, uint32_t b, int lane, AwRaw<BITS>& r) {
+  const uint32_t mine = b - t.first;
+  const long long base = (long long)mine * AW_BLOCK;
+  const int left = FULL ? AW_BLOCK : (int)min((long long)AW_BLOCK, t.n - base);
+  aw_load_g<FULL>(t, base, left, lane, r.g);
+  aw_load_f32<FULL>(t.p, base, left, lane, r.p);
+  if (BITS == 8 || (BITS == 0 && t.bits8)) {
+    aw_load_codes<FULL>(t.m, base, left, lane, r.cm);
+    aw_load_codes<FULL>(t.v, base, left, lane, r.cv);
+    r.ms = t.m_scale[mine];
+    r.vs = t.v_scale[mine];
+  } else if constexpr (BITS != 8) {
+    aw_load_f32<FULL>(static_cast<const float*>(t.m), base, left, lane, r.m);
+    aw_load_f32<FULL>(static_cast<const float*>(t.v), base, left, lane, r.v);
+  }
+}
+
+template <int BITS, bool FULL>
+__device__ __forceinline__ void aw_update(const AwStep& s, const AwNow& now, const AwTensor& t, uint32_t b, int lane, const AwRaw<BITS>& r) {
+  const uint32_t mine = b - t.first;
+  const long long base = (long long)mine * AW_BLOCK;
+  const int left = FULL ? AW_BLOCK : (int)min((long long)AW_BLOCK, t.n - base);
+  const bool bits8 = BITS == 8 || (BITS == 0 && t.bits8);
+  float p[8], m[8], v[8];
+  const float (&g)[8] = r.g;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) p[i] = r.p[i];
+  if (bits8) {
+    aw_from_codes(r.cm, r.ms, m);
+    aw_from_codes(r.cv, r.vs, v);
+#pragma unroll
+    for (int i = 0; i < 8; i += 2) {
+      const unsigned long long r = aw_two(v[i], v[i + 1]);
+      aw_split(aw_mul2(r, r), v[i], v[i + 1]);
+    }
+  } else if constexpr (BITS != 8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { m[i] = r.m[i]; v[i] = r.v[i]; }
+  }
+  const float rate = now.lr * t.lr_mult;
+  float root[8];
+  const unsigned long long up1 = aw_two(now.up1, now.up1), up2 = aw_two(now.up2, now.up2), eps = aw_two(s.eps, s.eps), decay = aw_two(t.decay, t.decay), back = aw_two(-rate, -rate);
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+#pragma unroll
+    for (int e = i; e < i + 2; ++e) {
+      const float x = __fmul_rn(g[e], now.factor);
+      m[e] = __fadd_rn(__fmul_rn(s.b1, m[e]), __fmul_rn(s.c1, x));
+      v[e] = __fadd_rn(__fmul_rn(s.b2, v[e]), __fmul_rn(s.c2, __fmul_rn(x, x)));
+    }
+    const unsigned long long mm = aw_two(m[i], m[i + 1]);
+    // held in 8 bits, the root is a result itself; in 32 it only divides
+    root[i] = bits8 ? __fsqrt_rn(v[i]) : aw_sqrt(v[i]);
+    root[i + 1] = bits8 ? __fsqrt_rn(v[i + 1]) : aw_sqrt(v[i + 1]);
+    float d0, d1;                              // 0 or at least 2^-75: no flush to zero
+    aw_split(aw_fma2(aw_two(root[i], root[i + 1]), up2, eps), d0, d1);
+    const unsigned long long pp = aw_two(p[i], p[i + 1]);
+    const unsigned long long up = aw_mul2(aw_mul2(mm, up1), aw_two(aw_rcp(d0), aw_rcp(d1)));
+    aw_split(aw_fma2(back, aw_fma2(decay, pp, up), pp), p[i], p[i + 1]);
+  }
+  aw_store_f32<FULL>(t.p, base, left, lane, p);
+  if (t.copy) {
+    if constexpr (FULL) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(p[4 * h], p[4 * h + 1]), c = __floats2bfloat162_rn(p[4 * h + 2], p[4 * h + 3]);
+        *reinterpret_cast<uint2*>(t.copy + base + h * 128 + 4 * lane) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&c));
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (aw_elem(lane, i) < left) t.copy[base + aw_elem(lane, i)] = __float2bfloat16_rn(p[i]);
+    }
+  }
+  if (bits8) {
+    uint32_t rnd[8];
+    const uint32_t e0 = (b * AW_BLOCK + 4 * lane) * 0x9E3779B1u + now.key;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) rnd[i] = aw_mix(e0 + (uint32_t)((i >> 2) * 128 + (i & 3)) * 0x9E3779B1u);
+    aw_store_codes<FULL>(t.m, t.m_scale + mine, base, left, lane, m, rnd, 0);
+    aw_store_codes<FULL>(t.v, t.v_scale + mine, base, left, lane, root, rnd, 16);
+  } else {
+    aw_store_f32<FULL>(static_cast<float*>(t.m), base, left, lane, m);
+    aw_store_f32<FULL>(static_cast<float*>(t.v), base, left, lane, v);
+  }
+}
+
+// Calls f(tensor, first block, blocks) for the blocks of this warp: runs of up to `run` neighbours of one tensor.
+template <class F>
+__device__ __forceinline__ void aw_each(const AwView& w, uint32_t blocks, uint32_t run, F&& f) {
+  const uint32_t warps = gridDim.x * AW_WARPS, me = blockIdx.x * AW_WARPS + (threadIdx.x >> 5);
+  int k = 0;
+  for (unsigned long long b0 = (unsigned long long)me * run; b0 < blocks; b0 += (unsigned long long)warps * run) {
+    uint32_t b = (uint32_t)b0;
+    const uint32_t end = (uint32_t)min((unsigned long long)blocks, b0 + run);
+    while (b < end) {
+      k = aw_find(w, b, k);
+      const AwTensor t = w.table[k];
+      const uint32_t stop = min(end, __ldg(w.first + k + 1));
+      f(t, b, stop - b);
+      b = stop;
+    }
+  }
+}
+__device__ __forceinline__ bool aw_full(const AwTensor& t, uint32_t b) {
+  return t.wide && (long long)(b - t.first + 1) * AW_BLOCK <= t.n;
+}
+// Neighbouring blocks per warp and turn: four where every warp has many turns, else one, so that all SMs have work.
+__device__ __forceinline__ uint32_t aw_run(uint32_t blocks) { return blocks / (gridDim.x * AW_WARPS) >= 16 ? 4u : 1u; }
+
 // BITS: of the states of all tensors; 0: they are mixed
 template <int BITS>
-__global__ void __launch_bounds__(AW_THREADS, BITS == 8 ? 4 : 3) adamw_kernel(const __grid_constant__ AwStep s) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_constant__ AwStep s) {
+  const int lane = threadIdx.x & 31;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const AwView& w = s.w;
   const int taken = *reinterpret_cast<volatile const int*>(s.steps);
-  const float factor = s.clipped ? *reinterpret_cast<volatile const float*>(&w.ctl->factor) : 1.0f;
+  AwNow now;
+  now.factor = s.clipped ? *reinterpret_cast<volatile const float*>(&w.ctl->factor) : 1.0f;
   const uint32_t blocks = w.ctl->blocks;
-  if (factor >= 0.f) {
-    const double now = (double)taken + 1.0;
+  if (now.factor >= 0.f) {
+    const double t = (double)taken + 1.0;
     // 1 - beta^t, without the cancellation that beta^t near 1 would bring
-    const float fix1 = -expm1f((float)(now * s.log_b1)), fix2 = -expm1f((float)(now * s.log_b2));
-    const float lr = *s.lr, up1 = __fdiv_rn(1.0f, fix1), up2 = sqrtf(__fdiv_rn(1.0f, fix2));
-    const uint32_t key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
-    int k = 0;
-    for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
-      k = aw_find(w, b, k);
-      const AwTensor t = w.table[k];
-      const long long base = (long long)(b - t.first) * AW_BLOCK;
-      const int left = (int)min((long long)AW_BLOCK, t.n - base);
-      float g[8], p[8], m[8], v[8];
-      aw_load_g(t, base, left, lane, g);
-      aw_load_f32(t.p, base, left, t.wide, lane, p);
-      const bool bits8 = BITS == 8 || (BITS == 0 && t.bits8);
-      if (bits8) {
-        aw_load_codes(t.m, base, left, t.wide, lane, t.m_scale[b - t.first], m);
-        aw_load_codes(t.v, base, left, t.wide, lane, t.v_scale[b - t.first], v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __fmul_rn(v[i], v[i]);
-      } else {
-        aw_load_f32(static_cast<const float*>(t.m), base, left, t.wide, lane, m);
-        aw_load_f32(static_cast<const float*>(t.v), base, left, t.wide, lane, v);
-      }
-      const float rate = lr * t.lr_mult;
-      float root[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float x = __fmul_rn(g[i], factor);
-        m[i] = __fadd_rn(__fmul_rn(s.b1, m[i]), __fmul_rn(s.c1, x));
-        v[i] = __fadd_rn(__fmul_rn(s.b2, v[i]), __fmul_rn(s.c2, __fmul_rn(x, x)));
-        root[i] = __fsqrt_rn(v[i]);
-        const float up = __fdividef(m[i] * up1, fmaf(root[i], up2, s.eps));
-        p[i] = fmaf(-rate, fmaf(t.decay, p[i], up), p[i]);
-      }
-      aw_store_f32(t.p, base, left, t.wide, lane, p);
-      if (t.copy) {
-        if (t.wide && left >= AW_BLOCK) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const __nv_bfloat162 a = __floats2bfloat162_rn(p[4 * h], p[4 * h + 1]), c = __floats2bfloat162_rn(p[4 * h + 2], p[4 * h + 3]);
-            *reinterpret_cast<uint2*>(t.copy + base + h * 128 + 4 * lane) =
-                make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&c));
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (aw_elem(lane, i) < left) t.copy[base + aw_elem(lane, i)] = __float2bfloat16_rn(p[i]);
+    now.up1 = __fdiv_rn(1.0f, -expm1f((float)(t * s.log_b1)));
+    now.up2 = sqrtf(__fdiv_rn(1.0f, -expm1f((float)(t * s.log_b2))));
+    now.lr = *s.lr;
+    now.key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
+    aw_each(w, blocks, aw_run(blocks), [&](const AwTensor& t, uint32_t b, uint32_t n) {
+      uint32_t i = 0;
+      if (BITS == 8) {                         // few bytes to a block: the loads of two on their way at once
+        for (; i + 2 <= n && aw_full(t, b + i + 1); i += 2) {
+          AwRaw<BITS> r0, r1;
+          aw_fetch<BITS, true>(t, b + i, lane, r0);
+          aw_fetch<BITS, true>(t, b + i + 1, lane, r1);
+          aw_update<BITS, true>(s, now, t, b + i, lane, r0);
+          aw_update<BITS, true>(s, now, t, b + i + 1, lane, r1);
         }
       }
-      if (bits8) {
-        uint32_t rnd[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) rnd[i] = aw_mix((b * AW_BLOCK + aw_elem(lane, i)) * 0x9E3779B1u + key);
-        aw_store_codes(t.m, t.m_scale + (b - t.first), base, left, t.wide, lane, m, rnd, 0);
-        aw_store_codes(t.v, t.v_scale + (b - t.first), base, left, t.wide, lane, root, rnd, 16);
-      } else {
-        aw_store_f32(static_cast<float*>(t.m), base, left, t.wide, lane, m);
-        aw_store_f32(static_cast<float*>(t.v), base, left, t.wide, lane, v);
+      for (; i < n; ++i) {
+        AwRaw<BITS> r;
+        if (aw_full(t, b + i)) {
+          aw_fetch<BITS, true>(t, b + i, lane, r);
+          aw_update<BITS, true>(s, now, t, b + i, lane, r);
+        } else {
+          aw_fetch<BITS, false>(t, b + i, lane, r);
+          aw_update<BITS, false>(s, now, t, b + i, lane, r);
+        }
       }
-    }
+    });
   }
   // every CTA has read the count when the last one comes here
   __syncthreads();
@@ -296,7 +418,7 @@ __global__ void __launch_bounds__(AW_THREADS, BITS == 8 ? 4 : 3) adamw_kernel(co
     __threadfence();
     if (atomicAdd(&w.ctl->step_ticket, 1u) + 1u == gridDim.x) {
       w.ctl->step_ticket = 0u;
-      if (factor >= 0.f) *s.steps = taken + 1;
+      if (now.factor >= 0.f) *s.steps = taken + 1;
     }
   }
 }
@@ -309,17 +431,29 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_con
   const AwView& w = s.w;
   const uint32_t blocks = w.ctl->blocks;
   double sum = 0.0;
-  int k = 0;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the step waits for this grid's end before it reads anything
-  for (uint32_t b = blockIdx.x * AW_WARPS + warp; b < blocks; b += gridDim.x * AW_WARPS) {
-    k = aw_find(w, b, k);
-    const AwTensor t = w.table[k];
-    const long long base = (long long)(b - t.first) * AW_BLOCK;
-    float g[8];
-    aw_load_g(t, base, (int)min((long long)AW_BLOCK, t.n - base), lane, g);
+  auto add = [&](const float (&g)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum = fma((double)g[i], (double)g[i], sum);
-  }
+  };
+  aw_each(w, blocks, aw_run(blocks), [&](const AwTensor& t, uint32_t b, uint32_t n) {
+    const long long base = (long long)(b - t.first) * AW_BLOCK;
+    uint32_t i = 0;
+    for (; i + 4 <= n && aw_full(t, b + i + 3); i += 4) {
+      float g[4][8];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) aw_load_g<true>(t, base + (i + j) * AW_BLOCK, AW_BLOCK, lane, g[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) add(g[j]);
+    }
+    for (; i < n; ++i) {
+      float g[8];
+      const long long at = base + i * AW_BLOCK;
+      if (aw_full(t, b + i)) aw_load_g<true>(t, at, AW_BLOCK, lane, g);
+      else aw_load_g<false>(t, at, (int)min((long long)AW_BLOCK, t.n - at), lane, g);
+      add(g);
+    }
+  });
   auto join = [&](double x) {                  // over the CTA; the result in thread 0
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
@@ -425,7 +559,7 @@ int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t bl
   if (kinds > 3 || blocks > 0x7fffffff) return QBLORA_ERR_INVALID_ARG;
   if (!ptr_ok(cfg->lr, 4) || !ptr_ok(cfg->steps, 4) || (cfg->norm && !ptr_ok(cfg->norm, 4))) return QBLORA_ERR_INVALID_ARG;
   if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return QBLORA_ERR_INVALID_ARG;
-  if (!(cfg->eps >= 0.0 && std::isfinite(cfg->eps)) || !(cfg->max_norm >= 0.0 && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
+  if (!(cfg->eps == 0.0 || (cfg->eps >= FLT_MIN && cfg->eps <= FLT_MAX)) || !(cfg->max_norm >= 0.0 && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adamw_workspace_bytes(n_tensors)) return QBLORA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   AwStep s{};
@@ -447,7 +581,7 @@ int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t bl
     count_launch();
     QB_CUDA(cudaGetLastError());
   }
-  int64_t grid = (kinds == 2 ? 4LL : 3LL) * sms;
+  int64_t grid = 3LL * sms;
   if (grid > want) grid = want;
   if (grid < 1) grid = 1;
   cudaLaunchConfig_t lc = {};
