@@ -505,7 +505,7 @@ int qblora_adapter_plan(const int32_t* cu, const int32_t* ids, int32_t n_request
  *   rows [tokens], start [n_adapters + 1]: DEVICE int32, as written by qblora_adapter_plan (each row at most once; entries out of
  *   range are passed over).  X DEVICE bf16, x_stride elements between rows; Y DEVICE bf16 or fp32 (y_dtype), y_stride likewise;
  *   X and Y do not overlap.  x' and x' A are carried as pairs of bf16 numbers, within 2^-16.
- * Any sizes; rank and Q multiples of 8, rank <= 256, d_in, d_out and the strides multiples of 8 and all tensors 16-byte
+ * Any sizes; rank and Q multiples of 8, d_in, d_out and the strides multiples of 8 and all tensors 16-byte
  * aligned take the fast kernels.
  *   ws: qblora_adapters_workspace_bytes(bank, tokens, 0) bytes.
  */

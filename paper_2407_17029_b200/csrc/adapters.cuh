@@ -45,4 +45,11 @@ size_t simt_adapters_ws_bytes(const BankView& k, int64_t T, bool backward);
 int simt_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st);
 int simt_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st);
 
+// Tensor cores (tc_adapters.cu): rank and Q multiples of 8, rows of multiples of 8 elements, 16-byte aligned.
+bool tc_adapters_sizes_ok(const BankView& k, int64_t T);
+bool tc_adapters_supported(const AdaptersCall& c);
+size_t tc_adapters_ws_bytes(const BankView& k, int64_t T, bool backward);
+int tc_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st);
+int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st);
+
 }  // namespace qb

@@ -1,5 +1,8 @@
 // extern "C" entry points of the bank of adapters (include/qblora.h, last part): host-side argument checks and dispatch.
 // No device memory is allocated here.
+#include <algorithm>
+#include <cstdlib>
+
 #include "adapters.cuh"
 
 namespace qb {
@@ -25,6 +28,11 @@ bool rows_ok(const void* data, int64_t stride, int width, int dtype, RowsView* v
   if (reinterpret_cast<uintptr_t>(data) % (dtype == QBLORA_F32 ? 4 : 2)) return false;
   *v = {const_cast<void*>(data), stride, dtype};
   return true;
+}
+
+bool force_general() {
+  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
+  return e && e[0] == '1';
 }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
@@ -63,7 +71,9 @@ int qblora_adapter_plan(const int32_t* cu, const int32_t* ids, int32_t n_request
 size_t qblora_adapters_workspace_bytes(const qblora_adapter_bank* bank, int64_t tokens, int backward) {
   BankView k;
   if (!bank_ok(bank, false, &k) || tokens < 1 || tokens >= (int64_t)1 << 31) return 0;
-  return simt_adapters_ws_bytes(k, tokens, backward != 0);
+  // alignment, which the sizes do not tell, may send a call to the general path
+  const size_t general = simt_adapters_ws_bytes(k, tokens, backward != 0);
+  return tc_adapters_sizes_ok(k, tokens) ? std::max(general, tc_adapters_ws_bytes(k, tokens, backward != 0)) : general;
 }
 
 int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, const int32_t* start, const void* X,
@@ -74,6 +84,7 @@ int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, co
   if (rc) return rc;
   if (!rows_ok(X, x_stride, bank->d_in, QBLORA_BF16, &c.X) || !rows_ok(Y, y_stride, bank->d_out, y_dtype, &c.Y) || X == Y) return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adapters_workspace_bytes(bank, tokens, 0)) return QBLORA_ERR_WORKSPACE;
+  if (!force_general() && tc_adapters_supported(c)) return tc_adapters_fwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
   return simt_adapters_fwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
 }
 
@@ -90,6 +101,7 @@ int qblora_adapters_bwd(const qblora_adapter_bank* bank, const int32_t* rows, co
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adapters_workspace_bytes(bank, tokens, 1)) return QBLORA_ERR_WORKSPACE;
   if (!dX && !dA && !dB) return QBLORA_OK;
   c.dA = dA; c.dB = dB;
+  if (!force_general() && tc_adapters_supported(c)) return tc_adapters_bwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
   return simt_adapters_bwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
 }
 

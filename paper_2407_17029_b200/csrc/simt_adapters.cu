@@ -118,6 +118,7 @@ size_t simt_adapters_ws_bytes(const BankView& k, int64_t T, bool backward) {
 #define QB_TRY(call) do { const int rc_ = (call); if (rc_) return rc_; } while (0)
 
 int simt_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
+  QB_CUDA(cudaMemsetAsync(ws, 0, 16, st));       // status word
   const BankView& k = c.k;
   const SimtScratch s = scratch(k, c.T, ws);
   const unsigned T = (unsigned)c.T;
@@ -130,6 +131,7 @@ int simt_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
 }
 
 int simt_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
+  QB_CUDA(cudaMemsetAsync(ws, 0, 16, st));
   const BankView& k = c.k;
   const SimtScratch s = scratch(k, c.T, ws);
   const unsigned T = (unsigned)c.T;
