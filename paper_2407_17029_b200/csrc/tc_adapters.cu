@@ -3,19 +3,21 @@
 //
 // The adapter's products are thin: their operands are small beside X, Y and dX, which pass once.  So three kinds of kernels, all
 // over the rows in the plan's order, where every adapter's rows are neighbours:
-//   pool    x' of every row (and the sums of dY's neighbours) as pairs of bf16 numbers, hi + lo: reads X at the memory's rate
-//   shrink  u = x' A (and du = dv B^T): the pairs in, pairs out
+//   pool    x' of every row (and the sums of dY's neighbours) as two or three bf16 parts: reads X at the memory's rate
+//   shrink  u = x' A (and du = dv B^T): parts in, parts out
 //   spread  Y += s repeat(u B) (and dX += repeat(du A^T) / lambda): the memory-bound end
 //   grad    dA = x'^T du, dB = u^T dv: sums over an adapter's rows
 // In shrink and spread the weights are the 128 rows of the tensor core's tile and the tokens its columns, 16 to 128 of them as an
-// adapter has rows: a lone decoding row costs a tile of 16, not of 128, and in the result a warp's lanes are neighbouring
-// outputs, so that Y is read and written in whole lines straight from tensor memory.  Pairs: one bf16 number would put 2^-9 on
-// everything that the adapter adds; hi and lo are two MMAs with the same weights, 2^-16 at worst.
+// adapter has rows: a lone decoding row costs a tile of 16, not of 128.
+//
+// Parts: a number in fp32 is the sum of bf16 numbers, each the rounding of what the ones before leave.  One would put 2^-9 on everything
+// that the adapter adds; two leave 2^-16 and are taken where the result is bf16; results in fp32 take three (2^-24, the rounding of
+// fp32 itself).  Each part is an MMA with the same weights; x' of lambda = 1 is a bf16 number, one part.
 //
 // Rows in the workspace: adapter a's begin at a multiple of 16 (pad[a]) and are filled up to one with zeros, so that the sums over
 // rows in grad run in whole steps of 16.  Which adapter has which tile is found by every CTA for itself from the plan's offsets.
 //
-// All loops are persistent: 148 CTAs take the (row tile, weight tile) units in turn; warp 0 loads by TMA, warp 1 issues the MMAs, eight
+// All loops are persistent: one CTA per SM takes the units in turn; warp 0 loads by TMA, warp 1 issues the MMAs, eight
 // warps empty one accumulator while the next is filled.
 #include <algorithm>
 #include <atomic>
@@ -29,11 +31,13 @@ using namespace ptx;
 namespace {
 
 constexpr int AG_THREADS = 320, AG_EPI = 256;       // TMA warp, MMA warp, eight epilogue warps
-constexpr int AG_TN = 128;                          // most rows of a tile
-constexpr int AG_PART = 16384;                      // bytes of one 128 x 64 operand tile
+constexpr int AG_TILE = 16384;                      // bytes of one 128 x 64 operand tile
 constexpr int AG_POOL_THREADS = 256;
+constexpr int AG_SMEM = 232448 - 1024 - 512;        // of a CTA, without alignment and static variables
+constexpr int AG_BARS = 512;                        // of those, barriers
 
 // ---- adapters' rows: where they lie in the workspace, and their tiles ------------------------------------------------------------
+size_t ag_table_bytes(int n) { return (size_t)2 * (n + 1) * 4; }
 struct AgGroups {
   const uint32_t* pad;      // [n + 1] first row of each adapter in the workspace, multiples of 16
   const uint32_t* tile;     // [n + 1] tiles in front of it
@@ -42,8 +46,9 @@ struct AgGroups {
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }   // both below 2^31
 
 // by the whole CTA; s: 2 (n + 1) words of shared memory
+// tn: rows of a tile
 template <int NT>
-__device__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_there) {
+__device__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_there, int tn) {
   __shared__ uint32_t s_part[2][NT / 32];
   __shared__ int s_kept;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = c.k.n;
@@ -52,7 +57,7 @@ __device__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_
   uint32_t mine = 0, tiles = 0;
   for (int a = lo; a < hi; ++a) {
     const uint32_t rows = (uint32_t)max(plan_start(c, a + 1) - plan_start(c, a), 0);
-    const uint32_t p = (min(rows, 0x7ffffff0u) + 15u) & ~15u, t = (rows + AG_TN - 1) / AG_TN;
+    const uint32_t p = (min(rows, 0x7ffffff0u) + 15u) & ~15u, t = (rows + tn - 1) / tn;
     pad[a] = p;
     tile[a] = t;
     mine = sat_add(mine, p);
@@ -96,39 +101,62 @@ __device__ __forceinline__ int ag_find(const uint32_t* v, int n, uint32_t x) {
 }
 
 // ---- pool ---------------------------------------------------------------------------------------------------------------------
+// A matrix of rows in the workspace in np parts: element (part, row, i) at part * stride + row * ld + i.
+struct Parts { __nv_bfloat16* p; int np, width, ld; int64_t stride; };
+
 struct AgPool {
   RowsView x;
-  int d, lam, small, ld, wide;          // elements of a row, of its pooled form and its pitch; wide: 16-byte loads, lam a power of two
+  int d, lam, wide;                     // elements of a row, pooled by lam; wide: 16-byte loads, lam a power of two
   float factor;                         // 1 / lam or 1
-  __nv_bfloat16 *hi, *lo;               // lo == nullptr: the pooled values are bf16 numbers already (lam 1)
+  Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
 struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; };
 
-__device__ __forceinline__ void ag_pair(float x, __nv_bfloat16& hi, __nv_bfloat16& lo) {
-  hi = __float2bfloat16_rn(x);
-  lo = __float2bfloat16_rn(x - __bfloat162float(hi));
-}
 __device__ __forceinline__ float ag_low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float ag_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
 
-// One row by one warp.  x: nullptr for a row of zeros.
-__device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t out, int lane) {
-  __nv_bfloat16 *hi = p.hi + out * p.ld, *lo = p.lo ? p.lo + out * p.ld : nullptr;
-  if (!x) {
-    for (int i = lane; i < p.small; i += 32) {
-      hi[i] = __float2bfloat16_rn(0.f);
-      if (lo) lo[i] = __float2bfloat16_rn(0.f);
+// N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
+template <int N>
+__device__ __forceinline__ void ag_store_parts(const Parts& o, int64_t at, const float (&x)[N]) {
+  float left[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) left[i] = x[i];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    if (k >= o.np) break;
+    __nv_bfloat16* out = o.p + k * o.stride + at;
+    if constexpr (N == 1) {
+      const __nv_bfloat16 h = __float2bfloat16_rn(left[0]);
+      *out = h;
+      left[0] -= __bfloat162float(h);
+    } else {
+      uint32_t h[N / 2];
+#pragma unroll
+      for (int i = 0; i < N / 2; ++i) {
+        h[i] = pack_bf16x2(left[2 * i], left[2 * i + 1]);
+        left[2 * i] -= ag_low(h[i]);
+        left[2 * i + 1] -= ag_high(h[i]);
+      }
+      if constexpr (N == 2) *reinterpret_cast<uint32_t*>(out) = h[0];
+      else *reinterpret_cast<uint2*>(out) = make_uint2(h[0], h[1]);
     }
+  }
+}
+
+// One row by one warp.  x: nullptr for a row of zeros.
+__device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row, int lane) {
+  const int64_t at = row * p.out.ld;
+  if (!x) {
+    const float zero[1] = {0.f};
+    for (int i = lane; i < p.out.width; i += 32) ag_store_parts<1>(p.out, at + i, zero);
     return;
   }
   if (!p.wide) {
-    for (int i = lane; i < p.small; i += 32) {
-      float acc = 0.f;
-      for (int l = 0; l < p.lam; ++l) acc += __bfloat162float(x[(int64_t)i * p.lam + l]);
-      __nv_bfloat16 h, l;
-      ag_pair(p.factor == 1.f ? acc : acc / (float)p.lam, h, l);
-      hi[i] = h;
-      if (lo) lo[i] = l;
+    for (int i = lane; i < p.out.width; i += 32) {
+      float acc[1] = {0.f};
+      for (int l = 0; l < p.lam; ++l) acc[0] += __bfloat162float(x[(int64_t)i * p.lam + l]);
+      if (p.factor != 1.f) acc[0] /= (float)p.lam;
+      ag_store_parts<1>(p.out, at + i, acc);
     }
     return;
   }
@@ -139,49 +167,35 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t out
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int ch = c0 + u * 32 + lane;
-      w[u] = ch < chunks ? *reinterpret_cast<const uint4*>(x + 8 * (int64_t)ch) : make_uint4(0, 0, 0, 0);
+      w[u] = ch < chunks ? __ldcs(reinterpret_cast<const uint4*>(x) + ch) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int ch = c0 + u * 32 + lane;
+      const bool there = ch < chunks;
       const uint32_t e[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
       if (p.lam == 1) {
-        if (ch < chunks) *reinterpret_cast<uint4*>(hi + 8 * (int64_t)ch) = w[u];
+        if (there) *reinterpret_cast<uint4*>(p.out.p + at + 8 * (int64_t)ch) = w[u];
         continue;
       }
       float s[4];                                       // sums of neighbouring two
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[i] = ag_low(e[i]) + ag_high(e[i]);
       if (p.lam == 2) {
-        if (ch < chunks) {
-          __nv_bfloat16 h[4], l[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) ag_pair(s[i] * p.factor, h[i], l[i]);
-          *reinterpret_cast<uint2*>(hi + 4 * (int64_t)ch) = *reinterpret_cast<const uint2*>(h);
-          *reinterpret_cast<uint2*>(lo + 4 * (int64_t)ch) = *reinterpret_cast<const uint2*>(l);
-        }
+        for (int i = 0; i < 4; ++i) s[i] *= p.factor;
+        if (there) ag_store_parts<4>(p.out, at + 4 * (int64_t)ch, s);
         continue;
       }
-      const float f0 = s[0] + s[1], f1 = s[2] + s[3];
+      const float f[2] = {(s[0] + s[1]) * p.factor, (s[2] + s[3]) * p.factor};
       if (p.lam == 4) {
-        if (ch < chunks) {
-          __nv_bfloat16 h[2], l[2];
-          ag_pair(f0 * p.factor, h[0], l[0]);
-          ag_pair(f1 * p.factor, h[1], l[1]);
-          *reinterpret_cast<uint32_t*>(hi + 2 * (int64_t)ch) = *reinterpret_cast<const uint32_t*>(h);
-          *reinterpret_cast<uint32_t*>(lo + 2 * (int64_t)ch) = *reinterpret_cast<const uint32_t*>(l);
-        }
+        if (there) ag_store_parts<2>(p.out, at + 2 * (int64_t)ch, f);
         continue;
       }
-      float g = f0 + f1;                                // of eight; lam / 8 lanes have the rest
+      float g[1] = {f[0] + f[1]};                       // of eight; lam / 8 lanes have the rest
       const int lanes = p.lam >> 3;
-      for (int d = 1; d < lanes; d <<= 1) g += __shfl_xor_sync(0xffffffffu, g, d);
-      if (ch < chunks && (ch & (lanes - 1)) == 0) {
-        __nv_bfloat16 h, l;
-        ag_pair(g * p.factor, h, l);
-        hi[ch / lanes] = h;
-        lo[ch / lanes] = l;
-      }
+      for (int d = 1; d < lanes; d <<= 1) g[0] += __shfl_xor_sync(0xffffffffu, g[0], d);
+      if (there && (ch & (lanes - 1)) == 0) ag_store_parts<1>(p.out, at + ch / lanes, g);
     }
   }
 }
@@ -190,7 +204,7 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
   extern __shared__ uint32_t ag_smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
-  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there);
+  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128);
   const int lane = threadIdx.x & 31, warps = AG_POOL_THREADS / 32;
   const uint32_t rows = g.pad[g.kept];
   for (int64_t i = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); i < (int64_t)rows * p.sources; i += (int64_t)gridDim.x * warps) {
@@ -205,289 +219,115 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
   }
 }
 
-// ---- shrink, spread, grad --------------------------------------------------------------------------------------------------------
-enum { AG_SHRINK = 0, AG_SPREAD = 1, AG_GRAD = 2 };
-
-struct AgMaps {
-  CUtensorMap w;                        // shrink, spread: the bank's matrix, three dimensions
-  CUtensorMap hi, lo, hi16, lo16;       // their rows: boxes of 128 and of 16.  grad: x' and du
-  CUtensorMap hi2, lo2, u_hi, u_lo;     // grad: (hi, lo) x', (hi2, lo2) du, (u_hi, u_lo) u, (hi16, lo16) dv; boxes 64 x 64
-};
-struct AgParams {
+// ---- shrink -------------------------------------------------------------------------------------------------------------------
+struct AgShrink {
   AdaptersCall c;
   uint32_t rows_there;
-  int m_tiles, M;                       // shrink: of the rank; spread: of Q or P
-  int K;                                // shrink: P or Q
-  int w_kmajor;                         // the weight's contiguous dimension is the contraction's
-  int lo_on, lo2_on;                    // x' (dv) has a lo part
-  int scaled;                           // times the adapter's factor
-  __nv_bfloat16 *hi, *lo; int ld;       // shrink: out
-  RowsView y; int lam; float factor;    // spread
-  float *dA, *dB;                       // grad
+  int tn, stages, np;                   // rows of a tile; of the ring; parts of the input
+  int m_tiles, K, w_kmajor, scaled;     // tiles of 128 ranks; contraction; the weight's contiguous dimension is the contraction's;
+                                        // times the adapter's factor
+  Parts out;
   int* status;
   long long wait_limit;
 };
+struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the rows' parts in boxes of tn rows and of 16
 
-// One unit of work: a tile of 128 weights' rows by the rows of one adapter's tile; grad: 128 by 128 of dA or dB.
-struct AgUnit {
-  int a, m0, n0;                        // adapter, first row and (grad) column of the result
-  uint32_t at;                          // first row in the workspace
-  int j, rows, n16;                     // first entry in the plan, rows, rows or columns in whole steps
-  int steps;                            // of 16 along the contraction; 0: nothing to contract
-  int which;                            // grad: 0 dA, 1 dB
-  int rank;
-};
-
-template <int KIND>
-struct AgWork {
-  const AgParams& p;
-  const AgGroups& g;
-  int ta, tb, na, nb;                   // grad: tiles of dA (ta x na) and dB (tb x nb)
-  long long units;
-  __device__ AgWork(const AgParams& p_, const AgGroups& g_) : p(p_), g(g_) {
-    if (KIND == AG_GRAD) {
-      const BankView& k = p.c.k;
-      na = p.dA ? (k.r + 127) / 128 : 0;
-      ta = (k.P + 127) / 128;
-      tb = p.dB ? (k.r + 127) / 128 : 0;
-      nb = (k.Q + 127) / 128;
-      units = (long long)k.n * (ta * na + tb * nb);
-    } else {
-      units = (long long)g.tile[g.kept] * p.m_tiles;
-    }
-  }
-  __device__ __forceinline__ void get(long long u, AgUnit& t) const {
-    const BankView& k = p.c.k;
-    if (KIND == AG_GRAD) {
-      const int per = ta * na + tb * nb;
-      t.a = (int)(u / per);
-      int x = (int)(u - (long long)t.a * per);
-      t.which = x >= ta * na;
-      if (t.which) x -= ta * na;
-      const int cols = t.which ? nb : na;
-      t.m0 = x / cols * 128;
-      t.n0 = x % cols * 128;
-      t.rank = bank_rank(k, t.a);
-      t.n16 = min(128, ((t.which ? k.Q : k.r) - t.n0 + 15) & ~15);
-      t.at = t.a < g.kept ? g.pad[t.a] : 0;
-      t.rows = t.a < g.kept ? (int)(g.pad[t.a + 1] - g.pad[t.a]) : 0;
-      t.steps = (t.which ? t.m0 : t.n0) < t.rank ? t.rows / 16 : 0;
-      t.j = 0;
-    } else {
-      const uint32_t tile = (uint32_t)(u / p.m_tiles);
-      t.a = ag_find(g.tile, g.kept, tile);
-      const int i = (int)(tile - g.tile[t.a]) * AG_TN, s0 = plan_start(p.c, t.a);
-      t.at = g.pad[t.a] + i;
-      t.j = s0 + i;
-      t.rows = min(AG_TN, plan_start(p.c, t.a + 1) - t.j);
-      t.n16 = (t.rows + 15) & ~15;
-      t.m0 = (int)(u - (long long)tile * p.m_tiles) * 128;
-      t.n0 = 0;
-      t.which = 0;
-      t.rank = bank_rank(k, t.a);
-      t.steps = KIND == AG_SHRINK ? (t.m0 < t.rank ? (p.K + 15) / 16 : 0) : (t.rank + 15) / 16;
-    }
-  }
-};
-
-template <int KIND> struct AgShape {
-  static constexpr int A_PARTS = KIND == AG_GRAD ? 2 : 1;          // 128 x 64: weights, or the pair of x' or u
-  static constexpr int STAGE = (A_PARTS + 2) * AG_PART;            // and a pair of 64 x up to 128
-  static constexpr int STAGES = KIND == AG_GRAD ? 3 : 4;
-  static constexpr int COLS = KIND == AG_GRAD ? 256 : 128;         // tensor memory of one accumulator
-};
-template <int KIND> size_t ag_smem_bytes(int n) {
-  return (size_t)AgShape<KIND>::STAGES * AgShape<KIND>::STAGE + 1024 + 256 + (size_t)2 * (n + 1) * 4;
+// A tile of one adapter's rows.
+struct AgRows { int a, j, rows, n16; uint32_t at; };   // adapter, first entry in the plan, rows, the same in steps of 16, place in the workspace
+__device__ __forceinline__ AgRows ag_rows(const AdaptersCall& c, const AgGroups& g, uint32_t tile, int tn) {
+  AgRows t;
+  t.a = ag_find(g.tile, g.kept, tile);
+  const int i = (int)(tile - g.tile[t.a]) * tn;
+  t.at = g.pad[t.a] + i;
+  t.j = plan_start(c, t.a) + i;
+  t.rows = min(tn, plan_start(c, t.a + 1) - t.j);
+  t.n16 = (t.rows + 15) & ~15;
+  return t;
 }
-
-// y[0 .. W bytes) += x at element type F32 or bf16, W = 2, 4, 8, 16
-template <int W, bool F32> struct AgVec;
-template <> struct AgVec<2, false> { using T = uint16_t; };
-template <> struct AgVec<4, false> { using T = uint32_t; };
-template <> struct AgVec<8, false> { using T = uint2; };
-template <> struct AgVec<16, false> { using T = uint4; };
-template <> struct AgVec<4, true> { using T = float; };
-template <> struct AgVec<8, true> { using T = float2; };
-template <> struct AgVec<16, true> { using T = float4; };
-template <class T, bool F32>
-__device__ __forceinline__ T ag_add(T y, float x) {
-  if constexpr (F32) {
-    float* e = reinterpret_cast<float*>(&y);
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 4); ++i) e[i] += x;
-  } else if constexpr (sizeof(T) == 2) {
-    const __nv_bfloat16 b = __float2bfloat16_rn(__uint_as_float((uint32_t)y << 16) + x);
-    y = *reinterpret_cast<const uint16_t*>(&b);
+// Rows of part `part`, 64 columns from k0 on.  Returns nothing: the bytes are n16 * 128.
+__device__ __forceinline__ void ag_load_rows(const AgMaps3& maps, uint32_t dst, uint32_t bar, int k0, const AgRows& t, int tn, int part) {
+  if (t.n16 == tn) {
+    tma_load_3d(dst, &maps.rows, bar, k0, (int)t.at, part);
   } else {
-    uint32_t* e = reinterpret_cast<uint32_t*>(&y);
-#pragma unroll
-    for (int i = 0; i < (int)(sizeof(T) / 4); ++i) e[i] = pack_bf16x2(ag_low(e[i]) + x, ag_high(e[i]) + x);
+    for (int i = 0; i < t.n16; i += 16) tma_load_3d(dst + i * 128, &maps.rows16, bar, k0, (int)t.at + i, part);
   }
-  return y;
+}
+// 128 rows m of the bank's matrix, 64 of the contraction
+__device__ __forceinline__ void ag_load_weights(const AgMaps3& maps, uint32_t dst, uint32_t bar, bool kmajor, int k0, int m0, int a) {
+  if (kmajor) {
+    tma_load_3d(dst, &maps.w, bar, k0, m0, a);
+  } else {
+    tma_load_3d(dst, &maps.w, bar, m0, k0, a);
+    tma_load_3d(dst + 8192, &maps.w, bar, m0 + 64, k0, a);
+  }
+}
+// D fp32, A and B bf16; transposed: the operand's rows, not the contraction, are contiguous
+__device__ __forceinline__ uint32_t ag_idesc(bool a_transposed, bool b_transposed, int n) {
+  return (1u << 4) | (1u << 7) | (1u << 10) | ((a_transposed ? 1u : 0u) << 15) | ((b_transposed ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
+         ((uint32_t)(128 >> 4) << 24);
+}
+// step e (of 16) of a 64-wide block of the contraction
+__device__ __forceinline__ uint64_t ag_desc(uint32_t block, bool transposed, int e) {
+  return transposed ? smem_desc(block + e * 2048, 8192, 1024) : smem_desc(block + e * 32, 16, 1024);
 }
 
-// 32 columns (rows of Y, numbers in `row` of lane j, -1: none) of 32 weights' rows from m on, one per lane, in v.
-template <int W, bool F32>
-__device__ __forceinline__ void ag_spread_narrow(const AgParams& p, const float (&v)[32], int row, int m, bool there) {
-  using V = typename AgVec<W, F32>::T;
-  char* base = static_cast<char*>(p.y.data) + (int64_t)m * W;
-  const int64_t pitch = p.y.stride * (F32 ? 4 : 2);
-#pragma unroll
-  for (int j0 = 0; j0 < 32; j0 += 8) {
-    V y[8];
-    int r[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      r[j] = __shfl_sync(0xffffffffu, row, j0 + j);
-      if (!there) r[j] = -1;
-      if (r[j] >= 0) y[j] = *reinterpret_cast<const V*>(base + r[j] * pitch);
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (r[j] >= 0) *reinterpret_cast<V*>(base + r[j] * pitch) = ag_add<V, F32>(y[j], v[j0 + j]);
-  }
-}
-// lam elements of 16 * per bytes: chunk i of 16 bytes of the 32 weights' rows belongs to row i / per
-template <bool F32>
-__device__ __forceinline__ void ag_spread_wide(const AgParams& p, const float (&v)[32], int row, int m_first, int per, int M, int lane) {
-  using V = typename AgVec<16, F32>::T;
-  char* base = static_cast<char*>(p.y.data) + (int64_t)m_first * per * 16;
-  const int64_t pitch = p.y.stride * (F32 ? 4 : 2);
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const int r = __shfl_sync(0xffffffffu, row, j);
-    if (r < 0) continue;
-    char* out = base + r * pitch;
-#pragma unroll 1
-    for (int i0 = 0; i0 < per; i0 += 4) {
-      V y[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ch = (i0 + i) * 32 + lane;
-        if (i0 + i < per && m_first + ch / per < M) y[i] = *reinterpret_cast<const V*>(out + (int64_t)ch * 16);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int ch = (i0 + i) * 32 + lane;
-        const float x = __shfl_sync(0xffffffffu, v[j], min(ch / per, 31));
-        if (i0 + i < per && m_first + ch / per < M) *reinterpret_cast<V*>(out + (int64_t)ch * 16) = ag_add<V, F32>(y[i], x);
-      }
-    }
-  }
-}
-// any lam
-__device__ __forceinline__ void ag_spread_any(const AgParams& p, const float (&v)[32], int row, int m, bool there) {
-#pragma unroll
-  for (int j = 0; j < 32; ++j) {
-    const int r = __shfl_sync(0xffffffffu, row, j);
-    if (r < 0 || !there) continue;
-    const int64_t at = r * p.y.stride + (int64_t)m * p.lam;
-    for (int l = 0; l < p.lam; ++l) {
-      if (p.y.dtype == QBLORA_F32) static_cast<float*>(p.y.data)[at + l] += v[j];
-      else {
-        __nv_bfloat16* y = static_cast<__nv_bfloat16*>(p.y.data) + at + l;
-        *y = __float2bfloat16_rn(__bfloat162float(*y) + v[j]);
-      }
-    }
-  }
-}
-template <bool F32>
-__device__ __forceinline__ void ag_spread(const AgParams& p, const float (&v)[32], int row, int m_first, int M, int lane) {
-  const int w = p.lam * (F32 ? 4 : 2);
-  const bool there = m_first + lane < M;
-  if (w == 16) ag_spread_narrow<16, F32>(p, v, row, m_first + lane, there);
-  else if (w == 8) ag_spread_narrow<8, F32>(p, v, row, m_first + lane, there);
-  else if (w == 4) ag_spread_narrow<4, F32>(p, v, row, m_first + lane, there);
-  else if (!F32 && w == 2) ag_spread_narrow<F32 ? 4 : 2, F32>(p, v, row, m_first + lane, there);
-  else if (w % 16 == 0) ag_spread_wide<F32>(p, v, row, m_first, w / 16, M, lane);
-  else ag_spread_any(p, v, row, m_first + lane, there);
-}
-
-template <int KIND>
-__global__ void __launch_bounds__(AG_THREADS, 1) adapters_gemm_kernel(const __grid_constant__ AgMaps maps, const __grid_constant__ AgParams p) {
-  using Sh = AgShape<KIND>;
-  constexpr int STAGES = Sh::STAGES;
+__global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __grid_constant__ AgMaps3 maps, const __grid_constant__ AgShrink p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
-  const uint32_t bars = base + STAGES * Sh::STAGE;
-  auto full = [&](int s) { return bars + 8u * s; };
-  auto empty = [&](int s) { return bars + 8u * (STAGES + s); };
-  auto accfull = [&](int b) { return bars + 8u * (2 * STAGES + b); };
-  auto accempty = [&](int b) { return bars + 8u * (2 * STAGES + 2 + b); };
-  const uint32_t tmem_slot = bars + 8u * (2 * STAGES + 4);
+  const uint32_t stage_bytes = AG_TILE + (uint32_t)p.np * p.tn * 128, bars = base + p.stages * stage_bytes;
+  auto full = [&](int s) { return bars + 16u * s; };
+  auto empty = [&](int s) { return bars + 16u * s + 8; };
+  auto accfull = [&](int b) { return bars + 16u * p.stages + 8u * b; };
+  auto accempty = [&](int b) { return bars + 16u * p.stages + 16 + 8u * b; };
+  const uint32_t tmem_slot = bars + 16u * p.stages + 32;
   volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
-  uint32_t* table = reinterpret_cast<uint32_t*>(smem_raw + (bars + 256 - raw));
-
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
-    for (int s = 0; s < STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int s = 0; s < p.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
     for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(2 * Sh::COLS) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups groups = ag_groups<AG_THREADS>(p.c, table, p.rows_there);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot_g;
-  const AgWork<KIND> work(p, groups);
+  const long long units = (long long)g.tile[g.kept] * p.m_tiles;
+  const int steps = (p.K + 15) / 16;
   asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
-
+  // unit u: tile u / m_tiles, ranks from 128 (u % m_tiles) on; an adapter of a lower rank has none there
+  auto unit = [&](long long u, AgRows& t, int& m0) {
+    const uint32_t tile = (uint32_t)(u / p.m_tiles);
+    m0 = (int)(u - (long long)tile * p.m_tiles) * 128;
+    t = ag_rows(p.c, g, tile, p.tn);
+    return m0 < bank_rank(p.c.k, t.a);
+  };
+  AgRows t;
+  int m0;
   if (warp == 0) {
     if (lane == 0) {
       uint32_t it = 0, ph = 0;
       int s = 0;
       bool ok = true;
-      for (long long u = blockIdx.x; u < work.units && ok; u += gridDim.x) {
-        AgUnit t;
-        work.get(u, t);
-        for (int k = 0; k < t.steps; k += 4, ++it) {
+      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        if (!unit(u, t, m0)) continue;
+        for (int k = 0; k < steps; k += 4, ++it) {
           if (!mbar_wait(empty(s), ph ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          const uint32_t a = base + s * Sh::STAGE, b = a + Sh::A_PARTS * AG_PART;
-          const int k0 = k * 16;
-          if (KIND == AG_GRAD) {
-            const CUtensorMap *ah = t.which ? &maps.u_hi : &maps.hi, *al = t.which ? &maps.u_lo : &maps.lo;
-            const CUtensorMap *bh = t.which ? &maps.hi16 : &maps.hi2, *bl = t.which ? &maps.lo16 : &maps.lo2;
-            const bool a_lo = t.which ? true : p.lo_on, b_lo = t.which ? p.lo2_on : true;
-            const int nb = (t.n16 + 63) / 64, y0 = (int)t.at + k0;
-            mbar_arrive_expect_tx(full(s), (uint32_t)(8192 * (2 * (1 + a_lo) + nb * (1 + b_lo))));
-            for (int i = 0; i < 2; ++i) {
-              tma_load_2d(a + i * 8192, ah, full(s), t.m0 + i * 64, y0);
-              if (a_lo) tma_load_2d(a + AG_PART + i * 8192, al, full(s), t.m0 + i * 64, y0);
-            }
-            for (int i = 0; i < nb; ++i) {
-              tma_load_2d(b + i * 8192, bh, full(s), t.n0 + i * 64, y0);
-              if (b_lo) tma_load_2d(b + AG_PART + i * 8192, bl, full(s), t.n0 + i * 64, y0);
-            }
-          } else {
-            const bool lo = KIND == AG_SPREAD || p.lo_on;
-            mbar_arrive_expect_tx(full(s), (uint32_t)(AG_PART + t.n16 * 128 * (1 + lo)));
-            if (p.w_kmajor) {
-              tma_load_3d(a, &maps.w, full(s), k0, t.m0, t.a);
-            } else {
-              tma_load_3d(a, &maps.w, full(s), t.m0, k0, t.a);
-              tma_load_3d(a + 8192, &maps.w, full(s), t.m0 + 64, k0, t.a);
-            }
-            if (t.n16 == AG_TN) {
-              tma_load_2d(b, &maps.hi, full(s), k0, (int)t.at);
-              if (lo) tma_load_2d(b + AG_PART, &maps.lo, full(s), k0, (int)t.at);
-            } else {
-              for (int i = 0; i < t.n16; i += 16) {
-                tma_load_2d(b + i * 128, &maps.hi16, full(s), k0, (int)t.at + i);
-                if (lo) tma_load_2d(b + AG_PART + i * 128, &maps.lo16, full(s), k0, (int)t.at + i);
-              }
-            }
-          }
-          if (++s == STAGES) { s = 0; ph ^= 1u; }
+          const uint32_t w = base + s * stage_bytes;
+          mbar_arrive_expect_tx(full(s), AG_TILE + (uint32_t)p.np * t.n16 * 128);
+          ag_load_weights(maps, w, full(s), p.w_kmajor, k * 16, m0, t.a);
+          for (int i = 0; i < p.np; ++i) ag_load_rows(maps, w + AG_TILE + i * p.tn * 128, full(s), k * 16, t, p.tn, i);
+          if (++s == p.stages) { s = 0; ph ^= 1u; }
         }
       }
       if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
-        const uint32_t lo = it > (uint32_t)STAGES ? it - STAGES : 0;
-        for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % STAGES), (j / STAGES) & 1u, p.status, p.wait_limit);
+        const uint32_t n = (uint32_t)p.stages, lo = it > n ? it - n : 0;
+        for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % n), (j / n) & 1u, p.status, p.wait_limit);
       }
     }
   } else if (warp == 1) {
@@ -495,40 +335,21 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_gemm_kernel(const __gr
       uint32_t ph = 0, done = 0;
       int s = 0;
       bool ok = true;
-      const bool w_kmajor = KIND != AG_GRAD && p.w_kmajor;
-      for (long long u = blockIdx.x; u < work.units && ok; u += gridDim.x) {
-        AgUnit t;
-        work.get(u, t);
-        if (t.steps == 0) continue;
+      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        if (!unit(u, t, m0)) continue;
         const int b = done & 1;
         if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
         tc_fence_after();
-        const uint32_t d = tmem_base + b * Sh::COLS;
-        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((w_kmajor ? 0u : 1u) << 15) | ((KIND == AG_GRAD ? 1u : 0u) << 16) |
-                               ((uint32_t)(t.n16 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
-        const bool a_lo = KIND == AG_GRAD && (t.which || p.lo_on);
-        const bool b_lo = KIND == AG_GRAD ? !t.which || p.lo2_on : KIND == AG_SPREAD || p.lo_on;
-        for (int k = 0; k < t.steps; k += 4) {
+        const uint32_t d = tmem_base + b * 128, idesc = ag_idesc(!p.w_kmajor, false, t.n16);
+        for (int k = 0; k < steps; k += 4) {
           if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t pa = base + s * Sh::STAGE, pb = pa + Sh::A_PARTS * AG_PART;
-          const int n = min(4, t.steps - k);
-          for (int e = 0; e < n; ++e) {
-            const uint32_t acc = k + e > 0 ? 1u : 0u;
-            const uint64_t ad = w_kmajor ? smem_desc(pa + e * 32, 16, 1024) : smem_desc(pa + e * 2048, 8192, 1024);
-            const uint64_t bd = KIND == AG_GRAD ? smem_desc(pb + e * 2048, 8192, 1024) : smem_desc(pb + e * 32, 16, 1024);
-            constexpr uint64_t next = AG_PART >> 4;                   // a pair's lo part, in descriptor units
-            tc_mma(d, ad, bd, idesc, acc);
-            if (KIND == AG_GRAD) {
-              // the small products apart, so that the sum of the large ones is rounded no more often than it must
-              if (b_lo) tc_mma(d + 128, ad, bd + next, idesc, acc);
-              if (a_lo) tc_mma(d + 128, ad + next, bd, idesc, b_lo ? 1u : acc);
-            } else if (b_lo) {
-              tc_mma(d, ad, bd + next, idesc, 1u);
-            }
-          }
+          const uint32_t w = base + s * stage_bytes;
+          for (int e = 0; e < min(4, steps - k); ++e)
+            for (int i = 0; i < p.np; ++i)
+              tc_mma(d, ag_desc(w, !p.w_kmajor, e), ag_desc(w + AG_TILE + i * p.tn * 128, false, e), idesc, k + e + i > 0 ? 1u : 0u);
           tc_commit(empty(s));
-          if (++s == STAGES) { s = 0; ph ^= 1u; }
+          if (++s == p.stages) { s = 0; ph ^= 1u; }
         }
         if (ok) tc_commit(accfull(b));
         ++done;
@@ -537,74 +358,537 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_gemm_kernel(const __gr
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;        // quarter of tensor memory's lanes; half of the columns
     uint32_t done = 0;
-    bool ok = true;
-    for (long long u = blockIdx.x; u < work.units && ok; u += gridDim.x) {
-      AgUnit t;
-      work.get(u, t);
-      if (t.steps == 0 && KIND != AG_GRAD) continue;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+      if (!unit(u, t, m0)) continue;
       const int b = done & 1;
-      if (t.steps > 0) {
-        ok = mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit);
-        if (!__all_sync(0xffffffffu, ok)) { ok = false; break; }
-        tc_fence_after();
-      }
-      const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * Sh::COLS;
-      const int m_first = t.m0 + q * 32, m = m_first + lane;
-      const float scale = p.scaled && t.rows > 0 ? __ldg(p.c.k.s + t.a) : 1.0f;
+      if (!__all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit))) break;
+      tc_fence_after();
+      const float scale = p.scaled ? __ldg(p.c.k.s + t.a) : 1.0f;
+      const int m = m0 + q * 32 + (lane & ~1);
 #pragma unroll 1
       for (int c = half * 64; c < min(half * 64 + 64, t.n16); c += 32) {
         uint32_t w[32];
+        tc_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + c, w);
+        // lanes 2 i and 2 i + 1 swap, so that each has two neighbouring ranks of every other row
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) {
+          const float v0 = __uint_as_float(w[j]) * scale, v1 = __uint_as_float(w[j + 1]) * scale;
+          const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
+          const int col = c + j + (lane & 1);
+          const float x[2] = {(lane & 1) ? got : v0, (lane & 1) ? v1 : got};
+          if (col < t.n16 && m < p.out.width) ag_store_parts<2>(p.out, (int64_t)(t.at + col) * p.out.ld + m, x);   // (the rank is a multiple of 8)
+        }
+      }
+      tc_fence_before();
+      mbar_arrive(accempty(b));
+      ++done;
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256) : "memory");
+  }
+}
+
+// ---- spread -------------------------------------------------------------------------------------------------------------------
+// One row tile's u stays in shared memory while tiles of 128 outputs of the pooled kind (q) pass.  Y comes and goes in slabs of up to
+// 16 KB, pieces of whole rows' 128 q, by bulk copies that a warp of its own issues rows ahead of the sums: with plain loads the eight
+// epilogue warps had 16 KB on their way (7000 rows to 11008 outputs 259 us, 1.2 TB/s); here it is every free slab.  The products go
+// through shared memory (V), so that the sums run over a slab in whole 16-byte chunks whatever lambda is.
+constexpr int AS_THREADS = 384, AS_SLAB = 16384, AS_RING = 3;      // loads, MMAs, slabs in, slabs out; eight warps
+struct AgSpread {
+  AdaptersCall c;
+  uint32_t rows_there;
+  int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
+  int slabs;
+  int m_tiles, M, w_kmajor, scaled;
+  RowsView y;
+  int lam, shift;                       // shift: log2 of the bytes of one q, -1 where they are no power of two
+  float factor;
+  int* status;
+  long long wait_limit;
+};
+
+__device__ __forceinline__ void as_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void as_bulk_store(void* dst, uint32_t src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
+}
+
+// whether any thread of the eight epilogue warps says so; a barrier of theirs
+__device__ __forceinline__ bool as_any(bool x) {
+  uint32_t y;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(y) : "r"((uint32_t)x) : "memory");
+  return y != 0;
+}
+
+// Y's part of one (row tile, q tile): rows in slabs
+struct AsSlabs {
+  int row_bytes, pitch, per, pieces, n;        // bytes of a row's q; of a row in a slab; rows in a slab; slabs to a row; slabs
+  __device__ __forceinline__ AsSlabs(const AgSpread& p, int m0, int rows) {
+    const int w = p.lam * (p.y.dtype == QBLORA_F32 ? 4 : 2), whole = 128 * w;
+    row_bytes = min(128, p.M - m0) * w;
+    per = max(1, AS_SLAB / whole);
+    pitch = min(whole, AS_SLAB);
+    pieces = (row_bytes + AS_SLAB - 1) / AS_SLAB;
+    n = pieces > 1 ? rows * pieces : (rows + per - 1) / per;
+  }
+  // slab i: rows [r0, r0 + count), bytes [off, off + len) of each
+  __device__ __forceinline__ void get(int i, int rows, int& r0, int& count, int& off, int& len) const {
+    if (pieces > 1) {
+      r0 = i / pieces;
+      count = 1;
+      off = (i - r0 * pieces) * AS_SLAB;
+      len = min(AS_SLAB, row_bytes - off);
+    } else {
+      r0 = i * per;
+      count = min(per, rows - r0);
+      off = 0;
+      len = row_bytes;
+    }
+  }
+};
+
+// 16 bytes of Y += the products of their elements.  QPC: different q in them; 0: lam is no power of two
+template <bool F32, int QPC>
+__device__ __forceinline__ uint4 as_add(uint4 y, const float* v, int first, int lam) {
+  constexpr int E = F32 ? 4 : 8;
+  float x[E];
+  if constexpr (QPC == 0) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = v[(first + e) / lam];
+  } else if constexpr (QPC == 8) {
+    const float4 a = *reinterpret_cast<const float4*>(v), b = *reinterpret_cast<const float4*>(v + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  } else {
+    float q[QPC];
+    if constexpr (QPC == 4) { const float4 a = *reinterpret_cast<const float4*>(v); q[0] = a.x; q[1] = a.y; q[2] = a.z; q[3] = a.w; }
+    else if constexpr (QPC == 2) { const float2 a = *reinterpret_cast<const float2*>(v); q[0] = a.x; q[1] = a.y; }
+    else q[0] = *v;
+#pragma unroll
+    for (int e = 0; e < E; ++e) x[e] = q[e * QPC / E];
+  }
+  uint32_t* w = reinterpret_cast<uint32_t*>(&y);
+  if constexpr (F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) + x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(ag_low(w[e]) + x[2 * e], ag_high(w[e]) + x[2 * e + 1]);
+  }
+  return y;
+}
+// `count` rows of `len` bytes at `slab`; v: the products of the first row, the others 128 floats on
+template <bool F32, int QPC>
+__device__ __forceinline__ void as_sums(uint8_t* slab, int pitch, const float* v, int count, int off, int len, int lam, int shift, int tid) {
+  const int per = len >> 4, all = per * count;
+  const bool pow2 = (per & (per - 1)) == 0;
+  const int down = 31 - __clz(per);
+#pragma unroll 2
+  for (int i = tid; i < all; i += AG_EPI) {
+    const int row = pow2 ? i >> down : i / per, at = (i - row * per) << 4;
+    const float* vr = v + row * 128;
+    uint4* y = reinterpret_cast<uint4*>(slab + row * pitch + at);
+    if constexpr (QPC == 0) *y = as_add<F32, 0>(*y, vr, (off + at) / (F32 ? 4 : 2), lam);
+    else *y = as_add<F32, QPC>(*y, vr + ((off + at) >> shift), 0, lam);
+  }
+}
+template <bool F32>
+__device__ __forceinline__ void as_sums_any(uint8_t* slab, int pitch, const float* v, int count, int off, int len, int lam, int shift, int tid) {
+  if (shift < 0) as_sums<F32, 0>(slab, pitch, v, count, off, len, lam, shift, tid);
+  else if (shift >= 4) as_sums<F32, 1>(slab, pitch, v, count, off, len, lam, shift, tid);
+  else if (shift == 3) as_sums<F32, 2>(slab, pitch, v, count, off, len, lam, shift, tid);
+  else if (shift == 2) as_sums<F32, 4>(slab, pitch, v, count, off, len, lam, shift, tid);
+  else if constexpr (!F32) as_sums<F32, 8>(slab, pitch, v, count, off, len, lam, shift, tid);
+}
+
+__global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __grid_constant__ AgMaps3 maps, const __grid_constant__ AgSpread p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), s_u = (raw + 1023u) & ~1023u;
+  const uint32_t block = (uint32_t)p.tn * 128;                        // one part's 64 ranks
+  const uint32_t s_w = s_u + p.np * p.kb * block, s_slab = s_w + AS_RING * AG_TILE, s_v = s_slab + p.slabs * AS_SLAB;
+  const uint32_t bars = s_v + p.tn * 512;
+  auto wfull = [&](int s) { return bars + 16u * s; };
+  auto wempty = [&](int s) { return bars + 16u * s + 8; };
+  const uint32_t ufull = bars + 16u * AS_RING, uempty = ufull + 8;
+  auto accfull = [&](int b) { return ufull + 16 + 8u * b; };
+  auto accempty = [&](int b) { return ufull + 32 + 8u * b; };
+  auto in = [&](int i) { return ufull + 48 + 24u * i; };              // the slab's rows have come
+  auto summed = [&](int i) { return ufull + 56 + 24u * i; };
+  auto gone = [&](int i) { return ufull + 64 + 24u * i; };            // they have been read by their stores
+  const uint32_t tmem_slot = ufull + 48 + 24u * p.slabs;
+  volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    for (int s = 0; s < AS_RING; ++s) { mbar_init(wfull(s), 1); mbar_init(wempty(s), 1); }
+    mbar_init(ufull, 1);
+    mbar_init(uempty, 1);
+    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
+    for (int i = 0; i < p.slabs; ++i) { mbar_init(in(i), 1); mbar_init(summed(i), AG_EPI); mbar_init(gone(i), 1); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(128) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot_g;
+  // A unit is one row tile and some neighbouring q tiles: as many as leave every CTA about four units, so that u is loaded seldom and the
+  // CTAs still end together.
+  const uint32_t tiles = g.tile[g.kept];
+  const int run = (int)min((long long)p.m_tiles, max(1LL, (long long)tiles * p.m_tiles / (4 * gridDim.x)));
+  const int runs = (p.m_tiles + run - 1) / run;
+  const long long units = (long long)tiles * runs;
+  asm volatile("griddepcontrol.wait;" ::: "memory");                  // what the kernels in front have written
+  // calls f(rows, steps of 16 ranks, first and last q tile) for this CTA's units, until it returns false
+  auto each = [&](auto&& f) {
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+      const uint32_t tile = (uint32_t)(u / runs);
+      const int first = (int)(u - (long long)tile * runs) * run;
+      const AgRows t = ag_rows(p.c, g, tile, p.tn);
+      const int steps = (bank_rank(p.c.k, t.a) + 15) / 16;
+      if (steps > 0 && !f(t, steps, first, min(first + run, p.m_tiles))) return;
+    }
+  };
+  auto row_of = [&](const AgRows& t, int r) {                         // the row of Y of the tile's row r; -1: none
+    const int row = __ldg(p.c.rows + t.j + r);
+    return row < p.c.T ? row : -1;
+  };
+  const int64_t y_pitch = p.y.stride * (p.y.dtype == QBLORA_F32 ? 4 : 2);
+  const int w = p.lam * (p.y.dtype == QBLORA_F32 ? 4 : 2);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0, ph = 0, n = 0;
+      int s = 0;
+      bool ok = true;
+      each([&](const AgRows& t, int steps, int first, int last) {
+        if (!mbar_wait(uempty, (n & 1u) ^ 1u, p.status, p.wait_limit)) return ok = false;
+        const int kb = (steps + 3) / 4;
+        mbar_arrive_expect_tx(ufull, (uint32_t)(p.np * kb * t.n16 * 128));
+        for (int i = 0; i < p.np; ++i)
+          for (int k = 0; k < kb; ++k) ag_load_rows(maps, s_u + (i * p.kb + k) * block, ufull, k * 64, t, p.tn, i);
+        ++n;
+        for (int m = first; m < last; ++m)
+          for (int k = 0; k < kb; ++k, ++it) {
+            if (!mbar_wait(wempty(s), ph ^ 1u, p.status, p.wait_limit)) return ok = false;
+            mbar_arrive_expect_tx(wfull(s), AG_TILE);
+            ag_load_weights(maps, s_w + s * AG_TILE, wfull(s), p.w_kmajor, k * 64, m * 128, t.a);
+            if (++s == AS_RING) { s = 0; ph ^= 1u; }
+          }
+        return true;
+      });
+      if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
+        if (n) mbar_wait(ufull, (n - 1) & 1u, p.status, p.wait_limit);
+        const uint32_t lo = it > (uint32_t)AS_RING ? it - AS_RING : 0;
+        for (uint32_t j = lo; j < it; ++j) mbar_wait(wfull(j % AS_RING), (j / AS_RING) & 1u, p.status, p.wait_limit);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t ph = 0, done = 0, n = 0;
+      int s = 0;
+      each([&](const AgRows& t, int steps, int first, int last) {
+        if (!mbar_wait(ufull, n & 1u, p.status, p.wait_limit)) return false;
+        const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
+        for (int m = first; m < last; ++m, ++done) {
+          const int b = done & 1;
+          if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
+          tc_fence_after();
+          for (int k = 0; k < steps; k += 4) {
+            if (!mbar_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
+            tc_fence_after();
+            for (int e = 0; e < min(4, steps - k); ++e)
+              for (int i = 0; i < p.np; ++i)
+                tc_mma(tmem_base + b * 64, ag_desc(s_w + s * AG_TILE, !p.w_kmajor, e), ag_desc(s_u + (i * p.kb + k / 4) * block, false, e), idesc,
+                       k + e + i > 0 ? 1u : 0u);
+            tc_commit(wempty(s));
+            if (++s == AS_RING) { s = 0; ph ^= 1u; }
+          }
+          tc_commit(accfull(b));
+        }
+        tc_commit(uempty);
+        ++n;
+        return true;
+      });
+    }
+  } else if (warp == 2) {
+    // ---- Y's rows in: a lane per row
+    uint32_t it = 0, ph = 0;
+    int s = 0;
+    bool ok = true;
+    each([&](const AgRows& t, int, int first, int last) {
+      for (int m = first; m < last; ++m) {
+        const AsSlabs y(p, m * 128, t.rows);
+        const char* from = static_cast<const char*>(p.y.data) + (int64_t)m * 128 * w;
+        for (int i = 0; i < y.n; ++i, ++it) {
+          int r0, count, off, len;
+          y.get(i, t.rows, r0, count, off, len);
+          if (!__all_sync(0xffffffffu, mbar_wait(gone(s), ph ^ 1u, p.status, p.wait_limit))) return ok = false;
+          int there = 0;
+          for (int r = lane; r < count; r += 32) there += row_of(t, r0 + r) >= 0;
+          there = __reduce_add_sync(0xffffffffu, there);
+          if (lane == 0) mbar_arrive_expect_tx(in(s), (uint32_t)(there * len));
+          __syncwarp();
+          for (int r = lane; r < count; r += 32) {
+            const int row = row_of(t, r0 + r);
+            if (row >= 0) as_bulk_load(s_slab + s * AS_SLAB + r * y.pitch, from + row * y_pitch + off, (uint32_t)len, in(s));
+          }
+          if (++s == p.slabs) { s = 0; ph ^= 1u; }
+        }
+      }
+      return true;
+    });
+    if (!ok) {
+      const uint32_t n = (uint32_t)p.slabs, lo = it > n ? it - n : 0;
+      for (uint32_t j = lo; j < it; ++j) mbar_wait(in(j % n), (j / n) & 1u, p.status, p.wait_limit);
+    }
+  } else if (warp == 3) {
+    // ---- and out
+    uint32_t ph = 0;
+    int s = 0;
+    each([&](const AgRows& t, int, int first, int last) {
+      for (int m = first; m < last; ++m) {
+        const AsSlabs y(p, m * 128, t.rows);
+        char* to = static_cast<char*>(p.y.data) + (int64_t)m * 128 * w;
+        for (int i = 0; i < y.n; ++i) {
+          int r0, count, off, len;
+          y.get(i, t.rows, r0, count, off, len);
+          if (!__all_sync(0xffffffffu, mbar_wait(summed(s), ph, p.status, p.wait_limit))) return false;
+          for (int r = lane; r < count; r += 32) {
+            const int row = row_of(t, r0 + r);
+            if (row >= 0) as_bulk_store(to + row * y_pitch + off, s_slab + s * AS_SLAB + r * y.pitch, (uint32_t)len);
+          }
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) mbar_arrive(gone(s));
+          if (++s == p.slabs) { s = 0; ph ^= 1u; }
+        }
+      }
+      return true;
+    });
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");         // written, not only read
+  } else {
+    const int q = warp & 3, half = (warp - 4) >> 2, etid = tid - 128;
+    uint32_t done = 0, ph = 0;
+    int s = 0;
+    float* v = reinterpret_cast<float*>(smem_raw + (s_v - raw));
+    bool ok = true;
+    each([&](const AgRows& t, int, int first, int last) {
+      const float scale = p.scaled ? __ldg(p.c.k.s + t.a) * p.factor : p.factor;
+      for (int m = first; m < last; ++m, ++done) {
+        const int b = done & 1;
+        ok = mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit);
+        if (as_any(!ok)) return false;                                // (and V's readers of the tile before are done)
+        tc_fence_after();
+        if (half * 32 < t.n16) {
+          uint32_t x[32];
+          tc_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + b * 64 + half * 32, x);
+#pragma unroll
+          for (int j = 0; j < 32; ++j)
+            if (half * 32 + j < p.tn) v[(half * 32 + j) * 128 + q * 32 + lane] = __uint_as_float(x[j]) * scale;
+        }
+        tc_fence_before();
+        mbar_arrive(accempty(b));
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const AsSlabs y(p, m * 128, t.rows);
+        for (int i = 0; i < y.n; ++i) {
+          int r0, count, off, len;
+          y.get(i, t.rows, r0, count, off, len);
+          ok = __all_sync(0xffffffffu, mbar_wait(in(s), ph, p.status, p.wait_limit));
+          if (ok) {
+            uint8_t* slab = smem_raw + (s_slab - raw) + s * AS_SLAB;
+            if (p.y.dtype == QBLORA_F32) as_sums_any<true>(slab, y.pitch, v + r0 * 128, count, off, len, p.lam, p.shift, etid);
+            else as_sums_any<false>(slab, y.pitch, v + r0 * 128, count, off, len, p.lam, p.shift, etid);
+          }
+          fence_async_proxy();                                        // the stores read what was written here
+          mbar_arrive(summed(s));
+          if (++s == p.slabs) { s = 0; ph ^= 1u; }
+        }
+      }
+      return true;
+    });
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(128) : "memory");
+  }
+}
+
+// ---- grad ---------------------------------------------------------------------------------------------------------------------
+// Tiles of 128 x 128 of dA and dB.  Both operands are rows of the workspace, contraction over the rows: parts 0 x 0 are one
+// accumulator, the smaller products (0 x 1, 1 x 0, 1 x 1, 0 x 2, 2 x 0: the others are below 2^-24) a second, so that the sum of the large
+// ones is rounded no more often than it must be.
+constexpr int AR_STAGES = 2, AR_STAGE = 6 * AG_TILE;
+struct AgGradSide { int parts_a, parts_b, M, N; float* out; };        // dA: x' (P) by du (r); dB: u (r) by dv (Q)
+struct AgGrad {
+  AdaptersCall c;
+  uint32_t rows_there;
+  AgGradSide side[2];                   // out == nullptr: not wanted
+  int* status;
+  long long wait_limit;
+};
+struct AgGradMaps { CUtensorMap a[2], b[2]; };
+
+__global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __grid_constant__ AgGradMaps maps, const __grid_constant__ AgGrad p) {
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u, bars = base + AR_STAGES * AR_STAGE;
+  auto full = [&](int s) { return bars + 16u * s; };
+  auto empty = [&](int s) { return bars + 16u * s + 8; };
+  auto accfull = [&](int b) { return bars + 16u * AR_STAGES + 8u * b; };
+  auto accempty = [&](int b) { return bars + 16u * AR_STAGES + 16 + 8u * b; };
+  const uint32_t tmem_slot = bars + 16u * AR_STAGES + 32;
+  volatile uint32_t* tmem_slot_g = reinterpret_cast<volatile uint32_t*>(smem_raw + (tmem_slot - raw));
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (tid == 0) {
+    for (int s = 0; s < AR_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, 128);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot_g;
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
+  const BankView& k = p.c.k;
+  const AgGradSide &sa = p.side[0], &sb = p.side[1];
+  const int ca = (sa.N + 127) / 128, cb = (sb.N + 127) / 128;
+  const int ta = sa.out ? (sa.M + 127) / 128 * ca : 0, tb = sb.out ? (sb.M + 127) / 128 * cb : 0;
+  const long long units = (long long)k.n * (ta + tb);
+  struct Unit { int a, side, m0, n0, n16, steps, rank; uint32_t at; };
+  auto unit = [&](long long u) {
+    Unit t;
+    t.a = (int)(u / (ta + tb));
+    int x = (int)(u - (long long)t.a * (ta + tb));
+    t.side = x >= ta;
+    if (t.side) x -= ta;
+    const int cols = t.side ? cb : ca;
+    t.m0 = x / cols * 128;
+    t.n0 = x % cols * 128;
+    t.n16 = min(128, ((t.side ? sb.N : sa.N) - t.n0 + 15) & ~15);
+    t.rank = bank_rank(k, t.a);
+    t.at = t.a < g.kept ? g.pad[t.a] : 0;
+    t.steps = t.a < g.kept && (t.side ? t.m0 : t.n0) < t.rank ? (int)(g.pad[t.a + 1] - t.at) / 16 : 0;
+    return t;
+  };
+
+  if (warp == 0) {
+    if (lane == 0) {
+      uint32_t it = 0, ph = 0;
+      int s = 0;
+      bool ok = true;
+      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        const Unit t = unit(u);
+        const AgGradSide& side = p.side[t.side];
+        const int nb = (t.n16 + 63) / 64;
+        for (int x = 0; x < t.steps; x += 4, ++it) {
+          if (!mbar_wait(empty(s), ph ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
+          const uint32_t a = base + s * AR_STAGE, b = a + 3 * AG_TILE;
+          const int y = (int)t.at + x * 16;
+          mbar_arrive_expect_tx(full(s), (uint32_t)(8192 * (2 * side.parts_a + nb * side.parts_b)));
+          for (int i = 0; i < side.parts_a; ++i)
+            for (int j = 0; j < 2; ++j) tma_load_3d(a + i * AG_TILE + j * 8192, &maps.a[t.side], full(s), t.m0 + j * 64, y, i);
+          for (int i = 0; i < side.parts_b; ++i)
+            for (int j = 0; j < nb; ++j) tma_load_3d(b + i * AG_TILE + j * 8192, &maps.b[t.side], full(s), t.n0 + j * 64, y, i);
+          if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
+        }
+      }
+      if (!ok) {
+        const uint32_t lo = it > (uint32_t)AR_STAGES ? it - AR_STAGES : 0;
+        for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % AR_STAGES), (j / AR_STAGES) & 1u, p.status, p.wait_limit);
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      uint32_t ph = 0, done = 0;
+      int s = 0;
+      bool ok = true;
+      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+        const Unit t = unit(u);
+        if (t.steps == 0) continue;
+        const AgGradSide& side = p.side[t.side];
+        const int b = done & 1;
+        if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d = tmem_base + b * 256, idesc = ag_idesc(true, true, t.n16);
+        uint32_t small = 0;
+        for (int x = 0; x < t.steps; x += 4) {
+          if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
+          tc_fence_after();
+          const uint32_t pa = base + s * AR_STAGE, pb = pa + 3 * AG_TILE;
+          for (int e = 0; e < min(4, t.steps - x); ++e) {
+            tc_mma(d, ag_desc(pa, true, e), ag_desc(pb, true, e), idesc, x + e > 0 ? 1u : 0u);
+            for (int i = 0; i < side.parts_a; ++i)
+              for (int j = 0; j < side.parts_b; ++j)
+                if (i + j > 0 && i + j <= 2) {
+                  tc_mma(d + 128, ag_desc(pa + i * AG_TILE, true, e), ag_desc(pb + j * AG_TILE, true, e), idesc, small);
+                  small = 1;
+                }
+          }
+          tc_commit(empty(s));
+          if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
+        }
+        if (ok) tc_commit(accfull(b));
+        ++done;
+      }
+    }
+  } else {
+    const int q = warp & 3, half = (warp - 2) >> 2;
+    uint32_t done = 0;
+    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+      const Unit t = unit(u);
+      const AgGradSide& side = p.side[t.side];
+      const int b = done & 1;
+      if (t.steps > 0) {
+        if (!__all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit))) break;
+        tc_fence_after();
+      }
+      const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256;
+      const int m = t.m0 + q * 32 + lane;
+      const float scale = t.side ? __ldg(k.s + t.a) : 1.0f;           // du has it already
+#pragma unroll 1
+      for (int c = half * 64; c < min(half * 64 + 64, t.n16); c += 32) {
         float v[32];
         if (t.steps > 0) {
+          uint32_t w[32];
           tc_ld32(d + c, w);
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(w[j]);
+          tc_ld32(d + 128 + c, w);
+#pragma unroll
+          for (int j = 0; j < 32; ++j) v[j] = (v[j] + __uint_as_float(w[j])) * scale;
         } else {
 #pragma unroll
           for (int j = 0; j < 32; ++j) v[j] = 0.f;
         }
-        if (KIND == AG_GRAD) {
-          if (t.steps > 0) {
-            tc_ld32(d + 128 + c, w);
+        if (m < side.M) {
+          float* out = side.out + ((int64_t)t.a * side.M + m) * side.N + t.n0 + c;
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
+          for (int j = 0; j < 32; j += 4) {
+            if (t.n0 + c + j >= side.N) break;                        // N is a multiple of 8
+            float x[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = (t.side ? m : t.n0 + c + j + e) < t.rank ? v[j + e] : 0.f;
+            *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
           }
-          const BankView& k = p.c.k;
-          const int M = t.which ? k.r : k.P, N = t.which ? k.Q : k.r;
-          if (m < M) {
-            const float f = t.which ? scale : 1.0f;
-            float* out = (t.which ? p.dB : p.dA) + ((int64_t)t.a * M + m) * N + t.n0 + c;
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-              if (t.n0 + c + j >= N) break;                // N is a multiple of 8
-              float x[4];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) x[e] = (t.which ? m : t.n0 + c + j + e) < t.rank ? v[j + e] * f : 0.f;
-              *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
-            }
-          }
-        } else if (KIND == AG_SHRINK) {
-          // lanes 2 i and 2 i + 1 swap, so that each has two neighbouring ranks of every other row
-#pragma unroll
-          for (int j = 0; j < 32; j += 2) {
-            const float send = (lane & 1) ? v[j] : v[j + 1], keep = ((lane & 1) ? v[j + 1] : v[j]) * scale;
-            const float got = __shfl_xor_sync(0xffffffffu, send, 1) * scale;
-            const float x0 = (lane & 1) ? got : keep, x1 = (lane & 1) ? keep : got;
-            const int col = c + j + (lane & 1), mm = m & ~1;
-            if (col >= t.n16 || mm >= p.M) continue;       // M (the rank) is a multiple of 8
-            const uint32_t h = pack_bf16x2(x0, x1);
-            const int64_t o = (int64_t)(t.at + col) * p.ld + mm;
-            *reinterpret_cast<uint32_t*>(p.hi + o) = h;
-            *reinterpret_cast<uint32_t*>(p.lo + o) = pack_bf16x2(x0 - ag_low(h), x1 - ag_high(h));
-          }
-        } else {
-          int row = -1;
-          if (c + lane < t.rows) row = __ldg(p.c.rows + t.j + c + lane);
-          if (row >= p.c.T) row = -1;
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] *= scale * p.factor;
-          if (p.y.dtype == QBLORA_F32) ag_spread<true>(p, v, row, m_first, p.M, lane);
-          else ag_spread<false>(p, v, row, m_first, p.M, lane);
         }
       }
       if (t.steps > 0) {
@@ -618,42 +902,38 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_gemm_kernel(const __gr
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * Sh::COLS) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------
-// A pair of bf16 matrices in the workspace.
-struct Pair { __nv_bfloat16 *hi, *lo; int width, ld; };
-struct Layout { Pair x, dv, u, du; size_t bytes; uint32_t rows; };
+struct Layout { Parts x, dv, u, du; size_t bytes; uint32_t rows; };
 
-int pitch8(int n) { return (n + 7) & ~7; }
-
-Layout ag_layout(const BankView& k, int64_t T, bool backward, char* ws) {
+// parts: of numbers that are no bf16 numbers
+Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* ws) {
   Layout l{};
   l.rows = (uint32_t)std::min<int64_t>(T + 15 * std::min<int64_t>(T, k.n), 0x7ffffff0);
   size_t at = kStatusBytes;
-  auto pair = [&](Pair& p, int width, bool lo) {
+  auto place = [&](Parts& p, int width, int np) {
+    p.np = np;
     p.width = width;
-    p.ld = pitch8(width);
-    const size_t bytes = align_up((size_t)l.rows * p.ld * 2, 256);
-    p.hi = reinterpret_cast<__nv_bfloat16*>(ws + at);
-    at += bytes;
-    p.lo = lo ? reinterpret_cast<__nv_bfloat16*>(ws + at) : nullptr;
-    if (lo) at += bytes;
+    p.ld = (width + 7) & ~7;
+    p.stride = (int64_t)align_up((size_t)l.rows * p.ld, 128);
+    p.p = reinterpret_cast<__nv_bfloat16*>(ws + at);
+    at += (size_t)p.stride * 2 * np;
   };
-  pair(l.x, k.P, k.l1 > 1);
-  pair(l.u, k.r, true);
+  place(l.x, k.P, k.l1 > 1 ? parts : 1);
+  place(l.u, k.r, parts);
   if (backward) {
-    pair(l.dv, k.Q, k.l2 > 1);
-    pair(l.du, k.r, true);
+    place(l.dv, k.Q, k.l2 > 1 ? parts : 1);
+    place(l.du, k.r, parts);
   }
   l.bytes = align_up(at, 256);
   return l;
 }
 
-AgPool ag_source(const RowsView& x, int d, int lam, bool mean, const Pair& out) {
-  AgPool p{x, d, lam, out.width, out.ld, 0, mean ? 1.0f / (float)lam : 1.0f, out.hi, out.lo};
+AgPool ag_source(const RowsView& x, int d, int lam, bool mean, const Parts& out) {
+  AgPool p{x, d, lam, 0, mean ? 1.0f / (float)lam : 1.0f, out};
   p.wide = lam <= 256 && (lam & (lam - 1)) == 0;
   return p;
 }
@@ -665,23 +945,23 @@ int ag_sms(int* n) {
   return QBLORA_OK;
 }
 
-template <int KIND>
-int ag_launch(const AgMaps& maps, const AgParams& p, int64_t most_units, cudaStream_t st) {
-  int sms = 0, rc = ag_sms(&sms);
+// A persistent kernel behind the ones in front, which it may overlap.
+template <class Maps, class Params>
+int ag_launch(void (*kernel)(Maps, Params), std::atomic<bool>* ready, const Maps& maps, const Params& p, int threads, size_t smem, int64_t most_units,
+              cudaStream_t st) {
+  int sms = 0, dev = 0;
+  const int rc = ag_sms(&sms);
   if (rc) return rc;
-  auto kernel = adapters_gemm_kernel<KIND>;
-  static std::atomic<bool> done[64];
-  int dev = 0;
   QB_CUDA(cudaGetDevice(&dev));
   if (dev < 0 || dev >= 64) return QBLORA_ERR_UNSUPPORTED;
-  if (!done[dev].load(std::memory_order_acquire)) {
-    QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ag_smem_bytes<KIND>(kMaxAdapters)));
-    done[dev].store(true, std::memory_order_release);
+  if (!ready[dev].load(std::memory_order_acquire)) {
+    QB_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, AG_SMEM + 1024));
+    ready[dev].store(true, std::memory_order_release);
   }
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(sms, most_units)));
-  cfg.blockDim = dim3(AG_THREADS);
-  cfg.dynamicSmemBytes = ag_smem_bytes<KIND>(p.c.k.n);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem + 1024;
   cfg.stream = st;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -697,14 +977,17 @@ int ag_launch_pool(const AgPoolParams& p, int64_t rows, cudaStream_t st) {
   const int rc = ag_sms(&sms);
   if (rc) return rc;
   const int64_t want = (rows * p.sources + AG_POOL_THREADS / 32 - 1) / (AG_POOL_THREADS / 32);
-  adapters_pool_kernel<<<(unsigned)std::min<int64_t>(want, 8LL * sms), AG_POOL_THREADS, (size_t)2 * (p.c.k.n + 1) * 4, st>>>(p);
+  adapters_pool_kernel<<<(unsigned)std::min<int64_t>(want, 8LL * sms), AG_POOL_THREADS, ag_table_bytes(p.c.k.n), st>>>(p);
   count_launch();
   QB_CUDA(cudaGetLastError());
   return QBLORA_OK;
 }
 
-int rows_map(CUtensorMap* tm, const __nv_bfloat16* ptr, const Pair& p, uint32_t rows, int box_rows) {
-  return make_tensor_map_2d(tm, false, ptr, (uint64_t)p.width, rows, (uint64_t)p.ld * 2, 64, (uint32_t)box_rows, true);
+int parts_map(CUtensorMap* tm, const Parts& p, uint32_t rows, int box_rows) {
+  const uint64_t dims[3] = {(uint64_t)p.width, rows, (uint64_t)p.np};
+  const uint64_t pitch[2] = {(uint64_t)p.ld * 2, (uint64_t)p.stride * 2};
+  const uint32_t box[3] = {64, (uint32_t)box_rows, 1};
+  return make_tensor_map_nd(tm, 3, p.p, dims, pitch, box);
 }
 // element (i, j) of slot a at a * rows * width + i * width + j: boxes of 64 j by `box` i
 int bank_map(CUtensorMap* tm, const __nv_bfloat16* ptr, int width, int rows, int n, int box) {
@@ -716,75 +999,84 @@ int bank_map(CUtensorMap* tm, const __nv_bfloat16* ptr, int width, int rows, int
 
 #define QB_TRY(call) do { const int rc_ = (call); if (rc_) return rc_; } while (0)
 
-int pair_maps(AgMaps* m, const Pair& p, uint32_t rows) {
-  const __nv_bfloat16* lo = p.lo ? p.lo : p.hi;
-  QB_TRY(rows_map(&m->hi, p.hi, p, rows, 128));
-  QB_TRY(rows_map(&m->lo, lo, p, rows, 128));
-  QB_TRY(rows_map(&m->hi16, p.hi, p, rows, 16));
-  return rows_map(&m->lo16, lo, p, rows, 16);
-}
-
-AgParams ag_params(const AdaptersCall& c, const Layout& l, int* status) {
-  AgParams p{};
-  p.c = c;
-  p.rows_there = l.rows;
-  p.status = status;
-  p.wait_limit = wait_limit_cycles();
-  p.lam = 1;
-  p.factor = 1.0f;
-  return p;
-}
-
-int64_t most_tiles(const AdaptersCall& c) { return c.T / AG_TN + std::min<int64_t>(c.T, c.k.n); }
+int64_t most_tiles(const AdaptersCall& c, int tn) { return c.T / tn + std::min<int64_t>(c.T, c.k.n); }
 
 // u = x' A, or du = s dv B^T
-int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Pair& in, const Pair& out, const __nv_bfloat16* W, bool kmajor,
+int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Parts& in, const Parts& out, const __nv_bfloat16* W, bool kmajor,
               bool scaled, cudaStream_t st) {
-  AgMaps maps{};
-  AgParams p = ag_params(c, l, status);
-  QB_TRY(pair_maps(&maps, in, l.rows));
+  static std::atomic<bool> ready[64];
+  AgMaps3 maps{};
+  AgShrink p{};
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.np = in.np; p.m_tiles = (c.k.r + 127) / 128; p.K = in.width; p.w_kmajor = kmajor; p.scaled = scaled; p.out = out;
+  // smaller tiles where large ones would leave SMs without any
+  p.tn = 128;
+  while (p.tn > 32 && (int64_t)c.T * p.m_tiles / p.tn < 100) p.tn /= 2;
+  const size_t stage = AG_TILE + (size_t)p.np * p.tn * 128, table = ag_table_bytes(c.k.n);
+  p.stages = (int)std::min<size_t>(8, (AG_SMEM - AG_BARS - table) / stage);
+  QB_TRY(parts_map(&maps.rows, in, l.rows, p.tn));
+  QB_TRY(parts_map(&maps.rows16, in, l.rows, 16));
   // A [P][r]: the contraction runs over its rows; B [r][Q]: along them
   QB_TRY(kmajor ? bank_map(&maps.w, W, in.width, c.k.r, c.k.n, 128) : bank_map(&maps.w, W, c.k.r, in.width, c.k.n, 64));
-  p.m_tiles = (c.k.r + 127) / 128; p.M = c.k.r; p.K = in.width;
-  p.w_kmajor = kmajor; p.lo_on = in.lo != nullptr; p.scaled = scaled;
-  p.hi = out.hi; p.lo = out.lo; p.ld = out.ld;
-  return ag_launch<AG_SHRINK>(maps, p, most_tiles(c) * p.m_tiles, st);
+  return ag_launch(adapters_shrink_kernel, ready, maps, p, AG_THREADS, p.stages * stage + AG_BARS + table, most_tiles(c, p.tn) * p.m_tiles, st);
+}
+
+// shared memory of the spread kernel without slabs; 0: u does not fit with at least two of them
+size_t as_fixed(int n, int np, int kb, int tn) {
+  const size_t need = (size_t)np * kb * tn * 128 + AS_RING * AG_TILE + (size_t)tn * 512 + AG_BARS + ag_table_bytes(n);
+  return need + 2 * AS_SLAB <= (size_t)AG_SMEM ? need : 0;
+}
+int as_rows(const BankView& k, int np) {
+  int tn = 64;
+  while (tn > 16 && !as_fixed(k.n, np, (k.r + 63) / 64, tn)) tn /= 2;
+  return as_fixed(k.n, np, (k.r + 63) / 64, tn) ? tn : 0;
 }
 // Y += s repeat(u B), or dX += repeat(du A^T) / lam
-int ag_expand(const AdaptersCall& c, const Layout& l, int* status, const Pair& in, const __nv_bfloat16* W, int M, bool kmajor, const RowsView& y,
+int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& in, const __nv_bfloat16* W, int M, bool kmajor, const RowsView& y,
               int lam, bool forward, cudaStream_t st) {
-  AgMaps maps{};
-  AgParams p = ag_params(c, l, status);
-  QB_TRY(pair_maps(&maps, in, l.rows));
+  static std::atomic<bool> ready[64];
+  AgMaps3 maps{};
+  AgSpread p{};
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.np = in.np; p.kb = (c.k.r + 63) / 64; p.tn = as_rows(c.k, in.np);
+  const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
+  p.slabs = (int)std::min<size_t>(6, (AG_SMEM - fixed) / AS_SLAB);
+  p.m_tiles = (M + 127) / 128; p.M = M; p.w_kmajor = kmajor; p.scaled = forward; p.y = y; p.lam = lam;
+  p.factor = forward ? 1.0f : 1.0f / (float)lam;
+  const int w = lam * (y.dtype == QBLORA_F32 ? 4 : 2);
+  p.shift = -1;
+  for (int i = 0; i < 31; ++i)
+    if (w == 1 << i) p.shift = i;
+  QB_TRY(parts_map(&maps.rows, in, l.rows, p.tn));
+  QB_TRY(parts_map(&maps.rows16, in, l.rows, 16));
   QB_TRY(kmajor ? bank_map(&maps.w, W, c.k.r, M, c.k.n, 128) : bank_map(&maps.w, W, M, c.k.r, c.k.n, 64));
-  p.m_tiles = (M + 127) / 128; p.M = M;
-  p.w_kmajor = kmajor; p.scaled = forward;
-  p.y = y; p.lam = lam; p.factor = forward ? 1.0f : 1.0f / (float)lam;
-  return ag_launch<AG_SPREAD>(maps, p, most_tiles(c) * p.m_tiles, st);
+  return ag_launch(adapters_spread_kernel, ready, maps, p, AS_THREADS, fixed + (size_t)p.slabs * AS_SLAB, most_tiles(c, p.tn) * p.m_tiles, st);
 }
 int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st) {
-  AgMaps maps{};
-  AgParams p = ag_params(c, l, status);
-  auto both = [&](CUtensorMap* hi, CUtensorMap* lo, const Pair& q) -> int {
-    QB_TRY(rows_map(hi, q.hi, q, l.rows, 64));
-    return rows_map(lo, q.lo ? q.lo : q.hi, q, l.rows, 64);
-  };
-  QB_TRY(both(&maps.hi, &maps.lo, l.x));
-  QB_TRY(both(&maps.hi2, &maps.lo2, l.du));
-  QB_TRY(both(&maps.u_hi, &maps.u_lo, l.u));
-  QB_TRY(both(&maps.hi16, &maps.lo16, l.dv));
-  p.lo_on = l.x.lo != nullptr; p.lo2_on = l.dv.lo != nullptr; p.scaled = 1;
-  p.dA = c.dA; p.dB = c.dB;
+  static std::atomic<bool> ready[64];
+  AgGradMaps maps{};
+  AgGrad p{};
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
+  p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
+  QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 64));
+  QB_TRY(parts_map(&maps.b[0], l.du, l.rows, 64));
+  QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 64));
+  QB_TRY(parts_map(&maps.b[1], l.dv, l.rows, 64));
   const int64_t per = (int64_t)((c.k.P + 127) / 128 + (c.k.Q + 127) / 128) * ((c.k.r + 127) / 128);
-  return ag_launch<AG_GRAD>(maps, p, per * c.k.n, st);
+  return ag_launch(adapters_grad_kernel, ready, maps, p, AG_THREADS, AR_STAGES * AR_STAGE + AG_BARS + ag_table_bytes(c.k.n), per * c.k.n, st);
 }
+
+constexpr int kBackwardParts = 3;
+int forward_parts(int y_dtype) { return y_dtype == QBLORA_F32 ? 3 : 2; }
 
 }  // namespace
 
-size_t tc_adapters_ws_bytes(const BankView& k, int64_t T, bool backward) { return ag_layout(k, T, backward, nullptr).bytes; }
+size_t tc_adapters_ws_bytes(const BankView& k, int64_t T, bool backward) { return ag_layout(k, T, backward, 3, nullptr).bytes; }
 
 bool tc_adapters_sizes_ok(const BankView& k, int64_t T) {
-  return k.r % 8 == 0 && k.Q % 8 == 0 && k.d_in % 8 == 0 && k.d_out % 8 == 0 && T + 15 * std::min<int64_t>(T, k.n) <= 0x7ffffff0;
+  return k.r % 8 == 0 && k.Q % 8 == 0 && k.d_in % 8 == 0 && k.d_out % 8 == 0 && T + 15 * std::min<int64_t>(T, k.n) <= 0x7ffffff0 &&
+         as_rows(k, 3) > 0;
 }
 
 bool tc_adapters_supported(const AdaptersCall& c) {
@@ -795,18 +1087,18 @@ bool tc_adapters_supported(const AdaptersCall& c) {
 }
 
 int tc_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
-  const Layout l = ag_layout(c.k, c.T, false, ws);
+  const Layout l = ag_layout(c.k, c.T, false, forward_parts(c.Y.dtype), ws);
   int* status = reinterpret_cast<int*>(ws);
   AgPoolParams pool{};
   pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = 1;
   pool.src[0] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
   QB_TRY(ag_launch_pool(pool, l.rows, st));
   QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
-  return ag_expand(c, l, status, l.u, c.k.B, c.k.Q, false, c.Y, c.k.l2, true, st);
+  return ag_spread(c, l, status, l.u, c.k.B, c.k.Q, false, c.Y, c.k.l2, true, st);
 }
 
 int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
-  const Layout l = ag_layout(c.k, c.T, true, ws);
+  const Layout l = ag_layout(c.k, c.T, true, kBackwardParts, ws);
   int* status = reinterpret_cast<int*>(ws);
   const bool grads = c.dA || c.dB;
   AgPoolParams pool{};
@@ -816,7 +1108,7 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   QB_TRY(ag_launch_pool(pool, l.rows, st));
   if (c.dX.data || c.dA) QB_TRY(ag_shrink(c, l, status, l.dv, l.du, c.k.B, true, true, st));
   if (c.dB) QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
-  if (c.dX.data) QB_TRY(ag_expand(c, l, status, l.du, c.k.A, c.k.P, true, c.dX, c.k.l1, false, st));
+  if (c.dX.data) QB_TRY(ag_spread(c, l, status, l.du, c.k.A, c.k.P, true, c.dX, c.k.l1, false, st));
   if (grads) QB_TRY(ag_grad(c, l, status, st));
   return QBLORA_OK;
 }
