@@ -224,6 +224,7 @@ struct AgShrink {
   AdaptersCall c;
   uint32_t rows_there;
   int tn, stages, np;                   // rows of a tile; of the ring; parts of the input
+  int segment;                          // 64-wide blocks of the contraction that one accumulator takes
   int m_tiles, K, w_kmajor, scaled;     // tiles of 128 ranks; contraction; the weight's contiguous dimension is the contraction's;
                                         // times the adapter's factor
   Parts out;
@@ -266,9 +267,40 @@ __device__ __forceinline__ uint32_t ag_idesc(bool a_transposed, bool b_transpose
   return (1u << 4) | (1u << 7) | (1u << 10) | ((a_transposed ? 1u : 0u) << 15) | ((b_transposed ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) |
          ((uint32_t)(128 >> 4) << 24);
 }
-// step e (of 16) of a 64-wide block of the contraction
-__device__ __forceinline__ uint64_t ag_desc(uint32_t block, bool transposed, int e) {
-  return transposed ? smem_desc(block + e * 2048, 8192, 1024) : smem_desc(block + e * 32, 16, 1024);
+// Operand descriptors of a block of the contraction: K-major, or transposed with `group` bytes between runs of 64 rows.  A step of 16
+// is AG_STEP_K or AG_STEP_T further.
+constexpr uint64_t AG_STEP_K = 32 >> 4, AG_STEP_T = 2048 >> 4;
+__device__ __forceinline__ uint64_t ag_desc(uint32_t block, bool transposed, uint32_t group = 8192) {
+  return transposed ? smem_desc(block, group, 1024) : smem_desc(block, 16, 1024);
+}
+// The MMAs of up to four steps of 16: the weights by the first part of the rows into d0, by the others into d1.  One thread issues them:
+// with loops that are not unrolled and descriptors built for each, a block of eight MMAs cost it a microsecond (200 decoding rows with an adapter
+// each: shrink 66 us), so everything that can be is a constant here.  fresh: the accumulators begin with this block.
+template <int NP>
+__device__ __forceinline__ void ag_issue(uint32_t d0, uint32_t d1, uint64_t a, uint64_t a_step, uint64_t b, uint64_t part, uint32_t idesc, int n, bool fresh) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= n) break;
+    const uint32_t acc = fresh && e == 0 ? 0u : 1u;
+    tc_mma(d0, a, b, idesc, acc);
+#pragma unroll
+    for (int i = 1; i < NP; ++i) tc_mma(d1, a, b + i * part, idesc, i == 1 ? acc : 1u);
+    a += a_step;
+    b += AG_STEP_K;
+  }
+}
+__device__ __forceinline__ void ag_issue_parts(int np, uint32_t d0, uint32_t d1, uint64_t a, uint64_t a_step, uint64_t b, uint64_t part, uint32_t idesc,
+                                               int n, bool fresh) {
+  if (np == 1) ag_issue<1>(d0, d1, a, a_step, b, part, idesc, n, fresh);
+  else if (np == 2) ag_issue<2>(d0, d1, a, a_step, b, part, idesc, n, fresh);
+  else ag_issue<3>(d0, d1, a, a_step, b, part, idesc, n, fresh);
+}
+// v += 32 columns of tensor memory
+__device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
+  uint32_t w[32];
+  tc_ld32(taddr, w);
+#pragma unroll
+  for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
 }
 
 __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __grid_constant__ AgMaps3 maps, const __grid_constant__ AgShrink p) {
@@ -289,7 +321,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(256) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
@@ -337,58 +369,71 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
       bool ok = true;
       for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
         if (!unit(u, t, m0)) continue;
-        const int b = done & 1;
-        if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t d = tmem_base + b * 128, idesc = ag_idesc(!p.w_kmajor, false, t.n16);
-        for (int k = 0; k < steps; k += 4) {
+        const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
+        int left = 0, b = 0;                               // blocks left of the segment; its accumulator
+        for (int k = 0; k < steps && ok; k += 4) {
+          const bool fresh = left == 0;
+          if (fresh) {
+            left = p.segment;
+            b = done & 1;
+            if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
+          }
           if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t w = base + s * stage_bytes;
-          for (int e = 0; e < min(4, steps - k); ++e)
-            for (int i = 0; i < p.np; ++i)
-              tc_mma(d, ag_desc(w, !p.w_kmajor, e), ag_desc(w + AG_TILE + i * p.tn * 128, false, e), idesc, k + e + i > 0 ? 1u : 0u);
+          const uint32_t w = base + s * stage_bytes, d = tmem_base + b * 256;
+          ag_issue_parts(p.np, d, d + 128, ag_desc(w, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T, ag_desc(w + AG_TILE, false),
+                         (uint64_t)(p.tn * 128) >> 4, idesc, min(4, steps - k), fresh);
           tc_commit(empty(s));
           if (++s == p.stages) { s = 0; ph ^= 1u; }
+          if (--left == 0 || k + 4 >= steps) { tc_commit(accfull(b)); ++done; left = 0; }
         }
-        if (ok) tc_commit(accfull(b));
-        ++done;
       }
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;        // quarter of tensor memory's lanes; half of the columns
     uint32_t done = 0;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       if (!unit(u, t, m0)) continue;
-      const int b = done & 1;
-      if (!__all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit))) break;
-      tc_fence_after();
+      float v[64];
+#pragma unroll
+      for (int j = 0; j < 64; ++j) v[j] = 0.f;
+      for (int k = 0; k < steps && ok; k += 4 * p.segment) {
+        const int b = done & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256 + half * 64;
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          if (half * 64 + c >= t.n16) break;
+          ag_gather(d + c, v + c);
+          if (p.np > 1) ag_gather(d + 128 + c, v + c);
+        }
+        tc_fence_before();
+        mbar_arrive(accempty(b));
+        ++done;
+      }
+      if (!ok) break;
       const float scale = p.scaled ? __ldg(p.c.k.s + t.a) : 1.0f;
       const int m = m0 + q * 32 + (lane & ~1);
-#pragma unroll 1
-      for (int c = half * 64; c < min(half * 64 + 64, t.n16); c += 32) {
-        uint32_t w[32];
-        tc_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + c, w);
-        // lanes 2 i and 2 i + 1 swap, so that each has two neighbouring ranks of every other row
+      // lanes 2 i and 2 i + 1 swap, so that each has two neighbouring ranks of every other row
 #pragma unroll
-        for (int j = 0; j < 32; j += 2) {
-          const float v0 = __uint_as_float(w[j]) * scale, v1 = __uint_as_float(w[j + 1]) * scale;
-          const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
-          const int col = c + j + (lane & 1);
-          const float x[2] = {(lane & 1) ? got : v0, (lane & 1) ? v1 : got};
-          if (col < t.n16 && m < p.out.width) ag_store_parts<2>(p.out, (int64_t)(t.at + col) * p.out.ld + m, x);   // (the rank is a multiple of 8)
-        }
+      for (int j = 0; j < 64; j += 2) {
+        if (half * 64 + j >= t.n16) break;
+        const float v0 = v[j] * scale, v1 = v[j + 1] * scale;
+        const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
+        const int col = half * 64 + j + (lane & 1);
+        const float x[2] = {(lane & 1) ? got : v0, (lane & 1) ? v1 : got};
+        if (m < p.out.width) ag_store_parts<2>(p.out, (int64_t)(t.at + col) * p.out.ld + m, x);      // (the rank is a multiple of 8)
       }
-      tc_fence_before();
-      mbar_arrive(accempty(b));
-      ++done;
     }
   }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");
   }
 }
 
@@ -534,7 +579,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(128) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
@@ -607,10 +652,9 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
           for (int k = 0; k < steps; k += 4) {
             if (!mbar_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
             tc_fence_after();
-            for (int e = 0; e < min(4, steps - k); ++e)
-              for (int i = 0; i < p.np; ++i)
-                tc_mma(tmem_base + b * 64, ag_desc(s_w + s * AG_TILE, !p.w_kmajor, e), ag_desc(s_u + (i * p.kb + k / 4) * block, false, e), idesc,
-                       k + e + i > 0 ? 1u : 0u);
+            const uint32_t d = tmem_base + b * 128;
+            ag_issue_parts(p.np, d, d + 64, ag_desc(s_w + s * AG_TILE, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T,
+                           ag_desc(s_u + (k / 4) * block, false), (uint64_t)(p.kb * block) >> 4, idesc, min(4, steps - k), k == 0);
             tc_commit(wempty(s));
             if (++s == AS_RING) { s = 0; ph ^= 1u; }
           }
@@ -692,11 +736,15 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
         if (as_any(!ok)) return false;                                // (and V's readers of the tile before are done)
         tc_fence_after();
         if (half * 32 < t.n16) {
-          uint32_t x[32];
-          tc_ld32(tmem_base + ((uint32_t)(q * 32) << 16) + b * 64 + half * 32, x);
+          float x[32];
+          const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + half * 32;
+#pragma unroll
+          for (int j = 0; j < 32; ++j) x[j] = 0.f;
+          ag_gather(d, x);
+          if (p.np > 1) ag_gather(d + 64, x);
 #pragma unroll
           for (int j = 0; j < 32; ++j)
-            if (half * 32 + j < p.tn) v[(half * 32 + j) * 128 + q * 32 + lane] = __uint_as_float(x[j]) * scale;
+            if (half * 32 + j < p.tn) v[(half * 32 + j) * 128 + q * 32 + lane] = x[j] * scale;
         }
         tc_fence_before();
         mbar_arrive(accempty(b));
@@ -723,7 +771,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
   __syncthreads();
   if (warp == 1) {
     tc_fence_after();
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(128) : "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(256) : "memory");
   }
 }
 
@@ -731,7 +779,30 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
 // Tiles of 128 x 128 of dA and dB.  Both operands are rows of the workspace, contraction over the rows: parts 0 x 0 are one
 // accumulator, the smaller products (0 x 1, 1 x 0, 1 x 1, 0 x 2, 2 x 0: the others are below 2^-24) a second, so that the sum of the large
 // ones is rounded no more often than it must be.
-constexpr int AR_STAGES = 2, AR_STAGE = 6 * AG_TILE;
+// Every AR_SEGMENT blocks of 32 rows the accumulators are emptied into registers: the tensor core's sums lose about 2^-26 of themselves
+// per step of 16, always towards zero (4096 terms in one go: 4e-6 of the result; in pieces of 256: below 1e-6).
+constexpr int AR_BLOCK = AG_TILE / 2, AR_STAGES = 4, AR_STAGE = 6 * AR_BLOCK, AR_SEGMENT = 8;
+// up to two steps of 16: parts 0 x 0 into d, the smaller products into d + 128
+template <int PA, int PB>
+__device__ __forceinline__ void ar_issue(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, int n, bool fresh) {
+  constexpr uint64_t part = AR_BLOCK >> 4;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    if (e >= n) break;
+    uint32_t acc = fresh && e == 0 ? 0u : 1u;
+    tc_mma(d, a, b, idesc, acc);
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+#pragma unroll
+      for (int j = 0; j < PB; ++j)
+        if (i + j > 0 && i + j <= 2) {
+          tc_mma(d + 128, a + i * part, b + j * part, idesc, acc);
+          acc = 1u;
+        }
+    a += AG_STEP_T;
+    b += AG_STEP_T;
+  }
+}
 struct AgGradSide { int parts_a, parts_b, M, N; float* out; };        // dA: x' (P) by du (r); dB: u (r) by dv (Q)
 struct AgGrad {
   AdaptersCall c;
@@ -799,15 +870,15 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
         const Unit t = unit(u);
         const AgGradSide& side = p.side[t.side];
         const int nb = (t.n16 + 63) / 64;
-        for (int x = 0; x < t.steps; x += 4, ++it) {
+        for (int x = 0; x < t.steps; x += 2, ++it) {
           if (!mbar_wait(empty(s), ph ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          const uint32_t a = base + s * AR_STAGE, b = a + 3 * AG_TILE;
+          const uint32_t a = base + s * AR_STAGE, b = a + 3 * AR_BLOCK;
           const int y = (int)t.at + x * 16;
-          mbar_arrive_expect_tx(full(s), (uint32_t)(8192 * (2 * side.parts_a + nb * side.parts_b)));
+          mbar_arrive_expect_tx(full(s), (uint32_t)(4096 * (2 * side.parts_a + nb * side.parts_b)));
           for (int i = 0; i < side.parts_a; ++i)
-            for (int j = 0; j < 2; ++j) tma_load_3d(a + i * AG_TILE + j * 8192, &maps.a[t.side], full(s), t.m0 + j * 64, y, i);
+            for (int j = 0; j < 2; ++j) tma_load_3d(a + i * AR_BLOCK + j * 4096, &maps.a[t.side], full(s), t.m0 + j * 64, y, i);
           for (int i = 0; i < side.parts_b; ++i)
-            for (int j = 0; j < nb; ++j) tma_load_3d(b + i * AG_TILE + j * 8192, &maps.b[t.side], full(s), t.n0 + j * 64, y, i);
+            for (int j = 0; j < nb; ++j) tma_load_3d(b + i * AR_BLOCK + j * 4096, &maps.b[t.side], full(s), t.n0 + j * 64, y, i);
           if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
         }
       }
@@ -825,76 +896,68 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
         const Unit t = unit(u);
         if (t.steps == 0) continue;
         const AgGradSide& side = p.side[t.side];
-        const int b = done & 1;
-        if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-        tc_fence_after();
-        const uint32_t d = tmem_base + b * 256, idesc = ag_idesc(true, true, t.n16);
-        uint32_t small = 0;
-        for (int x = 0; x < t.steps; x += 4) {
+        const uint32_t idesc = ag_idesc(true, true, t.n16);
+        int left = 0, b = 0;                               // blocks left of the segment; its accumulator
+        for (int x = 0; x < t.steps && ok; x += 2) {
+          const bool fresh = left == 0;
+          if (fresh) {
+            left = AR_SEGMENT;
+            b = done & 1;
+            if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
+          }
           if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
           tc_fence_after();
-          const uint32_t pa = base + s * AR_STAGE, pb = pa + 3 * AG_TILE;
-          for (int e = 0; e < min(4, t.steps - x); ++e) {
-            tc_mma(d, ag_desc(pa, true, e), ag_desc(pb, true, e), idesc, x + e > 0 ? 1u : 0u);
-            for (int i = 0; i < side.parts_a; ++i)
-              for (int j = 0; j < side.parts_b; ++j)
-                if (i + j > 0 && i + j <= 2) {
-                  tc_mma(d + 128, ag_desc(pa + i * AG_TILE, true, e), ag_desc(pb + j * AG_TILE, true, e), idesc, small);
-                  small = 1;
-                }
-          }
+          const uint32_t pa = base + s * AR_STAGE, d = tmem_base + b * 256;
+          const uint64_t da = ag_desc(pa, true, 4096), db = ag_desc(pa + 3 * AR_BLOCK, true, 4096);
+          const int n = min(2, t.steps - x);
+          if (side.parts_a == 3 && side.parts_b == 3) ar_issue<3, 3>(d, da, db, idesc, n, fresh);
+          else if (side.parts_a == 3) ar_issue<3, 1>(d, da, db, idesc, n, fresh);
+          else ar_issue<1, 3>(d, da, db, idesc, n, fresh);
           tc_commit(empty(s));
           if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
+          if (--left == 0 || x + 2 >= t.steps) { tc_commit(accfull(b)); ++done; left = 0; }
         }
-        if (ok) tc_commit(accfull(b));
-        ++done;
       }
     }
   } else {
     const int q = warp & 3, half = (warp - 2) >> 2;
     uint32_t done = 0;
-    for (long long u = blockIdx.x; u < units; u += gridDim.x) {
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       const Unit t = unit(u);
       const AgGradSide& side = p.side[t.side];
-      const int b = done & 1;
-      if (t.steps > 0) {
-        if (!__all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit))) break;
+      float v[64];
+#pragma unroll
+      for (int j = 0; j < 64; ++j) v[j] = 0.f;
+      for (int x = 0; x < t.steps && ok; x += 2 * AR_SEGMENT) {
+        const int b = done & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit));
+        if (!ok) break;
         tc_fence_after();
-      }
-      const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256;
-      const int m = t.m0 + q * 32 + lane;
-      const float scale = t.side ? __ldg(k.s + t.a) : 1.0f;           // du has it already
-#pragma unroll 1
-      for (int c = half * 64; c < min(half * 64 + 64, t.n16); c += 32) {
-        float v[32];
-        if (t.steps > 0) {
-          uint32_t w[32];
-          tc_ld32(d + c, w);
+        const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256 + half * 64;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = __uint_as_float(w[j]);
-          tc_ld32(d + 128 + c, w);
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = (v[j] + __uint_as_float(w[j])) * scale;
-        } else {
-#pragma unroll
-          for (int j = 0; j < 32; ++j) v[j] = 0.f;
+        for (int c = 0; c < 64; c += 32) {
+          if (half * 64 + c >= t.n16) break;
+          ag_gather(d + c, v + c);
+          ag_gather(d + 128 + c, v + c);
         }
-        if (m < side.M) {
-          float* out = side.out + ((int64_t)t.a * side.M + m) * side.N + t.n0 + c;
-#pragma unroll
-          for (int j = 0; j < 32; j += 4) {
-            if (t.n0 + c + j >= side.N) break;                        // N is a multiple of 8
-            float x[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) x[e] = (t.side ? m : t.n0 + c + j + e) < t.rank ? v[j + e] : 0.f;
-            *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
-          }
-        }
-      }
-      if (t.steps > 0) {
         tc_fence_before();
         mbar_arrive(accempty(b));
         ++done;
+      }
+      if (!ok) break;
+      const int m = t.m0 + q * 32 + lane;
+      const float scale = t.side ? __ldg(k.s + t.a) : 1.0f;           // du has it already
+      if (m < side.M) {
+        float* out = side.out + ((int64_t)t.a * side.M + m) * side.N + t.n0 + half * 64;
+#pragma unroll
+        for (int j = 0; j < 64; j += 4) {
+          if (t.n0 + half * 64 + j >= side.N) break;                  // N is a multiple of 8
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = (t.side ? m : t.n0 + half * 64 + j + e) < t.rank ? v[j + e] * scale : 0.f;
+          *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
+        }
       }
     }
   }
@@ -1012,6 +1075,7 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   // smaller tiles where large ones would leave SMs without any
   p.tn = 128;
   while (p.tn > 32 && (int64_t)c.T * p.m_tiles / p.tn < 100) p.tn /= 2;
+  p.segment = out.np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
   const size_t stage = AG_TILE + (size_t)p.np * p.tn * 128, table = ag_table_bytes(c.k.n);
   p.stages = (int)std::min<size_t>(8, (AG_SMEM - AG_BARS - table) / stage);
   QB_TRY(parts_map(&maps.rows, in, l.rows, p.tn));
@@ -1059,10 +1123,10 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
   p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
-  QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 64));
-  QB_TRY(parts_map(&maps.b[0], l.du, l.rows, 64));
-  QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 64));
-  QB_TRY(parts_map(&maps.b[1], l.dv, l.rows, 64));
+  QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 32));
+  QB_TRY(parts_map(&maps.b[0], l.du, l.rows, 32));
+  QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 32));
+  QB_TRY(parts_map(&maps.b[1], l.dv, l.rows, 32));
   const int64_t per = (int64_t)((c.k.P + 127) / 128 + (c.k.Q + 127) / 128) * ((c.k.r + 127) / 128);
   return ag_launch(adapters_grad_kernel, ready, maps, p, AG_THREADS, AR_STAGES * AR_STAGE + AG_BARS + ag_table_bytes(c.k.n), per * c.k.n, st);
 }
