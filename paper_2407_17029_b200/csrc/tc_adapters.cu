@@ -233,6 +233,18 @@ struct AgShrink {
 };
 struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the rows' parts in boxes of tn rows and of 16
 
+// The warps that load and that issue MMAs walk their loops whole, on values that are the same in every lane, and one elected lane
+// issues: the operands then lie in uniform registers (12 cycles an MMA; from one lane's private loop 60).
+__device__ __forceinline__ int ag_uni(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ bool ag_elect() {
+  uint32_t leader;
+  asm volatile("{\n .reg .pred q;\n elect.sync _|q, 0xffffffff;\n selp.u32 %0, 1, 0, q;\n}" : "=r"(leader));
+  return leader != 0;
+}
+__device__ __forceinline__ bool ag_wait(uint32_t bar, uint32_t parity, int* status, long long limit) {     // by a whole warp
+  return __all_sync(0xffffffffu, mbar_wait(bar, parity, status, limit));
+}
+
 // A tile of one adapter's rows.
 struct AgRows { int a, j, rows, n16; uint32_t at; };   // adapter, first entry in the plan, rows, the same in steps of 16, place in the workspace
 __device__ __forceinline__ AgRows ag_rows(const AdaptersCall& c, const AgGroups& g, uint32_t tile, int tn) {
@@ -244,6 +256,9 @@ __device__ __forceinline__ AgRows ag_rows(const AdaptersCall& c, const AgGroups&
   t.rows = min(tn, plan_start(c, t.a + 1) - t.j);
   t.n16 = (t.rows + 15) & ~15;
   return t;
+}
+__device__ __forceinline__ AgRows ag_uni(const AgRows& t) {
+  return AgRows{ag_uni(t.a), ag_uni(t.j), ag_uni(t.rows), ag_uni(t.n16), (uint32_t)ag_uni((int)t.at)};
 }
 // Rows of part `part`, 64 columns from k0 on.  Returns nothing: the bytes are n16 * 128.
 __device__ __forceinline__ void ag_load_rows(const AgMaps3& maps, uint32_t dst, uint32_t bar, int k0, const AgRows& t, int tn, int part) {
@@ -342,51 +357,64 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
   AgRows t;
   int m0;
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0, ph = 0;
-      int s = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        if (!unit(u, t, m0)) continue;
-        for (int k = 0; k < steps; k += 4, ++it) {
-          if (!mbar_wait(empty(s), ph ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          const uint32_t w = base + s * stage_bytes;
+    const uint32_t ring = (uint32_t)ag_uni((int)base);
+    const bool leader = ag_elect();
+    uint32_t it = 0, ph = 0;
+    int s = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+      if (!unit(u, t, m0)) continue;
+      t = ag_uni(t);
+      m0 = ag_uni(m0);
+      for (int k = 0; k < steps; k += 4, ++it) {
+        ok = ag_wait(empty(s), ph ^ 1u, p.status, p.wait_limit);
+        if (!ok) break;
+        const uint32_t w = ring + s * stage_bytes;
+        if (leader) {
           mbar_arrive_expect_tx(full(s), AG_TILE + (uint32_t)p.np * t.n16 * 128);
           ag_load_weights(maps, w, full(s), p.w_kmajor, k * 16, m0, t.a);
           for (int i = 0; i < p.np; ++i) ag_load_rows(maps, w + AG_TILE + i * p.tn * 128, full(s), k * 16, t, p.tn, i);
-          if (++s == p.stages) { s = 0; ph ^= 1u; }
         }
-      }
-      if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
-        const uint32_t n = (uint32_t)p.stages, lo = it > n ? it - n : 0;
-        for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % n), (j / n) & 1u, p.status, p.wait_limit);
+        __syncwarp();
+        if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
     }
+    if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
+      const uint32_t n = (uint32_t)p.stages, lo = it > n ? it - n : 0;
+      for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % n), (j / n) & 1u, p.status, p.wait_limit);
+    }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t ph = 0, done = 0;
-      int s = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        if (!unit(u, t, m0)) continue;
-        const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
-        int left = 0, b = 0;                               // blocks left of the segment; its accumulator
-        for (int k = 0; k < steps && ok; k += 4) {
-          const bool fresh = left == 0;
-          if (fresh) {
-            left = p.segment;
-            b = done & 1;
-            if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          }
-          if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t w = base + s * stage_bytes, d = tmem_base + b * 256;
+    const uint32_t ring = (uint32_t)ag_uni((int)base), tmem = (uint32_t)ag_uni((int)tmem_base);
+    const bool leader = ag_elect();
+    uint32_t ph = 0, done = 0;
+    int s = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+      if (!unit(u, t, m0)) continue;
+      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, ag_uni(t.n16));
+      int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
+      for (int k = 0; k < steps; k += 4) {
+        const bool fresh = left == 0;
+        if (fresh) {
+          left = p.segment;
+          b = done & 1;
+          ok = ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit);
+          if (!ok) break;
+        }
+        ok = ag_wait(full(s), ph, p.status, p.wait_limit);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t w = ring + s * stage_bytes, d = tmem + b * 256;
+        const bool last = --left == 0 || k + 4 >= steps;
+        if (leader) {
           ag_issue_parts(p.np, d, d + 128, ag_desc(w, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T, ag_desc(w + AG_TILE, false),
                          (uint64_t)(p.tn * 128) >> 4, idesc, min(4, steps - k), fresh);
           tc_commit(empty(s));
-          if (++s == p.stages) { s = 0; ph ^= 1u; }
-          if (--left == 0 || k + 4 >= steps) { tc_commit(accfull(b)); ++done; left = 0; }
+          if (last) tc_commit(accfull(b));
         }
+        __syncwarp();
+        if (last) { ++done; left = 0; }
+        if (++s == p.stages) { s = 0; ph ^= 1u; }
       }
     }
   } else {
@@ -612,116 +640,125 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
   const int w = p.lam * (p.y.dtype == QBLORA_F32 ? 4 : 2);
 
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0, ph = 0, n = 0;
-      int s = 0;
-      bool ok = true;
-      each([&](const AgRows& t, int steps, int first, int last) {
-        if (!mbar_wait(uempty, (n & 1u) ^ 1u, p.status, p.wait_limit)) return ok = false;
-        const int kb = (steps + 3) / 4;
+    const uint32_t ring = (uint32_t)ag_uni((int)s_w), at_u = (uint32_t)ag_uni((int)s_u);
+    const bool leader = ag_elect();
+    uint32_t it = 0, ph = 0, n = 0;
+    int s = 0;
+    bool ok = true;
+    each([&](const AgRows& t_, int steps, int first, int last) {
+      const AgRows t = ag_uni(t_);
+      const int kb = (ag_uni(steps) + 3) / 4;
+      ok = ag_wait(uempty, (n & 1u) ^ 1u, p.status, p.wait_limit);
+      if (!ok) return false;
+      if (leader) {
         mbar_arrive_expect_tx(ufull, (uint32_t)(p.np * kb * t.n16 * 128));
         for (int i = 0; i < p.np; ++i)
-          for (int k = 0; k < kb; ++k) ag_load_rows(maps, s_u + (i * p.kb + k) * block, ufull, k * 64, t, p.tn, i);
-        ++n;
-        for (int m = first; m < last; ++m)
-          for (int k = 0; k < kb; ++k, ++it) {
-            if (!mbar_wait(wempty(s), ph ^ 1u, p.status, p.wait_limit)) return ok = false;
-            mbar_arrive_expect_tx(wfull(s), AG_TILE);
-            ag_load_weights(maps, s_w + s * AG_TILE, wfull(s), p.w_kmajor, k * 64, m * 128, t.a);
-            if (++s == AS_RING) { s = 0; ph ^= 1u; }
-          }
-        return true;
-      });
-      if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
-        if (n) mbar_wait(ufull, (n - 1) & 1u, p.status, p.wait_limit);
-        const uint32_t lo = it > (uint32_t)AS_RING ? it - AS_RING : 0;
-        for (uint32_t j = lo; j < it; ++j) mbar_wait(wfull(j % AS_RING), (j / AS_RING) & 1u, p.status, p.wait_limit);
+          for (int k = 0; k < kb; ++k) ag_load_rows(maps, at_u + (i * p.kb + k) * block, ufull, k * 64, t, p.tn, i);
       }
+      __syncwarp();
+      ++n;
+      for (int m = first; m < last; ++m)
+        for (int k = 0; k < kb; ++k, ++it) {
+          ok = ag_wait(wempty(s), ph ^ 1u, p.status, p.wait_limit);
+          if (!ok) return false;
+          if (leader) {
+            mbar_arrive_expect_tx(wfull(s), AG_TILE);
+            ag_load_weights(maps, ring + s * AG_TILE, wfull(s), p.w_kmajor, k * 64, m * 128, t.a);
+          }
+          __syncwarp();
+          if (++s == AS_RING) { s = 0; ph ^= 1u; }
+        }
+      return true;
+    });
+    if (!ok) {   // give copies already in flight a bounded chance to land before the CTA exits
+      if (n) mbar_wait(ufull, (n - 1) & 1u, p.status, p.wait_limit);
+      const uint32_t lo = it > (uint32_t)AS_RING ? it - AS_RING : 0;
+      for (uint32_t j = lo; j < it; ++j) mbar_wait(wfull(j % AS_RING), (j / AS_RING) & 1u, p.status, p.wait_limit);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t ph = 0, done = 0, n = 0;
-      int s = 0;
-      each([&](const AgRows& t, int steps, int first, int last) {
-        if (!mbar_wait(ufull, n & 1u, p.status, p.wait_limit)) return false;
-        const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
-        for (int m = first; m < last; ++m, ++done) {
-          const int b = done & 1;
-          if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
+    const uint32_t ring = (uint32_t)ag_uni((int)s_w), at_u = (uint32_t)ag_uni((int)s_u), tmem = (uint32_t)ag_uni((int)tmem_base);
+    const bool leader = ag_elect();
+    uint32_t ph = 0, done = 0, n = 0;
+    int s = 0;
+    each([&](const AgRows& t, int steps_, int first, int last) {
+      const int steps = ag_uni(steps_);
+      if (!ag_wait(ufull, n & 1u, p.status, p.wait_limit)) return false;
+      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, ag_uni(t.n16));
+      for (int m = first; m < last; ++m, ++done) {
+        const int b = done & 1;
+        if (!ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
+        tc_fence_after();
+        for (int k = 0; k < steps; k += 4) {
+          if (!ag_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
           tc_fence_after();
-          for (int k = 0; k < steps; k += 4) {
-            if (!mbar_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
-            tc_fence_after();
-            const uint32_t d = tmem_base + b * 128;
-            ag_issue_parts(p.np, d, d + 64, ag_desc(s_w + s * AG_TILE, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T,
-                           ag_desc(s_u + (k / 4) * block, false), (uint64_t)(p.kb * block) >> 4, idesc, min(4, steps - k), k == 0);
+          const uint32_t d = tmem + b * 128;
+          if (leader) {
+            ag_issue_parts(p.np, d, d + 64, ag_desc(ring + s * AG_TILE, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T,
+                           ag_desc(at_u + (k / 4) * block, false), (uint64_t)(p.kb * block) >> 4, idesc, min(4, steps - k), k == 0);
             tc_commit(wempty(s));
-            if (++s == AS_RING) { s = 0; ph ^= 1u; }
+            if (k + 4 >= steps) {
+              tc_commit(accfull(b));
+              if (m + 1 == last) tc_commit(uempty);
+            }
           }
-          tc_commit(accfull(b));
+          __syncwarp();
+          if (++s == AS_RING) { s = 0; ph ^= 1u; }
         }
-        tc_commit(uempty);
-        ++n;
-        return true;
-      });
-    }
-  } else if (warp == 2) {
-    // ---- Y's rows in: a lane per row
+      }
+      ++n;
+      return true;
+    });
+  } else if (warp == 2 || warp == 3) {
+    // ---- Y's rows in (warp 2) and out: a lane per row.  The tile's row numbers are looked up once: lane l has rows l and l + 32.
+    const bool out = warp == 3;
     uint32_t it = 0, ph = 0;
     int s = 0;
     bool ok = true;
     each([&](const AgRows& t, int, int first, int last) {
+      const int rows0 = lane < t.rows ? row_of(t, lane) : -1, rows1 = lane + 32 < t.rows ? row_of(t, lane + 32) : -1;
       for (int m = first; m < last; ++m) {
         const AsSlabs y(p, m * 128, t.rows);
-        const char* from = static_cast<const char*>(p.y.data) + (int64_t)m * 128 * w;
+        char* tile = static_cast<char*>(p.y.data) + (int64_t)m * 128 * w;
         for (int i = 0; i < y.n; ++i, ++it) {
           int r0, count, off, len;
           y.get(i, t.rows, r0, count, off, len);
-          if (!__all_sync(0xffffffffu, mbar_wait(gone(s), ph ^ 1u, p.status, p.wait_limit))) return ok = false;
-          int there = 0;
-          for (int r = lane; r < count; r += 32) there += row_of(t, r0 + r) >= 0;
-          there = __reduce_add_sync(0xffffffffu, there);
-          if (lane == 0) mbar_arrive_expect_tx(in(s), (uint32_t)(there * len));
-          __syncwarp();
-          for (int r = lane; r < count; r += 32) {
-            const int row = row_of(t, r0 + r);
-            if (row >= 0) as_bulk_load(s_slab + s * AS_SLAB + r * y.pitch, from + row * y_pitch + off, (uint32_t)len, in(s));
+          if (!ag_wait(out ? summed(s) : gone(s), out ? ph : ph ^ 1u, p.status, p.wait_limit)) return ok = false;
+          // this lane's rows of the slab: r0 + lane and r0 + lane + 32
+          int row[2];
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int r = r0 + lane + 32 * e, x0 = __shfl_sync(0xffffffffu, rows0, r & 31), x1 = __shfl_sync(0xffffffffu, rows1, r & 31);
+            row[e] = lane + 32 * e < count ? (r < 32 ? x0 : x1) : -1;
+          }
+          const uint32_t slab = s_slab + s * AS_SLAB + lane * y.pitch;
+          if (out) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (row[e] >= 0) as_bulk_store(tile + row[e] * y_pitch + off, slab + 32 * e * y.pitch, (uint32_t)len);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            // the slab before has been read by its stores; this one's go on
+            asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
+            __syncwarp();
+            if (lane == 0 && it > 0) mbar_arrive(gone(s == 0 ? p.slabs - 1 : s - 1));
+          } else {
+            const int there = __popc(__ballot_sync(0xffffffffu, row[0] >= 0)) + __popc(__ballot_sync(0xffffffffu, row[1] >= 0));
+            if (lane == 0) mbar_arrive_expect_tx(in(s), (uint32_t)(there * len));
+            __syncwarp();
+#pragma unroll
+            for (int e = 0; e < 2; ++e)
+              if (row[e] >= 0) as_bulk_load(slab + 32 * e * y.pitch, tile + row[e] * y_pitch + off, (uint32_t)len, in(s));
           }
           if (++s == p.slabs) { s = 0; ph ^= 1u; }
         }
       }
       return true;
     });
-    if (!ok) {
+    if (out) {
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");       // written, not only read
+    } else if (!ok) {
       const uint32_t n = (uint32_t)p.slabs, lo = it > n ? it - n : 0;
       for (uint32_t j = lo; j < it; ++j) mbar_wait(in(j % n), (j / n) & 1u, p.status, p.wait_limit);
     }
-  } else if (warp == 3) {
-    // ---- and out
-    uint32_t ph = 0;
-    int s = 0;
-    each([&](const AgRows& t, int, int first, int last) {
-      for (int m = first; m < last; ++m) {
-        const AsSlabs y(p, m * 128, t.rows);
-        char* to = static_cast<char*>(p.y.data) + (int64_t)m * 128 * w;
-        for (int i = 0; i < y.n; ++i) {
-          int r0, count, off, len;
-          y.get(i, t.rows, r0, count, off, len);
-          if (!__all_sync(0xffffffffu, mbar_wait(summed(s), ph, p.status, p.wait_limit))) return false;
-          for (int r = lane; r < count; r += 32) {
-            const int row = row_of(t, r0 + r);
-            if (row >= 0) as_bulk_store(to + row * y_pitch + off, s_slab + s * AS_SLAB + r * y.pitch, (uint32_t)len);
-          }
-          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
-          __syncwarp();
-          if (lane == 0) mbar_arrive(gone(s));
-          if (++s == p.slabs) { s = 0; ph ^= 1u; }
-        }
-      }
-      return true;
-    });
-    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");         // written, not only read
   } else {
     const int q = warp & 3, half = (warp - 4) >> 2, etid = tid - 128;
     uint32_t done = 0, ph = 0;
@@ -861,62 +898,76 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     return t;
   };
 
+  auto uniform = [&](Unit t) {
+    t.a = ag_uni(t.a); t.side = ag_uni(t.side); t.m0 = ag_uni(t.m0); t.n0 = ag_uni(t.n0); t.n16 = ag_uni(t.n16); t.steps = ag_uni(t.steps);
+    t.at = (uint32_t)ag_uni((int)t.at);
+    return t;
+  };
   if (warp == 0) {
-    if (lane == 0) {
-      uint32_t it = 0, ph = 0;
-      int s = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        const Unit t = unit(u);
-        const AgGradSide& side = p.side[t.side];
-        const int nb = (t.n16 + 63) / 64;
-        for (int x = 0; x < t.steps; x += 2, ++it) {
-          if (!mbar_wait(empty(s), ph ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          const uint32_t a = base + s * AR_STAGE, b = a + 3 * AR_BLOCK;
-          const int y = (int)t.at + x * 16;
-          mbar_arrive_expect_tx(full(s), (uint32_t)(4096 * (2 * side.parts_a + nb * side.parts_b)));
-          for (int i = 0; i < side.parts_a; ++i)
+    const uint32_t ring = (uint32_t)ag_uni((int)base);
+    const bool leader = ag_elect();
+    uint32_t it = 0, ph = 0;
+    int s = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+      const Unit t = uniform(unit(u));
+      const int parts_a = p.side[t.side].parts_a, parts_b = p.side[t.side].parts_b, nb = (t.n16 + 63) / 64;
+      for (int x = 0; x < t.steps; x += 2, ++it) {
+        ok = ag_wait(empty(s), ph ^ 1u, p.status, p.wait_limit);
+        if (!ok) break;
+        const uint32_t a = ring + s * AR_STAGE, b = a + 3 * AR_BLOCK;
+        const int y = (int)t.at + x * 16;
+        if (leader) {
+          mbar_arrive_expect_tx(full(s), (uint32_t)(4096 * (2 * parts_a + nb * parts_b)));
+          for (int i = 0; i < parts_a; ++i)
             for (int j = 0; j < 2; ++j) tma_load_3d(a + i * AR_BLOCK + j * 4096, &maps.a[t.side], full(s), t.m0 + j * 64, y, i);
-          for (int i = 0; i < side.parts_b; ++i)
+          for (int i = 0; i < parts_b; ++i)
             for (int j = 0; j < nb; ++j) tma_load_3d(b + i * AR_BLOCK + j * 4096, &maps.b[t.side], full(s), t.n0 + j * 64, y, i);
-          if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
         }
-      }
-      if (!ok) {
-        const uint32_t lo = it > (uint32_t)AR_STAGES ? it - AR_STAGES : 0;
-        for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % AR_STAGES), (j / AR_STAGES) & 1u, p.status, p.wait_limit);
+        __syncwarp();
+        if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
       }
     }
+    if (!ok) {
+      const uint32_t lo = it > (uint32_t)AR_STAGES ? it - AR_STAGES : 0;
+      for (uint32_t j = lo; j < it; ++j) mbar_wait(full(j % AR_STAGES), (j / AR_STAGES) & 1u, p.status, p.wait_limit);
+    }
   } else if (warp == 1) {
-    if (lane == 0) {
-      uint32_t ph = 0, done = 0;
-      int s = 0;
-      bool ok = true;
-      for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-        const Unit t = unit(u);
-        if (t.steps == 0) continue;
-        const AgGradSide& side = p.side[t.side];
-        const uint32_t idesc = ag_idesc(true, true, t.n16);
-        int left = 0, b = 0;                               // blocks left of the segment; its accumulator
-        for (int x = 0; x < t.steps && ok; x += 2) {
-          const bool fresh = left == 0;
-          if (fresh) {
-            left = AR_SEGMENT;
-            b = done & 1;
-            if (!mbar_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) { ok = false; break; }
-          }
-          if (!mbar_wait(full(s), ph, p.status, p.wait_limit)) { ok = false; break; }
-          tc_fence_after();
-          const uint32_t pa = base + s * AR_STAGE, d = tmem_base + b * 256;
+    const uint32_t ring = (uint32_t)ag_uni((int)base), tmem = (uint32_t)ag_uni((int)tmem_base);
+    const bool leader = ag_elect();
+    uint32_t ph = 0, done = 0;
+    int s = 0;
+    bool ok = true;
+    for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
+      const Unit t = uniform(unit(u));
+      const int parts_a = p.side[t.side].parts_a, parts_b = p.side[t.side].parts_b;
+      const uint32_t idesc = ag_idesc(true, true, t.n16);
+      int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
+      for (int x = 0; x < t.steps; x += 2) {
+        const bool fresh = left == 0;
+        if (fresh) {
+          left = AR_SEGMENT;
+          b = done & 1;
+          ok = ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit);
+          if (!ok) break;
+        }
+        ok = ag_wait(full(s), ph, p.status, p.wait_limit);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t pa = ring + s * AR_STAGE, d = tmem + b * 256;
+        const bool last = --left == 0 || x + 2 >= t.steps;
+        if (leader) {
           const uint64_t da = ag_desc(pa, true, 4096), db = ag_desc(pa + 3 * AR_BLOCK, true, 4096);
           const int n = min(2, t.steps - x);
-          if (side.parts_a == 3 && side.parts_b == 3) ar_issue<3, 3>(d, da, db, idesc, n, fresh);
-          else if (side.parts_a == 3) ar_issue<3, 1>(d, da, db, idesc, n, fresh);
+          if (parts_a == 3 && parts_b == 3) ar_issue<3, 3>(d, da, db, idesc, n, fresh);
+          else if (parts_a == 3) ar_issue<3, 1>(d, da, db, idesc, n, fresh);
           else ar_issue<1, 3>(d, da, db, idesc, n, fresh);
           tc_commit(empty(s));
-          if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
-          if (--left == 0 || x + 2 >= t.steps) { tc_commit(accfull(b)); ++done; left = 0; }
+          if (last) tc_commit(accfull(b));
         }
+        __syncwarp();
+        if (last) { ++done; left = 0; }
+        if (++s == AR_STAGES) { s = 0; ph ^= 1u; }
       }
     }
   } else {
