@@ -33,7 +33,7 @@ namespace {
 constexpr int AG_THREADS = 320, AG_EPI = 256;       // TMA warp, MMA warp, eight epilogue warps
 constexpr int AG_TILE = 16384;                      // bytes of one 128 x 64 operand tile
 constexpr int AG_POOL_THREADS = 256;
-constexpr int AG_SMEM = 232448 - 1024 - 512;        // of a CTA, without alignment and static variables
+constexpr int AG_SMEM = 232448 - 1024 - 1024;        // of a CTA, without alignment and static variables
 constexpr int AG_BARS = 512;                        // of those, barriers
 
 // ---- adapters' rows: where they lie in the workspace, and their tiles ------------------------------------------------------------
@@ -245,20 +245,17 @@ __device__ __forceinline__ bool ag_wait(uint32_t bar, uint32_t parity, int* stat
   return __all_sync(0xffffffffu, mbar_wait(bar, parity, status, limit));
 }
 
-// A tile of one adapter's rows.
+// A tile of one adapter's rows; the same in every lane of a warp.
 struct AgRows { int a, j, rows, n16; uint32_t at; };   // adapter, first entry in the plan, rows, the same in steps of 16, place in the workspace
 __device__ __forceinline__ AgRows ag_rows(const AdaptersCall& c, const AgGroups& g, uint32_t tile, int tn) {
   AgRows t;
-  t.a = ag_find(g.tile, g.kept, tile);
-  const int i = (int)(tile - g.tile[t.a]) * tn;
-  t.at = g.pad[t.a] + i;
-  t.j = plan_start(c, t.a) + i;
-  t.rows = min(tn, plan_start(c, t.a + 1) - t.j);
+  t.a = ag_uni(ag_find(g.tile, g.kept, tile));
+  const int i = ag_uni((int)(tile - g.tile[t.a])) * tn;
+  t.at = (uint32_t)ag_uni((int)g.pad[t.a]) + i;
+  t.j = ag_uni(plan_start(c, t.a)) + i;
+  t.rows = min(tn, ag_uni(plan_start(c, t.a + 1)) - t.j);
   t.n16 = (t.rows + 15) & ~15;
   return t;
-}
-__device__ __forceinline__ AgRows ag_uni(const AgRows& t) {
-  return AgRows{ag_uni(t.a), ag_uni(t.j), ag_uni(t.rows), ag_uni(t.n16), (uint32_t)ag_uni((int)t.at)};
 }
 // Rows of part `part`, 64 columns from k0 on.  Returns nothing: the bytes are n16 * 128.
 __device__ __forceinline__ void ag_load_rows(const AgMaps3& maps, uint32_t dst, uint32_t bar, int k0, const AgRows& t, int tn, int part) {
@@ -288,27 +285,33 @@ constexpr uint64_t AG_STEP_K = 32 >> 4, AG_STEP_T = 2048 >> 4;
 __device__ __forceinline__ uint64_t ag_desc(uint32_t block, bool transposed, uint32_t group = 8192) {
   return transposed ? smem_desc(block, group, 1024) : smem_desc(block, 16, 1024);
 }
-// The MMAs of up to four steps of 16: the weights by the first part of the rows into d0, by the others into d1.  One thread issues them:
-// with loops that are not unrolled and descriptors built for each, a block of eight MMAs cost it a microsecond (200 decoding rows with an adapter
-// each: shrink 66 us), so everything that can be is a constant here.  fresh: the accumulators begin with this block.
-template <int NP>
-__device__ __forceinline__ void ag_issue(uint32_t d0, uint32_t d1, uint64_t a, uint64_t a_step, uint64_t b, uint64_t part, uint32_t idesc, int n, bool fresh) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (e >= n) break;
-    const uint32_t acc = fresh && e == 0 ? 0u : 1u;
-    tc_mma(d0, a, b, idesc, acc);
-#pragma unroll
-    for (int i = 1; i < NP; ++i) tc_mma(d1, a, b + i * part, idesc, i == 1 ? acc : 1u);
-    a += a_step;
-    b += AG_STEP_K;
+// The MMAs of up to four steps of 16: the weights by the first part of the rows into d0, by the others (each `part` further) into d1.  One
+// lane issues them, and what it computes for an MMA is time between them: whole blocks take constants alone.  fresh: the accumulators
+// begin with this block.
+template <int NP, bool KMAJOR>
+__device__ __forceinline__ void ag_issue(uint32_t d0, uint32_t d1, uint64_t a, uint64_t b, uint64_t part, uint32_t idesc, int n, uint32_t fresh) {
+  constexpr uint64_t STEP = KMAJOR ? AG_STEP_K : AG_STEP_T;
+  const uint64_t b1 = b + part, b2 = b1 + part;
+  auto step = [&](uint64_t x, uint64_t y, uint32_t acc) {
+    tc_mma(d0, a + x, b + y, idesc, acc);
+    if constexpr (NP > 1) tc_mma(d1, a + x, b1 + y, idesc, acc);
+    if constexpr (NP > 2) tc_mma(d1, a + x, b2 + y, idesc, 1u);
+  };
+  step(0, 0, fresh ^ 1u);
+  if (n == 4) {
+    step(STEP, AG_STEP_K, 1u);
+    step(2 * STEP, 2 * AG_STEP_K, 1u);
+    step(3 * STEP, 3 * AG_STEP_K, 1u);
+  } else {
+    for (int e = 1; e < n; ++e) step(e * STEP, e * AG_STEP_K, 1u);
   }
 }
-__device__ __forceinline__ void ag_issue_parts(int np, uint32_t d0, uint32_t d1, uint64_t a, uint64_t a_step, uint64_t b, uint64_t part, uint32_t idesc,
-                                               int n, bool fresh) {
-  if (np == 1) ag_issue<1>(d0, d1, a, a_step, b, part, idesc, n, fresh);
-  else if (np == 2) ag_issue<2>(d0, d1, a, a_step, b, part, idesc, n, fresh);
-  else ag_issue<3>(d0, d1, a, a_step, b, part, idesc, n, fresh);
+template <bool KMAJOR>
+__device__ __forceinline__ void ag_issue_parts(int np, uint32_t d0, uint32_t d1, uint64_t a, uint64_t b, uint64_t part, uint32_t idesc, int n,
+                                               uint32_t fresh) {
+  if (np == 2) ag_issue<2, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
+  else if (np == 3) ag_issue<3, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
+  else ag_issue<1, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
 }
 // v += 32 columns of tensor memory
 __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
@@ -332,7 +335,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
     for (int s = 0; s < p.stages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
+    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI / 32); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -344,7 +347,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot_g;
-  const long long units = (long long)g.tile[g.kept] * p.m_tiles;
+  const long long units = (long long)ag_uni((int)g.tile[g.kept]) * p.m_tiles;
   const int steps = (p.K + 15) / 16;
   asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
   // unit u: tile u / m_tiles, ranks from 128 (u % m_tiles) on; an adapter of a lower rank has none there
@@ -352,7 +355,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     const uint32_t tile = (uint32_t)(u / p.m_tiles);
     m0 = (int)(u - (long long)tile * p.m_tiles) * 128;
     t = ag_rows(p.c, g, tile, p.tn);
-    return m0 < bank_rank(p.c.k, t.a);
+    return m0 < ag_uni(bank_rank(p.c.k, t.a));
   };
   AgRows t;
   int m0;
@@ -364,8 +367,6 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       if (!unit(u, t, m0)) continue;
-      t = ag_uni(t);
-      m0 = ag_uni(m0);
       for (int k = 0; k < steps; k += 4, ++it) {
         ok = ag_wait(empty(s), ph ^ 1u, p.status, p.wait_limit);
         if (!ok) break;
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       if (!unit(u, t, m0)) continue;
-      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, ag_uni(t.n16));
+      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
       int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
       for (int k = 0; k < steps; k += 4) {
         const bool fresh = left == 0;
@@ -407,8 +408,10 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         const uint32_t w = ring + s * stage_bytes, d = tmem + b * 256;
         const bool last = --left == 0 || k + 4 >= steps;
         if (leader) {
-          ag_issue_parts(p.np, d, d + 128, ag_desc(w, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T, ag_desc(w + AG_TILE, false),
-                         (uint64_t)(p.tn * 128) >> 4, idesc, min(4, steps - k), fresh);
+          const uint64_t rows = ag_desc(w + AG_TILE, false), part = (uint64_t)(p.tn * 128) >> 4;
+          const int n = min(4, steps - k);
+          if (p.w_kmajor) ag_issue_parts<true>(p.np, d, d + 128, ag_desc(w, false), rows, part, idesc, n, fresh);
+          else ag_issue_parts<false>(p.np, d, d + 128, ag_desc(w, true), rows, part, idesc, n, fresh);
           tc_commit(empty(s));
           if (last) tc_commit(accfull(b));
         }
@@ -439,7 +442,8 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
           if (p.np > 1) ag_gather(d + 128 + c, v + c);
         }
         tc_fence_before();
-        mbar_arrive(accempty(b));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(accempty(b));
         ++done;
       }
       if (!ok) break;
@@ -466,11 +470,13 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
 }
 
 // ---- spread -------------------------------------------------------------------------------------------------------------------
-// One row tile's u stays in shared memory while tiles of 128 outputs of the pooled kind (q) pass.  Y comes and goes in slabs of up to
-// 16 KB, pieces of whole rows' 128 q, by bulk copies that a warp of its own issues rows ahead of the sums: with plain loads the eight
-// epilogue warps had 16 KB on their way (7000 rows to 11008 outputs 259 us, 1.2 TB/s); here it is every free slab.  The products go
-// through shared memory (V), so that the sums run over a slab in whole 16-byte chunks whatever lambda is.
-constexpr int AS_THREADS = 384, AS_SLAB = 16384, AS_RING = 3;      // loads, MMAs, slabs in, slabs out; eight warps
+// One row tile's u stays in shared memory while tiles of 128 outputs of the pooled kind (q) pass.  What bounds it: Y, in and out.  The
+// products go through shared memory (V), so that Y comes and goes in whole rows' pieces whatever lambda is: slabs of up to 16 KB, asked
+// for as long as one is free by a warp of its own and sent back by another -- in one copy where the tile's rows are neighbours
+// in Y, else row by row.  (Plain loads have no place to come to: what the operands leave of an SM's memory for its L1 is 24 KB,
+// 2.2 TB/s at most.)
+constexpr int AS_EPI = 512, AS_THREADS = 128 + AS_EPI;     // loads, MMAs, slabs in, slabs out; sixteen warps
+constexpr int AS_SLAB = 16384, AS_RING = 3;
 struct AgSpread {
   AdaptersCall c;
   uint32_t rows_there;
@@ -478,11 +484,13 @@ struct AgSpread {
   int slabs;
   int m_tiles, M, w_kmajor, scaled;
   RowsView y;
-  int lam, shift;                       // shift: log2 of the bytes of one q, -1 where they are no power of two
+  int lam, shift;                       // shift: log2 of the bytes of one q, where they are a power of two
+  int boxes;                            // whole slabs of neighbouring rows by tensor copies: pieces of a row's 128 q; 0: none
   float factor;
   int* status;
   long long wait_limit;
 };
+struct AsMaps { AgMaps3 in; CUtensorMap y; };
 
 __device__ __forceinline__ void as_bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
@@ -491,96 +499,105 @@ __device__ __forceinline__ void as_bulk_load(uint32_t dst, const void* src, uint
 __device__ __forceinline__ void as_bulk_store(void* dst, uint32_t src, uint32_t bytes) {
   asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst), "r"(src), "r"(bytes) : "memory");
 }
+__device__ __forceinline__ void as_tensor_store(const CUtensorMap* tm, uint32_t src, int c0, int c1, int c2) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.bulk_group [%0, {%2, %3, %4}], [%1];"
+               ::"l"(tm), "r"(src), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
 
-// whether any thread of the eight epilogue warps says so; a barrier of theirs
+// whether any thread of the epilogue warps says so; a barrier of theirs
 __device__ __forceinline__ bool as_any(bool x) {
   uint32_t y;
-  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 512, p;\n selp.u32 %0, 1, 0, q;\n}"
                : "=r"(y) : "r"((uint32_t)x) : "memory");
   return y != 0;
 }
+__device__ __forceinline__ void ag_gather16(uint32_t taddr, float* v) {
+  uint32_t w[16];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+               : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7]), "=r"(w[8]), "=r"(w[9]),
+                 "=r"(w[10]), "=r"(w[11]), "=r"(w[12]), "=r"(w[13]), "=r"(w[14]), "=r"(w[15])
+               : "r"(taddr) : "memory");
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int j = 0; j < 16; ++j) v[j] += __uint_as_float(w[j]);
+}
 
-// Y's part of one (row tile, q tile): rows in slabs
+// Y's part of one (row tile, q tile) in slabs: `count` rows from r0 on, bytes off .. off + len - 1 of each.  Where a row's 128 q fit a slab
+// several times, whole rows; else pieces of one row.
 struct AsSlabs {
-  int row_bytes, pitch, per, pieces, n;        // bytes of a row's q; of a row in a slab; rows in a slab; slabs to a row; slabs
-  __device__ __forceinline__ AsSlabs(const AgSpread& p, int m0, int rows) {
-    const int w = p.lam * (p.y.dtype == QBLORA_F32 ? 4 : 2), whole = 128 * w;
-    row_bytes = min(128, p.M - m0) * w;
-    per = max(1, AS_SLAB / whole);
+  int rows, row_bytes, per, pitch;             // of the tile; bytes of a row's q; rows to a slab; bytes of a row in a slab
+  int r0, off, count, len;
+  __device__ __forceinline__ AsSlabs(const AgSpread& p, int whole, int m, int rows_) : rows(rows_) {
+    row_bytes = min(128, p.M - m * 128) * (whole >> 7);
+    per = whole <= AS_SLAB ? AS_SLAB / whole : 1;
     pitch = min(whole, AS_SLAB);
-    pieces = (row_bytes + AS_SLAB - 1) / AS_SLAB;
-    n = pieces > 1 ? rows * pieces : (rows + per - 1) / per;
+    r0 = off = 0;
+    size();
   }
-  // slab i: rows [r0, r0 + count), bytes [off, off + len) of each
-  __device__ __forceinline__ void get(int i, int rows, int& r0, int& count, int& off, int& len) const {
-    if (pieces > 1) {
-      r0 = i / pieces;
-      count = 1;
-      off = (i - r0 * pieces) * AS_SLAB;
-      len = min(AS_SLAB, row_bytes - off);
+  __device__ __forceinline__ void size() {
+    count = min(per, rows - r0);
+    len = min(pitch, row_bytes - off);
+  }
+  __device__ __forceinline__ bool there() const { return r0 < rows; }
+  __device__ __forceinline__ void next() {
+    if (off + pitch < row_bytes) {
+      off += pitch;
     } else {
-      r0 = i * per;
-      count = min(per, rows - r0);
       off = 0;
-      len = row_bytes;
+      r0 += per;
     }
+    size();
   }
 };
 
-// 16 bytes of Y += the products of their elements.  QPC: different q in them; 0: lam is no power of two
+// The products of a chunk of 16 bytes of Y.  QPC: different q in it.
+template <int QPC>
+__device__ __forceinline__ void as_products(const float* f, float (&q)[QPC]) {
+  if constexpr (QPC == 1) q[0] = *f;
+  else if constexpr (QPC == 2) { const float2 x = *reinterpret_cast<const float2*>(f); q[0] = x.x; q[1] = x.y; }
+  else {
+#pragma unroll
+    for (int j = 0; j < QPC; j += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(f + j);
+      q[j] = x.x; q[j + 1] = x.y; q[j + 2] = x.z; q[j + 3] = x.w;
+    }
+  }
+}
 template <bool F32, int QPC>
-__device__ __forceinline__ uint4 as_add(uint4 y, const float* v, int first, int lam) {
+__device__ __forceinline__ uint4 as_add(uint4 y, const float (&q)[QPC]) {
   constexpr int E = F32 ? 4 : 8;
-  float x[E];
-  if constexpr (QPC == 0) {
+  uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = v[(first + e) / lam];
-  } else if constexpr (QPC == 8) {
-    const float4 a = *reinterpret_cast<const float4*>(v), b = *reinterpret_cast<const float4*>(v + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
-  } else {
-    float q[QPC];
-    if constexpr (QPC == 4) { const float4 a = *reinterpret_cast<const float4*>(v); q[0] = a.x; q[1] = a.y; q[2] = a.z; q[3] = a.w; }
-    else if constexpr (QPC == 2) { const float2 a = *reinterpret_cast<const float2*>(v); q[0] = a.x; q[1] = a.y; }
-    else q[0] = *v;
-#pragma unroll
-    for (int e = 0; e < E; ++e) x[e] = q[e * QPC / E];
+  for (int e = 0; e < 4; ++e) {
+    if constexpr (F32) w[e] = __float_as_uint(__uint_as_float(w[e]) + q[e * QPC / E]);
+    else w[e] = pack_bf16x2(ag_low(w[e]) + q[2 * e * QPC / E], ag_high(w[e]) + q[(2 * e + 1) * QPC / E]);
   }
-  uint32_t* w = reinterpret_cast<uint32_t*>(&y);
-  if constexpr (F32) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) + x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = pack_bf16x2(ag_low(w[e]) + x[2 * e], ag_high(w[e]) + x[2 * e + 1]);
-  }
-  return y;
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// `count` rows of `len` bytes at `slab`; v: the products of the first row, the others 128 floats on
+// Any slab; v: the products of its first row, the others 128 floats on.  QPC 0: lam is no power of two.
 template <bool F32, int QPC>
-__device__ __forceinline__ void as_sums(uint8_t* slab, int pitch, const float* v, int count, int off, int len, int lam, int shift, int tid) {
+__device__ __noinline__ void as_sums(uint8_t* slab, int pitch, const float* v, int count, int off, int len, int lam, int shift, int tid) {
   const int per = len >> 4, all = per * count;
-  const bool pow2 = (per & (per - 1)) == 0;
-  const int down = 31 - __clz(per);
-#pragma unroll 2
-  for (int i = tid; i < all; i += AG_EPI) {
-    const int row = pow2 ? i >> down : i / per, at = (i - row * per) << 4;
-    const float* vr = v + row * 128;
-    uint4* y = reinterpret_cast<uint4*>(slab + row * pitch + at);
-    if constexpr (QPC == 0) *y = as_add<F32, 0>(*y, vr, (off + at) / (F32 ? 4 : 2), lam);
-    else *y = as_add<F32, QPC>(*y, vr + ((off + at) >> shift), 0, lam);
+  for (int i = tid; i < all; i += AS_EPI) {
+    const int row = i / per, b = (i - row * per) << 4;
+    uint4* at = reinterpret_cast<uint4*>(slab + row * pitch + b);
+    const float* f = v + row * 128;
+    if constexpr (QPC == 0) {
+      constexpr int E = F32 ? 4 : 8;
+      float q[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) q[e] = f[((off + b) / (F32 ? 4 : 2) + e) / lam];
+      *at = as_add<F32, E>(*at, q);
+    } else {
+      float q[QPC];
+      as_products<QPC>(f + ((off + b) >> shift), q);
+      *at = as_add<F32, QPC>(*at, q);
+    }
   }
-}
-template <bool F32>
-__device__ __forceinline__ void as_sums_any(uint8_t* slab, int pitch, const float* v, int count, int off, int len, int lam, int shift, int tid) {
-  if (shift < 0) as_sums<F32, 0>(slab, pitch, v, count, off, len, lam, shift, tid);
-  else if (shift >= 4) as_sums<F32, 1>(slab, pitch, v, count, off, len, lam, shift, tid);
-  else if (shift == 3) as_sums<F32, 2>(slab, pitch, v, count, off, len, lam, shift, tid);
-  else if (shift == 2) as_sums<F32, 4>(slab, pitch, v, count, off, len, lam, shift, tid);
-  else if constexpr (!F32) as_sums<F32, 8>(slab, pitch, v, count, off, len, lam, shift, tid);
 }
 
-__global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __grid_constant__ AgMaps3 maps, const __grid_constant__ AgSpread p) {
+template <bool F32, int QPC>
+__global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __grid_constant__ AsMaps maps, const __grid_constant__ AgSpread p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), s_u = (raw + 1023u) & ~1023u;
   const uint32_t block = (uint32_t)p.tn * 128;                        // one part's 64 ranks
@@ -602,8 +619,8 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     for (int s = 0; s < AS_RING; ++s) { mbar_init(wfull(s), 1); mbar_init(wempty(s), 1); }
     mbar_init(ufull, 1);
     mbar_init(uempty, 1);
-    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
-    for (int i = 0; i < p.slabs; ++i) { mbar_init(in(i), 1); mbar_init(summed(i), AG_EPI); mbar_init(gone(i), 1); }
+    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AS_EPI / 32); }
+    for (int i = 0; i < p.slabs; ++i) { mbar_init(in(i), 1); mbar_init(summed(i), AS_EPI / 32); mbar_init(gone(i), 1); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -615,29 +632,26 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot_g;
-  // A unit is one row tile and some neighbouring q tiles: as many as leave every CTA about four units, so that u is loaded seldom and the
-  // CTAs still end together.
-  const uint32_t tiles = g.tile[g.kept];
+  // A unit is one row tile and every `runs`-th q tile: as many as leave every CTA about four units, so that u is loaded seldom and the
+  // CTAs still end together; neighbouring CTAs are at neighbouring parts of the same rows.
+  const uint32_t tiles = (uint32_t)ag_uni((int)g.tile[g.kept]);
   const int run = (int)min((long long)p.m_tiles, max(1LL, (long long)tiles * p.m_tiles / (4 * gridDim.x)));
   const int runs = (p.m_tiles + run - 1) / run;
   const long long units = (long long)tiles * runs;
   asm volatile("griddepcontrol.wait;" ::: "memory");                  // what the kernels in front have written
-  // calls f(rows, steps of 16 ranks, first and last q tile) for this CTA's units, until it returns false
+  // calls f(rows, steps of 16 ranks, first q tile) for this CTA's units, until it returns false
   auto each = [&](auto&& f) {
     for (long long u = blockIdx.x; u < units; u += gridDim.x) {
       const uint32_t tile = (uint32_t)(u / runs);
-      const int first = (int)(u - (long long)tile * runs) * run;
+      const int first = (int)(u - (long long)tile * runs);
       const AgRows t = ag_rows(p.c, g, tile, p.tn);
-      const int steps = (bank_rank(p.c.k, t.a) + 15) / 16;
-      if (steps > 0 && !f(t, steps, first, min(first + run, p.m_tiles))) return;
+      const int steps = (ag_uni(bank_rank(p.c.k, t.a)) + 15) / 16;
+      if (steps > 0 && !f(t, steps, first)) return;
     }
   };
-  auto row_of = [&](const AgRows& t, int r) {                         // the row of Y of the tile's row r; -1: none
-    const int row = __ldg(p.c.rows + t.j + r);
-    return row < p.c.T ? row : -1;
-  };
-  const int64_t y_pitch = p.y.stride * (p.y.dtype == QBLORA_F32 ? 4 : 2);
-  const int w = p.lam * (p.y.dtype == QBLORA_F32 ? 4 : 2);
+  constexpr int ES = F32 ? 4 : 2;
+  const int whole = 128 * p.lam * ES;                                 // bytes of a row's 128 q
+  const int64_t y_pitch = p.y.stride * ES;
 
   if (warp == 0) {
     const uint32_t ring = (uint32_t)ag_uni((int)s_w), at_u = (uint32_t)ag_uni((int)s_u);
@@ -645,25 +659,24 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     uint32_t it = 0, ph = 0, n = 0;
     int s = 0;
     bool ok = true;
-    each([&](const AgRows& t_, int steps, int first, int last) {
-      const AgRows t = ag_uni(t_);
-      const int kb = (ag_uni(steps) + 3) / 4;
+    each([&](const AgRows& t, int steps, int first) {
+      const int kb = (steps + 3) / 4;
       ok = ag_wait(uempty, (n & 1u) ^ 1u, p.status, p.wait_limit);
       if (!ok) return false;
       if (leader) {
         mbar_arrive_expect_tx(ufull, (uint32_t)(p.np * kb * t.n16 * 128));
         for (int i = 0; i < p.np; ++i)
-          for (int k = 0; k < kb; ++k) ag_load_rows(maps, at_u + (i * p.kb + k) * block, ufull, k * 64, t, p.tn, i);
+          for (int k = 0; k < kb; ++k) ag_load_rows(maps.in, at_u + (i * p.kb + k) * block, ufull, k * 64, t, p.tn, i);
       }
       __syncwarp();
       ++n;
-      for (int m = first; m < last; ++m)
+      for (int m = first; m < p.m_tiles; m += runs)
         for (int k = 0; k < kb; ++k, ++it) {
           ok = ag_wait(wempty(s), ph ^ 1u, p.status, p.wait_limit);
           if (!ok) return false;
           if (leader) {
             mbar_arrive_expect_tx(wfull(s), AG_TILE);
-            ag_load_weights(maps, ring + s * AG_TILE, wfull(s), p.w_kmajor, k * 64, m * 128, t.a);
+            ag_load_weights(maps.in, ring + s * AG_TILE, wfull(s), p.w_kmajor, k * 64, m * 128, t.a);
           }
           __syncwarp();
           if (++s == AS_RING) { s = 0; ph ^= 1u; }
@@ -680,11 +693,10 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     const bool leader = ag_elect();
     uint32_t ph = 0, done = 0, n = 0;
     int s = 0;
-    each([&](const AgRows& t, int steps_, int first, int last) {
-      const int steps = ag_uni(steps_);
+    each([&](const AgRows& t, int steps, int first) {
       if (!ag_wait(ufull, n & 1u, p.status, p.wait_limit)) return false;
-      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, ag_uni(t.n16));
-      for (int m = first; m < last; ++m, ++done) {
+      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
+      for (int m = first; m < p.m_tiles; m += runs, ++done) {
         const int b = done & 1;
         if (!ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
         tc_fence_after();
@@ -693,12 +705,15 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
           tc_fence_after();
           const uint32_t d = tmem + b * 128;
           if (leader) {
-            ag_issue_parts(p.np, d, d + 64, ag_desc(ring + s * AG_TILE, !p.w_kmajor), p.w_kmajor ? AG_STEP_K : AG_STEP_T,
-                           ag_desc(at_u + (k / 4) * block, false), (uint64_t)(p.kb * block) >> 4, idesc, min(4, steps - k), k == 0);
+            const uint32_t w = ring + s * AG_TILE;
+            const uint64_t rows = ag_desc(at_u + (k / 4) * block, false), part = (uint64_t)(p.kb * block) >> 4;
+            const int some = min(4, steps - k);
+            if (p.w_kmajor) ag_issue_parts<true>(p.np, d, d + 64, ag_desc(w, false), rows, part, idesc, some, k == 0);
+            else ag_issue_parts<false>(p.np, d, d + 64, ag_desc(w, true), rows, part, idesc, some, k == 0);
             tc_commit(wempty(s));
             if (k + 4 >= steps) {
               tc_commit(accfull(b));
-              if (m + 1 == last) tc_commit(uempty);
+              if (m + runs >= p.m_tiles) tc_commit(uempty);
             }
           }
           __syncwarp();
@@ -709,44 +724,61 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
       return true;
     });
   } else if (warp == 2 || warp == 3) {
-    // ---- Y's rows in (warp 2) and out: a lane per row.  The tile's row numbers are looked up once: lane l has rows l and l + 32.
+    // ---- Y's slabs in (warp 2) and out.  The tile's row numbers are looked up once: lane l has rows l and l + 32.
     const bool out = warp == 3;
     uint32_t it = 0, ph = 0;
     int s = 0;
     bool ok = true;
-    each([&](const AgRows& t, int, int first, int last) {
-      const int rows0 = lane < t.rows ? row_of(t, lane) : -1, rows1 = lane + 32 < t.rows ? row_of(t, lane + 32) : -1;
-      for (int m = first; m < last; ++m) {
-        const AsSlabs y(p, m * 128, t.rows);
-        char* tile = static_cast<char*>(p.y.data) + (int64_t)m * 128 * w;
-        for (int i = 0; i < y.n; ++i, ++it) {
-          int r0, count, off, len;
-          y.get(i, t.rows, r0, count, off, len);
+    each([&](const AgRows& t, int, int first) {
+      int rows0 = lane < t.rows ? __ldg(p.c.rows + t.j + lane) : -1, rows1 = lane + 32 < t.rows ? __ldg(p.c.rows + t.j + lane + 32) : -1;
+      if (rows0 >= p.c.T) rows0 = -1;
+      if (rows1 >= p.c.T) rows1 = -1;
+      const int row_a = __shfl_sync(0xffffffffu, rows0, 0);
+      const bool neighbours = p.boxes && row_a >= 0 &&
+                              __all_sync(0xffffffffu, (lane >= t.rows || rows0 == row_a + lane) && (lane + 32 >= t.rows || rows1 == row_a + lane + 32));
+      for (int m = first; m < p.m_tiles; m += runs) {
+        char* tile = static_cast<char*>(p.y.data) + (int64_t)m * whole;
+        for (AsSlabs y(p, whole, m, t.rows); y.there(); y.next(), ++it) {
           if (!ag_wait(out ? summed(s) : gone(s), out ? ph : ph ^ 1u, p.status, p.wait_limit)) return ok = false;
-          // this lane's rows of the slab: r0 + lane and r0 + lane + 32
-          int row[2];
+          const uint32_t slab = s_slab + s * AS_SLAB;
+          if (neighbours && y.count == y.per) {
+            // one copy of `per` rows' pieces; what would lie behind the row's end is filled with zeros, and left out on the way back
+            if (lane == 0) {
+              if (out) {
+                as_tensor_store(&maps.y, slab, 0, m * p.boxes, row_a + y.r0);
+              } else {
+                mbar_arrive_expect_tx(in(s), (uint32_t)(y.per * whole));
+                tma_load_3d(slab, &maps.y, in(s), 0, m * p.boxes, row_a + y.r0);
+              }
+            }
+          } else {
+            // this lane's rows of the slab: r0 + lane and r0 + lane + 32
+            int row[2];
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int r = r0 + lane + 32 * e, x0 = __shfl_sync(0xffffffffu, rows0, r & 31), x1 = __shfl_sync(0xffffffffu, rows1, r & 31);
-            row[e] = lane + 32 * e < count ? (r < 32 ? x0 : x1) : -1;
+            for (int e = 0; e < 2; ++e) {
+              const int r = y.r0 + lane + 32 * e, x0 = __shfl_sync(0xffffffffu, rows0, r & 31), x1 = __shfl_sync(0xffffffffu, rows1, r & 31);
+              row[e] = lane + 32 * e < y.count ? (r < 32 ? x0 : x1) : -1;
+            }
+            if (!out) {
+              const int there = __popc(__ballot_sync(0xffffffffu, row[0] >= 0)) + __popc(__ballot_sync(0xffffffffu, row[1] >= 0));
+              if (lane == 0) mbar_arrive_expect_tx(in(s), (uint32_t)(there * y.len));
+              __syncwarp();
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              if (row[e] < 0) continue;
+              const uint32_t at = slab + (lane + 32 * e) * y.pitch;
+              char* g = tile + row[e] * y_pitch + y.off;
+              if (out) as_bulk_store(g, at, (uint32_t)y.len);
+              else as_bulk_load(at, g, (uint32_t)y.len, in(s));
+            }
           }
-          const uint32_t slab = s_slab + s * AS_SLAB + lane * y.pitch;
           if (out) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (row[e] >= 0) as_bulk_store(tile + row[e] * y_pitch + off, slab + 32 * e * y.pitch, (uint32_t)len);
             asm volatile("cp.async.bulk.commit_group;" ::: "memory");
             // the slab before has been read by its stores; this one's go on
             asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
             __syncwarp();
             if (lane == 0 && it > 0) mbar_arrive(gone(s == 0 ? p.slabs - 1 : s - 1));
-          } else {
-            const int there = __popc(__ballot_sync(0xffffffffu, row[0] >= 0)) + __popc(__ballot_sync(0xffffffffu, row[1] >= 0));
-            if (lane == 0) mbar_arrive_expect_tx(in(s), (uint32_t)(there * len));
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              if (row[e] >= 0) as_bulk_load(slab + 32 * e * y.pitch, tile + row[e] * y_pitch + off, (uint32_t)len, in(s));
           }
           if (++s == p.slabs) { s = 0; ph ^= 1u; }
         }
@@ -760,44 +792,61 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
       for (uint32_t j = lo; j < it; ++j) mbar_wait(in(j % n), (j / n) & 1u, p.status, p.wait_limit);
     }
   } else {
-    const int q = warp & 3, half = (warp - 4) >> 2, etid = tid - 128;
+    const int q = warp & 3, part = (warp - 4) >> 2, etid = tid - 128;    // quarter of the lanes, 16 of the columns
+    float* v = reinterpret_cast<float*>(smem_raw + (s_v - raw));
+    // Where a row's 128 q are a power of two of bytes, a whole slab's chunks have the same places every time: chunk etid and
+    // chunk etid + 512 of the slab's 1024, their bytes in the slab and their products in V.
+    const int at0 = etid * 16, at1 = at0 + AS_EPI * 16;
+    int f0 = 0, f1 = 0;
+    if constexpr (QPC > 0) {
+      const int pitch = min(whole, AS_SLAB);
+      f0 = at0 / pitch * 128 + ((at0 & (pitch - 1)) >> p.shift);
+      f1 = at1 / pitch * 128 + ((at1 & (pitch - 1)) >> p.shift);
+    }
     uint32_t done = 0, ph = 0;
     int s = 0;
-    float* v = reinterpret_cast<float*>(smem_raw + (s_v - raw));
-    bool ok = true;
-    each([&](const AgRows& t, int, int first, int last) {
+    each([&](const AgRows& t, int, int first) {
       const float scale = p.scaled ? __ldg(p.c.k.s + t.a) * p.factor : p.factor;
-      for (int m = first; m < last; ++m, ++done) {
+      for (int m = first; m < p.m_tiles; m += runs, ++done) {
         const int b = done & 1;
-        ok = mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit);
+        bool ok = mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit);
         if (as_any(!ok)) return false;                                // (and V's readers of the tile before are done)
         tc_fence_after();
-        if (half * 32 < t.n16) {
-          float x[32];
-          const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + half * 32;
+        if (part * 16 < t.n16) {
+          float x[16];
+          const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + part * 16;
 #pragma unroll
-          for (int j = 0; j < 32; ++j) x[j] = 0.f;
-          ag_gather(d, x);
-          if (p.np > 1) ag_gather(d + 64, x);
+          for (int j = 0; j < 16; ++j) x[j] = 0.f;
+          ag_gather16(d, x);
+          if (p.np > 1) ag_gather16(d + 64, x);
 #pragma unroll
-          for (int j = 0; j < 32; ++j)
-            if (half * 32 + j < p.tn) v[(half * 32 + j) * 128 + q * 32 + lane] = x[j] * scale;
+          for (int j = 0; j < 16; ++j) v[(part * 16 + j) * 128 + q * 32 + lane] = x[j] * scale;
         }
         tc_fence_before();
-        mbar_arrive(accempty(b));
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        const AsSlabs y(p, m * 128, t.rows);
-        for (int i = 0; i < y.n; ++i) {
-          int r0, count, off, len;
-          y.get(i, t.rows, r0, count, off, len);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(accempty(b));
+        asm volatile("bar.sync 1, 512;" ::: "memory");
+        for (AsSlabs y(p, whole, m, t.rows); y.there(); y.next()) {
           ok = __all_sync(0xffffffffu, mbar_wait(in(s), ph, p.status, p.wait_limit));
           if (ok) {
             uint8_t* slab = smem_raw + (s_slab - raw) + s * AS_SLAB;
-            if (p.y.dtype == QBLORA_F32) as_sums_any<true>(slab, y.pitch, v + r0 * 128, count, off, len, p.lam, p.shift, etid);
-            else as_sums_any<false>(slab, y.pitch, v + r0 * 128, count, off, len, p.lam, p.shift, etid);
+            if (QPC > 0 && y.count * y.len == AS_SLAB) {
+              constexpr int N = QPC > 0 ? QPC : 1;
+              const float* f = v + y.r0 * 128 + (y.off >> p.shift);
+              uint4 *a0 = reinterpret_cast<uint4*>(slab + at0), *a1 = reinterpret_cast<uint4*>(slab + at1);
+              const uint4 y0 = *a0, y1 = *a1;
+              float q0[N], q1[N];
+              as_products<N>(f + f0, q0);
+              as_products<N>(f + f1, q1);
+              *a0 = as_add<F32, N>(y0, q0);
+              *a1 = as_add<F32, N>(y1, q1);
+            } else {
+              as_sums<F32, QPC>(slab, y.pitch, v + y.r0 * 128, y.count, y.off, y.len, p.lam, p.shift, etid);
+            }
           }
           fence_async_proxy();                                        // the stores read what was written here
-          mbar_arrive(summed(s));
+          __syncwarp();
+          if (lane == 0) mbar_arrive(summed(s));
           if (++s == p.slabs) { s = 0; ph ^= 1u; }
         }
       }
@@ -863,7 +912,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
     for (int s = 0; s < AR_STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI); }
+    for (int b = 0; b < 2; ++b) { mbar_init(accfull(b), 1); mbar_init(accempty(b), AG_EPI / 32); }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
@@ -993,7 +1042,8 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
           ag_gather(d + 128 + c, v + c);
         }
         tc_fence_before();
-        mbar_arrive(accempty(b));
+        __syncwarp();
+        if (lane == 0) mbar_arrive(accempty(b));
         ++done;
       }
       if (!ok) break;
@@ -1136,36 +1186,61 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   return ag_launch(adapters_shrink_kernel, ready, maps, p, AG_THREADS, p.stages * stage + AG_BARS + table, most_tiles(c, p.tn) * p.m_tiles, st);
 }
 
-// shared memory of the spread kernel without slabs; 0: u does not fit with at least two of them
+// shared memory of the spread kernel without slabs
 size_t as_fixed(int n, int np, int kb, int tn) {
-  const size_t need = (size_t)np * kb * tn * 128 + AS_RING * AG_TILE + (size_t)tn * 512 + AG_BARS + ag_table_bytes(n);
-  return need + 2 * AS_SLAB <= (size_t)AG_SMEM ? need : 0;
+  return (size_t)np * kb * tn * 128 + AS_RING * AG_TILE + (size_t)tn * 512 + AG_BARS + ag_table_bytes(n);
 }
+// rows of a tile: as many as leave room for five slabs, or for two where even the least do not; 0: none
 int as_rows(const BankView& k, int np) {
-  int tn = 64;
-  while (tn > 16 && !as_fixed(k.n, np, (k.r + 63) / 64, tn)) tn /= 2;
-  return as_fixed(k.n, np, (k.r + 63) / 64, tn) ? tn : 0;
+  for (int slabs : {5, 2})
+    for (int tn = 64; tn >= 16; tn /= 2)
+      if (as_fixed(k.n, np, (k.r + 63) / 64, tn) + (size_t)slabs * AS_SLAB <= (size_t)AG_SMEM) return tn;
+  return 0;
+}
+// Y as [rows][pieces][elements of a piece]: a box is all pieces of 128 q by the rows of a slab.  The number of pieces, or 0 where
+// such boxes cannot be had: rows that are no whole pieces, slabs that are less than a row.
+int as_y_map(CUtensorMap* tm, const RowsView& y, int64_t T, int d, int lam, int* rc) {
+  const int size = y.dtype == QBLORA_F32 ? 4 : 2, q = 128 * lam, whole = q * size, inner = q % 256 ? 128 : 256, n = q / inner;
+  *rc = QBLORA_OK;
+  if (whole > AS_SLAB || q % inner || d % inner || n > 256) return 0;
+  *rc = make_tensor_map_rows(tm, y.dtype == QBLORA_F32, y.data, (uint64_t)inner, (uint64_t)(d / inner), (uint64_t)T, (uint64_t)inner * size,
+                             (uint64_t)y.stride * size, (uint32_t)n, (uint32_t)(AS_SLAB / whole));
+  return n;
 }
 // Y += s repeat(u B), or dX += repeat(du A^T) / lam
 int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& in, const __nv_bfloat16* W, int M, bool kmajor, const RowsView& y,
               int lam, bool forward, cudaStream_t st) {
-  static std::atomic<bool> ready[64];
-  AgMaps3 maps{};
+  static std::atomic<bool> ready[9][64];
+  AsMaps maps{};
   AgSpread p{};
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.np = in.np; p.kb = (c.k.r + 63) / 64; p.tn = as_rows(c.k, in.np);
   const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
-  p.slabs = (int)std::min<size_t>(6, (AG_SMEM - fixed) / AS_SLAB);
+  p.slabs = (int)std::min<size_t>(8, (AG_SMEM - fixed) / AS_SLAB);
   p.m_tiles = (M + 127) / 128; p.M = M; p.w_kmajor = kmajor; p.scaled = forward; p.y = y; p.lam = lam;
   p.factor = forward ? 1.0f : 1.0f / (float)lam;
   const int w = lam * (y.dtype == QBLORA_F32 ? 4 : 2);
   p.shift = -1;
   for (int i = 0; i < 31; ++i)
     if (w == 1 << i) p.shift = i;
-  QB_TRY(parts_map(&maps.rows, in, l.rows, p.tn));
-  QB_TRY(parts_map(&maps.rows16, in, l.rows, 16));
-  QB_TRY(kmajor ? bank_map(&maps.w, W, c.k.r, M, c.k.n, 128) : bank_map(&maps.w, W, M, c.k.r, c.k.n, 64));
-  return ag_launch(adapters_spread_kernel, ready, maps, p, AS_THREADS, fixed + (size_t)p.slabs * AS_SLAB, most_tiles(c, p.tn) * p.m_tiles, st);
+  int rc = QBLORA_OK;
+  p.boxes = as_y_map(&maps.y, y, c.T, M * lam, lam, &rc);
+  QB_TRY(rc);
+  QB_TRY(parts_map(&maps.in.rows, in, l.rows, p.tn));
+  QB_TRY(parts_map(&maps.in.rows16, in, l.rows, 16));
+  QB_TRY(kmajor ? bank_map(&maps.in.w, W, c.k.r, M, c.k.n, 128) : bank_map(&maps.in.w, W, M, c.k.r, c.k.n, 64));
+  auto launch = [&](auto kernel, int form) {
+    return ag_launch(kernel, ready[form], maps, p, AS_THREADS, fixed + (size_t)p.slabs * AS_SLAB, most_tiles(c, p.tn) * p.m_tiles, st);
+  };
+  if (y.dtype == QBLORA_F32) {
+    if (p.shift < 0) return launch(adapters_spread_kernel<true, 0>, 0);
+    if (p.shift >= 4) return launch(adapters_spread_kernel<true, 1>, 1);
+    return p.shift == 3 ? launch(adapters_spread_kernel<true, 2>, 2) : launch(adapters_spread_kernel<true, 4>, 3);
+  }
+  if (p.shift < 0) return launch(adapters_spread_kernel<false, 0>, 4);
+  if (p.shift >= 4) return launch(adapters_spread_kernel<false, 1>, 5);
+  if (p.shift == 3) return launch(adapters_spread_kernel<false, 2>, 6);
+  return p.shift == 2 ? launch(adapters_spread_kernel<false, 4>, 7) : launch(adapters_spread_kernel<false, 8>, 8);
 }
 int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st) {
   static std::atomic<bool> ready[64];

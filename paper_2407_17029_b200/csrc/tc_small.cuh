@@ -52,4 +52,8 @@ int make_tensor_map_2d_typed(void* tm, int elem, const void* ptr, uint64_t inner
 // dimension i + 1.
 int make_tensor_map_nd(void* tm, int rank, const void* ptr, const uint64_t* dims, const uint64_t* pitch_bytes, const uint32_t* box);
 
+// bf16 or fp32 rows as [rows][pieces][inner], no swizzle: a box is `box_pieces` whole pieces of `box_rows` rows.
+int make_tensor_map_rows(void* tm, bool f32, const void* ptr, uint64_t inner, uint64_t pieces, uint64_t rows, uint64_t piece_bytes, uint64_t row_bytes,
+                         uint32_t box_pieces, uint32_t box_rows);
+
 }  // namespace qb

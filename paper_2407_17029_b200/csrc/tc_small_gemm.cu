@@ -284,6 +284,18 @@ int make_tensor_map_nd(void* tm, int rank, const void* ptr, const uint64_t* dims
   return r == CUDA_SUCCESS ? QBLORA_OK : QBLORA_ERR_CUDA;
 }
 
+int make_tensor_map_rows(void* tm, bool f32, const void* ptr, uint64_t inner, uint64_t pieces, uint64_t rows, uint64_t piece_bytes, uint64_t row_bytes,
+                         uint32_t box_pieces, uint32_t box_rows) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return QBLORA_ERR_CUDA;
+  const cuuint64_t dims[3] = {inner, pieces, rows}, strides[2] = {piece_bytes, row_bytes};
+  const cuuint32_t box[3] = {(cuuint32_t)inner, box_pieces, box_rows}, estr[3] = {1, 1, 1};
+  const CUresult r = fn(static_cast<CUtensorMap*>(tm), f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3,
+                        const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                        CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? QBLORA_OK : QBLORA_ERR_CUDA;
+}
+
 int small_gemm_splits(int M, int N, int K) {
   const int n64 = (N + 63) / 64 * 64;
   const int bn = n64 < 256 ? n64 : 256;
