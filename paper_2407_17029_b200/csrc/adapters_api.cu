@@ -35,6 +35,10 @@ bool force_general() {
   return e && e[0] == '1';
 }
 
+// The host does not know how many rows an adapter has.  Calls of at most kFewTokens rows are all adapters_rows.cu's; larger ones have
+// adapters of at most kFewRows rows there and the others in tc_adapters.cu.
+constexpr int kFewTokens = 512, kFewRows = 32;
+
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
@@ -84,7 +88,17 @@ int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, co
   if (rc) return rc;
   if (!rows_ok(X, x_stride, bank->d_in, QBLORA_BF16, &c.X) || !rows_ok(Y, y_stride, bank->d_out, y_dtype, &c.Y) || X == Y) return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adapters_workspace_bytes(bank, tokens, 0)) return QBLORA_ERR_WORKSPACE;
-  if (!force_general() && tc_adapters_supported(c)) return tc_adapters_fwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
+  if (!force_general() && tc_adapters_supported(c)) {
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int above = 0;
+    if (rows_adapters_supported(c)) {
+      const bool all = tokens <= kFewTokens;
+      const int done = rows_adapters_fwd(c, all ? 0x7fffffff : kFewRows, true, static_cast<int*>(ws), st);
+      if (done || all) return done;
+      above = kFewRows;
+    }
+    return tc_adapters_fwd(c, static_cast<char*>(ws), above, st);
+  }
   return simt_adapters_fwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
 }
 

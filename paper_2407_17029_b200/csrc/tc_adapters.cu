@@ -22,7 +22,7 @@
 #include <algorithm>
 #include <atomic>
 
-#include "adapters.cuh"
+#include "adapter_groups.cuh"
 #include "tc_ptx.cuh"
 #include "tc_small.cuh"
 
@@ -36,70 +36,6 @@ constexpr int AG_POOL_THREADS = 256;
 constexpr int AG_SMEM = 232448 - 1024 - 1024;        // of a CTA, without alignment and static variables
 constexpr int AG_BARS = 512;                        // of those, barriers
 
-// ---- adapters' rows: where they lie in the workspace, and their tiles ------------------------------------------------------------
-size_t ag_table_bytes(int n) { return (size_t)2 * (n + 1) * 4; }
-struct AgGroups {
-  const uint32_t* pad;      // [n + 1] first row of each adapter in the workspace, multiples of 16
-  const uint32_t* tile;     // [n + 1] tiles in front of it
-  int kept;                 // adapters whose rows lie in the workspace: all, for a plan whose offsets rise
-};
-__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }   // both below 2^31
-
-// by the whole CTA; s: 2 (n + 1) words of shared memory
-// tn: rows of a tile
-template <int NT>
-__device__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_there, int tn) {
-  __shared__ uint32_t s_part[2][NT / 32];
-  __shared__ int s_kept;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = c.k.n;
-  uint32_t *pad = s, *tile = s + n + 1;
-  const int per = (n + NT - 1) / NT, lo = min(tid * per, n), hi = min(lo + per, n);
-  uint32_t mine = 0, tiles = 0;
-  for (int a = lo; a < hi; ++a) {
-    const uint32_t rows = (uint32_t)max(plan_start(c, a + 1) - plan_start(c, a), 0);
-    const uint32_t p = (min(rows, 0x7ffffff0u) + 15u) & ~15u, t = (rows + tn - 1) / tn;
-    pad[a] = p;
-    tile[a] = t;
-    mine = sat_add(mine, p);
-    tiles = sat_add(tiles, t);
-  }
-  uint32_t x = mine, y = tiles;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const uint32_t px = __shfl_up_sync(0xffffffffu, x, d), py = __shfl_up_sync(0xffffffffu, y, d);
-    if (lane >= d) { x = sat_add(x, px); y = sat_add(y, py); }
-  }
-  // exclusive within the warp (the saturated case only has to stay large)
-  uint32_t ex = __shfl_up_sync(0xffffffffu, x, 1), ey = __shfl_up_sync(0xffffffffu, y, 1);
-  if (lane == 0) ex = ey = 0;
-  if (lane == 31) { s_part[0][warp] = x; s_part[1][warp] = y; }
-  if (tid == 0) s_kept = n;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < NT / 32; ++w)
-    if (w < warp) { ex = sat_add(ex, s_part[0][w]); ey = sat_add(ey, s_part[1][w]); }
-  for (int a = lo; a < hi; ++a) {
-    const uint32_t p = pad[a], t = tile[a];
-    pad[a] = ex;
-    tile[a] = ey;
-    ex = sat_add(ex, p);
-    ey = sat_add(ey, t);
-    if (ex > rows_there) atomicMin(&s_kept, a);
-  }
-  if (lo < hi && hi == n) { pad[n] = ex; tile[n] = ey; }
-  __syncthreads();
-  return {pad, tile, s_kept};
-}
-// the last a in [0, n) with v[a] <= x; v[0] <= x < v[n]
-__device__ __forceinline__ int ag_find(const uint32_t* v, int n, uint32_t x) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (v[mid] <= x) lo = mid; else hi = mid;
-  }
-  return lo;
-}
-
 // ---- pool ---------------------------------------------------------------------------------------------------------------------
 // A matrix of rows in the workspace in np parts: element (part, row, i) at part * stride + row * ld + i.
 struct Parts { __nv_bfloat16* p; int np, width, ld; int64_t stride; };
@@ -110,10 +46,7 @@ struct AgPool {
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
-struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; };
-
-__device__ __forceinline__ float ag_low(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float ag_high(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources, clear; uint32_t rows_there, above; int* status; };
 
 // N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
 template <int N>
@@ -203,8 +136,8 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row
 __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __grid_constant__ AgPoolParams p) {
   extern __shared__ uint32_t ag_smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
-  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128);
+  if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
+  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128, p.above, 0x7fffffffu);
   const int lane = threadIdx.x & 31, warps = AG_POOL_THREADS / 32;
   const uint32_t rows = g.pad[g.kept];
   for (int64_t i = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); i < (int64_t)rows * p.sources; i += (int64_t)gridDim.x * warps) {
@@ -217,12 +150,13 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
     const bool real = row >= 0 && row < p.c.T;
     ag_pool_row(s, real ? static_cast<const __nv_bfloat16*>(s.x.data) + row * s.x.stride : nullptr, at, lane);
   }
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // no grid ends before the one in front of it
 }
 
 // ---- shrink -------------------------------------------------------------------------------------------------------------------
 struct AgShrink {
   AdaptersCall c;
-  uint32_t rows_there;
+  uint32_t rows_there, above;           // of the workspace; adapters of no more rows than this are another kernel's
   int tn, stages, np;                   // rows of a tile; of the ring; parts of the input
   int segment;                          // 64-wide blocks of the contraction that one accumulator takes
   int m_tiles, K, w_kmajor, scaled;     // tiles of 128 ranks; contraction; the weight's contiguous dimension is the contraction's;
@@ -342,7 +276,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn, p.above, 0x7fffffffu);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -479,7 +413,7 @@ constexpr int AS_EPI = 512, AS_THREADS = 128 + AS_EPI;     // loads, MMAs, slabs
 constexpr int AS_SLAB = 16384, AS_RING = 3;
 struct AgSpread {
   AdaptersCall c;
-  uint32_t rows_there;
+  uint32_t rows_there, above;           // of the workspace; adapters of no more rows than this are another kernel's
   int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
   int slabs;
   int m_tiles, M, w_kmajor, scaled;
@@ -627,7 +561,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
+  const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn, p.above, 0x7fffffffu);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -892,7 +826,7 @@ __device__ __forceinline__ void ar_issue(uint32_t d, uint64_t a, uint64_t b, uin
 struct AgGradSide { int parts_a, parts_b, M, N; float* out; };        // dA: x' (P) by du (r); dB: u (r) by dv (Q)
 struct AgGrad {
   AdaptersCall c;
-  uint32_t rows_there;
+  uint32_t rows_there, above;
   AgGradSide side[2];                   // out == nullptr: not wanted
   int* status;
   long long wait_limit;
@@ -919,7 +853,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, 128);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, 128, p.above, 0x7fffffffu);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1071,7 +1005,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------
-struct Layout { Parts x, dv, u, du; size_t bytes; uint32_t rows; };
+struct Layout { Parts x, dv, u, du; size_t bytes; uint32_t rows, above; };
 
 // parts: of numbers that are no bf16 numbers
 Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* ws) {
@@ -1136,14 +1070,24 @@ int ag_launch(void (*kernel)(Maps, Params), std::atomic<bool>* ready, const Maps
   return QBLORA_OK;
 }
 
-int ag_launch_pool(const AgPoolParams& p, int64_t rows, cudaStream_t st) {
+// beside: the kernel in front on the stream is adapters_rows.cu's, of other rows: this one need not wait for its end before it
+// begins, only before it ends itself.
+int ag_launch_pool(const AgPoolParams& p, int64_t rows, bool beside, cudaStream_t st) {
   int sms = 0;
   const int rc = ag_sms(&sms);
   if (rc) return rc;
   const int64_t want = (rows * p.sources + AG_POOL_THREADS / 32 - 1) / (AG_POOL_THREADS / 32);
-  adapters_pool_kernel<<<(unsigned)std::min<int64_t>(want, 8LL * sms), AG_POOL_THREADS, ag_table_bytes(p.c.k.n), st>>>(p);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(want, 8LL * sms));
+  cfg.blockDim = dim3(AG_POOL_THREADS);
+  cfg.dynamicSmemBytes = ag_table_bytes(p.c.k.n);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = beside ? 1 : 0;
+  QB_CUDA(cudaLaunchKernelEx(&cfg, adapters_pool_kernel, p));
   count_launch();
-  QB_CUDA(cudaGetLastError());
   return QBLORA_OK;
 }
 
@@ -1171,7 +1115,7 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   static std::atomic<bool> ready[64];
   AgMaps3 maps{};
   AgShrink p{};
-  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
   p.np = in.np; p.m_tiles = (c.k.r + 127) / 128; p.K = in.width; p.w_kmajor = kmajor; p.scaled = scaled; p.out = out;
   // smaller tiles where large ones would leave SMs without any
   p.tn = 128;
@@ -1213,7 +1157,7 @@ int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   static std::atomic<bool> ready[9][64];
   AsMaps maps{};
   AgSpread p{};
-  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
   p.np = in.np; p.kb = (c.k.r + 63) / 64; p.tn = as_rows(c.k, in.np);
   const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
   p.slabs = (int)std::min<size_t>(8, (AG_SMEM - fixed) / AS_SLAB);
@@ -1246,7 +1190,7 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   static std::atomic<bool> ready[64];
   AgGradMaps maps{};
   AgGrad p{};
-  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
   p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
   p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
   QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 32));
@@ -1276,13 +1220,14 @@ bool tc_adapters_supported(const AdaptersCall& c) {
   return aligned16(c.dA) && aligned16(c.dB);
 }
 
-int tc_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
-  const Layout l = ag_layout(c.k, c.T, false, forward_parts(c.Y.dtype), ws);
+int tc_adapters_fwd(const AdaptersCall& c, char* ws, int above, cudaStream_t st) {
+  Layout l = ag_layout(c.k, c.T, false, forward_parts(c.Y.dtype), ws);
+  l.above = (uint32_t)above;
   int* status = reinterpret_cast<int*>(ws);
   AgPoolParams pool{};
-  pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = 1;
+  pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = 1; pool.clear = above == 0;
   pool.src[0] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
-  QB_TRY(ag_launch_pool(pool, l.rows, st));
+  QB_TRY(ag_launch_pool(pool, l.rows, above > 0, st));
   QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
   return ag_spread(c, l, status, l.u, c.k.B, c.k.Q, false, c.Y, c.k.l2, true, st);
 }
@@ -1292,10 +1237,10 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   int* status = reinterpret_cast<int*>(ws);
   const bool grads = c.dA || c.dB;
   AgPoolParams pool{};
-  pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = grads ? 2 : 1;
+  pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = grads ? 2 : 1; pool.clear = 1;
   pool.src[0] = ag_source(c.Y, c.k.d_out, c.k.l2, false, l.dv);
   if (grads) pool.src[1] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
-  QB_TRY(ag_launch_pool(pool, l.rows, st));
+  QB_TRY(ag_launch_pool(pool, l.rows, false, st));
   if (c.dX.data || c.dA) QB_TRY(ag_shrink(c, l, status, l.dv, l.du, c.k.B, true, true, st));
   if (c.dB) QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
   if (c.dX.data) QB_TRY(ag_spread(c, l, status, l.du, c.k.A, c.k.P, true, c.dX, c.k.l1, false, st));

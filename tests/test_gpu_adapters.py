@@ -57,7 +57,8 @@ SIZES = [(256, 512, 64, 8, 32), (512, 256, 4, 4, 64), (128, 128, 1, 1, 16), (102
          (60, 36, 4, 4, 7), (256, 260, 4, 4, 16), (130, 34, 2, 2, 3), (64, 64, 8, 8, 300)]       # the last four: general path
 LENGTHS = {"one": ([1], [0], 1), "none": ([3, 2], [-1, -1], 2), "decode": ([1] * 40, None, 7), "empty": ([0, 1, 0, 5, 0], [1, 2, 0, 2, 3], 4),
            "tiles": ([16, 17, 15, 32, 33, 1, 64, 65], [0, 1, 2, 3, 4, 5, 6, 7], 9), "wide": ([127, 128, 129, 300, 2], [3, 0, 2, 1, 2], 4),
-           "one adapter": ([200, 1, 77], [1, 1, 1], 2), "mixed": ([1] * 20 + [150] + [1] * 9, None, 5)}
+           "one adapter": ([200, 1, 77], [1, 1, 1], 2), "mixed": ([1] * 20 + [150] + [1] * 9, None, 5),
+           "long": ([33, 1, 47, 48, 49, 9, 63, 64, 65, 300, 32], [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 1], 11)}
 
 
 CASES = [(size, lengths, dtype, general) for size in SIZES for lengths in LENGTHS for dtype in (torch.float32, torch.bfloat16)
