@@ -195,17 +195,22 @@ __device__ __forceinline__ void aw_load_codes(const void* a, long long base, int
       if (aw_elem(lane, i) < left) w[i >> 2] |= (uint32_t)c[base + aw_elem(lane, i)] << (8 * (i & 3));
   }
 }
-// The neighbour of y by chance: with y 2^-120, e4m3's exponent is at the lower end of fp32's, where its subnormal numbers are subnormal
-// too, and 20 bits of the mantissa are to go.  What the random bits, added to the upper 16 of them, carry out decides.  `shift`: which 16
-// of the random bits.  Codes in the top byte of z.  The block's largest y may be three units of fp32 above 448 (its factor and the product
-// are rounded): 3 + 16 * 65535 still carries nothing out.
-__device__ __forceinline__ uint32_t aw_round(float y, uint32_t rnd, int shift) {
-  const uint32_t bits16 = shift ? rnd >> 16 : rnd & 0xffffu;
-  return (__float_as_uint(y) + (bits16 << 4)) << 4;
+// The neighbour of |y| by chance: with y 2^-120, e4m3's exponent is at the lower end of fp32's, where its subnormal numbers are subnormal
+// too, and 20 bits of the mantissa are to go.  What the random bits, added to the upper 16 of them, carry out decides.  The code comes
+// in the top byte of the result (y's sign is shifted out).  RND: which 16 of the random bits, as a byte permutation that puts them into
+// the middle bytes.  The block's largest y may be three units of fp32 above 448 (its factor and the product are rounded): 3 + 16 * 65535
+// still carries nothing out.
+template <uint32_t RND>
+__device__ __forceinline__ uint32_t aw_round(float y, uint32_t rnd) {
+  uint32_t low;          // (as assembly: the compiler folds this permutation and the ones that gather the codes into zeros)
+  asm("prmt.b32 %0, %1, 0, %2;" : "=r"(low) : "r"(rnd), "n"(RND));
+  return (__float_as_uint(y) << 4) + low;
 }
-template <bool FULL>
+constexpr uint32_t AW_LOW = 0x4104, AW_HIGH = 0x4324;
+// SIGNED: else no x is below zero.
+template <bool FULL, uint32_t RND, bool SIGNED>
 __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long base, int left, int lane, const float (&x)[8],
-                                               const uint32_t (&rnd)[8], int shift) {
+                                               const uint32_t (&rnd)[8]) {
   float most = fabsf(x[0]);
 #pragma unroll
   for (int i = 1; i < 8; ++i) most = aw_max(most, fabsf(x[i]));
@@ -222,18 +227,26 @@ __device__ __forceinline__ void aw_store_codes(void* a, float* scale, long long 
   }
   float top = __uint_as_float(all);
   if (top < 0x1p-118f) top = 0.f;
-  const float inv = top > 0.f ? __fmul_rn(__frcp_rn(top), 448.0f) * 0x1p-120f : 0.f;
+  const float inv = top > 0.f ? __fmul_rn(__frcp_rn(top), 448.0f) : 0.f;
+  const unsigned long long inv2 = aw_two(inv, inv), down2 = aw_two(0x1p-120f, 0x1p-120f);
   uint32_t w[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t z[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[e] = aw_round(fabsf(x[4 * h + e] * inv), rnd[4 * h + e], shift);
-    const uint32_t code = __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
-    const float* y = x + 4 * h;
-    const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0073),
-                                      __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0073), 0x5410);
-    w[h] = (code & 0x7f7f7f7fu) | (sign & 0x80808080u);
+    for (int e = 0; e < 4; e += 2) {
+      float y0, y1;
+      aw_split(aw_mul2(aw_mul2(aw_two(x[4 * h + e], x[4 * h + e + 1]), inv2), down2), y0, y1);
+      z[e] = aw_round<RND>(y0, rnd[4 * h + e]);
+      z[e + 1] = aw_round<RND>(y1, rnd[4 * h + e + 1]);
+    }
+    w[h] = __byte_perm(__byte_perm(z[0], z[1], 0x0073), __byte_perm(z[2], z[3], 0x0073), 0x5410);
+    if (SIGNED) {
+      const float* y = x + 4 * h;
+      const uint32_t sign = __byte_perm(__byte_perm(__float_as_uint(y[0]), __float_as_uint(y[1]), 0x0073),
+                                        __byte_perm(__float_as_uint(y[2]), __float_as_uint(y[3]), 0x0073), 0x5410);
+      w[h] = (w[h] & 0x7f7f7f7fu) | (sign & 0x80808080u);
+    }
   }
   if (odd) {
 #pragma unroll
@@ -302,15 +315,21 @@ __device__ __forceinline__ void aw_update(const AwStep& s, const AwNow& now, con
   }
   const float rate = now.lr * t.lr_mult;
   float root[8];
-  const unsigned long long up1 = aw_two(now.up1, now.up1), up2 = aw_two(now.up2, now.up2), eps = aw_two(s.eps, s.eps), decay = aw_two(t.decay, t.decay), back = aw_two(-rate, -rate);
+  const unsigned long long factor = aw_two(now.factor, now.factor), b1 = aw_two(s.b1, s.b1), b2 = aw_two(s.b2, s.b2), c1 = aw_two(s.c1, s.c1),
+                           c2 = aw_two(s.c2, s.c2), up1 = aw_two(now.up1, now.up1), up2 = aw_two(now.up2, now.up2), eps = aw_two(s.eps, s.eps), decay = aw_two(t.decay, t.decay), back = aw_two(-rate, -rate);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
-#pragma unroll
-    for (int e = i; e < i + 2; ++e) {
-      const float x = __fmul_rn(g[e], now.factor);
-      m[e] = __fadd_rn(__fmul_rn(s.b1, m[e]), __fmul_rn(s.c1, x));
-      v[e] = __fadd_rn(__fmul_rn(s.b2, v[e]), __fmul_rn(s.c2, __fmul_rn(x, x)));
-    }
+    // (packed products, single sums: a packed sum of packed products comes out as one operation of one rounding)
+    const unsigned long long x = aw_mul2(aw_two(g[i], g[i + 1]), factor);
+    float m0, m1, x0, x1, v0, v1, q0, q1;
+    aw_split(aw_mul2(b1, aw_two(m[i], m[i + 1])), m0, m1);
+    aw_split(aw_mul2(c1, x), x0, x1);
+    aw_split(aw_mul2(b2, aw_two(v[i], v[i + 1])), v0, v1);
+    aw_split(aw_mul2(c2, aw_mul2(x, x)), q0, q1);
+    m[i] = __fadd_rn(m0, x0);
+    m[i + 1] = __fadd_rn(m1, x1);
+    v[i] = __fadd_rn(v0, q0);
+    v[i + 1] = __fadd_rn(v1, q1);
     const unsigned long long mm = aw_two(m[i], m[i + 1]);
     // held in 8 bits, the root is a result itself; in 32 it only divides
     root[i] = bits8 ? __fsqrt_rn(v[i]) : aw_sqrt(v[i]);
@@ -341,8 +360,8 @@ __device__ __forceinline__ void aw_update(const AwStep& s, const AwNow& now, con
     const uint32_t e0 = (b * AW_BLOCK + 4 * lane) * 0x9E3779B1u + now.key;
 #pragma unroll
     for (int i = 0; i < 8; ++i) rnd[i] = aw_mix(e0 + (uint32_t)((i >> 2) * 128 + (i & 3)) * 0x9E3779B1u);
-    aw_store_codes<FULL>(t.m, t.m_scale + mine, base, left, lane, m, rnd, 0);
-    aw_store_codes<FULL>(t.v, t.v_scale + mine, base, left, lane, root, rnd, 16);
+    aw_store_codes<FULL, AW_LOW, true>(t.m, t.m_scale + mine, base, left, lane, m, rnd);
+    aw_store_codes<FULL, AW_HIGH, false>(t.v, t.v_scale + mine, base, left, lane, root, rnd);
   } else {
     aw_store_f32<FULL>(static_cast<float*>(t.m), base, left, lane, m);
     aw_store_f32<FULL>(static_cast<float*>(t.v), base, left, lane, v);
@@ -369,8 +388,10 @@ __device__ __forceinline__ void aw_each(const AwView& w, uint32_t blocks, uint32
 __device__ __forceinline__ bool aw_full(const AwTensor& t, uint32_t b) {
   return t.wide && (long long)(b - t.first + 1) * AW_BLOCK <= t.n;
 }
-// Neighbouring blocks per warp and turn: four where every warp has many turns, else one, so that all SMs have work.
-__device__ __forceinline__ uint32_t aw_run(uint32_t blocks) { return blocks / (gridDim.x * AW_WARPS) >= 16 ? 4u : 1u; }
+// Neighbouring blocks per warp and turn: `most` where every warp has some turns of them, else fewer, so that all SMs have work.
+__device__ __forceinline__ uint32_t aw_run(uint32_t blocks, uint32_t most) {
+  return min(most, max(1u, blocks / (gridDim.x * AW_WARPS * 4)));
+}
 
 // BITS: of the states of all tensors; 0: they are mixed
 template <int BITS>
@@ -389,7 +410,7 @@ __global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_const
     now.up2 = sqrtf(__fdiv_rn(1.0f, -expm1f((float)(t * s.log_b2))));
     now.lr = *s.lr;
     now.key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
-    aw_each(w, blocks, aw_run(blocks), [&](const AwTensor& t, uint32_t b, uint32_t n) {
+    aw_each(w, blocks, aw_run(blocks, 4), [&](const AwTensor& t, uint32_t b, uint32_t n) {
       uint32_t i = 0;
       if (BITS == 8) {                         // few bytes to a block: the loads of two on their way at once
         for (; i + 2 <= n && aw_full(t, b + i + 1); i += 2) {
@@ -432,11 +453,12 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_con
   const uint32_t blocks = w.ctl->blocks;
   double sum = 0.0;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");    // the step waits for this grid's end before it reads anything
+  double sums[4] = {0.0, 0.0, 0.0, 0.0};         // (chains of their own)
   auto add = [&](const float (&g)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum = fma((double)g[i], (double)g[i], sum);
+    for (int i = 0; i < 8; ++i) sums[i & 3] = fma((double)g[i], (double)g[i], sums[i & 3]);
   };
-  aw_each(w, blocks, aw_run(blocks), [&](const AwTensor& t, uint32_t b, uint32_t n) {
+  aw_each(w, blocks, aw_run(blocks, 16), [&](const AwTensor& t, uint32_t b, uint32_t n) {
     const long long base = (long long)(b - t.first) * AW_BLOCK;
     uint32_t i = 0;
     for (; i + 4 <= n && aw_full(t, b + i + 3); i += 4) {
@@ -454,6 +476,7 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_norm_kernel(const __grid_con
       add(g);
     }
   });
+  sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
   auto join = [&](double x) {                  // over the CTA; the result in thread 0
 #pragma unroll
     for (int d = 16; d; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);

@@ -154,18 +154,23 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
 }
 
 // ---- shrink -------------------------------------------------------------------------------------------------------------------
+struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the rows' parts in boxes of tn rows and of 16
+// u = x' A, du = s dv B^T, or both side by side.
+struct AgShrinkSide {
+  int np, K, w_kmajor, scaled;          // parts of the input; contraction; the weight's contiguous dimension is the contraction's; times
+  Parts out;                            // the adapter's factor
+};
 struct AgShrink {
   AdaptersCall c;
   uint32_t rows_there, above;           // of the workspace; adapters of no more rows than this are another kernel's
-  int tn, stages, np;                   // rows of a tile; of the ring; parts of the input
+  int tn, stages, np;                   // rows of a tile; of the ring; most parts
   int segment;                          // 64-wide blocks of the contraction that one accumulator takes
-  int m_tiles, K, w_kmajor, scaled;     // tiles of 128 ranks; contraction; the weight's contiguous dimension is the contraction's;
-                                        // times the adapter's factor
-  Parts out;
+  int m_tiles, sides;                   // tiles of 128 ranks
+  AgShrinkSide side[2];
   int* status;
   long long wait_limit;
 };
-struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the rows' parts in boxes of tn rows and of 16
+struct AgShrinkMaps { AgMaps3 side[2]; };
 
 // The warps that load and that issue MMAs walk their loops whole, on values that are the same in every lane, and one elected lane
 // issues: the operands then lie in uniform registers (12 cycles an MMA; from one lane's private loop 60).
@@ -255,7 +260,7 @@ __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
   for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
 }
 
-__global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __grid_constant__ AgMaps3 maps, const __grid_constant__ AgShrink p) {
+__global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __grid_constant__ AgShrinkMaps maps, const __grid_constant__ AgShrink p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
   const uint32_t stage_bytes = AG_TILE + (uint32_t)p.np * p.tn * 128, bars = base + p.stages * stage_bytes;
@@ -281,18 +286,21 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot_g;
-  const long long units = (long long)ag_uni((int)g.tile[g.kept]) * p.m_tiles;
-  const int steps = (p.K + 15) / 16;
+  const uint32_t tiles = (uint32_t)ag_uni((int)g.tile[g.kept]);
+  const long long per_side = (long long)tiles * p.m_tiles, units = per_side * p.sides;
   asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
-  // unit u: tile u / m_tiles, ranks from 128 (u % m_tiles) on; an adapter of a lower rank has none there
-  auto unit = [&](long long u, AgRows& t, int& m0) {
+  // unit u: a side, tile u / m_tiles of it, ranks from 128 (u % m_tiles) on; an adapter of a lower rank has none there
+  AgRows t;
+  int m0, side, steps;
+  auto unit = [&](long long u) {
+    side = u >= per_side ? 1 : 0;
+    if (side) u -= per_side;
     const uint32_t tile = (uint32_t)(u / p.m_tiles);
     m0 = (int)(u - (long long)tile * p.m_tiles) * 128;
     t = ag_rows(p.c, g, tile, p.tn);
+    steps = (p.side[side].K + 15) / 16;
     return m0 < ag_uni(bank_rank(p.c.k, t.a));
   };
-  AgRows t;
-  int m0;
   if (warp == 0) {
     const uint32_t ring = (uint32_t)ag_uni((int)base);
     const bool leader = ag_elect();
@@ -300,15 +308,16 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     int s = 0;
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-      if (!unit(u, t, m0)) continue;
+      if (!unit(u)) continue;
+      const int np = p.side[side].np, kmajor = p.side[side].w_kmajor;
       for (int k = 0; k < steps; k += 4, ++it) {
         ok = ag_wait(empty(s), ph ^ 1u, p.status, p.wait_limit);
         if (!ok) break;
         const uint32_t w = ring + s * stage_bytes;
         if (leader) {
-          mbar_arrive_expect_tx(full(s), AG_TILE + (uint32_t)p.np * t.n16 * 128);
-          ag_load_weights(maps, w, full(s), p.w_kmajor, k * 16, m0, t.a);
-          for (int i = 0; i < p.np; ++i) ag_load_rows(maps, w + AG_TILE + i * p.tn * 128, full(s), k * 16, t, p.tn, i);
+          mbar_arrive_expect_tx(full(s), AG_TILE + (uint32_t)np * t.n16 * 128);
+          ag_load_weights(maps.side[side], w, full(s), kmajor, k * 16, m0, t.a);
+          for (int i = 0; i < np; ++i) ag_load_rows(maps.side[side], w + AG_TILE + i * p.tn * 128, full(s), k * 16, t, p.tn, i);
         }
         __syncwarp();
         if (++s == p.stages) { s = 0; ph ^= 1u; }
@@ -325,8 +334,9 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     int s = 0;
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-      if (!unit(u, t, m0)) continue;
-      const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
+      if (!unit(u)) continue;
+      const int np = p.side[side].np, kmajor = p.side[side].w_kmajor;
+      const uint32_t idesc = ag_idesc(!kmajor, false, t.n16);
       int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
       for (int k = 0; k < steps; k += 4) {
         const bool fresh = left == 0;
@@ -344,8 +354,8 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         if (leader) {
           const uint64_t rows = ag_desc(w + AG_TILE, false), part = (uint64_t)(p.tn * 128) >> 4;
           const int n = min(4, steps - k);
-          if (p.w_kmajor) ag_issue_parts<true>(p.np, d, d + 128, ag_desc(w, false), rows, part, idesc, n, fresh);
-          else ag_issue_parts<false>(p.np, d, d + 128, ag_desc(w, true), rows, part, idesc, n, fresh);
+          if (kmajor) ag_issue_parts<true>(np, d, d + 128, ag_desc(w, false), rows, part, idesc, n, fresh);
+          else ag_issue_parts<false>(np, d, d + 128, ag_desc(w, true), rows, part, idesc, n, fresh);
           tc_commit(empty(s));
           if (last) tc_commit(accfull(b));
         }
@@ -359,7 +369,8 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     uint32_t done = 0;
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
-      if (!unit(u, t, m0)) continue;
+      if (!unit(u)) continue;
+      const AgShrinkSide& sd = p.side[side];
       float v[64];
 #pragma unroll
       for (int j = 0; j < 64; ++j) v[j] = 0.f;
@@ -373,7 +384,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         for (int c = 0; c < 64; c += 32) {
           if (half * 64 + c >= t.n16) break;
           ag_gather(d + c, v + c);
-          if (p.np > 1) ag_gather(d + 128 + c, v + c);
+          if (sd.np > 1) ag_gather(d + 128 + c, v + c);
         }
         tc_fence_before();
         __syncwarp();
@@ -381,7 +392,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         ++done;
       }
       if (!ok) break;
-      const float scale = p.scaled ? __ldg(p.c.k.s + t.a) : 1.0f;
+      const float scale = sd.scaled ? __ldg(p.c.k.s + t.a) : 1.0f;
       const int m = m0 + q * 32 + (lane & ~1);
       // lanes 2 i and 2 i + 1 swap, so that each has two neighbouring ranks of every other row
 #pragma unroll
@@ -391,7 +402,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
         const int col = half * 64 + j + (lane & 1);
         const float x[2] = {(lane & 1) ? got : v0, (lane & 1) ? v1 : got};
-        if (m < p.out.width) ag_store_parts<2>(p.out, (int64_t)(t.at + col) * p.out.ld + m, x);      // (the rank is a multiple of 8)
+        if (m < sd.out.width) ag_store_parts<2>(sd.out, (int64_t)(t.at + col) * sd.out.ld + m, x);      // (the rank is a multiple of 8)
       }
     }
   }
@@ -1109,25 +1120,31 @@ int bank_map(CUtensorMap* tm, const __nv_bfloat16* ptr, int width, int rows, int
 
 int64_t most_tiles(const AdaptersCall& c, int tn) { return c.T / tn + std::min<int64_t>(c.T, c.k.n); }
 
-// u = x' A, or du = s dv B^T
-int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const Parts& in, const Parts& out, const __nv_bfloat16* W, bool kmajor,
-              bool scaled, cudaStream_t st) {
+struct ShrinkWork { const Parts *in, *out; const __nv_bfloat16* W; bool kmajor, scaled; };
+// u = x' A, du = s dv B^T, or both
+int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkWork* work, int sides, cudaStream_t st) {
   static std::atomic<bool> ready[64];
-  AgMaps3 maps{};
+  AgShrinkMaps maps{};
   AgShrink p{};
   p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
-  p.np = in.np; p.m_tiles = (c.k.r + 127) / 128; p.K = in.width; p.w_kmajor = kmajor; p.scaled = scaled; p.out = out;
+  p.m_tiles = (c.k.r + 127) / 128; p.sides = sides;
   // smaller tiles where large ones would leave SMs without any
   p.tn = 128;
-  while (p.tn > 32 && (int64_t)c.T * p.m_tiles / p.tn < 100) p.tn /= 2;
-  p.segment = out.np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
+  while (p.tn > 32 && (int64_t)c.T * p.m_tiles * sides / p.tn < 100) p.tn /= 2;
+  for (int i = 0; i < sides; ++i) {
+    const ShrinkWork& w = work[i];
+    const Parts& in = *w.in;
+    p.side[i] = {in.np, in.width, w.kmajor, w.scaled, *w.out};
+    p.np = std::max(p.np, in.np);
+    p.segment = w.out->np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
+    QB_TRY(parts_map(&maps.side[i].rows, in, l.rows, p.tn));
+    QB_TRY(parts_map(&maps.side[i].rows16, in, l.rows, 16));
+    // A [P][r]: the contraction runs over its rows; B [r][Q]: along them
+    QB_TRY(w.kmajor ? bank_map(&maps.side[i].w, w.W, in.width, c.k.r, c.k.n, 128) : bank_map(&maps.side[i].w, w.W, c.k.r, in.width, c.k.n, 64));
+  }
   const size_t stage = AG_TILE + (size_t)p.np * p.tn * 128, table = ag_table_bytes(c.k.n);
   p.stages = (int)std::min<size_t>(8, (AG_SMEM - AG_BARS - table) / stage);
-  QB_TRY(parts_map(&maps.rows, in, l.rows, p.tn));
-  QB_TRY(parts_map(&maps.rows16, in, l.rows, 16));
-  // A [P][r]: the contraction runs over its rows; B [r][Q]: along them
-  QB_TRY(kmajor ? bank_map(&maps.w, W, in.width, c.k.r, c.k.n, 128) : bank_map(&maps.w, W, c.k.r, in.width, c.k.n, 64));
-  return ag_launch(adapters_shrink_kernel, ready, maps, p, AG_THREADS, p.stages * stage + AG_BARS + table, most_tiles(c, p.tn) * p.m_tiles, st);
+  return ag_launch(adapters_shrink_kernel, ready, maps, p, AG_THREADS, p.stages * stage + AG_BARS + table, most_tiles(c, p.tn) * p.m_tiles * sides, st);
 }
 
 // shared memory of the spread kernel without slabs
@@ -1228,7 +1245,8 @@ int tc_adapters_fwd(const AdaptersCall& c, char* ws, int above, cudaStream_t st)
   pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = 1; pool.clear = above == 0;
   pool.src[0] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
   QB_TRY(ag_launch_pool(pool, l.rows, above > 0, st));
-  QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
+  const ShrinkWork u{&l.x, &l.u, c.k.A, false, false};
+  QB_TRY(ag_shrink(c, l, status, &u, 1, st));
   return ag_spread(c, l, status, l.u, c.k.B, c.k.Q, false, c.Y, c.k.l2, true, st);
 }
 
@@ -1241,8 +1259,11 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   pool.src[0] = ag_source(c.Y, c.k.d_out, c.k.l2, false, l.dv);
   if (grads) pool.src[1] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
   QB_TRY(ag_launch_pool(pool, l.rows, false, st));
-  if (c.dX.data || c.dA) QB_TRY(ag_shrink(c, l, status, l.dv, l.du, c.k.B, true, true, st));
-  if (c.dB) QB_TRY(ag_shrink(c, l, status, l.x, l.u, c.k.A, false, false, st));
+  ShrinkWork work[2];
+  int sides = 0;
+  if (c.dX.data || c.dA) work[sides++] = {&l.dv, &l.du, c.k.B, true, true};
+  if (c.dB) work[sides++] = {&l.x, &l.u, c.k.A, false, false};
+  QB_TRY(ag_shrink(c, l, status, work, sides, st));
   if (c.dX.data) QB_TRY(ag_spread(c, l, status, l.du, c.k.A, c.k.P, true, c.dX, c.k.l1, false, st));
   if (grads) QB_TRY(ag_grad(c, l, status, st));
   return QBLORA_OK;

@@ -236,6 +236,22 @@ def test_zero_and_tiny_blocks_in_8_bits(qb):
     assert bool(torch.isfinite(opt.params[0]).all())
 
 
+@pytest.mark.parametrize("size", [1e-16, 1e-8, 1e6, 1e15])
+def test_gradients_of_any_size_in_8_bits(qb, size):
+    # beta = 0: m = g and r = |g|, each a neighbour of the number itself.  v = g^2 is held in fp32, whose numbers below 2^-126 are 2^-149
+    # apart: off by 2^-150 at most, and with it r by 2^-150 / (2 |g|) and the update, g / r, by 2^-150 / (2 g^2) of itself
+    g = _randn(3, 5000, gain=size)
+    off = 2.0 ** -150 / (2 * g.double().abs())
+    opt = qb.AdamW([torch.zeros(5000, device=DEV)], [g], state_bits=8, betas=(0.0, 0.0), eps=0.0, lr=1.0)
+    opt.step()
+    assert bool(((opt.params[0] + g.sign()).abs() <= 2.0 ** -20 + off / g.double().abs()).all())      # 0 - 1 g / |g|
+    for got, want, scale in ((_wide(opt.m[0], opt.m_scale[0]), g.double(), opt.m_scale[0]), (_wide(opt.v[0], opt.v_scale[0]), g.double().abs(), opt.v_scale[0])):
+        s = scale.double().repeat_interleave(256)[:5000]
+        y = want.abs() / s
+        step = torch.where(y < 2.0 ** -6, torch.full_like(y, 2.0 ** -9), 2.0 ** (torch.floor(torch.log2(y.clamp(min=2.0 ** -6))) - 3))
+        assert bool(((got - want).abs() <= (step + y * 2.0 ** -20) * s + off).all())
+
+
 def test_mixed_states_many_tensors_equal_bits(qb):
     # 700 tensors, 8 and 32 bits side by side, equal inputs twice, the same tensors one by one in 32 bits
     sizes = [(37 * k) % 1200 for k in range(700)]
