@@ -42,7 +42,7 @@ struct Parts { __nv_bfloat16* p; int np, width, ld; int64_t stride; };
 
 struct AgPool {
   RowsView x;
-  int d, lam, wide;                     // elements of a row, pooled by lam; wide: 16-byte loads, lam a power of two
+  int d, lam, log;                      // elements of a row, pooled by lam = 2^log; -1: another lam, or a large one
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
@@ -76,6 +76,69 @@ __device__ __forceinline__ void ag_store_parts(const Parts& o, int64_t at, const
   }
 }
 
+// One row by one warp, lam = 2^LOG, in 16-byte loads: four of them per lane and turn, the next turn's on their way.  The kernel would be bound
+// by its instructions (117 per load with lam at run time and a store of its own per load: 3.3 TB/s), so everything here is fixed.
+template <int LOG>
+__device__ __forceinline__ void ag_pool_fast(const AgPool& p, const __nv_bfloat16* x, int64_t at, int lane) {
+  constexpr int U = 4, LANES = LOG > 3 ? 1 << (LOG - 3) : 1;      // lanes that share a result
+  const int chunks = p.d >> 3;
+  uint4 next[U];
+  auto ask = [&](int c0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int ch = c0 + u * 32 + lane;
+      next[u] = ch < chunks ? __ldcs(reinterpret_cast<const uint4*>(x) + ch) : make_uint4(0, 0, 0, 0);
+    }
+  };
+  ask(0);
+  for (int c0 = 0; c0 < chunks; c0 += 32 * U) {
+    uint4 w[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) w[u] = next[u];
+    ask(c0 + 32 * U);
+    float g[U];                                           // LOG >= 3: of eight, then of all
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int ch = c0 + u * 32 + lane;
+      const uint32_t e[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
+      if constexpr (LOG == 0) {
+        if (ch < chunks) *reinterpret_cast<uint4*>(p.out.p + at + 8 * (int64_t)ch) = w[u];
+      } else {
+        float s[4];                                       // sums of neighbouring two
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[i] = ag_low(e[i]) + ag_high(e[i]);
+        if constexpr (LOG == 1) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s[i] *= p.factor;
+          if (ch < chunks) ag_store_parts<4>(p.out, at + 4 * (int64_t)ch, s);
+        } else if constexpr (LOG == 2) {
+          const float f[2] = {(s[0] + s[1]) * p.factor, (s[2] + s[3]) * p.factor};
+          if (ch < chunks) ag_store_parts<2>(p.out, at + 2 * (int64_t)ch, f);
+        } else {
+          g[u] = ((s[0] + s[1]) + (s[2] + s[3])) * p.factor;
+#pragma unroll
+          for (int d = 1; d < LANES; d <<= 1) g[u] += __shfl_xor_sync(0xffffffffu, g[u], d);
+        }
+      }
+    }
+    if constexpr (LOG >= 3) {
+      // the lanes that share a result hold it for every u: each stores another one's
+      constexpr int K = LANES < U ? LANES : U;            // results that go out side by side
+      const int mine = lane & (LANES - 1);
+#pragma unroll
+      for (int u = 0; u < U; u += K) {
+        float v[1] = {g[u]};
+        int which = 0;
+#pragma unroll
+        for (int i = 1; i < K; ++i)
+          if (mine == i) { v[0] = g[u + i]; which = i; }
+        const int ch = c0 + (u + which) * 32 + lane;
+        if (mine < K && ch < chunks) ag_store_parts<1>(p.out, at + ch / LANES, v);
+      }
+    }
+  }
+}
+
 // One row by one warp.  x: nullptr for a row of zeros.
 __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row, int lane) {
   const int64_t at = row * p.out.ld;
@@ -84,52 +147,22 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row
     for (int i = lane; i < p.out.width; i += 32) ag_store_parts<1>(p.out, at + i, zero);
     return;
   }
-  if (!p.wide) {
-    for (int i = lane; i < p.out.width; i += 32) {
-      float acc[1] = {0.f};
-      for (int l = 0; l < p.lam; ++l) acc[0] += __bfloat162float(x[(int64_t)i * p.lam + l]);
-      if (p.factor != 1.f) acc[0] /= (float)p.lam;
-      ag_store_parts<1>(p.out, at + i, acc);
-    }
-    return;
+  switch (p.log) {
+    case 0: return ag_pool_fast<0>(p, x, at, lane);
+    case 1: return ag_pool_fast<1>(p, x, at, lane);
+    case 2: return ag_pool_fast<2>(p, x, at, lane);
+    case 3: return ag_pool_fast<3>(p, x, at, lane);
+    case 4: return ag_pool_fast<4>(p, x, at, lane);
+    case 5: return ag_pool_fast<5>(p, x, at, lane);
+    case 6: return ag_pool_fast<6>(p, x, at, lane);
+    case 7: return ag_pool_fast<7>(p, x, at, lane);
+    case 8: return ag_pool_fast<8>(p, x, at, lane);
   }
-  const int chunks = p.d >> 3;
-  constexpr int U = 4;                                  // 16-byte loads in flight per lane
-  for (int c0 = 0; c0 < chunks; c0 += 32 * U) {
-    uint4 w[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int ch = c0 + u * 32 + lane;
-      w[u] = ch < chunks ? __ldcs(reinterpret_cast<const uint4*>(x) + ch) : make_uint4(0, 0, 0, 0);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int ch = c0 + u * 32 + lane;
-      const bool there = ch < chunks;
-      const uint32_t e[4] = {w[u].x, w[u].y, w[u].z, w[u].w};
-      if (p.lam == 1) {
-        if (there) *reinterpret_cast<uint4*>(p.out.p + at + 8 * (int64_t)ch) = w[u];
-        continue;
-      }
-      float s[4];                                       // sums of neighbouring two
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[i] = ag_low(e[i]) + ag_high(e[i]);
-      if (p.lam == 2) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] *= p.factor;
-        if (there) ag_store_parts<4>(p.out, at + 4 * (int64_t)ch, s);
-        continue;
-      }
-      const float f[2] = {(s[0] + s[1]) * p.factor, (s[2] + s[3]) * p.factor};
-      if (p.lam == 4) {
-        if (there) ag_store_parts<2>(p.out, at + 2 * (int64_t)ch, f);
-        continue;
-      }
-      float g[1] = {f[0] + f[1]};                       // of eight; lam / 8 lanes have the rest
-      const int lanes = p.lam >> 3;
-      for (int d = 1; d < lanes; d <<= 1) g[0] += __shfl_xor_sync(0xffffffffu, g[0], d);
-      if (there && (ch & (lanes - 1)) == 0) ag_store_parts<1>(p.out, at + ch / lanes, g);
-    }
+  for (int i = lane; i < p.out.width; i += 32) {
+    float acc[1] = {0.f};
+    for (int l = 0; l < p.lam; ++l) acc[0] += __bfloat162float(x[(int64_t)i * p.lam + l]);
+    if (p.factor != 1.f) acc[0] /= (float)p.lam;
+    ag_store_parts<1>(p.out, at + i, acc);
   }
 }
 
@@ -1042,8 +1075,9 @@ Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* w
 }
 
 AgPool ag_source(const RowsView& x, int d, int lam, bool mean, const Parts& out) {
-  AgPool p{x, d, lam, 0, mean ? 1.0f / (float)lam : 1.0f, out};
-  p.wide = lam <= 256 && (lam & (lam - 1)) == 0;
+  AgPool p{x, d, lam, -1, mean ? 1.0f / (float)lam : 1.0f, out};
+  for (int i = 0; i <= 8; ++i)
+    if (lam == 1 << i) p.log = i;
   return p;
 }
 
