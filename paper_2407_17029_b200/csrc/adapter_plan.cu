@@ -41,14 +41,13 @@ __global__ void __launch_bounds__(AP_THREADS) adapter_plan_kernel(const __grid_c
       if (a < 0) len = 0;
     }
     const unsigned same = __match_any_sync(0xffffffffu, a);
-    int before = 0, all = 0;
-    for (unsigned left = __reduce_or_sync(0xffffffffu, a >= 0 ? same : 0u); left; left &= left - 1) {
-      const int j = __ffs(left) - 1, x = __shfl_sync(0xffffffffu, len, j);
-      if ((same >> j) & 1u) {
-        all += x;
-        if (j < lane) before += x;
-      }
+    // the fellows in front, one after the other: as many turns as the largest group of the chunk has lanes
+    int before = 0;
+    for (unsigned left = a >= 0 ? same & ((1u << lane) - 1u) : 0u; __any_sync(0xffffffffu, left != 0u); left &= left - 1u) {
+      const int x = __shfl_sync(0xffffffffu, len, left ? __ffs(left) - 1 : lane);
+      if (left) before += x;
     }
+    const int all = __shfl_sync(0xffffffffu, before + len, 31 - __clz(same));      // up to and with the last of them
     if (b < c.R) {
       const int lead = __ffs(same) - 1;
       s_id[b] = a;
