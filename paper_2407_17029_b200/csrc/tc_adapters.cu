@@ -46,7 +46,7 @@ struct AgPool {
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
-struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources, clear; uint32_t rows_there, above; int* status; };
+struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources, clear; uint32_t rows_there, above; int* status; uint32_t* tickets; int n_tickets; };
 
 // N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
 template <int N>
@@ -170,6 +170,7 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
   extern __shared__ uint32_t ag_smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
+  for (int i = blockIdx.x * AG_POOL_THREADS + threadIdx.x; i < p.n_tickets; i += gridDim.x * AG_POOL_THREADS) p.tickets[i] = 0u;
   const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128, p.above, 0x7fffffffu);
   const int lane = threadIdx.x & 31, warps = AG_POOL_THREADS / 32;
   const uint32_t rows = g.pad[g.kept];
@@ -872,13 +873,25 @@ struct AgGrad {
   AdaptersCall c;
   uint32_t rows_there, above;
   AgGradSide side[2];                   // out == nullptr: not wanted
+  int split;                            // an adapter of more rows is cut into parts, of at least half as many
+  float* parts;                         // their tiles, [slot][tile][128 x 128], where a part's slot is its first row / (split / 2)
+  uint32_t* tickets;                    // [slot][tile]: parts that are there; zero before the call
   int* status;
   long long wait_limit;
 };
 struct AgGradMaps { CUtensorMap a[2], b[2]; };
 
+// whether any of the eight epilogue warps says so; a barrier of theirs
+__device__ __forceinline__ bool ar_any(bool x) {
+  uint32_t y;
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
+               : "=r"(y) : "r"((uint32_t)x) : "memory");
+  return y != 0;
+}
+
 __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __grid_constant__ AgGradMaps maps, const __grid_constant__ AgGrad p) {
   extern __shared__ uint8_t smem_raw[];
+  __shared__ bool s_last;
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u, bars = base + AR_STAGES * AR_STAGE;
   auto full = [&](int s) { return bars + 16u * s; };
   auto empty = [&](int s) { return bars + 16u * s + 8; };
@@ -897,7 +910,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, 128, p.above, 0x7fffffffu);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.split, p.above, 0x7fffffffu);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -907,12 +920,19 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
   const AgGradSide &sa = p.side[0], &sb = p.side[1];
   const int ca = (sa.N + 127) / 128, cb = (sb.N + 127) / 128;
   const int ta = sa.out ? (sa.M + 127) / 128 * ca : 0, tb = sb.out ? (sb.M + 127) / 128 * cb : 0;
-  const long long units = (long long)k.n * (ta + tb);
-  struct Unit { int a, side, m0, n0, n16, steps, rank; uint32_t at; };
+  const int per = ta + tb;
+  // Units: the tiles of all parts, then those of all adapters, of which only those without rows have anything to do: zeros.
+  const long long work = (long long)ag_uni((int)g.tile[g.kept]) * per, units = work + (long long)k.n * per;
+  struct Unit { int a, side, m0, n0, n16, steps, rank, first, all, part, parts, tile; uint32_t at; bool skip; };
+  auto part_at = [](const Unit& t, int i) { return t.parts > 1 ? (int)((long long)t.all * i / t.parts) : i ? t.all : 0; };   // in 16 rows
   auto unit = [&](long long u) {
     Unit t;
-    t.a = (int)(u / (ta + tb));
-    int x = (int)(u - (long long)t.a * (ta + tb));
+    const bool zeros = u >= work;
+    if (zeros) u -= work;
+    const int w = (int)(u / per);
+    int x = (int)(u - (long long)w * per);
+    t.tile = x;
+    t.a = zeros ? w : ag_find(g.tile, g.kept, (uint32_t)w);
     t.side = x >= ta;
     if (t.side) x -= ta;
     const int cols = t.side ? cb : ca;
@@ -920,14 +940,20 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     t.n0 = x % cols * 128;
     t.n16 = min(128, ((t.side ? sb.N : sa.N) - t.n0 + 15) & ~15);
     t.rank = bank_rank(k, t.a);
-    t.at = t.a < g.kept ? g.pad[t.a] : 0;
-    t.steps = t.a < g.kept && (t.side ? t.m0 : t.n0) < t.rank ? (int)(g.pad[t.a + 1] - t.at) / 16 : 0;
+    const bool there = t.a < g.kept;
+    t.first = there ? (int)g.pad[t.a] : 0;
+    t.all = there ? (int)(g.pad[t.a + 1] - g.pad[t.a]) / 16 : 0;
+    t.parts = zeros ? 1 : (int)(g.tile[t.a + 1] - g.tile[t.a]);
+    t.part = zeros ? 0 : w - (int)g.tile[t.a];
+    const int from = part_at(t, t.part);
+    t.at = (uint32_t)(t.first + from * 16);
+    t.steps = (t.side ? t.m0 : t.n0) < t.rank ? part_at(t, t.part + 1) - from : 0;
+    t.skip = zeros ? t.all > 0 : t.steps == 0 && t.part > 0;
     return t;
   };
-
   auto uniform = [&](Unit t) {
     t.a = ag_uni(t.a); t.side = ag_uni(t.side); t.m0 = ag_uni(t.m0); t.n0 = ag_uni(t.n0); t.n16 = ag_uni(t.n16); t.steps = ag_uni(t.steps);
-    t.at = (uint32_t)ag_uni((int)t.at);
+    t.at = (uint32_t)ag_uni((int)t.at); t.skip = ag_uni(t.skip) != 0;
     return t;
   };
   if (warp == 0) {
@@ -938,6 +964,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       const Unit t = uniform(unit(u));
+      if (t.skip) continue;
       const int parts_a = p.side[t.side].parts_a, parts_b = p.side[t.side].parts_b, nb = (t.n16 + 63) / 64;
       for (int x = 0; x < t.steps; x += 2, ++it) {
         ok = ag_wait(empty(s), ph ^ 1u, p.status, p.wait_limit);
@@ -967,6 +994,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       const Unit t = uniform(unit(u));
+      if (t.skip) continue;
       const int parts_a = p.side[t.side].parts_a, parts_b = p.side[t.side].parts_b;
       const uint32_t idesc = ag_idesc(true, true, t.n16);
       int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
@@ -1003,6 +1031,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     bool ok = true;
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       const Unit t = unit(u);
+      if (t.skip) continue;
       const AgGradSide& side = p.side[t.side];
       float v[64];
 #pragma unroll
@@ -1010,7 +1039,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
       for (int x = 0; x < t.steps && ok; x += 2 * AR_SEGMENT) {
         const int b = done & 1;
         ok = __all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit));
-        if (!ok) break;
+        if (!ok) break;                                               // (all leave together, below)
         tc_fence_after();
         const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 256 + half * 64;
 #pragma unroll
@@ -1024,7 +1053,32 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
         if (lane == 0) mbar_arrive(accempty(b));
         ++done;
       }
+      ok = !ar_any(!ok);
       if (!ok) break;
+      if (t.parts > 1 && t.steps > 0) {
+        // This part's tile goes to memory; whoever comes last adds all of them up, in the parts' order
+        const int etid = tid - 64;
+        auto slot = [&](int i) { return (int64_t)((t.first + part_at(t, i) * 16) / (p.split / 2)) * per + t.tile; };
+        float4* mine = reinterpret_cast<float4*>(p.parts + slot(t.part) * 16384) + etid;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) mine[j * 256] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        __threadfence();
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (etid == 0) s_last = atomicAdd(p.tickets + slot(0), 1u) + 1u == (uint32_t)t.parts;
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (!s_last) continue;
+        __threadfence();
+#pragma unroll
+        for (int j = 0; j < 64; ++j) v[j] = 0.f;
+        for (int i = 0; i < t.parts; ++i) {
+          const float4* from = reinterpret_cast<const float4*>(p.parts + slot(i) * 16384) + etid;
+#pragma unroll
+          for (int j = 0; j < 16; ++j) {
+            const float4 x = __ldcg(from + j * 256);
+            v[4 * j] += x.x; v[4 * j + 1] += x.y; v[4 * j + 2] += x.z; v[4 * j + 3] += x.w;
+          }
+        }
+      }
       const int m = t.m0 + q * 32 + lane;
       const float scale = t.side ? __ldg(k.s + t.a) : 1.0f;           // du has it already
       if (m < side.M) {
@@ -1049,7 +1103,12 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------------------
-struct Layout { Parts x, dv, u, du; size_t bytes; uint32_t rows, above; };
+struct Layout {
+  Parts x, dv, u, du;
+  int split;                            // of the gradients: AgGrad
+  float* parts; uint32_t* tickets; int n_tickets;
+  size_t bytes; uint32_t rows, above;
+};
 
 // parts: of numbers that are no bf16 numbers
 Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* ws) {
@@ -1066,9 +1125,22 @@ Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* w
   };
   place(l.x, k.P, k.l1 > 1 ? parts : 1);
   place(l.u, k.r, parts);
+  l.split = 0x3ffffff0;
   if (backward) {
     place(l.dv, k.Q, k.l2 > 1 ? parts : 1);
     place(l.du, k.r, parts);
+    // Where one adapter's tiles do not fill the SMs twice, its rows are cut: into at most eight parts of all rows there are, and not below
+    // 512 rows, which the tiles' way through memory would cost.
+    const int64_t per = (int64_t)((k.P + 127) / 128 + (k.Q + 127) / 128) * ((k.r + 127) / 128), cuts = std::min<int64_t>(8, 296 / per);
+    if (cuts > 1) {
+      l.split = (int)std::max<int64_t>(512, (T / cuts + 31) / 32 * 32);
+      const int64_t slots = (int64_t)l.rows / (l.split / 2) + 1;
+      l.n_tickets = (int)(slots * per);
+      l.tickets = reinterpret_cast<uint32_t*>(ws + at);
+      at += align_up((size_t)l.n_tickets * 4, 256);
+      l.parts = reinterpret_cast<float*>(ws + at);
+      at += (size_t)l.n_tickets * 65536;
+    }
   }
   l.bytes = align_up(at, 256);
   return l;
@@ -1242,6 +1314,7 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   AgGradMaps maps{};
   AgGrad p{};
   p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.split = l.split; p.parts = l.parts; p.tickets = l.tickets;
   p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
   p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
   QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 32));
@@ -1249,7 +1322,8 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 32));
   QB_TRY(parts_map(&maps.b[1], l.dv, l.rows, 32));
   const int64_t per = (int64_t)((c.k.P + 127) / 128 + (c.k.Q + 127) / 128) * ((c.k.r + 127) / 128);
-  return ag_launch(adapters_grad_kernel, ready, maps, p, AG_THREADS, AR_STAGES * AR_STAGE + AG_BARS + ag_table_bytes(c.k.n), per * c.k.n, st);
+  const int64_t most = per * (c.k.n + (int64_t)l.rows / (l.split / 2) + 1);
+  return ag_launch(adapters_grad_kernel, ready, maps, p, AG_THREADS, AR_STAGES * AR_STAGE + AG_BARS + ag_table_bytes(c.k.n), most, st);
 }
 
 constexpr int kBackwardParts = 3;
@@ -1290,6 +1364,7 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   const bool grads = c.dA || c.dB;
   AgPoolParams pool{};
   pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = grads ? 2 : 1; pool.clear = 1;
+  pool.tickets = l.tickets; pool.n_tickets = grads ? l.n_tickets : 0;
   pool.src[0] = ag_source(c.Y, c.k.d_out, c.k.l2, false, l.dv);
   if (grads) pool.src[1] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
   QB_TRY(ag_launch_pool(pool, l.rows, false, st));
