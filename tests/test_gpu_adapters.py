@@ -359,3 +359,31 @@ def test_refusals(qb):
     assert empty.shape == (0, 256)
     _, dA, dB = qb.adapters_bwd(bank, plan, X[:0], Y[:0])
     assert not bool(dA.any()) and not bool(dB.any())
+
+
+@pytest.mark.parametrize("size", [(512, 256, 4, 4, 64), (1024, 1024, 8, 8, 256), (640, 1152, 2, 16, 136)], ids=str)
+@pytest.mark.parametrize("lens,ids", [([513, 528, 512, 40, 1100], [0, 1, 2, 3, 5]), ([4100, 3, 530, 1025], [0, 1, 2, 3]), ([250, 300, 700, 7, 2400], [1, 1, 0, 2, 1])],
+                         ids=["near the least", "one large", "in pieces"])
+def test_gradients_of_many_rows(qb, size, lens, ids):
+    # adapters whose rows are cut into parts, next to ones that are not, the last one's rows up to the end of the workspace
+    n = 6
+    bank = ra.make_bank(qb, n, *size, seed=21, ranks=[size[4], 5, size[4], size[4] // 2, 1, size[4]])
+    cu, di, T = ra.requests(lens, ids)
+    plan = qb.adapter_plan(cu, di, n, T)
+    X, dY = _randn(3, T, size[0]), _randn(4, T, size[1])
+    ws = qb.alloc_adapters_workspace(bank, T, backward=True)
+    ws.fill_(0xff)                                           # whatever a call finds there
+    nan = lambda t: torch.full(t.shape, float("nan"), device=DEV)  # noqa: E731
+    _, dA, dB = qb.adapters_bwd(bank, plan, X, dY, outs=(nan(bank.A), nan(bank.B)), ws=ws)
+    want, bound = ra.ref_bwd(bank, cu.tolist(), ids, X, dY, torch.zeros(T, size[0], device=DEV))
+    ra.check(dA, want[1], bound[1], 4, size[1] + size[0] // size[2] + T, ("dA", torch.float32))
+    ra.check(dB, want[2], bound[2], 4, size[0] + size[1] // size[3] + T, ("dB", torch.float32))
+    for _ in range(3):
+        again = qb.adapters_bwd(bank, plan, X, dY, ws=ws)
+        assert torch.equal(again[1], dA) and torch.equal(again[2], dB)
+    # the numbers of other adapters' rows change nothing
+    lens2, ids2 = lens[:1] + [900], ids[:1] + [4]
+    cu2, di2, T2 = ra.requests(lens2, ids2, T)
+    other = qb.adapters_bwd(bank, qb.adapter_plan(cu2, di2, n, T), X, dY, ws=ws)
+    if ids.count(ids[0]) == 1:
+        assert torch.equal(other[1][ids[0]], dA[ids[0]]) and torch.equal(other[2][ids[0]], dB[ids[0]])
