@@ -20,9 +20,13 @@ namespace qb {
 using namespace ptx;
 namespace {
 
-constexpr int NR_THREADS = 256, NR_WARPS = 8, NR_ROWS = 16;
+constexpr int NR_THREADS = 256, NR_WARPS = 8, NR_ROWS = 8;
 constexpr int NR_CHUNK = 512;                     // of the pooled input in shared memory at a time
 constexpr int NR_MAX_RANK = 512;
+constexpr int NR_STEP = 2048;                     // bytes of a step's weights: 16 of the contraction by 64 ranks (outputs)
+constexpr int NR_PART = NR_WARPS * NR_ROWS * (64 + 4) * 4;
+// steps of a warp whose weights are on their way
+template <int NP> constexpr int NR_AHEAD = NP == 3 ? 6 : 4;
 
 struct NrParams {
   AdaptersCall c;
@@ -32,91 +36,107 @@ struct NrParams {
   int* status;
 };
 
-// Bytes of shared memory: pooled input (later the products), partial sums of u, u.
+// Bytes of shared memory: the warps' weights, pooled input (later the products), partial sums of u, u.
 struct NrLayout { int x, part, u, table, all; };
 __host__ __device__ inline NrLayout nr_layout(int np, int r, int n) {
-  const int blocks = (r + 63) / 64;               // of 64 ranks; an adapter of fewer has more partial sums of each, eight blocks in all
   NrLayout l;
-  l.x = 0;
-  const int x = np * NR_ROWS * (NR_CHUNK + 8) * 2, v = NR_WARPS * NR_ROWS * 64 * 4;
-  l.part = x > v ? x : v;
-  l.u = l.part + (blocks > NR_WARPS ? blocks : NR_WARPS) * NR_ROWS * 64 * 4;
-  l.table = l.u + np * NR_ROWS * (blocks * 64 + 8) * 2;
-  l.all = l.table + 2 * (n + 1) * 4;
+  l.x = NR_WARPS * NR_STEP * (np == 3 ? NR_AHEAD<3> : NR_AHEAD<2>);
+  const int x = np * NR_ROWS * (NR_CHUNK + 8) * 2;
+  l.part = l.x + (x > NR_PART ? x : NR_PART);
+  l.u = l.part + NR_PART;                         // (at most eight sums of 64 ranks: more warps share a contraction where ranks are few)
+  l.table = l.u + np * NR_ROWS * ((r + 63) / 64 * 64 + 8) * 2;
+  l.all = l.table + 2 * (n + 1) * 4 + 127;
   return l;
 }
 
-// four rows k of 64 ranks (outputs) from m0 on: this lane's 8 from m0 + 8 (lane / 4) on
-struct NrWeights { uint4 w[4]; };
-__device__ __forceinline__ void nr_load(NrWeights& x, const __nv_bfloat16* W, int pitch, int k0, int K, int m, int M, int tig) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int k = k0 + 2 * tig + (i & 1) + 8 * (i >> 1);
-    x.w[i] = k < K && m < M ? __ldg(reinterpret_cast<const uint4*>(W + (int64_t)k * pitch + m)) : make_uint4(0, 0, 0, 0);
-  }
+// A matrix [K][pitch] from rank (output) m on, of which the first M are there, and a warp's steps through its contraction: first, first +
+// stride, ... < last.  A lane copies 16 bytes, chunk lane % 8, of rows lane / 8 + 0, 4, 8, 12 of a step; chunk c of row k lies at place c ^ (k % 8)
+// of the row's 128 bytes.  What is not there becomes zeros, also behind an adapter's own rank.
+struct NrSteps { const __nv_bfloat16* at; int64_t pitch; int rows, first, last, stride; bool in; };
+__device__ __forceinline__ NrSteps nr_steps(const __nv_bfloat16* W, int pitch, int K, int m, int M, int first, int last, int stride, int lane) {
+  const int c = m + 8 * (lane & 7), k = lane >> 3;
+  return {W + (int64_t)k * pitch + c, pitch, K - k, first, last, stride, c < M};
 }
-__device__ __forceinline__ uint32_t nr_word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ void nr_copy(const NrSteps& w, int s, uint32_t stage, int lane) {
+  if (s < w.last) {
+    const uint32_t to = stage + (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4);       // rows 4 and 12 further: the other half of the places
+    const __nv_bfloat16* from = w.at + (int64_t)s * 16 * w.pitch;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const bool there = w.in && s * 16 + 4 * i < w.rows;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((to ^ (i & 1) * 64) + i * 512), "l"(there ? from + 4 * i * w.pitch : w.at),
+                   "r"(there ? 16 : 0) : "memory");
+    }
+  }
+  asm volatile("cp.async.commit_group;" ::: "memory");
+}
+// the first steps' weights on their way
+template <int AHEAD>
+__device__ __forceinline__ void nr_ahead(const NrSteps& w, uint32_t ring, int lane) {
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) nr_copy(w, w.first + i * w.stride, ring + i * NR_STEP, lane);
+}
 
-// d[tile][n8] += the step's weights by the rows' parts; x: [part][16 rows][pitch] bf16 from the step's first column on
-template <int NP, int N8>
-__device__ __forceinline__ void nr_step(float (&d)[4][N8][4], const NrWeights& w, const __nv_bfloat16* x, int pitch, int part, int lane) {
-  uint32_t b[NP][N8][2];
+// d[tile] += the step's weights by the rows' parts; x: this lane's place in [part][8 rows][pitch] bf16, at the step's first column
+template <int NP>
+__device__ __forceinline__ void nr_step(float (&d)[4][4], uint32_t w, const __nv_bfloat16* x, int part) {
+  uint32_t b[NP][2];
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    b[p][0] = *reinterpret_cast<const uint32_t*>(x + p * part);
+    b[p][1] = *reinterpret_cast<const uint32_t*>(x + p * part + 8);
+  }
+  uint32_t a[4][4];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) frag_ldm4t(a[t], w ^ (t * 32));
 #pragma unroll
   for (int p = 0; p < NP; ++p)
 #pragma unroll
-    for (int n = 0; n < N8; ++n) {
-      const __nv_bfloat16* row = x + p * part + (n * 8 + (lane >> 2)) * pitch + 2 * (lane & 3);
-      b[p][n][0] = *reinterpret_cast<const uint32_t*>(row);
-      b[p][n][1] = *reinterpret_cast<const uint32_t*>(row + 8);
-    }
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    // rows of the tile: ranks 8 (lane / 4) + 2 t and + 2 t + 1 of the 64
-    const uint32_t k0 = nr_word(w.w[0], t), k1 = nr_word(w.w[1], t), k8 = nr_word(w.w[2], t), k9 = nr_word(w.w[3], t);
-    const uint32_t a[4] = {__byte_perm(k0, k1, 0x5410), __byte_perm(k0, k1, 0x7632), __byte_perm(k8, k9, 0x5410), __byte_perm(k8, k9, 0x7632)};
-#pragma unroll
-    for (int p = 0; p < NP; ++p)
-#pragma unroll
-      for (int n = 0; n < N8; ++n) frag_mma(d[t][n], a, b[p][n][0], b[p][n][1]);
-  }
+    for (int t = 0; t < 4; ++t) frag_mma(d[t], a[t], b[p][0], b[p][1]);
 }
-// Steps first, first + stride, ... < last of the contraction; w: the weights of the first AHEAD of them (nr_ahead).  NP = 3: emptied every
-// 16 steps, as the tensor core's sums lose a little per step.
-template <int NP, int N8, int AHEAD, class Rows>
-__device__ __forceinline__ void nr_product(float (&sum)[4][N8][4], NrWeights (&w)[AHEAD], const __nv_bfloat16* W, int pitch, int K, int m, int M, int first,
-                                           int last, int stride, int lane, Rows&& rows, int x_pitch, int part) {
-  float d[4][N8][4];
+// All of w's steps, after nr_ahead; x: the rows at step 0.  NP = 3: emptied every 16 steps, as the tensor core's sums lose a little per step.
+template <int NP>
+__device__ __forceinline__ void nr_product(float (&sum)[4][4], const NrSteps& w, uint32_t ring, const __nv_bfloat16* x, int pitch, int part, int lane) {
+  constexpr int AHEAD = NR_AHEAD<NP>;
+  // ldmatrix: lanes 8 i ... give the rows of matrix i; contraction 0..7 of ranks 0..7 and 8..15, then 8..15 of them
+  const int k = (lane & 7) + 8 * (lane >> 4);
+  const uint32_t mine = ring + k * 128 + ((((lane >> 3) & 1) ^ (k & 7)) << 4);
+  const __nv_bfloat16* xl = x + (lane >> 2) * pitch + 2 * (lane & 3);
+  float d[4][4];
   auto each = [&](auto&& f) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int n = 0; n < N8; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) f(d[t][n][e], sum[t][n][e]);
+      for (int e = 0; e < 4; ++e) f(d[t][e], sum[t][e]);
   };
   if (NP == 3) each([](float& x, float&) { x = 0.f; });
   int count = 0;
-  for (int s = first; s < last; s += AHEAD * stride) {
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) {
-      const int at = s + i * stride;
-      if (at >= last) break;
-      if constexpr (NP == 3) nr_step<NP, N8>(d, w[i], rows(at), x_pitch, part, lane);
-      else nr_step<NP, N8>(sum, w[i], rows(at), x_pitch, part, lane);
-      if (at + AHEAD * stride < last) nr_load(w[i], W, pitch, (at + AHEAD * stride) * 16, K, m, M, lane & 3);
-    }
-    if (NP == 3 && (count += AHEAD) >= 16) {
+  uint32_t stage = 0;
+  for (int s = w.first; s < w.last; s += w.stride) {
+    asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+    __syncwarp();
+    if constexpr (NP == 3) nr_step<NP>(d, mine + stage, xl + s * 16, part);
+    else nr_step<NP>(sum, mine + stage, xl + s * 16, part);
+    __syncwarp();
+    nr_copy(w, s + AHEAD * w.stride, ring + stage, lane);
+    if ((stage += NR_STEP) == AHEAD * NR_STEP) stage = 0;
+    if (NP == 3 && ++count == 16) {
       each([](float& x, float& y) { y += x; x = 0.f; });
       count = 0;
     }
   }
   if (NP == 3) each([](float& x, float& y) { y += x; });
 }
-template <int AHEAD>
-__device__ __forceinline__ void nr_ahead(NrWeights (&w)[AHEAD], const __nv_bfloat16* W, int pitch, int K, int m, int M, int first, int last, int stride, int lane) {
+// this lane's sums to out[row][rank]
+__device__ __forceinline__ void nr_put(const float (&d)[4][4], float* out, int pitch, int lane) {
+  float* to = out + 2 * (lane & 3) * pitch + (lane >> 2);
 #pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-    if (first + i * stride < last) nr_load(w[i], W, pitch, (first + i * stride) * 16, K, m, M, lane & 3);
+  for (int t = 0; t < 4; ++t) {
+    to[16 * t] = d[t][0];
+    to[16 * t + pitch] = d[t][1];
+    to[16 * t + 8] = d[t][2];
+    to[16 * t + 8 + pitch] = d[t][3];
+  }
 }
 
 template <int NP>
@@ -181,41 +201,39 @@ __device__ __forceinline__ void nr_pool(const AdaptersCall& c, const int* rows, 
   }
 }
 
-// One item: n rows (at most 8 N8) of adapter a, entries j ... of the plan, by all CTAs of the cluster.  AHEAD: steps of 16 whose weights a
-// warp has on their way, 2 KB each (two of them: 3.2 TB/s with an adapter per request).
-template <int NP, int N8, int AHEAD, bool F32>
+// One item: n rows (at most 8) of adapter a, entries j ... of the plan, by all CTAs of the cluster.
+template <int NP, bool F32>
 __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, uint8_t* nr_smem, int a, int j, int n) {
   __shared__ int s_row[NR_ROWS];
   const AdaptersCall& c = p.c;
   const BankView& k = c.k;
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, tig = lane & 3;
+  constexpr int AHEAD = NR_AHEAD<NP>;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int cs = (int)cluster_ctas(), rank = (int)cluster_ctarank();
   const int r_read = bank_rank(k, a), r16 = (r_read + 15) & ~15;
   if (tid < NR_ROWS) {
     const int row = tid < n ? __ldg(c.rows + j + tid) : -1;
     s_row[tid] = row < c.T ? row : -1;
   }
-  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(nr_smem);
+  const uint32_t ring = smem_u32(nr_smem) + warp * (AHEAD * NR_STEP);
+  __nv_bfloat16* xs = reinterpret_cast<__nv_bfloat16*>(nr_smem + l.x);
   float* part = reinterpret_cast<float*>(nr_smem + l.part);
   __nv_bfloat16* us = reinterpret_cast<__nv_bfloat16*>(nr_smem + l.u);
   constexpr int XP = NR_CHUNK + 8, XPART = NR_ROWS * XP;
-  const int blocks = (r16 + 63) / 64, wide = blocks * 64, splits = blocks >= NR_WARPS ? 1 : NR_WARPS / blocks;
+  const int blocks = (r16 + 63) / 64, wide = blocks * 64 + 4, splits = NR_WARPS / blocks;
 
   // ---- u's part: ranks [64 mb, ...) by warps mb, the contraction's steps dealt out over the splits
   const __nv_bfloat16* A = k.A + (int64_t)a * k.P * k.r;
   const int steps = (k.P + 15) / 16, s_lo = (int)((long long)steps * rank / cs), s_hi = (int)((long long)steps * (rank + 1) / cs);
   const int mb = warp % blocks, split = warp / blocks;
   const bool mine = split < splits;
-  const int m = mb * 64 + 8 * (lane >> 2);
-  float d[4][N8][4];
+  float d[4][4];
 #pragma unroll
-  for (int t = 0; t < 4; ++t)
-#pragma unroll
-    for (int e = 0; e < N8; ++e) d[t][e][0] = d[t][e][1] = d[t][e][2] = d[t][e][3] = 0.f;
+  for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
   for (int c0 = s_lo; c0 < s_hi; c0 += NR_CHUNK / 16) {
     const int c1 = min(s_hi, c0 + NR_CHUNK / 16);
-    NrWeights w[AHEAD];
-    if (mine) nr_ahead<AHEAD>(w, A, k.r, k.P, m, r_read, c0 + split, c1, splits, lane);
+    const NrSteps w = nr_steps(A, k.r, k.P, mb * 64, r_read, c0 + split, c1, splits, lane);
+    if (mine) nr_ahead<AHEAD>(w, ring, lane);
     __syncthreads();
     nr_pool<NP>(c, s_row, n, c0 * 16, min(c1 * 16, k.P), xs, XP, XPART);
     // columns behind the last of the contraction: their weights are zeros, but what lies here may be no number
@@ -224,19 +242,9 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
       if (col < (c1 - c0) * 16) xs[i / 16 / n * XPART + i / 16 % n * XP + col] = __float2bfloat16_rn(0.f);
     }
     __syncthreads();
-    if (mine)
-      nr_product<NP, N8, AHEAD>(d, w, A, k.r, k.P, m, r_read, c0 + split, c1, splits, lane, [&](int s) { return xs + (s - c0) * 16; }, XP, XPART);
+    if (mine) nr_product<NP>(d, w, ring, xs - c0 * 16, XP, XPART, lane);
   }
-  if (mine) {
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int e = 0; e < N8; ++e) {
-        float* to = part + (split * NR_ROWS + e * 8 + 2 * tig) * wide + m + 2 * t;
-        *reinterpret_cast<float2*>(to) = make_float2(d[t][e][0], d[t][e][2]);
-        *reinterpret_cast<float2*>(to + wide) = make_float2(d[t][e][1], d[t][e][3]);
-      }
-  }
+  if (mine) nr_put(d, part + split * NR_ROWS * wide + mb * 64, wide, lane);
   __syncthreads();
   if (splits > 1) {
     for (int i = tid; i < n * wide; i += NR_THREADS) {
@@ -247,16 +255,20 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
   }
 
   // ---- u: the cluster's parts, in order
-  const int up = wide + 8, upart = NR_ROWS * up;
+  const int up = blocks * 64 + 8, upart = NR_ROWS * up;
   const __nv_bfloat16* B = k.B + (int64_t)a * k.r * k.Q;
   const int q_blocks = (k.Q + 63) / 64, own = rank < q_blocks ? (q_blocks - rank + cs - 1) / cs : 0;
   const int steps2 = r16 / 16;
-  int kw = 1;                                     // warps that share a block's contraction
-  while (kw * 2 * own <= NR_WARPS && kw * 2 <= steps2) kw *= 2;
+  // kw warps share a block's contraction: as many as give the fewest rounds of steps, with two more a round for its end
+  int kw = 1, best = 0x7fffffff;
+  for (int t = 1; t <= NR_WARPS; t *= 2) {
+    const int cost = (own * t + NR_WARPS - 1) / NR_WARPS * ((steps2 + t - 1) / t + 2);
+    if (cost < best) { best = cost; kw = t; }
+  }
   const int team = warp / kw, sub = warp % kw, teams = NR_WARPS / kw;
   auto q0_of = [&](int b) { return (rank + b * cs) * 64; };
-  NrWeights w2[AHEAD];
-  if (team < own) nr_ahead<AHEAD>(w2, B, k.Q, r_read, q0_of(team) + 8 * (lane >> 2), k.Q, sub, steps2, kw, lane);
+  auto b_steps = [&](int b) { return nr_steps(B, k.Q, r_read, q0_of(b), k.Q, sub, steps2, kw, lane); };
+  if (team < own) nr_ahead<AHEAD>(b_steps(team), ring, lane);
   if (cs > 1) cluster_sync_all();
   else __syncthreads();
   const uint32_t remote = smem_u32(part);
@@ -281,42 +293,43 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
   __syncthreads();
 
   // ---- Y: blocks of 64 outputs of the pooled kind, in turn over the teams of kw warps
-  float* vs = reinterpret_cast<float*>(nr_smem);  // [warp][row][64]
+  float* vs = reinterpret_cast<float*>(nr_smem + l.x);  // [warp][row][64]
   const float scale = __ldg(k.s + a);
-  constexpr int ES = F32 ? 4 : 2, E = 16 / ES;
+  constexpr int ES = F32 ? 4 : 2, E = 16 / ES, VP = 64 + 4;
   const int w_q = k.l2 * ES;                      // bytes of one q
   for (int b0 = 0; b0 < own; b0 += teams) {
     const int b = b0 + team;
     const bool there = b < own;
     const int q0 = there ? q0_of(b) : 0;
+    // whole rows' 16-byte chunks; what this lane adds to first is under way meanwhile
+    const int chunks = there ? min(64, k.Q - q0) * w_q / 16 : 0;
+    auto y_at = [&](int i) {
+      const int row = i / chunks, y_row = s_row[row];
+      return y_row < 0 ? nullptr
+                       : reinterpret_cast<uint4*>(static_cast<char*>(c.Y.data) + y_row * c.Y.stride * ES + (int64_t)q0 * w_q) + (i - row * chunks);
+    };
+    uint4 y0 = make_uint4(0, 0, 0, 0);
+    if (sub * 32 + lane < n * chunks) {
+      const uint4* at = y_at(sub * 32 + lane);
+      if (at) y0 = *at;
+    }
     if (there) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < N8; ++e) d[t][e][0] = d[t][e][1] = d[t][e][2] = d[t][e][3] = 0.f;
-      nr_product<NP, N8, AHEAD>(d, w2, B, k.Q, r_read, q0 + 8 * (lane >> 2), k.Q, sub, steps2, kw, lane, [&](int s) { return us + s * 16; }, up, upart);
-      if (b + teams < own) nr_ahead<AHEAD>(w2, B, k.Q, r_read, q0_of(b + teams) + 8 * (lane >> 2), k.Q, sub, steps2, kw, lane);
-      float* v = vs + warp * NR_ROWS * 64;
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int e = 0; e < N8; ++e) {
-          float* to = v + (e * 8 + 2 * tig) * 64 + 8 * (lane >> 2) + 2 * t;
-          *reinterpret_cast<float2*>(to) = make_float2(d[t][e][0], d[t][e][2]);
-          *reinterpret_cast<float2*>(to + 64) = make_float2(d[t][e][1], d[t][e][3]);
-        }
+      for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
+      nr_product<NP>(d, b_steps(b), ring, us, up, upart, lane);
+      if (b + teams < own) nr_ahead<AHEAD>(b_steps(b + teams), ring, lane);
+      nr_put(d, vs + warp * NR_ROWS * VP, VP, lane);
     }
     if (kw > 1) __syncthreads();
     else __syncwarp();
     if (there) {
-      // whole rows' 16-byte chunks; the sums of the team's parts and the factor on the way
-      const int chunks = min(64, k.Q - q0) * w_q / 16;
-      const float* v0 = vs + team * kw * NR_ROWS * 64;
+      // the sums of the team's parts and the factor on the way
+      const float* v0 = vs + team * kw * NR_ROWS * VP;
       for (int i = sub * 32 + lane; i < n * chunks; i += kw * 32) {
-        const int row = i / chunks, ch = i - row * chunks, y_row = s_row[row];
-        if (y_row < 0) continue;
-        uint4* at = reinterpret_cast<uint4*>(static_cast<char*>(c.Y.data) + y_row * c.Y.stride * ES + (int64_t)q0 * w_q) + ch;
-        const uint4 y = *at;
+        const int row = i / chunks, ch = i - row * chunks;
+        uint4* at = y_at(i);
+        if (!at) continue;
+        const uint4 y = i == sub * 32 + lane ? y0 : *at;
         uint32_t e[4] = {y.x, y.y, y.z, y.w};
         float x[E];
         int last = -1;
@@ -326,7 +339,7 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
           const int q = p.shift >= 0 ? (ch * 16 + f * ES) >> p.shift : (ch * E + f) / k.l2;
           if (q != last) {
             now = 0.f;
-            for (int s = 0; s < kw; ++s) now += v0[(s * NR_ROWS + row) * 64 + q];
+            for (int s = 0; s < kw; ++s) now += v0[(s * NR_ROWS + row) * VP + q];
             last = q;
           }
           x[f] = now * scale;
@@ -347,7 +360,8 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
 
 template <int NP, bool F32>
 __global__ void __launch_bounds__(NR_THREADS, NP == 3 ? 1 : 2) adapters_rows_kernel(const __grid_constant__ NrParams p) {
-  extern __shared__ __align__(16) uint8_t nr_smem[];
+  extern __shared__ __align__(16) uint8_t nr_raw[];
+  uint8_t* nr_smem = nr_raw + (-smem_u32(nr_raw) & 127u);        // the places of nr_copy
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const AdaptersCall& c = p.c;
   const BankView& k = c.k;
@@ -361,8 +375,7 @@ __global__ void __launch_bounds__(NR_THREADS, NP == 3 ? 1 : 2) adapters_rows_ker
   const int a = ag_find(g.tile, g.kept, item), i0 = (int)(item - g.tile[a]) * NR_ROWS, j = plan_start(c, a) + i0;
   const int n = min(NR_ROWS, plan_start(c, a + 1) - j);
   if (bank_rank(k, a) == 0) return;
-  if (n <= 8) nr_item<NP, 1, NP == 3 ? 6 : 4, F32>(p, l, nr_smem, a, j, n);
-  else nr_item<NP, 2, NP == 3 ? 4 : 3, F32>(p, l, nr_smem, a, j, n);
+  nr_item<NP, F32>(p, l, nr_smem, a, j, n);
 }
 
 template <int NP, bool F32>
