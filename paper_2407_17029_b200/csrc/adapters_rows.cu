@@ -52,27 +52,40 @@ __host__ __device__ inline NrLayout nr_layout(int np, int r, int n) {
 // A matrix [K][pitch] from rank (output) m on, of which the first M are there, and a warp's steps through its contraction: first, first +
 // stride, ... < last.  A lane copies 16 bytes, chunk lane % 8, of rows lane / 8 + 0, 4, 8, 12 of a step; chunk c of row k lies at place c ^ (k % 8)
 // of the row's 128 bytes.  What is not there becomes zeros, also behind an adapter's own rank.
-struct NrSteps { const __nv_bfloat16* at; int64_t pitch; int rows, first, last, stride; bool in; };
+struct NrSteps {
+  const __nv_bfloat16* at;                        // of the lane, at the step that is copied next
+  int64_t next, four;                             // elements from step to step; of four rows
+  int rows, first, last, stride;                  // rows from the lane's first on
+  bool in, all_in;
+};
 __device__ __forceinline__ NrSteps nr_steps(const __nv_bfloat16* W, int pitch, int K, int m, int M, int first, int last, int stride, int lane) {
   const int c = m + 8 * (lane & 7), k = lane >> 3;
-  return {W + (int64_t)k * pitch + c, pitch, K - k, first, last, stride, c < M};
+  return {W + (int64_t)(first * 16 + k) * pitch + c, (int64_t)stride * 16 * pitch, (int64_t)4 * pitch, K - k, first, last, stride, c < M, m + 64 <= M};
 }
-__device__ __forceinline__ void nr_copy(const NrSteps& w, int s, uint32_t stage, int lane) {
+__device__ __forceinline__ void nr_copy(NrSteps& w, int s, uint32_t stage, int lane) {
   if (s < w.last) {
-    const uint32_t to = stage + (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 3)) << 4);       // rows 4 and 12 further: the other half of the places
-    const __nv_bfloat16* from = w.at + (int64_t)s * 16 * w.pitch;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const bool there = w.in && s * 16 + 4 * i < w.rows;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((to ^ (i & 1) * 64) + i * 512), "l"(there ? from + 4 * i * w.pitch : w.at),
-                   "r"(there ? 16 : 0) : "memory");
+    const int k = lane >> 3, c = lane & 7;
+    const uint32_t to = stage + k * 128 + ((c ^ k) << 4), to4 = stage + k * 128 + ((c ^ k ^ 4) << 4);      // rows 4 and 12 further: to4
+    const __nv_bfloat16 *f0 = w.at, *f1 = f0 + w.four, *f2 = f1 + w.four, *f3 = f2 + w.four;
+    w.at += w.next;
+    auto copy = [](uint32_t to, const __nv_bfloat16* from) {
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+    };
+    auto copy_if = [&](uint32_t to, const __nv_bfloat16* from, int row) {
+      if (w.in && row < w.rows) copy(to, from);
+      else asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0) : "memory");
+    };
+    if (w.all_in && s * 16 + 12 < w.rows) {
+      copy(to, f0); copy(to4 + 512, f1); copy(to + 1024, f2); copy(to4 + 1536, f3);
+    } else {
+      copy_if(to, f0, s * 16); copy_if(to4 + 512, f1, s * 16 + 4); copy_if(to + 1024, f2, s * 16 + 8); copy_if(to4 + 1536, f3, s * 16 + 12);
     }
   }
   asm volatile("cp.async.commit_group;" ::: "memory");
 }
 // the first steps' weights on their way
 template <int AHEAD>
-__device__ __forceinline__ void nr_ahead(const NrSteps& w, uint32_t ring, int lane) {
+__device__ __forceinline__ void nr_ahead(NrSteps& w, uint32_t ring, int lane) {
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) nr_copy(w, w.first + i * w.stride, ring + i * NR_STEP, lane);
 }
@@ -96,7 +109,7 @@ __device__ __forceinline__ void nr_step(float (&d)[4][4], uint32_t w, const __nv
 }
 // All of w's steps, after nr_ahead; x: the rows at step 0.  NP = 3: emptied every 16 steps, as the tensor core's sums lose a little per step.
 template <int NP>
-__device__ __forceinline__ void nr_product(float (&sum)[4][4], const NrSteps& w, uint32_t ring, const __nv_bfloat16* x, int pitch, int part, int lane) {
+__device__ __forceinline__ void nr_product(float (&sum)[4][4], NrSteps& w, uint32_t ring, const __nv_bfloat16* x, int pitch, int part, int lane) {
   constexpr int AHEAD = NR_AHEAD<NP>;
   // ldmatrix: lanes 8 i ... give the rows of matrix i; contraction 0..7 of ranks 0..7 and 8..15, then 8..15 of them
   const int k = (lane & 7) + 8 * (lane >> 4);
@@ -232,7 +245,7 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
   for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
   for (int c0 = s_lo; c0 < s_hi; c0 += NR_CHUNK / 16) {
     const int c1 = min(s_hi, c0 + NR_CHUNK / 16);
-    const NrSteps w = nr_steps(A, k.r, k.P, mb * 64, r_read, c0 + split, c1, splits, lane);
+    NrSteps w = nr_steps(A, k.r, k.P, mb * 64, r_read, c0 + split, c1, splits, lane);
     if (mine) nr_ahead<AHEAD>(w, ring, lane);
     __syncthreads();
     nr_pool<NP>(c, s_row, n, c0 * 16, min(c1 * 16, k.P), xs, XP, XPART);
@@ -268,7 +281,8 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
   const int team = warp / kw, sub = warp % kw, teams = NR_WARPS / kw;
   auto q0_of = [&](int b) { return (rank + b * cs) * 64; };
   auto b_steps = [&](int b) { return nr_steps(B, k.Q, r_read, q0_of(b), k.Q, sub, steps2, kw, lane); };
-  if (team < own) nr_ahead<AHEAD>(b_steps(team), ring, lane);
+  NrSteps w2 = b_steps(team);
+  if (team < own) nr_ahead<AHEAD>(w2, ring, lane);
   if (cs > 1) cluster_sync_all();
   else __syncthreads();
   const uint32_t remote = smem_u32(part);
@@ -316,8 +330,9 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
     if (there) {
 #pragma unroll
       for (int t = 0; t < 4; ++t) d[t][0] = d[t][1] = d[t][2] = d[t][3] = 0.f;
-      nr_product<NP>(d, b_steps(b), ring, us, up, upart, lane);
-      if (b + teams < own) nr_ahead<AHEAD>(b_steps(b + teams), ring, lane);
+      nr_product<NP>(d, w2, ring, us, up, upart, lane);
+      w2 = b_steps(b + teams);
+      if (b + teams < own) nr_ahead<AHEAD>(w2, ring, lane);
       nr_put(d, vs + warp * NR_ROWS * VP, VP, lane);
     }
     if (kw > 1) __syncthreads();
