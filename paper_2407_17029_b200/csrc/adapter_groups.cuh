@@ -14,9 +14,9 @@ struct AgGroups {
 __device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, 0x7fffffffu); }   // both below 2^31
 
 // by the whole CTA; s: 2 (n + 1) words of shared memory
-// tn: rows of a tile; only adapters of more than `above` and at most `most` rows count.
+// tn: rows of a tile
 template <int NT>
-__device__ __forceinline__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_there, int tn, uint32_t above, uint32_t most) {
+__device__ __forceinline__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s, uint32_t rows_there, int tn) {
   __shared__ uint32_t s_part[2][NT / 32];
   __shared__ int s_kept;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n = c.k.n;
@@ -24,8 +24,7 @@ __device__ __forceinline__ AgGroups ag_groups(const AdaptersCall& c, uint32_t* s
   const int per = (n + NT - 1) / NT, lo = min(tid * per, n), hi = min(lo + per, n);
   uint32_t mine = 0, tiles = 0;
   for (int a = lo; a < hi; ++a) {
-    uint32_t rows = (uint32_t)max(plan_start(c, a + 1) - plan_start(c, a), 0);
-    if (rows <= above || rows > most) rows = 0;
+    const uint32_t rows = (uint32_t)max(plan_start(c, a + 1) - plan_start(c, a), 0);
     const uint32_t p = (min(rows, 0x7ffffff0u) + 15u) & ~15u, t = (rows + tn - 1) / tn;
     pad[a] = p;
     tile[a] = t;

@@ -49,13 +49,11 @@ int simt_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st);
 bool tc_adapters_sizes_ok(const BankView& k, int64_t T);
 bool tc_adapters_supported(const AdaptersCall& c);
 size_t tc_adapters_ws_bytes(const BankView& k, int64_t T, bool backward);
-// adapters of more than `above` rows
-int tc_adapters_fwd(const AdaptersCall& c, char* ws, int above, cudaStream_t st);
+int tc_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st);
 int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st);
 
-// Few rows per adapter, forward (adapters_rows.cu): adapters of at most `most` rows, in one launch without workspace but the status
-// word, which is cleared if `first`.
+// Few rows, forward (adapters_rows.cu): one launch, without workspace but the status word.
 bool rows_adapters_supported(const AdaptersCall& c);
-int rows_adapters_fwd(const AdaptersCall& c, int most, bool first, int* status, cudaStream_t st);
+int rows_adapters_fwd(const AdaptersCall& c, int* status, cudaStream_t st);
 
 }  // namespace qb

@@ -35,9 +35,10 @@ bool force_general() {
   return e && e[0] == '1';
 }
 
-// The host does not know how many rows an adapter has.  Calls of at most kFewTokens rows are all adapters_rows.cu's; larger ones have
-// adapters of at most kFewRows rows there and the others in tc_adapters.cu.
-constexpr int kFewTokens = 512, kFewRows = 32;
+// Calls of no more rows go to adapters_rows.cu, by the type of Y; larger ones, whose adapters have many rows then, or are many, to
+// tc_adapters.cu.  (Both in us, graph replays.  bf16: 4096 -> 4096, rank 64, 64 adapters of 8 rows 14 and 31, 16 of 32 14 and 25, 16 of 64 23 and 28;
+// 4096 -> 11008, rank 256, 64 of 8 40 and 57, 16 of 32 33 and 35, 16 of 64 52 and 38.  fp32: 16 of 16 14 and 25, of 64 46 and 32; 36 and 36, 115 and 53.)
+int few_rows(int y_dtype) { return y_dtype == QBLORA_F32 ? 256 : 512; }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
@@ -90,14 +91,8 @@ int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, co
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adapters_workspace_bytes(bank, tokens, 0)) return QBLORA_ERR_WORKSPACE;
   if (!force_general() && tc_adapters_supported(c)) {
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int above = 0;
-    if (rows_adapters_supported(c)) {
-      const bool all = tokens <= kFewTokens;
-      const int done = rows_adapters_fwd(c, all ? 0x7fffffff : kFewRows, true, static_cast<int*>(ws), st);
-      if (done || all) return done;
-      above = kFewRows;
-    }
-    return tc_adapters_fwd(c, static_cast<char*>(ws), above, st);
+    if (tokens <= few_rows(y_dtype) && rows_adapters_supported(c)) return rows_adapters_fwd(c, static_cast<int*>(ws), st);
+    return tc_adapters_fwd(c, static_cast<char*>(ws), st);
   }
   return simt_adapters_fwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));
 }

@@ -30,9 +30,7 @@ template <int NP> constexpr int NR_AHEAD = NP == 3 ? 6 : 4;
 
 struct NrParams {
   AdaptersCall c;
-  int most;                                       // rows of an adapter that is this kernel's
   int shift;                                      // log2 of the bytes of one q of Y, -1: no power of two
-  int clear;
   int* status;
 };
 
@@ -377,13 +375,12 @@ template <int NP, bool F32>
 __global__ void __launch_bounds__(NR_THREADS, NP == 3 ? 1 : 2) adapters_rows_kernel(const __grid_constant__ NrParams p) {
   extern __shared__ __align__(16) uint8_t nr_raw[];
   uint8_t* nr_smem = nr_raw + (-smem_u32(nr_raw) & 127u);        // the places of nr_copy
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const AdaptersCall& c = p.c;
   const BankView& k = c.k;
   const NrLayout l = nr_layout(NP, k.r, k.n);
   const int tid = threadIdx.x;
-  if (p.clear && blockIdx.x == 0 && tid == 0) *p.status = QBLORA_OK;
-  const AgGroups g = ag_groups<NR_THREADS>(c, reinterpret_cast<uint32_t*>(nr_smem + l.table), 0x7fffffffu, NR_ROWS, 0, (uint32_t)p.most);
+  if (blockIdx.x == 0 && tid == 0) *p.status = QBLORA_OK;
+  const AgGroups g = ag_groups<NR_THREADS>(c, reinterpret_cast<uint32_t*>(nr_smem + l.table), 0x7fffffffu, NR_ROWS);
   const int cs = (int)cluster_ctas();
   const uint32_t item = blockIdx.x / cs;
   if (item >= g.tile[g.kept]) return;             // (the whole cluster)
@@ -424,21 +421,27 @@ bool rows_adapters_supported(const AdaptersCall& c) {
   return c.k.r <= NR_MAX_RANK && nr_layout(c.Y.dtype == QBLORA_F32 ? 3 : 2, c.k.r, c.k.n).all <= 230 * 1024;
 }
 
-int rows_adapters_fwd(const AdaptersCall& c, int most, bool first, int* status, cudaStream_t st) {
+int rows_adapters_fwd(const AdaptersCall& c, int* status, cudaStream_t st) {
   NrParams p{};
-  p.c = c; p.most = most; p.clear = first; p.status = status;
+  p.c = c; p.status = status;
   const int w = c.k.l2 * (c.Y.dtype == QBLORA_F32 ? 4 : 2);
   p.shift = -1;
   for (int i = 0; i < 31; ++i)
     if (w == 1 << i) p.shift = i;
-  // at most: an item for each adapter that begins, and one for each 16 rows
-  const int64_t tiles = std::min<int64_t>(c.T / NR_ROWS, (int64_t)c.k.n * (most / NR_ROWS));
-  const int64_t items = std::min<int64_t>(c.T, tiles + c.k.n);
+  // at most: an item for each adapter that begins, and one for each 8 rows
+  const int64_t items = std::min<int64_t>(c.T, c.T / NR_ROWS + c.k.n);
   int sms = 0, dev = 0;
   QB_CUDA(cudaGetDevice(&dev));
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  // Clusters as large as there is room for at once: two CTAs an SM, or one where their shared memory or registers are too many, and of one an
+  // SM a quarter less, as a cluster lies within a GPC and leaves what does not make another one.  (4096 -> 11008, rank 256, one row each, in
+  // us by clusters of 1, 2, 4, 8: 16 adapters 35, 21, 16, 14; 48: 39, 23, 20, 27; 100: 47, 38, 47, 61; 200: 69, 77, 75, 110.)  How many items there are
+  // only the plan knows; between this and twice as many.
+  const int np = c.Y.dtype == QBLORA_F32 ? 3 : 2;
+  const bool two = np == 2 && nr_layout(np, c.k.r, c.k.n).all <= 113 * 1024;
+  const int64_t likely = std::max<int64_t>(std::min(c.T, c.k.n), c.T / NR_ROWS), room = two ? 2 * sms : sms * 3 / 4;
   int cs = 8;
-  while (cs > 1 && items * cs > 2 * sms) cs /= 2;
+  while (cs > 1 && likely * cs > room) cs /= 2;
   return c.Y.dtype == QBLORA_F32 ? nr_launch<3, true>(p, items, cs, st) : nr_launch<2, false>(p, items, cs, st);
 }
 

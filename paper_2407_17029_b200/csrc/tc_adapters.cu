@@ -46,7 +46,7 @@ struct AgPool {
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
-struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources, clear; uint32_t rows_there, above; int* status; uint32_t* tickets; int n_tickets; };
+struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; uint32_t* tickets; int n_tickets; };
 
 // N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
 template <int N>
@@ -169,9 +169,9 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row
 __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __grid_constant__ AgPoolParams p) {
   extern __shared__ uint32_t ag_smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  if (p.clear && blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
   for (int i = blockIdx.x * AG_POOL_THREADS + threadIdx.x; i < p.n_tickets; i += gridDim.x * AG_POOL_THREADS) p.tickets[i] = 0u;
-  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128, p.above, 0x7fffffffu);
+  const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128);
   const int lane = threadIdx.x & 31, warps = AG_POOL_THREADS / 32;
   const uint32_t rows = g.pad[g.kept];
   for (int64_t i = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); i < (int64_t)rows * p.sources; i += (int64_t)gridDim.x * warps) {
@@ -196,7 +196,7 @@ struct AgShrinkSide {
 };
 struct AgShrink {
   AdaptersCall c;
-  uint32_t rows_there, above;           // of the workspace; adapters of no more rows than this are another kernel's
+  uint32_t rows_there;                  // of the workspace
   int tn, stages, np;                   // rows of a tile; of the ring; most parts
   int segment;                          // 64-wide blocks of the contraction that one accumulator takes
   int m_tiles, sides;                   // tiles of 128 ranks
@@ -315,7 +315,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn, p.above, 0x7fffffffu);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -458,7 +458,7 @@ constexpr int AS_EPI = 512, AS_THREADS = 128 + AS_EPI;     // loads, MMAs, slabs
 constexpr int AS_SLAB = 16384, AS_RING = 3;
 struct AgSpread {
   AdaptersCall c;
-  uint32_t rows_there, above;           // of the workspace; adapters of no more rows than this are another kernel's
+  uint32_t rows_there;                  // of the workspace
   int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
   int slabs;
   int m_tiles, M, w_kmajor, scaled;
@@ -606,7 +606,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(256) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn, p.above, 0x7fffffffu);
+  const AgGroups g = ag_groups<AS_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.tn);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -871,7 +871,7 @@ __device__ __forceinline__ void ar_issue(uint32_t d, uint64_t a, uint64_t b, uin
 struct AgGradSide { int parts_a, parts_b, M, N; float* out; };        // dA: x' (P) by du (r); dB: u (r) by dv (Q)
 struct AgGrad {
   AdaptersCall c;
-  uint32_t rows_there, above;
+  uint32_t rows_there;
   AgGradSide side[2];                   // out == nullptr: not wanted
   int split;                            // an adapter of more rows is cut into parts, of at least half as many
   float* parts;                         // their tiles, [slot][tile][128 x 128], where a part's slot is its first row / (split / 2)
@@ -910,7 +910,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.split, p.above, 0x7fffffffu);
+  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.split);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -1107,7 +1107,7 @@ struct Layout {
   Parts x, dv, u, du;
   int split;                            // of the gradients: AgGrad
   float* parts; uint32_t* tickets; int n_tickets;
-  size_t bytes; uint32_t rows, above;
+  size_t bytes; uint32_t rows;
 };
 
 // parts: of numbers that are no bf16 numbers
@@ -1189,7 +1189,7 @@ int ag_launch(void (*kernel)(Maps, Params), std::atomic<bool>* ready, const Maps
 
 // beside: the kernel in front on the stream is adapters_rows.cu's, of other rows: this one need not wait for its end before it
 // begins, only before it ends itself.
-int ag_launch_pool(const AgPoolParams& p, int64_t rows, bool beside, cudaStream_t st) {
+int ag_launch_pool(const AgPoolParams& p, int64_t rows, cudaStream_t st) {
   int sms = 0;
   const int rc = ag_sms(&sms);
   if (rc) return rc;
@@ -1199,10 +1199,6 @@ int ag_launch_pool(const AgPoolParams& p, int64_t rows, bool beside, cudaStream_
   cfg.blockDim = dim3(AG_POOL_THREADS);
   cfg.dynamicSmemBytes = ag_table_bytes(p.c.k.n);
   cfg.stream = st;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr; cfg.numAttrs = beside ? 1 : 0;
   QB_CUDA(cudaLaunchKernelEx(&cfg, adapters_pool_kernel, p));
   count_launch();
   return QBLORA_OK;
@@ -1232,7 +1228,7 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
   static std::atomic<bool> ready[64];
   AgShrinkMaps maps{};
   AgShrink p{};
-  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.m_tiles = (c.k.r + 127) / 128; p.sides = sides;
   // smaller tiles where large ones would leave SMs without any
   p.tn = 128;
@@ -1280,7 +1276,7 @@ int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   static std::atomic<bool> ready[9][64];
   AsMaps maps{};
   AgSpread p{};
-  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.np = in.np; p.kb = (c.k.r + 63) / 64; p.tn = as_rows(c.k, in.np);
   const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
   p.slabs = (int)std::min<size_t>(8, (AG_SMEM - fixed) / AS_SLAB);
@@ -1313,7 +1309,7 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   static std::atomic<bool> ready[64];
   AgGradMaps maps{};
   AgGrad p{};
-  p.c = c; p.rows_there = l.rows; p.above = l.above; p.status = status; p.wait_limit = wait_limit_cycles();
+  p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.split = l.split; p.parts = l.parts; p.tickets = l.tickets;
   p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
   p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
@@ -1345,14 +1341,13 @@ bool tc_adapters_supported(const AdaptersCall& c) {
   return aligned16(c.dA) && aligned16(c.dB);
 }
 
-int tc_adapters_fwd(const AdaptersCall& c, char* ws, int above, cudaStream_t st) {
-  Layout l = ag_layout(c.k, c.T, false, forward_parts(c.Y.dtype), ws);
-  l.above = (uint32_t)above;
+int tc_adapters_fwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
+  const Layout l = ag_layout(c.k, c.T, false, forward_parts(c.Y.dtype), ws);
   int* status = reinterpret_cast<int*>(ws);
   AgPoolParams pool{};
-  pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = 1; pool.clear = above == 0;
+  pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = 1;
   pool.src[0] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
-  QB_TRY(ag_launch_pool(pool, l.rows, above > 0, st));
+  QB_TRY(ag_launch_pool(pool, l.rows, st));
   const ShrinkWork u{&l.x, &l.u, c.k.A, false, false};
   QB_TRY(ag_shrink(c, l, status, &u, 1, st));
   return ag_spread(c, l, status, l.u, c.k.B, c.k.Q, false, c.Y, c.k.l2, true, st);
@@ -1363,11 +1358,11 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   int* status = reinterpret_cast<int*>(ws);
   const bool grads = c.dA || c.dB;
   AgPoolParams pool{};
-  pool.c = c; pool.rows_there = l.rows; pool.above = l.above; pool.status = status; pool.sources = grads ? 2 : 1; pool.clear = 1;
+  pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = grads ? 2 : 1;
   pool.tickets = l.tickets; pool.n_tickets = grads ? l.n_tickets : 0;
   pool.src[0] = ag_source(c.Y, c.k.d_out, c.k.l2, false, l.dv);
   if (grads) pool.src[1] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
-  QB_TRY(ag_launch_pool(pool, l.rows, false, st));
+  QB_TRY(ag_launch_pool(pool, l.rows, st));
   ShrinkWork work[2];
   int sides = 0;
   if (c.dX.data || c.dA) work[sides++] = {&l.dv, &l.du, c.k.B, true, true};
