@@ -46,7 +46,7 @@ struct AgPool {
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
-struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; uint32_t* tickets; int n_tickets; };
+struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; uint32_t* tickets; int n_tickets, per, least, sms; };   // tickets: of grad
 
 // N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
 template <int N>
@@ -166,15 +166,67 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row
   }
 }
 
+// Parts begin at least this far apart in the plan: they have half of `least` rows, as filled up to a multiple of 16.
+__host__ __device__ inline int ag_apart(int least) { return least / 2 - 16; }
+// Rows above which an adapter is cut: the largest adapter in 1 to 16 parts, whichever takes the least time as counted in rows: rounds of the units
+// over the SMs, each the longest part and about 150 rows' time for its beginning and end, and 400 more where tiles go through memory.
+// One CTA of
+// the pooling kernel finds it beside the others: in front of the gradients it takes 7 us.  (4096 -> 4096, lambda 4, the whole backward pass without dX, us.  Rank 64: one adapter of 8192 rows whole 219, in 4 parts 109, 8 94, 16 102; six of
+// 1100 whole 77, cut in two 85.  Rank 256: one of 1800 67, in 4 parts 49; three of 600 46, cut in two 55.)
+__device__ int ag_split(const AdaptersCall& c, int per, int least, int sms) {
+  __shared__ int s_most, s_units[8], s_longest[8];
+  const int tid = threadIdx.x;
+  if (tid < 8) s_units[tid] = s_longest[tid] = 0;
+  if (tid == 0) s_most = 0;
+  __syncthreads();
+  auto rows_of = [&](int a) { return max(plan_start(c, a + 1) - plan_start(c, a), 0); };
+  int most = 0;
+  for (int a = tid; a < c.k.n; a += AG_POOL_THREADS) most = max(most, rows_of(a));
+  most = __reduce_max_sync(0xffffffffu, most);
+  if ((tid & 31) == 0) atomicMax(&s_most, most);
+  __syncthreads();
+  most = s_most;
+  auto cuts = [](int i) { return i < 4 ? i + 1 : i == 4 ? 6 : i == 5 ? 8 : i == 6 ? 12 : 16; };
+  auto rows_at = [&](int i) { return max((uint32_t)least, (((uint32_t)most + cuts(i) - 1) / cuts(i) + 31) & ~31u); };
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t limit = rows_at(i);
+    int units = 0, longest = 0;
+    for (int a = tid; a < c.k.n; a += AG_POOL_THREADS) {
+      const uint32_t rows = rows_of(a), parts = (rows + limit - 1) / limit;
+      units += parts;
+      if (parts) longest = max(longest, (int)(rows / parts));
+    }
+    units = __reduce_add_sync(0xffffffffu, units);
+    longest = __reduce_max_sync(0xffffffffu, longest);
+    if ((tid & 31) == 0) { atomicAdd(&s_units[i], units); atomicMax(&s_longest[i], longest); }
+  }
+  __syncthreads();
+  int best = 0;
+  long long lowest = 0;
+  for (int i = 0; i < 8; ++i) {
+    const long long rounds = ((long long)s_units[i] * per + sms - 1) / sms, cost = rounds * (s_longest[i] + 150) + (rows_at(i) < (uint32_t)most ? 400 : 0);
+    if (i == 0 || cost < lowest) { lowest = cost; best = i; }
+  }
+  return (int)rows_at(best);
+}
+
 __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __grid_constant__ AgPoolParams p) {
   extern __shared__ uint32_t ag_smem[];
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (blockIdx.x == 0 && threadIdx.x == 0) *p.status = QBLORA_OK;
-  for (int i = blockIdx.x * AG_POOL_THREADS + threadIdx.x; i < p.n_tickets; i += gridDim.x * AG_POOL_THREADS) p.tickets[i] = 0u;
+  const int extra = p.n_tickets > 0, block = (int)blockIdx.x - extra, blocks = (int)gridDim.x - extra;
+  if (block < 0) {
+    for (int i = threadIdx.x; i < p.n_tickets; i += AG_POOL_THREADS) p.tickets[i] = 0u;
+    const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, ag_split(p.c, p.per, p.least, p.sms));
+    uint32_t* out = p.tickets + p.n_tickets;
+    if (threadIdx.x == 0) out[0] = (uint32_t)g.kept;
+    for (int i = threadIdx.x; i < 2 * (p.c.k.n + 1); i += AG_POOL_THREADS) out[1 + i] = ag_smem[i];
+    return;
+  }
   const AgGroups g = ag_groups<AG_POOL_THREADS>(p.c, ag_smem, p.rows_there, 128);
   const int lane = threadIdx.x & 31, warps = AG_POOL_THREADS / 32;
   const uint32_t rows = g.pad[g.kept];
-  for (int64_t i = (int64_t)blockIdx.x * warps + (threadIdx.x >> 5); i < (int64_t)rows * p.sources; i += (int64_t)gridDim.x * warps) {
+  for (int64_t i = (int64_t)block * warps + (threadIdx.x >> 5); i < (int64_t)rows * p.sources; i += (int64_t)blocks * warps) {
     const int which = i >= rows ? 1 : 0;
     const uint32_t at = (uint32_t)(which ? i - rows : i);
     const int a = ag_find(g.pad, g.kept, at), j = plan_start(p.c, a) + (int)(at - g.pad[a]);
@@ -873,9 +925,10 @@ struct AgGrad {
   AdaptersCall c;
   uint32_t rows_there;
   AgGradSide side[2];                   // out == nullptr: not wanted
-  int split;                            // an adapter of more rows is cut into parts, of at least half as many
-  float* parts;                         // their tiles, [slot][tile][128 x 128], where a part's slot is its first row / (split / 2)
-  uint32_t* tickets;                    // [slot][tile]: parts that are there; zero before the call
+  int least;                            // an adapter of more rows than ag_split says is cut into parts; it says no less than this
+  float* parts;                         // their tiles, [slot][tile][128 x 128], where a part's slot is its first place in the plan / ag_apart(least)
+  uint32_t* tickets;                    // [slot][tile]: parts that are there; zero before the call.  Then its AgGroups: kept, pad, tile
+  int n_tickets;                        // 0: no adapter can be cut
   int* status;
   long long wait_limit;
 };
@@ -910,17 +963,24 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(tmem_slot), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const AgGroups g = ag_groups<AG_THREADS>(p.c, reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw)), p.rows_there, p.split);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem_base = *tmem_slot_g;
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
   const BankView& k = p.c.k;
   const AgGradSide &sa = p.side[0], &sb = p.side[1];
   const int ca = (sa.N + 127) / 128, cb = (sb.N + 127) / 128;
   const int ta = sa.out ? (sa.M + 127) / 128 * ca : 0, tb = sb.out ? (sb.M + 127) / 128 * cb : 0;
   const int per = ta + tb;
+  uint32_t* table = reinterpret_cast<uint32_t*>(smem_raw + (bars + AG_BARS - raw));
+  AgGroups g;
+  if (p.n_tickets == 0) g = ag_groups<AG_THREADS>(p.c, table, p.rows_there, 0x7fffffe0);
+  asm volatile("griddepcontrol.wait;" ::: "memory");     // what the kernels in front have written
+  if (p.n_tickets > 0) {
+    const uint32_t* from = p.tickets + p.n_tickets;
+    for (int i = tid; i < 2 * (k.n + 1); i += AG_THREADS) table[i] = from[1 + i];
+    g = {table, table + k.n + 1, (int)from[0]};
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot_g;
   // Units: the tiles of all parts, then those of all adapters, of which only those without rows have anything to do: zeros.
   const long long work = (long long)ag_uni((int)g.tile[g.kept]) * per, units = work + (long long)k.n * per;
   struct Unit { int a, side, m0, n0, n16, steps, rank, first, all, part, parts, tile; uint32_t at; bool skip; };
@@ -1058,7 +1118,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
       if (t.parts > 1 && t.steps > 0) {
         // This part's tile goes to memory; whoever comes last adds all of them up, in the parts' order
         const int etid = tid - 64;
-        auto slot = [&](int i) { return (int64_t)((t.first + part_at(t, i) * 16) / (p.split / 2)) * per + t.tile; };
+        auto slot = [&](int i) { return (int64_t)((plan_start(p.c, t.a) + part_at(t, i) * 16) / ag_apart(p.least)) * per + t.tile; };
         float4* mine = reinterpret_cast<float4*>(p.parts + slot(t.part) * 16384) + etid;
 #pragma unroll
         for (int j = 0; j < 16; ++j) mine[j * 256] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
@@ -1105,11 +1165,13 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
 // ---- host ------------------------------------------------------------------------------------------------------------------------
 struct Layout {
   Parts x, dv, u, du;
-  int split;                            // of the gradients: AgGrad
+  int least;                            // of the gradients: AgGrad
   float* parts; uint32_t* tickets; int n_tickets;
   size_t bytes; uint32_t rows;
 };
 
+// tiles of one adapter's dA and dB
+int64_t ag_tiles(const BankView& k) { return (int64_t)((k.P + 127) / 128 + (k.Q + 127) / 128) * ((k.r + 127) / 128); }
 // parts: of numbers that are no bf16 numbers
 Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* ws) {
   Layout l{};
@@ -1125,22 +1187,17 @@ Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* w
   };
   place(l.x, k.P, k.l1 > 1 ? parts : 1);
   place(l.u, k.r, parts);
-  l.split = 0x3ffffff0;
   if (backward) {
     place(l.dv, k.Q, k.l2 > 1 ? parts : 1);
     place(l.du, k.r, parts);
-    // Where one adapter's tiles do not fill the SMs twice, its rows are cut: into at most eight parts of all rows there are, and not below
-    // 512 rows, which the tiles' way through memory would cost.
-    const int64_t per = (int64_t)((k.P + 127) / 128 + (k.Q + 127) / 128) * ((k.r + 127) / 128), cuts = std::min<int64_t>(8, 296 / per);
-    if (cuts > 1) {
-      l.split = (int)std::max<int64_t>(512, (T / cuts + 31) / 32 * 32);
-      const int64_t slots = (int64_t)l.rows / (l.split / 2) + 1;
-      l.n_tickets = (int)(slots * per);
-      l.tickets = reinterpret_cast<uint32_t*>(ws + at);
-      at += align_up((size_t)l.n_tickets * 4, 256);
-      l.parts = reinterpret_cast<float*>(ws + at);
-      at += (size_t)l.n_tickets * 65536;
-    }
+    // parts of no fewer rows than would make two rounds over 148 SMs of one adapter's: that bounds their tiles' memory
+    const int64_t per = ag_tiles(k);
+    l.least = (int)std::min<int64_t>(std::max<int64_t>(256, (T * per / 296 + 31) / 32 * 32), 0x3fffffe0);
+    l.n_tickets = T > l.least ? (int)(((T + 15) / ag_apart(l.least) + 1) * per) : 0;
+    l.tickets = reinterpret_cast<uint32_t*>(ws + at);
+    at += align_up(((size_t)l.n_tickets + 1) * 4 + ag_table_bytes(k.n), 256);
+    l.parts = reinterpret_cast<float*>(ws + at);
+    at += (size_t)l.n_tickets * 65536;
   }
   l.bytes = align_up(at, 256);
   return l;
@@ -1195,11 +1252,13 @@ int ag_launch_pool(const AgPoolParams& p, int64_t rows, cudaStream_t st) {
   if (rc) return rc;
   const int64_t want = (rows * p.sources + AG_POOL_THREADS / 32 - 1) / (AG_POOL_THREADS / 32);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)std::min<int64_t>(want, 8LL * sms));
+  AgPoolParams q = p;
+  q.sms = sms;
+  cfg.gridDim = dim3((unsigned)std::min<int64_t>(want, 8LL * sms) + (p.n_tickets > 0));
   cfg.blockDim = dim3(AG_POOL_THREADS);
   cfg.dynamicSmemBytes = ag_table_bytes(p.c.k.n);
   cfg.stream = st;
-  QB_CUDA(cudaLaunchKernelEx(&cfg, adapters_pool_kernel, p));
+  QB_CUDA(cudaLaunchKernelEx(&cfg, adapters_pool_kernel, q));
   count_launch();
   return QBLORA_OK;
 }
@@ -1310,15 +1369,14 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   AgGradMaps maps{};
   AgGrad p{};
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
-  p.split = l.split; p.parts = l.parts; p.tickets = l.tickets;
+  p.least = l.least; p.parts = l.parts; p.tickets = l.tickets; p.n_tickets = l.n_tickets;
   p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
   p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
   QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 32));
   QB_TRY(parts_map(&maps.b[0], l.du, l.rows, 32));
   QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 32));
   QB_TRY(parts_map(&maps.b[1], l.dv, l.rows, 32));
-  const int64_t per = (int64_t)((c.k.P + 127) / 128 + (c.k.Q + 127) / 128) * ((c.k.r + 127) / 128);
-  const int64_t most = per * (c.k.n + (int64_t)l.rows / (l.split / 2) + 1);
+  const int64_t per = ag_tiles(c.k), most = per * (2 * c.k.n + 2 * (int64_t)c.T / l.least);
   return ag_launch(adapters_grad_kernel, ready, maps, p, AG_THREADS, AR_STAGES * AR_STAGE + AG_BARS + ag_table_bytes(c.k.n), most, st);
 }
 
@@ -1360,6 +1418,8 @@ int tc_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
   AgPoolParams pool{};
   pool.c = c; pool.rows_there = l.rows; pool.status = status; pool.sources = grads ? 2 : 1;
   pool.tickets = l.tickets; pool.n_tickets = grads ? l.n_tickets : 0;
+  pool.per = (int)ag_tiles(c.k);      // (also where one of the two is wanted: the same sums)
+  pool.least = l.least;
   pool.src[0] = ag_source(c.Y, c.k.d_out, c.k.l2, false, l.dv);
   if (grads) pool.src[1] = ag_source(c.X, c.k.d_in, c.k.l1, true, l.x);
   QB_TRY(ag_launch_pool(pool, l.rows, st));
