@@ -1,10 +1,12 @@
 // AdamW over many tensors at once, states in 32 bits or in 8, with the global gradient norm and clipping
 // (qblora_adamw_prepare, qblora_adamw_step; the formulas stand in include/qblora.h).
 //
-// What bounds it: memory.  An element moves 30 bytes with states in 32 bits (p, m, v in and out, g in, the bf16 copy out) and
-// 16 to 18 with states in 8.  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane:
+// What bounds it: memory with states in 32 bits, 30 bytes an element (p, m, v in and out, g in, the bf16 copy out): 125 M elements in
+// 607 us, 6.2 TB/s.  With states in 8 bits, 16 to 18 bytes an element, the instructions (640 for a warp's 256 elements, 2.3 a cycle): 480 us, and
+// 68 for the norm's pass over bf16 gradients; more bytes on their way, by more CTAs an SM or asynchronous copies, changed nothing (488 to 653).  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane:
 // a scale's block lies within a warp, so its maximum is five shuffles and no element is read twice.  The tensors are a table in the
-// workspace; a warp finds its block's tensor by a search over the first blocks, which 24 warps per SM hide.  Lane l holds elements
+// workspace; a warp takes runs of neighbouring blocks and searches the first blocks for their tensor where the last one's does not
+// fit.  Lane l holds elements
 // 4 l .. 4 l + 3 and 128 + 4 l .. of the block, so every load and store of a warp is one contiguous run.
 //
 // One launch without the norm, two with it: the step's count is read by every CTA as it starts and written by the CTA that
@@ -388,7 +390,9 @@ __device__ __forceinline__ void aw_each(const AwView& w, uint32_t blocks, uint32
 __device__ __forceinline__ bool aw_full(const AwTensor& t, uint32_t b) {
   return t.wide && (long long)(b - t.first + 1) * AW_BLOCK <= t.n;
 }
-// Neighbouring blocks per warp and turn: `most` where every warp has some turns of them, else fewer, so that all SMs have work.
+// Neighbouring blocks per warp and turn: `most` where every warp has some turns of them, else fewer, so that all SMs have work.  (125 M elements.  States in
+// 32 bits, runs of 1, 2, 4, 8: 609, 606, 607, 620 us.  In 8 bits, 4 and 8: 565 and 552, with 16 to a run of the norm; the norm's of 4, 16, 64: 595, 565,
+// 572, single blocks throughout 750.  One turn or 16 in place of four: 565 and 576.)
 __device__ __forceinline__ uint32_t aw_run(uint32_t blocks, uint32_t most) {
   return min(most, max(1u, blocks / (gridDim.x * AW_WARPS * 4)));
 }
@@ -410,7 +414,7 @@ __global__ void __launch_bounds__(AW_THREADS, 3) adamw_kernel(const __grid_const
     now.up2 = sqrtf(__fdiv_rn(1.0f, -expm1f((float)(t * s.log_b2))));
     now.lr = *s.lr;
     now.key = aw_mix(aw_mix(s.seed) + (uint32_t)(taken + 1));
-    aw_each(w, blocks, aw_run(blocks, 4), [&](const AwTensor& t, uint32_t b, uint32_t n) {
+    aw_each(w, blocks, aw_run(blocks, BITS == 8 ? 8 : 4), [&](const AwTensor& t, uint32_t b, uint32_t n) {
       uint32_t i = 0;
       if (BITS == 8) {                         // few bytes to a block: the loads of two on their way at once
         for (; i + 2 <= n && aw_full(t, b + i + 1); i += 2) {

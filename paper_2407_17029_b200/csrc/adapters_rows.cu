@@ -1,14 +1,15 @@
 // Many adapters over one weight, forward, few rows per adapter (decoding): one launch.
 //
-// An item is up to 16 rows of one adapter and belongs to a cluster of 1 to 8 CTAs.  Each CTA pools its part of the rows' input and
+// An item is up to 8 rows of one adapter and belongs to a cluster of 1 to 8 CTAs.  Each CTA pools its part of the rows' input and
 // forms its part of the sum u = x' A; the parts are added over the cluster's shared memory; then each CTA has all of u and takes its
 // share of the outputs, Y += s repeat(u B).
 //
-// What bounds it: with an adapter per request the adapters' bytes, with few requests latency.  A and B are read once per item,
-// straight from memory into the fragments of mma.sync.m16n8k16, whose 16 rows are ranks (outputs) and whose 8 columns are tokens:
-// the memory's rows run along the ranks, so a lane takes 16 bytes (8 ranks) of four rows of the contraction, and one byte permutation per
-// register makes the pairs that the MMA wants of them; which ranks make up the 16 rows of a tile is free.  No shared memory, no
-// barrier lies on that way.  x' and u are two bf16 parts (three where Y is fp32), as in tc_adapters.cu.
+// What bounds it: with an adapter per request the adapters' bytes (200 requests of as many adapters, 5120 -> 5120, rank 256: 262 MB in
+// 49 us, 5.4 TB/s), with few requests latency (one token, 4096 -> 4096: 8 us: the plan, the rows, x', the sums over the cluster, one after another).
+// A and B are read once per item.  Each warp has a ring of its own, steps of 16 by 64 weights brought by asynchronous copies, so no
+// barrier lies on that way; loads straight into registers came to 3.7 TB/s, as a warp cannot wait for the older of two loads alone.  The products are
+// mma.sync.m16n8k16, 16 ranks (outputs) by 8 tokens: a tile of 128 ranks on the other path's tensor memory would want a tile of 16 tokens and a
+// kernel to itself for each product (200 of 200: 2.5 times as long).  x' and u are two bf16 parts (three where Y is fp32), as in tc_adapters.cu.
 #include <algorithm>
 #include <atomic>
 
@@ -25,7 +26,7 @@ constexpr int NR_CHUNK = 512;                     // of the pooled input in shar
 constexpr int NR_MAX_RANK = 512;
 constexpr int NR_STEP = 2048;                     // bytes of a step's weights: 16 of the contraction by 64 ranks (outputs)
 constexpr int NR_PART = NR_WARPS * NR_ROWS * (64 + 4) * 4;
-// steps of a warp whose weights are on their way
+// steps of a warp whose weights are on their way: with four, two CTAs share an SM
 template <int NP> constexpr int NR_AHEAD = NP == 3 ? 6 : 4;
 
 struct NrParams {
@@ -270,7 +271,8 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
   const __nv_bfloat16* B = k.B + (int64_t)a * k.r * k.Q;
   const int q_blocks = (k.Q + 63) / 64, own = rank < q_blocks ? (q_blocks - rank + cs - 1) / cs : 0;
   const int steps2 = r16 / 16;
-  // kw warps share a block's contraction: as many as give the fewest rounds of steps, with two more a round for its end
+  // kw warps share a block's contraction: as many as give the fewest rounds of steps, with two more a round for its end (20 blocks of 16 steps:
+  // one warp each takes three rounds of 16, two warps each five of 8)
   int kw = 1, best = 0x7fffffff;
   for (int t = 1; t <= NR_WARPS; t *= 2) {
     const int cost = (own * t + NR_WARPS - 1) / NR_WARPS * ((steps2 + t - 1) / t + 2);
