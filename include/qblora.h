@@ -507,7 +507,7 @@ int qblora_adapter_plan(const int32_t* cu, const int32_t* ids, int32_t n_request
  *   X and Y do not overlap.  x' and x' A are carried as sums of bf16 numbers: two where Y is bf16, within 2^-16, three where
  *   it is fp32 (and throughout the backward pass), within 2^-24.
  * Any sizes; rank and Q multiples of 8, d_in, d_out and the strides multiples of 8 and all tensors 16-byte
- * aligned take the fast kernels, up to the rank whose x' A of 16 rows fits in shared memory beside a weight tile (about 1000).
+ * aligned take the fast kernels, up to the rank whose x' A of 16 rows fits in shared memory beside a weight tile (1024 at least).
  *   ws: qblora_adapters_workspace_bytes(bank, tokens, 0) bytes.
  */
 size_t qblora_adapters_workspace_bytes(const qblora_adapter_bank* bank, int64_t tokens, int backward);

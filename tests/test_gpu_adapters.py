@@ -387,3 +387,54 @@ def test_gradients_of_many_rows(qb, size, lens, ids):
     other = qb.adapters_bwd(bank, qb.adapter_plan(cu2, di2, n, T), X, dY, ws=ws)
     if ids.count(ids[0]) == 1:
         assert torch.equal(other[1][ids[0]], dA[ids[0]]) and torch.equal(other[2][ids[0]], dB[ids[0]])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("size,n,rows", [((5200, 2112, 4, 4, 136), 60, 1), ((5200, 2112, 4, 4, 136), 200, 1), ((1024, 4160, 1, 1, 512), 40, 3),
+                                         ((2080, 1040, 5, 2, 40), 150, 2), ((8192, 640, 64, 1, 256), 16, 16), ((64, 64, 1, 1, 8), 4096, 0),
+                                         ((128, 192, 2, 2, 16), 300, 4)],
+                         ids=["60 of one", "200 of one", "rank 512", "lambda 5", "16 of 16", "4096 adapters", "300 of four"])
+def test_forward_of_many_adapters(qb, size, n, rows, dtype):
+    # as many adapters as make the clusters small, some left out, ranks of all kinds; both sides of the number of rows that changes the path
+    r = random.Random(n)
+    ids = r.sample(range(n), min(n, 250))
+    lens = [rows + b % 3 if rows else 1 + b % 2 for b in range(len(ids))]
+    bank = ra.make_bank(qb, n, *size, ranks=[r.choice([size[4], size[4], size[4] // 2 + 1, 1, 0]) for _ in range(n)], seed=n)
+    cu, di, T = ra.requests(lens, ids)
+    for T in (T, max(T, 520)):
+        X, Y0 = _randn(1, T, size[0]), _randn(2, T, size[1], dtype=dtype)
+        Y = qb.adapters_fwd(bank, qb.adapter_plan(cu, di, n, T), X, Y0.clone())
+        want, bound = ra.ref_fwd(bank, cu.tolist(), ids, X, Y0)
+        ra.check(Y, want, bound, 2, size[0] + size[4], ("Y", dtype), Y0)
+        assert torch.equal(Y[int(cu[-1]):], Y0[int(cu[-1]):])
+
+
+def test_backward_of_many_adapters(qb):
+    n, size = 4096, (64, 64, 1, 1, 8)
+    r = random.Random(3)
+    ids = [r.randrange(n) for _ in range(500)]
+    lens = [r.choice([0, 1, 1, 2, 9]) for _ in ids]
+    bank = ra.make_bank(qb, n, *size, seed=5)
+    cu, di, T = ra.requests(lens, ids)
+    X, dY, dX0 = _randn(3, T, 64), _randn(4, T, 64), _randn(5, T, 64, dtype=torch.float32)
+    dX, dA, dB = qb.adapters_bwd(bank, qb.adapter_plan(cu, di, n, T), X, dY, dX0.clone())
+    want, bound = ra.ref_bwd(bank, cu.tolist(), ids, X, dY, dX0)
+    for got, w, b, name, base in zip((dX, dA, dB), want, bound, ("dX", "dA", "dB"), (dX0, None, None)):
+        ra.check(got, w, b, 4, 128 + T, (name, torch.float32), base)
+
+
+@pytest.mark.parametrize("rank", [504, 520, 1024, 1400, 1416, 2000])
+def test_large_ranks(qb, rank):
+    # both sides of what the kernels' shared memory holds
+    size, n = (256, 192, 2, 4, rank), 3
+    bank = ra.make_bank(qb, n, *size, ranks=[rank, 5, rank - 9], seed=rank)
+    cu, di, T = ra.requests([20, 3, 1, 30], [0, 1, -1, 2])
+    X, Y0, dY, dX0 = _randn(1, T, 256), _randn(2, T, 192, dtype=torch.float32), _randn(3, T, 192), _randn(4, T, 256)
+    plan = qb.adapter_plan(cu, di, n, T)
+    want, bound = ra.ref_fwd(bank, cu.tolist(), [0, 1, -1, 2], X, Y0)
+    ra.check(qb.adapters_fwd(bank, plan, X, Y0.clone()), want, bound, 2, 256 + rank, ("Y", torch.float32), Y0)
+    want, bound = ra.ref_bwd(bank, cu.tolist(), [0, 1, -1, 2], X, dY, dX0)
+    dX, dA, dB = qb.adapters_bwd(bank, plan, X, dY, dX0.clone())
+    ra.check(dX, want[0], bound[0], 2, 192 + rank, ("dX", torch.bfloat16), dX0)
+    ra.check(dA, want[1], bound[1], 4, 320 + T, ("dA", torch.float32))
+    ra.check(dB, want[2], bound[2], 4, 448 + T, ("dB", torch.float32))
