@@ -720,11 +720,12 @@ def adapter_plan(cu_rows: torch.Tensor, adapter_ids: torch.Tensor, n_adapters: i
 
 def _rows(t: torch.Tensor, tokens: int, width: int, name: str, dtypes=(torch.bfloat16,)) -> int:
     """Checks a [tokens][width] tensor with contiguous rows; returns its row stride."""
-    if t.dim() != 2 or t.shape[0] != tokens or t.shape[1] != width or not t.is_cuda or t.dtype not in dtypes:
+    if tuple(t.shape) != (tokens, width) or not t.is_cuda or t.dtype not in dtypes:
         raise ValueError(f"{name}: [{tokens}][{width}] device tensor of {' or '.join(str(d) for d in dtypes)}")
-    if (t.stride(1) != 1 and width > 1) or (t.stride(0) < width and tokens > 1):
+    step, one = t.stride()
+    if (one != 1 and width > 1) or (step < width and tokens > 1):
         raise ValueError(f"{name}: rows are contiguous and do not overlap")
-    return max(t.stride(0), width)
+    return step if step > width else width
 
 
 def adapters_workspace_bytes(bank: AdapterBank, tokens: int, backward: bool = False) -> int:

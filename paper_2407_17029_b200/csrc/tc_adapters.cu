@@ -240,8 +240,8 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
 }
 
 // ---- shrink -------------------------------------------------------------------------------------------------------------------
-// What bounds it: the operands' way from L2 (6.6 TB/s; 1800 rows, contraction 1024, rank 256, both sides: 80 MB in 19 us with 7 of beginning and
-// end, as for every kernel of the chain).
+// What bounds it: the operands' way into shared memory, about 40 bytes a cycle of each SM however many there are (a step of 64 of the
+// contraction: 24 KB 0.39 us, 32 KB 0.44), and 7 us of beginning and end.  1800 rows, contraction 1024, rank 256, both sides: 19 us.
 struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the rows' parts in boxes of tn rows and of 16
 // u = x' A, du = s dv B^T, or both side by side.
 struct AgShrinkSide {
@@ -348,6 +348,20 @@ __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
   for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
 }
 
+// The same, with the parts one behind the other (and a third apart, if not 0, whose sums go to the second's): the weights are read once for
+// all of them (contraction 4096, 1800 rows, three parts: 39.5 -> 35.6 us).
+template <bool KMAJOR>
+__device__ __forceinline__ void ag_issue_together(uint32_t d, uint32_t d1, uint64_t a, uint64_t b, uint64_t third, uint32_t idesc, uint32_t idesc1, int n,
+                                                  uint32_t fresh) {
+  constexpr uint64_t STEP = KMAJOR ? AG_STEP_K : AG_STEP_T;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (e >= n) break;
+    tc_mma(d, a + e * STEP, b + e * AG_STEP_K, idesc, e ? 1u : fresh ^ 1u);
+    if (third) tc_mma(d1, a + e * STEP, b + third + e * AG_STEP_K, idesc1, 1u);
+  }
+}
+
 __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __grid_constant__ AgShrinkMaps maps, const __grid_constant__ AgShrink p) {
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw), base = (raw + 1023u) & ~1023u;
@@ -405,7 +419,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         if (leader) {
           mbar_arrive_expect_tx(full(s), AG_TILE + (uint32_t)np * t.n16 * 128);
           ag_load_weights(maps.side[side], w, full(s), kmajor, k * 16, m0, t.a);
-          for (int i = 0; i < np; ++i) ag_load_rows(maps.side[side], w + AG_TILE + i * p.tn * 128, full(s), k * 16, t, p.tn, i);
+          for (int i = 0; i < np; ++i) ag_load_rows(maps.side[side], w + AG_TILE + i * t.n16 * 128, full(s), k * 16, t, p.tn, i);
         }
         __syncwarp();
         if (++s == p.stages) { s = 0; ph ^= 1u; }
@@ -424,7 +438,9 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       if (!unit(u)) continue;
       const int np = p.side[side].np, kmajor = p.side[side].w_kmajor;
-      const uint32_t idesc = ag_idesc(!kmajor, false, t.n16);
+      // the parts lie one behind the other: one MMA takes them all as its columns, or the first two where three are too many
+      const int together = np * t.n16 <= 256 ? np : 2;
+      const uint32_t idesc = ag_idesc(!kmajor, false, together * t.n16), idesc1 = ag_idesc(!kmajor, false, t.n16);
       int left = 0, b = 0;                                 // blocks left of the segment; its accumulator
       for (int k = 0; k < steps; k += 4) {
         const bool fresh = left == 0;
@@ -440,10 +456,10 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         const uint32_t w = ring + s * stage_bytes, d = tmem + b * 256;
         const bool last = --left == 0 || k + 4 >= steps;
         if (leader) {
-          const uint64_t rows = ag_desc(w + AG_TILE, false), part = (uint64_t)(p.tn * 128) >> 4;
+          const uint64_t rows = ag_desc(w + AG_TILE, false), third = together < np ? (uint64_t)(2 * t.n16 * 128) >> 4 : 0;
           const int n = min(4, steps - k);
-          if (kmajor) ag_issue_parts<true>(np, d, d + 128, ag_desc(w, false), rows, part, idesc, n, fresh);
-          else ag_issue_parts<false>(np, d, d + 128, ag_desc(w, true), rows, part, idesc, n, fresh);
+          if (kmajor) ag_issue_together<true>(d, d + t.n16, ag_desc(w, false), rows, third, idesc, idesc1, n, fresh);
+          else ag_issue_together<false>(d, d + t.n16, ag_desc(w, true), rows, third, idesc, idesc1, n, fresh);
           tc_commit(empty(s));
           if (last) tc_commit(accfull(b));
         }
@@ -459,6 +475,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
     for (long long u = blockIdx.x; u < units && ok; u += gridDim.x) {
       if (!unit(u)) continue;
       const AgShrinkSide& sd = p.side[side];
+      const int together = sd.np * t.n16 <= 256 ? sd.np : 2;
       float v[64];
 #pragma unroll
       for (int j = 0; j < 64; ++j) v[j] = 0.f;
@@ -471,8 +488,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
 #pragma unroll
         for (int c = 0; c < 64; c += 32) {
           if (half * 64 + c >= t.n16) break;
-          ag_gather(d + c, v + c);
-          if (sd.np > 1) ag_gather(d + 128 + c, v + c);
+          for (int i = 0; i < together; ++i) ag_gather(d + i * t.n16 + c, v + c);
         }
         tc_fence_before();
         __syncwarp();
