@@ -350,15 +350,22 @@ __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
 
 // The same, with the parts one behind the other (and a third apart, if not 0, whose sums go to the second's): the weights are read once for
 // all of them (contraction 4096, 1800 rows, three parts: 39.5 -> 35.6 us).
-template <bool KMAJOR>
+template <bool KMAJOR, bool THIRD>
 __device__ __forceinline__ void ag_issue_together(uint32_t d, uint32_t d1, uint64_t a, uint64_t b, uint64_t third, uint32_t idesc, uint32_t idesc1, int n,
                                                   uint32_t fresh) {
   constexpr uint64_t STEP = KMAJOR ? AG_STEP_K : AG_STEP_T;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (e >= n) break;
-    tc_mma(d, a + e * STEP, b + e * AG_STEP_K, idesc, e ? 1u : fresh ^ 1u);
-    if (third) tc_mma(d1, a + e * STEP, b + third + e * AG_STEP_K, idesc1, 1u);
+  const uint64_t b2 = b + third;
+  auto step = [&](uint64_t x, uint64_t y, uint32_t acc) {
+    tc_mma(d, a + x, b + y, idesc, acc);
+    if constexpr (THIRD) tc_mma(d1, a + x, b2 + y, idesc1, 1u);
+  };
+  step(0, 0, fresh ^ 1u);
+  if (n == 4) {
+    step(STEP, AG_STEP_K, 1u);
+    step(2 * STEP, 2 * AG_STEP_K, 1u);
+    step(3 * STEP, 3 * AG_STEP_K, 1u);
+  } else {
+    for (int e = 1; e < n; ++e) step(e * STEP, e * AG_STEP_K, 1u);
   }
 }
 
@@ -458,8 +465,11 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         if (leader) {
           const uint64_t rows = ag_desc(w + AG_TILE, false), third = together < np ? (uint64_t)(2 * t.n16 * 128) >> 4 : 0;
           const int n = min(4, steps - k);
-          if (kmajor) ag_issue_together<true>(d, d + t.n16, ag_desc(w, false), rows, third, idesc, idesc1, n, fresh);
-          else ag_issue_together<false>(d, d + t.n16, ag_desc(w, true), rows, third, idesc, idesc1, n, fresh);
+          const uint64_t dk = ag_desc(w, !kmajor);
+          if (third && kmajor) ag_issue_together<true, true>(d, d + t.n16, dk, rows, third, idesc, idesc1, n, fresh);
+          else if (third) ag_issue_together<false, true>(d, d + t.n16, dk, rows, third, idesc, idesc1, n, fresh);
+          else if (kmajor) ag_issue_together<true, false>(d, d, dk, rows, 0, idesc, idesc, n, fresh);
+          else ag_issue_together<false, false>(d, d, dk, rows, 0, idesc, idesc, n, fresh);
           tc_commit(empty(s));
           if (last) tc_commit(accfull(b));
         }
@@ -1311,14 +1321,23 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
   AgShrink p{};
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.m_tiles = (c.k.r + 127) / 128; p.sides = sides;
-  // smaller tiles where large ones would leave SMs without any
-  p.tn = 128;
-  while (p.tn > 32 && (int64_t)c.T * p.m_tiles * sides / p.tn < 100) p.tn /= 2;
+  for (int i = 0; i < sides; ++i) p.np = std::max(p.np, work[i].in->np);
+  // Rows of a tile: what takes the least time as counted in rows of 128 bytes: rounds of the units over the SMs, each its steps' operands and
+  // about 1280 for beginning and end.  (Backward pass without dX, us, tiles of 128 / 64 / 32: 4096 -> 4096, rank 64, lambda 4, 20 adapters of 300 rows
+  // 75 / 82 / 87, three of 600 - / 41 / 39; lambda 1, six of 1100 123 / 145 / 161.)
+  int sms = 0;
+  QB_TRY(ag_sms(&sms));
+  int64_t least = -1, blocks = 0;
+  for (int i = 0; i < sides; ++i) blocks = std::max<int64_t>(blocks, (work[i].in->width + 63) / 64);
+  for (int tn = 128; tn >= 32; tn /= 2) {
+    const int64_t tiles = c.T / tn + 1, units = (tiles + std::min<int64_t>(c.k.n, tiles) / 2) * p.m_tiles * sides;
+    const int64_t cost = (units + sms - 1) / sms * ((128 + p.np * tn) * blocks + 1280);
+    if (least < 0 || cost < least) { least = cost; p.tn = tn; }
+  }
   for (int i = 0; i < sides; ++i) {
     const ShrinkWork& w = work[i];
     const Parts& in = *w.in;
     p.side[i] = {in.np, in.width, w.kmajor, w.scaled, *w.out};
-    p.np = std::max(p.np, in.np);
     p.segment = w.out->np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
     QB_TRY(parts_map(&maps.side[i].rows, in, l.rows, p.tn));
     QB_TRY(parts_map(&maps.side[i].rows16, in, l.rows, 16));
