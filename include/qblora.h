@@ -519,7 +519,7 @@ int qblora_adapters_fwd(const qblora_adapter_bank* bank, const int32_t* rows, co
  * Its backward pass.  With dv_t = scaling[a] * (sums of lambda_out neighbours of dY_t), du_t = dv_t B_a^T, u_t = x'_t A_a:
  *   dX[t][i] += (du_t A_a^T)[i / lambda_in] / lambda_in        (on what the shared projection's backward pass has written)
  *   dA[a] = sum over its rows of x'_t^T du_t,   dB[a] = sum of u_t^T dv_t      (fp32 [n][P][rank], [n][rank][Q])
- * dA and dB are written whole: zeros for adapters without rows, and from ranks[a] (rounded up to 16) on.  Rows of dX that are
+ * dA and dB do not overlap and are written whole: zeros for adapters without rows, and from ranks[a] (rounded up to 16) on.  Rows of dX that are
  * not in the plan are left as they were.  Any of dX, dA, dB may be NULL (skipped).
  *   dY DEVICE bf16, dX DEVICE bf16 or fp32 (dx_dtype); strides in elements.  X is not needed (may be NULL) without dA and dB.
  *   ws: qblora_adapters_workspace_bytes(bank, tokens, 1) bytes.  Sums run in a fixed order: equal inputs, equal bits.

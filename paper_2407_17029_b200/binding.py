@@ -746,7 +746,7 @@ def _workspace(ws: torch.Tensor) -> torch.Tensor:
 def adapters_fwd(bank: AdapterBank, plan: AdapterPlan, X: torch.Tensor, Y: torch.Tensor, ws: Optional[torch.Tensor] = None,
                  stream=None) -> torch.Tensor:
     """qblora_adapters_fwd: adds every planned row's adapter term to Y [tokens][d_out] (bf16 or fp32, what the shared
-    projection of X has written) in place; returns Y."""
+    projection of X has written) in place; returns Y.  X and Y have the `tokens` rows that the plan was made for."""
     T = X.shape[0]
     xs = _rows(X, T, bank.d_in, "X")
     ys = _rows(Y, T, bank.d_out, "Y", (torch.bfloat16, torch.float32))

@@ -108,6 +108,8 @@ int qblora_adapters_bwd(const qblora_adapter_bank* bank, const int32_t* rows, co
   if (dX && (!rows_ok(dX, dx_stride, bank->d_in, dx_dtype, &c.dX) || dX == X || dX == dY)) return QBLORA_ERR_INVALID_ARG;
   if ((dA && !int_ptr_ok(dA)) || (dB && !int_ptr_ok(dB)) || (dA && dA == dB)) return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adapters_workspace_bytes(bank, tokens, 1)) return QBLORA_ERR_WORKSPACE;
+  const size_t slots = (size_t)c.k.n * c.k.r * 4;
+  if (dA && dB && overlap(dA, slots * c.k.P, dB, slots * c.k.Q)) return QBLORA_ERR_INVALID_ARG;
   if (!dX && !dA && !dB) return QBLORA_OK;
   c.dA = dA; c.dB = dB;
   if (!force_general() && tc_adapters_supported(c)) return tc_adapters_bwd(c, static_cast<char*>(ws), static_cast<cudaStream_t>(stream));

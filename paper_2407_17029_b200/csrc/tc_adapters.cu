@@ -1225,11 +1225,15 @@ Layout ag_layout(const BankView& k, int64_t T, bool backward, int parts, char* w
     // parts of no fewer rows than would make two rounds over 148 SMs of one adapter's: that bounds their tiles' memory
     const int64_t per = ag_tiles(k);
     l.least = (int)std::min<int64_t>(std::max<int64_t>(256, (T * per / 296 + 31) / 32 * 32), 0x3fffffe0);
-    l.n_tickets = T > l.least ? (int)(((T + 15) / ag_apart(l.least) + 1) * per) : 0;
+    // Room for tickets and tiles must not shrink as T grows, since a workspace serves fewer rows too: it is a bound on what follows, (T + 15) /
+    // ag_apart + 1 parts, with ag_apart >= 7/16 least and least >= T per / 296.
+    const int64_t room = T <= 256 || per >= 296 ? 0 : std::min<int64_t>(((T + 15) / ag_apart(256) + 1) * per, 720 + per);
+    const int64_t want = T > l.least ? ((T + 15) / ag_apart(l.least) + 1) * per : 0;
+    l.n_tickets = want <= room ? (int)want : 0;
     l.tickets = reinterpret_cast<uint32_t*>(ws + at);
-    at += align_up(((size_t)l.n_tickets + 1) * 4 + ag_table_bytes(k.n), 256);
+    at += align_up(((size_t)room + 1) * 4 + ag_table_bytes(k.n), 256);
     l.parts = reinterpret_cast<float*>(ws + at);
-    at += (size_t)l.n_tickets * 65536;
+    at += (size_t)room * 65536;
   }
   l.bytes = align_up(at, 256);
   return l;

@@ -126,3 +126,18 @@ def test_adamw_refuses_on_the_host(qb):
                dict(beta1=-0.1), dict(beta2=float("nan")), dict(eps=-1.0), dict(eps=inf), dict(max_norm=-1.0), dict(max_norm=inf)):
         assert step(**kw) == qb.ERR_INVALID_ARG, kw
     assert step(ws=None) == qb.ERR_WORKSPACE and step(size=16) == qb.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_a_workspace_for_more_rows_serves_fewer(qb, backward):
+    # alloc_adapters_workspace(bank, tokens) promises "up to `tokens` rows": the size never falls as the rows grow
+    for P, Q, rank, n in ((1000, 32, 128, 50), (1024, 1024, 256, 3), (216, 640, 256, 6), (4096, 2752, 64, 1), (16, 8, 8, 4096), (4096, 4096, 1024, 2), (7, 9, 5, 3)):
+        bank = qb._CAdapterBank(2 * P, 4 * Q, 2, 4, n, rank, None, None, None, None)
+        sizes = [qb._lib.qblora_adapters_workspace_bytes(ctypes.byref(bank), T, backward) for T in list(range(1, 1500)) + list(range(1500, 40000, 97))]
+        assert all(s > 0 for s in sizes) and sizes == sorted(sizes)
+
+
+def test_gradients_that_overlap_are_refused(qb):
+    # dA: 3 x 64 x 16, dB: 3 x 16 x 64 numbers of four bytes
+    for dA, dB in ((0x60000, 0x60000), (0x60000, 0x60000 + 3 * 64 * 16 * 4 - 4), (0x60000 + 4, 0x60000)):
+        assert _bwd(qb, _bank(qb), dA=dA, dB=dB) == qb.ERR_INVALID_ARG

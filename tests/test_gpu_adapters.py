@@ -438,3 +438,25 @@ def test_large_ranks(qb, rank):
     ra.check(dX, want[0], bound[0], 2, 192 + rank, ("dX", torch.bfloat16), dX0)
     ra.check(dA, want[1], bound[1], 4, 320 + T, ("dA", torch.float32))
     ra.check(dB, want[2], bound[2], 4, 448 + T, ("dB", torch.float32))
+
+
+def test_gradients_side_by_side_in_one_buffer_and_a_large_workspace(qb):
+    bank, cu, ids, plan, T = _case(qb, (512, 256, 4, 4, 64), "wide", 31)
+    X, dY = _randn(1, T, 512), _randn(2, T, 256)
+    ws = qb.alloc_adapters_workspace(bank, 5000, backward=True)      # for more rows than there are
+    both = torch.full((bank.A.numel() + bank.B.numel() + 2,), 7.0, device=DEV)
+    dA, dB = both[1:1 + bank.A.numel()].view(bank.A.shape), both[1 + bank.A.numel():-1].view(bank.B.shape)
+    qb.adapters_bwd(bank, plan, X, dY, outs=(dA, dB), ws=ws)         # (one element further than 16 bytes: the general path)
+    want, bound = ra.ref_bwd(bank, cu, ids, X, dY, torch.zeros(T, 512, device=DEV))
+    ra.check(dA, want[1], bound[1], 4, 384 + T, ("dA", torch.float32))
+    ra.check(dB, want[2], bound[2], 4, 576 + T, ("dB", torch.float32))
+    assert both[0] == 7 and both[-1] == 7
+    with pytest.raises(qb.QbloraError) as e:
+        qb.adapters_bwd(bank, plan, X, dY, outs=(dA, both[5:5 + bank.B.numel()].view(bank.B.shape)), ws=ws)
+    assert e.value.status == qb.ERR_INVALID_ARG
+    # the fast path: the same buffer for gradients on 16 bytes, and the same workspace for fewer rows
+    dA, dB = both[:bank.A.numel()].view(bank.A.shape), both[bank.A.numel():-2].view(bank.B.shape)
+    qb.adapters_bwd(bank, plan, X, dY, outs=(dA, dB), ws=ws)
+    ra.check(dA, want[1], bound[1], 4, 384 + T, ("dA", torch.float32))
+    ra.check(dB, want[2], bound[2], 4, 576 + T, ("dB", torch.float32))
+    assert both[-1] == 7
