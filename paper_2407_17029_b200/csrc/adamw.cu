@@ -1,13 +1,13 @@
 // AdamW over many tensors at once, states in 32 bits or in 8, with the global gradient norm and clipping
 // (qblora_adamw_prepare, qblora_adamw_step; the formulas stand in include/qblora.h).
 //
-// What bounds it: memory with states in 32 bits, 30 bytes an element (p, m, v in and out, g in, the bf16 copy out): 125 M elements in
-// 607 us, 6.2 TB/s.  With states in 8 bits, 16 to 18 bytes an element, the instructions (640 for a warp's 256 elements, 2.3 a cycle): 480 us, and
-// 68 for the norm's pass over bf16 gradients; more bytes on their way, by more CTAs an SM or asynchronous copies, changed nothing (488 to 653).  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane:
-// a scale's block lies within a warp, so its maximum is five shuffles and no element is read twice.  The tensors are a table in the
-// workspace; a warp takes runs of neighbouring blocks and searches the first blocks for their tensor where the last one's does not
-// fit.  Lane l holds elements
-// 4 l .. 4 l + 3 and 128 + 4 l .. of the block, so every load and store of a warp is one contiguous run.
+// What bounds it: memory with states in 32 bits, 30 bytes an element (p, m, v in and out, g in, the bf16 copy out): 125 M elements in 607
+// us, 6.2 TB/s.  With states in 8 bits, 16 to 18 bytes an element, the instructions (640 for a warp's 256 elements, 2.3 a cycle): 480 us,
+// and 68 for the norm's pass over bf16 gradients; more bytes on their way, by more CTAs an SM or asynchronous copies, changed nothing (488
+// to 653).  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane: a scale's block lies
+// within a warp, so its maximum is five shuffles and no element is read twice.  The tensors are a table in the workspace; a warp takes
+// runs of neighbouring blocks and searches the first blocks for their tensor where the last one's does not fit.  Lane l holds elements 4 l
+// .. 4 l + 3 and 128 + 4 l .. of the block, so every load and store of a warp is one contiguous run.
 //
 // One launch without the norm, two with it: the step's count is read by every CTA as it starts and written by the CTA that
 // ends last.
@@ -318,7 +318,8 @@ __device__ __forceinline__ void aw_update(const AwStep& s, const AwNow& now, con
   const float rate = now.lr * t.lr_mult;
   float root[8];
   const unsigned long long factor = aw_two(now.factor, now.factor), b1 = aw_two(s.b1, s.b1), b2 = aw_two(s.b2, s.b2), c1 = aw_two(s.c1, s.c1),
-                           c2 = aw_two(s.c2, s.c2), up1 = aw_two(now.up1, now.up1), up2 = aw_two(now.up2, now.up2), eps = aw_two(s.eps, s.eps), decay = aw_two(t.decay, t.decay), back = aw_two(-rate, -rate);
+                           c2 = aw_two(s.c2, s.c2), up1 = aw_two(now.up1, now.up1), up2 = aw_two(now.up2, now.up2),
+                           eps = aw_two(s.eps, s.eps), decay = aw_two(t.decay, t.decay), back = aw_two(-rate, -rate);
 #pragma unroll
   for (int i = 0; i < 8; i += 2) {
     // (packed products, single sums: a packed sum of packed products comes out as one operation of one rounding)
@@ -390,9 +391,9 @@ __device__ __forceinline__ void aw_each(const AwView& w, uint32_t blocks, uint32
 __device__ __forceinline__ bool aw_full(const AwTensor& t, uint32_t b) {
   return t.wide && (long long)(b - t.first + 1) * AW_BLOCK <= t.n;
 }
-// Neighbouring blocks per warp and turn: `most` where every warp has some turns of them, else fewer, so that all SMs have work.  (125 M elements.  States in
-// 32 bits, runs of 1, 2, 4, 8: 609, 606, 607, 620 us.  In 8 bits, 4 and 8: 565 and 552, with 16 to a run of the norm; the norm's of 4, 16, 64: 595, 565,
-// 572, single blocks throughout 750.  One turn or 16 in place of four: 565 and 576.)
+// Neighbouring blocks per warp and turn: `most` where every warp has some turns of them, else fewer, so that all SMs have work.  (125 M
+// elements.  States in 32 bits, runs of 1, 2, 4, 8: 609, 606, 607, 620 us.  In 8 bits, 4 and 8: 565 and 552, with 16 to a run of the norm;
+// the norm's of 4, 16, 64: 595, 565, 572, single blocks throughout 750.  One turn or 16 in place of four: 565 and 576.)
 __device__ __forceinline__ uint32_t aw_run(uint32_t blocks, uint32_t most) {
   return min(most, max(1u, blocks / (gridDim.x * AW_WARPS * 4)));
 }
@@ -586,7 +587,8 @@ int qblora_adamw_step(const qblora_adamw_cfg* cfg, int32_t n_tensors, int64_t bl
   if (kinds > 3 || blocks > 0x7fffffff) return QBLORA_ERR_INVALID_ARG;
   if (!ptr_ok(cfg->lr, 4) || !ptr_ok(cfg->steps, 4) || (cfg->norm && !ptr_ok(cfg->norm, 4))) return QBLORA_ERR_INVALID_ARG;
   if (!(cfg->beta1 >= 0.0 && cfg->beta1 < 1.0 && cfg->beta2 >= 0.0 && cfg->beta2 < 1.0)) return QBLORA_ERR_INVALID_ARG;
-  if (!(cfg->eps == 0.0 || (cfg->eps >= FLT_MIN && cfg->eps <= FLT_MAX)) || !(cfg->max_norm >= 0.0 && std::isfinite(cfg->max_norm))) return QBLORA_ERR_INVALID_ARG;
+  if (!(cfg->eps == 0.0 || (cfg->eps >= FLT_MIN && cfg->eps <= FLT_MAX)) || !(cfg->max_norm >= 0.0 && std::isfinite(cfg->max_norm)))
+    return QBLORA_ERR_INVALID_ARG;
   if (!ws || !aligned16(ws) || ws_bytes < qblora_adamw_workspace_bytes(n_tensors)) return QBLORA_ERR_WORKSPACE;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   AwStep s{};

@@ -6,8 +6,8 @@
 // Across chunks one warp walks in order over a table of running sums, one step of a few instructions per chunk.  Whole numbers
 // only, no order but the requests': the result does not depend on the launch.
 //
-// What bounds it: latency (48 requests 3.2 us, 700 of 11,200 rows 6.9 us).  One launch, in which every CTA forms the sums for itself in shared memory; the rows are then spread
-// over the grid.
+// What bounds it: latency (48 requests 3.2 us, 700 of 11,200 rows 6.9 us).  One launch, in which every CTA forms the sums for itself in
+// shared memory; the rows are then spread over the grid.
 #include <atomic>
 
 #include "adapters.cuh"

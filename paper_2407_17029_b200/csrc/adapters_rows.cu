@@ -4,12 +4,13 @@
 // forms its part of the sum u = x' A; the parts are added over the cluster's shared memory; then each CTA has all of u and takes its
 // share of the outputs, Y += s repeat(u B).
 //
-// What bounds it: with an adapter per request the adapters' bytes (200 requests of as many adapters, 5120 -> 5120, rank 256: 262 MB in
-// 49 us, 5.4 TB/s), with few requests latency (one token, 4096 -> 4096: 8 us: the plan, the rows, x', the sums over the cluster, one after another).
-// A and B are read once per item.  Each warp has a ring of its own, steps of 16 by 64 weights brought by asynchronous copies, so no
-// barrier lies on that way; loads straight into registers came to 3.7 TB/s, as a warp cannot wait for the older of two loads alone.  The products are
-// mma.sync.m16n8k16, 16 ranks (outputs) by 8 tokens: a tile of 128 ranks on the other path's tensor memory would want a tile of 16 tokens and a
-// kernel to itself for each product (200 of 200: 2.5 times as long).  x' and u are two bf16 parts (three where Y is fp32), as in tc_adapters.cu.
+// What bounds it: with an adapter per request the adapters' bytes (200 requests of as many adapters, 5120 -> 5120, rank 256: 262 MB in 49
+// us, 5.4 TB/s), with few requests latency (one token, 4096 -> 4096: 8 us: the plan, the rows, x', the sums over the cluster, one after
+// another). A and B are read once per item.  Each warp has a ring of its own, steps of 16 by 64 weights brought by asynchronous copies, so
+// no barrier lies on that way; loads straight into registers came to 3.7 TB/s, as a warp cannot wait for the older of two loads alone.
+// The products are mma.sync.m16n8k16, 16 ranks (outputs) by 8 tokens: a tile of 128 ranks on the other path's tensor memory would want a
+// tile of 16 tokens and a kernel to itself for each product (64 adapters of 4 rows, 4096 -> 11008, rank 256: 56 us against 32 here).  x'
+// and u are two bf16 parts (three where Y is fp32), as in tc_adapters.cu.
 #include <algorithm>
 #include <atomic>
 

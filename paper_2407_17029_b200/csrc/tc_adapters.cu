@@ -46,7 +46,15 @@ struct AgPool {
   float factor;                         // 1 / lam or 1
   Parts out;                            // one part: lam = 1, the values are bf16 numbers already
 };
-struct AgPoolParams { AdaptersCall c; AgPool src[2]; int sources; uint32_t rows_there; int* status; uint32_t* tickets; int n_tickets, per, least, sms; };   // tickets: of grad
+struct AgPoolParams {
+  AdaptersCall c;
+  AgPool src[2];
+  int sources;
+  uint32_t rows_there;
+  int* status;
+  uint32_t* tickets;                    // of grad
+  int n_tickets, per, least, sms;
+};
 
 // N neighbouring values (1, 2 or 4) as parts, at `at` of the first part
 template <int N>
@@ -168,11 +176,11 @@ __device__ void ag_pool_row(const AgPool& p, const __nv_bfloat16* x, int64_t row
 
 // Parts begin at least this far apart in the plan: they have half of `least` rows, as filled up to a multiple of 16.
 __host__ __device__ inline int ag_apart(int least) { return least / 2 - 16; }
-// Rows above which an adapter is cut: the largest adapter in 1 to 16 parts, whichever takes the least time as counted in rows: rounds of the units
-// over the SMs, each the longest part and about 150 rows' time for its beginning and end, and 400 more where tiles go through memory.
-// One CTA of
-// the pooling kernel finds it beside the others: in front of the gradients it takes 7 us.  (4096 -> 4096, lambda 4, the whole backward pass without dX, us.  Rank 64: one adapter of 8192 rows whole 219, in 4 parts 109, 8 94, 16 102; six of
-// 1100 whole 77, cut in two 85.  Rank 256: one of 1800 67, in 4 parts 49; three of 600 46, cut in two 55.)
+// Rows above which an adapter is cut: the largest adapter in 1 to 16 parts, whichever takes the least time as counted in rows: rounds of
+// the units over the SMs, each the longest part and about 150 rows' time for its beginning and end, and 400 more where tiles go through
+// memory. One CTA of the pooling kernel finds it beside the others: in front of the gradients it takes 7 us.  (4096 -> 4096, lambda 4, the
+// whole backward pass without dX, us.  Rank 64: one adapter of 8192 rows whole 219, in 4 parts 109, 8 94, 16 102; six of 1100 whole 77,
+// cut in two 85.  Rank 256: one of 1800 67, in 4 parts 49; three of 600 46, cut in two 55.)
 __device__ int ag_split(const AdaptersCall& c, int per, int least, int sms) {
   __shared__ int s_most, s_units[8], s_longest[8];
   const int tid = threadIdx.x;
@@ -1326,9 +1334,9 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.m_tiles = (c.k.r + 127) / 128; p.sides = sides;
   for (int i = 0; i < sides; ++i) p.np = std::max(p.np, work[i].in->np);
-  // Rows of a tile: what takes the least time as counted in rows of 128 bytes: rounds of the units over the SMs, each its steps' operands and
-  // about 1280 for beginning and end.  (Backward pass without dX, us, tiles of 128 / 64 / 32: 4096 -> 4096, rank 64, lambda 4, 20 adapters of 300 rows
-  // 75 / 82 / 87, three of 600 - / 41 / 39; lambda 1, six of 1100 123 / 145 / 161.)
+  // Rows of a tile: what takes the least time as counted in rows of 128 bytes: rounds of the units over the SMs, each its steps' operands
+  // and about 1280 for beginning and end.  (Backward pass without dX, us, tiles of 128 / 64 / 32: 4096 -> 4096, rank 64, lambda 4, 20
+  // adapters of 300 rows 75 / 82 / 87, three of 600 - / 41 / 39; lambda 1, six of 1100 123 / 145 / 161.)
   int sms = 0;
   QB_TRY(ag_sms(&sms));
   int64_t least = -1, blocks = 0;
@@ -1357,7 +1365,8 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
 size_t as_fixed(int n, int np, int kb, int tn) {
   return (size_t)np * kb * tn * 128 + AS_RING * AG_TILE + (size_t)tn * 512 + AG_BARS + ag_table_bytes(n);
 }
-// rows of a tile: as many as leave room for five slabs, or for two where even the least do not; 0: none
+// rows of a tile: as many as leave room for five slabs, or for two where even the least do not; 0: none.  (7168 rows by 11008, rank 256, the
+// whole call: tiles of 64 with five slabs 109 us, of 32 with eight 128.)
 int as_rows(const BankView& k, int np) {
   for (int slabs : {5, 2})
     for (int tn = 64; tn >= 16; tn /= 2)
