@@ -129,3 +129,47 @@ def test_served_bank_against_the_layer_with_one_adapter(qb):
             want = qb.linear_fwd(qw, one, X[t]).double()
             # both within 1e-2 of the formula in root mean square (linear_fwd's and lowbit_gemm's bound); one rounding more here
             assert float((Y[t].double() - want).norm()) <= (2e-2 + 2.0 ** -8) * float(want.norm())
+
+
+def test_two_host_threads_on_their_own_streams(qb):
+    # sizes of both forward paths, gradients in parts, a step each time: the bits of the calls alone
+    import threading
+    problems, alone, errors = [], [], []
+    for k, (size, lens, ids) in enumerate((((512, 768, 4, 4, 64), [700, 1, 30], [0, 1, 1]), ((1024, 512, 8, 2, 128), [1] * 40, [b % 3 for b in range(40)]))):
+        bank = ra.make_bank(qb, 3, *size, seed=40 + k)
+        cu, di, T = ra.requests(lens, ids)
+        g = torch.Generator(device=DEV).manual_seed(k)
+        X, Y, dY = (torch.randn(T, w, generator=g, device=DEV).bfloat16() for w in (size[0], size[1], size[1]))
+        problems.append((bank, cu, di, T, X, Y, dY, torch.randn(bank.A.shape, generator=g, device=DEV)))
+
+    def once(bank, cu, di, T, X, Y, dY, param):
+        plan = qb.adapter_plan(cu, di, 3, T)
+        y = qb.adapters_fwd(bank, plan, X, Y.clone())
+        dx, dA, dB = qb.adapters_bwd(bank, plan, X, dY, torch.zeros(X.shape, device=DEV))
+        p = param.clone()
+        qb.AdamW([p], [dA], state_bits=8, lr=1e-2, max_norm=1.0).step()
+        return y, dx, dA, dB, p
+
+    alone = [once(*problem) for problem in problems]
+    torch.cuda.synchronize()
+    start = threading.Barrier(2)
+
+    def worker(k):
+        try:
+            stream = torch.cuda.Stream()
+            start.wait()
+            with torch.cuda.stream(stream):
+                for _ in range(25):
+                    got = once(*problems[k])
+                    stream.synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, alone[k])):
+                        errors.append(k)
+        except Exception as ex:      # surface in the main thread
+            errors.append(repr(ex))
+
+    threads = [threading.Thread(target=worker, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
