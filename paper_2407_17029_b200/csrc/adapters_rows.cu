@@ -458,15 +458,15 @@ int rows_adapters_fwd(const AdaptersCall& c, int* status, cudaStream_t st) {
   int sms = 0, dev = 0;
   QB_CUDA(cudaGetDevice(&dev));
   QB_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  // Clusters as large as there is room for at once: two CTAs an SM, or one where their shared memory or registers are too many, and of one an
-  // SM a quarter less, as a cluster lies within a GPC and leaves what does not make another one.  (4096 -> 11008, rank 256, one row each, in
-  // us by clusters of 1, 2, 4, 8: 16 adapters 35, 21, 16, 14; 48: 39, 23, 20, 27; 100: 47, 38, 47, 61; 200: 69, 77, 75, 110.)  How many items there are
-  // only the plan knows; between this and twice as many.
-  const int np = c.Y.dtype == QBLORA_F32 ? 3 : 2;
-  const bool two = np == 2 && nr_layout(np, c.k.r, c.k.n).all <= 113 * 1024;
-  const int64_t likely = std::max<int64_t>(std::min(c.T, c.k.n), c.T / NR_ROWS), room = two ? 2 * sms : sms * 3 / 4;
+  // Clusters as large as there is room for at once: two CTAs an SM, or one where their shared memory or registers are too many, less what the
+  // GPCs have left over that does not make a cluster (six for each CTA above two, as measured).  How many items there are only the plan
+  // knows; between this and twice as many.  (4096 -> 11008, rank 256, us by clusters of 1, 2, 4, 8.  bf16, one row each: 16 adapters 35, 21, 16, 14; 48:
+  // 39, 23, 20, 27; 100: 47, 38, 47, 61; 200: 69, 77, 75, 110.  fp32, eight rows: 14 70, 40, 27, 19; 16 75, 42, 27, 35; 32 86, 48, 32, 62; seven
+  // rows: 36 83, 47, 58, 62; three: 74 61, 41, 71, 81.)
+  const int np = c.Y.dtype == QBLORA_F32 ? 3 : 2, fit = np == 2 && nr_layout(np, c.k.r, c.k.n).all <= 113 * 1024 ? 2 : 1;
+  const int64_t likely = std::max<int64_t>(std::min(c.T, c.k.n), c.T / NR_ROWS);
   int cs = 8;
-  while (cs > 1 && likely * cs > room) cs /= 2;
+  while (cs > 1 && likely * cs > fit * sms - 6 * (cs - 2)) cs /= 2;
   return c.Y.dtype == QBLORA_F32 ? nr_launch<3, true>(p, items, cs, st) : nr_launch<2, false>(p, items, cs, st);
 }
 
