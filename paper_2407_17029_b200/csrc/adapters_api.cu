@@ -37,8 +37,8 @@ bool force_general() {
 
 // Calls of no more rows go to adapters_rows.cu, by the type of Y; larger ones, whose adapters have many rows then, or are many, to
 // tc_adapters.cu.  (Both in us, graph replays.  bf16: 4096 -> 4096, rank 64, 64 adapters of 8 rows 13 and 29, 16 of 32 13 and 22, of 64 20 and 25;
-// 4096 -> 11008, rank 256, 64 of 8 37 and 54, 16 of 32 30 and 32, of 64 43 and 35.  fp32: 32 of 8 14 and 24, 16 of 32 32 and 24; 32 of 8 32 and 34, 16 of
-// 32 87 and 35.)
+// 4096 -> 11008, rank 256, 64 of 8 37 and 54, 16 of 32 30 and 32, of 64 43 and 35.  fp32: 64 of 4 13 and 31, 16 of 32 20 and 24, of 64
+// 38 and 29; 41 and 59, 49 and 36, 89 and 48.)
 int few_rows(int y_dtype) { return y_dtype == QBLORA_F32 ? 256 : 512; }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
