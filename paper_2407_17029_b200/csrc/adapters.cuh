@@ -33,9 +33,9 @@ struct AdaptersCall {
   float *dA, *dB;
 };
 
-// Rank of adapter a that the kernels work with: a multiple of 16, or the slots' rank.
+// Rank of adapter a that the kernels work with: a multiple of 16, or the slots' rank.  (Unsigned: the largest int32 rounded up passes 2^31.)
 __device__ __forceinline__ int bank_rank(const BankView& k, int a) {
-  return k.ranks ? min((max(__ldg(k.ranks + a), 0) + 15) & ~15, k.r) : k.r;
+  return k.ranks ? (int)min(((uint32_t)max(__ldg(k.ranks + a), 0) + 15u) & ~15u, (uint32_t)k.r) : k.r;
 }
 // Entry i of the plan's offsets, forced into 0 .. T.
 __device__ __forceinline__ int plan_start(const AdaptersCall& c, int i) { return min(max(__ldg(c.start + i), 0), c.T); }
