@@ -505,7 +505,8 @@ int qblora_adapter_plan(const int32_t* cu, const int32_t* ids, int32_t n_request
  *   rows [tokens], start [n_adapters + 1]: DEVICE int32, as written by qblora_adapter_plan (each row at most once; entries out of
  *   range are passed over).  X DEVICE bf16, x_stride elements between rows; Y DEVICE bf16 or fp32 (y_dtype), y_stride likewise;
  *   X and Y do not overlap.  x' and x' A are carried as sums of bf16 numbers: two where Y is bf16, within 2^-16, three where
- *   it is fp32 (and throughout the backward pass), within 2^-24.
+ *   it is fp32 (and throughout the backward pass), within 2^-24.  Infinite numbers in X, A and B (and dY) leave the infinities and the
+ *   NaN of the formula.
  * Any sizes; rank and Q multiples of 8, d_in, d_out and the strides multiples of 8 and all tensors 16-byte
  * aligned take the fast kernels, up to the rank whose x' A of 16 rows fits in shared memory beside a weight tile (1024 at least).
  *   ws: qblora_adapters_workspace_bytes(bank, tokens, 0) bytes.

@@ -164,6 +164,51 @@ __device__ __forceinline__ void nr_store_parts(__nv_bfloat16* out, int part, flo
   }
 }
 
+// What is not finite.  Where a factor is infinite, or a sum is, the smaller parts make NaN of it: the rest of an infinity is inf - inf, and a part that
+// is zero or of the other sign meets an infinite weight.  So where u or a product has come out as NaN it is formed once more: u from x' whole,
+// a product from u's first part, which is zero only where u is.  Out of line, as all that a call runs it fetches for the first time: 0.1 us a call;
+// inline 0.3; the warp's steps once more through its ring 0.2 to 0.8.
+// four ranks of u, at `to` in parts; A: the first of them
+template <int NP>
+__device__ __noinline__ void nr_mend_u(const AdaptersCall& c, int row, const __nv_bfloat16* A, __nv_bfloat16* to, int part) {
+  for (int e = 0; e < 4; ++e) {
+    if (!isnan(__bfloat162float(to[e]))) continue;
+    const __nv_bfloat16 *x = static_cast<const __nv_bfloat16*>(c.X.data) + row * c.X.stride, *a = A + e;
+    float sum = 0.f;
+    for (int p = 0; p < c.k.P && !isnan(sum); ++p, a += c.k.r) {
+      float mean = 0.f;
+      for (int l = 0; l < c.k.l1; ++l) mean += __bfloat162float(*x++);
+      sum = fmaf(mean / (float)c.k.l1, __bfloat162float(*a), sum);
+    }
+    nr_store_parts<NP>(to + e, part, sum);
+  }
+}
+// A lane's products as nr_put has put them, of u's first part and steps first, first + stride ... of B.
+__device__ __noinline__ void nr_mend_put(float* put, int pitch, const __nv_bfloat16* u, int u_pitch, const __nv_bfloat16* B, int Q, int q0, int r, int n,
+                                         int first, int stride) {
+  const int lane = threadIdx.x & 31;
+  for (int i = 0; i < 16; ++i) {
+    const int row = 2 * (lane & 3) + (i & 1), q = (i >> 1) * 8 + (lane >> 2);
+    if (row >= n || q0 + q >= Q || !isnan(put[row * pitch + q])) continue;
+    float sum = 0.f;
+    for (int s = first * 16; s < r; s += stride * 16)
+      for (int k = s; k < min(s + 16, r); ++k) sum = fmaf(__bfloat162float(u[row * u_pitch + k]), __bfloat162float(B[(int64_t)k * Q + q0 + q]), sum);
+    put[row * pitch + q] = sum;
+  }
+}
+// whether there is NaN among a lane's products of the first n rows
+__device__ __forceinline__ bool nr_any_nan(const float (&d)[4][4], int n, int lane) {
+  float any[2] = {0.f, 0.f};                      // rows 2 (lane % 4) and the next; two numbers by one instruction
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+#pragma unroll
+    for (int e = 0; e < 4; e += 2)
+      asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+          : "+f"(any[0]), "+f"(any[1]) : "f"(d[t][e]), "f"(d[t][e + 1]));
+  const int row = 2 * (lane & 3);
+  return (row < n && isnan(any[0])) || (row + 1 < n && isnan(any[1]));
+}
+
 // Columns [lo, hi) of x' of the rows, as parts, at out[p * part + row * pitch + column - lo].
 template <int NP>
 __device__ __forceinline__ void nr_pool(const AdaptersCall& c, const int* rows, int n, int lo, int hi, __nv_bfloat16* out, int pitch, int part) {
@@ -300,11 +345,14 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
     } else {
       x = *reinterpret_cast<const float4*>(part + row * wide + col);
     }
+    // no ranks behind the slots' last one: there infinite inputs have met weights of zero
+    if (col >= r_read) x = make_float4(0.f, 0.f, 0.f, 0.f);
     __nv_bfloat16* to = us + row * up + col;
     nr_store_parts<NP>(to, upart, x.x);
     nr_store_parts<NP>(to + 1, upart, x.y);
     nr_store_parts<NP>(to + 2, upart, x.z);
     nr_store_parts<NP>(to + 3, upart, x.w);
+    if (__builtin_expect(isnan((x.x + x.y) + (x.z + x.w)), 0) && s_row[row] >= 0) nr_mend_u<NP>(c, s_row[row], A + col, to, upart);
   }
   if (cs > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");     // this CTA has read the others' parts
   __syncthreads();
@@ -345,7 +393,9 @@ __device__ __forceinline__ void nr_item(const NrParams& p, const NrLayout& l, ui
       nr_product<NP>(d, w2, ring, us, up, upart, lane);
       w2 = b_steps(b + teams);
       if (b + teams < own) nr_ahead<AHEAD>(w2, ring, lane);
-      nr_put(d, vs + warp * NR_ROWS * VP, VP, lane);
+      float* put = vs + warp * NR_ROWS * VP;
+      nr_put(d, put, VP, lane);
+      if (__builtin_expect(nr_any_nan(d, n, lane), 0)) nr_mend_put(put, VP, us, up, B, k.Q, q0, r_read, n, sub, kw);
     }
     if (kw > 1) __syncthreads();
     else __syncwarp();

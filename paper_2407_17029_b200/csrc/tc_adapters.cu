@@ -255,6 +255,8 @@ struct AgMaps3 { CUtensorMap w, rows, rows16; };      // the bank's matrix; the 
 struct AgShrinkSide {
   int np, K, w_kmajor, scaled;          // parts of the input; contraction; the weight's contiguous dimension is the contraction's; times
   Parts out;                            // the adapter's factor
+  const __nv_bfloat16 *in, *W;          // what the tensor maps describe: the input's first part, the bank's matrix
+  int in_ld;
 };
 struct AgShrink {
   AdaptersCall c;
@@ -356,6 +358,37 @@ __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
   for (int j = 0; j < 32; ++j) v[j] += __uint_as_float(w[j]);
 }
 
+// What is not finite.  Where a factor is infinite, or a sum is, the products of the first parts have what the formula has there (they are zero only where
+// the number is), but the smaller ones make NaN of it: the rest of an infinity is inf - inf, and a part that is zero or of the other sign meets
+// an infinite weight.  So a result that is NaN is formed once more, of the first parts alone, on the CUDA cores and out of line.  (A look at each
+// number as it leaves tensor memory: 2 to 3 us of each call of 70, for its instructions' way into the SM more than for their number.)
+template <int N>
+__device__ __forceinline__ bool ag_any_nan(const float* x) {
+  float sum[2] = {0.f, 0.f};                              // two numbers by one instruction
+#pragma unroll
+  for (int j = 0; j < N; j += 2)
+    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+        : "+f"(sum[0]), "+f"(sum[1]) : "f"(x[j]), "f"(x[j + 1]));
+  return isnan(sum[0] + sum[1]);
+}
+// sum[e] = sum over i of a[i a_step] b[i b_step + e b_next]; nothing changes a sum that is NaN already
+template <int N>
+__device__ __forceinline__ void ag_first_parts(float (&sum)[N], const __nv_bfloat16* a, int64_t a_step, const __nv_bfloat16* b, int64_t b_step,
+                                               int64_t b_next, int n) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+#pragma unroll 4
+    for (int i = i0; i < min(n, i0 + 64); ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] = fmaf(__bfloat162float(a[i * a_step]), __bfloat162float(b[i * b_step + e * b_next]), sum[e]);
+    bool done = true;
+#pragma unroll
+    for (int e = 0; e < N; ++e) done = done && isnan(sum[e]);
+    if (done) break;
+  }
+}
+
 // The same, with the parts one behind the other (and a third apart, if not 0, whose sums go to the second's): the weights are read once for
 // all of them (contraction 4096, 1800 rows, three parts: 39.5 -> 35.6 us).
 template <bool KMAJOR, bool THIRD>
@@ -374,6 +407,28 @@ __device__ __forceinline__ void ag_issue_together(uint32_t d, uint32_t d1, uint6
     step(3 * STEP, 3 * AG_STEP_K, 1u);
   } else {
     for (int e = 1; e < n; ++e) step(e * STEP, e * AG_STEP_K, 1u);
+  }
+}
+
+// NaN among a tile's results: rows at .. of the workspace, one rank m to a lane.
+__device__ __noinline__ void ag_mend_shrink(const AgShrink& p, int side, int a, uint32_t at, int rows, int m) {
+  const AgShrinkSide& s = p.side[side];
+  if (m >= bank_rank(p.c.k, a)) return;
+  const __nv_bfloat16* W = s.W + (int64_t)a * p.c.k.r * s.K + (s.w_kmajor ? (int64_t)m * s.K : m);
+  const float scale = s.scaled ? __ldg(p.c.k.s + a) : 1.0f;
+  for (int j = 0; j < rows; j += 8) {                     // (the workspace has rows up to a multiple of 16)
+    __nv_bfloat16* to = s.out.p + (int64_t)(at + j) * s.out.ld + m;
+    bool odd[8], any = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) any |= odd[e] = j + e < rows && isnan(__bfloat162float(to[e * s.out.ld]));
+    if (!any) continue;
+    float sum[8];
+    ag_first_parts(sum, W, s.w_kmajor ? 1 : p.c.k.r, s.in + (int64_t)(at + j) * s.in_ld, 1, s.in_ld, s.K);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x[1] = {sum[e] * scale};
+      if (odd[e]) ag_store_parts<1>(s.out, (int64_t)(at + j + e) * s.out.ld + m, x);
+    }
   }
 }
 
@@ -494,6 +549,13 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
       if (!unit(u)) continue;
       const AgShrinkSide& sd = p.side[side];
       const int together = sd.np * t.n16 <= 256 ? sd.np : 2;
+      // which of its columns are rows; the others, also those that are passed over, are zeros for the gradients, whatever the weights are
+      uint32_t real[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = half * 64 + e * 32 + lane, row = i < t.rows ? __ldg(p.c.rows + t.j + i) : -1;
+        real[e] = __ballot_sync(0xffffffffu, row >= 0 && row < p.c.T) >> (lane & 1);
+      }
       float v[64];
 #pragma unroll
       for (int j = 0; j < 64; ++j) v[j] = 0.f;
@@ -523,8 +585,13 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         const float v0 = v[j] * scale, v1 = v[j + 1] * scale;
         const float got = __shfl_xor_sync(0xffffffffu, (lane & 1) ? v0 : v1, 1);
         const int col = half * 64 + j + (lane & 1);
-        const float x[2] = {(lane & 1) ? got : v0, (lane & 1) ? v1 : got};
+        const bool there = real[j >> 5] & 1u << (j & 31);
+        const float x[2] = {!there ? 0.f : (lane & 1) ? got : v0, !there ? 0.f : (lane & 1) ? v1 : got};
         if (m < sd.out.width) ag_store_parts<2>(sd.out, (int64_t)(t.at + col) * sd.out.ld + m, x);      // (the rank is a multiple of 8)
+      }
+      if (__any_sync(0xffffffffu, ag_any_nan<64>(v))) {
+        __syncwarp();
+        ag_mend_shrink(p, side, t.a, t.at + half * 64, min(64, t.rows - half * 64), m0 + q * 32 + lane);
       }
     }
   }
@@ -551,6 +618,8 @@ struct AgSpread {
   int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
   int slabs;
   int m_tiles, M, w_kmajor, scaled;
+  const __nv_bfloat16 *u, *W;           // what the tensor maps describe: u's first part, the bank's matrix
+  int u_ld;
   RowsView y;
   int lam, shift;                       // shift: log2 of the bytes of one q, where they are a power of two
   int boxes;                            // whole slabs of neighbouring rows by tensor copies: pieces of a row's 128 q; 0: none
@@ -662,6 +731,19 @@ __device__ __noinline__ void as_sums(uint8_t* slab, int pitch, const float* v, i
       *at = as_add<F32, QPC>(*at, q);
     }
   }
+}
+
+// NaN among V's rows j .. j + 15 of the tile, column q of it, which is output m.
+__device__ __noinline__ void as_mend(const AgSpread& p, float* v, int a, uint32_t at, int rows, int m, float scale) {
+  if (m >= p.M) return;
+  const int r = bank_rank(p.c.k, a);
+  const __nv_bfloat16* W = p.W + (int64_t)a * p.c.k.r * p.M + (p.w_kmajor ? (int64_t)m * p.c.k.r : m);
+  for (int j = 0; j < rows; ++j)
+    if (isnan(v[j * 128])) {
+      float sum[1];
+      ag_first_parts(sum, p.u + (int64_t)(at + j) * p.u_ld, 1, W, p.w_kmajor ? 1 : p.M, 0, r);
+      v[j * 128] = sum[0] * scale;
+    }
 }
 
 template <bool F32, int QPC>
@@ -889,6 +971,8 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
           if (p.np > 1) ag_gather16(d + 64, x);
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[(part * 16 + j) * 128 + q * 32 + lane] = x[j] * scale;
+          if (ag_any_nan<16>(x))
+            as_mend(p, v + part * 16 * 128 + q * 32 + lane, t.a, t.at + part * 16, min(16, t.rows - part * 16), m * 128 + q * 32 + lane, scale);
         }
         tc_fence_before();
         __syncwarp();
@@ -960,7 +1044,7 @@ __device__ __forceinline__ void ar_issue(uint32_t d, uint64_t a, uint64_t b, uin
     b += AG_STEP_T;
   }
 }
-struct AgGradSide { int parts_a, parts_b, M, N; float* out; };        // dA: x' (P) by du (r); dB: u (r) by dv (Q)
+struct AgGradSide { int parts_a, parts_b, M, N; float* out; const __nv_bfloat16 *a, *b; int a_ld, b_ld; };     // dA: x' (P) by du (r); dB: u (r) by dv (Q)
 struct AgGrad {
   AdaptersCall c;
   uint32_t rows_there;
@@ -980,6 +1064,21 @@ __device__ __forceinline__ bool ar_any(bool x) {
   asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 p, %1, 0;\n barrier.cta.red.or.pred q, 1, 256, p;\n selp.u32 %0, 1, 0, q;\n}"
                : "=r"(y) : "r"((uint32_t)x) : "memory");
   return y != 0;
+}
+
+// NaN among a thread's results: row m, columns n .. of them, at `out`; the adapter's rows in the workspace.
+__device__ __noinline__ void ar_mend(const AgGradSide& s, float* out, int m, int n, int columns, uint32_t at, int rows, float scale) {
+  for (int j = 0; j < columns; j += 8) {                  // (they are a multiple of 8)
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) any |= isnan(out[j + e]);
+    if (!any) continue;
+    float sum[8];
+    ag_first_parts(sum, s.a + (int64_t)at * s.a_ld + m, s.a_ld, s.b + (int64_t)at * s.b_ld + n + j, s.b_ld, 1, rows);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (isnan(out[j + e])) out[j + e] = sum[e] * scale;
+  }
 }
 
 __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __grid_constant__ AgGradMaps maps, const __grid_constant__ AgGrad p) {
@@ -1191,6 +1290,8 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
           for (int e = 0; e < 4; ++e) x[e] = (t.side ? m : t.n0 + half * 64 + j + e) < t.rank ? v[j + e] * scale : 0.f;
           *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
         }
+        if (ag_any_nan<64>(v))
+          ar_mend(side, out, m, t.n0 + half * 64, min(64, side.N - t.n0 - half * 64), (uint32_t)t.first, t.all * 16, scale);
       }
     }
   }
@@ -1349,7 +1450,7 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
   for (int i = 0; i < sides; ++i) {
     const ShrinkWork& w = work[i];
     const Parts& in = *w.in;
-    p.side[i] = {in.np, in.width, w.kmajor, w.scaled, *w.out};
+    p.side[i] = {in.np, in.width, w.kmajor, w.scaled, *w.out, in.p, w.W, in.ld};
     p.segment = w.out->np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
     QB_TRY(parts_map(&maps.side[i].rows, in, l.rows, p.tn));
     QB_TRY(parts_map(&maps.side[i].rows16, in, l.rows, 16));
@@ -1394,6 +1495,7 @@ int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
   p.slabs = (int)std::min<size_t>(8, (AG_SMEM - fixed) / AS_SLAB);
   p.m_tiles = (M + 127) / 128; p.M = M; p.w_kmajor = kmajor; p.scaled = forward; p.y = y; p.lam = lam;
+  p.u = in.p; p.u_ld = in.ld; p.W = W;
   p.factor = forward ? 1.0f : 1.0f / (float)lam;
   const int w = lam * (y.dtype == QBLORA_F32 ? 4 : 2);
   p.shift = -1;
@@ -1424,8 +1526,8 @@ int ag_grad(const AdaptersCall& c, const Layout& l, int* status, cudaStream_t st
   AgGrad p{};
   p.c = c; p.rows_there = l.rows; p.status = status; p.wait_limit = wait_limit_cycles();
   p.least = l.least; p.parts = l.parts; p.tickets = l.tickets; p.n_tickets = l.n_tickets;
-  p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA};
-  p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB};
+  p.side[0] = {l.x.np, l.du.np, c.k.P, c.k.r, c.dA, l.x.p, l.du.p, l.x.ld, l.du.ld};
+  p.side[1] = {l.u.np, l.dv.np, c.k.r, c.k.Q, c.dB, l.u.p, l.dv.p, l.u.ld, l.dv.ld};
   QB_TRY(parts_map(&maps.a[0], l.x, l.rows, 32));
   QB_TRY(parts_map(&maps.b[0], l.du, l.rows, 32));
   QB_TRY(parts_map(&maps.a[1], l.u, l.rows, 32));
