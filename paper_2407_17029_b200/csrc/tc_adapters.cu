@@ -617,6 +617,7 @@ struct AgSpread {
   uint32_t rows_there;                  // of the workspace
   int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
   int slabs;
+  int segment;                          // as in AgShrink
   int m_tiles, M, w_kmajor, scaled;
   const __nv_bfloat16 *u, *W;           // what the tensor maps describe: u's first part, the bank's matrix
   int u_ld;
@@ -846,30 +847,31 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     each([&](const AgRows& t, int steps, int first) {
       if (!ag_wait(ufull, n & 1u, p.status, p.wait_limit)) return false;
       const uint32_t idesc = ag_idesc(!p.w_kmajor, false, t.n16);
-      for (int m = first; m < p.m_tiles; m += runs, ++done) {
-        const int b = done & 1;
-        if (!ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
-        tc_fence_after();
-        for (int k = 0; k < steps; k += 4) {
-          if (!ag_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
+      for (int m = first; m < p.m_tiles; m += runs)
+        for (int k0 = 0; k0 < steps; k0 += 4 * p.segment, ++done) {
+          const int b = done & 1, end = min(steps, k0 + 4 * p.segment);
+          if (!ag_wait(accempty(b), ((done >> 1) & 1u) ^ 1u, p.status, p.wait_limit)) return false;
           tc_fence_after();
-          const uint32_t d = tmem + b * 128;
-          if (leader) {
-            const uint32_t w = ring + s * AG_TILE;
-            const uint64_t rows = ag_desc(at_u + (k / 4) * block, false), part = (uint64_t)(p.kb * block) >> 4;
-            const int some = min(4, steps - k);
-            if (p.w_kmajor) ag_issue_parts<true>(p.np, d, d + 64, ag_desc(w, false), rows, part, idesc, some, k == 0);
-            else ag_issue_parts<false>(p.np, d, d + 64, ag_desc(w, true), rows, part, idesc, some, k == 0);
-            tc_commit(wempty(s));
-            if (k + 4 >= steps) {
-              tc_commit(accfull(b));
-              if (m + runs >= p.m_tiles) tc_commit(uempty);
+          for (int k = k0; k < end; k += 4) {
+            if (!ag_wait(wfull(s), ph, p.status, p.wait_limit)) return false;
+            tc_fence_after();
+            const uint32_t d = tmem + b * 128;
+            if (leader) {
+              const uint32_t w = ring + s * AG_TILE;
+              const uint64_t rows = ag_desc(at_u + (k / 4) * block, false), part = (uint64_t)(p.kb * block) >> 4;
+              const int some = min(4, steps - k);
+              if (p.w_kmajor) ag_issue_parts<true>(p.np, d, d + 64, ag_desc(w, false), rows, part, idesc, some, k == k0);
+              else ag_issue_parts<false>(p.np, d, d + 64, ag_desc(w, true), rows, part, idesc, some, k == k0);
+              tc_commit(wempty(s));
+              if (k + 4 >= end) {
+                tc_commit(accfull(b));
+                if (end == steps && m + runs >= p.m_tiles) tc_commit(uempty);
+              }
             }
+            __syncwarp();
+            if (++s == AS_RING) { s = 0; ph ^= 1u; }
           }
-          __syncwarp();
-          if (++s == AS_RING) { s = 0; ph ^= 1u; }
         }
-      }
       ++n;
       return true;
     });
@@ -955,28 +957,34 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
     }
     uint32_t done = 0, ph = 0;
     int s = 0;
-    each([&](const AgRows& t, int, int first) {
+    each([&](const AgRows& t, int steps, int first) {
       const float scale = p.scaled ? __ldg(p.c.k.s + t.a) * p.factor : p.factor;
-      for (int m = first; m < p.m_tiles; m += runs, ++done) {
-        const int b = done & 1;
-        bool ok = mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit);
-        if (as_any(!ok)) return false;                                // (and V's readers of the tile before are done)
-        tc_fence_after();
-        if (part * 16 < t.n16) {
-          float x[16];
-          const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + part * 16;
+      for (int m = first; m < p.m_tiles; m += runs) {
+        float x[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = 0.f;
-          ag_gather16(d, x);
-          if (p.np > 1) ag_gather16(d + 64, x);
+        for (int j = 0; j < 16; ++j) x[j] = 0.f;
+        bool ok = true;
+        for (int k = 0; k < steps && ok; k += 4 * p.segment, ++done) {
+          const int b = done & 1;
+          ok = __all_sync(0xffffffffu, mbar_wait(accfull(b), (done >> 1) & 1u, p.status, p.wait_limit));
+          if (!ok) break;                                             // (all leave together, below)
+          tc_fence_after();
+          if (part * 16 < t.n16) {
+            const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + part * 16;
+            ag_gather16(d, x);
+            if (p.np > 1) ag_gather16(d + 64, x);
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(accempty(b));
+        }
+        if (as_any(!ok)) return false;                                // (and V's readers of the tile before are done)
+        if (part * 16 < t.n16) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[(part * 16 + j) * 128 + q * 32 + lane] = x[j] * scale;
           if (ag_any_nan<16>(x))
             as_mend(p, v + part * 16 * 128 + q * 32 + lane, t.a, t.at + part * 16, min(16, t.rows - part * 16), m * 128 + q * 32 + lane, scale);
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(accempty(b));
         asm volatile("bar.sync 1, 512;" ::: "memory");
         for (AsSlabs y(p, whole, m, t.rows); y.there(); y.next()) {
           ok = __all_sync(0xffffffffu, mbar_wait(in(s), ph, p.status, p.wait_limit));
@@ -1426,6 +1434,9 @@ int bank_map(CUtensorMap* tm, const __nv_bfloat16* ptr, int width, int rows, int
 
 int64_t most_tiles(const AdaptersCall& c, int tn) { return c.T / tn + std::min<int64_t>(c.T, c.k.n); }
 
+// 64-wide blocks between two emptyings of an accumulator.  Results in fp32, which are three parts: see AR_SEGMENT.
+int ag_segment(int parts) { return parts == 3 ? 4 : 1 << 20; }
+
 struct ShrinkWork { const Parts *in, *out; const __nv_bfloat16* W; bool kmajor, scaled; };
 // u = x' A, du = s dv B^T, or both
 int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkWork* work, int sides, cudaStream_t st) {
@@ -1451,7 +1462,7 @@ int ag_shrink(const AdaptersCall& c, const Layout& l, int* status, const ShrinkW
     const ShrinkWork& w = work[i];
     const Parts& in = *w.in;
     p.side[i] = {in.np, in.width, w.kmajor, w.scaled, *w.out, in.p, w.W, in.ld};
-    p.segment = w.out->np == 3 ? 4 : 1 << 20;      // results in fp32: see AR_SEGMENT
+    p.segment = ag_segment(w.out->np);
     QB_TRY(parts_map(&maps.side[i].rows, in, l.rows, p.tn));
     QB_TRY(parts_map(&maps.side[i].rows16, in, l.rows, 16));
     // A [P][r]: the contraction runs over its rows; B [r][Q]: along them
@@ -1494,7 +1505,7 @@ int ag_spread(const AdaptersCall& c, const Layout& l, int* status, const Parts& 
   p.np = in.np; p.kb = (c.k.r + 63) / 64; p.tn = as_rows(c.k, in.np);
   const size_t fixed = as_fixed(c.k.n, p.np, p.kb, p.tn);
   p.slabs = (int)std::min<size_t>(8, (AG_SMEM - fixed) / AS_SLAB);
-  p.m_tiles = (M + 127) / 128; p.M = M; p.w_kmajor = kmajor; p.scaled = forward; p.y = y; p.lam = lam;
+  p.segment = ag_segment(in.np); p.m_tiles = (M + 127) / 128; p.M = M; p.w_kmajor = kmajor; p.scaled = forward; p.y = y; p.lam = lam;
   p.u = in.p; p.u_ld = in.ld; p.W = W;
   p.factor = forward ? 1.0f : 1.0f / (float)lam;
   const int w = lam * (y.dtype == QBLORA_F32 ? 4 : 2);
