@@ -577,7 +577,8 @@ typedef struct {
  * qblora_adamw_prepare lays the tensors' table into ws and writes to *blocks the number that the step wants (an opaque one); ws then belongs to
  * these tensors (their addresses, not their values) until it is prepared again.  At most 65536 tensors, 2^31 - 1 blocks.
  * No tensor may overlap another.  qblora_adamw_step may be captured in a graph: lr, steps and the gradients' values are
- * read when it runs.  Two steps over one ws run one after the other.
+ * read when it runs.  The calls over one ws, qblora_adamw_prepare among them, run one after the other: on one stream, or with the
+ * caller's events between their streams (a table that is written beside a step that reads it leaves neither).
  */
 size_t qblora_adamw_workspace_bytes(int32_t n_tensors);
 int qblora_adamw_prepare(const qblora_adamw_tensor* tensors, int32_t n_tensors, void* ws, size_t ws_bytes, int64_t* blocks,

@@ -795,6 +795,36 @@ def adapters_bwd(bank: AdapterBank, plan: AdapterPlan, X: Optional[torch.Tensor]
     return dX, dA, dB
 
 
+class _Order:
+    """Calls that share buffers, one behind the other whatever streams they are on; called with a call's stream it gives the handle.
+    `tensors`: memory of the first stream, which the others use too."""
+
+    def __init__(self, tensors=()):
+        self._handle, self._stream, self._tensors = None, None, tensors
+
+    def __call__(self, stream) -> int:
+        handle = _stream_ptr(stream)
+        if handle != self._handle:
+            self._change(stream if stream is not None else torch.cuda.current_stream(), handle)
+        return handle
+
+    def _change(self, stream, handle) -> None:
+        if _capturing(stream):              # nothing runs now, and a graph cannot wait for work outside
+            return
+        if self._stream is not None:
+            if _capturing(self._stream):
+                raise RuntimeError("the stream of the call before is being captured: order the two streams when that has ended")
+            stream.wait_stream(self._stream)
+            for t in self._tensors:
+                t.record_stream(stream)
+        self._handle, self._stream = handle, stream
+
+
+def _capturing(stream) -> bool:
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _zero(t: torch.Tensor, stream) -> None:
     if stream is None:
         t.zero_()
@@ -811,7 +841,11 @@ class AdamW:
     the second one's square root with one fp32 scale per 256 elements in m_scale, v_scale.  They start at zero; `states` takes
     kept ones (a dict of lists with these names), `steps` a kept count (int32 [1], device).  lr: a number, or an fp32 device tensor [1]
     that a schedule writes; lr_mult and weight_decay: numbers or lists.  max_norm > 0 clips by the global norm, need_norm asks
-    for it alone (self.norm, fp32 [1])."""
+    for it alone (self.norm, fp32 [1]).
+
+    The constructor, set_grads and step share the table: each of them waits, on its own stream, for the one before it, whatever stream that
+    was on.  A step that is captured waits for nothing and nothing waits for it: its graph is replayed behind the constructor and the
+    last set_grads, and not beside another step."""
 
     def __init__(self, params, grads, copies=None, state_bits=32, states=None, lr=1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
                  weight_decay=0.0, lr_mult=1.0, max_norm: float = 0.0, need_norm: bool = False, seed: int = 0, steps=None, stream=None):
@@ -861,13 +895,16 @@ class AdamW:
                                      p(self.m_scale[k]) if bits[k] == 8 else None, p(self.v_scale[k]) if bits[k] == 8 else None, size,
                                      _dt(self.grads[k].dtype), bits[k], mult[k], decay[k])
         self._n, self._blocks, self._table = n, ctypes.c_int64(), table
+        made = [t for t in (self.steps if steps is None else None, self.lr, self.norm) if t is not None]
+        made += [t for name in make for k, t in enumerate(getattr(self, name)) if t is not None and states.get(name) is None]
         self.ws = _empty(max(int(_lib.qblora_adamw_workspace_bytes(n)), 256), torch.uint8, self.device, stream)
         self._cfg = _CAdamWCfg(self.lr.data_ptr(), self.steps.data_ptr(), float(betas[0]), float(betas[1]), float(eps), float(max_norm),
                                int(seed) & 0xffffffff, p(self.norm))
+        self._order = _Order([self.ws] + made)
         self._prepare(stream)
 
     def _prepare(self, stream):
-        _check(_lib.qblora_adamw_prepare(self._table, self._n, self.ws.data_ptr(), self.ws.numel(), ctypes.byref(self._blocks), _stream_ptr(stream)),
+        _check(_lib.qblora_adamw_prepare(self._table, self._n, self.ws.data_ptr(), self.ws.numel(), ctypes.byref(self._blocks), self._order(stream)),
                "qblora_adamw_prepare")
 
     def set_grads(self, grads, stream=None) -> None:
@@ -884,7 +921,7 @@ class AdamW:
 
     def step(self, stream=None) -> Optional[torch.Tensor]:
         """One step on the gradients as they are when it runs; returns the norm's tensor, where it is formed."""
-        st = _lib.qblora_adamw_step(ctypes.byref(self._cfg), self._n, self._blocks.value, self.ws.data_ptr(), self.ws.numel(), _stream_ptr(stream))
+        st = _lib.qblora_adamw_step(ctypes.byref(self._cfg), self._n, self._blocks.value, self.ws.data_ptr(), self.ws.numel(), self._order(stream))
         if st != OK:
             _check(st, "qblora_adamw_step")
         return self.norm
