@@ -1555,7 +1555,8 @@ int forward_parts(int y_dtype) { return y_dtype == QBLORA_F32 ? 3 : 2; }
 size_t tc_adapters_ws_bytes(const BankView& k, int64_t T, bool backward) { return ag_layout(k, T, backward, 3, nullptr).bytes; }
 
 bool tc_adapters_sizes_ok(const BankView& k, int64_t T) {
-  return k.r % 8 == 0 && k.Q % 8 == 0 && k.d_in % 8 == 0 && k.d_out % 8 == 0 && T + 15 * std::min<int64_t>(T, k.n) <= 0x7ffffff0 &&
+  constexpr int most = (1 << 22) - 1;             // 128 q of a row in fp32 are below 2^31 bytes
+  return k.l1 <= most && k.l2 <= most && k.r % 8 == 0 && k.Q % 8 == 0 && k.d_in % 8 == 0 && k.d_out % 8 == 0 && T + 15 * std::min<int64_t>(T, k.n) <= 0x7ffffff0 &&
          as_rows(k, 3) > 0;
 }
 
