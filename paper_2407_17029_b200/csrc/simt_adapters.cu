@@ -90,6 +90,7 @@ __global__ void gradient_kernel(const __grid_constant__ AdaptersCall c, const fl
     }
 }
 
+unsigned grid_rows(int n) { return (unsigned)(n > 1024 ? 1024 : n); }     // (the kernel goes on from there; a grid's y ends at 65535)
 unsigned parts(int n, int per) { const int x = (n + per - 1) / per; return (unsigned)(x > 64 ? 64 : x); }
 
 int launched() {
@@ -150,13 +151,13 @@ int simt_adapters_bwd(const AdaptersCall& c, char* ws, cudaStream_t st) {
     QB_TRY(launched());
   }
   if (c.dA) {
-    gradient_kernel<<<dim3(parts(k.r, 256), (unsigned)(k.P > 1024 ? 1024 : k.P), (unsigned)k.n), 256, 0, st>>>(c, s.x, k.P, s.du, k.r, 0, c.dA);
+    gradient_kernel<<<dim3(parts(k.r, 256), grid_rows(k.P), (unsigned)k.n), 256, 0, st>>>(c, s.x, k.P, s.du, k.r, 0, c.dA);
     QB_TRY(launched());
   }
   if (c.dB) {
     product_kernel<<<dim3(T, parts(k.r, 256)), 256, 0, st>>>(c, s.x, k.P, k.A, (int64_t)k.P * k.r, k.r, 1, k.r, 0, s.u);
     QB_TRY(launched());
-    gradient_kernel<<<dim3(parts(k.Q, 256), (unsigned)k.r, (unsigned)k.n), 256, 0, st>>>(c, s.u, k.r, s.dv, k.Q, 1, c.dB);
+    gradient_kernel<<<dim3(parts(k.Q, 256), grid_rows(k.r), (unsigned)k.n), 256, 0, st>>>(c, s.u, k.r, s.dv, k.Q, 1, c.dB);
     QB_TRY(launched());
   }
   return QBLORA_OK;

@@ -164,3 +164,19 @@ def test_infinities_where_gradients_are_cut(qb, where):
     X[::3, ::5], dY[::2, ::7] = float("inf"), -float("inf")
     dX, dA, dB = qb.adapters_bwd(bank, plan, X, dY, dX0.clone(), ws=ws)
     assert not bool(torch.isfinite(dA).any()) and qb.device_status(ws) == qb.OK
+
+
+def test_ranks_of_more_rows_than_a_grid_has(qb):
+    # the general path takes any rank: here above 65535
+    size, n = (12, 6, 2, 3, 65536 + 77), 2
+    bank = ra.make_bank(qb, n, *size, seed=3)
+    cu, di, T = ra.requests([3, 1, 2], [1, -1, 0])
+    plan, cu = qb.adapter_plan(cu, di, n, T), cu.tolist()
+    X, dY, Y0, dX0 = _randn(1, T, 12), _randn(2, T, 6), _randn(3, T, 6, dtype=torch.float32), _randn(4, T, 12, dtype=torch.float32)
+    want, bound = ra.ref_fwd(bank, cu, [1, -1, 0], X, Y0)
+    ra.check(qb.adapters_fwd(bank, plan, X, Y0.clone()), want, bound, 0, 12 + size[4], ("Y", torch.float32), Y0)
+    want, bound = ra.ref_bwd(bank, cu, [1, -1, 0], X, dY, dX0)
+    dX, dA, dB = qb.adapters_bwd(bank, plan, X, dY, dX0.clone())
+    ra.check(dX, want[0], bound[0], 0, 6 + size[4], ("dX", torch.float32), dX0)
+    ra.check(dA, want[1], bound[1], 0, 18 + T, ("dA", torch.float32))
+    ra.check(dB, want[2], bound[2], 0, 18 + T, ("dB", torch.float32))
