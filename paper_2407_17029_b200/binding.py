@@ -258,6 +258,9 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _raw_device = getattr(torch._C, "_cuda_getDevice", None)
 
 
+_current_device = _raw_device if _raw_device is not None else torch.cuda.current_device
+
+
 def _stream_ptr(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
@@ -688,14 +691,26 @@ class AdapterBank:
         if self.lambda_in < 1 or self.lambda_out < 1 or A.dim() != 3:
             raise ValueError("lambda_in, lambda_out >= 1; A: [n][d_in / lambda_in][rank]")
         n, P, r = A.shape
-        if P * self.lambda_in != self.d_in or tuple(B.shape) != (n, r, self.d_out // self.lambda_out) or B.shape[2] * self.lambda_out != self.d_out:
+        if P * self.lambda_in != self.d_in or B.shape != (n, r, self.d_out // self.lambda_out) or B.shape[2] * self.lambda_out != self.d_out:
             raise ValueError("A: [n][d_in / lambda_in][rank], B: [n][rank][d_out / lambda_out]")
-        if A.dtype is not torch.bfloat16 or B.dtype is not torch.bfloat16 or not (A.is_contiguous() and B.is_contiguous() and A.is_cuda and B.is_cuda):
+        at = A.get_device()
+        if A.dtype is not torch.bfloat16 or B.dtype is not torch.bfloat16 or not (A.is_contiguous() and B.is_contiguous()) or at < 0 or B.get_device() != at:
             raise ValueError("A, B: contiguous bf16 device tensors")
-        if s.dtype is not torch.float32 or s.numel() != n or not s.is_contiguous() or not s.is_cuda:
+        if s.dtype is not torch.float32 or s.numel() != n or not s.is_contiguous() or s.get_device() != at:
             raise ValueError("scaling: contiguous fp32 device tensor [n]")
         return _CAdapterBank(self.d_in, self.d_out, self.lambda_in, self.lambda_out, n, r, A.data_ptr(), B.data_ptr(), s.data_ptr(),
-                             None if k is None else _ints(k, n, "ranks"))
+                             None if k is None else _ints_at(k, n, "ranks", at))
+
+
+def _elsewhere(t: torch.Tensor):
+    """t.get_device() is not the current device, where a call's kernels run."""
+    raise ValueError(f"tensors on the current device (there are some on {t.device})")
+
+
+def _ints_at(t: torch.Tensor, n: int, name: str, at: int) -> int:
+    if t.dtype is not torch.int32 or t.numel() < n or not t.is_contiguous() or t.get_device() != at:
+        raise ValueError(f"{name}: contiguous int32 tensor of at least {n} entries on the other tensors' device")
+    return t.data_ptr()
 
 
 @dataclass
@@ -709,19 +724,21 @@ def adapter_plan(cu_rows: torch.Tensor, adapter_ids: torch.Tensor, n_adapters: i
                  stream=None) -> AdapterPlan:
     """qblora_adapter_plan: request b has the rows cu_rows[b] .. cu_rows[b + 1] - 1 and uses adapter_ids[b] (-1: none).
     `tokens`: rows of the step's buffers.  `outs`: preallocated (rows, start)."""
-    B = adapter_ids.numel()
+    B, at = adapter_ids.numel(), adapter_ids.get_device()
+    if at < 0 or at != _current_device():
+        _elsewhere(adapter_ids)
     rows, start = outs if outs is not None else (_empty(n, torch.int32, adapter_ids.device, stream) for n in (tokens, n_adapters + 1))
-    st = _lib.qblora_adapter_plan(_ints(cu_rows, B + 1, "cu_rows"), _ints(adapter_ids, B, "adapter_ids"), B, n_adapters, tokens,
-                                  _ints(rows, tokens, "rows"), _ints(start, n_adapters + 1, "start"), _stream_ptr(stream))
+    st = _lib.qblora_adapter_plan(_ints_at(cu_rows, B + 1, "cu_rows", at), _ints_at(adapter_ids, B, "adapter_ids", at), B, n_adapters, tokens,
+                                  _ints_at(rows, tokens, "rows", at), _ints_at(start, n_adapters + 1, "start", at), _stream_ptr(stream))
     if st != OK:
         _check(st, "qblora_adapter_plan")
     return AdapterPlan(rows, start)
 
 
-def _rows(t: torch.Tensor, tokens: int, width: int, name: str, dtypes=(torch.bfloat16,)) -> int:
-    """Checks a [tokens][width] tensor with contiguous rows; returns its row stride."""
-    if tuple(t.shape) != (tokens, width) or not t.is_cuda or t.dtype not in dtypes:
-        raise ValueError(f"{name}: [{tokens}][{width}] device tensor of {' or '.join(str(d) for d in dtypes)}")
+def _rows(t: torch.Tensor, tokens: int, width: int, name: str, at: int, dtypes=(torch.bfloat16,)) -> int:
+    """Checks a [tokens][width] tensor with contiguous rows on device `at`; returns its row stride."""
+    if t.shape != (tokens, width) or t.get_device() != at or t.dtype not in dtypes:
+        raise ValueError(f"{name}: [{tokens}][{width}] tensor on the bank's device, of {' or '.join(str(d) for d in dtypes)}")
     step, one = t.stride()
     if (one != 1 and width > 1) or (step < width and tokens > 1):
         raise ValueError(f"{name}: rows are contiguous and do not overlap")
@@ -737,9 +754,9 @@ def alloc_adapters_workspace(bank: AdapterBank, tokens: int, backward: bool = Fa
     return _empty(max(adapters_workspace_bytes(bank, max(tokens, 1), backward), 256), torch.uint8, bank.A.device, stream)
 
 
-def _workspace(ws: torch.Tensor) -> torch.Tensor:
-    if not ws.is_cuda or ws.dtype is not torch.uint8 or not ws.is_contiguous():
-        raise ValueError("ws: contiguous uint8 device tensor")
+def _workspace(ws: torch.Tensor, at: int) -> torch.Tensor:
+    if ws.get_device() != at or ws.dtype is not torch.uint8 or not ws.is_contiguous():
+        raise ValueError("ws: contiguous uint8 tensor on the bank's device")
     return ws
 
 
@@ -747,14 +764,16 @@ def adapters_fwd(bank: AdapterBank, plan: AdapterPlan, X: torch.Tensor, Y: torch
                  stream=None) -> torch.Tensor:
     """qblora_adapters_fwd: adds every planned row's adapter term to Y [tokens][d_out] (bf16 or fp32, what the shared
     projection of X has written) in place; returns Y.  X and Y have the `tokens` rows that the plan was made for."""
-    T = X.shape[0]
-    xs = _rows(X, T, bank.d_in, "X")
-    ys = _rows(Y, T, bank.d_out, "Y", (torch.bfloat16, torch.float32))
+    T, at = X.shape[0], bank.A.get_device()
+    if at < 0 or at != _current_device():
+        _elsewhere(bank.A)
+    xs = _rows(X, T, bank.d_in, "X", at)
+    ys = _rows(Y, T, bank.d_out, "Y", at, (torch.bfloat16, torch.float32))
     c = bank.c_struct()
     if T == 0:
         return Y
-    ws = alloc_adapters_workspace(bank, T, stream=stream) if ws is None else _workspace(ws)
-    st = _lib.qblora_adapters_fwd(ctypes.byref(c), _ints(plan.rows, T, "rows"), _ints(plan.start, c.n_adapters + 1, "start"), X.data_ptr(),
+    ws = alloc_adapters_workspace(bank, T, stream=stream) if ws is None else _workspace(ws, at)
+    st = _lib.qblora_adapters_fwd(ctypes.byref(c), _ints_at(plan.rows, T, "rows", at), _ints_at(plan.start, c.n_adapters + 1, "start", at), X.data_ptr(),
                                   xs, T, Y.data_ptr(), ys, _dt(Y.dtype), ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if st != OK:
         _check(st, "qblora_adapters_fwd")
@@ -767,27 +786,29 @@ def adapters_bwd(bank: AdapterBank, plan: AdapterPlan, X: Optional[torch.Tensor]
     """qblora_adapters_bwd: adds the adapters' part to dX [tokens][d_in] (bf16 or fp32, what the shared projection's backward
     pass has written; None: not wanted) in place and returns (dX, dA, dB), dA and dB fp32 of the shapes of A and B.
     `outs`: preallocated (dA, dB), entries None where not wanted."""
-    T = dY.shape[0]
-    ds = _rows(dY, T, bank.d_out, "dY")
+    T, at = dY.shape[0], bank.A.get_device()
+    if at < 0 or at != _current_device():
+        _elsewhere(bank.A)
+    ds = _rows(dY, T, bank.d_out, "dY", at)
     c = bank.c_struct()
     if outs is not None:
         dA, dB = outs
         for g, like, name in ((dA, bank.A, "dA"), (dB, bank.B, "dB")):
-            if g is not None and (g.shape != like.shape or g.dtype is not torch.float32 or not g.is_contiguous() or not g.is_cuda):
+            if g is not None and (g.shape != like.shape or g.dtype is not torch.float32 or not g.is_contiguous() or g.get_device() != at):
                 raise ValueError(f"{name}: contiguous fp32 device tensor of the shape of {name[1]}")
     else:
         dA = _empty(bank.A.shape, torch.float32, dY.device, stream) if need_da else None
         dB = _empty(bank.B.shape, torch.float32, dY.device, stream) if need_db else None
-    gs = _rows(dX, T, bank.d_in, "dX", (torch.bfloat16, torch.float32)) if dX is not None else 0
-    xs = _rows(X, T, bank.d_in, "X") if X is not None else 0
+    gs = _rows(dX, T, bank.d_in, "dX", at, (torch.bfloat16, torch.float32)) if dX is not None else 0
+    xs = _rows(X, T, bank.d_in, "X", at) if X is not None else 0
     if T == 0:
         for g in (dA, dB):
             if g is not None:
                 _zero(g, stream)
         return dX, dA, dB
-    ws = alloc_adapters_workspace(bank, T, backward=True, stream=stream) if ws is None else _workspace(ws)
+    ws = alloc_adapters_workspace(bank, T, backward=True, stream=stream) if ws is None else _workspace(ws, at)
     p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    st = _lib.qblora_adapters_bwd(ctypes.byref(c), _ints(plan.rows, T, "rows"), _ints(plan.start, c.n_adapters + 1, "start"), p(X), xs,
+    st = _lib.qblora_adapters_bwd(ctypes.byref(c), _ints_at(plan.rows, T, "rows", at), _ints_at(plan.start, c.n_adapters + 1, "start", at), p(X), xs,
                                   dY.data_ptr(), ds, T, p(dX), gs, _dt(dX.dtype) if dX is not None else BF16, p(dA), p(dB),
                                   ws.data_ptr(), ws.numel(), _stream_ptr(stream))
     if st != OK:
@@ -856,6 +877,9 @@ class AdamW:
         bits, decay, mult = each(state_bits), each(weight_decay), each(lr_mult)
         if len(bits) != n or len(decay) != n or len(mult) != n or any(b not in (8, 32) for b in bits):
             raise ValueError("state_bits (8 or 32), weight_decay, lr_mult: a value, or a list with one for each tensor")
+        self._index = params[0].get_device()
+        if self._index < 0 or self._index != _current_device():
+            _elsewhere(params[0])
         self.device = params[0].device
         self.params, self.grads, self.copies = list(params), list(grads), list(copies) if copies is not None else [None] * n
         new = lambda shape, dtype: _zeros(shape, dtype, self.device, stream)  # noqa: E731
@@ -904,6 +928,8 @@ class AdamW:
         self._prepare(stream)
 
     def _prepare(self, stream):
+        if self._index != _current_device():
+            _elsewhere(self.ws)
         _check(_lib.qblora_adamw_prepare(self._table, self._n, self.ws.data_ptr(), self.ws.numel(), ctypes.byref(self._blocks), self._order(stream)),
                "qblora_adamw_prepare")
 
@@ -921,6 +947,8 @@ class AdamW:
 
     def step(self, stream=None) -> Optional[torch.Tensor]:
         """One step on the gradients as they are when it runs; returns the norm's tensor, where it is formed."""
+        if self._index != _current_device():
+            _elsewhere(self.ws)
         st = _lib.qblora_adamw_step(ctypes.byref(self._cfg), self._n, self._blocks.value, self.ws.data_ptr(), self.ws.numel(), self._order(stream))
         if st != OK:
             _check(st, "qblora_adamw_step")

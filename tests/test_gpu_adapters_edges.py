@@ -180,3 +180,32 @@ def test_ranks_of_more_rows_than_a_grid_has(qb):
     ra.check(dX, want[0], bound[0], 0, 6 + size[4], ("dX", torch.float32), dX0)
     ra.check(dA, want[1], bound[1], 0, 18 + T, ("dA", torch.float32))
     ra.check(dB, want[2], bound[2], 0, 18 + T, ("dB", torch.float32))
+
+
+def test_tensors_of_another_device_than_the_current_one_are_refused(qb, monkeypatch):
+    # kernels run on the current device, where another one's addresses would be nobody's
+    bank = ra.make_bank(qb, 2, 256, 512, 4, 4, 32, seed=8)
+    cu, di, T = ra.requests([5, 20, 3], [0, 1, 0])
+    plan = qb.adapter_plan(cu, di, 2, T)
+    X, Y, p = _randn(1, T, 256), _randn(2, T, 512), torch.zeros(10, device=DEV)
+    opt = qb.AdamW([p], [p.clone()])
+    calls = [lambda: qb.adapter_plan(cu, di, 2, T), lambda: qb.adapters_fwd(bank, plan, X, Y), lambda: qb.adapters_bwd(bank, plan, X, Y),
+             lambda: qb.AdamW([p], [p.clone()]), lambda: opt.set_grads([p.clone()]), opt.step]
+    for call in calls:
+        call()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(qb, "_current_device", lambda: DEV_OTHER)
+    for call in calls:
+        with pytest.raises(ValueError):
+            call()
+    monkeypatch.undo()
+    # tensors that are not where the bank is
+    for bad in (lambda: qb.adapters_fwd(bank, plan, X.cpu(), Y), lambda: qb.adapters_fwd(bank, plan, X, Y, ws=torch.empty(1 << 20, dtype=torch.uint8)),
+                lambda: qb.adapters_fwd(bank, qb.AdapterPlan(plan.rows.cpu(), plan.start), X, Y), lambda: qb.adapter_plan(cu.cpu(), di, 2, T),
+                lambda: qb.adapter_plan(cu, di.cpu(), 2, T), lambda: qb.adapters_bwd(bank, plan, X.cpu(), Y),
+                lambda: qb.adapters_fwd(qb.AdapterBank(256, 512, 4, 4, bank.A, bank.B.cpu(), bank.scaling), plan, X, Y)):
+        with pytest.raises(ValueError):
+            bad()
+
+
+DEV_OTHER = 1                                                # an index; no such device is touched
