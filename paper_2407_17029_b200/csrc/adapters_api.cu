@@ -1,7 +1,6 @@
 // extern "C" entry points of the bank of adapters (include/qblora.h, last part): host-side argument checks and dispatch.
 // No device memory is allocated here.
 #include <algorithm>
-#include <cstdlib>
 
 #include "adapters.cuh"
 
@@ -28,11 +27,6 @@ bool rows_ok(const void* data, int64_t stride, int width, int dtype, RowsView* v
   if (reinterpret_cast<uintptr_t>(data) % (dtype == QBLORA_F32 ? 4 : 2)) return false;
   *v = {const_cast<void*>(data), stride, dtype};
   return true;
-}
-
-bool force_general() {
-  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
-  return e && e[0] == '1';
 }
 
 // Calls of no more rows go to adapters_rows.cu, by the type of Y; larger ones, whose adapters have many rows then, or are many, to

@@ -40,8 +40,8 @@ struct NrParams {
 
 // Bytes of shared memory: the warps' weights, pooled input (later the products), partial sums of u, u.
 struct NrLayout { int x, part, u, table, all; };
-__host__ __device__ inline NrLayout nr_layout(int np, int r, int n) {
-  NrLayout l;
+__host__ __device__ constexpr NrLayout nr_layout(int np, int r, int n) {
+  NrLayout l{};
   l.x = NR_WARPS * NR_STEP * (np == 3 ? NR_AHEAD<3> : NR_AHEAD<2>);
   const int x = np * NR_ROWS * (NR_CHUNK + 8) * 2;
   l.part = l.x + (x > NR_PART ? x : NR_PART);
@@ -50,6 +50,7 @@ __host__ __device__ inline NrLayout nr_layout(int np, int r, int n) {
   l.all = l.table + 2 * (n + 1) * 4 + 127;
   return l;
 }
+static_assert(nr_layout(3, NR_MAX_RANK, kMaxAdapters).all <= 230 * 1024 && nr_layout(2, NR_MAX_RANK, kMaxAdapters).all <= 230 * 1024, "shared memory");
 
 // A matrix [K][pitch] from rank (output) m on, of which the first M are there, and a warp's steps through its contraction: first, first +
 // stride, ... < last.  A lane copies 16 bytes, chunk lane % 8, of rows lane / 8 + 0, 4, 8, 12 of a step; chunk c of row k lies at place c ^ (k % 8)
@@ -491,7 +492,7 @@ int nr_launch(const NrParams& p, int64_t items, int cs, cudaStream_t st) {
 }  // namespace
 
 bool rows_adapters_supported(const AdaptersCall& c) {
-  return c.k.r <= NR_MAX_RANK && nr_layout(c.Y.dtype == QBLORA_F32 ? 3 : 2, c.k.r, c.k.n).all <= 230 * 1024;
+  return c.k.r <= NR_MAX_RANK;
 }
 
 int rows_adapters_fwd(const AdaptersCall& c, int* status, cudaStream_t st) {

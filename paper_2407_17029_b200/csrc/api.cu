@@ -1,7 +1,6 @@
 // extern "C" entry points declared in include/qblora.h: host-side argument checks, workspace
 // accounting and dispatch to the kernels.  No device memory is allocated here.
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 
 #include "common.cuh"
@@ -23,11 +22,6 @@ double normal_quantile(double p) {
     x = xn;
   }
   return x;
-}
-
-bool force_general() {
-  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
-  return e && e[0] == '1';
 }
 
 // code_bits: 0 or 4 = one code per nibble; 2 or 3 = dense storage (min-max format, d_in a multiple of 32)

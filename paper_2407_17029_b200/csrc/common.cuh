@@ -1,5 +1,6 @@
 // Shared declarations of the CUDA library behind include/qblora.h.
 #pragma once
+#include <cstdlib>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -44,6 +45,11 @@ __host__ __device__ __forceinline__ int scale_src(int op, int idx, int lam, int 
 constexpr size_t kStatusBytes = 256;  // first bytes of every workspace: device status word
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+// QBLORA_FORCE_GENERAL=1: every call by its general path (tests).
+inline bool force_general() {
+  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
+  return e && e[0] == '1';
+}
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // ---- instrumentation (instrument.cu) ------------------------------------------------------------

@@ -1,7 +1,6 @@
 // extern "C" entry points of the last part of include/qblora.h (rotary positions, paged cache plan, attention): host-side
 // argument checks and dispatch.  No device memory is allocated here.
 #include <cmath>
-#include <cstdlib>
 
 #include "serving.cuh"
 
@@ -48,11 +47,6 @@ bool rope_ok(const qblora_rope_cfg* c, int inverse, RopeView* v) {
 // with all of them there, 61 us with those above 16 rows here.  So a call whose requests all have 17 to 32 rows would be better off
 // with a border of 16; the host, which does not know the lengths, cannot tell it from one that straddles the border.
 constexpr int kNarrowRows = 32;
-
-bool force_general() {
-  const char* e = std::getenv("QBLORA_FORCE_GENERAL");
-  return e && e[0] == '1';
-}
 
 bool int_ptr_ok(const void* p) { return p && reinterpret_cast<uintptr_t>(p) % 4 == 0; }
 

@@ -1,7 +1,7 @@
 // Many adapters over one weight on the tensor cores (tcgen05): forward and backward of qblora_adapters_fwd / _bwd for rows of any
 // number, fast sizes (tc_adapters_supported).
 //
-// The adapter's products are thin: their operands are small beside X, Y and dX, which pass once.  So three kinds of kernels, all
+// The adapter's products are thin: their operands are small beside X, Y and dX, which pass once.  So four kinds of kernels, all
 // over the rows in the plan's order, where every adapter's rows are neighbours:
 //   pool    x' of every row (and the sums of dY's neighbours) as two or three bf16 parts: reads X at the memory's rate
 //   shrink  u = x' A (and du = dv B^T): parts in, parts out
@@ -17,8 +17,8 @@
 // Rows in the workspace: adapter a's begin at a multiple of 16 (pad[a]) and are filled up to one with zeros, so that the sums over
 // rows in grad run in whole steps of 16.  Which adapter has which tile is found by every CTA for itself from the plan's offsets.
 //
-// All loops are persistent: one CTA per SM takes the units in turn; warp 0 loads by TMA, warp 1 issues the MMAs, eight
-// warps empty one accumulator while the next is filled.
+// The loops of the last three are persistent: one CTA per SM takes the units in turn; warp 0 loads by TMA, warp 1 issues the MMAs, eight
+// warps (sixteen in spread) empty one accumulator while the next is filled.
 #include <algorithm>
 #include <atomic>
 
@@ -244,7 +244,6 @@ __global__ void __launch_bounds__(AG_POOL_THREADS) adapters_pool_kernel(const __
     const bool real = row >= 0 && row < p.c.T;
     ag_pool_row(s, real ? static_cast<const __nv_bfloat16*>(s.x.data) + row * s.x.stride : nullptr, at, lane);
   }
-  asm volatile("griddepcontrol.wait;" ::: "memory");     // no grid ends before the one in front of it
 }
 
 // ---- shrink -------------------------------------------------------------------------------------------------------------------
@@ -331,7 +330,7 @@ __device__ __forceinline__ void ag_issue(uint32_t d0, uint32_t d1, uint64_t a, u
   const uint64_t b1 = b + part, b2 = b1 + part;
   auto step = [&](uint64_t x, uint64_t y, uint32_t acc) {
     tc_mma(d0, a + x, b + y, idesc, acc);
-    if constexpr (NP > 1) tc_mma(d1, a + x, b1 + y, idesc, acc);
+    tc_mma(d1, a + x, b1 + y, idesc, acc);
     if constexpr (NP > 2) tc_mma(d1, a + x, b2 + y, idesc, 1u);
   };
   step(0, 0, fresh ^ 1u);
@@ -347,8 +346,7 @@ template <bool KMAJOR>
 __device__ __forceinline__ void ag_issue_parts(int np, uint32_t d0, uint32_t d1, uint64_t a, uint64_t b, uint64_t part, uint32_t idesc, int n,
                                                uint32_t fresh) {
   if (np == 2) ag_issue<2, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
-  else if (np == 3) ag_issue<3, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
-  else ag_issue<1, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
+  else ag_issue<3, KMAJOR>(d0, d1, a, b, part, idesc, n, fresh);
 }
 // v += 32 columns of tensor memory
 __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
@@ -615,7 +613,7 @@ constexpr int AS_SLAB = 16384, AS_RING = 3;
 struct AgSpread {
   AdaptersCall c;
   uint32_t rows_there;                  // of the workspace
-  int tn, np, kb;                       // rows of a tile (at most 64); parts of u; 64-wide blocks of the slots' rank
+  int tn, np, kb;                       // rows of a tile (at most 64); parts of u, 2 or 3; 64-wide blocks of the slots' rank
   int slabs;
   int segment;                          // as in AgShrink
   int m_tiles, M, w_kmajor, scaled;
@@ -972,7 +970,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
           if (part * 16 < t.n16) {
             const uint32_t d = tmem_base + ((uint32_t)(q * 32) << 16) + b * 128 + part * 16;
             ag_gather16(d, x);
-            if (p.np > 1) ag_gather16(d + 64, x);
+            ag_gather16(d + 64, x);
           }
           tc_fence_before();
           __syncwarp();
@@ -1397,8 +1395,7 @@ int ag_launch(void (*kernel)(Maps, Params), std::atomic<bool>* ready, const Maps
   return QBLORA_OK;
 }
 
-// beside: the kernel in front on the stream is adapters_rows.cu's, of other rows: this one need not wait for its end before it
-// begins, only before it ends itself.
+// The first of a call, behind all that is in front of it on the stream.
 int ag_launch_pool(const AgPoolParams& p, int64_t rows, cudaStream_t st) {
   int sms = 0;
   const int rc = ag_sms(&sms);
