@@ -560,7 +560,8 @@ typedef struct {
  *   m = beta1 m + (1 - beta1) g~;   v = beta2 v + (1 - beta2) g~^2;
  *   p = p - lr lr_mult (m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps) + weight_decay p);   copy = bf16(p).
  * Everything is formed in fp32 from the stored states; the update uses m and v before they are stored again.  m and v take one
- * rounding per operation in the order written (g~ * g~ before its factor), so states in 8 bits are unique.
+ * rounding per operation in the order written (g~ * g~ before its factor), so states in 8 bits are unique.  The update's own root (of states
+ * in 32 bits) and reciprocal are approximations, within 2^-22 of themselves.
  *
  * States in 8 bits: m and r = sqrt(v) are held as e4m3 codes (sign, 4 exponent bits with bias 7, 3 mantissa bits; the largest
  * number is 448) times one fp32 scale per block of 256 consecutive elements, scale = (largest |m| of the block) / 448.  A value
@@ -570,11 +571,13 @@ typedef struct {
  * x ^= x >> 15, x *= 0x5D8E3B97, x ^= x >> 16 (32 bits), h = mix(e * 0x9E3779B1 + mix(mix(seed) + t)); the low 16 bits of h
  * belong to m, the high ones to r: the neighbour further from zero is taken if the fraction of the way to it plus bits / 65536 is
  * at least 1.  Equal inputs give equal bits.  States that are not finite are held as NaN and do not count for the scale; a block
- * whose largest value is below 2^-118 is held as zeros.
+ * whose largest value is below 2^-118 is held as zeros.  The smallest code is 2^-17.8 of the largest: an element whose averages lie that far
+ * below its block's largest is held as zero or as that code, by chance for each of m and r, and its update is as uneven.
  *
  * The norm is summed over the gradients of all tensors in the call, in fp64 and in a fixed order.  Where it is formed and is not finite, the step is left out: nothing but *norm is written.
  *
- * qblora_adamw_prepare lays the tensors' table into ws and writes to *blocks the number that the step wants (an opaque one); ws then belongs to
+ * qblora_adamw_prepare lays the tensors' table into ws (a launch for every 32 tensors, 0.5 ms of the host's time for 560: keep the gradients' tensors
+ * rather than prepare anew for each step's) and writes to *blocks the number that the step wants (an opaque one); ws then belongs to
  * these tensors (their addresses, not their values) until it is prepared again.  At most 65536 tensors, 2^31 - 1 blocks.
  * No tensor may overlap another.  qblora_adamw_step may be captured in a graph: lr, steps and the gradients' values are
  * read when it runs.  The calls over one ws, qblora_adamw_prepare among them, run one after the other: on one stream, or with the

@@ -934,7 +934,8 @@ class AdamW:
                "qblora_adamw_prepare")
 
     def set_grads(self, grads, stream=None) -> None:
-        """Other gradient tensors from the next step on (a new table; not while a captured step of this object may run)."""
+        """Other gradient tensors from the next step on (a new table: about 0.5 ms of the host's time for 560 tensors, so a training loop had better
+        keep its gradients' tensors; not while a captured step of this object may run)."""
         if len(grads) != self._n:
             raise ValueError("grads: one tensor for each parameter")
         for k, g in enumerate(grads):

@@ -2,9 +2,11 @@
 // (qblora_adamw_prepare, qblora_adamw_step; the formulas stand in include/qblora.h).
 //
 // What bounds it: memory with states in 32 bits, 30 bytes an element (p, m, v in and out, g in, the bf16 copy out): 125 M elements in 607
-// us, 6.2 TB/s.  With states in 8 bits, 16 to 18 bytes an element, the instructions (640 for a warp's 256 elements, 2.3 a cycle): 480 us,
-// and 68 for the norm's pass over bf16 gradients; more bytes on their way, by more CTAs an SM or asynchronous copies, changed nothing (488
-// to 653).  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane: a scale's block lies
+// us, 6.2 TB/s.  With states in 8 bits, 16 to 18 bytes an element, the instructions (640 for a warp's 256 elements, 2.0 to 2.3 a cycle) and,
+// behind them, the wait for loads (3.9 of the stalls an issue): 480 us, and 68 for the norm's pass over bf16 gradients (3.7 TB/s); more bytes on
+// their way, by more CTAs an SM or asynchronous copies, changed nothing (488 to 653).  At the 80 registers that three CTAs an SM leave, two
+// blocks in flight beside a copy of the tensor's table entry in every lane do not fit: adamw_kernel<8> spills 100 bytes of stores and 148 of
+// loads a thread, adamw_kernel<0> 112 and 260, adamw_kernel<32> 8 and 12.  The unit of work is a block of 256 consecutive elements of one tensor, one warp's 8 elements per lane: a scale's block lies
 // within a warp, so its maximum is five shuffles and no element is read twice.  The tensors are a table in the workspace; a warp takes
 // runs of neighbouring blocks and searches the first blocks for their tensor where the last one's does not fit.  Lane l holds elements 4 l
 // .. 4 l + 3 and 128 + 4 l .. of the block, so every load and store of a warp is one contiguous run.

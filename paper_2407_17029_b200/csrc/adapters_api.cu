@@ -30,9 +30,12 @@ bool rows_ok(const void* data, int64_t stride, int width, int dtype, RowsView* v
 }
 
 // Calls of no more rows go to adapters_rows.cu, by the type of Y; larger ones, whose adapters have many rows then, or are many, to
-// tc_adapters.cu.  (Both in us, graph replays.  bf16: 4096 -> 4096, rank 64, 64 adapters of 8 rows 13 and 29, 16 of 32 13 and 22, of 64 20 and 25;
-// 4096 -> 11008, rank 256, 64 of 8 37 and 54, 16 of 32 30 and 32, of 64 43 and 35.  fp32: 64 of 4 13 and 31, 16 of 32 20 and 24, of 64
-// 38 and 29; 41 and 59, 49 and 36, 89 and 48.)
+// tc_adapters.cu.  An item of eight rows brings its adapter's weights for itself, from L2 where other items have them too, and yet few adapters
+// are not the other path's earlier than many.  (Both in us, graph replays, one adapter / 16 / 64 of as many rows in all.  bf16, 512 rows:
+// 4096 -> 11008, lambda 4, rank 256 28.8 and 27.8 / 29.6 and 32.1 / 37.2 and 53.9; 4096 -> 4096, rank 64 13.0 and 21.7 / 13.1 and 22.4 / 13.1
+// and 29.0; 11008 -> 11008, lambda 1, rank 256 80 and 87 / 82 and 108 / 125 and 182.  16 adapters of 64 rows: 43 and 35, rank 64 20 and 25.
+// fp32, 256 rows: 28.8 and 29.3 / 30.8 and 34.0 / 40.9 and 58.9; 12.5 and 23.4 / 13.1 and 23.9 / 13.3 and 31.0; 77 and 94 / 79 and 112 / 143
+// and 194.  512 rows: 48 and 34 / 49 and 36 / 55 and 60; 18 and 24 / 20 and 24 / 21 and 31; 141 and 105 / 142 and 115 / 165 and 195.)
 int few_rows(int y_dtype) { return y_dtype == QBLORA_F32 ? 256 : 512; }
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
