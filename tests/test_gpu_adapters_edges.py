@@ -209,3 +209,18 @@ def test_tensors_of_another_device_than_the_current_one_are_refused(qb, monkeypa
 
 
 DEV_OTHER = 1                                                # an index; no such device is touched
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("rows", [255, 256, 257, 511, 512, 513])
+def test_one_adapter_on_either_side_of_the_border(qb, rows, dtype):
+    # all rows of the step belong to one adapter: both sides of the number of rows that changes the forward path
+    size = (1024, 1408, 4, 8, 128)
+    bank = ra.make_bank(qb, 3, *size, seed=rows)
+    cu, di, T = ra.requests([rows], [1])
+    X, Y0 = _randn(1, T, size[0]), _randn(2, T, size[1], dtype=dtype)
+    plan = qb.adapter_plan(cu, di, 3, T)
+    Y = qb.adapters_fwd(bank, plan, X, Y0.clone())
+    want, bound = ra.ref_fwd(bank, cu.tolist(), [1], X, Y0)
+    ra.check(Y, want, bound, 2, size[0] + size[4], ("Y", dtype), Y0)
+    assert torch.equal(Y, qb.adapters_fwd(bank, plan, X, Y0.clone()))
