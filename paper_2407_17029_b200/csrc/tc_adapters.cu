@@ -360,13 +360,18 @@ __device__ __forceinline__ void ag_gather(uint32_t taddr, float* v) {
 // the number is), but the smaller ones make NaN of it: the rest of an infinity is inf - inf, and a part that is zero or of the other sign meets
 // an infinite weight.  So a result that is NaN is formed once more, of the first parts alone, on the CUDA cores and out of line.  (A look at each
 // number as it leaves tensor memory: 2 to 3 us of each call of 70, for its instructions' way into the SM more than for their number.)
+// x: n columns are there, a multiple of 16; what lies behind them is of other tiles
 template <int N>
-__device__ __forceinline__ bool ag_any_nan(const float* x) {
+__device__ __forceinline__ bool ag_any_nan(const float* x, int n) {
   float sum[2] = {0.f, 0.f};                              // two numbers by one instruction
 #pragma unroll
-  for (int j = 0; j < N; j += 2)
-    asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
-        : "+f"(sum[0]), "+f"(sum[1]) : "f"(x[j]), "f"(x[j + 1]));
+  for (int c = 0; c < N; c += 16) {
+    if (c >= n) break;
+#pragma unroll
+    for (int j = c; j < c + 16; j += 2)
+      asm("{\n .reg .b64 x, y;\n mov.b64 x, {%0, %1};\n mov.b64 y, {%2, %3};\n add.rn.f32x2 x, x, y;\n mov.b64 {%0, %1}, x;\n}"
+          : "+f"(sum[0]), "+f"(sum[1]) : "f"(x[j]), "f"(x[j + 1]));
+  }
   return isnan(sum[0] + sum[1]);
 }
 // sum[e] = sum over i of a[i a_step] b[i b_step + e b_next]; nothing changes a sum that is NaN already
@@ -587,7 +592,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_shrink_kernel(const __
         const float x[2] = {!there ? 0.f : (lane & 1) ? got : v0, !there ? 0.f : (lane & 1) ? v1 : got};
         if (m < sd.out.width) ag_store_parts<2>(sd.out, (int64_t)(t.at + col) * sd.out.ld + m, x);      // (the rank is a multiple of 8)
       }
-      if (__any_sync(0xffffffffu, ag_any_nan<64>(v))) {
+      if (__any_sync(0xffffffffu, ag_any_nan<64>(v, t.n16 - half * 64))) {
         __syncwarp();
         ag_mend_shrink(p, side, t.a, t.at + half * 64, min(64, t.rows - half * 64), m0 + q * 32 + lane);
       }
@@ -980,7 +985,7 @@ __global__ void __launch_bounds__(AS_THREADS, 1) adapters_spread_kernel(const __
         if (part * 16 < t.n16) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[(part * 16 + j) * 128 + q * 32 + lane] = x[j] * scale;
-          if (ag_any_nan<16>(x))
+          if (ag_any_nan<16>(x, 16))
             as_mend(p, v + part * 16 * 128 + q * 32 + lane, t.a, t.at + part * 16, min(16, t.rows - part * 16), m * 128 + q * 32 + lane, scale);
         }
         asm volatile("bar.sync 1, 512;" ::: "memory");
@@ -1296,7 +1301,7 @@ __global__ void __launch_bounds__(AG_THREADS, 1) adapters_grad_kernel(const __gr
           for (int e = 0; e < 4; ++e) x[e] = (t.side ? m : t.n0 + half * 64 + j + e) < t.rank ? v[j + e] * scale : 0.f;
           *reinterpret_cast<float4*>(out + j) = make_float4(x[0], x[1], x[2], x[3]);
         }
-        if (ag_any_nan<64>(v))
+        if (ag_any_nan<64>(v, t.n16 - half * 64))
           ar_mend(side, out, m, t.n0 + half * 64, min(64, side.N - t.n0 - half * 64), (uint32_t)t.first, t.all * 16, scale);
       }
     }
